@@ -507,6 +507,106 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
                       const void *ent, int64_t n, int32_t F, int32_t max_bins, double eta, float *margin,
                       void *workspace, size_t workspace_bytes);
 
+/* ---- rows with a history: attention over ragged sequences ---------------- */
+
+/*
+ * A table's row may come with a history of events beside its columns.  These calls are the attention that reads
+ * such histories, its backward pass, and the clipping of the gradients that come of it.  A sequence is one
+ * history; sequences lie one after the other, as rows of packed matrices, and row pointers say where each begins.
+ *
+ * For query i of nq and key j of nk of one sequence, and head h of key head h / (heads / kv_heads):
+ *     t      = j - (i + nk - nq)       distance: 0 the query's own place (the last query is at the last key)
+ *     S      = scale * q_i . k_j + bias[bucket(t)][h],  bucket(t) = #{cuts <= t} as symbols are binned above;
+ *              causal: keys with t > 0 do not count
+ *     out_i  = sum_j softmax_j(S) v_j;   a query without any key: zeros
+ * Scores, softmax statistics and all sums are held in 32 bits; probabilities are rounded to the inputs' type as
+ * operands of the products with v and out's gradient, scores' gradients as operands of those with q and k.
+ * A non-finite element of a sequence makes that sequence's results of its key head non-finite in part; no
+ * sequence depends on elements outside its own rows.
+ *
+ * Rows of q, k and v may be any distance apart (parts of one fused projection, slots of a store): strides are in
+ * elements, multiples of 8, as head_dim; data is 16-byte aligned; a head's elements lie side by side.
+ */
+#define GBT_F32 0
+#define GBT_BF16 1
+#define GBT_F16 2
+#define GBT_MAX_HEAD_DIM 128
+#define GBT_MAX_BUCKETS 256
+
+typedef struct gbt_heads {       /* [dev] rows x heads x head_dim elements */
+    void *data;
+    int64_t row_stride, head_stride;
+} gbt_heads;
+
+typedef struct gbt_attention_params {
+    int32_t dtype;               /* GBT_BF16 or GBT_F16 (others: GBT_EUNSUPPORTED), of q, k, v, out and their gradients */
+    int32_t heads, kv_heads;     /* heads a multiple of kv_heads */
+    int32_t head_dim;            /* 8..128, a multiple of 8 (others: GBT_EUNSUPPORTED) */
+    int32_t n_seq;
+    int32_t max_q, max_k;        /* no sequence is longer (rows beyond are not used) */
+    int32_t causal;
+    int32_t n_buckets;           /* 0 (no bias) .. 256 */
+    float scale;
+    int64_t q_rows, k_rows;      /* rows of the q and k tensors; rows of a sequence that lie outside do not exist */
+    const int64_t *q_ptr;        /* [dev] int64[n_seq + 1]; NULL: sequence s has rows s * max_q .. (s + 1) * max_q */
+    const int64_t *k_ptr;        /* [dev] int64[n_seq + 1]; NULL: the same with max_k */
+    const int32_t *k_len;        /* [dev] int32[n_seq], or NULL: only the first k_len[s] rows of the slot
+                                    k_ptr[s] .. k_ptr[s + 1] are used (a store with room to grow) */
+    const float *bias;           /* [dev] float[n_buckets][heads] */
+    const int32_t *cuts;         /* [host] int32[n_buckets - 1], strictly increasing */
+} gbt_attention_params;
+
+/*
+ * out [dev] as q.  Rows of no sequence are not written.  For gbt_attention_backward:
+ *   lse_out  [dev] float[heads][q_rows], or NULL: log sum_j exp S, -inf for a query without keys
+ *   rest_out [dev] [q_rows][heads][head_dim] of dtype, 16-byte aligned, or NULL: what rounding took from out
+ * Asynchronous.  workspace [dev]: gbt_attention_workspace_bytes (0: none needed, NULL allowed).  The workspace
+ * queries return 0 for parameters that the calls refuse.
+ */
+GBT_API size_t gbt_attention_workspace_bytes(const gbt_attention_params *params);
+GBT_API int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *params, const gbt_heads *q, const gbt_heads *k,
+                              const gbt_heads *v, const gbt_heads *out, float *lse_out, void *rest_out, void *workspace,
+                              size_t workspace_bytes);
+
+/*
+ * Gradients of q, k, v (dk and dv summed over the heads that share them) and of the bias table, from dout and
+ * what gbt_attention returned for the same parameters (rest may be NULL; dq is then less exact).
+ *   dbias_out [dev] float[n_buckets][heads], overwritten (ignored where n_buckets = 0)
+ * Probabilities are recomputed; sums are taken in a fixed order, so results are the same on every run.  Rows of
+ * no sequence, and key rows beyond k_len, are not written.  Asynchronous.
+ */
+GBT_API size_t gbt_attention_backward_workspace_bytes(const gbt_attention_params *params);
+GBT_API int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_params *params, const gbt_heads *dout,
+                                       const gbt_heads *q, const gbt_heads *k, const gbt_heads *v, const gbt_heads *out,
+                                       const float *lse, const void *rest, const gbt_heads *dq, const gbt_heads *dk,
+                                       const gbt_heads *dv, float *dbias_out, void *workspace, size_t workspace_bytes);
+
+/* ---- clipping by the global norm ----------------------------------------- */
+
+typedef struct gbt_gradient {    /* one tensor of n elements, any alignment of its type */
+    const void *src;             /* [dev] */
+    void *dst;                   /* [dev] may be src; must not overlap otherwise */
+    int64_t n;
+    int32_t dtype;               /* GBT_F32, GBT_BF16, GBT_F16 */
+} gbt_gradient;
+
+/*
+ * Lays a list of tensors out for gbt_clip_gradients, once for as long as their addresses and sizes hold:
+ * list_out [dev, 16-byte aligned] of gbt_gradient_list_bytes bytes, *pieces_out [host] its length.  Lists whose
+ * table exceeds 4 MB (some 170,000 tensors) are refused with GBT_EUNSUPPORTED (and 0 bytes).  Asynchronous.
+ */
+GBT_API size_t gbt_gradient_list_bytes(const gbt_gradient *gradients, int64_t n_gradients);
+GBT_API int32_t gbt_gradient_list(gbt_ctx *ctx, const gbt_gradient *gradients, int64_t n_gradients, void *list_out,
+                                  size_t list_bytes, int32_t *pieces_out);
+
+/*
+ * *norm_out [dev] = sqrt(sum of all elements' squares), summed in 64 bits in a fixed order; every
+ * dst = src * min(1, max_norm / (norm + 1e-6)), rounded once.  A norm that is not finite leaves the values as
+ * they are (dst = src).  max_norm >= 0.  workspace [dev] >= 16384 bytes.  Asynchronous.
+ */
+GBT_API int32_t gbt_clip_gradients(gbt_ctx *ctx, const void *list, int32_t pieces, double max_norm, float *norm_out,
+                                   void *workspace, size_t workspace_bytes);
+
 /* ---- measurement -------------------------------------------------------- */
 
 /* Kernel classes timed by the optional profiler. */

@@ -7,6 +7,7 @@ MI355X, loading or ``Context()`` raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -35,6 +36,8 @@ SYMBOLS = [
     "gbt_sparse_entry_bytes", "gbt_sparse_capacity", "gbt_compress_sparse_workspace_bytes", "gbt_compress_sparse_count", "gbt_compress_sparse",
     "gbt_build_hist_sparse", "gbt_grow_tree_sparse_workspace_bytes", "gbt_grow_tree_sparse", "gbt_predict_sparse",
     "gbt_grow_tree_sparse_lossguide_workspace_bytes", "gbt_grow_tree_sparse_lossguide",
+    "gbt_attention_workspace_bytes", "gbt_attention", "gbt_attention_backward_workspace_bytes", "gbt_attention_backward",
+    "gbt_gradient_list_bytes", "gbt_gradient_list", "gbt_clip_gradients",
 ]
 
 PROF_LEVELS = 18   # GBT_PROF_LEVELS
@@ -73,6 +76,24 @@ class Tree(C.Structure):
                 ("weight", C.c_void_p), ("gain", C.c_void_p), ("sumG", C.c_void_p),
                 ("sumH", C.c_void_p), ("n_rows", C.c_void_p)]
 
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class AttentionParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_seq", C.c_int32), ("max_q", C.c_int32), ("max_k", C.c_int32), ("causal", C.c_int32),
+                ("n_buckets", C.c_int32), ("scale", C.c_float), ("q_rows", C.c_int64), ("k_rows", C.c_int64),
+                ("q_ptr", C.c_void_p), ("k_ptr", C.c_void_p), ("k_len", C.c_void_p), ("bias", C.c_void_p),
+                ("cuts", C.c_void_p)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # GBT_F32, GBT_BF16, GBT_F16
 
 _TREE_FIELDS = [("feature", np.int32), ("bin", np.int32), ("default_left", np.int32), ("left", np.int32),
                 ("right", np.int32), ("threshold", np.float32), ("weight", np.float64),
@@ -142,6 +163,16 @@ def load():
     L.gbt_grow_tree_sparse_lossguide_workspace_bytes.restype = sz
     L.gbt_grow_tree_sparse_lossguide.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz]
     L.gbt_predict_sparse.argtypes = [vp, vp, i32, vp, vp, i64, i32, i32, f64, vp, vp, sz]
+    L.gbt_attention_workspace_bytes.argtypes = [vp]
+    L.gbt_attention_workspace_bytes.restype = sz
+    L.gbt_attention.argtypes = [vp] * 9 + [sz]
+    L.gbt_attention_backward_workspace_bytes.argtypes = [vp]
+    L.gbt_attention_backward_workspace_bytes.restype = sz
+    L.gbt_attention_backward.argtypes = [vp] * 14 + [sz]
+    L.gbt_gradient_list_bytes.argtypes = [vp, i64]
+    L.gbt_gradient_list_bytes.restype = sz
+    L.gbt_gradient_list.argtypes = [vp, vp, i64, vp, sz, vp]
+    L.gbt_clip_gradients.argtypes = [vp, vp, i32, f64, vp, vp, sz]
     L.gbt_profile_enable.argtypes = [vp, i32]
     L.gbt_profile_read.argtypes = [vp, vp]
     L.gbt_measure_stream_read.argtypes = [vp, vp, sz, i32, vp, vp, sz]
@@ -227,6 +258,36 @@ def _need(t, dtype, name):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
     return t
+
+
+def distance_cuts(n_buckets: int, far: int, causal: bool = True) -> list:
+    """Cuts between n_buckets buckets of distance (0 = the query's own place, negative = the past): about half of them
+    one distance each, the others growing geometrically up to `far`; in both directions alike unless causal."""
+    n = n_buckets - 1
+    back = n if causal else (n + 1) // 2
+    near = max(1, back // 2)
+    steps = []
+    for i in range(back):
+        at = i if i < near else near * (far / near) ** ((i - near + 1) / (back - near))
+        steps.append(max(int(round(at)), steps[-1] + 1) if steps else 0)
+    return [-s for s in reversed(steps)] + [s + 1 for s in steps[:n - back]]
+
+
+def _heads(t, name, dtype, heads=None):
+    """gbt_heads of a tensor [rows][heads][head_dim] whose last axis is contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 3 and (t.stride(2) == 1 or t.numel() == 0)):
+        raise TypeError(f"{name}: expected a CUDA tensor [rows][heads][head_dim] of {dtype} with a contiguous last axis")
+    if heads is not None and t.shape[1:] != heads:
+        raise TypeError(f"{name}: expected [rows][{heads[0]}][{heads[1]}], not {tuple(t.shape)}")
+    rows, h, d = t.shape     # an axis of one element has no stride to speak of
+    return Heads(t.data_ptr(), t.stride(0) if rows > 1 else h * d, t.stride(1) if h > 1 else d)
+
+
+class GradientList:
+    """Tensors laid out for Context.clip_gradients; holds on to them."""
+
+    def __init__(self, tensors, outs, table, pieces):
+        self.tensors, self.outs, self.table, self.pieces = tensors, outs, table, pieces
 
 
 class Context:
@@ -585,3 +646,139 @@ class Context:
         self._check(self.lib.gbt_predict(self.h, arr, len(trees), _ptr(packed), bits, missing_sym, _ptr(X), n, F,
                                          eta, _ptr(margin), _ptr(ws), ws.numel()))
         return margin
+
+    # -- rows with a history ---------------------------------------------------
+    def _on_stream(self, *tensors):
+        """Outputs are allocated on the context's stream.  Where that is not torch's current one, the inputs' memory is
+        kept from reuse until this call's work is done (waiting for their contents is the caller's, as for every call)."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return contextlib.nullcontext()
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+        return torch.cuda.stream(self.stream)
+
+    def _attention_params(self, q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts):
+        rows, heads, dim = q.shape
+        n_seq = 1
+        for nm, t, dt in (("q_ptr", q_ptr, torch.int64), ("k_ptr", k_ptr, torch.int64), ("k_len", k_len, torch.int32)):
+            if t is not None:
+                _need(t, dt, nm)
+                n_seq = t.numel() - (nm != "k_len")
+        for nm, t in (("q_ptr", q_ptr), ("k_ptr", k_ptr), ("k_len", k_len)):
+            if t is not None and t.numel() - (nm != "k_len") != n_seq:
+                raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
+        for nm, ptr, t, longest in (("q", q_ptr, q, max_q), ("k", k_ptr, k, max_k)):
+            if ptr is None and (t.shape[0] % max(1, n_seq) or longest not in (None, t.shape[0] // max(1, n_seq))):
+                raise TypeError(f"{nm}: without {nm}_ptr all of {n_seq} sequences have the same length")
+        if max_q is None:
+            max_q = rows if q_ptr is not None else rows // max(1, n_seq)
+        if max_k is None:
+            max_k = k.shape[0] if k_ptr is not None else k.shape[0] // max(1, n_seq)
+        n_buckets, table, edges = 0, None, None
+        if bias is not None:
+            _need(bias, torch.float32, "bias")
+            if bias.dim() != 2 or bias.shape[1] != heads or bias.shape[0] < 1:
+                raise TypeError(f"bias: expected [n_buckets][{heads}], not {tuple(bias.shape)}")
+            n_buckets, table = bias.shape[0], bias.data_ptr()
+            if cuts is None or len(cuts) != n_buckets - 1:
+                raise TypeError(f"cuts: expected {n_buckets - 1} of them")
+            edges = (C.c_int32 * max(1, n_buckets - 1))(*(cuts.tolist() if hasattr(cuts, "tolist") else cuts))
+        p = AttentionParams(DTYPES.get(q.dtype, -1), heads, k.shape[1], dim, n_seq, max_q, max_k, int(causal), n_buckets,
+                            dim ** -0.5 if scale is None else scale, rows, k.shape[0], None if q_ptr is None else q_ptr.data_ptr(),
+                            None if k_ptr is None else k_ptr.data_ptr(), None if k_len is None else k_len.data_ptr(), table,
+                            None if edges is None else C.addressof(edges))
+        return p, edges      # edges: alive as long as the parameters
+
+    def attention(self, q, k, v, *, q_ptr=None, k_ptr=None, k_len=None, max_q=None, max_k=None, causal=False, scale=None,
+                  bias=None, cuts=None, save=False, out=None):
+        """Attention of q [rows][heads][head_dim] over k, v [rows][kv_heads][head_dim], sequence by sequence.
+
+        q_ptr, k_ptr  int64[n_seq + 1] on the device: where each sequence's rows begin (None: sequences of one length)
+        k_len         int32[n_seq] on the device: how many rows of each slot of k and v are in use (None: all)
+        max_q, max_k  the longest sequence (None: taken to be all rows, which costs idle workgroups)
+        bias, cuts    float32 [n_buckets][heads] and the ascending cuts between buckets of distance, on the host
+        save          also return what attention_backward needs: (out, saved)
+        """
+        if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
+        p, keep = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
+        hq = _heads(q, "q", q.dtype)
+        hk, hv = _heads(k, "k", q.dtype, (k.shape[1], q.shape[2])), _heads(v, "v", q.dtype, (k.shape[1], q.shape[2]))
+        if v.shape[0] != k.shape[0]:
+            raise TypeError("v: expected as many rows as k")
+        if out is not None and out.shape != q.shape:
+            raise TypeError(f"out: expected {tuple(q.shape)}")
+        ws_bytes = self.lib.gbt_attention_workspace_bytes(C.byref(p))
+        with self._on_stream(q, k, v, q_ptr, k_ptr, k_len, bias, out):
+            if out is None:
+                out = self.empty(q.shape, q.dtype)
+            lse = self.empty((q.shape[1], q.shape[0]), torch.float32) if save else None
+            rest = self.empty(q.shape, q.dtype) if save else None
+            ws = self.workspace("attention", ws_bytes) if ws_bytes else None
+        ho = _heads(out, "out", q.dtype)
+        self._check(self.lib.gbt_attention(self.h, C.byref(p), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), _ptr(lse), _ptr(rest),
+                                           _ptr(ws), 0 if ws is None else ws.numel()))
+        return (out, (lse, rest)) if save else out
+
+    def attention_backward(self, dout, q, k, v, out, saved, *, q_ptr=None, k_ptr=None, k_len=None, max_q=None, max_k=None, causal=False,
+                           scale=None, bias=None, cuts=None):
+        """(dq, dk, dv, dbias) of attention(..., save=True) with the same arguments; dbias is None without a bias.  Rows of k and v
+        that no sequence uses get zeros."""
+        if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
+        p, keep = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
+        lse, rest = saved
+        _need(lse, torch.float32, "saved[0]")
+        if rest is not None:
+            _need(rest, q.dtype, "saved[1]")
+        if lse.shape != (q.shape[1], q.shape[0]) or (rest is not None and rest.shape != q.shape):
+            raise TypeError(f"saved: not of a call with q of {tuple(q.shape)}")
+        like_q, like_k = tuple(q.shape[1:]), (k.shape[1], q.shape[2])
+        for nm, t, n in (("dout", dout, q.shape[0]), ("out", out, q.shape[0]), ("v", v, k.shape[0])):
+            if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[0] != n:
+                raise TypeError(f"{nm}: expected {n} rows")
+        views = [_heads(dout, "dout", q.dtype, like_q), _heads(q, "q", q.dtype), _heads(k, "k", q.dtype, like_k), _heads(v, "v", q.dtype, like_k),
+                 _heads(out, "out", q.dtype, like_q)]
+        ws_bytes = self.lib.gbt_attention_backward_workspace_bytes(C.byref(p))
+        with self._on_stream(dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias):
+            dq = self.empty(q.shape, q.dtype)
+            rows = torch.empty if k_len is None else torch.zeros
+            dk, dv = (rows(k.shape, dtype=q.dtype, device=self.device) for _ in range(2))
+            dbias = None if bias is None else self.empty(bias.shape, torch.float32)
+            ws = self.workspace("attention", ws_bytes)
+        grads = [_heads(dq, "dq", q.dtype), _heads(dk, "dk", q.dtype), _heads(dv, "dv", q.dtype)]
+        self._check(self.lib.gbt_attention_backward(self.h, C.byref(p), *[C.byref(x) for x in views], _ptr(lse), _ptr(rest),
+                                                    *[C.byref(x) for x in grads], _ptr(dbias), _ptr(ws), ws.numel()))
+        return dq, dk, dv, dbias
+
+    def gradient_list(self, tensors, outs=None) -> GradientList:
+        """Lays gradient tensors out for clip_gradients; outs receive the results (None: the tensors themselves).  Good for as long
+        as the tensors stay where they are; the list holds on to them."""
+        tensors = list(tensors)
+        outs = tensors if outs is None else list(outs)
+        if len(outs) != len(tensors):
+            raise TypeError("outs: expected one for each tensor")
+        arr = (Gradient * max(1, len(tensors)))()
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype in DTYPES):
+                raise TypeError(f"tensors[{i}]: expected a contiguous CUDA tensor of float32, bfloat16 or float16")
+            _need(o, t.dtype, f"outs[{i}]")
+            if o.numel() != t.numel():
+                raise TypeError(f"outs[{i}]: expected {t.numel()} elements")
+            arr[i] = Gradient(t.data_ptr(), o.data_ptr(), t.numel(), DTYPES[t.dtype])
+        nbytes = self.lib.gbt_gradient_list_bytes(arr, len(tensors))
+        with self._on_stream():
+            table = self.empty((max(16, nbytes),), torch.uint8)
+        pieces = C.c_int32()
+        self._check(self.lib.gbt_gradient_list(self.h, arr, len(tensors), _ptr(table), table.numel(), C.byref(pieces)))
+        return GradientList(tensors, outs, table, pieces.value)
+
+    def clip_gradients(self, gradients: GradientList, max_norm: float):
+        """Scales every tensor of the list by min(1, max_norm / (norm + 1e-6)) into its out; returns the global norm, a float32 scalar
+        on the device.  A norm that is not finite leaves the values as they are."""
+        with self._on_stream(*gradients.tensors, *gradients.outs):
+            norm = self.empty((), torch.float32)
+            ws = self.workspace("clip", 16384)
+        self._check(self.lib.gbt_clip_gradients(self.h, _ptr(gradients.table), gradients.pieces, max_norm, _ptr(norm), _ptr(ws), ws.numel()))
+        return norm

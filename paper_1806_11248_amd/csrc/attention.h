@@ -1,0 +1,237 @@
+// What the attention kernels share: arguments, the ragged rows, matrix instructions, tiles in LDS, buckets of distance.
+//
+// Everything is arranged around v_mfma_f32_32x32x16: a lane holds ONE column of the 32 x 32 result (column lane % 32) and
+// sixteen of its rows (register r: row 8 * (r / 4) + 4 * (lane / 32) + r % 4).  The kernels take scores transposed where a wave
+// owns queries (rows keys, columns queries), so a query's maximum and sum are sums over a lane's own registers and one exchange
+// between the two halves of the wave.  Sixteen rows of such a result, as they lie in eight registers of the two halves, are the second
+// operand of the next product without any move between lanes, as long as the first operand takes its rows in the same order:
+// slot e of half hl is row 4 * hl + e for e < 4 and 8 + 4 * hl + e - 4 beyond.  That order is what two transposing LDS reads
+// (ds_read_b64_tr_b16) of rows 4 * hl .. + 3 and 8 + 4 * hl .. + 3 give.
+#pragma once
+
+#include "gbt_internal.h"
+
+constexpr int kAttnBuckets = 256;   // most buckets of distance
+
+struct AttnView {   // rows x heads x head_dim elements; strides in elements, the head's elements side by side
+    char *data;
+    int64_t row, head;
+};
+
+struct AttnArgs {
+    AttnView q, k, v, out;
+    const int64_t *q_ptr, *k_ptr;   // NULL: sequence s has rows s * max .. (s + 1) * max
+    const int32_t *k_len;           // NULL: all of a sequence's key rows are used
+    int64_t q_rows, k_rows;
+    int n_seq, heads, kv_heads, group, dim, max_q, max_k, causal, n_buckets;
+    float scale, scale2;            // scale2 = scale * log2(e): probabilities are powers of two here
+    const float *bias;              // [n_buckets][heads]
+    float *lse;                     // [heads][q_rows], natural logarithm, or NULL
+    char *rest;                     // what rounding took from out, [q_rows][heads][dim], or NULL
+    // backward
+    AttnView dout, dq, dk, dv;
+    float *delta;                   // [heads][q_rows]
+    float *strips;                  // [heads][n_seq * k_blocks][n_buckets]: the bias gradient of each block of keys
+    float *dbias;                   // [n_buckets][heads]
+    // few rows
+    float *part;                    // partial results of the pieces of the key axis
+    int pieces, piece_len;
+};
+
+struct AttnCuts {   // ascending; filled up with INT32_MAX to a power of two less one
+    int32_t at[kAttnBuckets - 1];
+    int32_t steps;   // of the binary search: 2^steps - 1 cuts are looked at
+};
+
+hipError_t gbt_launch_attention(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
+hipError_t gbt_launch_attention_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
+hipError_t gbt_launch_attention_grad(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
+constexpr int kAttnQueries = 128;   // of a workgroup of the block kernels (keys, where a workgroup owns keys)
+constexpr int kAttnFewRows = 32;    // (query, head of the group) columns of a workgroup of the few-rows kernel
+
+#define GBT_LOG2E 1.44269504088896340736f
+#define GBT_LN2 0.69314718055994530942f
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+struct Bf16 {
+    typedef __bf16 elem;
+    typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct F16 {
+    typedef _Float16 elem;
+    typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <typename V>
+__device__ __forceinline__ V as_vec(i32x4 x) {
+    return __builtin_bit_cast(V, x);
+}
+
+// Rows of a tile lie `pitch` elements apart in LDS: head_dim and a pad with which both kinds of read (sixteen bytes of 32 rows;
+// 64 bytes of eight rows, transposed) meet every bank equally often.
+template <int DP>
+constexpr int attn_pitch() { return DP + (DP % 64 == 0 && DP != 64 ? 16 : DP == 32 ? 16 : 8); }
+
+struct AttnSeq {
+    int64_t q0, k0;
+    int nq, nk;
+};
+// The rows of sequence s.  Pointers that do not describe rows of the tensors describe none: no kernel reads past them.
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s) {
+    AttnSeq r;
+    int64_t q1, k1;
+    if (a.q_ptr) {
+        r.q0 = a.q_ptr[s];
+        q1 = a.q_ptr[s + 1];
+    } else {
+        r.q0 = (int64_t)s * a.max_q;
+        q1 = r.q0 + a.max_q;
+    }
+    if (a.k_ptr) {
+        r.k0 = a.k_ptr[s];
+        k1 = a.k_ptr[s + 1];
+    } else {
+        r.k0 = (int64_t)s * a.max_k;
+        k1 = r.k0 + a.max_k;
+    }
+    if (a.k_len) {
+        const int64_t len = a.k_len[s];
+        if (len < k1 - r.k0) k1 = r.k0 + len;
+    }
+    r.nq = r.q0 >= 0 && q1 <= a.q_rows && q1 > r.q0 ? (int)min(q1 - r.q0, (int64_t)a.max_q) : 0;
+    r.nk = r.k0 >= 0 && k1 <= a.k_rows && k1 > r.k0 ? (int)min(k1 - r.k0, (int64_t)a.max_k) : 0;
+    return r;
+}
+
+// Workgroups go to the eight XCDs in turn; the items of one stretch of the order share keys, so each XCD takes a stretch.
+__device__ __forceinline__ int64_t attn_item(int64_t items) {
+    const int64_t each = (items + 7) / 8;
+    return (int64_t)(blockIdx.x % 8) * each + blockIdx.x / 8;
+}
+
+// Sixteen bytes of a row, or zeros where the row or the elements do not exist.
+__device__ __forceinline__ i32x4 load16(const char *base, int64_t byte, bool there) {
+    i32x4 z = {0, 0, 0, 0};
+    if (there) z = *(const i32x4 *)(base + byte);
+    return z;
+}
+
+// One tile of ROWS rows on its way from memory to LDS, through registers of 256 threads.
+template <int DP, int ROWS>
+struct TileLoad {
+    static constexpr int kChunks = DP / 8, kEach = ROWS * kChunks / 256;
+    static_assert(ROWS * kChunks % 256 == 0, "whole chunks for every thread");
+    i32x4 reg[kEach];
+    __device__ __forceinline__ void load(const char *base, int64_t row_bytes, int rows, int dim) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = threadIdx.x + 256 * i, r = at / kChunks, c = at % kChunks;
+            reg[i] = load16(base, r * row_bytes + c * 16, r < rows && c * 8 < dim);
+        }
+    }
+    template <typename E>
+    __device__ __forceinline__ void store(E *tile) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = threadIdx.x + 256 * i, r = at / kChunks, c = at % kChunks;
+            *(i32x4 *)(tile + r * attn_pitch<DP>() + c * 8) = reg[i];
+        }
+    }
+};
+
+// First operand, rows of the tile as they are: row `row0 + lane % 32`, elements 16 * step + 8 * (lane / 32) .. + 7.
+template <typename P, int DP>
+__device__ __forceinline__ typename P::vec8 tile_rows(const typename P::elem *tile, int row0, int step, int lane) {
+    return *(const typename P::vec8 *)(tile + (row0 + (lane & 31)) * attn_pitch<DP>() + 16 * step + 8 * (lane >> 5));
+}
+
+// First operand, the tile transposed: row d = 32 * block + lane % 32, over the sixteen tile rows row0 .. row0 + 15 in the order
+// that a result's registers have (see above).
+template <typename P, int DP>
+__device__ __forceinline__ typename P::vec8 tile_cols(const typename P::elem *tile, int row0, int block, int lane) {
+    const int p = lane & 15;
+    const typename P::elem *at = tile + (row0 + 4 * (lane >> 5) + (p >> 2)) * attn_pitch<DP>() + 32 * block + 16 * ((lane >> 4) & 1) + 4 * (p & 3);
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * attn_pitch<DP>()));
+    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(typename P::vec8, both);
+}
+
+// Second operand from eight registers of a result, rounded to the inputs' type (to nearest, ties to even).
+template <typename P>
+__device__ __forceinline__ typename P::vec8 operand(const f32x16 &x, int half) {
+    typename P::vec8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (typename P::elem)x[8 * half + e];
+    return v;
+}
+
+// Row of register r of a 32 x 32 result.
+__device__ __forceinline__ constexpr int result_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+// Over the two halves of a column.
+__device__ __forceinline__ float column_max(float x) {
+    const int i = __builtin_bit_cast(int, x);
+    const auto both = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    return fmaxf(__builtin_bit_cast(float, (int)both[0]), __builtin_bit_cast(float, (int)both[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    const int i = __builtin_bit_cast(int, x);
+    const auto both = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    return __builtin_bit_cast(float, (int)both[0]) + __builtin_bit_cast(float, (int)both[1]);
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) x += __shfl_xor(x, s);
+    return x;
+}
+
+// Buckets of distance.  A bucket's number is how many cuts are at most the distance, as a symbol's is of its value.
+struct Buckets {
+    int cut[kAttnBuckets];
+    float value[kAttnBuckets];   // the head's, times log2(e)
+};
+__device__ __forceinline__ void buckets_load_cuts(Buckets &b, const AttnArgs &a, const AttnCuts &c) {
+    const int n = (1 << c.steps) - 1;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) b.cut[i] = c.at[i];
+}
+__device__ __forceinline__ void buckets_load_values(Buckets &b, const AttnArgs &a, int head) {
+    for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) b.value[i] = a.bias[(int64_t)i * a.heads + head] * GBT_LOG2E;
+}
+__device__ __forceinline__ int bucket_of(const Buckets &b, int steps, int t) {
+    int lo = 0;   // cuts known to be at most t
+    for (int s = steps - 1; s >= 0; --s) lo += b.cut[lo + (1 << s) - 1] <= t ? 1 << s : 0;
+    return lo;
+}
+
+// The distances that a tile of 64 rows against a workgroup's 128 meets are 191 in a row, and 64 new ones come with each step.  They
+// are kept in a ring of 256, twice, so that a stretch is read without wrapping.
+struct DistanceRing {
+    float value[512];
+    int bucket[512];
+};
+__device__ __forceinline__ void ring_put(DistanceRing &ring, const Buckets &b, int steps, int t) {
+    const int n = bucket_of(b, steps, t), at = t & 255;
+    const float v = b.value[n];
+    ring.value[at] = v;
+    ring.value[at + 256] = v;
+    ring.bucket[at] = n;
+    ring.bucket[at + 256] = n;
+}
+
+}  // namespace

@@ -251,6 +251,8 @@ int32_t upload2(gbt_ctx *ctx, const void *a, size_t a_bytes, const void *b, size
 
 }  // namespace
 
+int32_t gbt_upload(gbt_ctx *ctx, const void *host, size_t bytes, void *dev) { return upload(ctx, host, bytes, dev); }
+
 // ------------------------------------------------------------------ context --
 extern "C" const char *gbt_version(void) { return "libgbt 0.1 (gfx950)"; }
 

@@ -90,6 +90,9 @@ int32_t gbt_fail(gbt_ctx *ctx, int32_t code, const char *fmt, ...);
         if (!(cond)) return gbt_fail((ctx), (code), __VA_ARGS__); \
     } while (0)
 
+// Copies `bytes` bytes of a host table into `dev` on the context's stream, through the pinned staging.
+int32_t gbt_upload(gbt_ctx *ctx, const void *host, size_t bytes, void *dev);
+
 static constexpr inline size_t gbt_align(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
 // ---- job descriptors (host-built, read by kernels) --------------------------
@@ -104,6 +107,15 @@ struct HistJob {
     uint32_t pad0;   // 1: this is the only job of its (node, feature tile): it may store its bins instead of adding them
     uint32_t pad1;
 };
+
+// A stretch of one gradient tensor for the clipping kernels.
+struct ClipPiece {
+    const void *src;
+    void *dst;
+    int32_t n, dtype;
+};
+int gbt_clip_blocks(int64_t n_pieces);   // workgroups, and doubles of workspace
+hipError_t gbt_launch_clip(hipStream_t stream, const ClipPiece *pieces, int n_pieces, double max_norm, float *norm_out, double *sums);
 
 // One node for the split kernel.
 struct EvalNode {

@@ -1,0 +1,436 @@
+// Attention over ragged rows, with a bias for each bucket of distance.
+//
+//   S_ij = scale * q_i . k_j + bias[b(t)][h],  t = j - (i + nk - nq);   out_i = sum_j softmax_j(S_ij) v_j
+//
+// One pass over the keys with a running maximum and sum: out is kept as sum_j 2^(s_ij - m) v_j and scaled when m grows.
+// Sums, maxima and out are held in 32 bits; the probabilities are rounded to the inputs' type for the second product, while their
+// sum is taken of the unrounded ones (the rounding errors of a row then average out in out, whose own last place is of that size).
+#include "attention.h"
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ blocks of queries --
+// A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.
+template <typename P, int DP>
+__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a, AttnCuts c) {
+    typedef typename P::elem E;
+    typedef typename P::vec8 V8;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
+    __shared__ __align__(16) E k_tile[64 * kPitch];
+    __shared__ __align__(16) E v_tile[64 * kPitch];
+    __shared__ Buckets buckets;
+    __shared__ DistanceRing ring;
+
+    const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
+    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(items);
+    if (item >= items) return;
+    // the blocks that see the most keys first
+    const int block = q_blocks - 1 - (int)(item % q_blocks), head = (int)(item / q_blocks % a.heads), seq = (int)(item / q_blocks / a.heads);
+    const AttnSeq rows = attn_seq(a, seq);
+    const int first = block * kAttnQueries;
+    if (first >= rows.nq) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int off = rows.nk - rows.nq;
+    const int query = first + wave * 32 + (lane & 31);
+    const bool bias = a.n_buckets > 0;
+    if (bias) {
+        buckets_load_cuts(buckets, a, c);
+        buckets_load_values(buckets, a, head);
+    }
+
+    V8 qf[kSteps];
+    {
+        const char *base = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            qf[s] = as_vec<V8>(load16(base, (16 * s + 8 * half) * 2, query < rows.nq && 16 * s + 8 * half < a.dim));
+    }
+    // keys 0 .. last are seen by this lane's query; `end` by any of the workgroup's
+    const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
+    const int end = a.causal ? min(rows.nk, min(first + kAttnQueries, rows.nq) + off) : rows.nk;
+    const int wave_first = first + wave * 32;                                               // the wave's keys end before
+    const int wave_end = a.causal ? min(rows.nk, min(wave_first + 32, rows.nq) + off) : rows.nk;
+    const int wave_all = a.causal ? min(rows.nk, wave_first + off + 1) : rows.nk;           // and all of its queries see those before
+
+    const int kv_head = head / a.group;
+    const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
+    const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
+
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+
+    TileLoad<DP, 64> k_load, v_load;
+    k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
+    v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
+    __syncthreads();
+    if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
+
+    for (int kb = 0; kb < end; kb += 64) {
+        __syncthreads();   // the tile before has been read
+        k_load.store(k_tile);
+        v_load.store(v_tile);
+        __syncthreads();
+        if (kb + 64 < end) {
+            k_load.load(k_base + (int64_t)(kb + 64) * a.k.row * 2, a.k.row * 2, min(64, end - kb - 64), a.dim);
+            v_load.load(v_base + (int64_t)(kb + 64) * a.v.row * 2, a.v.row * 2, min(64, end - kb - 64), a.dim);
+        }
+        const int lowest = kb - (first + 127 + off);   // distance
+        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest + 191 + lane);
+        if (kb >= wave_end) continue;
+
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(tile_rows<P, DP>(k_tile, 32 * b, i, lane), qf[i], s[b]);
+        }
+        // scores in powers of two
+        const int at = (lowest & 255) + 96 - 32 * wave;   // of the wave's lowest distance, of 95
+        const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;
+        if (b0 == b1) {
+            const float add = bias ? buckets.value[b0] : 0.0f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, add);
+        } else {
+            const float *add = ring.value + at + 31 - (lane & 31);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, add[32 * b + result_row(r, half)]);
+        }
+        if (kb + 64 > wave_all) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = kb + 32 * b + result_row(r, half) <= last ? s[b][r] : -INFINITY;
+        }
+        float now = top;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) now = fmaxf(now, s[b][r]);
+        now = column_max(now);
+        const float base = now == -INFINITY ? 0.0f : now;   // a row that has seen nothing yet
+        if (__any(now > top)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - base);
+            sum *= shrink;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
+            top = now;
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - base);
+                sum += s[b][r];
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const V8 p = operand<P>(s[i / 2], i % 2);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(tile_cols<P, DP>(v_tile, 16 * i, b, lane), p, o[b]);
+        }
+    }
+
+    sum = column_sum(sum);
+    if (query >= rows.nq) return;
+    const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // no key: zeros; a sum that is no number stays none
+    if (a.lse && half == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * GBT_LN2;
+    E *out = (E *)a.out.data + (rows.q0 + query) * a.out.row + (int64_t)head * a.out.head;
+    E *rest = (E *)a.rest + ((rows.q0 + query) * a.heads + head) * a.dim;
+    typedef E E4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * b + 8 * g + 4 * half;
+            if (d < a.dim) {
+                E4 x, y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float w = o[b][4 * g + e] * inv;
+                    x[e] = (E)w;
+                    y[e] = (E)(w - (float)x[e]);
+                }
+                *(E4 *)(out + d) = x;
+                if (a.rest) *(E4 *)(rest + d) = y;
+            }
+        }
+}
+
+// -------------------------------------------------------------------------------------------------------- few rows --
+// Single new events against a long store: what there is to do is to read the store once.  The columns of a wave are the (query, head
+// of the group) pairs of one key head, 32 of them at most, so that all heads that share keys read them together; the four waves of a
+// workgroup take every fourth 32 keys of its piece of the key axis and are joined at its end, the pieces by a second launch.  Keys
+// come from memory in the order of the first operand (a lane reads sixteen bytes of its row), values through a wave's own part
+// of LDS for the transposing reads, so no wave waits for another.
+template <typename P, int DP>
+__global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts c) {
+    typedef typename P::elem E;
+    typedef typename P::vec8 V8;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>(), kChunks = DP / 8, kEach = 32 * kChunks / 64;
+    __shared__ __align__(16) E v_tile[4][32 * kPitch];
+    __shared__ int cut[kAttnBuckets];
+    __shared__ int near_bucket[4][64];
+    __shared__ float join_top[4][32], join_sum[4][32];
+    __shared__ float join_o[4][32 * 33];
+
+    const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
+    const int64_t items = (int64_t)a.pieces * blocks * a.kv_heads * a.n_seq, item = attn_item(items);
+    if (item >= items) return;
+    const int piece = (int)(item % a.pieces), block = (int)(item / a.pieces % blocks);
+    const int kv_head = (int)(item / a.pieces / blocks % a.kv_heads), seq = (int)(item / a.pieces / blocks / a.kv_heads);
+    const AttnSeq rows = attn_seq(a, seq);
+    const int begin = piece * a.piece_len;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int column = block * kAttnFewRows + (lane & 31), query = column / a.group, head = kv_head * a.group + column % a.group;
+    if (block * kAttnFewRows / a.group >= rows.nq) return;
+    if (begin > 0 && begin >= rows.nk) return;   // the first piece writes the rows without keys
+    const int off = rows.nk - rows.nq;
+    const bool there = query < rows.nq;
+    const bool bias = a.n_buckets > 0;
+    if (bias) {
+        const int n = (1 << c.steps) - 1;
+        for (int i = threadIdx.x; i < n; i += 256) cut[i] = c.at[i];
+    }
+    __syncthreads();
+
+    V8 qf[kSteps];
+    {
+        const char *base = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            qf[s] = as_vec<V8>(load16(base, (16 * s + 8 * half) * 2, there && 16 * s + 8 * half < a.dim));
+    }
+    const int q_low = block * kAttnFewRows / a.group, q_high = min(rows.nq - 1, (block * kAttnFewRows + kAttnFewRows - 1) / a.group);
+    const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
+    const int end = min(min(rows.nk, begin + a.piece_len), a.causal ? q_high + off + 1 : rows.nk);
+    const int all = a.causal ? min(rows.nk, q_low + off + 1) : rows.nk;   // every query sees the keys before
+    const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
+    const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
+    const float *value = a.bias + (there ? head : 0);
+
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+
+    i32x4 k_reg[kSteps], v_reg[kEach];
+    auto load = [&](int kb) {
+        const char *kr = k_base + (int64_t)(kb + (lane & 31)) * a.k.row * 2;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) k_reg[s] = load16(kr, (16 * s + 8 * half) * 2, kb + (lane & 31) < end && 16 * s + 8 * half < a.dim);
+        const char *vr = v_base + (int64_t)kb * a.v.row * 2;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = lane + 64 * i, r = at / kChunks, ch = at % kChunks;
+            v_reg[i] = load16(vr, r * a.v.row * 2 + ch * 16, kb + r < end && ch * 8 < a.dim);
+        }
+    };
+    const int start = begin + 32 * wave;
+    if (start < end) load(start);
+    for (int kb = start; kb < end; kb += 128) {
+        f32x16 s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) s = P::mma(as_vec<V8>(k_reg[i]), qf[i], s);
+        // a wave's LDS reads and writes are done in their order: the values of the step before have been read
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int at = lane + 64 * i, r = at / kChunks, ch = at % kChunks;
+            *(i32x4 *)(v_tile[wave] + r * kPitch + ch * 8) = v_reg[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (kb + 128 < end) load(kb + 128);
+        const int lowest = kb - (q_high + off), span = 31 + q_high - q_low;   // distances lowest .. lowest + span, 63 at most
+        int mine = 0;
+        if (bias) {
+            const int t = lowest + min(lane, span);
+            for (int st = c.steps - 1; st >= 0; --st) mine += cut[mine + (1 << st) - 1] <= t ? 1 << st : 0;
+        }
+        const int b0 = __builtin_amdgcn_readlane(mine, 0), b1 = __builtin_amdgcn_readlane(mine, 63);
+        if (b0 == b1) {
+            const float add = bias ? value[(int64_t)b0 * a.heads] * GBT_LOG2E : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, add);
+        } else {
+            near_bucket[wave][lane] = mine;
+            __builtin_amdgcn_wave_barrier();
+            const int *at = near_bucket[wave] + (there ? q_high - query : 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, value[(int64_t)at[result_row(r, half)] * a.heads] * GBT_LOG2E);
+        }
+        if (kb + 32 > min(all, end)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = kb + result_row(r, half);
+                s[r] = key <= last && key < end ? s[r] : -INFINITY;
+            }
+        }
+        float now = top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) now = fmaxf(now, s[r]);
+        now = column_max(now);
+        const float base = now == -INFINITY ? 0.0f : now;
+        if (__any(now > top)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - base);
+            sum *= shrink;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
+            top = now;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+            sum += s[r];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const V8 p = operand<P>(s, i);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(tile_cols<P, DP>(v_tile[wave], 16 * i, b, lane), p, o[b]);
+        }
+    }
+
+    // the four waves' rows together
+    sum = column_sum(sum);
+    if (half == 0) {
+        join_top[wave][lane] = top;
+        join_sum[wave][lane] = sum;
+    }
+    __syncthreads();
+    const int col = lane & 31;
+    float all_top = -INFINITY, all_sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) all_top = fmaxf(all_top, join_top[w][col]);
+    const float base = all_top == -INFINITY ? 0.0f : all_top;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) all_sum += join_sum[w][col] * __builtin_amdgcn_exp2f(join_top[w][col] - base);
+    const bool whole = a.pieces == 1;
+    const float factor = __builtin_amdgcn_exp2f(top - base) * (whole ? all_sum > 0.0f ? 1.0f / all_sum : all_sum == 0.0f ? 0.0f : all_sum : 1.0f);
+    const int64_t part = ((((int64_t)seq * a.kv_heads + kv_head) * columns + column) * a.pieces + piece) * (a.dim + 2);
+    if (wave == 0 && half == 0 && there) {
+        if (whole) {
+            if (a.lse) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = all_sum == 0.0f ? -INFINITY : (all_top + __builtin_amdgcn_logf(all_sum)) * GBT_LN2;
+        } else {
+            a.part[part + a.dim] = all_top;
+            a.part[part + a.dim + 1] = all_sum;
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        if (b) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) join_o[wave][col * 33 + result_row(r, half)] = o[b][r] * factor;
+        __syncthreads();
+        // thread: elements d, d + 8, .. of a column
+        for (int i = threadIdx.x; i < 32 * 32; i += 256) {
+            const int cc = i >> 5, d = 32 * b + (i & 31), column2 = block * kAttnFewRows + cc, query2 = column2 / a.group;
+            if (query2 >= rows.nq || d >= a.dim) continue;
+            const int x = cc * 33 + (i & 31);
+            const float w = (join_o[0][x] + join_o[1][x]) + (join_o[2][x] + join_o[3][x]);
+            const int head2 = kv_head * a.group + column2 % a.group;
+            if (whole) {
+                const E y = (E)w;
+                ((E *)a.out.data)[(rows.q0 + query2) * a.out.row + (int64_t)head2 * a.out.head + d] = y;
+                if (a.rest) ((E *)a.rest)[((rows.q0 + query2) * a.heads + head2) * a.dim + d] = (E)(w - (float)y);
+            } else {
+                a.part[((((int64_t)seq * a.kv_heads + kv_head) * columns + column2) * a.pieces + piece) * (a.dim + 2) + d] = w;
+            }
+        }
+    }
+}
+
+// The pieces of the key axis together: a wave takes a (sequence, key head, column), its lanes the elements.
+template <typename P>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
+    typedef typename P::elem E;
+    const int columns = a.group * a.max_q;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= (int64_t)a.n_seq * a.kv_heads * columns) return;
+    const int lane = threadIdx.x & 63;
+    const int column = (int)(at % columns), kv_head = (int)(at / columns % a.kv_heads), seq = (int)(at / columns / a.kv_heads);
+    const int query = column / a.group, head = kv_head * a.group + column % a.group;
+    const AttnSeq rows = attn_seq(a, seq);
+    if (query >= rows.nq) return;
+    const int n = max(1, (rows.nk + a.piece_len - 1) / a.piece_len);
+    const float *part = a.part + at * a.pieces * (a.dim + 2);
+    float top = -INFINITY;
+    for (int p = lane; p < n; p += 64) top = fmaxf(top, part[(int64_t)p * (a.dim + 2) + a.dim]);
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int p = 0; p < n; ++p) {
+        const float *x = part + (int64_t)p * (a.dim + 2);
+        const float f = __builtin_amdgcn_exp2f(x[a.dim] - base);
+        sum += x[a.dim + 1] * f;
+        if (lane < a.dim) o0 += x[lane] * f;
+        if (lane + 64 < a.dim) o1 += x[lane + 64] * f;
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+    if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * GBT_LN2;
+    E *out = (E *)a.out.data + (rows.q0 + query) * a.out.row + (int64_t)head * a.out.head;
+    E *rest = (E *)a.rest + ((rows.q0 + query) * a.heads + head) * a.dim;
+    auto put = [&](int d, float w) {
+        const E y = (E)w;
+        out[d] = y;
+        if (a.rest) rest[d] = (E)(w - (float)y);
+    };
+    if (lane < a.dim) put(lane, o0 * inv);
+    if (lane + 64 < a.dim) put(lane + 64, o1 * inv);
+}
+
+unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
+
+template <typename P, int DP>
+hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
+    const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
+    attention_kernel<P, DP><<<grid_of(blocks * a.heads * a.n_seq), 256, 0, stream>>>(a, c);
+    return hipGetLastError();
+}
+
+template <typename P, int DP>
+hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
+    const int64_t columns = (int64_t)a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
+    attention_few_kernel<P, DP><<<grid_of(a.pieces * blocks * a.kv_heads * a.n_seq), 256, 0, stream>>>(a, c);
+    if (a.pieces > 1) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        attention_join_kernel<P><<<(unsigned)((columns * a.kv_heads * a.n_seq + 3) / 4), 256, 0, stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <typename P>
+hipError_t by_dim(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, bool few) {
+    if (a.dim <= 32) return few ? launch_few<P, 32>(stream, a, c) : launch<P, 32>(stream, a, c);
+    if (a.dim <= 64) return few ? launch_few<P, 64>(stream, a, c) : launch<P, 64>(stream, a, c);
+    if (a.dim <= 96) return few ? launch_few<P, 96>(stream, a, c) : launch<P, 96>(stream, a, c);
+    return few ? launch_few<P, 128>(stream, a, c) : launch<P, 128>(stream, a, c);
+}
+
+}  // namespace
+
+hipError_t gbt_launch_attention(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype) {
+    return dtype == GBT_BF16 ? by_dim<Bf16>(stream, a, c, false) : by_dim<F16>(stream, a, c, false);
+}
+hipError_t gbt_launch_attention_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype) {
+    return dtype == GBT_BF16 ? by_dim<Bf16>(stream, a, c, true) : by_dim<F16>(stream, a, c, true);
+}

@@ -1,0 +1,124 @@
+// The global norm of many gradient tensors, and the gradients scaled down to a limit.
+//
+// Two launches over the same pieces: one adds up squares, the other scales (every workgroup adds up the few partial sums for itself,
+// so no third launch stands between).  Squares are summed in 64 bits: a square of any float is representable there, so neither large
+// nor tiny gradients leave the range, and the order of the partial sums is fixed.  Bound: memory.
+#include "gbt_internal.h"
+
+namespace {
+
+constexpr int kClipBlocks = 2048;   // workgroups of 256 threads: what the compute units hold at once
+
+template <typename E>
+struct alignas(16) Vec {
+    E x[16 / sizeof(E)];
+};
+
+template <typename E>
+__device__ __forceinline__ void add_squares(const ClipPiece &p, double (&sum)[4]) {
+    constexpr int kVec = 16 / sizeof(E);
+    const E *src = (const E *)p.src;
+    int i = 0;
+    if (((uintptr_t)src & 15) == 0) {
+        const int vecs = p.n / kVec;
+        const Vec<E> *v = (const Vec<E> *)src;
+        for (int at = threadIdx.x; at < vecs; at += 1024) {
+            Vec<E> x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (at + 256 * u < vecs) x[u] = v[at + 256 * u];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (at + 256 * u < vecs)
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) {
+                        const double w = (double)(float)x[u].x[e];
+                        sum[e & 3] = fma(w, w, sum[e & 3]);
+                    }
+        }
+        i = vecs * kVec;
+    }
+    for (i += threadIdx.x; i < p.n; i += 256) {
+        const double w = (double)(float)src[i];
+        sum[0] = fma(w, w, sum[0]);
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ void scale_piece(const ClipPiece &p, float coef) {
+    constexpr int kVec = 16 / sizeof(E);
+    const E *src = (const E *)p.src;
+    E *dst = (E *)p.dst;
+    int i = 0;
+    if ((((uintptr_t)src | (uintptr_t)dst) & 15) == 0) {
+        const int vecs = p.n / kVec;
+        for (int at = threadIdx.x; at < vecs; at += 1024) {
+            Vec<E> x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (at + 256 * u < vecs) x[u] = ((const Vec<E> *)src)[at + 256 * u];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (at + 256 * u < vecs) {
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) x[u].x[e] = (E)((float)x[u].x[e] * coef);
+                    ((Vec<E> *)dst)[at + 256 * u] = x[u];
+                }
+        }
+        i = vecs * kVec;
+    }
+    for (i += threadIdx.x; i < p.n; i += 256) dst[i] = (E)((float)src[i] * coef);
+}
+
+__device__ __forceinline__ double block_sum(double x, double *part) {
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) x += __shfl_xor(x, s);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__global__ __launch_bounds__(256) void clip_norm_kernel(const ClipPiece *pieces, int n_pieces, double *sums) {
+    __shared__ double part[4];
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int i = blockIdx.x; i < n_pieces; i += gridDim.x) {
+        const ClipPiece p = pieces[i];
+        if (p.dtype == GBT_F32) add_squares<float>(p, sum);
+        else if (p.dtype == GBT_BF16) add_squares<__bf16>(p, sum);
+        else add_squares<_Float16>(p, sum);
+    }
+    const double all = block_sum((sum[0] + sum[1]) + (sum[2] + sum[3]), part);
+    if (threadIdx.x == 0) sums[blockIdx.x] = all;
+}
+
+// Pieces in the opposite order: those read last are still in the cache behind L2.
+__global__ __launch_bounds__(256) void clip_scale_kernel(const ClipPiece *pieces, int n_pieces, const double *sums, int n_sums, double max_norm,
+                                                         float *norm_out) {
+    __shared__ double part[4];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n_sums; i += 256) sum += sums[i];
+    const double norm = sqrt(block_sum(sum, part));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    // a norm that is no finite number says nothing about how to scale: the gradients stay as they are
+    const float coef = isfinite((float)norm) ? (float)fmin(1.0, max_norm / (norm + 1e-6)) : 1.0f;
+    for (int i = n_pieces - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
+        const ClipPiece p = pieces[i];
+        if (coef == 1.0f && p.src == p.dst) continue;
+        if (p.dtype == GBT_F32) scale_piece<float>(p, coef);
+        else if (p.dtype == GBT_BF16) scale_piece<__bf16>(p, coef);
+        else scale_piece<_Float16>(p, coef);
+    }
+}
+
+}  // namespace
+
+int gbt_clip_blocks(int64_t n_pieces) { return (int)std::max<int64_t>(1, std::min<int64_t>(n_pieces, kClipBlocks)); }
+
+hipError_t gbt_launch_clip(hipStream_t stream, const ClipPiece *pieces, int n_pieces, double max_norm, float *norm_out, double *sums) {
+    const int blocks = gbt_clip_blocks(n_pieces);
+    clip_norm_kernel<<<blocks, 256, 0, stream>>>(pieces, n_pieces, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    clip_scale_kernel<<<blocks, 256, 0, stream>>>(pieces, n_pieces, sums, blocks, max_norm, norm_out);
+    return hipGetLastError();
+}

@@ -1,0 +1,359 @@
+"""Attention over ragged rows with a bias by buckets of distance, and its backward pass, against the formulas in 64 bits (-m gpu)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from attention_ref import Reference, close, rows_of
+
+pytestmark = pytest.mark.gpu
+
+BF, HF = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_1806_11248_amd as g
+    c = g.Context(0)
+    yield c
+    c.close()
+
+
+def _make(nq, nk, H, K, D, dtype, *, causal, buckets=0, far=40, room=0, fused=False, seed=0, spread=1.0, poison=True):
+    """Inputs on the GPU and what the call takes.  Rows that belong to no sequence hold NaN."""
+    import paper_1806_11248_amd as g
+    rng = torch.Generator().manual_seed(seed)
+    q_ptr = rows_of(nq)
+    k_ptr = rows_of([n + room for n in nk])
+    same = fused and nq == nk and room == 0
+    if same:
+        qkv = (torch.randn(q_ptr[-1], H + 2 * K, D, generator=rng) * spread).to(dtype).cuda()
+        q, k, v = qkv.split([H, K, K], dim=1)
+    else:
+        q, k, v = ((torch.randn(n, h, D, generator=rng) * spread).to(dtype) for n, h in ((q_ptr[-1], H), (k_ptr[-1], K), (k_ptr[-1], K)))
+        if room and poison:
+            for s, n in enumerate(nk):
+                k[k_ptr[s] + n:k_ptr[s + 1]] = math.nan
+                v[k_ptr[s] + n:k_ptr[s + 1]] = math.inf
+        q, k, v = q.cuda(), k.cuda(), v.cuda()
+    cuts = g.distance_cuts(buckets, far, causal) if buckets else None
+    bias = torch.randn(buckets, H, generator=rng).cuda() if buckets else None
+    dout = torch.randn(q_ptr[-1], H, D, generator=rng).to(dtype).cuda()
+    args = dict(q_ptr=torch.tensor(q_ptr).cuda(), k_ptr=torch.tensor(k_ptr).cuda(), max_q=max(nq), max_k=max(nk), causal=causal, bias=bias, cuts=cuts)
+    if room:
+        args["k_len"] = torch.tensor(nk, dtype=torch.int32).cuda()
+    spans = list(zip(q_ptr[:-1], nq, k_ptr[:-1], nk))
+    return q, k, v, dout, args, spans
+
+
+def _reference(q, k, v, args, spans, dout=None, scale=None):
+    D = q.shape[2]
+    return Reference(q.cpu(), k.cpu(), v.cpu(), spans, args["causal"], D ** -0.5 if scale is None else scale,
+                     None if args["bias"] is None else args["bias"].cpu(), args["cuts"], None if dout is None else dout.cpu())
+
+
+def _check(ctx, made, backward=True):
+    q, k, v, dout, args, spans = made
+    ref = _reference(q, k, v, args, spans, dout if backward else None)
+    out = ctx.attention(q, k, v, **args)
+    close(out, ref.out, ref.out_tol, "out")
+    saved_out, saved = ctx.attention(q, k, v, save=True, **args)
+    close(saved_out, ref.out, ref.out_tol, "out of a saved pass")
+    close(saved[0], ref.lse, ref.lse_tol, "lse")
+    if not backward:
+        return
+    grads = ctx.attention_backward(dout, q, k, v, saved_out, saved, **args)
+    again = ctx.attention_backward(dout, q, k, v, saved_out, saved, **args)
+    for name, a, b in zip(("dq", "dk", "dv", "dbias"), grads, again):
+        if a is None:
+            assert name == "dbias" and args["bias"] is None
+            continue
+        assert torch.equal(a, b), f"{name} differs from run to run"
+        close(a, getattr(ref, name), getattr(ref, name + "_tol"), name)
+    # rows of no sequence get zeros
+    assert not grads[1].cpu()[~ref.covered_k].any() and not grads[2].cpu()[~ref.covered_k].any()
+
+
+SHAPES = [
+    # one token; the tile edges of 32, 64 and 128 rows; nothing at all; the last of each kind without neighbours
+    ([1], [1], 1, 1, 8), ([31, 32, 33], [31, 32, 33], 2, 1, 32), ([63, 64, 65, 0, 1], [63, 64, 65, 0, 1], 4, 4, 64),
+    ([127, 129, 2], [127, 129, 2], 2, 2, 128), ([257], [257], 3, 1, 96), ([40], [40], 6, 2, 80), ([70, 5], [70, 5], 2, 1, 24),
+    ([50, 50], [50, 50], 2, 2, 104), ([192], [192], 1, 1, 40),
+    # more keys than queries, fewer (causal: the first rows see none), none, and no queries
+    ([33, 64, 100], [90, 300, 101], 4, 2, 64), ([100, 150, 40], [30, 140, 1], 2, 1, 64), ([36, 0, 50], [0, 17, 200], 2, 2, 32),
+]
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_against_the_formulas(ctx, shape, causal, dtype):
+    nq, nk, H, K, D = SHAPES[shape]
+    buckets = [0, 1, 2, 7, 32, 256][(shape + causal) % 6]
+    _check(ctx, _make(nq, nk, H, K, D, dtype, causal=causal, buckets=buckets, far=max(60, 2 * buckets), seed=shape, fused=shape % 2 == 1))
+
+
+@pytest.mark.parametrize("far,buckets", [(20, 32), (64, 33), (700, 24), (5000, 40), (100_000, 5)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_buckets_near_and_far(ctx, far, buckets, causal):
+    """Buckets of one distance, wider than a tile, wider than the rows: every way a tile's distances fall into them."""
+    _check(ctx, _make([700, 321], [700, 321], 2, 1, 32, BF, causal=causal, buckets=buckets, far=far, seed=far))
+
+
+def test_cuts_anywhere(ctx):
+    """Cuts are the caller's: far from zero, on one side only, or none that any pair reaches."""
+    for cuts in ([5, 6, 90], [-400, -399, -130], [10 ** 9], [-2 ** 31, 0, 2 ** 31 - 2]):
+        made = _make([150, 40], [260, 40], 2, 2, 64, BF, causal=False, buckets=len(cuts) + 1, seed=7)
+        made[4]["cuts"] = cuts
+        _check(ctx, made)
+
+
+# (queries, keys, heads, kv_heads, head_dim, room)
+STORES = [
+    ([1], [1], 1, 1, 64, 0), ([1, 1, 1], [5, 64, 333], 8, 2, 64, 7), ([1, 1], [4097, 1500], 16, 4, 128, 16), ([1] * 5, [1, 0, 2, 127, 129], 4, 4, 32, 3),
+    ([2, 1, 3], [900, 3, 2500], 8, 8, 96, 1), ([4, 1], [40, 600], 6, 2, 80, 5), ([7], [3000], 4, 1, 40, 0), ([5, 0, 6], [2, 30, 6], 3, 1, 64, 2),
+    ([32, 9], [333, 2000], 1, 1, 64, 0), ([1], [20_000], 32, 1, 128, 0),
+]
+
+
+@pytest.mark.parametrize("store", range(len(STORES)))
+@pytest.mark.parametrize("causal", [False, True])
+def test_new_events_against_a_store(ctx, store, causal):
+    """Few query rows: the form that is split over the keys and joined; slots' unused rows hold NaN and infinities."""
+    nq, nk, H, K, D, room = STORES[store]
+    dtype = BF if store % 2 else HF
+    made = _make(nq, nk, H, K, D, dtype, causal=causal, buckets=[0, 16, 40][store % 3], far=1000, room=room, seed=store)
+    _check(ctx, made, backward=max(nk) < 5000)
+
+
+def test_one_new_event_is_the_last_row_of_the_whole(ctx):
+    q, k, v, dout, args, spans = _make([300], [300], 4, 2, 64, BF, causal=True, buckets=20, seed=1)
+    whole = ctx.attention(q, k, v, causal=True, bias=args["bias"], cuts=args["cuts"])
+    one = ctx.attention(q[-1:].contiguous(), k, v, causal=True, bias=args["bias"], cuts=args["cuts"])
+    ref = _reference(q, k, v, args, spans)
+    close(one, ref.out[-1:], ref.out_tol[-1:], "new event")
+    close(whole[-1:], ref.out[-1:], ref.out_tol[-1:], "last row")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_large_scores(ctx, dtype):
+    """Scores in the hundreds, both signs: probabilities that underflow, rows that one key owns."""
+    _check(ctx, _make([130, 5], [130, 5], 2, 2, 64, dtype, causal=True, buckets=8, spread=6.0, seed=2))
+    q, k, v, dout, args, spans = _make([70], [70], 1, 1, 32, dtype, causal=False, buckets=4, seed=3)
+    args["bias"][:] = torch.tensor([[-300.0], [80.0], [-3e38], [0.0]]).cuda()        # a bias of the type's lowest values shuts a bucket out
+    ref = _reference(q, k, v, args, spans)
+    out = ctx.attention(q, k, v, **args)
+    close(out, ref.out, ref.out_tol, "out")
+
+
+def test_minus_infinity_in_the_bias_shuts_a_bucket_out(ctx):
+    """A bucket at -inf takes no part; a row all of whose keys are shut out is a row without keys."""
+    made = _make([90], [90], 2, 1, 64, BF, causal=False, buckets=5, seed=4)
+    q, k, v, dout, args, spans = made
+    args["cuts"] = [-30, -3, 3, 30]
+    args["bias"][0] = args["bias"][3] = -math.inf
+    _check(ctx, made)
+    args["bias"][2] = -math.inf                # the nearest too: rows at the ends keep one side, the middle both
+    _check(ctx, made)
+    args["bias"][:] = -math.inf
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+    assert not out.any() and torch.isinf(saved[0]).all()
+    grads = ctx.attention_backward(dout, q, k, v, out, saved, **args)
+    assert all(not x.any() for x in grads)
+    args["bias"][0] = 1.0                      # the first rows see nothing still
+    _check(ctx, made)
+
+
+def test_non_finite_values_stay_in_their_sequence(ctx):
+    nq = [40, 65, 30]
+    q, k, v, dout, args, spans = _make(nq, nq, 2, 1, 64, BF, causal=True, buckets=6, seed=5)
+    ref = _reference(q, k, v, args, spans, dout)
+    k[50], v[60], q[70], dout[80] = math.nan, math.inf, math.nan, math.nan           # all of the second sequence
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+    dq, dk, dv, _ = ctx.attention_backward(dout, q, k, v, out, saved, **args)
+    for a, b in ((0, 40), (105, 135)):
+        for name, x in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv)):
+            close(x[a:b], getattr(ref, name)[a:b], getattr(ref, name + "_tol")[a:b], name)
+    assert torch.isnan(out[40:105]).any()
+
+
+def test_gradients_against_differences(ctx):
+    """Directional differences of the 64-bit values, within what the bounds of the gradients allow along the direction."""
+    made = _make([60, 100], [60, 100], 4, 2, 32, HF, causal=True, buckets=9, seed=6)
+    q, k, v, dout, args, spans = made
+    ref = _reference(q, k, v, args, spans, dout)
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+    grads = dict(zip(("q", "k", "v", "bias"), ctx.attention_backward(dout, q, k, v, out, saved, **args)))
+    base = dict(q=q.cpu().double(), k=k.cpu().double(), v=v.cpu().double(), bias=args["bias"].cpu().double())
+    g = dout.cpu().double()
+    rng = torch.Generator().manual_seed(9)
+
+    def value(x):
+        return float((Reference(x["q"], x["k"], x["v"], spans, True, 32 ** -0.5, x["bias"], args["cuts"]).out * g).sum())
+
+    for name in base:
+        d = torch.randn(base[name].shape, generator=rng, dtype=torch.float64)
+        h = 1e-5
+        diff = (value({**base, name: base[name] + h * d}) - value({**base, name: base[name] - h * d})) / (2 * h)
+        tol = float((getattr(ref, "d" + name + "_tol") * d.abs()).sum()) + 1e-6 * abs(diff) + 1e-6
+        assert abs(float((grads[name].cpu().double() * d).sum()) - diff) <= tol, name
+
+
+def test_rows_far_apart(ctx):
+    """Strides of a fused projection with other parts between, outputs into the caller's tensor, sequences of equal length without pointers."""
+    rng = torch.Generator().manual_seed(11)
+    big = torch.randn(96, 3, 12, 64, generator=rng).to(BF).cuda()
+    q, k, v = big[:, 0, :8], big[:, 1, 2:6], big[:, 2, 8:12]
+    spans = [(0, 32, 0, 32), (32, 32, 32, 32), (64, 32, 64, 32)]
+    ref = Reference(q.cpu(), k.cpu(), v.cpu(), spans, False, 64 ** -0.5)
+    ptr = torch.tensor([0, 32, 64, 96]).cuda()
+    wide = torch.full((96, 2, 8, 64), 7.0, dtype=BF).cuda()
+    out = ctx.attention(q, k, v, q_ptr=ptr, k_ptr=ptr, max_q=32, max_k=32, out=wide[:, 1])
+    assert out.data_ptr() == wide[:, 1].data_ptr() and bool((wide[:, 0] == 7.0).all())
+    close(out, ref.out, ref.out_tol, "out")
+    plain = ctx.attention(q[:32], k[:32], v[:32])
+    assert torch.equal(plain, out[:32])
+
+
+def test_pointers_beyond_the_rows_describe_nothing(ctx):
+    """Row pointers come from the device unchecked: what does not lie inside the tensors is not read, and not written."""
+    q, k, v, dout, args, spans = _make([40, 40], [40, 40], 2, 2, 64, BF, causal=True, buckets=4, seed=12)
+    out = torch.full_like(q, 5.0)
+    for bad in ([0, 10 ** 12, 80], [-5, 40, 10 ** 15], [60, 20, 10]):
+        a = dict(args, q_ptr=torch.tensor(bad).cuda(), k_ptr=torch.tensor(bad).cuda())
+        ctx.attention(q, k, v, out=out, **a)
+        torch.cuda.synchronize()
+    assert bool((out[10:] == 5.0).any())
+
+
+def test_another_stream_than_the_current_one(ctx):
+    import paper_1806_11248_amd as g
+    side = torch.cuda.Stream()
+    other = g.Context(0, stream=side)
+    try:
+        q, k, v, dout, args, spans = _make([200, 77], [200, 77], 4, 2, 64, BF, causal=True, buckets=12, seed=13)
+        want_out, saved = ctx.attention(q, k, v, save=True, **args)
+        want = ctx.attention_backward(dout, q, k, v, want_out, saved, **args)
+        side.wait_stream(torch.cuda.current_stream())
+        out, saved = other.attention(q, k, v, save=True, **args)
+        got = other.attention_backward(dout, q, k, v, out, saved, **args)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(out, want_out) and all(torch.equal(a, b) for a, b in zip(got, want))
+    finally:
+        other.close()
+
+
+def test_in_a_graph(ctx):
+    """The calls allocate nothing and wait for nothing, so they can be recorded; every replay gives the eager result."""
+    import paper_1806_11248_amd as g
+    side = torch.cuda.Stream()
+    own = g.Context(0, stream=side)
+    try:
+        for nq, nk in (([150, 90], [150, 90]), ([1, 1], [3000, 40])):
+            q, k, v, dout, args, spans = _make(nq, nk, 4, 2, 64, BF, causal=True, buckets=12, seed=14)
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                out, saved = own.attention(q, k, v, save=True, **args)
+                own.attention_backward(dout, q, k, v, out, saved, **args)
+                side.synchronize()
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=side):
+                    out, saved = own.attention(q, k, v, save=True, **args)
+                    grads = own.attention_backward(dout, q, k, v, out, saved, **args)
+                for step in range(3):
+                    q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(step)).to(BF))
+                    graph.replay()
+                    side.synchronize()
+                    eager, s2 = own.attention(q, k, v, save=True, **args)
+                    want = own.attention_backward(dout, q, k, v, eager, s2, **args)
+                    side.synchronize()
+                    assert torch.equal(out, eager) and all(torch.equal(a, b) for a, b in zip(grads, want))
+    finally:
+        own.close()
+
+
+def test_no_rows_at_all(ctx):
+    q = torch.empty(0, 4, 64, dtype=BF, device="cuda")
+    k = torch.empty(0, 2, 64, dtype=BF, device="cuda")
+    bias = torch.ones(3, 4, device="cuda")
+    ptr = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out, saved = ctx.attention(q, k, k, q_ptr=ptr, k_ptr=ptr, max_q=0, max_k=0, bias=bias, cuts=[-1, 0], save=True)
+    dq, dk, dv, dbias = ctx.attention_backward(q, q, k, k, out, saved, q_ptr=ptr, k_ptr=ptr, max_q=0, max_k=0, bias=bias, cuts=[-1, 0])
+    assert out.shape == q.shape and not dbias.any()
+
+
+def test_refusals(ctx):
+    import ctypes as C
+    import paper_1806_11248_amd as g
+    b = g.binding
+    q, k, v, dout, args, spans = _make([20], [20], 4, 2, 64, BF, causal=True, buckets=4, seed=15)
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+
+    def refused(code, call):
+        with pytest.raises(g.GbtError) as e:
+            call()
+        assert e.value.code == code
+
+    with pytest.raises(TypeError):
+        ctx.attention(q, k.half(), v, **args)
+    with pytest.raises(TypeError):
+        ctx.attention(q.cpu(), k, v, **args)
+    with pytest.raises(TypeError):
+        ctx.attention(q, k, v[:, :1], **args)
+    with pytest.raises(TypeError):
+        ctx.attention(q, k, v, **dict(args, cuts=[1]))
+    with pytest.raises(TypeError):
+        ctx.attention(q, k, v, **dict(args, bias=args["bias"][:, :2]))
+    with pytest.raises(TypeError):
+        ctx.attention(q, k, v, **dict(args, q_ptr=args["q_ptr"].int()))
+    with pytest.raises(TypeError):
+        ctx.attention(q, k, v, **dict(args, k_len=torch.ones(3, dtype=torch.int32, device="cuda")))
+    with pytest.raises(TypeError):
+        ctx.attention_backward(dout[:5], q, k, v, out, saved, **args)
+    with pytest.raises(TypeError):
+        ctx.attention_backward(dout, q, k, v, out, (saved[0][:, :3], saved[1]), **args)
+    refused(b.EUNSUPPORTED, lambda: ctx.attention(q.float(), k.float(), v.float(), **args))
+    odd = torch.zeros(20, 2, 12, dtype=BF, device="cuda")
+    refused(b.EUNSUPPORTED, lambda: ctx.attention(odd, odd, odd))
+    wide = torch.zeros(20, 2, 136, dtype=BF, device="cuda")
+    refused(b.EUNSUPPORTED, lambda: ctx.attention(wide, wide, wide))
+    three = torch.zeros(20, 3, 64, dtype=BF, device="cuda")
+    refused(b.EINVAL, lambda: ctx.attention(q, three, three))
+    refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, cuts=[1, 1, 2])))
+    refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, scale=math.inf)))
+    shifted = torch.zeros(20 * 4 * 64 + 8, dtype=BF, device="cuda")[4:20 * 4 * 64 + 4].view(20, 4, 64)
+    refused(b.EINVAL, lambda: ctx.attention(shifted, k, v, **args))
+    many = torch.zeros(300, 4, device="cuda")
+    refused(b.EUNSUPPORTED, lambda: ctx.attention(q, k, v, **dict(args, bias=many, cuts=list(range(299)))))
+    # the C entry: missing arguments and short workspaces come back as codes, nothing is written
+    lib, n = ctx.lib, None
+    assert lib.gbt_attention(None, n, n, n, n, n, n, n, n, 0) == b.EINVAL
+    assert lib.gbt_attention(ctx.h, n, n, n, n, n, n, n, n, 0) == b.EINVAL
+    p, keep = ctx._attention_params(q, k, args["q_ptr"], args["k_ptr"], None, 20, 20, True, None, args["bias"], args["cuts"])
+    views = [C.byref(b._heads(t, "t", BF)) for t in (dout, q, k, v, out, q, k, v)]
+    need = lib.gbt_attention_backward_workspace_bytes(C.byref(p))
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    dbias = torch.full((4, 4), 3.0, device="cuda")
+    tail = [*views[5:], b._ptr(dbias), b._ptr(ws)]
+    assert lib.gbt_attention_backward(ctx.h, C.byref(p), *views[:5], b._ptr(saved[0]), n, *tail, need - 1) == b.ENOMEM
+    assert lib.gbt_attention_backward(ctx.h, C.byref(p), *views[:5], n, n, *tail, need) == b.EINVAL
+    p.max_q = -1
+    assert lib.gbt_attention_backward_workspace_bytes(C.byref(p)) == 0
+    assert lib.gbt_attention_backward(ctx.h, C.byref(p), *views[:5], b._ptr(saved[0]), n, *tail, need) == b.EINVAL
+    torch.cuda.synchronize()
+    assert bool((dbias == 3.0).all())
+
+
+
+def test_without_what_rounding_took(ctx):
+    """saved without its second part: dk, dv and dbias as exact as ever, dq within the bounds of a delta of the rounded out."""
+    made = _make([80], [80], 2, 2, 64, BF, causal=False, buckets=5, seed=16)
+    q, k, v, dout, args, spans = made
+    ref = _reference(q, k, v, args, spans, dout)
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+    dq, dk, dv, dbias = ctx.attention_backward(dout, q, k, v, out, (saved[0], None), **args)
+    for name, x in (("dk", dk), ("dv", dv), ("dbias", dbias)):
+        close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
+    assert float((dq.cpu().double() - ref.dq).norm() / ref.dq.norm()) < 2.0 ** -7

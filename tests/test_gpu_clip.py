@@ -1,0 +1,181 @@
+"""Clipping by the global norm, against 64-bit sums (-m gpu).
+
+Squares are summed in 64 bits, so the norm is off by its rounding to a float only; a factor of the division and its rounding to 32 bits,
+and a value by one product in 32 bits and one rounding to its type.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = {t: torch.finfo(t).eps / 2 for t in (torch.float32, torch.bfloat16, torch.float16)}
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_1806_11248_amd as g
+    c = g.Context(0)
+    yield c
+    c.close()
+
+
+def _tensors(sizes, seed=0, scale=1.0):
+    rng = torch.Generator().manual_seed(seed)
+    types = [torch.float32, torch.bfloat16, torch.float16]
+    return [(torch.randn(n, generator=rng) * scale).to(types[i % 3]).cuda() for i, n in enumerate(sizes)]
+
+
+def _norm(ts):
+    return math.sqrt(sum(float((t.cpu().double() ** 2).sum()) for t in ts))
+
+
+def _check(ctx, ts, max_norm, outs=None):
+    before = [t.cpu().double() for t in ts]
+    want = _norm(ts)
+    coef = min(1.0, max_norm / (want + 1e-6))
+    lst = ctx.gradient_list(ts, outs)
+    norm = ctx.clip_gradients(lst, max_norm)
+    assert norm.shape == () and abs(float(norm) - want) <= 2.0 ** -23 * want + 1e-30
+    for t, o, x in zip(ts, lst.outs, before):
+        got, y = o.cpu().double(), x * coef
+        tol = 1.001 * U[t.dtype] * y.abs() + 2.0 ** -22 * y.abs() + TINY[t.dtype]
+        assert bool(((got - y).abs() <= tol).all())
+        if coef == 1.0:
+            assert torch.equal(got, x)
+        if o is not t:
+            assert torch.equal(t.cpu().double(), x)
+    return lst, norm
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 1, 0], [7, 8, 9], [2047, 2048, 2049], [100_003, 5, 0, 31, 4096], [1] * 300, [3_000_001, 70_000]])
+@pytest.mark.parametrize("ratio", [0.3, 1.0, 4.0])
+def test_norm_and_values(ctx, sizes, ratio):
+    ts = _tensors(sizes, seed=len(sizes))
+    _check(ctx, [t.clone() for t in ts], ratio * _norm(ts))                       # in place
+    _check(ctx, ts, ratio * _norm(ts), [torch.full_like(t, 9.0) for t in ts])     # into other tensors
+
+
+def test_the_smaller_side_of_the_limit_changes_nothing(ctx):
+    ts = _tensors([1000, 77])
+    keep = [t.clone() for t in ts]
+    ctx.clip_gradients(ctx.gradient_list(ts), 1e9)
+    assert all(torch.equal(a, b) for a, b in zip(ts, keep))
+
+
+def test_empty_lists(ctx):
+    norm = ctx.clip_gradients(ctx.gradient_list([]), 1.0)
+    assert float(norm) == 0.0
+    norm = ctx.clip_gradients(ctx.gradient_list([torch.empty(0, device="cuda")]), 0.0)
+    assert float(norm) == 0.0
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3, 5])
+def test_any_alignment(ctx, shift):
+    """Parts of a flat buffer begin anywhere; the elements before and behind stay as they are."""
+    for dtype in U:
+        flat = torch.randn(20_000, device="cuda").to(dtype)
+        keep = flat.clone()
+        part = flat[shift:shift + 10_001]
+        _check(ctx, [part], 1.0)
+        assert torch.equal(flat[:shift], keep[:shift]) and torch.equal(flat[shift + 10_001:], keep[shift + 10_001:])
+        out = torch.zeros(10_008, device="cuda", dtype=dtype)
+        _check(ctx, [keep[shift:shift + 10_001]], 1.0, [out[:10_001]])            # one aligned, one not
+
+
+def test_extremes(ctx):
+    """Squares beyond a float's range on both sides; a norm that is not finite leaves the values alone."""
+    _check(ctx, [torch.full((5000,), 1e25, device="cuda")], 1.0)
+    _check(ctx, [torch.full((5000,), 1e-30, device="cuda")], 1e-30)
+    for bad in (math.nan, math.inf, -math.inf):
+        t = torch.randn(3000, device="cuda")
+        t[1234] = bad
+        out = torch.zeros_like(t)
+        norm = ctx.clip_gradients(ctx.gradient_list([t], [out]), 1.0)
+        assert not math.isfinite(float(norm)) and torch.equal(torch.nan_to_num(out, 5.0), torch.nan_to_num(t, 5.0))
+    big = torch.full((5000,), 3e38, device="cuda")                                # each finite, the norm is none that a float holds
+    keep = big.clone()
+    norm = ctx.clip_gradients(ctx.gradient_list([big]), 1.0)
+    assert math.isinf(float(norm)) and torch.equal(big, keep)
+
+
+def test_same_result_on_every_run_and_every_call(ctx):
+    ts = _tensors([1_234_567, 999, 40_001], seed=3)
+    outs = [torch.empty_like(t) for t in ts]
+    lst = ctx.gradient_list(ts, outs)
+    first = ctx.clip_gradients(lst, 3.0).clone()
+    keep = [o.clone() for o in outs]
+    for step in range(3):
+        assert torch.equal(ctx.clip_gradients(lst, 3.0), first) and all(torch.equal(a, b) for a, b in zip(outs, keep))
+    for t in ts:
+        t.mul_(0.5)                                                               # new values in the same places
+    assert abs(float(ctx.clip_gradients(lst, 3.0)) - 0.5 * float(first)) <= 2.0 ** -9 * float(first)
+
+
+def test_in_a_graph():
+    import paper_1806_11248_amd as g
+    side = torch.cuda.Stream()
+    own = g.Context(0, stream=side)
+    try:
+        ts = _tensors([50_000, 333])
+        outs = [torch.empty_like(t) for t in ts]
+        side.wait_stream(torch.cuda.current_stream())
+        lst = own.gradient_list(ts, outs)
+        with torch.cuda.stream(side):
+            own.clip_gradients(lst, 1.0)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                norm = own.clip_gradients(lst, 1.0)
+            for step in range(3):
+                for t in ts:
+                    t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(step)).to(t.dtype))
+                graph.replay()
+                side.synchronize()
+                got, got_outs = norm.clone(), [o.clone() for o in outs]
+                assert torch.equal(own.clip_gradients(lst, 1.0), got)
+                side.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(outs, got_outs))
+    finally:
+        own.close()
+
+
+def test_refusals(ctx):
+    import ctypes as C
+    import paper_1806_11248_amd as g
+    b = g.binding
+    t = torch.ones(10, device="cuda")
+    with pytest.raises(TypeError):
+        ctx.gradient_list([t.double()])
+    with pytest.raises(TypeError):
+        ctx.gradient_list([torch.ones(4, 4, device="cuda").t()[:2]])
+    with pytest.raises(TypeError):
+        ctx.gradient_list([t], [t[:5]])
+    with pytest.raises(TypeError):
+        ctx.gradient_list([t], [])
+    lst = ctx.gradient_list([t])
+    for bad in (-1.0, math.nan):
+        with pytest.raises(g.GbtError) as e:
+            ctx.clip_gradients(lst, bad)
+        assert e.value.code == b.EINVAL
+    lib = ctx.lib
+    arr = (b.Gradient * 1)(b.Gradient(t.data_ptr(), t.data_ptr(), 10, 0))
+    need = lib.gbt_gradient_list_bytes(arr, 1)
+    pieces = C.c_int32(77)
+    ws = torch.zeros(16384, dtype=torch.uint8, device="cuda")
+    assert need >= 16
+    assert lib.gbt_gradient_list(None, arr, 1, b._ptr(ws), need, C.byref(pieces)) == b.EINVAL
+    assert lib.gbt_gradient_list(ctx.h, arr, 1, b._ptr(ws), need - 1, C.byref(pieces)) == b.ENOMEM
+    arr[0].dtype = 5
+    assert lib.gbt_gradient_list_bytes(arr, 1) == 0
+    assert lib.gbt_gradient_list(ctx.h, arr, 1, b._ptr(ws), need, C.byref(pieces)) == b.EINVAL
+    arr[0].dtype, arr[0].src = 0, t.data_ptr() + 2
+    assert lib.gbt_gradient_list(ctx.h, arr, 1, b._ptr(ws), need, C.byref(pieces)) == b.EINVAL
+    assert pieces.value == 77
+    assert lib.gbt_clip_gradients(ctx.h, b._ptr(lst.table), -1, 1.0, b._ptr(t), b._ptr(ws), 16384) == b.EINVAL
+    assert lib.gbt_clip_gradients(ctx.h, b._ptr(lst.table), lst.pieces, 1.0, b._ptr(t), b._ptr(ws), 16383) == b.ENOMEM
+    assert lib.gbt_clip_gradients(None, None, 0, 1.0, None, None, 0) == b.EINVAL
+    assert bool((t == 1).all())
