@@ -129,17 +129,19 @@ __device__ __forceinline__ i32x4 load16(const char *base, int64_t byte, bool the
     return z;
 }
 
-// One tile of ROWS rows on its way from memory to LDS, through registers of 256 threads.
+// One tile of ROWS rows on its way from memory to LDS, through registers of 256 threads.  Rows past the last and elements past the head's
+// are taken from the last there are, so no load hangs on a condition: such rows' probabilities are zero, and such elements meet zeros
+// of the other operand or are not stored.
 template <int DP, int ROWS>
 struct TileLoad {
     static constexpr int kChunks = DP / 8, kEach = ROWS * kChunks / 256;
     static_assert(ROWS * kChunks % 256 == 0, "whole chunks for every thread");
     i32x4 reg[kEach];
-    __device__ __forceinline__ void load(const char *base, int64_t row_bytes, int rows, int dim) {
+    __device__ __forceinline__ void load(const char *base, int64_t row_bytes, int rows, int dim) {   // rows, dim > 0
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int at = threadIdx.x + 256 * i, r = at / kChunks, c = at % kChunks;
-            reg[i] = load16(base, r * row_bytes + c * 16, r < rows && c * 8 < dim);
+            reg[i] = *(const i32x4 *)(base + min(r, rows - 1) * row_bytes + min(c, dim / 8 - 1) * 16);
         }
     }
     template <typename E>

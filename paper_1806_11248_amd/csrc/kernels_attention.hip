@@ -12,7 +12,7 @@ namespace {
 // ------------------------------------------------------------------------------------------------ blocks of queries --
 // A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.
 template <typename P, int DP>
-__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a, AttnCuts c) {
+__global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
@@ -64,8 +64,10 @@ __global__ __launch_bounds__(256) void attention_kernel(AttnArgs a, AttnCuts c) 
     float top = -INFINITY, sum = 0.0f;
 
     TileLoad<DP, 64> k_load, v_load;
-    k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
-    v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
+    if (end > 0) {
+        k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
+        v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
+    }
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 

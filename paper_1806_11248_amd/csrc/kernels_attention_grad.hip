@@ -38,7 +38,7 @@ __device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int l
 // ---------------------------------------------------------------------------------------------------------- queries --
 // As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS.
 template <typename P, int DP>
-__global__ __launch_bounds__(256) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
+__global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
@@ -104,8 +104,10 @@ __global__ __launch_bounds__(256) void grad_queries_kernel(AttnArgs a, AttnCuts 
     float row_sum = 0.0f;   // of dS: this lane's half of the column
 
     TileLoad<DP, 64> k_load, v_load;
-    k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
-    v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
+    if (end > 0) {
+        k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
+        v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
+    }
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
@@ -186,7 +188,7 @@ __global__ __launch_bounds__(256) void grad_queries_kernel(AttnArgs a, AttnCuts 
 // Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane.  Others are laid out by
 // diagonals in LDS and added up along them (64 distances, one a lane), and then over each run of lanes of one bucket.
 template <typename P, int DP>
-__global__ __launch_bounds__(256) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
+__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
