@@ -525,7 +525,8 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
  * sequence depends on elements outside its own rows.
  *
  * Rows of q, k and v may be any distance apart (parts of one fused projection, slots of a store): strides are in
- * elements, multiples of 8, as head_dim; data is 16-byte aligned; a head's elements lie side by side.
+ * elements, multiples of 8, as head_dim, rows less than 2^24 apart; data is 16-byte aligned; a head's elements
+ * lie side by side.
  */
 #define GBT_F32 0
 #define GBT_BF16 1

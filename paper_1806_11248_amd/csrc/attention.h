@@ -80,11 +80,6 @@ __device__ __forceinline__ V as_vec(i32x4 x) {
     return __builtin_bit_cast(V, x);
 }
 
-// Rows of a tile lie `pitch` elements apart in LDS: head_dim and a pad with which both kinds of read (sixteen bytes of 32 rows;
-// 64 bytes of eight rows, transposed) meet every bank equally often.
-template <int DP>
-constexpr int attn_pitch() { return DP + (DP % 64 == 0 && DP != 64 ? 16 : DP == 32 ? 16 : 8); }
-
 struct AttnSeq {
     int64_t q0, k0;
     int nq, nk;
@@ -129,48 +124,61 @@ __device__ __forceinline__ i32x4 load16(const char *base, int64_t byte, bool the
     return z;
 }
 
-// One tile of ROWS rows on its way from memory to LDS, through registers of 256 threads.  Rows past the last and elements past the head's
-// are taken from the last there are, so no load hangs on a condition: such rows' probabilities are zero, and such elements meet zeros
-// of the other operand or are not stored.
-template <int DP, int ROWS>
-struct TileLoad {
-    static constexpr int kChunks = DP / 8, kEach = ROWS * kChunks / 256;
-    static_assert(ROWS * kChunks % 256 == 0, "whole chunks for every thread");
-    i32x4 reg[kEach];
-    __device__ __forceinline__ void load(const char *base, int64_t row_bytes, int rows, int dim) {   // rows, dim > 0
+// A tile of 64 rows in LDS.  A row's sixteen-byte pieces are stored in an order of its own, piece c at place c ^ fold(row), with which both
+// kinds of read meet each of the 64 banks once a clock: sixteen bytes of sixteen rows, and 64 bytes of four rows (transposed).  Measured, a
+// compute unit reads 219 to 235 bytes a clock so; with rows 16 or 32 bytes further apart instead, 122 to 125 by one kind of read or both.
+template <int DP>
+struct Tile {
+    static constexpr int kRowBytes = DP == 96 ? 256 : DP * 2, kPlaces = kRowBytes / 16, kBytes = 64 * kRowBytes, kLoads = kPlaces / 4;
+    static __device__ __forceinline__ constexpr int fold(int row) {
+        return kPlaces == 4 ? (row >> 2) & 3 : kPlaces == 8 ? ((row >> 1) & 1) * 4 | ((row >> 2) & 3) : (row & 3) * 4 | ((row >> 2) & 3);
+    }
+    // From memory straight into LDS, a wave's 64 pieces at a time; 256 threads.  Rows past the last and elements past the head's are taken from
+    // the last there are, so that nothing hangs on a condition: such rows' probabilities are zero, and such elements meet zeros of the
+    // other operand or are not stored.  rows, dim > 0; 64 * row_bytes < 2^32.
+    static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim) {
+        typedef const __attribute__((address_space(1))) void gvoid;
+        typedef __attribute__((address_space(3))) void lvoid;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        constexpr int kRows = 64 / kPlaces;                       // of a wave's load
+        const int row = wave * kRows + lane / kPlaces;            // the i-th load's is 4 * kRows further, with the same fold
+        const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;
+        char *to = tile + wave * 1024;
+        if (rows >= 64) {
+            const uint32_t at = row * row_bytes + col;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + 256 * i, r = at / kChunks, c = at % kChunks;
-            reg[i] = *(const i32x4 *)(base + min(r, rows - 1) * row_bytes + min(c, dim / 8 - 1) * 16);
+            for (int i = 0; i < kLoads; ++i)
+                __builtin_amdgcn_global_load_lds((gvoid *)(base + (uint64_t)(i * 4 * kRows) * row_bytes + at), (lvoid *)(to + i * 4096), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                __builtin_amdgcn_global_load_lds((gvoid *)(base + (min(row + i * 4 * kRows, rows - 1) * row_bytes + col)), (lvoid *)(to + i * 4096), 16, 0, 0);
         }
     }
-    template <typename E>
-    __device__ __forceinline__ void store(E *tile) const {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = threadIdx.x + 256 * i, r = at / kChunks, c = at % kChunks;
-            *(i32x4 *)(tile + r * attn_pitch<DP>() + c * 8) = reg[i];
-        }
+    // First operand, rows as they are: row row0 + lane % 32 (row0 a multiple of 32), elements 16 * step + 8 * (lane / 32) .. + 7.
+    template <typename P>
+    static __device__ __forceinline__ typename P::vec8 rows(const char *tile, int row0, int step, int lane) {
+        const int row = lane & 31, mine = row * kRowBytes + (((lane >> 5) ^ fold(row)) << 4);
+        return *(const typename P::vec8 *)(tile + row0 * kRowBytes + (mine ^ (step << 5)));
+    }
+    // First operand, the tile transposed: row d = 32 * block + lane % 32, over the sixteen tile rows row0 .. row0 + 15 (row0 a multiple of 16)
+    // in the order that a result's registers have (see above).
+    template <typename P>
+    static __device__ __forceinline__ typename P::vec8 cols(const char *tile, int row0, int block, int lane) {
+        const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        const int lo_at = row * kRowBytes + ((piece ^ fold(row)) << 4) + 8 * (lane & 1);
+        const int hi_at = (row + 8) * kRowBytes + ((piece ^ fold(row + 8)) << 4) + 8 * (lane & 1);
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + row0 * kRowBytes + (lo_at ^ (block << 6))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + row0 * kRowBytes + (hi_at ^ (block << 6))));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(typename P::vec8, both);
     }
 };
-
-// First operand, rows of the tile as they are: row `row0 + lane % 32`, elements 16 * step + 8 * (lane / 32) .. + 7.
-template <typename P, int DP>
-__device__ __forceinline__ typename P::vec8 tile_rows(const typename P::elem *tile, int row0, int step, int lane) {
-    return *(const typename P::vec8 *)(tile + (row0 + (lane & 31)) * attn_pitch<DP>() + 16 * step + 8 * (lane >> 5));
-}
-
-// First operand, the tile transposed: row d = 32 * block + lane % 32, over the sixteen tile rows row0 .. row0 + 15 in the order
-// that a result's registers have (see above).
-template <typename P, int DP>
-__device__ __forceinline__ typename P::vec8 tile_cols(const typename P::elem *tile, int row0, int block, int lane) {
-    const int p = lane & 15;
-    const typename P::elem *at = tile + (row0 + 4 * (lane >> 5) + (p >> 2)) * attn_pitch<DP>() + 32 * block + 16 * ((lane >> 4) & 1) + 4 * (p & 3);
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * attn_pitch<DP>()));
-    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(typename P::vec8, both);
+// Waits for this wave's fetches, then for the other waves: the tiles fetched last can be read, and those read before written.
+__device__ __forceinline__ void tiles_ready() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    __syncthreads();
 }
 
 // Second operand from eight registers of a result, rounded to the inputs' type (to nearest, ties to even).

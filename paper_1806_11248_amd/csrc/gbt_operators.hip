@@ -59,12 +59,12 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
 
 bool view_ok(const gbt_heads *h) {
     return h && ((uintptr_t)h->data & 15u) == 0 && h->row_stride >= 0 && h->head_stride >= 0 && h->row_stride % 8 == 0 && h->head_stride % 8 == 0 &&
-           h->row_stride < ((int64_t)1 << 40) && h->head_stride < ((int64_t)1 << 40);
+           h->row_stride < ((int64_t)1 << 24) && h->head_stride < ((int64_t)1 << 40);
 }
 AttnView view(const gbt_heads *h) { return AttnView{(char *)h->data, h->row_stride, h->head_stride}; }
 
 #define GBT_VIEW(ctx, h, rows)                                                                                                        \
-    GBT_REQUIRE(ctx, view_ok(h), GBT_EINVAL, #h ": NULL, not 16-byte aligned, or strides that are negative or no multiples of 8");    \
+    GBT_REQUIRE(ctx, view_ok(h), GBT_EINVAL, #h ": NULL, not 16-byte aligned, or strides that are negative, no multiples of 8 or (rows) 2^24 and more");    \
     GBT_REQUIRE(ctx, (h)->data || (rows) == 0, GBT_EINVAL, #h ": data is NULL")
 
 void fill(AttnArgs &a, AttnCuts &c, const gbt_attention_params &p) {

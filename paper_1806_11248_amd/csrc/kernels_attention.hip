@@ -15,9 +15,10 @@ template <typename P, int DP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
-    __shared__ __align__(16) E k_tile[64 * kPitch];
-    __shared__ __align__(16) E v_tile[64 * kPitch];
+    typedef Tile<DP> T;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    __shared__ __align__(16) char k_tile[2][T::kBytes];
+    __shared__ __align__(16) char v_tile[2][T::kBytes];
     __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
 
@@ -63,23 +64,18 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
 
-    TileLoad<DP, 64> k_load, v_load;
-    if (end > 0) {
-        k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
-        v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
-    }
+    auto fetch = [&](int kb) {
+        T::fetch(k_tile[(kb >> 6) & 1], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
+        T::fetch(v_tile[(kb >> 6) & 1], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+    };
+    if (end > 0) fetch(0);
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
     for (int kb = 0; kb < end; kb += 64) {
-        __syncthreads();   // the tile before has been read
-        k_load.store(k_tile);
-        v_load.store(v_tile);
-        __syncthreads();
-        if (kb + 64 < end) {
-            k_load.load(k_base + (int64_t)(kb + 64) * a.k.row * 2, a.k.row * 2, min(64, end - kb - 64), a.dim);
-            v_load.load(v_base + (int64_t)(kb + 64) * a.v.row * 2, a.v.row * 2, min(64, end - kb - 64), a.dim);
-        }
+        tiles_ready();
+        if (kb + 64 < end) fetch(kb + 64);
+        const char *k_now = k_tile[(kb >> 6) & 1], *v_now = v_tile[(kb >> 6) & 1];
         const int lowest = kb - (first + 127 + off);   // distance
         if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest + 191 + lane);
         if (kb >= wave_end) continue;
@@ -90,7 +86,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(tile_rows<P, DP>(k_tile, 32 * b, i, lane), qf[i], s[b]);
+            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s[b]);
         }
         // scores in powers of two
         const int at = (lowest & 255) + 96 - 32 * wave;   // of the wave's lowest distance, of 95
@@ -141,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         for (int i = 0; i < 4; ++i) {
             const V8 p = operand<P>(s[i / 2], i % 2);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(tile_cols<P, DP>(v_tile, 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_now, 16 * i, b, lane), p, o[b]);
         }
     }
 
@@ -181,8 +177,9 @@ template <typename P, int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>(), kChunks = DP / 8, kEach = 32 * kChunks / 64;
-    __shared__ __align__(16) E v_tile[4][32 * kPitch];
+    typedef Tile<DP> T;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kChunks = DP / 8, kEach = 32 * kChunks / 64;
+    __shared__ __align__(16) char v_tile[4][T::kBytes / 2];
     __shared__ int cut[kAttnBuckets];
     __shared__ int near_bucket[4][64];
     __shared__ float join_top[4][32], join_sum[4][32];
@@ -254,7 +251,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int at = lane + 64 * i, r = at / kChunks, ch = at % kChunks;
-            *(i32x4 *)(v_tile[wave] + r * kPitch + ch * 8) = v_reg[i];
+            *(i32x4 *)(v_tile[wave] + r * T::kRowBytes + ((ch ^ T::fold(r)) << 4)) = v_reg[i];
         }
         __builtin_amdgcn_wave_barrier();
         if (kb + 128 < end) load(kb + 128);
@@ -306,7 +303,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
         for (int i = 0; i < 2; ++i) {
             const V8 p = operand<P>(s, i);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(tile_cols<P, DP>(v_tile[wave], 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile[wave], 16 * i, b, lane), p, o[b]);
         }
     }
 

@@ -41,9 +41,10 @@ template <typename P, int DP>
 __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
-    __shared__ __align__(16) E k_tile[64 * kPitch];
-    __shared__ __align__(16) E v_tile[64 * kPitch];
+    typedef Tile<DP> T;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    __shared__ __align__(16) char k_tile[2][T::kBytes];
+    __shared__ __align__(16) char v_tile[2][T::kBytes];
     __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
 
@@ -103,23 +104,18 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
         for (int r = 0; r < 16; ++r) dq[b][r] = 0.0f;
     float row_sum = 0.0f;   // of dS: this lane's half of the column
 
-    TileLoad<DP, 64> k_load, v_load;
-    if (end > 0) {
-        k_load.load(k_base, a.k.row * 2, min(64, end), a.dim);
-        v_load.load(v_base, a.v.row * 2, min(64, end), a.dim);
-    }
+    auto fetch = [&](int kb) {
+        T::fetch(k_tile[(kb >> 6) & 1], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
+        T::fetch(v_tile[(kb >> 6) & 1], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+    };
+    if (end > 0) fetch(0);
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
     for (int kb = 0; kb < end; kb += 64) {
-        __syncthreads();
-        k_load.store(k_tile);
-        v_load.store(v_tile);
-        __syncthreads();
-        if (kb + 64 < end) {
-            k_load.load(k_base + (int64_t)(kb + 64) * a.k.row * 2, a.k.row * 2, min(64, end - kb - 64), a.dim);
-            v_load.load(v_base + (int64_t)(kb + 64) * a.v.row * 2, a.v.row * 2, min(64, end - kb - 64), a.dim);
-        }
+        tiles_ready();
+        if (kb + 64 < end) fetch(kb + 64);
+        const char *k_now = k_tile[(kb >> 6) & 1], *v_now = v_tile[(kb >> 6) & 1];
         const int lowest = kb - (first + 127 + off);
         if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest + 191 + lane);
         if (kb >= wave_end) continue;
@@ -133,8 +129,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                s = P::mma(tile_rows<P, DP>(k_tile, 32 * b, i, lane), qf[i], s);
-                dp = P::mma(tile_rows<P, DP>(v_tile, 32 * b, i, lane), gf[i], dp);
+                s = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s);
+                dp = P::mma(T::template rows<P>(v_now, 32 * b, i, lane), gf[i], dp);
             }
             if (b0 == b1) {
                 const float add = (bias ? buckets.value[b0] : 0.0f) + minus;
@@ -158,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             for (int i = 0; i < 2; ++i) {
                 const V8 ds = operand<P>(s, i);
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(tile_cols<P, DP>(k_tile, 32 * b + 16 * i, d, lane), ds, dq[d]);
+                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(T::template cols<P>(k_now, 32 * b + 16 * i, d, lane), ds, dq[d]);
             }
         }
     }
@@ -191,10 +187,11 @@ template <typename P, int DP>
 __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kPitch = attn_pitch<DP>();
-    __shared__ __align__(16) E q_tile[64 * kPitch];
-    __shared__ __align__(16) E g_tile[64 * kPitch];
-    __shared__ __align__(16) float row_minus[64], row_delta[64];
+    typedef Tile<DP> T;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    __shared__ __align__(16) char q_tile[2][T::kBytes];
+    __shared__ __align__(16) char g_tile[2][T::kBytes];
+    __shared__ __align__(16) float row_minus[2][64], row_delta[2][64];
     __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
     __shared__ BucketSums sums;
@@ -246,7 +243,6 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
     const int wave_all = a.causal ? first + wave * 32 + 31 - off : 0;  // and all of them
     const bool wave_last = first + wave * 32 + 32 > rows.nk;           // some of the wave's keys do not exist
 
-    TileLoad<DP, 64> q_load, g_load;
     for (int g = 0; g < a.group; ++g) {
         const int head = kv_head * a.group + g;
         const char *q_base = a.q.data + (rows.q0 * a.q.row + (int64_t)head * a.q.head) * 2;
@@ -259,27 +255,25 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
             buckets_load_values(buckets, a, head);
             for (int i = threadIdx.x; i < 4 * kAttnBuckets; i += 256) (&sums.at[0][0])[i] = 0.0f;
         }
-        if (start < rows.nq) {
-            q_load.load(q_base + (int64_t)start * a.q.row * 2, a.q.row * 2, min(64, rows.nq - start), a.dim);
-            g_load.load(g_base + (int64_t)start * a.dout.row * 2, a.dout.row * 2, min(64, rows.nq - start), a.dim);
-        }
-        __syncthreads();
-        if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (start + 63 + off));
-        for (int qb = start; qb < rows.nq; qb += 64) {
-            __syncthreads();
-            q_load.store(q_tile);
-            g_load.store(g_tile);
+        auto fetch = [&](int qb) {
+            const int n = (qb >> 6) & 1;
+            T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim);
+            T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim);
             if (threadIdx.x < 64) {
                 const int q = qb + threadIdx.x;
                 const float l = q < rows.nq ? lse[q] : -INFINITY;
-                row_minus[threadIdx.x] = l == -INFINITY ? -INFINITY : -l * GBT_LOG2E;   // no query, or one that saw no key
-                row_delta[threadIdx.x] = q < rows.nq ? delta[q] : 0.0f;
+                row_minus[n][threadIdx.x] = l == -INFINITY ? -INFINITY : -l * GBT_LOG2E;   // no query, or one that saw no key
+                row_delta[n][threadIdx.x] = q < rows.nq ? delta[q] : 0.0f;
             }
-            __syncthreads();
-            if (qb + 64 < rows.nq) {
-                q_load.load(q_base + (int64_t)(qb + 64) * a.q.row * 2, a.q.row * 2, min(64, rows.nq - qb - 64), a.dim);
-                g_load.load(g_base + (int64_t)(qb + 64) * a.dout.row * 2, a.dout.row * 2, min(64, rows.nq - qb - 64), a.dim);
-            }
+        };
+        if (start < rows.nq) fetch(start);
+        __syncthreads();
+        if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (start + 63 + off));
+        for (int qb = start; qb < rows.nq; qb += 64) {
+            tiles_ready();
+            if (qb + 64 < rows.nq) fetch(qb + 64);
+            const int now = (qb >> 6) & 1;
+            const char *q_now = q_tile[now], *g_now = g_tile[now];
             const int lowest = first - (qb + 63 + off);
             if (bias && wave == ((qb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest - 64 + lane);
 #pragma unroll
@@ -292,13 +286,13 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                 for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    s = P::mma(tile_rows<P, DP>(q_tile, 32 * b, i, lane), kf[i], s);
-                    dp = P::mma(tile_rows<P, DP>(g_tile, 32 * b, i, lane), vf[i], dp);
+                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, lane), kf[i], s);
+                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, lane), vf[i], dp);
                 }
                 f32x16 minus, del;
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
-                    const f32x4 m = *(const f32x4 *)(row_minus + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_delta + 32 * b + 8 * r4 + 4 * half);
+                    const f32x4 m = *(const f32x4 *)(row_minus[now] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_delta[now] + 32 * b + 8 * r4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         minus[4 * r4 + e] = m[e];
@@ -350,8 +344,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                     const V8 p = operand<P>(s, i), ds = operand<P>(dp, i);
 #pragma unroll
                     for (int d = 0; d < kBlocks; ++d) {
-                        dv[d] = P::mma(tile_cols<P, DP>(g_tile, 32 * b + 16 * i, d, lane), p, dv[d]);
-                        dk[d] = P::mma(tile_cols<P, DP>(q_tile, 32 * b + 16 * i, d, lane), ds, dk[d]);
+                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, lane), p, dv[d]);
+                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, lane), ds, dk[d]);
                     }
                 }
             }
