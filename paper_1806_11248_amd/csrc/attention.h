@@ -124,6 +124,16 @@ __device__ __forceinline__ i32x4 load16(const char *base, int64_t byte, bool the
     return z;
 }
 
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+// Sixteen bytes for each lane from base + offset (base and `to` the same in all lanes) to LDS, the lanes' side by side from `to` on.  It has no
+// result in registers; tiles_ready() waits for it.  Not the builtin: with that one the compiler waits for every load under way before LDS reads
+// that it cannot tell apart from the loads' targets, and so for the next tile before it reads this one.
+__device__ __forceinline__ void load_to_lds(uint32_t to, const char *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+
 // A tile of 64 rows in LDS.  A row's sixteen-byte pieces are stored in an order of its own, piece c at place c ^ fold(row), with which both
 // kinds of read meet each of the 64 banks once a clock: sixteen bytes of sixteen rows, and 64 bytes of four rows (transposed).  Measured, a
 // compute unit reads 219 to 235 bytes a clock so; with rows 16 or 32 bytes further apart instead, 122 to 125 by one kind of read or both.
@@ -137,22 +147,20 @@ struct Tile {
     // the last there are, so that nothing hangs on a condition: such rows' probabilities are zero, and such elements meet zeros of the
     // other operand or are not stored.  rows, dim > 0; 64 * row_bytes < 2^32.
     static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim) {
-        typedef const __attribute__((address_space(1))) void gvoid;
-        typedef __attribute__((address_space(3))) void lvoid;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
         constexpr int kRows = 64 / kPlaces;                       // of a wave's load
         const int row = wave * kRows + lane / kPlaces;            // the i-th load's is 4 * kRows further, with the same fold
         const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;
-        char *to = tile + wave * 1024;
+        const uint32_t to = lds_address(tile) + wave * 1024;
         if (rows >= 64) {
             const uint32_t at = row * row_bytes + col;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                __builtin_amdgcn_global_load_lds((gvoid *)(base + (uint64_t)(i * 4 * kRows) * row_bytes + at), (lvoid *)(to + i * 4096), 16, 0, 0);
+                load_to_lds(to + i * 4096, base + (uint64_t)(i * 4 * kRows) * row_bytes, at);
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                __builtin_amdgcn_global_load_lds((gvoid *)(base + (min(row + i * 4 * kRows, rows - 1) * row_bytes + col)), (lvoid *)(to + i * 4096), 16, 0, 0);
+                load_to_lds(to + i * 4096, base, min(row + i * 4 * kRows, rows - 1) * row_bytes + col);
         }
     }
     // First operand, rows as they are: row row0 + lane % 32 (row0 a multiple of 32), elements 16 * step + 8 * (lane / 32) .. + 7.
@@ -175,9 +183,15 @@ struct Tile {
         return __builtin_bit_cast(typename P::vec8, both);
     }
 };
+// The compiler waits for loaded registers where they are first used, and inside a loop for everything under way.  Done with them here.
+template <typename V, int N>
+__device__ __forceinline__ void arrived(V (&regs)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(regs[i]));
+}
 // Waits for this wave's fetches, then for the other waves: the tiles fetched last can be read, and those read before written.
 __device__ __forceinline__ void tiles_ready() {
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 }
 
@@ -242,6 +256,17 @@ __device__ __forceinline__ void ring_put(DistanceRing &ring, const Buckets &b, i
     ring.value[at + 256] = v;
     ring.bucket[at] = n;
     ring.bucket[at + 256] = n;
+}
+
+// The 64 distances from t0 on, by one wave.  Beyond the first or the last cut there is nothing to search.
+__device__ __forceinline__ void ring_next(DistanceRing &ring, const Buckets &b, const AttnCuts &c, int n_buckets, int t0, int lane) {
+    if (t0 + 63 >= c.at[0] && (n_buckets < 2 || t0 < c.at[n_buckets - 2])) {
+        ring_put(ring, b, c.steps, t0 + lane);
+    } else {
+        const int n = t0 + 63 < c.at[0] ? 0 : n_buckets - 1, at = (t0 + lane) & 255;
+        ring.value[at] = ring.value[at + 256] = b.value[n];
+        ring.bucket[at] = ring.bucket[at + 256] = n;
+    }
 }
 
 }  // namespace

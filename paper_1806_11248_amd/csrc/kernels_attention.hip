@@ -2,12 +2,18 @@
 //
 //   S_ij = scale * q_i . k_j + bias[b(t)][h],  t = j - (i + nk - nq);   out_i = sum_j softmax_j(S_ij) v_j
 //
-// One pass over the keys with a running maximum and sum: out is kept as sum_j 2^(s_ij - m) v_j and scaled when m grows.
+// One pass over the keys with a running maximum and sum: out is kept as sum_j 2^(s_ij - m) v_j.  m follows the row's maximum only when
+// that has grown by more than kSlack: some row of a wave meets a new maximum in most tiles, but seldom one that much larger, and a factor of
+// 2^kSlack more or less matters to no 32-bit sum and to no rounding of a probability.
 // Sums, maxima and out are held in 32 bits; the probabilities are rounded to the inputs' type for the second product, while their
 // sum is taken of the unrounded ones (the rounding errors of a row then average out in out, whose own last place is of that size).
 #include "attention.h"
 
+#include <type_traits>
+
 namespace {
+
+constexpr float kSlack = 8.0f;
 
 // ------------------------------------------------------------------------------------------------ blocks of queries --
 // A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.
@@ -64,21 +70,23 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
 
-    auto fetch = [&](int kb) {
-        T::fetch(k_tile[(kb >> 6) & 1], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
-        T::fetch(v_tile[(kb >> 6) & 1], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+    auto fetch = [&](int which, int kb) {
+        T::fetch(k_tile[which], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
+        T::fetch(v_tile[which], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
     };
-    if (end > 0) fetch(0);
+    if (end > 0) fetch(0, 0);
+    arrived(qf);
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
-    for (int kb = 0; kb < end; kb += 64) {
+    // one tile; which of the two copies it lies in is known at compile time, so that LDS addresses are constants of the lane
+    auto step = [&](auto which, int kb) {
+        constexpr int kNow = decltype(which)::value;
         tiles_ready();
-        if (kb + 64 < end) fetch(kb + 64);
-        const char *k_now = k_tile[(kb >> 6) & 1], *v_now = v_tile[(kb >> 6) & 1];
+        if (kb + 64 < end) fetch(1 - kNow, kb + 64);
         const int lowest = kb - (first + 127 + off);   // distance
-        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest + 191 + lane);
-        if (kb >= wave_end) continue;
+        if (bias && wave == ((kb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest + 191, lane);
+        if (kb >= wave_end) return;
 
         f32x16 s[2];
 #pragma unroll
@@ -86,23 +94,21 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s[b]);
+            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s[b]);
         }
-        // scores in powers of two
+        // scores in powers of two are s * factor + add
         const int at = (lowest & 255) + 96 - 32 * wave;   // of the wave's lowest distance, of 95
         const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;
-        if (b0 == b1) {
-            const float add = bias ? buckets.value[b0] : 0.0f;
+        float factor = a.scale2, add = 0.0f;
+        if (b0 != b1) {
+            const float *value = ring.value + at + 31 - (lane & 31);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, add);
-        } else {
-            const float *add = ring.value + at + 31 - (lane & 31);
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, add[32 * b + result_row(r, half)]);
+                for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, value[32 * b + result_row(r, half)]);
+            factor = 1.0f;
+        } else if (bias) {
+            add = buckets.value[b0];
         }
         if (kb + 64 > wave_all) {
 #pragma unroll
@@ -110,15 +116,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[b][r] = kb + 32 * b + result_row(r, half) <= last ? s[b][r] : -INFINITY;
         }
-        float now = top;
+        float now = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) now = fmaxf(now, s[b][r]);
-        now = column_max(now);
-        const float base = now == -INFINITY ? 0.0f : now;   // a row that has seen nothing yet
-        if (__any(now > top)) {
-            const float shrink = __builtin_amdgcn_exp2f(top - base);
+        now = fmaxf(top, column_max(fmaf(now, factor, add)));
+        if (__any(now > top + kSlack)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.0f : now));
             sum *= shrink;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -126,19 +131,24 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
                 for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
             top = now;
         }
+        add -= top == -INFINITY ? 0.0f : top;   // a row that has seen nothing yet
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - base);
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], factor, add));
                 sum += s[b][r];
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const V8 p = operand<P>(s[i / 2], i % 2);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_now, 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile[kNow], 16 * i, b, lane), p, o[b]);
         }
+    };
+    for (int kb = 0; kb < end; kb += 128) {
+        step(std::integral_constant<int, 0>{}, kb);
+        if (kb + 64 < end) step(std::integral_constant<int, 1>{}, kb + 64);
     }
 
     sum = column_sum(sum);
@@ -284,9 +294,8 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
 #pragma unroll
         for (int r = 0; r < 16; ++r) now = fmaxf(now, s[r]);
         now = column_max(now);
-        const float base = now == -INFINITY ? 0.0f : now;
-        if (__any(now > top)) {
-            const float shrink = __builtin_amdgcn_exp2f(top - base);
+        if (__any(now > top + kSlack)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.0f : now));
             sum *= shrink;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -294,6 +303,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
                 for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
             top = now;
         }
+        const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             s[r] = __builtin_amdgcn_exp2f(s[r] - base);

@@ -109,6 +109,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
         T::fetch(v_tile[(kb >> 6) & 1], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
     };
     if (end > 0) fetch(0);
+    arrived(qf);
+    arrived(gf);
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
@@ -267,6 +269,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
             }
         };
         if (start < rows.nq) fetch(start);
+        arrived(kf);
+        arrived(vf);
         __syncthreads();
         if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (start + 63 + off));
         for (int qb = start; qb < rows.nq; qb += 64) {
