@@ -90,12 +90,19 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 
         f32x16 s[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+        for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s[b] = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s[b]);
+            for (int b = 0; b < 2; ++b) s[b] = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s[b]);
+        // reads a few products ahead
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < kSteps - 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         // scores in powers of two are s * factor + add
         const int at = (lowest & 255) + 96 - 32 * wave;   // of the wave's lowest distance, of 95
         const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;
