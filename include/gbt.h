@@ -547,7 +547,7 @@ typedef struct gbt_attention_params {
     int32_t max_q, max_k;        /* no sequence is longer (rows beyond are not used) */
     int32_t causal;
     int32_t n_buckets;           /* 0 (no bias) .. 256 */
-    float scale;
+    float scale;                 /* 1e-6..1e6 */
     int64_t q_rows, k_rows;      /* rows of the q and k tensors; rows of a sequence that lie outside do not exist */
     const int64_t *q_ptr;        /* [dev] int64[n_seq + 1]; NULL: sequence s has rows s * max_q .. (s + 1) * max_q */
     const int64_t *k_ptr;        /* [dev] int64[n_seq + 1]; NULL: the same with max_k */

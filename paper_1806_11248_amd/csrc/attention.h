@@ -30,11 +30,13 @@ struct AttnArgs {
     char *rest;                     // what rounding took from out, [q_rows][heads][dim], or NULL
     // backward
     AttnView dout, dq, dk, dv;
-    float *delta;                   // [heads][q_rows]
-    float *strips;                  // [heads][n_seq * k_blocks][n_buckets]: the bias gradient of each block of keys
+    float *row_start;               // [heads][q_rows]: what a row's products with the keys are added to, -lse / scale (-inf: a row without keys)
+    float *row_minus;               // [heads][q_rows]: and its products of gradients with values, -delta
+    float *strips;                  // [heads][n_seq * k_blocks * q_parts][n_buckets]: the bias gradient of each block of keys
     float *dbias;                   // [n_buckets][heads]
-    // few rows
-    float *part;                    // partial results of the pieces of the key axis
+    int head_parts, q_parts;        // a block of keys is shared by so many workgroups: by heads of the group, by queries
+    // partial results: few rows' of the pieces of the key axis; keys' gradients [head_parts * q_parts][2][k_rows][kv_heads][dim]
+    float *part;
     int pieces, piece_len;
 };
 
@@ -132,6 +134,11 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
 // that it cannot tell apart from the loads' targets, and so for the next tile before it reads this one.
 __device__ __forceinline__ void load_to_lds(uint32_t to, const char *base, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+
+// Four bytes for each lane likewise.
+__device__ __forceinline__ void load_word_to_lds(uint32_t to, const float *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // A tile of 64 rows in LDS.  A row's sixteen-byte pieces are stored in an order of its own, piece c at place c ^ fold(row), with which both

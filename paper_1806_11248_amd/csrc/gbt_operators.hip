@@ -39,7 +39,7 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
     if (p.n_seq < 0 || p.max_q < 0 || p.max_k < 0 || p.max_q > (1 << 29) || p.max_k > (1 << 29)) return "n_seq, max_q or max_k out of range";
     if (p.q_rows < 0 || p.k_rows < 0) return "q_rows or k_rows < 0";
     if (p.n_buckets < 0) return "n_buckets < 0";
-    if (!(p.scale - p.scale == 0.0f)) return "scale is not finite";
+    if (!(p.scale >= 1e-6f && p.scale <= 1e6f)) return "scale outside 1e-6..1e6";
     if (p.n_seq > 0 && !p.q_ptr && p.q_rows / p.n_seq < p.max_q) return "q_rows < n_seq * max_q without q_ptr";
     if (p.n_seq > 0 && !p.k_ptr && p.k_rows / p.n_seq < p.max_k) return "k_rows < n_seq * max_k without k_ptr";
     if (p.n_buckets > 0) {
@@ -51,7 +51,7 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
     }
     const int64_t limit = (int64_t)1 << 30;   // workgroups of a launch
     const FewPlan f = few_plan(p);
-    if (std::max(blocks_of(p.max_q) * p.heads, blocks_of(p.max_k) * p.kv_heads) > limit / std::max(1, p.n_seq) ||
+    if (std::max(blocks_of(p.max_q) * p.heads, (p.max_k + 15) / 16 * (int64_t)p.kv_heads) > limit / std::max(1, p.n_seq) ||
         f.columns * p.kv_heads > limit / std::max(1, p.n_seq))
         return "too many sequences";
     return nullptr;
@@ -142,18 +142,41 @@ extern "C" int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *param
 }
 
 namespace {
-size_t backward_layout(const gbt_attention_params &p, size_t *strips_at) {
-    const size_t delta = gbt_align((size_t)p.heads * p.q_rows * sizeof(float));
-    *strips_at = delta;
-    return delta + gbt_align((size_t)p.heads * p.n_seq * blocks_of(p.max_k) * p.n_buckets * sizeof(float));
+
+// Workgroups that a block of keys is shared by: its heads' queries one after the other are all the work there is, so where blocks are few they
+// go to several workgroups, head by head first (the tiles of queries are then not cut), and never less than four tiles each.
+constexpr int64_t kKeyWorkgroups = 768;
+struct KeyParts {
+    int heads, queries;
+};
+KeyParts key_parts(const gbt_attention_params &p) {
+    const int group = p.heads / p.kv_heads;
+    const int64_t base = std::max<int64_t>(1, blocks_of(p.max_k) * p.kv_heads * p.n_seq), want = std::max<int64_t>(1, kKeyWorkgroups / base);
+    KeyParts k;
+    k.heads = (int)std::min<int64_t>(want, group);
+    k.queries = (int)std::min<int64_t>(std::max<int64_t>(1, want / k.heads), std::max(1, p.max_q / 256));
+    return k;
+}
+struct BackwardLayout {
+    size_t row_minus, strips, part, bytes;
+};
+BackwardLayout backward_layout(const gbt_attention_params &p) {
+    const KeyParts k = key_parts(p);
+    const size_t row = gbt_align((size_t)p.heads * p.q_rows * sizeof(float));
+    BackwardLayout l;
+    l.row_minus = row;
+    l.strips = l.row_minus + row;
+    l.part = l.strips + gbt_align((size_t)p.heads * p.n_seq * blocks_of(p.max_k) * k.queries * p.n_buckets * sizeof(float));
+    const int parts = k.heads * k.queries;
+    l.bytes = l.part + (parts > 1 ? gbt_align((size_t)parts * 2 * p.k_rows * p.kv_heads * p.head_dim * sizeof(float)) : 0);
+    return l;
 }
 }  // namespace
 
 extern "C" size_t gbt_attention_backward_workspace_bytes(const gbt_attention_params *params) {
     int32_t code;
-    size_t at;
     if (!params || params_fault(*params, &code)) return 0;
-    return backward_layout(*params, &at);
+    return backward_layout(*params).bytes;
 }
 
 extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_params *params, const gbt_heads *dout, const gbt_heads *q, const gbt_heads *k,
@@ -177,8 +200,8 @@ extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_para
     GBT_REQUIRE(ctx, dbias_out || p.n_buckets == 0, GBT_EINVAL, "dbias_out is NULL");
     GBT_REQUIRE(ctx, ((uintptr_t)rest & 15u) == 0 && (((uintptr_t)lse | (uintptr_t)dbias_out) & 3u) == 0, GBT_EINVAL,
                 "rest, lse or dbias_out is not aligned");
-    size_t strips_at;
-    const size_t need = backward_layout(p, &strips_at);
+    const BackwardLayout l = backward_layout(p);
+    const size_t need = l.bytes;
     GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
     GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     GBT_REQUIRE(ctx, ((uintptr_t)workspace & 15u) == 0, GBT_EINVAL, "workspace is not 16-byte aligned");
@@ -195,8 +218,13 @@ extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_para
     a.dv = view(dv);
     a.lse = (float *)lse;
     a.rest = (char *)rest;
-    a.delta = (float *)workspace;
-    a.strips = (float *)((char *)workspace + strips_at);
+    a.row_start = (float *)workspace;
+    a.row_minus = (float *)((char *)workspace + l.row_minus);
+    a.strips = (float *)((char *)workspace + l.strips);
+    a.part = (float *)((char *)workspace + l.part);
+    const KeyParts k_parts = key_parts(p);
+    a.head_parts = k_parts.heads;
+    a.q_parts = k_parts.queries;
     a.dbias = dbias_out;
     GBT_HIP(ctx, gbt_launch_attention_grad(ctx->stream, a, c, p.dtype));
     return GBT_OK;

@@ -14,6 +14,8 @@
 // and rest 7e-4, with the row sums 2e-7 .. 5e-7; of dq, rows of 5 .. 60 keys, without rest 2.9e-3, with it 2.4e-3.)
 #include "attention.h"
 
+#include <type_traits>
+
 namespace {
 
 // A head's bias gradient of one workgroup's keys, by wave.
@@ -104,23 +106,23 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
         for (int r = 0; r < 16; ++r) dq[b][r] = 0.0f;
     float row_sum = 0.0f;   // of dS: this lane's half of the column
 
-    auto fetch = [&](int kb) {
-        T::fetch(k_tile[(kb >> 6) & 1], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
-        T::fetch(v_tile[(kb >> 6) & 1], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+    auto fetch = [&](int n, int kb) {
+        T::fetch(k_tile[n], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
+        T::fetch(v_tile[n], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
     };
-    if (end > 0) fetch(0);
+    if (end > 0) fetch(0, 0);
     arrived(qf);
     arrived(gf);
     __syncthreads();
     if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
 
-    for (int kb = 0; kb < end; kb += 64) {
+    auto step = [&](auto which, int kb) {
+        constexpr int kNow = decltype(which)::value;
         tiles_ready();
-        if (kb + 64 < end) fetch(kb + 64);
-        const char *k_now = k_tile[(kb >> 6) & 1], *v_now = v_tile[(kb >> 6) & 1];
+        if (kb + 64 < end) fetch(1 - kNow, kb + 64);
         const int lowest = kb - (first + 127 + off);
-        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest + 191 + lane);
-        if (kb >= wave_end) continue;
+        if (bias && wave == ((kb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest + 191, lane);
+        if (kb >= wave_end) return;
 
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -128,11 +130,14 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
             f32x16 s, dp;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+            for (int r = 0; r < 16; ++r) {
+                s[r] = 0.0f;
+                dp[r] = -delta;
+            }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                s = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s);
-                dp = P::mma(T::template rows<P>(v_now, 32 * b, i, lane), gf[i], dp);
+                s = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s);
+                dp = P::mma(T::template rows<P>(v_tile[kNow], 32 * b, i, lane), gf[i], dp);
             }
             if (b0 == b1) {
                 const float add = (bias ? buckets.value[b0] : 0.0f) + minus;
@@ -149,20 +154,28 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] *= dp[r] - delta;
+                s[r] *= dp[r];
                 row_sum += s[r];
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const V8 ds = operand<P>(s, i);
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(T::template cols<P>(k_now, 32 * b + 16 * i, d, lane), ds, dq[d]);
+                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(T::template cols<P>(k_tile[kNow], 32 * b + 16 * i, d, lane), ds, dq[d]);
             }
         }
+    };
+    for (int kb = 0; kb < end; kb += 128) {
+        step(std::integral_constant<int, 0>{}, kb);
+        if (kb + 64 < end) step(std::integral_constant<int, 1>{}, kb + 64);
     }
     row_sum = column_sum(row_sum);
     if (!there) return;
-    if (half == 0) a.delta[(int64_t)head * a.q_rows + rows.q0 + query] = delta + row_sum;
+    if (half == 0) {
+        const int64_t at = (int64_t)head * a.q_rows + rows.q0 + query;
+        a.row_start[at] = minus == -INFINITY ? -INFINITY : -a.lse[at] / a.scale;
+        a.row_minus[at] = -(delta + row_sum);
+    }
     E *out = (E *)a.dq.data + (rows.q0 + query) * a.dq.row + (int64_t)head * a.dq.head;
     typedef E E4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -180,11 +193,13 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
 }
 
 // ------------------------------------------------------------------------------------------------------------- keys --
-// A workgroup takes 128 keys of one key head, a wave 32 of them (its columns); the queries of every head that shares them pass through
-// LDS with their output gradients, 64 at a time.
+// A workgroup takes 128 keys of one key head, a wave 32 of them (its columns); the queries of the heads that share them pass through LDS with
+// their output gradients, 64 at a time.  Products start from what the row has instead of zero, so that scores come out less their
+// row's statistic, and gradients of probabilities less delta.  Where there are few blocks of keys, several workgroups share one, by heads and by
+// queries, and their sums are added up by a kernel of its own.
 //
 // Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane.  Others are laid out by
-// diagonals in LDS and added up along them (64 distances, one a lane), and then over each run of lanes of one bucket.
+// diagonals in LDS, sixteen rows at a time, and added up along them (63 distances, one a lane), and then over each run of lanes of one bucket.
 template <typename P, int DP>
 __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
@@ -193,22 +208,27 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     __shared__ __align__(16) char q_tile[2][T::kBytes];
     __shared__ __align__(16) char g_tile[2][T::kBytes];
-    __shared__ __align__(16) float row_minus[2][64], row_delta[2][64];
+    __shared__ __align__(16) float row_start[2][64], row_minus[2][64];
     __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
     __shared__ BucketSums sums;
-    __shared__ float skew[4][32 * 64];   // [key][key - query + 31]: a 32 x 32 result by its diagonals
+    __shared__ float skew[4][16 * 64];   // [query][key - query + 31]: sixteen rows of a result by its diagonals
 
-    const int k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
-    const int64_t items = (int64_t)k_blocks * a.kv_heads * a.n_seq, item = attn_item(items);
+    const int k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries, parts = a.head_parts * a.q_parts;
+    const int64_t items = (int64_t)k_blocks * parts * a.kv_heads * a.n_seq, item = attn_item(items);
     if (item >= items) return;
-    const int block = (int)(item % k_blocks), kv_head = (int)(item / k_blocks % a.kv_heads), seq = (int)(item / k_blocks / a.kv_heads);
+    const int block = (int)(item % k_blocks), part = (int)(item / k_blocks % parts);
+    const int kv_head = (int)(item / k_blocks / parts % a.kv_heads), seq = (int)(item / k_blocks / parts / a.kv_heads);
+    const int q_part = part % a.q_parts, head_part = part / a.q_parts;
+    const int g_from = a.group * head_part / a.head_parts, g_to = a.group * (head_part + 1) / a.head_parts;
     const AttnSeq rows = attn_seq(a, seq);
     const int first = block * kAttnQueries;
     const bool bias = a.n_buckets > 0;
-    auto strip = [&](int head) { return a.strips + (((int64_t)head * a.n_seq + seq) * k_blocks + block) * a.n_buckets; };
+    auto strip = [&](int head) {
+        return a.strips + (((int64_t)head * a.n_seq + seq) * k_blocks * a.q_parts + (int64_t)block * a.q_parts + q_part) * a.n_buckets;
+    };
     if (first >= rows.nk) {
-        for (int g = 0; g < a.group; ++g)
+        for (int g = g_from; g < g_to; ++g)
             for (int i = threadIdx.x; i < a.n_buckets; i += 256) strip(kv_head * a.group + g)[i] = 0.0f;
         return;
     }
@@ -218,7 +238,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
     const bool there = key < rows.nk;
     if (bias) {
         buckets_load_cuts(buckets, a, c);
-        for (int i = threadIdx.x; i < 4 * 32 * 64; i += 256) (&skew[0][0])[i] = 0.0f;
+        for (int i = threadIdx.x; i < 4 * 16 * 64; i += 256) (&skew[0][0])[i] = 0.0f;
     }
 
     V8 kf[kSteps], vf[kSteps];
@@ -232,24 +252,27 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
             vf[s] = as_vec<V8>(load16(vb, d * 2, there && d < a.dim));
         }
     }
+    arrived(kf);
+    arrived(vf);
     f32x16 dk[kBlocks], dv[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.0f;
 
-    // queries from `start` on see one of the workgroup's keys
-    const int start = a.causal ? max(0, first - off) & ~63 : 0;
+    // queries from here on see one of the workgroup's keys; this workgroup takes its part of them, in whole tiles
+    const int seen = a.causal ? max(0, first - off) & ~63 : 0, tiles = max(0, (rows.nq - seen + 63) >> 6);
+    const int from = seen + 64 * (int)((int64_t)tiles * q_part / a.q_parts), to = min(rows.nq, seen + 64 * (int)((int64_t)tiles * (q_part + 1) / a.q_parts));
     const int sees = a.causal ? key - off : 0;                         // the first query that sees this lane's key
     const int wave_from = a.causal ? first + wave * 32 - off : 0;      // and one of the wave's,
     const int wave_all = a.causal ? first + wave * 32 + 31 - off : 0;  // and all of them
     const bool wave_last = first + wave * 32 + 32 > rows.nk;           // some of the wave's keys do not exist
 
-    for (int g = 0; g < a.group; ++g) {
+    for (int g = g_from; g < g_to; ++g) {
         const int head = kv_head * a.group + g;
         const char *q_base = a.q.data + (rows.q0 * a.q.row + (int64_t)head * a.q.head) * 2;
         const char *g_base = a.dout.data + (rows.q0 * a.dout.row + (int64_t)head * a.dout.head) * 2;
-        const float *lse = a.lse + (int64_t)head * a.q_rows + rows.q0, *delta = a.delta + (int64_t)head * a.q_rows + rows.q0;
+        const int64_t at_row = (int64_t)head * a.q_rows + rows.q0;
         __syncthreads();   // the head before is done with the values, the ring and the sums
         float run = 0.0f;  // this lane's part of the sum over results of one bucket
         int run_bucket = 0;
@@ -257,29 +280,23 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
             buckets_load_values(buckets, a, head);
             for (int i = threadIdx.x; i < 4 * kAttnBuckets; i += 256) (&sums.at[0][0])[i] = 0.0f;
         }
-        auto fetch = [&](int qb) {
-            const int n = (qb >> 6) & 1;
+        auto fetch = [&](int n, int qb) {
             T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim);
             T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim);
-            if (threadIdx.x < 64) {
-                const int q = qb + threadIdx.x;
-                const float l = q < rows.nq ? lse[q] : -INFINITY;
-                row_minus[n][threadIdx.x] = l == -INFINITY ? -INFINITY : -l * GBT_LOG2E;   // no query, or one that saw no key
-                row_delta[n][threadIdx.x] = q < rows.nq ? delta[q] : 0.0f;
-            }
+            const uint32_t at = min(lane, rows.nq - qb - 1) * 4;
+            if (wave == 0) load_word_to_lds(lds_address(row_start[n]), a.row_start + at_row + qb, at);
+            if (wave == 1) load_word_to_lds(lds_address(row_minus[n]), a.row_minus + at_row + qb, at);
         };
-        if (start < rows.nq) fetch(start);
-        arrived(kf);
-        arrived(vf);
+        if (from < to) fetch(0, from);
         __syncthreads();
-        if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (start + 63 + off));
-        for (int qb = start; qb < rows.nq; qb += 64) {
+        if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (from + 63 + off));
+
+        auto step = [&](auto which, int qb) {
+            constexpr int kNow = decltype(which)::value;
             tiles_ready();
-            if (qb + 64 < rows.nq) fetch(qb + 64);
-            const int now = (qb >> 6) & 1;
-            const char *q_now = q_tile[now], *g_now = g_tile[now];
+            if (qb + 64 < to) fetch(1 - kNow, qb + 64);
             const int lowest = first - (qb + 63 + off);
-            if (bias && wave == ((qb >> 6) & 3)) ring_put(ring, buckets, c.steps, lowest - 64 + lane);
+            if (bias && wave == ((qb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest - 64, lane);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 if (qb + 32 * b + 31 < wave_from || qb + 32 * b >= rows.nq) continue;
@@ -287,37 +304,37 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                 const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
                 f32x16 s, dp;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, lane), kf[i], s);
-                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, lane), vf[i], dp);
-                }
-                f32x16 minus, del;
-#pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
-                    const f32x4 m = *(const f32x4 *)(row_minus[now] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_delta[now] + 32 * b + 8 * r4 + 4 * half);
+                    const f32x4 m = *(const f32x4 *)(row_start[kNow] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_minus[kNow] + 32 * b + 8 * r4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        minus[4 * r4 + e] = m[e];
-                        del[4 * r4 + e] = d[e];
+                        s[4 * r4 + e] = m[e];
+                        dp[4 * r4 + e] = d[e];
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    s = P::mma(T::template rows<P>(q_tile[kNow], 32 * b, i, lane), kf[i], s);
+                    dp = P::mma(T::template rows<P>(g_tile[kNow], 32 * b, i, lane), vf[i], dp);
                 }
                 if (b0 == b1) {
                     const float add = bias ? buckets.value[b0] : 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add + minus[r]));
+                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add));
                 } else {
                     const float *add = ring.value + at + 31 + (lane & 31);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add[-result_row(r, half)] + minus[r]));
+                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add[-result_row(r, half)]));
                 }
-                if (qb + 32 * b < wave_all) {
+                if (qb + 32 * b < wave_all || qb + 32 * b + 32 > rows.nq) {   // rows past the last are the last one's copies
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = qb + 32 * b + result_row(r, half) >= sees ? s[r] : 0.0f;
+                    for (int r = 0; r < 16; ++r) {
+                        const int q = qb + 32 * b + result_row(r, half);
+                        s[r] = q >= sees && q < rows.nq ? s[r] : 0.0f;
+                    }
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - del[r]);
+                for (int r = 0; r < 16; ++r) dp[r] *= s[r];
                 // a key beyond the last has scores of its bias alone
                 if (bias && wave_last) {
 #pragma unroll
@@ -334,13 +351,17 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
 #pragma unroll
                     for (int r = 0; r < 16; ++r) run += dp[r];
                 } else if (bias) {
-                    float *sk = skew[wave];
+                    float *sk = skew[wave], v = 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) sk[(lane & 31) * 65 + 31 - result_row(r, half)] = dp[r];
-                    __builtin_amdgcn_wave_barrier();
-                    float v = 0.0f;
+                    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v += sk[64 * i + lane];
+                        for (int r = 0; r < 8; ++r) sk[result_row(r, half) * 63 + 31 + (lane & 31)] = dp[8 * h + r];
+                        __builtin_amdgcn_wave_barrier();
+                        // the second sixteen rows' diagonals lie sixteen places further on; place 63 is never written
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v += sk[64 * i + min(lane + 16 * h, 63)];
+                        __builtin_amdgcn_wave_barrier();
+                    }
                     add_runs(sums.at[wave], v, ring.bucket[at + min(lane, 62)], lane);
                 }
 #pragma unroll
@@ -348,11 +369,15 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                     const V8 p = operand<P>(s, i), ds = operand<P>(dp, i);
 #pragma unroll
                     for (int d = 0; d < kBlocks; ++d) {
-                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, lane), p, dv[d]);
-                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, lane), ds, dk[d]);
+                        dv[d] = P::mma(T::template cols<P>(g_tile[kNow], 32 * b + 16 * i, d, lane), p, dv[d]);
+                        dk[d] = P::mma(T::template cols<P>(q_tile[kNow], 32 * b + 16 * i, d, lane), ds, dk[d]);
                     }
                 }
             }
+        };
+        for (int qb = from; qb < to; qb += 128) {
+            step(std::integral_constant<int, 0>{}, qb);
+            if (qb + 64 < to) step(std::integral_constant<int, 1>{}, qb + 64);
         }
         if (bias) {
             const float v = wave_sum(run);
@@ -363,6 +388,21 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         }
     }
     if (!there) return;
+    if (parts > 1) {
+        const int64_t tensor = a.k_rows * a.kv_heads * a.dim;
+        float *ko = a.part + 2 * part * tensor + ((rows.k0 + key) * a.kv_heads + kv_head) * a.dim, *vo = ko + tensor;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const int d = 32 * b + 8 * r4 + 4 * half;
+                if (d < a.dim) {
+                    *(f32x4 *)(ko + d) = f32x4{dk[b][4 * r4], dk[b][4 * r4 + 1], dk[b][4 * r4 + 2], dk[b][4 * r4 + 3]};
+                    *(f32x4 *)(vo + d) = f32x4{dv[b][4 * r4], dv[b][4 * r4 + 1], dv[b][4 * r4 + 2], dv[b][4 * r4 + 3]};
+                }
+            }
+        return;
+    }
     E *ko = (E *)a.dk.data + (rows.k0 + key) * a.dk.row + (int64_t)kv_head * a.dk.head;
     E *vo = (E *)a.dv.data + (rows.k0 + key) * a.dv.row + (int64_t)kv_head * a.dv.head;
     typedef E E4 __attribute__((ext_vector_type(4)));
@@ -384,11 +424,41 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         }
 }
 
+// The parts of the keys' gradients together: a workgroup takes sixteen key rows of a sequence, a thread four elements of one.
+template <typename P>
+__global__ __launch_bounds__(256) void grad_join_kernel(AttnArgs a) {
+    typedef typename P::elem E;
+    typedef E E4 __attribute__((ext_vector_type(4)));
+    const int row_blocks = (a.max_k + 15) / 16, seq = blockIdx.x / row_blocks, first = blockIdx.x % row_blocks * 16;
+    const AttnSeq rows = attn_seq(a, seq);
+    if (first >= rows.nk) return;
+    const int wide = a.kv_heads * a.dim / 4, parts = a.head_parts * a.q_parts;
+    const int64_t tensor = a.k_rows * a.kv_heads * a.dim;
+    for (int i = threadIdx.x; i < min(16, rows.nk - first) * wide; i += 256) {
+        const int64_t row = rows.k0 + first + i / wide;
+        const int e = i % wide * 4, kv_head = e / a.dim, d = e % a.dim;
+        const float *from = a.part + row * a.kv_heads * a.dim + e;
+        f32x4 k = {0.0f, 0.0f, 0.0f, 0.0f}, v = k;
+        for (int p = 0; p < parts; ++p) {
+            k += *(const f32x4 *)(from + 2 * p * tensor);
+            v += *(const f32x4 *)(from + (2 * p + 1) * tensor);
+        }
+        E4 x, y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = (E)(k[j] * a.scale);
+            y[j] = (E)v[j];
+        }
+        *(E4 *)((E *)a.dk.data + row * a.dk.row + (int64_t)kv_head * a.dk.head + d) = x;
+        *(E4 *)((E *)a.dv.data + row * a.dv.row + (int64_t)kv_head * a.dv.head + d) = y;
+    }
+}
+
 // The strips of every head together, in a fixed order: a workgroup takes a head, a thread every (256 / buckets)-th strip of a bucket.
 __global__ __launch_bounds__(256) void grad_bias_kernel(AttnArgs a) {
     __shared__ double part[256];
     const int head = blockIdx.x, n = a.n_buckets, lanes = 256 / n;   // threads of a bucket
-    const int64_t strips = (int64_t)a.n_seq * ((a.max_k + kAttnQueries - 1) / kAttnQueries);
+    const int64_t strips = (int64_t)a.n_seq * ((a.max_k + kAttnQueries - 1) / kAttnQueries) * a.q_parts;
     const float *from = a.strips + (int64_t)head * strips * n;
     const int b = threadIdx.x % n, l = threadIdx.x / n;
     double sum = 0.0;
@@ -413,8 +483,12 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {
-        grad_keys_kernel<P, DP><<<grid_of(k_blocks * a.kv_heads * a.n_seq), 256, 0, stream>>>(a, c);
+        grad_keys_kernel<P, DP><<<grid_of(k_blocks * a.head_parts * a.q_parts * a.kv_heads * a.n_seq), 256, 0, stream>>>(a, c);
         e = hipGetLastError();
+        if (e == hipSuccess && a.head_parts * a.q_parts > 1) {
+            grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 15) / 16 * a.n_seq), 256, 0, stream>>>(a);
+            e = hipGetLastError();
+        }
     }
     if (e == hipSuccess && a.n_buckets > 0) {
         grad_bias_kernel<<<(unsigned)a.heads, 256, 0, stream>>>(a);
