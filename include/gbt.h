@@ -532,7 +532,7 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
 #define GBT_BF16 1
 #define GBT_F16 2
 #define GBT_MAX_HEAD_DIM 128
-#define GBT_MAX_BUCKETS 256
+#define GBT_MAX_BUCKETS 128
 
 typedef struct gbt_heads {       /* [dev] rows x heads x head_dim elements */
     void *data;
@@ -546,7 +546,7 @@ typedef struct gbt_attention_params {
     int32_t n_seq;
     int32_t max_q, max_k;        /* no sequence is longer (rows beyond are not used) */
     int32_t causal;
-    int32_t n_buckets;           /* 0 (no bias) .. 256 */
+    int32_t n_buckets;           /* 0 (no bias) .. 128 */
     float scale;                 /* 1e-6..1e6 */
     int64_t q_rows, k_rows;      /* rows of the q and k tensors; rows of a sequence that lie outside do not exist */
     const int64_t *q_ptr;        /* [dev] int64[n_seq + 1]; NULL: sequence s has rows s * max_q .. (s + 1) * max_q */

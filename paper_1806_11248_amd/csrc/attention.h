@@ -11,7 +11,7 @@
 
 #include "gbt_internal.h"
 
-constexpr int kAttnBuckets = 256;   // most buckets of distance
+constexpr int kAttnBuckets = GBT_MAX_BUCKETS;   // of distance; a power of two
 
 struct AttnView {   // rows x heads x head_dim elements; strides in elements, the head's elements side by side
     char *data;
@@ -150,25 +150,17 @@ struct Tile {
     static __device__ __forceinline__ constexpr int fold(int row) {
         return kPlaces == 4 ? (row >> 2) & 3 : kPlaces == 8 ? ((row >> 1) & 1) * 4 | ((row >> 2) & 3) : (row & 3) * 4 | ((row >> 2) & 3);
     }
-    // From memory straight into LDS, a wave's 64 pieces at a time; 256 threads.  Rows past the last and elements past the head's are taken from
+    // From memory straight into LDS, a wave's 64 pieces at a time, by four waves, of which this one is number `wave`.  Rows past the last and elements past the head's are taken from
     // the last there are, so that nothing hangs on a condition: such rows' probabilities are zero, and such elements meet zeros of the
     // other operand or are not stored.  rows, dim > 0; 64 * row_bytes < 2^32.
-    static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim, int wave) {
+        const int lane = threadIdx.x & 63;
         constexpr int kRows = 64 / kPlaces;                       // of a wave's load
         const int row = wave * kRows + lane / kPlaces;            // the i-th load's is 4 * kRows further, with the same fold
         const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;
         const uint32_t to = lds_address(tile) + wave * 1024;
-        if (rows >= 64) {
-            const uint32_t at = row * row_bytes + col;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                load_to_lds(to + i * 4096, base + (uint64_t)(i * 4 * kRows) * row_bytes, at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                load_to_lds(to + i * 4096, base, min(row + i * 4 * kRows, rows - 1) * row_bytes + col);
-        }
+        for (int i = 0; i < kLoads; ++i) load_to_lds(to + i * 4096, base, (uint32_t)min(row + i * 4 * kRows, rows - 1) * row_bytes + col);
     }
     // First operand, rows as they are: row row0 + lane % 32 (row0 a multiple of 32), elements 16 * step + 8 * (lane / 32) .. + 7.
     template <typename P>
@@ -254,15 +246,14 @@ __device__ __forceinline__ int bucket_of(const Buckets &b, int steps, int t) {
 // are kept in a ring of 256, twice, so that a stretch is read without wrapping.
 struct DistanceRing {
     float value[512];
-    int bucket[512];
+    uint8_t bucket[512];
 };
 __device__ __forceinline__ void ring_put(DistanceRing &ring, const Buckets &b, int steps, int t) {
     const int n = bucket_of(b, steps, t), at = t & 255;
     const float v = b.value[n];
     ring.value[at] = v;
     ring.value[at + 256] = v;
-    ring.bucket[at] = n;
-    ring.bucket[at + 256] = n;
+    ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
 }
 
 // The 64 distances from t0 on, by one wave.  Beyond the first or the last cut there is nothing to search.
@@ -272,7 +263,7 @@ __device__ __forceinline__ void ring_next(DistanceRing &ring, const Buckets &b, 
     } else {
         const int n = t0 + 63 < c.at[0] ? 0 : n_buckets - 1, at = (t0 + lane) & 255;
         ring.value[at] = ring.value[at + 256] = b.value[n];
-        ring.bucket[at] = ring.bucket[at + 256] = n;
+        ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
     }
 }
 

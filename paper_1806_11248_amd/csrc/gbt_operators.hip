@@ -33,7 +33,7 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
     *code = GBT_EUNSUPPORTED;
     if (p.dtype != GBT_BF16 && p.dtype != GBT_F16) return "dtype is neither GBT_BF16 nor GBT_F16";
     if (p.head_dim < 8 || p.head_dim > GBT_MAX_HEAD_DIM || p.head_dim % 8) return "head_dim is no multiple of 8 in 8..128";
-    if (p.n_buckets > GBT_MAX_BUCKETS) return "n_buckets > 256";
+    if (p.n_buckets > GBT_MAX_BUCKETS) return "n_buckets > 128";
     *code = GBT_EINVAL;
     if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads || p.heads > (1 << 16)) return "heads is no multiple of kv_heads, or out of range";
     if (p.n_seq < 0 || p.max_q < 0 || p.max_k < 0 || p.max_q > (1 << 29) || p.max_k > (1 << 29)) return "n_seq, max_q or max_k out of range";

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     const AttnSeq rows = attn_seq(a, seq);
     const int first = block * kAttnQueries;
     if (first >= rows.nq) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool bias = a.n_buckets > 0;
@@ -71,8 +71,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     float top = -INFINITY, sum = 0.0f;
 
     auto fetch = [&](int which, int kb) {
-        T::fetch(k_tile[which], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
-        T::fetch(v_tile[which], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+        T::fetch(k_tile[which], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::fetch(v_tile[which], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
     };
     if (end > 0) fetch(0, 0);
     arrived(qf);

@@ -18,11 +18,6 @@
 
 namespace {
 
-// A head's bias gradient of one workgroup's keys, by wave.
-struct BucketSums {
-    float at[4][kAttnBuckets];
-};
-
 // Sums over equal buckets of neighbouring lanes (a lane's bucket is never below that of the lane before); the last lane of each run
 // adds its sum.
 __device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int lane) {
@@ -58,7 +53,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     const int first = block * kAttnQueries;
     const bool bias = a.n_buckets > 0;
     if (first >= rows.nq) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool there = query < rows.nq;
@@ -107,8 +102,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     float row_sum = 0.0f;   // of dS: this lane's half of the column
 
     auto fetch = [&](int n, int kb) {
-        T::fetch(k_tile[n], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim);
-        T::fetch(v_tile[n], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim);
+        T::fetch(k_tile[n], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::fetch(v_tile[n], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
     };
     if (end > 0) fetch(0, 0);
     arrived(qf);
@@ -199,20 +194,22 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
 // queries, and their sums are added up by a kernel of its own.
 //
 // Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane.  Others are laid out by
-// diagonals in LDS, sixteen rows at a time, and added up along them (63 distances, one a lane), and then over each run of lanes of one bucket.
-template <typename P, int DP>
-__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
+// diagonals in LDS, eight rows at a time, and added up along them (63 distances, one a lane), and then over each run of lanes of one bucket.
+template <typename P, int DP, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kThreads = 64 * kWaves;
+    constexpr bool kValuesInLds = kWaves == 8 && DP == 128;
     __shared__ __align__(16) char q_tile[2][T::kBytes];
     __shared__ __align__(16) char g_tile[2][T::kBytes];
+    __shared__ __align__(16) char v_block[kValuesInLds ? 2 * T::kBytes : 16];
     __shared__ __align__(16) float row_start[2][64], row_minus[2][64];
     __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
-    __shared__ BucketSums sums;
-    __shared__ float skew[4][16 * 64];   // [query][key - query + 31]: sixteen rows of a result by its diagonals
+    __shared__ float sums[kWaves][kAttnBuckets];   // the head's bias gradient of this workgroup's keys, by wave
+    __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
 
     const int k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries, parts = a.head_parts * a.q_parts;
     const int64_t items = (int64_t)k_blocks * parts * a.kv_heads * a.n_seq, item = attn_item(items);
@@ -229,19 +226,20 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
     };
     if (first >= rows.nk) {
         for (int g = g_from; g < g_to; ++g)
-            for (int i = threadIdx.x; i < a.n_buckets; i += 256) strip(kv_head * a.group + g)[i] = 0.0f;
+            for (int i = threadIdx.x; i < a.n_buckets; i += kThreads) strip(kv_head * a.group + g)[i] = 0.0f;
         return;
     }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int key_wave = wave & 3;   // of eight waves, 4 .. 7 take the second half of each tile for the keys of 0 .. 3
     const int off = rows.nk - rows.nq;
-    const int key = first + wave * 32 + (lane & 31);
+    const int key = first + key_wave * 32 + (lane & 31);
     const bool there = key < rows.nk;
     if (bias) {
         buckets_load_cuts(buckets, a, c);
-        for (int i = threadIdx.x; i < 4 * 16 * 64; i += 256) (&skew[0][0])[i] = 0.0f;
+        for (int i = threadIdx.x; i < kWaves * 8 * 64; i += kThreads) (&skew[0][0])[i] = 0.0f;
     }
 
-    V8 kf[kSteps], vf[kSteps];
+    V8 kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
     {
         const char *kb = a.k.data + ((rows.k0 + key) * a.k.row + (int64_t)kv_head * a.k.head) * 2;
         const char *vb = a.v.data + ((rows.k0 + key) * a.v.row + (int64_t)kv_head * a.v.head) * 2;
@@ -249,11 +247,27 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         for (int s = 0; s < kSteps; ++s) {
             const int d = 16 * s + 8 * half;
             kf[s] = as_vec<V8>(load16(kb, d * 2, there && d < a.dim));
-            vf[s] = as_vec<V8>(load16(vb, d * 2, there && d < a.dim));
+            if constexpr (!kValuesInLds) vf[s] = as_vec<V8>(load16(vb, d * 2, there && d < a.dim));
+        }
+        if constexpr (kValuesInLds) {
+            const int row = first + 64 * (wave >> 2);
+            if (row < rows.nk)
+                T::fetch(v_block + (wave >> 2) * T::kBytes, a.v.data + ((rows.k0 + row) * a.v.row + (int64_t)kv_head * a.v.head) * 2, (uint32_t)a.v.row * 2,
+                         rows.nk - row, a.dim, key_wave);
         }
     }
     arrived(kf);
-    arrived(vf);
+    if constexpr (!kValuesInLds) {
+        arrived(vf);
+    } else if (a.dim < DP) {   // elements past the head's, which the other operand has copies of
+        tiles_ready();
+        for (int i = threadIdx.x; i < 128 * T::kPlaces; i += kThreads)
+            if ((i % T::kPlaces ^ T::fold(i / T::kPlaces)) >= a.dim / 8) *(i32x4 *)(v_block + 16 * i) = i32x4{0, 0, 0, 0};
+    }
+    auto values = [&](int i) {
+        if constexpr (kValuesInLds) return T::template rows<P>(v_block + (key_wave >> 1) * T::kBytes, 32 * (key_wave & 1), i, lane);
+        else return vf[i];
+    };
     f32x16 dk[kBlocks], dv[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -261,12 +275,12 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.0f;
 
     // queries from here on see one of the workgroup's keys; this workgroup takes its part of them, in whole tiles
-    const int seen = a.causal ? max(0, first - off) & ~63 : 0, tiles = max(0, (rows.nq - seen + 63) >> 6);
-    const int from = seen + 64 * (int)((int64_t)tiles * q_part / a.q_parts), to = min(rows.nq, seen + 64 * (int)((int64_t)tiles * (q_part + 1) / a.q_parts));
+    const int seen = a.causal ? max(0, first - off) & ~63 : 0, n_tiles = max(0, (rows.nq - seen + 63) >> 6);
+    const int from = seen + 64 * (int)((int64_t)n_tiles * q_part / a.q_parts), to = min(rows.nq, seen + 64 * (int)((int64_t)n_tiles * (q_part + 1) / a.q_parts));
     const int sees = a.causal ? key - off : 0;                         // the first query that sees this lane's key
-    const int wave_from = a.causal ? first + wave * 32 - off : 0;      // and one of the wave's,
-    const int wave_all = a.causal ? first + wave * 32 + 31 - off : 0;  // and all of them
-    const bool wave_last = first + wave * 32 + 32 > rows.nk;           // some of the wave's keys do not exist
+    const int wave_from = a.causal ? first + key_wave * 32 - off : 0;      // and one of the wave's,
+    const int wave_all = a.causal ? first + key_wave * 32 + 31 - off : 0;  // and all of them
+    const bool wave_last = first + key_wave * 32 + 32 > rows.nk;           // some of the wave's keys do not exist
 
     for (int g = g_from; g < g_to; ++g) {
         const int head = kv_head * a.group + g;
@@ -278,11 +292,11 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         int run_bucket = 0;
         if (bias) {
             buckets_load_values(buckets, a, head);
-            for (int i = threadIdx.x; i < 4 * kAttnBuckets; i += 256) (&sums.at[0][0])[i] = 0.0f;
+            for (int i = threadIdx.x; i < kWaves * kAttnBuckets; i += kThreads) (&sums[0][0])[i] = 0.0f;
         }
         auto fetch = [&](int n, int qb) {
-            T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim);
-            T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim);
+            if (kWaves == 4 || wave < 4) T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
+            if (kWaves == 4 || wave >= 4) T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
             const uint32_t at = min(lane, rows.nq - qb - 1) * 4;
             if (wave == 0) load_word_to_lds(lds_address(row_start[n]), a.row_start + at_row + qb, at);
             if (wave == 1) load_word_to_lds(lds_address(row_minus[n]), a.row_minus + at_row + qb, at);
@@ -291,21 +305,23 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
         __syncthreads();
         if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (from + 63 + off));
 
-        auto step = [&](auto which, int qb) {
-            constexpr int kNow = decltype(which)::value;
+        int now = 0;   // which of the two copies; not known at compile time as in the other kernels, which would cost registers
+        for (int qb = from; qb < to; qb += 64, now ^= 1) {
             tiles_ready();
-            if (qb + 64 < to) fetch(1 - kNow, qb + 64);
+            if (qb + 64 < to) fetch(1 - now, qb + 64);
+            const char *q_now = q_tile[now], *g_now = g_tile[now];
             const int lowest = first - (qb + 63 + off);
-            if (bias && wave == ((qb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest - 64, lane);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            if (bias && wave == ((qb >> 6) & (kWaves - 1))) ring_next(ring, buckets, c, a.n_buckets, lowest - 64, lane);
+#pragma unroll 1
+            for (int turn = 0; turn < 8 / kWaves; ++turn) {
+                const int b = kWaves == 8 ? wave >> 2 : turn;
                 if (qb + 32 * b + 31 < wave_from || qb + 32 * b >= rows.nq) continue;
-                const int at = (lowest & 255) + 32 * wave + 32 - 32 * b;   // of this result's lowest distance, of 63
+                const int at = (lowest & 255) + 32 * key_wave + 32 - 32 * b;   // of this result's lowest distance, of 63
                 const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
                 f32x16 s, dp;
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
-                    const f32x4 m = *(const f32x4 *)(row_start[kNow] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_minus[kNow] + 32 * b + 8 * r4 + 4 * half);
+                    const f32x4 m = *(const f32x4 *)(row_start[now] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_minus[now] + 32 * b + 8 * r4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         s[4 * r4 + e] = m[e];
@@ -314,9 +330,19 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                 }
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    s = P::mma(T::template rows<P>(q_tile[kNow], 32 * b, i, lane), kf[i], s);
-                    dp = P::mma(T::template rows<P>(g_tile[kNow], 32 * b, i, lane), vf[i], dp);
+                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, lane), kf[i], s);
+                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, lane), values(i), dp);
                 }
+                // reads two products ahead, and no further: registers are what there is least of
+                constexpr int kReads = kValuesInLds ? 3 : 2;
+                __builtin_amdgcn_sched_group_barrier(0x100, 8 + 2 * kReads, 0);
+#pragma unroll
+                for (int i = 0; i < kSteps - 2; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+                __builtin_amdgcn_sched_barrier(0);
                 if (b0 == b1) {
                     const float add = bias ? buckets.value[b0] : 0.0f;
 #pragma unroll
@@ -343,7 +369,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                 if (bias && b0 == b1) {
                     if (b0 != run_bucket) {
                         const float v = wave_sum(run);
-                        if (lane == 0) sums.at[wave][run_bucket] += v;
+                        if (lane == 0) sums[wave][run_bucket] += v;
                         __builtin_amdgcn_wave_barrier();
                         run = 0.0f;
                         run_bucket = b0;
@@ -353,39 +379,65 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void grad_keys_kernel(AttnAr
                 } else if (bias) {
                     float *sk = skew[wave], v = 0.0f;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 4; ++h) {
 #pragma unroll
-                        for (int r = 0; r < 8; ++r) sk[result_row(r, half) * 63 + 31 + (lane & 31)] = dp[8 * h + r];
+                        for (int r = 0; r < 4; ++r) sk[result_row(r, half) * 63 + 31 + (lane & 31)] = dp[4 * h + r];
                         __builtin_amdgcn_wave_barrier();
-                        // the second sixteen rows' diagonals lie sixteen places further on; place 63 is never written
+                        // eight rows further on, the same diagonal lies eight places further on; place 63 is never written
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v += sk[64 * i + min(lane + 16 * h, 63)];
+                        for (int i = 0; i < 8; ++i) v += sk[64 * i + min(lane + 8 * h, 63)];
                         __builtin_amdgcn_wave_barrier();
                     }
-                    add_runs(sums.at[wave], v, ring.bucket[at + min(lane, 62)], lane);
+                    add_runs(sums[wave], v, ring.bucket[at + min(lane, 62)], lane);
                 }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const V8 p = operand<P>(s, i), ds = operand<P>(dp, i);
 #pragma unroll
                     for (int d = 0; d < kBlocks; ++d) {
-                        dv[d] = P::mma(T::template cols<P>(g_tile[kNow], 32 * b + 16 * i, d, lane), p, dv[d]);
-                        dk[d] = P::mma(T::template cols<P>(q_tile[kNow], 32 * b + 16 * i, d, lane), ds, dk[d]);
+                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, lane), p, dv[d]);
+                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, lane), ds, dk[d]);
                     }
                 }
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int i = 0; i < 4 * kBlocks - 2; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        for (int qb = from; qb < to; qb += 128) {
-            step(std::integral_constant<int, 0>{}, qb);
-            if (qb + 64 < to) step(std::integral_constant<int, 1>{}, qb + 64);
         }
         if (bias) {
             const float v = wave_sum(run);
-            if (lane == 0) sums.at[wave][run_bucket] += v;
+            if (lane == 0) sums[wave][run_bucket] += v;
             __syncthreads();
-            for (int i = threadIdx.x; i < a.n_buckets; i += 256)
-                strip(head)[i] = (sums.at[0][i] + sums.at[1][i]) + (sums.at[2][i] + sums.at[3][i]);
+            for (int i = threadIdx.x; i < a.n_buckets; i += kThreads) {
+                float v = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+                if (kWaves == 8) v += (sums[kWaves - 4][i] + sums[kWaves - 3][i]) + (sums[kWaves - 2][i] + sums[kWaves - 1][i]);
+                strip(head)[i] = v;
+            }
         }
+    }
+    if constexpr (kWaves == 8) {   // the two halves' sums together, through LDS; 0 .. 3 hold them then
+        float *mine = (float *)(key_wave < 2 ? &q_tile[0][0] : &g_tile[0][0]) + (key_wave & 1) * kBlocks * 16 * 64 + lane;
+        auto join = [&](f32x16 (&x)[kBlocks]) {
+            __syncthreads();
+            if (wave >= 4) {
+#pragma unroll
+                for (int i = 0; i < 16 * kBlocks; ++i) mine[64 * i] = x[i / 16][i % 16];
+            }
+            __syncthreads();
+            if (wave < 4) {
+#pragma unroll
+                for (int i = 0; i < 16 * kBlocks; ++i) x[i / 16][i % 16] += mine[64 * i];
+            }
+        };
+        join(dk);
+        join(dv);
+        if (wave >= 4) return;
     }
     if (!there) return;
     if (parts > 1) {
@@ -483,7 +535,8 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {
-        grad_keys_kernel<P, DP><<<grid_of(k_blocks * a.head_parts * a.q_parts * a.kv_heads * a.n_seq), 256, 0, stream>>>(a, c);
+        constexpr int kWaves = DP == 128 ? 8 : 4;
+        grad_keys_kernel<P, DP, kWaves><<<grid_of(k_blocks * a.head_parts * a.q_parts * a.kv_heads * a.n_seq), 64 * kWaves, 0, stream>>>(a, c);
         e = hipGetLastError();
         if (e == hipSuccess && a.head_parts * a.q_parts > 1) {
             grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 15) / 16 * a.n_seq), 256, 0, stream>>>(a);
