@@ -476,21 +476,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         }
 }
 
-// The parts of the keys' gradients together: a workgroup takes sixteen key rows of a sequence, a thread four elements of one.
+// The parts of the keys' gradients together: a workgroup takes four key rows of a sequence, a thread four elements of one.
 template <typename P>
 __global__ __launch_bounds__(256) void grad_join_kernel(AttnArgs a) {
     typedef typename P::elem E;
     typedef E E4 __attribute__((ext_vector_type(4)));
-    const int row_blocks = (a.max_k + 15) / 16, seq = blockIdx.x / row_blocks, first = blockIdx.x % row_blocks * 16;
+    const int row_blocks = (a.max_k + 3) / 4, seq = blockIdx.x / row_blocks, first = blockIdx.x % row_blocks * 4;
     const AttnSeq rows = attn_seq(a, seq);
     if (first >= rows.nk) return;
     const int wide = a.kv_heads * a.dim / 4, parts = a.head_parts * a.q_parts;
     const int64_t tensor = a.k_rows * a.kv_heads * a.dim;
-    for (int i = threadIdx.x; i < min(16, rows.nk - first) * wide; i += 256) {
+    for (int i = threadIdx.x; i < min(4, rows.nk - first) * wide; i += 256) {
         const int64_t row = rows.k0 + first + i / wide;
         const int e = i % wide * 4, kv_head = e / a.dim, d = e % a.dim;
         const float *from = a.part + row * a.kv_heads * a.dim + e;
         f32x4 k = {0.0f, 0.0f, 0.0f, 0.0f}, v = k;
+#pragma unroll 4
         for (int p = 0; p < parts; ++p) {
             k += *(const f32x4 *)(from + 2 * p * tensor);
             v += *(const f32x4 *)(from + (2 * p + 1) * tensor);
@@ -539,7 +540,7 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         grad_keys_kernel<P, DP, kWaves><<<grid_of(k_blocks * a.head_parts * a.q_parts * a.kv_heads * a.n_seq), 64 * kWaves, 0, stream>>>(a, c);
         e = hipGetLastError();
         if (e == hipSuccess && a.head_parts * a.q_parts > 1) {
-            grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 15) / 16 * a.n_seq), 256, 0, stream>>>(a);
+            grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 3) / 4 * a.n_seq), 256, 0, stream>>>(a);
             e = hipGetLastError();
         }
     }
