@@ -40,9 +40,8 @@ struct AttnArgs {
     int pieces, piece_len;
 };
 
-struct AttnCuts {   // ascending; filled up with INT32_MAX to a power of two less one
-    int32_t at[kAttnBuckets - 1];
-    int32_t steps;   // of the binary search: 2^steps - 1 cuts are looked at
+struct AttnCuts {
+    int32_t at[kAttnBuckets - 1];   // ascending
 };
 
 hipError_t gbt_launch_attention(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
@@ -225,46 +224,49 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 // Buckets of distance.  A bucket's number is how many cuts are at most the distance, as a symbol's is of its value.
-struct Buckets {
-    int cut[kAttnBuckets];
-    float value[kAttnBuckets];   // the head's, times log2(e)
-};
-__device__ __forceinline__ void buckets_load_cuts(Buckets &b, const AttnArgs &a, const AttnCuts &c) {
-    const int n = (1 << c.steps) - 1;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) b.cut[i] = c.at[i];
-}
-__device__ __forceinline__ void buckets_load_values(Buckets &b, const AttnArgs &a, int head) {
-    for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) b.value[i] = a.bias[(int64_t)i * a.heads + head] * GBT_LOG2E;
-}
-__device__ __forceinline__ int bucket_of(const Buckets &b, int steps, int t) {
-    int lo = 0;   // cuts known to be at most t
-    for (int s = steps - 1; s >= 0; --s) lo += b.cut[lo + (1 << s) - 1] <= t ? 1 << s : 0;
-    return lo;
-}
-
-// The distances that a tile of 64 rows against a workgroup's 128 meets are 191 in a row, and 64 new ones come with each step.  They
-// are kept in a ring of 256, twice, so that a stretch is read without wrapping.
+//
+// The distances that a tile of 64 rows against a workgroup's 128 meets are 191 in a row, and 64 new ones come with each step.  They are kept in a
+// ring of 256, twice, so that a stretch is read without wrapping.
 struct DistanceRing {
-    float value[512];
+    float value[512];              // the head's bias times log2(e)
     uint8_t bucket[512];
+    uint8_t is_cut[8][64];         // by wave
+    float of_bucket[kAttnBuckets];
+    int cut[kAttnBuckets];         // filled up with INT32_MAX
 };
-__device__ __forceinline__ void ring_put(DistanceRing &ring, const Buckets &b, int steps, int t) {
-    const int n = bucket_of(b, steps, t), at = t & 255;
-    const float v = b.value[n];
-    ring.value[at] = v;
-    ring.value[at + 256] = v;
-    ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
+// Two cuts for each lane of a wave.
+struct LaneCuts {
+    int lo, hi;
+};
+__device__ __forceinline__ void ring_cuts(DistanceRing &ring, const AttnArgs &a, const AttnCuts &c) {
+    if (threadIdx.x < kAttnBuckets) ring.cut[threadIdx.x] = (int)threadIdx.x < a.n_buckets - 1 ? c.at[threadIdx.x] : INT32_MAX;
 }
-
-// The 64 distances from t0 on, by one wave.  Beyond the first or the last cut there is nothing to search.
-__device__ __forceinline__ void ring_next(DistanceRing &ring, const Buckets &b, const AttnCuts &c, int n_buckets, int t0, int lane) {
-    if (t0 + 63 >= c.at[0] && (n_buckets < 2 || t0 < c.at[n_buckets - 2])) {
-        ring_put(ring, b, c.steps, t0 + lane);
-    } else {
-        const int n = t0 + 63 < c.at[0] ? 0 : n_buckets - 1, at = (t0 + lane) & 255;
-        ring.value[at] = ring.value[at + 256] = b.value[n];
-        ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
+__device__ __forceinline__ void ring_head(DistanceRing &ring, const AttnArgs &a, int head) {
+    for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) ring.of_bucket[i] = a.bias[(int64_t)i * a.heads + head] * GBT_LOG2E;
+}
+// The bucket of distance t0 + lane, for a whole wave.  The lane of each cut among the 64 distances marks its place in LDS; how many marks are at
+// or before a distance is then a count of bits.
+__device__ __forceinline__ int lane_bucket(uint8_t *mark, const LaneCuts &cuts, int t0, int lane) {
+    const int lo = cuts.lo - t0, hi = cuts.hi - t0;
+    int n = __popcll(__ballot(cuts.lo < t0)) + __popcll(__ballot(cuts.hi < t0));
+    const bool lo_in = cuts.lo >= t0 && (uint32_t)lo < 64u, hi_in = cuts.hi >= t0 && (uint32_t)hi < 64u;
+    if (__any(lo_in || hi_in)) {
+        mark[lane] = 0;
+        __builtin_amdgcn_wave_barrier();
+        if (lo_in) mark[lo] = 1;
+        if (hi_in) mark[hi] = 1;
+        __builtin_amdgcn_wave_barrier();
+        const uint64_t marks = __ballot(mark[lane] != 0);
+        n += __popcll(marks & (~0ull >> (63 - lane)));
     }
+    return n;
+}
+// The 64 distances from t0 on into the ring, by one wave.
+__device__ __forceinline__ void ring_put(DistanceRing &ring, int t0, int wave, int lane) {
+    const int n = lane_bucket(ring.is_cut[wave], LaneCuts{ring.cut[lane], ring.cut[lane + 64]}, t0, lane);
+    const int at = (t0 + lane) & 255;
+    ring.value[at] = ring.value[at + 256] = ring.of_bucket[n];
+    ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
 }
 
 }  // namespace

@@ -86,8 +86,6 @@ void fill(AttnArgs &a, AttnCuts &c, const gbt_attention_params &p) {
     a.scale = p.scale;
     a.scale2 = p.scale * GBT_LOG2E;
     a.bias = p.bias;
-    c.steps = 0;
-    while ((1 << c.steps) - 1 < p.n_buckets - 1) ++c.steps;
     for (int i = 0; i < kAttnBuckets - 1; ++i) c.at[i] = i < p.n_buckets - 1 ? p.cuts[i] : INT32_MAX;
 }
 

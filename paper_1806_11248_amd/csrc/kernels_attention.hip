@@ -25,7 +25,6 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     __shared__ __align__(16) char k_tile[2][T::kBytes];
     __shared__ __align__(16) char v_tile[2][T::kBytes];
-    __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
@@ -41,8 +40,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     const int query = first + wave * 32 + (lane & 31);
     const bool bias = a.n_buckets > 0;
     if (bias) {
-        buckets_load_cuts(buckets, a, c);
-        buckets_load_values(buckets, a, head);
+        ring_cuts(ring, a, c);
+        ring_head(ring, a, head);
     }
 
     V8 qf[kSteps];
@@ -77,7 +76,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     if (end > 0) fetch(0, 0);
     arrived(qf);
     __syncthreads();
-    if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
+    if (bias && wave < 3) ring_put(ring, 64 * wave - (first + 127 + off), wave, lane);
 
     // one tile; which of the two copies it lies in is known at compile time, so that LDS addresses are constants of the lane
     auto step = [&](auto which, int kb) {
@@ -85,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         tiles_ready();
         if (kb + 64 < end) fetch(1 - kNow, kb + 64);
         const int lowest = kb - (first + 127 + off);   // distance
-        if (bias && wave == ((kb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest + 191, lane);
+        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, lowest + 191, wave, lane);
         if (kb >= wave_end) return;
 
         f32x16 s[2];
@@ -115,7 +114,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
                 for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], a.scale2, value[32 * b + result_row(r, half)]);
             factor = 1.0f;
         } else if (bias) {
-            add = buckets.value[b0];
+            add = ring.of_bucket[b0];
         }
         if (kb + 64 > wave_all) {
 #pragma unroll
@@ -197,8 +196,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
     typedef Tile<DP> T;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32, kChunks = DP / 8, kEach = 32 * kChunks / 64;
     __shared__ __align__(16) char v_tile[4][T::kBytes / 2];
-    __shared__ int cut[kAttnBuckets];
-    __shared__ int near_bucket[4][64];
+    __shared__ uint8_t is_cut[4][64], near_bucket[4][64];
     __shared__ float join_top[4][32], join_sum[4][32];
     __shared__ float join_o[4][32 * 33];
 
@@ -216,11 +214,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
     const int off = rows.nk - rows.nq;
     const bool there = query < rows.nq;
     const bool bias = a.n_buckets > 0;
-    if (bias) {
-        const int n = (1 << c.steps) - 1;
-        for (int i = threadIdx.x; i < n; i += 256) cut[i] = c.at[i];
-    }
-    __syncthreads();
+    const LaneCuts cuts{lane < a.n_buckets - 1 ? c.at[lane] : INT32_MAX, lane + 64 < a.n_buckets - 1 ? c.at[lane + 64] : INT32_MAX};
 
     V8 qf[kSteps];
     {
@@ -273,20 +267,16 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
         __builtin_amdgcn_wave_barrier();
         if (kb + 128 < end) load(kb + 128);
         const int lowest = kb - (q_high + off), span = 31 + q_high - q_low;   // distances lowest .. lowest + span, 63 at most
-        int mine = 0;
-        if (bias) {
-            const int t = lowest + min(lane, span);
-            for (int st = c.steps - 1; st >= 0; --st) mine += cut[mine + (1 << st) - 1] <= t ? 1 << st : 0;
-        }
-        const int b0 = __builtin_amdgcn_readlane(mine, 0), b1 = __builtin_amdgcn_readlane(mine, 63);
+        int mine = bias ? lane_bucket(is_cut[wave], cuts, lowest, lane) : 0;
+        const int b0 = __builtin_amdgcn_readfirstlane(mine), b1 = __builtin_amdgcn_readlane(mine, span);
         if (b0 == b1) {
             const float add = bias ? value[(int64_t)b0 * a.heads] * GBT_LOG2E : 0.0f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, add);
         } else {
-            near_bucket[wave][lane] = mine;
+            near_bucket[wave][lane] = (uint8_t)mine;
             __builtin_amdgcn_wave_barrier();
-            const int *at = near_bucket[wave] + (there ? q_high - query : 0);
+            const uint8_t *at = near_bucket[wave] + (there ? q_high - query : 0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, value[(int64_t)at[result_row(r, half)] * a.heads] * GBT_LOG2E);
         }

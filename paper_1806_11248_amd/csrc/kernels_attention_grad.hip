@@ -18,16 +18,23 @@
 
 namespace {
 
-// Sums over equal buckets of neighbouring lanes (a lane's bucket is never below that of the lane before); the last lane of each run
-// adds its sum.
-__device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int lane) {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const float w = __shfl_up(v, s);
-        const int b = __shfl_up(bucket, s);
-        if (lane >= s && b == bucket) v += w;
-    }
-    const int next = __shfl_down(bucket, 1);
+// One step of a sum over equal buckets of neighbouring lanes (a lane's bucket is never below that of the lane before): what the lane that CTRL
+// names has summed, where it is of the same bucket.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ void run_step(float &v, int bucket) {
+    const int w = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROW_MASK, 0xf, false);
+    const int b = __builtin_amdgcn_update_dpp(-1, bucket, CTRL, ROW_MASK, 0xf, false);
+    v += b == bucket ? __builtin_bit_cast(float, w) : 0.0f;
+}
+// Adds each run's sum to its bucket: shifts by 1, 2, 4, 8 inside each row of 16 lanes, lane 15 of rows 0 and 2 into rows 1 and 3, lane 31 into rows
+// 2 and 3.  `next` is the bucket of the lane behind.
+__device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int next, int lane) {
+    run_step<0x111, 0xf>(v, bucket);
+    run_step<0x112, 0xf>(v, bucket);
+    run_step<0x114, 0xf>(v, bucket);
+    run_step<0x118, 0xf>(v, bucket);
+    run_step<0x142, 0xa>(v, bucket);
+    run_step<0x143, 0xc>(v, bucket);
     if (lane == 63 || next != bucket) sums[bucket] += v;
     __builtin_amdgcn_wave_barrier();
 }
@@ -42,7 +49,6 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     __shared__ __align__(16) char k_tile[2][T::kBytes];
     __shared__ __align__(16) char v_tile[2][T::kBytes];
-    __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
@@ -58,8 +64,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     const int query = first + wave * 32 + (lane & 31);
     const bool there = query < rows.nq;
     if (bias) {
-        buckets_load_cuts(buckets, a, c);
-        buckets_load_values(buckets, a, head);
+        ring_cuts(ring, a, c);
+        ring_head(ring, a, head);
     }
 
     V8 qf[kSteps], gf[kSteps];
@@ -109,14 +115,14 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     arrived(qf);
     arrived(gf);
     __syncthreads();
-    if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x - (first + 127 + off));
+    if (bias && wave < 3) ring_put(ring, 64 * wave - (first + 127 + off), wave, lane);
 
     auto step = [&](auto which, int kb) {
         constexpr int kNow = decltype(which)::value;
         tiles_ready();
         if (kb + 64 < end) fetch(1 - kNow, kb + 64);
         const int lowest = kb - (first + 127 + off);
-        if (bias && wave == ((kb >> 6) & 3)) ring_next(ring, buckets, c, a.n_buckets, lowest + 191, lane);
+        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, lowest + 191, wave, lane);
         if (kb >= wave_end) return;
 
 #pragma unroll
@@ -135,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
                 dp = P::mma(T::template rows<P>(v_tile[kNow], 32 * b, i, lane), gf[i], dp);
             }
             if (b0 == b1) {
-                const float add = (bias ? buckets.value[b0] : 0.0f) + minus;
+                const float add = (bias ? ring.of_bucket[b0] : 0.0f) + minus;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add));
             } else {
@@ -206,7 +212,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     __shared__ __align__(16) char g_tile[2][T::kBytes];
     __shared__ __align__(16) char v_block[kValuesInLds ? 2 * T::kBytes : 16];
     __shared__ __align__(16) float row_start[2][64], row_minus[2][64];
-    __shared__ Buckets buckets;
     __shared__ DistanceRing ring;
     __shared__ float sums[kWaves][kAttnBuckets];   // the head's bias gradient of this workgroup's keys, by wave
     __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     const int key = first + key_wave * 32 + (lane & 31);
     const bool there = key < rows.nk;
     if (bias) {
-        buckets_load_cuts(buckets, a, c);
+        ring_cuts(ring, a, c);
         for (int i = threadIdx.x; i < kWaves * 8 * 64; i += kThreads) (&skew[0][0])[i] = 0.0f;
     }
 
@@ -291,7 +296,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         float run = 0.0f;  // this lane's part of the sum over results of one bucket
         int run_bucket = 0;
         if (bias) {
-            buckets_load_values(buckets, a, head);
+            ring_head(ring, a, head);
             for (int i = threadIdx.x; i < kWaves * kAttnBuckets; i += kThreads) (&sums[0][0])[i] = 0.0f;
         }
         auto fetch = [&](int n, int qb) {
@@ -303,7 +308,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         };
         if (from < to) fetch(0, from);
         __syncthreads();
-        if (bias && threadIdx.x < 191) ring_put(ring, buckets, c.steps, (int)threadIdx.x + first - (from + 63 + off));
+        if (bias && wave < 3) ring_put(ring, 64 * wave + first - (from + 63 + off), wave, lane);
 
         int now = 0;   // which of the two copies; not known at compile time as in the other kernels, which would cost registers
         for (int qb = from; qb < to; qb += 64, now ^= 1) {
@@ -311,7 +316,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
             if (qb + 64 < to) fetch(1 - now, qb + 64);
             const char *q_now = q_tile[now], *g_now = g_tile[now];
             const int lowest = first - (qb + 63 + off);
-            if (bias && wave == ((qb >> 6) & (kWaves - 1))) ring_next(ring, buckets, c, a.n_buckets, lowest - 64, lane);
+            if (bias && wave == ((qb >> 6) & (kWaves - 1))) ring_put(ring, lowest - 64, wave, lane);
 #pragma unroll 1
             for (int turn = 0; turn < 8 / kWaves; ++turn) {
                 const int b = kWaves == 8 ? wave >> 2 : turn;
@@ -344,7 +349,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (b0 == b1) {
-                    const float add = bias ? buckets.value[b0] : 0.0f;
+                    const float add = bias ? ring.of_bucket[b0] : 0.0f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add));
                 } else {
@@ -388,7 +393,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                         for (int i = 0; i < 8; ++i) v += sk[64 * i + min(lane + 8 * h, 63)];
                         __builtin_amdgcn_wave_barrier();
                     }
-                    add_runs(sums[wave], v, ring.bucket[at + min(lane, 62)], lane);
+                    add_runs(sums[wave], v, ring.bucket[at + min(lane, 62)], ring.bucket[at + min(lane + 1, 62)], lane);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
