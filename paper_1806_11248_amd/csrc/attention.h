@@ -161,6 +161,20 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load_to_lds(to + i * 4096, base, (uint32_t)min(row + i * 4 * kRows, rows - 1) * row_bytes + col);
     }
+    // The first 32 rows likewise, by one wave.
+    static constexpr int kHalfLoads = kPlaces / 2;
+    static __device__ __forceinline__ void fetch_half(char *tile, const char *base, uint32_t row_bytes, int rows, int dim) {
+        const int lane = threadIdx.x & 63;
+        constexpr int kRows = 64 / kPlaces;
+        const uint32_t to = lds_address(tile);
+#pragma unroll
+        for (int i = 0; i < kHalfLoads; ++i) {
+            const int row = i * kRows + lane / kPlaces, col = min(lane % kPlaces ^ fold(row), dim / 8 - 1);
+            load_to_lds(to + i * 1024, base, (uint32_t)min(row, rows - 1) * row_bytes + col * 16);
+        }
+    }
+    // Waits until of this wave's fetches of 32 rows only the last is still under way.
+    static __device__ __forceinline__ void half_ready() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory"); }
     // First operand, rows as they are: row row0 + lane % 32 (row0 a multiple of 32), elements 16 * step + 8 * (lane / 32) .. + 7.
     template <typename P>
     static __device__ __forceinline__ typename P::vec8 rows(const char *tile, int row0, int step, int lane) {
@@ -187,6 +201,8 @@ __device__ __forceinline__ void arrived(V (&regs)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(regs[i]));
 }
+// This wave's LDS reads have their results: what it read may be fetched over.
+__device__ __forceinline__ void done_reading() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // Waits for this wave's fetches, then for the other waves: the tiles fetched last can be read, and those read before written.
 __device__ __forceinline__ void tiles_ready() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

@@ -7,8 +7,9 @@
 
 namespace {
 
-// Workgroups that a call with few query rows is cut into where its keys allow: four for each compute unit.
-constexpr int64_t kFewWorkgroups = 1024;
+// Workgroups that a call with few query rows is cut into where its keys allow, were all sequences the longest: two are on a compute unit at a time, and
+// with eight turns of them the last, partly empty one costs little.  A row's pieces are joined by 256 lanes.
+constexpr int64_t kFewWorkgroups = 4096, kFewPieces = 256;
 
 struct FewPlan {
     int64_t columns, blocks;   // (query, head of the group) pairs of a key head, and workgroups of them
@@ -21,7 +22,7 @@ FewPlan few_plan(const gbt_attention_params &p) {
     f.blocks = (f.columns + kAttnFewRows - 1) / kAttnFewRows;
     const int64_t base = std::max<int64_t>(1, f.blocks * p.kv_heads * p.n_seq);
     const int64_t want = std::max<int64_t>(1, kFewWorkgroups / base);
-    const int64_t len = std::max<int64_t>(1, (p.max_k + want - 1) / want);
+    const int64_t len = std::max<int64_t>(1, std::max((p.max_k + want - 1) / want, (p.max_k + kFewPieces - 1) / kFewPieces));
     f.piece_len = (int)((len + 127) / 128 * 128);
     f.pieces = (int)std::max<int64_t>(1, (p.max_k + f.piece_len - 1) / f.piece_len);
     return f;

@@ -186,19 +186,20 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 // -------------------------------------------------------------------------------------------------------- few rows --
 // Single new events against a long store: what there is to do is to read the store once.  The columns of a wave are the (query, head
 // of the group) pairs of one key head, 32 of them at most, so that all heads that share keys read them together; the four waves of a
-// workgroup take every fourth 32 keys of its piece of the key axis and are joined at its end, the pieces by a second launch.  Keys
-// come from memory in the order of the first operand (a lane reads sixteen bytes of its row), values through a wave's own part
-// of LDS for the transposing reads, so no wave waits for another.
+// workgroup take every fourth 32 keys of its piece of the key axis, each through its own part of LDS, so no wave waits for another.  The next
+// keys are under way as soon as the products with the last have been made, the next values likewise.  The waves are joined at the
+// end, the pieces by a second launch.
 template <typename P, int DP>
-__global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts c) {
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kChunks = DP / 8, kEach = 32 * kChunks / 64;
-    __shared__ __align__(16) char v_tile[4][T::kBytes / 2];
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    constexpr int kJoin = 32 * 33;   // floats of a wave's 32 x 32 block, rows 33 places apart
+    __shared__ __align__(16) char space[4 * T::kBytes >= 16 * kJoin ? 4 * T::kBytes : 16 * kJoin];   // keys and values of the waves; at the end such blocks
     __shared__ uint8_t is_cut[4][64], near_bucket[4][64];
     __shared__ float join_top[4][32], join_sum[4][32];
-    __shared__ float join_o[4][32 * 33];
+    extern __shared__ float table[];   // [n_buckets][32 columns]: the bias, times log2(e)
 
     const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
     const int64_t items = (int64_t)a.pieces * blocks * a.kv_heads * a.n_seq, item = attn_item(items);
@@ -207,15 +208,24 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
     const int kv_head = (int)(item / a.pieces / blocks % a.kv_heads), seq = (int)(item / a.pieces / blocks / a.kv_heads);
     const AttnSeq rows = attn_seq(a, seq);
     const int begin = piece * a.piece_len;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const int column = block * kAttnFewRows + (lane & 31), query = column / a.group, head = kv_head * a.group + column % a.group;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int column = block * kAttnFewRows + col, query = column / a.group, head = kv_head * a.group + column % a.group;
     if (block * kAttnFewRows / a.group >= rows.nq) return;
     if (begin > 0 && begin >= rows.nk) return;   // the first piece writes the rows without keys
     const int off = rows.nk - rows.nq;
     const bool there = query < rows.nq;
     const bool bias = a.n_buckets > 0;
-    const LaneCuts cuts{lane < a.n_buckets - 1 ? c.at[lane] : INT32_MAX, lane + 64 < a.n_buckets - 1 ? c.at[lane + 64] : INT32_MAX};
 
+    const int q_low = block * kAttnFewRows / a.group, q_high = min(rows.nq - 1, (block * kAttnFewRows + kAttnFewRows - 1) / a.group);
+    const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
+    const int end = min(min(rows.nk, begin + a.piece_len), a.causal ? q_high + off + 1 : rows.nk);
+    const int all = a.causal ? min(end, q_low + off + 1) : end;   // every query sees the keys before
+    const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
+    const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
+    char *k_tile = space + wave * (T::kBytes / 2), *v_tile = k_tile + 2 * T::kBytes;
+    auto fetch_k = [&](int kb) { T::fetch_half(k_tile, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim); };
+    auto fetch_v = [&](int kb) { T::fetch_half(v_tile, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim); };
+    const int start = begin + 32 * wave;
     V8 qf[kSteps];
     {
         const char *base = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
@@ -223,13 +233,17 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
         for (int s = 0; s < kSteps; ++s)
             qf[s] = as_vec<V8>(load16(base, (16 * s + 8 * half) * 2, there && 16 * s + 8 * half < a.dim));
     }
-    const int q_low = block * kAttnFewRows / a.group, q_high = min(rows.nq - 1, (block * kAttnFewRows + kAttnFewRows - 1) / a.group);
-    const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
-    const int end = min(min(rows.nk, begin + a.piece_len), a.causal ? q_high + off + 1 : rows.nk);
-    const int all = a.causal ? min(rows.nk, q_low + off + 1) : rows.nk;   // every query sees the keys before
-    const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
-    const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
-    const float *value = a.bias + (there ? head : 0);
+    const LaneCuts cuts{lane < a.n_buckets - 1 ? c.at[lane] : INT32_MAX, lane + 64 < a.n_buckets - 1 ? c.at[lane + 64] : INT32_MAX};
+    if (bias) {
+        const float *from = a.bias + (there ? head : 0);
+        for (int i = 2 * wave + half; i < a.n_buckets; i += 8) table[32 * i + col] = from[(int64_t)i * a.heads] * GBT_LOG2E;
+    }
+    arrived(qf);
+    if (start < end) {
+        fetch_k(start);
+        fetch_v(start);
+    }
+    __syncthreads();   // the table
 
     f32x16 o[kBlocks];
 #pragma unroll
@@ -238,59 +252,40 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
         for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
 
-    i32x4 k_reg[kSteps], v_reg[kEach];
-    auto load = [&](int kb) {
-        const char *kr = k_base + (int64_t)(kb + (lane & 31)) * a.k.row * 2;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) k_reg[s] = load16(kr, (16 * s + 8 * half) * 2, kb + (lane & 31) < end && 16 * s + 8 * half < a.dim);
-        const char *vr = v_base + (int64_t)kb * a.v.row * 2;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = lane + 64 * i, r = at / kChunks, ch = at % kChunks;
-            v_reg[i] = load16(vr, r * a.v.row * 2 + ch * 16, kb + r < end && ch * 8 < a.dim);
-        }
-    };
-    const int start = begin + 32 * wave;
-    if (start < end) load(start);
     for (int kb = start; kb < end; kb += 128) {
+        T::half_ready();   // the keys; the values after them are still under way
         f32x16 s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) s = P::mma(as_vec<V8>(k_reg[i]), qf[i], s);
-        // a wave's LDS reads and writes are done in their order: the values of the step before have been read
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = lane + 64 * i, r = at / kChunks, ch = at % kChunks;
-            *(i32x4 *)(v_tile[wave] + r * T::kRowBytes + ((ch ^ T::fold(r)) << 4)) = v_reg[i];
-        }
-        __builtin_amdgcn_wave_barrier();
-        if (kb + 128 < end) load(kb + 128);
+        for (int i = 0; i < kSteps; ++i) s = P::mma(T::template rows<P>(k_tile, 0, i, lane), qf[i], s);
+        done_reading();
+        fetch_k(min(kb + 128, end - 1));   // after the last step some key again, so that the count of loads under way stays the same
         const int lowest = kb - (q_high + off), span = 31 + q_high - q_low;   // distances lowest .. lowest + span, 63 at most
-        int mine = bias ? lane_bucket(is_cut[wave], cuts, lowest, lane) : 0;
+        const int mine = bias ? lane_bucket(is_cut[wave], cuts, lowest, lane) : 0;
         const int b0 = __builtin_amdgcn_readfirstlane(mine), b1 = __builtin_amdgcn_readlane(mine, span);
-        if (b0 == b1) {
-            const float add = bias ? value[(int64_t)b0 * a.heads] * GBT_LOG2E : 0.0f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, add);
-        } else {
+        float factor = a.scale2, add = 0.0f;
+        if (b0 != b1) {
             near_bucket[wave][lane] = (uint8_t)mine;
             __builtin_amdgcn_wave_barrier();
             const uint8_t *at = near_bucket[wave] + (there ? q_high - query : 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, value[(int64_t)at[result_row(r, half)] * a.heads] * GBT_LOG2E);
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, table[32 * at[result_row(r, half)] + col]);
+            factor = 1.0f;
+        } else if (bias) {
+            add = table[32 * b0 + col];
         }
-        if (kb + 32 > min(all, end)) {
+        if (kb + 32 > all) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = kb + result_row(r, half);
                 s[r] = key <= last && key < end ? s[r] : -INFINITY;
             }
         }
-        float now = top;
+        float now = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) now = fmaxf(now, s[r]);
-        now = column_max(now);
+        now = fmaxf(top, column_max(fmaf(now, factor, add)));
         if (__any(now > top + kSlack)) {
             const float shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.0f : now));
             sum *= shrink;
@@ -300,19 +295,23 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
                 for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
             top = now;
         }
-        const float base = top == -INFINITY ? 0.0f : top;
+        add -= top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], factor, add));
             sum += s[r];
         }
+        T::half_ready();   // the values; the next keys are under way
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const V8 p = operand<P>(s, i);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile[wave], 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile, 16 * i, b, lane), p, o[b]);
         }
+        done_reading();
+        fetch_v(min(kb + 128, end - 1));
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
     // the four waves' rows together
     sum = column_sum(sum);
@@ -321,7 +320,6 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
         join_sum[wave][lane] = sum;
     }
     __syncthreads();
-    const int col = lane & 31;
     float all_top = -INFINITY, all_sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) all_top = fmaxf(all_top, join_top[w][col]);
@@ -339,18 +337,19 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
             a.part[part + a.dim + 1] = all_sum;
         }
     }
+    // a block of 32 elements after the other
+    float *join_o = (float *)space;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
         if (b) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) join_o[wave][col * 33 + result_row(r, half)] = o[b][r] * factor;
+        for (int r = 0; r < 16; ++r) join_o[wave * kJoin + col * 33 + result_row(r, half)] = o[b][r] * factor;
         __syncthreads();
-        // thread: elements d, d + 8, .. of a column
         for (int i = threadIdx.x; i < 32 * 32; i += 256) {
             const int cc = i >> 5, d = 32 * b + (i & 31), column2 = block * kAttnFewRows + cc, query2 = column2 / a.group;
             if (query2 >= rows.nq || d >= a.dim) continue;
             const int x = cc * 33 + (i & 31);
-            const float w = (join_o[0][x] + join_o[1][x]) + (join_o[2][x] + join_o[3][x]);
+            const float w = (join_o[x] + join_o[kJoin + x]) + (join_o[2 * kJoin + x] + join_o[3 * kJoin + x]);
             const int head2 = kv_head * a.group + column2 % a.group;
             if (whole) {
                 const E y = (E)w;
@@ -363,44 +362,57 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a, AttnCuts
     }
 }
 
-// The pieces of the key axis together: a wave takes a (sequence, key head, column), its lanes the elements.
+// The pieces of the key axis together: a workgroup takes a (sequence, key head, column), a wave every fourth piece of it, its lanes the elements.
 template <typename P>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
     typedef typename P::elem E;
-    const int columns = a.group * a.max_q;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= (int64_t)a.n_seq * a.kv_heads * columns) return;
-    const int lane = threadIdx.x & 63;
-    const int column = (int)(at % columns), kv_head = (int)(at / columns % a.kv_heads), seq = (int)(at / columns / a.kv_heads);
+    __shared__ float join_top[4], join_sum[4], join_o[4][128];
+    const int columns = a.group * a.max_q, at = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int column = at % columns, kv_head = at / columns % a.kv_heads, seq = at / columns / a.kv_heads;
     const int query = column / a.group, head = kv_head * a.group + column % a.group;
     const AttnSeq rows = attn_seq(a, seq);
     if (query >= rows.nq) return;
-    const int n = max(1, (rows.nk + a.piece_len - 1) / a.piece_len);
-    const float *part = a.part + at * a.pieces * (a.dim + 2);
-    float top = -INFINITY;
-    for (int p = lane; p < n; p += 64) top = fmaxf(top, part[(int64_t)p * (a.dim + 2) + a.dim]);
+    const int n = max(1, (rows.nk + a.piece_len - 1) / a.piece_len), wide = a.dim + 2;
+    const float *part = a.part + (int64_t)at * a.pieces * wide;
+    // a lane's piece of this wave's, 64 of them at most
+    const int mine = wave + 4 * lane;
+    const float top = mine < n ? part[(int64_t)mine * wide + a.dim] : -INFINITY, sum = mine < n ? part[(int64_t)mine * wide + a.dim + 1] : 0.0f;
+    float most = top;
 #pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int p = 0; p < n; ++p) {
-        const float *x = part + (int64_t)p * (a.dim + 2);
-        const float f = __builtin_amdgcn_exp2f(x[a.dim] - base);
-        sum += x[a.dim + 1] * f;
-        if (lane < a.dim) o0 += x[lane] * f;
-        if (lane + 64 < a.dim) o1 += x[lane + 64] * f;
+    for (int s = 32; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    const float base = most == -INFINITY ? 0.0f : most, factor = __builtin_amdgcn_exp2f(top - base), total = wave_sum(sum * factor);
+    float o0 = 0.0f, o1 = 0.0f;
+    const int d0 = min(lane, a.dim - 1), d1 = min(lane + 64, a.dim - 1);
+#pragma unroll 8
+    for (int p = wave; p < n; p += 4) {
+        const float f = __shfl(factor, p >> 2);
+        o0 = fmaf(part[(int64_t)p * wide + d0], f, o0);
+        o1 = fmaf(part[(int64_t)p * wide + d1], f, o1);
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
-    if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * GBT_LN2;
-    E *out = (E *)a.out.data + (rows.q0 + query) * a.out.row + (int64_t)head * a.out.head;
-    E *rest = (E *)a.rest + ((rows.q0 + query) * a.heads + head) * a.dim;
-    auto put = [&](int d, float w) {
-        const E y = (E)w;
-        out[d] = y;
-        if (a.rest) rest[d] = (E)(w - (float)y);
-    };
-    if (lane < a.dim) put(lane, o0 * inv);
-    if (lane + 64 < a.dim) put(lane + 64, o1 * inv);
+    join_o[wave][lane] = o0;
+    join_o[wave][lane + 64] = o1;
+    if (lane == 0) {
+        join_top[wave] = most;
+        join_sum[wave] = total;
+    }
+    __syncthreads();
+    const float all = fmaxf(fmaxf(join_top[0], join_top[1]), fmaxf(join_top[2], join_top[3])), all_base = all == -INFINITY ? 0.0f : all;
+    float w[4], l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(join_top[i] - all_base);
+        l = fmaf(join_sum[i], w[i], l);
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    if (a.lse && threadIdx.x == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = l == 0.0f ? -INFINITY : (all + __builtin_amdgcn_logf(l)) * GBT_LN2;
+    if ((int)threadIdx.x < a.dim) {
+        const int d = threadIdx.x;
+        const float x = ((join_o[0][d] * w[0] + join_o[1][d] * w[1]) + (join_o[2][d] * w[2] + join_o[3][d] * w[3])) * inv;
+        const E y = (E)x;
+        ((E *)a.out.data)[(rows.q0 + query) * a.out.row + (int64_t)head * a.out.head + d] = y;
+        if (a.rest) ((E *)a.rest)[((rows.q0 + query) * a.heads + head) * a.dim + d] = (E)(x - (float)y);
+    }
 }
 
 unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
@@ -415,11 +427,11 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
 template <typename P, int DP>
 hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t columns = (int64_t)a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
-    attention_few_kernel<P, DP><<<grid_of(a.pieces * blocks * a.kv_heads * a.n_seq), 256, 0, stream>>>(a, c);
+    attention_few_kernel<P, DP><<<grid_of(a.pieces * blocks * a.kv_heads * a.n_seq), 256, a.n_buckets * 32 * sizeof(float), stream>>>(a, c);
     if (a.pieces > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        attention_join_kernel<P><<<(unsigned)((columns * a.kv_heads * a.n_seq + 3) / 4), 256, 0, stream>>>(a);
+        attention_join_kernel<P><<<(unsigned)(columns * a.kv_heads * a.n_seq), 256, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
