@@ -7,6 +7,7 @@ MI355X, loading or ``Context()`` raises.
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes as C
 import os
@@ -93,6 +94,7 @@ class Gradient(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
+_NO_STREAM = contextlib.nullcontext()
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # GBT_F32, GBT_BF16, GBT_F16
 
 _TREE_FIELDS = [("feature", np.int32), ("bin", np.int32), ("default_left", np.int32), ("left", np.int32),
@@ -273,14 +275,17 @@ def distance_cuts(n_buckets: int, far: int, causal: bool = True) -> list:
     return [-s for s in reversed(steps)] + [s + 1 for s in steps[:n - back]]
 
 
-def _heads(t, name, dtype, heads=None):
+def _heads(t, name, dtype, rows=None, heads=None, dim=None):
     """gbt_heads of a tensor [rows][heads][head_dim] whose last axis is contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 3 and (t.stride(2) == 1 or t.numel() == 0)):
-        raise TypeError(f"{name}: expected a CUDA tensor [rows][heads][head_dim] of {dtype} with a contiguous last axis")
-    if heads is not None and t.shape[1:] != heads:
-        raise TypeError(f"{name}: expected [rows][{heads[0]}][{heads[1]}], not {tuple(t.shape)}")
-    rows, h, d = t.shape     # an axis of one element has no stride to speak of
-    return Heads(t.data_ptr(), t.stride(0) if rows > 1 else h * d, t.stride(1) if h > 1 else d)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 3):
+        raise TypeError(f"{name}: expected a CUDA tensor [rows][heads][head_dim] of {dtype}")
+    n, h, d = t.shape
+    if (rows is not None and n != rows) or (heads is not None and h != heads) or (dim is not None and d != dim):
+        raise TypeError(f"{name}: expected [{rows}][{heads}][{dim}], not {tuple(t.shape)}")
+    row, head, one = t.stride()
+    if one != 1 and n and h and d > 1:
+        raise TypeError(f"{name}: expected a contiguous last axis")
+    return Heads(t.data_ptr(), row if n > 1 else h * d, head if h > 1 else d)     # an axis of one element has no stride to speak of
 
 
 class GradientList:
@@ -288,6 +293,7 @@ class GradientList:
 
     def __init__(self, tensors, outs, table, pieces):
         self.tensors, self.outs, self.table, self.pieces = tensors, outs, table, pieces
+        self.both = tensors + outs + [table]
 
 
 class Context:
@@ -648,33 +654,44 @@ class Context:
         return margin
 
     # -- rows with a history ---------------------------------------------------
-    def _on_stream(self, *tensors):
-        """Outputs are allocated on the context's stream.  Where that is not torch's current one, the inputs' memory is
-        kept from reuse until this call's work is done (waiting for their contents is the caller's, as for every call)."""
-        if torch.cuda.current_stream(self.device) == self.stream:
-            return contextlib.nullcontext()
+    def _on_stream(self, tensors=()):
+        """None where the context's stream is torch's current one.  Else outputs are to be allocated on it, within the manager returned, and
+        the inputs' memory is kept from reuse until this call's work is done (waiting for their contents is the caller's, as for every
+        call)."""
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self.stream.cuda_stream:
+            return None
         for t in tensors:
             if t is not None:
                 t.record_stream(self.stream)
         return torch.cuda.stream(self.stream)
 
     def _attention_params(self, q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts):
+        """(gbt_attention_params, what it points to on the host)."""
+        if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3):
+            raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
         rows, heads, dim = q.shape
-        n_seq = 1
-        for nm, t, dt in (("q_ptr", q_ptr, torch.int64), ("k_ptr", k_ptr, torch.int64), ("k_len", k_len, torch.int32)):
+        k_rows, kv_heads, _ = k.shape
+        n_seq = None
+        if q_ptr is not None:
+            n_seq = _need(q_ptr, torch.int64, "q_ptr").numel() - 1
+        for t, dtype, extra, name in ((k_ptr, torch.int64, 1, "k_ptr"), (k_len, torch.int32, 0, "k_len")):
             if t is not None:
-                _need(t, dt, nm)
-                n_seq = t.numel() - (nm != "k_len")
-        for nm, t in (("q_ptr", q_ptr), ("k_ptr", k_ptr), ("k_len", k_len)):
-            if t is not None and t.numel() - (nm != "k_len") != n_seq:
-                raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
-        for nm, ptr, t, longest in (("q", q_ptr, q, max_q), ("k", k_ptr, k, max_k)):
-            if ptr is None and (t.shape[0] % max(1, n_seq) or longest not in (None, t.shape[0] // max(1, n_seq))):
-                raise TypeError(f"{nm}: without {nm}_ptr all of {n_seq} sequences have the same length")
-        if max_q is None:
-            max_q = rows if q_ptr is not None else rows // max(1, n_seq)
-        if max_k is None:
-            max_k = k.shape[0] if k_ptr is not None else k.shape[0] // max(1, n_seq)
+                n = _need(t, dtype, name).numel() - extra
+                if n_seq is not None and n != n_seq:
+                    raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
+                n_seq = n
+        if n_seq is None:
+            n_seq = 1
+        if q_ptr is None:
+            each = rows // max(1, n_seq)
+            if each * n_seq != rows or max_q not in (None, each):
+                raise TypeError(f"q: without q_ptr all of {n_seq} sequences have the same length")
+            max_q = each
+        if k_ptr is None:
+            each = k_rows // max(1, n_seq)
+            if each * n_seq != k_rows or max_k not in (None, each):
+                raise TypeError(f"k: without k_ptr all of {n_seq} sequences have the same length")
+            max_k = each
         n_buckets, table, edges = 0, None, None
         if bias is not None:
             _need(bias, torch.float32, "bias")
@@ -683,12 +700,12 @@ class Context:
             n_buckets, table = bias.shape[0], bias.data_ptr()
             if cuts is None or len(cuts) != n_buckets - 1:
                 raise TypeError(f"cuts: expected {n_buckets - 1} of them")
-            edges = (C.c_int32 * max(1, n_buckets - 1))(*(cuts.tolist() if hasattr(cuts, "tolist") else cuts))
-        p = AttentionParams(DTYPES.get(q.dtype, -1), heads, k.shape[1], dim, n_seq, max_q, max_k, int(causal), n_buckets,
-                            dim ** -0.5 if scale is None else scale, rows, k.shape[0], None if q_ptr is None else q_ptr.data_ptr(),
+            edges = array.array("i", cuts.tolist() if hasattr(cuts, "tolist") else cuts)
+        p = AttentionParams(DTYPES.get(q.dtype, -1), heads, kv_heads, dim, n_seq, rows if max_q is None else max_q, k_rows if max_k is None else max_k,
+                            causal, n_buckets, dim ** -0.5 if scale is None else scale, rows, k_rows, None if q_ptr is None else q_ptr.data_ptr(),
                             None if k_ptr is None else k_ptr.data_ptr(), None if k_len is None else k_len.data_ptr(), table,
-                            None if edges is None else C.addressof(edges))
-        return p, edges      # edges: alive as long as the parameters
+                            None if edges is None else edges.buffer_info()[0])
+        return p, edges
 
     def attention(self, q, k, v, *, q_ptr=None, k_ptr=None, k_len=None, max_q=None, max_k=None, causal=False, scale=None,
                   bias=None, cuts=None, save=False, out=None):
@@ -700,56 +717,58 @@ class Context:
         bias, cuts    float32 [n_buckets][heads] and the ascending cuts between buckets of distance, on the host
         save          also return what attention_backward needs: (out, saved)
         """
-        if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
-            raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
-        p, keep = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
-        hq = _heads(q, "q", q.dtype)
-        hk, hv = _heads(k, "k", q.dtype, (k.shape[1], q.shape[2])), _heads(v, "v", q.dtype, (k.shape[1], q.shape[2]))
-        if v.shape[0] != k.shape[0]:
-            raise TypeError("v: expected as many rows as k")
-        if out is not None and out.shape != q.shape:
-            raise TypeError(f"out: expected {tuple(q.shape)}")
-        ws_bytes = self.lib.gbt_attention_workspace_bytes(C.byref(p))
-        with self._on_stream(q, k, v, q_ptr, k_ptr, k_len, bias, out):
+        p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
+        dtype = q.dtype
+        rows, heads, dim = q.shape
+        k_rows, kv_heads, _ = k.shape
+        hq, hk, hv = _heads(q, "q", dtype), _heads(k, "k", dtype, k_rows, kv_heads, dim), _heads(v, "v", dtype, k_rows, kv_heads, dim)
+        lib, at = self.lib, C.byref(p)
+        ws_bytes = lib.gbt_attention_workspace_bytes(at)
+        lse = rest = None
+        with self._on_stream((q, k, v, q_ptr, k_ptr, k_len, bias, out)) or _NO_STREAM:
             if out is None:
-                out = self.empty(q.shape, q.dtype)
-            lse = self.empty((q.shape[1], q.shape[0]), torch.float32) if save else None
-            rest = self.empty(q.shape, q.dtype) if save else None
+                out = self.empty((rows, heads, dim), dtype)
+            if save:
+                lse, rest = self.empty((heads, rows), torch.float32), self.empty((rows, heads, dim), dtype)
             ws = self.workspace("attention", ws_bytes) if ws_bytes else None
-        ho = _heads(out, "out", q.dtype)
-        self._check(self.lib.gbt_attention(self.h, C.byref(p), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), _ptr(lse), _ptr(rest),
-                                           _ptr(ws), 0 if ws is None else ws.numel()))
+        ho = _heads(out, "out", dtype, rows, heads, dim)
+        st = lib.gbt_attention(self.h, at, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr() if save else None,
+                               rest.data_ptr() if save else None, ws.data_ptr() if ws_bytes else None, ws_bytes)
+        if st:
+            self._check(st)
         return (out, (lse, rest)) if save else out
 
     def attention_backward(self, dout, q, k, v, out, saved, *, q_ptr=None, k_ptr=None, k_len=None, max_q=None, max_k=None, causal=False,
                            scale=None, bias=None, cuts=None):
         """(dq, dk, dv, dbias) of attention(..., save=True) with the same arguments; dbias is None without a bias.  Rows of k and v
         that no sequence uses get zeros."""
-        if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
-            raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
-        p, keep = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
+        p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
+        dtype = q.dtype
+        rows, heads, dim = q.shape
+        k_rows, kv_heads, _ = k.shape
         lse, rest = saved
         _need(lse, torch.float32, "saved[0]")
         if rest is not None:
-            _need(rest, q.dtype, "saved[1]")
-        if lse.shape != (q.shape[1], q.shape[0]) or (rest is not None and rest.shape != q.shape):
+            _need(rest, dtype, "saved[1]")
+        if lse.shape != (heads, rows) or (rest is not None and rest.shape != q.shape):
             raise TypeError(f"saved: not of a call with q of {tuple(q.shape)}")
-        like_q, like_k = tuple(q.shape[1:]), (k.shape[1], q.shape[2])
-        for nm, t, n in (("dout", dout, q.shape[0]), ("out", out, q.shape[0]), ("v", v, k.shape[0])):
-            if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[0] != n:
-                raise TypeError(f"{nm}: expected {n} rows")
-        views = [_heads(dout, "dout", q.dtype, like_q), _heads(q, "q", q.dtype), _heads(k, "k", q.dtype, like_k), _heads(v, "v", q.dtype, like_k),
-                 _heads(out, "out", q.dtype, like_q)]
-        ws_bytes = self.lib.gbt_attention_backward_workspace_bytes(C.byref(p))
-        with self._on_stream(dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias):
-            dq = self.empty(q.shape, q.dtype)
-            rows = torch.empty if k_len is None else torch.zeros
-            dk, dv = (rows(k.shape, dtype=q.dtype, device=self.device) for _ in range(2))
+        hg, hq, ho = (_heads(t, n, dtype, rows, heads, dim) for t, n in ((dout, "dout"), (q, "q"), (out, "out")))
+        hk, hv = _heads(k, "k", dtype, k_rows, kv_heads, dim), _heads(v, "v", dtype, k_rows, kv_heads, dim)
+        lib, at = self.lib, C.byref(p)
+        ws_bytes = lib.gbt_attention_backward_workspace_bytes(at)
+        with self._on_stream((dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias)) or _NO_STREAM:
+            dq = self.empty((rows, heads, dim), dtype)
+            make = torch.empty if k_len is None else torch.zeros
+            dk = make((k_rows, kv_heads, dim), dtype=dtype, device=self.device)
+            dv = make((k_rows, kv_heads, dim), dtype=dtype, device=self.device)
             dbias = None if bias is None else self.empty(bias.shape, torch.float32)
             ws = self.workspace("attention", ws_bytes)
-        grads = [_heads(dq, "dq", q.dtype), _heads(dk, "dk", q.dtype), _heads(dv, "dv", q.dtype)]
-        self._check(self.lib.gbt_attention_backward(self.h, C.byref(p), *[C.byref(x) for x in views], _ptr(lse), _ptr(rest),
-                                                    *[C.byref(x) for x in grads], _ptr(dbias), _ptr(ws), ws.numel()))
+        hdq, hdk, hdv = Heads(dq.data_ptr(), heads * dim, dim), Heads(dk.data_ptr(), kv_heads * dim, dim), Heads(dv.data_ptr(), kv_heads * dim, dim)
+        st = lib.gbt_attention_backward(self.h, at, C.byref(hg), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr(),
+                                        None if rest is None else rest.data_ptr(), C.byref(hdq), C.byref(hdk), C.byref(hdv),
+                                        None if dbias is None else dbias.data_ptr(), ws.data_ptr(), ws.numel())
+        if st:
+            self._check(st)
         return dq, dk, dv, dbias
 
     def gradient_list(self, tensors, outs=None) -> GradientList:
@@ -768,7 +787,7 @@ class Context:
                 raise TypeError(f"outs[{i}]: expected {t.numel()} elements")
             arr[i] = Gradient(t.data_ptr(), o.data_ptr(), t.numel(), DTYPES[t.dtype])
         nbytes = self.lib.gbt_gradient_list_bytes(arr, len(tensors))
-        with self._on_stream():
+        with self._on_stream() or _NO_STREAM:
             table = self.empty((max(16, nbytes),), torch.uint8)
         pieces = C.c_int32()
         self._check(self.lib.gbt_gradient_list(self.h, arr, len(tensors), _ptr(table), table.numel(), C.byref(pieces)))
@@ -777,8 +796,10 @@ class Context:
     def clip_gradients(self, gradients: GradientList, max_norm: float):
         """Scales every tensor of the list by min(1, max_norm / (norm + 1e-6)) into its out; returns the global norm, a float32 scalar
         on the device.  A norm that is not finite leaves the values as they are."""
-        with self._on_stream(*gradients.tensors, *gradients.outs):
+        with self._on_stream(gradients.both) or _NO_STREAM:
             norm = self.empty((), torch.float32)
             ws = self.workspace("clip", 16384)
-        self._check(self.lib.gbt_clip_gradients(self.h, _ptr(gradients.table), gradients.pieces, max_norm, _ptr(norm), _ptr(ws), ws.numel()))
+        st = self.lib.gbt_clip_gradients(self.h, gradients.table.data_ptr(), gradients.pieces, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel())
+        if st:
+            self._check(st)
         return norm

@@ -8,8 +8,12 @@
 namespace {
 
 // Workgroups that a call with few query rows is cut into where its keys allow, were all sequences the longest: two are on a compute unit at a time, and
-// with eight turns of them the last, partly empty one costs little.  A row's pieces are joined by 256 lanes.
-constexpr int64_t kFewWorkgroups = 4096, kFewPieces = 256;
+// with four turns of them the last, partly empty one costs little.  A row's pieces are joined by 256 lanes.  (Stores of 2000 to 30000 rows, kernel and
+// join, for 1024, 2048, 4096, 8192: 124, 126, 132, 157 us; few events for 64 rows 54, 53, 57, 67.)
+constexpr int64_t kFewWorkgroups = 2048, kFewPieces = 256;
+// Shorter pieces cost more by their beginnings and ends than they gain by being many: 32 stores of 1000 rows, 8 heads of 128 elements, at least 256, 512,
+// 1024 rows a piece: 32, 29, 25 us; 4 of 2000, 2 heads of 64: 9.3, 10.3, 12.3; 4 of 500: 9.2, 7.0, 7.0.
+constexpr int64_t kFewLeast = 1024;
 
 struct FewPlan {
     int64_t columns, blocks;   // (query, head of the group) pairs of a key head, and workgroups of them
@@ -23,7 +27,7 @@ FewPlan few_plan(const gbt_attention_params &p) {
     const int64_t base = std::max<int64_t>(1, f.blocks * p.kv_heads * p.n_seq);
     const int64_t want = std::max<int64_t>(1, kFewWorkgroups / base);
     const int64_t len = std::max<int64_t>(1, std::max((p.max_k + want - 1) / want, (p.max_k + kFewPieces - 1) / kFewPieces));
-    f.piece_len = (int)((len + 127) / 128 * 128);
+    f.piece_len = (int)((std::max(len, kFewLeast) + 127) / 128 * 128);
     f.pieces = (int)std::max<int64_t>(1, (p.max_k + f.piece_len - 1) / f.piece_len);
     return f;
 }

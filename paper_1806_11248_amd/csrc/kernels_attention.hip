@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     const float base = all_top == -INFINITY ? 0.0f : all_top;
 #pragma unroll
     for (int w = 0; w < 4; ++w) all_sum += join_sum[w][col] * __builtin_amdgcn_exp2f(join_top[w][col] - base);
-    const bool whole = a.pieces == 1;
+    const bool whole = rows.nk <= a.piece_len;   // a sequence of one piece needs no joining
     const float factor = __builtin_amdgcn_exp2f(top - base) * (whole ? all_sum > 0.0f ? 1.0f / all_sum : all_sum == 0.0f ? 0.0f : all_sum : 1.0f);
     const int64_t part = ((((int64_t)seq * a.kv_heads + kv_head) * columns + column) * a.pieces + piece) * (a.dim + 2);
     if (wave == 0 && half == 0 && there) {
@@ -373,7 +373,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
     const int query = column / a.group, head = kv_head * a.group + column % a.group;
     const AttnSeq rows = attn_seq(a, seq);
     if (query >= rows.nq) return;
-    const int n = max(1, (rows.nk + a.piece_len - 1) / a.piece_len), wide = a.dim + 2;
+    const int n = (rows.nk + a.piece_len - 1) / a.piece_len, wide = a.dim + 2;
+    if (n < 2) return;
     const float *part = a.part + (int64_t)at * a.pieces * wide;
     // a lane's piece of this wave's, 64 of them at most
     const int mine = wave + 4 * lane;
