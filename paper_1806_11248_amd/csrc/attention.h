@@ -24,6 +24,7 @@ struct AttnArgs {
     const int32_t *k_len;           // NULL: all of a sequence's key rows are used
     int64_t q_rows, k_rows;
     int n_seq, heads, kv_heads, group, dim, max_q, max_k, causal, n_buckets;
+    int stretch;                    // see attn_item
     float scale, scale2;            // scale2 = scale * log2(e): probabilities are powers of two here
     const float *bias;              // [n_buckets][heads]
     float *lse;                     // [heads][q_rows], natural logarithm, or NULL
@@ -39,6 +40,15 @@ struct AttnArgs {
     float *part;
     int pieces, piece_len;
 };
+
+// The stretch for `blocks` blocks of each of `units` units (heads, or key heads and parts) of a sequence.  Sequences are as long as they are, so
+// no XCD is to have more of one than another: an eighth of each where units divide so; else whole units where there are many, single blocks
+// where there are not.  (24 histories of 100 to 1000 rows, 8 heads: an eighth of all items in a row for each XCD 58 us,
+// so 48.)
+inline int attn_stretch(int64_t units, int64_t blocks, int64_t n_seq) {
+    return (int)(units % 8 == 0 ? units / 8 * blocks : units * n_seq >= 64 ? blocks : 1);
+}
+inline unsigned attn_grid(int64_t items, int stretch) { return (unsigned)((items + 8 * (int64_t)stretch - 1) / (8 * (int64_t)stretch) * 8 * stretch); }
 
 struct AttnCuts {
     int32_t at[kAttnBuckets - 1];   // ascending
@@ -112,10 +122,11 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s) {
     return r;
 }
 
-// Workgroups go to the eight XCDs in turn; the items of one stretch of the order share keys, so each XCD takes a stretch.
-__device__ __forceinline__ int64_t attn_item(int64_t items) {
-    const int64_t each = (items + 7) / 8;
-    return (int64_t)(blockIdx.x % 8) * each + blockIdx.x / 8;
+// Workgroups go to the eight XCDs in turn.  Items of one stretch of the order share keys (or queries), so an XCD takes `stretch` of them, the next
+// stretch the next XCD.
+__device__ __forceinline__ int64_t attn_item(int stretch) {
+    const int64_t at = blockIdx.x / 8;
+    return (at / stretch * 8 + blockIdx.x % 8) * stretch + at % stretch;
 }
 
 // Sixteen bytes of a row, or zeros where the row or the elements do not exist.

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     __shared__ DistanceRing ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
-    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(items);
+    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
     if (item >= items) return;
     // the blocks that see the most keys first
     const int block = q_blocks - 1 - (int)(item % q_blocks), head = (int)(item / q_blocks % a.heads), seq = (int)(item / q_blocks / a.heads);
@@ -202,8 +202,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     extern __shared__ float table[];   // [n_buckets][32 columns]: the bias, times log2(e)
 
     const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
-    const int64_t items = (int64_t)a.pieces * blocks * a.kv_heads * a.n_seq, item = attn_item(items);
-    if (item >= items) return;
+    const int64_t item = blockIdx.x;
     const int piece = (int)(item % a.pieces), block = (int)(item / a.pieces % blocks);
     const int kv_head = (int)(item / a.pieces / blocks % a.kv_heads), seq = (int)(item / a.pieces / blocks / a.kv_heads);
     const AttnSeq rows = attn_seq(a, seq);
@@ -416,19 +415,19 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
     }
 }
 
-unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
-
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
-    attention_kernel<P, DP><<<grid_of(blocks * a.heads * a.n_seq), 256, 0, stream>>>(a, c);
+    AttnArgs b = a;
+    b.stretch = attn_stretch(a.heads, blocks, a.n_seq);
+    attention_kernel<P, DP><<<attn_grid(blocks * a.heads * a.n_seq, b.stretch), 256, 0, stream>>>(b, c);
     return hipGetLastError();
 }
 
 template <typename P, int DP>
 hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t columns = (int64_t)a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
-    attention_few_kernel<P, DP><<<grid_of(a.pieces * blocks * a.kv_heads * a.n_seq), 256, a.n_buckets * 32 * sizeof(float), stream>>>(a, c);
+    attention_few_kernel<P, DP><<<(unsigned)(a.pieces * blocks * a.kv_heads * a.n_seq), 256, a.n_buckets * 32 * sizeof(float), stream>>>(a, c);
     if (a.pieces > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

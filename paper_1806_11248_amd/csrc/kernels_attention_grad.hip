@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     __shared__ DistanceRing ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
-    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(items);
+    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
     if (item >= items) return;
     const int block = q_blocks - 1 - (int)(item % q_blocks), head = (int)(item / q_blocks % a.heads), seq = (int)(item / q_blocks / a.heads);
     const AttnSeq rows = attn_seq(a, seq);
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
 
     const int k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries, parts = a.head_parts * a.q_parts;
-    const int64_t items = (int64_t)k_blocks * parts * a.kv_heads * a.n_seq, item = attn_item(items);
+    const int64_t items = (int64_t)k_blocks * parts * a.kv_heads * a.n_seq, item = attn_item(a.stretch);
     if (item >= items) return;
     const int block = (int)(item % k_blocks), part = (int)(item / k_blocks % parts);
     const int kv_head = (int)(item / k_blocks / parts % a.kv_heads), seq = (int)(item / k_blocks / parts / a.kv_heads);
@@ -530,19 +530,22 @@ __global__ __launch_bounds__(256) void grad_bias_kernel(AttnArgs a) {
     }
 }
 
-unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
-
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries, k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
     hipError_t e = hipSuccess;
     if (q_blocks > 0 && a.n_seq > 0) {
-        grad_queries_kernel<P, DP><<<grid_of(q_blocks * a.heads * a.n_seq), 256, 0, stream>>>(a, c);
+        AttnArgs b = a;
+        b.stretch = attn_stretch(a.heads, q_blocks, a.n_seq);
+        grad_queries_kernel<P, DP><<<attn_grid(q_blocks * a.heads * a.n_seq, b.stretch), 256, 0, stream>>>(b, c);
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {
         constexpr int kWaves = DP == 128 ? 8 : 4;
-        grad_keys_kernel<P, DP, kWaves><<<grid_of(k_blocks * a.head_parts * a.q_parts * a.kv_heads * a.n_seq), 64 * kWaves, 0, stream>>>(a, c);
+        const int64_t units = (int64_t)a.kv_heads * a.head_parts * a.q_parts;
+        AttnArgs b = a;
+        b.stretch = attn_stretch(units, k_blocks, a.n_seq);
+        grad_keys_kernel<P, DP, kWaves><<<attn_grid(k_blocks * units * a.n_seq, b.stretch), 64 * kWaves, 0, stream>>>(b, c);
         e = hipGetLastError();
         if (e == hipSuccess && a.head_parts * a.q_parts > 1) {
             grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 3) / 4 * a.n_seq), 256, 0, stream>>>(a);
