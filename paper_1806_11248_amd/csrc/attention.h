@@ -31,8 +31,8 @@ struct AttnArgs {
     char *rest;                     // what rounding took from out, [q_rows][heads][dim], or NULL
     // backward
     AttnView dout, dq, dk, dv;
-    float *row_start;               // [heads][q_rows]: what a row's products with the keys are added to, -lse / scale (-inf: a row without keys)
-    float *row_minus;               // [heads][q_rows]: and its products of gradients with values, -delta
+    float *row_less;                // [heads][q_rows]: what a row's scores lose, -lse * log2(e) (-inf: a row without keys)
+    float *row_minus;               // [heads][q_rows]: and what its products of gradients with values are added to, -delta
     float *strips;                  // [heads][n_seq * k_blocks * q_parts][n_buckets]: the bias gradient of each block of keys
     float *dbias;                   // [n_buckets][heads]
     int head_parts, q_parts;        // a block of keys is shared by so many workgroups: by heads of the group, by queries
@@ -48,6 +48,11 @@ struct AttnArgs {
 inline int attn_stretch(int64_t units, int64_t blocks, int64_t n_seq) {
     return (int)(units % 8 == 0 ? units / 8 * blocks : units * n_seq >= 64 ? blocks : 1);
 }
+// Where a launch has no more workgroups than there are compute units and its keys are several tiles, two groups of four waves share a workgroup's
+// queries and take the tiles in turn.  us forward and backward with one group and two (causal): 64 workgroups, 500 keys 13.4 + 45.8, 12.4 + 44.6;
+// 256, 1000 keys 22.3 + 85.1, 19.4 + 80.3; 256, 2000 keys of 128 elements 48.9 + 217.8, 41.3 + 181.1; but 512, 1000 keys 44.3 + 193, 53.4 + 199;
+// 4, 100 keys 7.1 + 23.8, 7.7 + 24.8.
+inline bool attn_two_groups(int64_t workgroups, int64_t max_k) { return workgroups <= 256 && max_k >= 256; }
 inline unsigned attn_grid(int64_t items, int stretch) { return (unsigned)((items + 8 * (int64_t)stretch - 1) / (8 * (int64_t)stretch) * 8 * stretch); }
 
 struct AttnCuts {
@@ -129,11 +134,16 @@ __device__ __forceinline__ int64_t attn_item(int stretch) {
     return (at / stretch * 8 + blockIdx.x % 8) * stretch + at % stretch;
 }
 
-// Sixteen bytes of a row, or zeros where the row or the elements do not exist.
-__device__ __forceinline__ i32x4 load16(const char *base, int64_t byte, bool there) {
-    i32x4 z = {0, 0, 0, 0};
-    if (there) z = *(const i32x4 *)(base + byte);
-    return z;
+// A lane's row as an operand: elements 16 * s + 8 * half .. + 7 in regs[s], zeros past the head's.
+template <typename V, int N>
+__device__ __forceinline__ void load_row(V (&regs)[N], const char *row, int half, int dim) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) regs[s] = *(const V *)(row + min(16 * s + 8 * half, dim - 8) * 2);
+    if (dim < 16 * N) {
+#pragma unroll
+        for (int s = 0; s < N; ++s)
+            if (16 * s + 8 * half >= dim) regs[s] = V{};
+    }
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
@@ -252,11 +262,13 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 // Buckets of distance.  A bucket's number is how many cuts are at most the distance, as a symbol's is of its value.
 //
-// The distances that a tile of 64 rows against a workgroup's 128 meets are 191 in a row, and 64 new ones come with each step.  They are kept in a
-// ring of 256, twice, so that a stretch is read without wrapping.
+// The distances that a step's 64 (or 128) rows against a workgroup's 128 meet are 191 (255) in a row, and as many new ones as rows come with each
+// step.  They are kept in a ring of 256 (512), twice, so that a stretch is read without wrapping.
+template <int SIZE>
 struct DistanceRing {
-    float value[512];              // the head's bias times log2(e)
-    uint8_t bucket[512];
+    static constexpr int kMask = SIZE - 1;
+    float value[2 * SIZE];         // the head's bias times log2(e)
+    uint8_t bucket[2 * SIZE];
     uint8_t is_cut[8][64];         // by wave
     float of_bucket[kAttnBuckets];
     int cut[kAttnBuckets];         // filled up with INT32_MAX
@@ -265,10 +277,12 @@ struct DistanceRing {
 struct LaneCuts {
     int lo, hi;
 };
-__device__ __forceinline__ void ring_cuts(DistanceRing &ring, const AttnArgs &a, const AttnCuts &c) {
+template <int SIZE>
+__device__ __forceinline__ void ring_cuts(DistanceRing<SIZE> &ring, const AttnArgs &a, const AttnCuts &c) {
     if (threadIdx.x < kAttnBuckets) ring.cut[threadIdx.x] = (int)threadIdx.x < a.n_buckets - 1 ? c.at[threadIdx.x] : INT32_MAX;
 }
-__device__ __forceinline__ void ring_head(DistanceRing &ring, const AttnArgs &a, int head) {
+template <int SIZE>
+__device__ __forceinline__ void ring_head(DistanceRing<SIZE> &ring, const AttnArgs &a, int head) {
     for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) ring.of_bucket[i] = a.bias[(int64_t)i * a.heads + head] * GBT_LOG2E;
 }
 // The bucket of distance t0 + lane, for a whole wave.  The lane of each cut among the 64 distances marks its place in LDS; how many marks are at
@@ -289,11 +303,12 @@ __device__ __forceinline__ int lane_bucket(uint8_t *mark, const LaneCuts &cuts, 
     return n;
 }
 // The 64 distances from t0 on into the ring, by one wave.
-__device__ __forceinline__ void ring_put(DistanceRing &ring, int t0, int wave, int lane) {
+template <int SIZE>
+__device__ __forceinline__ void ring_put(DistanceRing<SIZE> &ring, int t0, int wave, int lane) {
     const int n = lane_bucket(ring.is_cut[wave], LaneCuts{ring.cut[lane], ring.cut[lane + 64]}, t0, lane);
-    const int at = (t0 + lane) & 255;
-    ring.value[at] = ring.value[at + 256] = ring.of_bucket[n];
-    ring.bucket[at] = ring.bucket[at + 256] = (uint8_t)n;
+    const int at = (t0 + lane) & (SIZE - 1);
+    ring.value[at] = ring.value[at + SIZE] = ring.of_bucket[n];
+    ring.bucket[at] = ring.bucket[at + SIZE] = (uint8_t)n;
 }
 
 }  // namespace

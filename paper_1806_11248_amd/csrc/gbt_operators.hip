@@ -223,7 +223,7 @@ extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_para
     a.dv = view(dv);
     a.lse = (float *)lse;
     a.rest = (char *)rest;
-    a.row_start = (float *)workspace;
+    a.row_less = (float *)workspace;
     a.row_minus = (float *)((char *)workspace + l.row_minus);
     a.strips = (float *)((char *)workspace + l.strips);
     a.part = (float *)((char *)workspace + l.part);

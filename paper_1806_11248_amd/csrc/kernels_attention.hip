@@ -16,16 +16,17 @@ namespace {
 constexpr float kSlack = 8.0f;
 
 // ------------------------------------------------------------------------------------------------ blocks of queries --
-// A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.
-template <typename P, int DP>
-__global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
+// A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.  Of two groups of four
+// waves each takes every other tile for the same queries, and they are joined at the end: half the steps one after the other.
+template <typename P, int DP, int kGroups>
+__global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
-    __shared__ __align__(16) char k_tile[2][T::kBytes];
-    __shared__ __align__(16) char v_tile[2][T::kBytes];
-    __shared__ DistanceRing ring;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups;
+    __shared__ __align__(16) char k_tile[2][kGroups * T::kBytes];
+    __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
+    __shared__ DistanceRing<256 * kGroups> ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
     const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
@@ -35,22 +36,11 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     const AttnSeq rows = attn_seq(a, seq);
     const int first = block * kAttnQueries;
     if (first >= rows.nq) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int wave = any_wave & 3, group = any_wave >> 2;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool bias = a.n_buckets > 0;
-    if (bias) {
-        ring_cuts(ring, a, c);
-        ring_head(ring, a, head);
-    }
-
-    V8 qf[kSteps];
-    {
-        const char *base = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-            qf[s] = as_vec<V8>(load16(base, (16 * s + 8 * half) * 2, query < rows.nq && 16 * s + 8 * half < a.dim));
-    }
     // keys 0 .. last are seen by this lane's query; `end` by any of the workgroup's
     const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
     const int end = a.causal ? min(rows.nk, min(first + kAttnQueries, rows.nq) + off) : rows.nk;
@@ -62,29 +52,37 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
     const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
     const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
 
+    auto fetch = [&](int which, int kb) {
+        T::fetch(k_tile[which] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::fetch(v_tile[which] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
+    };
+    if (64 * group < end) fetch(0, 64 * group);
+    V8 qf[kSteps];
+    load_row(qf, a.q.data + ((rows.q0 + min(query, rows.nq - 1)) * a.q.row + (int64_t)head * a.q.head) * 2, half, a.dim);
+    if (bias) {
+        ring_cuts(ring, a, c);
+        ring_head(ring, a, head);
+    }
     f32x16 o[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
-
-    auto fetch = [&](int which, int kb) {
-        T::fetch(k_tile[which], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
-        T::fetch(v_tile[which], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
-    };
-    if (end > 0) fetch(0, 0);
     arrived(qf);
     __syncthreads();
-    if (bias && wave < 3) ring_put(ring, 64 * wave - (first + 127 + off), wave, lane);
+    if (bias && any_wave < 2 + kGroups) ring_put(ring, 64 * any_wave - (first + 127 + off), any_wave, lane);
 
     // one tile; which of the two copies it lies in is known at compile time, so that LDS addresses are constants of the lane
-    auto step = [&](auto which, int kb) {
+    auto step = [&](auto which, int k0) {
         constexpr int kNow = decltype(which)::value;
+        const char *k_now = k_tile[kNow] + group * T::kBytes, *v_now = v_tile[kNow] + group * T::kBytes;
+        const int kb = k0 + 64 * group;
         tiles_ready();
-        if (kb + 64 < end) fetch(1 - kNow, kb + 64);
-        const int lowest = kb - (first + 127 + off);   // distance
-        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, lowest + 191, wave, lane);
+        if (kb + kStride < end) fetch(1 - kNow, kb + kStride);
+        const int lowest = k0 - (first + 127 + off);   // distance
+        const int turn = (any_wave - (k0 >> 6)) & (4 * kGroups - 1);
+        if (bias && turn < kGroups) ring_put(ring, lowest + 127 + kStride + 64 * turn, any_wave, lane);
         if (kb >= wave_end) return;
 
         f32x16 s[2];
@@ -93,7 +91,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s[b]);
+            for (int b = 0; b < 2; ++b) s[b] = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s[b]);
         // reads a few products ahead
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -103,7 +101,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         // scores in powers of two are s * factor + add
-        const int at = (lowest & 255) + 96 - 32 * wave;   // of the wave's lowest distance, of 95
+        const int at = (lowest & ring.kMask) + 64 * group + 96 - 32 * wave;   // of the wave's lowest distance, of 95
         const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;
         float factor = a.scale2, add = 0.0f;
         if (b0 != b1) {
@@ -149,15 +147,34 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a, AttnCuts 
         for (int i = 0; i < 4; ++i) {
             const V8 p = operand<P>(s[i / 2], i % 2);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile[kNow], 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_now, 16 * i, b, lane), p, o[b]);
         }
     };
-    for (int kb = 0; kb < end; kb += 128) {
-        step(std::integral_constant<int, 0>{}, kb);
-        if (kb + 64 < end) step(std::integral_constant<int, 1>{}, kb + 64);
+    for (int k0 = 0; k0 < end; k0 += 2 * kStride) {
+        step(std::integral_constant<int, 0>{}, k0);
+        if (k0 + kStride < end) step(std::integral_constant<int, 1>{}, k0 + kStride);
     }
 
     sum = column_sum(sum);
+    if constexpr (kGroups == 2) {   // the second group's rows to the first, through LDS
+        float *theirs = (float *)(wave < 2 ? &k_tile[0][0] : &v_tile[0][0]) + (wave & 1) * (16 * kBlocks + 2) * 64 + lane;
+        static_assert(2 * (16 * kBlocks + 2) * 256 <= (int)sizeof k_tile, "two waves' sums fit where the keys were");
+        __syncthreads();
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < 16 * kBlocks; ++i) theirs[64 * i] = o[i / 16][i % 16];
+            theirs[64 * 16 * kBlocks] = top;
+            theirs[64 * (16 * kBlocks + 1)] = sum;
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float their_top = theirs[64 * 16 * kBlocks], all = fmaxf(top, their_top), base = all == -INFINITY ? 0.0f : all;
+        const float mine_by = __builtin_amdgcn_exp2f(top - base), theirs_by = __builtin_amdgcn_exp2f(their_top - base);
+        sum = sum * mine_by + theirs[64 * (16 * kBlocks + 1)] * theirs_by;
+        top = all;
+#pragma unroll
+        for (int i = 0; i < 16 * kBlocks; ++i) o[i / 16][i % 16] = o[i / 16][i % 16] * mine_by + theirs[64 * i] * theirs_by;
+    }
     if (query >= rows.nq) return;
     const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // no key: zeros; a sum that is no number stays none
     if (a.lse && half == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * GBT_LN2;
@@ -226,12 +243,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     auto fetch_v = [&](int kb) { T::fetch_half(v_tile, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim); };
     const int start = begin + 32 * wave;
     V8 qf[kSteps];
-    {
-        const char *base = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-            qf[s] = as_vec<V8>(load16(base, (16 * s + 8 * half) * 2, there && 16 * s + 8 * half < a.dim));
-    }
+    load_row(qf, a.q.data + ((rows.q0 + min(query, rows.nq - 1)) * a.q.row + (int64_t)head * a.q.head) * 2, half, a.dim);
     const LaneCuts cuts{lane < a.n_buckets - 1 ? c.at[lane] : INT32_MAX, lane + 64 < a.n_buckets - 1 ? c.at[lane + 64] : INT32_MAX};
     if (bias) {
         const float *from = a.bias + (there ? head : 0);
@@ -420,7 +432,9 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
     AttnArgs b = a;
     b.stretch = attn_stretch(a.heads, blocks, a.n_seq);
-    attention_kernel<P, DP><<<attn_grid(blocks * a.heads * a.n_seq, b.stretch), 256, 0, stream>>>(b, c);
+    const unsigned grid = attn_grid(blocks * a.heads * a.n_seq, b.stretch);
+    if (attn_two_groups(blocks * a.heads * a.n_seq, a.max_k)) attention_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
+    else attention_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
     return hipGetLastError();
 }
 

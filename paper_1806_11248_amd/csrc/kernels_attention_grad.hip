@@ -40,16 +40,16 @@ __device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int n
 }
 
 // ---------------------------------------------------------------------------------------------------------- queries --
-// As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS.
-template <typename P, int DP>
-__global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
+// As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS, one group of four waves or two.
+template <typename P, int DP, int kGroups>
+__global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
-    __shared__ __align__(16) char k_tile[2][T::kBytes];
-    __shared__ __align__(16) char v_tile[2][T::kBytes];
-    __shared__ DistanceRing ring;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups;
+    __shared__ __align__(16) char k_tile[2][kGroups * T::kBytes];
+    __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
+    __shared__ DistanceRing<256 * kGroups> ring;
 
     const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
     const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
@@ -59,37 +59,11 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     const int first = block * kAttnQueries;
     const bool bias = a.n_buckets > 0;
     if (first >= rows.nq) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int wave = any_wave & 3, group = any_wave >> 2;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool there = query < rows.nq;
-    if (bias) {
-        ring_cuts(ring, a, c);
-        ring_head(ring, a, head);
-    }
-
-    V8 qf[kSteps], gf[kSteps];
-    float delta = 0.0f;
-    {
-        const char *qb = a.q.data + ((rows.q0 + query) * a.q.row + (int64_t)head * a.q.head) * 2;
-        const char *gb = a.dout.data + ((rows.q0 + query) * a.dout.row + (int64_t)head * a.dout.head) * 2;
-        const char *ob = a.out.data + ((rows.q0 + query) * a.out.row + (int64_t)head * a.out.head) * 2;
-        const char *rb = a.rest + ((rows.q0 + query) * a.heads + head) * a.dim * 2;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = 16 * s + 8 * half;
-            const bool in = there && d < a.dim;
-            qf[s] = as_vec<V8>(load16(qb, d * 2, in));
-            gf[s] = as_vec<V8>(load16(gb, d * 2, in));
-            const V8 o = as_vec<V8>(load16(ob, d * 2, in)), r = as_vec<V8>(load16(rb, d * 2, in && a.rest));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[s][e], (float)o[e] + (float)r[e], delta);
-        }
-        delta = column_sum(delta);
-    }
-    // a query that does not exist, or saw no key: its probabilities are 2^-inf
-    const float lse = there ? a.lse[(int64_t)head * a.q_rows + rows.q0 + query] * GBT_LOG2E : INFINITY;
-    const float minus = lse == -INFINITY ? -INFINITY : -lse;
     const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
     const int end = a.causal ? min(rows.nk, min(first + kAttnQueries, rows.nq) + off) : rows.nk;
     const int wave_first = first + wave * 32;
@@ -100,34 +74,59 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
     const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
     const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
 
+    auto fetch = [&](int n, int kb) {
+        T::fetch(k_tile[n] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::fetch(v_tile[n] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
+    };
+    if (64 * group < end) fetch(0, 64 * group);
+    const int64_t row = rows.q0 + min(query, rows.nq - 1);
+    V8 qf[kSteps], gf[kSteps];
+    float delta = 0.0f, lse = a.lse[(int64_t)head * a.q_rows + row] * GBT_LOG2E;
+    load_row(qf, a.q.data + (row * a.q.row + (int64_t)head * a.q.head) * 2, half, a.dim);
+    load_row(gf, a.dout.data + (row * a.dout.row + (int64_t)head * a.dout.head) * 2, half, a.dim);
+    {
+        V8 o[kSteps], r[kSteps];
+        load_row(o, a.out.data + (row * a.out.row + (int64_t)head * a.out.head) * 2, half, a.dim);
+        // without `rest`, out once more, with a factor of zero
+        const bool rest = a.rest != nullptr;
+        load_row(r, rest ? a.rest + (row * a.heads + head) * a.dim * 2 : a.out.data + (row * a.out.row + (int64_t)head * a.out.head) * 2, half, a.dim);
+        if (bias) {
+            ring_cuts(ring, a, c);
+            ring_head(ring, a, head);
+        }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[s][e], (float)o[s][e] + (rest ? (float)r[s][e] : 0.0f), delta);
+    }
+    delta = column_sum(delta);
+    // a query that does not exist, or saw no key: its probabilities are 2^-inf
+    const float minus = !there || lse == -INFINITY ? -INFINITY : -lse;
     f32x16 dq[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dq[b][r] = 0.0f;
     float row_sum = 0.0f;   // of dS: this lane's half of the column
-
-    auto fetch = [&](int n, int kb) {
-        T::fetch(k_tile[n], k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
-        T::fetch(v_tile[n], v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
-    };
-    if (end > 0) fetch(0, 0);
     arrived(qf);
     arrived(gf);
     __syncthreads();
-    if (bias && wave < 3) ring_put(ring, 64 * wave - (first + 127 + off), wave, lane);
+    if (bias && any_wave < 2 + kGroups) ring_put(ring, 64 * any_wave - (first + 127 + off), any_wave, lane);
 
-    auto step = [&](auto which, int kb) {
+    auto step = [&](auto which, int k0) {
         constexpr int kNow = decltype(which)::value;
+        const char *k_now = k_tile[kNow] + group * T::kBytes, *v_now = v_tile[kNow] + group * T::kBytes;
+        const int kb = k0 + 64 * group;
         tiles_ready();
-        if (kb + 64 < end) fetch(1 - kNow, kb + 64);
-        const int lowest = kb - (first + 127 + off);
-        if (bias && wave == ((kb >> 6) & 3)) ring_put(ring, lowest + 191, wave, lane);
+        if (kb + kStride < end) fetch(1 - kNow, kb + kStride);
+        const int lowest = k0 - (first + 127 + off);
+        const int turn = (any_wave - (k0 >> 6)) & (4 * kGroups - 1);
+        if (bias && turn < kGroups) ring_put(ring, lowest + 127 + kStride + 64 * turn, any_wave, lane);
         if (kb >= wave_end) return;
 
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int at = (lowest & 255) + 96 - 32 * wave + 32 * b;   // of this 32 x 32 result's lowest distance, of 63
+            const int at = (lowest & ring.kMask) + 64 * group + 96 - 32 * wave + 32 * b;   // of this 32 x 32 result's lowest distance, of 63
             const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
             f32x16 s, dp;
 #pragma unroll
@@ -137,8 +136,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                s = P::mma(T::template rows<P>(k_tile[kNow], 32 * b, i, lane), qf[i], s);
-                dp = P::mma(T::template rows<P>(v_tile[kNow], 32 * b, i, lane), gf[i], dp);
+                s = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s);
+                dp = P::mma(T::template rows<P>(v_now, 32 * b, i, lane), gf[i], dp);
             }
             if (b0 == b1) {
                 const float add = (bias ? ring.of_bucket[b0] : 0.0f) + minus;
@@ -162,19 +161,34 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
             for (int i = 0; i < 2; ++i) {
                 const V8 ds = operand<P>(s, i);
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(T::template cols<P>(k_tile[kNow], 32 * b + 16 * i, d, lane), ds, dq[d]);
+                for (int d = 0; d < kBlocks; ++d) dq[d] = P::mma(T::template cols<P>(k_now, 32 * b + 16 * i, d, lane), ds, dq[d]);
             }
         }
     };
-    for (int kb = 0; kb < end; kb += 128) {
-        step(std::integral_constant<int, 0>{}, kb);
-        if (kb + 64 < end) step(std::integral_constant<int, 1>{}, kb + 64);
+    for (int k0 = 0; k0 < end; k0 += 2 * kStride) {
+        step(std::integral_constant<int, 0>{}, k0);
+        if (k0 + kStride < end) step(std::integral_constant<int, 1>{}, k0 + kStride);
+    }
+    if constexpr (kGroups == 2) {   // the second group's sums to the first, through LDS
+        float *theirs = (float *)(wave < 2 ? &k_tile[0][0] : &v_tile[0][0]) + (wave & 1) * (16 * kBlocks + 1) * 64 + lane;
+        static_assert(2 * (16 * kBlocks + 1) * 256 <= (int)sizeof k_tile, "two waves' sums fit where the keys were");
+        __syncthreads();
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < 16 * kBlocks; ++i) theirs[64 * i] = dq[i / 16][i % 16];
+            theirs[64 * 16 * kBlocks] = row_sum;
+        }
+        __syncthreads();
+        if (group == 1) return;
+        row_sum += theirs[64 * 16 * kBlocks];
+#pragma unroll
+        for (int i = 0; i < 16 * kBlocks; ++i) dq[i / 16][i % 16] += theirs[64 * i];
     }
     row_sum = column_sum(row_sum);
     if (!there) return;
     if (half == 0) {
         const int64_t at = (int64_t)head * a.q_rows + rows.q0 + query;
-        a.row_start[at] = minus == -INFINITY ? -INFINITY : -a.lse[at] / a.scale;
+        a.row_less[at] = minus;
         a.row_minus[at] = -(delta + row_sum);
     }
     E *out = (E *)a.dq.data + (rows.q0 + query) * a.dq.row + (int64_t)head * a.dq.head;
@@ -195,8 +209,9 @@ __global__ __launch_bounds__(256, 2) void grad_queries_kernel(AttnArgs a, AttnCu
 
 // ------------------------------------------------------------------------------------------------------------- keys --
 // A workgroup takes 128 keys of one key head, a wave 32 of them (its columns); the queries of the heads that share them pass through LDS with
-// their output gradients, 64 at a time.  Products start from what the row has instead of zero, so that scores come out less their
-// row's statistic, and gradients of probabilities less delta.  Where there are few blocks of keys, several workgroups share one, by heads and by
+// their output gradients, 64 at a time.  Products of gradients with values start from -delta instead of zero.  (Products of scores that start from
+// -lse / scale likewise save an addition each, but their sums are then some ten times as large and rounded as much more coarsely: the bias gradient
+// was twice as far off.)  Where there are few blocks of keys, several workgroups share one, by heads and by
 // queries, and their sums are added up by a kernel of its own.
 //
 // Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane.  Others are laid out by
@@ -211,8 +226,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     __shared__ __align__(16) char q_tile[2][T::kBytes];
     __shared__ __align__(16) char g_tile[2][T::kBytes];
     __shared__ __align__(16) char v_block[kValuesInLds ? 2 * T::kBytes : 16];
-    __shared__ __align__(16) float row_start[2][64], row_minus[2][64];
-    __shared__ DistanceRing ring;
+    __shared__ __align__(16) float row_less[2][64], row_minus[2][64];
+    __shared__ DistanceRing<256> ring;
     __shared__ float sums[kWaves][kAttnBuckets];   // the head's bias gradient of this workgroup's keys, by wave
     __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
 
@@ -246,14 +261,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
 
     V8 kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
     {
-        const char *kb = a.k.data + ((rows.k0 + key) * a.k.row + (int64_t)kv_head * a.k.head) * 2;
-        const char *vb = a.v.data + ((rows.k0 + key) * a.v.row + (int64_t)kv_head * a.v.head) * 2;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = 16 * s + 8 * half;
-            kf[s] = as_vec<V8>(load16(kb, d * 2, there && d < a.dim));
-            if constexpr (!kValuesInLds) vf[s] = as_vec<V8>(load16(vb, d * 2, there && d < a.dim));
-        }
+        const int64_t row = rows.k0 + min(key, rows.nk - 1);
+        load_row(kf, a.k.data + (row * a.k.row + (int64_t)kv_head * a.k.head) * 2, half, a.dim);
+        if constexpr (!kValuesInLds) load_row(vf, a.v.data + (row * a.v.row + (int64_t)kv_head * a.v.head) * 2, half, a.dim);
         if constexpr (kValuesInLds) {
             const int row = first + 64 * (wave >> 2);
             if (row < rows.nk)
@@ -295,18 +305,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         __syncthreads();   // the head before is done with the values, the ring and the sums
         float run = 0.0f;  // this lane's part of the sum over results of one bucket
         int run_bucket = 0;
-        if (bias) {
-            ring_head(ring, a, head);
-            for (int i = threadIdx.x; i < kWaves * kAttnBuckets; i += kThreads) (&sums[0][0])[i] = 0.0f;
-        }
         auto fetch = [&](int n, int qb) {
             if (kWaves == 4 || wave < 4) T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
             if (kWaves == 4 || wave >= 4) T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
             const uint32_t at = min(lane, rows.nq - qb - 1) * 4;
-            if (wave == 0) load_word_to_lds(lds_address(row_start[n]), a.row_start + at_row + qb, at);
+            if (wave == 0) load_word_to_lds(lds_address(row_less[n]), a.row_less + at_row + qb, at);
             if (wave == 1) load_word_to_lds(lds_address(row_minus[n]), a.row_minus + at_row + qb, at);
         };
         if (from < to) fetch(0, from);
+        if (bias) {
+            ring_head(ring, a, head);
+            for (int i = threadIdx.x; i < kWaves * kAttnBuckets; i += kThreads) (&sums[0][0])[i] = 0.0f;
+        }
         __syncthreads();
         if (bias && wave < 3) ring_put(ring, 64 * wave + first - (from + 63 + off), wave, lane);
 
@@ -326,10 +336,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 f32x16 s, dp;
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
-                    const f32x4 m = *(const f32x4 *)(row_start[now] + 32 * b + 8 * r4 + 4 * half), d = *(const f32x4 *)(row_minus[now] + 32 * b + 8 * r4 + 4 * half);
+                    const f32x4 d = *(const f32x4 *)(row_minus[now] + 32 * b + 8 * r4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[4 * r4 + e] = m[e];
+                        s[4 * r4 + e] = 0.0f;
                         dp[4 * r4 + e] = d[e];
                     }
                 }
@@ -340,7 +350,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 }
                 // reads two products ahead, and no further: registers are what there is least of
                 constexpr int kReads = kValuesInLds ? 3 : 2;
-                __builtin_amdgcn_sched_group_barrier(0x100, 8 + 2 * kReads, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4 + 2 * kReads, 0);
 #pragma unroll
                 for (int i = 0; i < kSteps - 2; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
@@ -348,14 +358,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 }
                 __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
                 __builtin_amdgcn_sched_barrier(0);
+                const float *less = row_less[now] + 32 * b + 4 * half;
                 if (b0 == b1) {
                     const float add = bias ? ring.of_bucket[b0] : 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add));
+                    for (int r4 = 0; r4 < 4; ++r4) {
+                        const f32x4 l = *(const f32x4 *)(less + 8 * r4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[4 * r4 + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + e], a.scale2, add + l[e]));
+                    }
                 } else {
                     const float *add = ring.value + at + 31 + (lane & 31);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add[-result_row(r, half)]));
+                    for (int r4 = 0; r4 < 4; ++r4) {
+                        const f32x4 l = *(const f32x4 *)(less + 8 * r4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[4 * r4 + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + e], a.scale2, add[-result_row(4 * r4 + e, half)] + l[e]));
+                    }
                 }
                 if (qb + 32 * b < wave_all || qb + 32 * b + 32 > rows.nq) {   // rows past the last are the last one's copies
 #pragma unroll
@@ -537,7 +557,9 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     if (q_blocks > 0 && a.n_seq > 0) {
         AttnArgs b = a;
         b.stretch = attn_stretch(a.heads, q_blocks, a.n_seq);
-        grad_queries_kernel<P, DP><<<attn_grid(q_blocks * a.heads * a.n_seq, b.stretch), 256, 0, stream>>>(b, c);
+        const unsigned grid = attn_grid(q_blocks * a.heads * a.n_seq, b.stretch);
+        if (attn_two_groups(q_blocks * a.heads * a.n_seq, a.max_k)) grad_queries_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
+        else grad_queries_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {
