@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     const int first = block * kAttnQueries;
     if (first >= rows.nq) return;
     const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int wave = any_wave & 3, group = any_wave >> 2;
+    const int wave = kGroups == 2 ? any_wave & 3 : any_wave, group = kGroups == 2 ? any_wave >> 2 : 0;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool bias = a.n_buckets > 0;
