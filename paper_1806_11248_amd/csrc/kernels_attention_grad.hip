@@ -139,6 +139,15 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
                 s = P::mma(T::template rows<P>(k_now, 32 * b, i, lane), qf[i], s);
                 dp = P::mma(T::template rows<P>(v_now, 32 * b, i, lane), gf[i], dp);
             }
+            // reads two products ahead
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < kSteps - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_barrier(0);
             if (b0 == b1) {
                 const float add = (bias ? ring.of_bucket[b0] : 0.0f) + minus;
 #pragma unroll
