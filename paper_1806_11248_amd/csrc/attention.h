@@ -173,8 +173,12 @@ struct Tile {
     // From memory straight into LDS, a wave's 64 pieces at a time, by four waves, of which this one is number `wave`.  Rows past the last and elements past the head's are taken from
     // the last there are, so that nothing hangs on a condition: such rows' probabilities are zero, and such elements meet zeros of the
     // other operand or are not stored.  rows, dim > 0; 64 * row_bytes < 2^32.
+    // kKeep: addresses may be kept in registers from one call to the next; else they are worked out each time, for kernels that have none to spare (what
+    // is kept in memory is waited for together with the loads before it).
+    template <bool kKeep = true>
     static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim, int wave) {
-        const int lane = threadIdx.x & 63;
+        int lane = kKeep ? threadIdx.x & 63 : __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        if (!kKeep) asm volatile("" : "+v"(lane));
         constexpr int kRows = 64 / kPlaces;                       // of a wave's load
         const int row = wave * kRows + lane / kPlaces;            // the i-th load's is 4 * kRows further, with the same fold
         const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;

@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         for (int i = threadIdx.x; i < 128 * T::kPlaces; i += kThreads)
             if ((i % T::kPlaces ^ T::fold(i / T::kPlaces)) >= a.dim / 8) *(i32x4 *)(v_block + 16 * i) = i32x4{0, 0, 0, 0};
     }
-    auto values = [&](int i) {
+    auto values = [&](int i, int lane) {
         if constexpr (kValuesInLds) return T::template rows<P>(v_block + (key_wave >> 1) * T::kBytes, 32 * (key_wave & 1), i, lane);
         else return vf[i];
     };
@@ -315,8 +315,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         float run = 0.0f;  // this lane's part of the sum over results of one bucket
         int run_bucket = 0;
         auto fetch = [&](int n, int qb) {
-            if (kWaves == 4 || wave < 4) T::fetch(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
-            if (kWaves == 4 || wave >= 4) T::fetch(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
+            if (kWaves == 4 || wave < 4) T::template fetch<DP <= 64>(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
+            if (kWaves == 4 || wave >= 4) T::template fetch<DP <= 64>(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
             const uint32_t at = min(lane, rows.nq - qb - 1) * 4;
             if (wave == 0) load_word_to_lds(lds_address(row_less[n]), a.row_less + at_row + qb, at);
             if (wave == 1) load_word_to_lds(lds_address(row_minus[n]), a.row_minus + at_row + qb, at);
@@ -339,6 +339,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
 #pragma unroll 1
             for (int turn = 0; turn < 8 / kWaves; ++turn) {
                 const int b = kWaves == 8 ? wave >> 2 : turn;
+                int here = lane;   // at large heads, LDS addresses are worked out each time: registers again
+                if (DP > 64) asm volatile("" : "+v"(here));
+                const int half = here >> 5;
                 if (qb + 32 * b + 31 < wave_from || qb + 32 * b >= rows.nq) continue;
                 const int at = (lowest & 255) + 32 * key_wave + 32 - 32 * b;   // of this result's lowest distance, of 63
                 const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
@@ -354,8 +357,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 }
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, lane), kf[i], s);
-                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, lane), values(i), dp);
+                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, here), kf[i], s);
+                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, here), values(i, here), dp);
                 }
                 // reads two products ahead, and no further: registers are what there is least of
                 constexpr int kReads = kValuesInLds ? 3 : 2;
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                         for (int e = 0; e < 4; ++e) s[4 * r4 + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + e], a.scale2, add + l[e]));
                     }
                 } else {
-                    const float *add = ring.value + at + 31 + (lane & 31);
+                    const float *add = ring.value + at + 31 + (here & 31);
 #pragma unroll
                     for (int r4 = 0; r4 < 4; ++r4) {
                         const f32x4 l = *(const f32x4 *)(less + 8 * r4);
@@ -415,14 +418,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) sk[result_row(r, half) * 63 + 31 + (lane & 31)] = dp[4 * h + r];
+                        for (int r = 0; r < 4; ++r) sk[result_row(r, half) * 63 + 31 + (here & 31)] = dp[4 * h + r];
                         __builtin_amdgcn_wave_barrier();
                         // eight rows further on, the same diagonal lies eight places further on; place 63 is never written
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v += sk[64 * i + min(lane + 8 * h, 63)];
+                        for (int i = 0; i < 8; ++i) v += sk[64 * i + min(here + 8 * h, 63)];
                         __builtin_amdgcn_wave_barrier();
                     }
-                    add_runs(sums[wave], v, ring.bucket[at + min(lane, 62)], ring.bucket[at + min(lane + 1, 62)], lane);
+                    add_runs(sums[wave], v, ring.bucket[at + min(here, 62)], ring.bucket[at + min(here + 1, 62)], here);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -430,8 +433,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                     const V8 p = operand<P>(s, i), ds = operand<P>(dp, i);
 #pragma unroll
                     for (int d = 0; d < kBlocks; ++d) {
-                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, lane), p, dv[d]);
-                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, lane), ds, dk[d]);
+                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, here), p, dv[d]);
+                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, here), ds, dk[d]);
                     }
                 }
                 __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
