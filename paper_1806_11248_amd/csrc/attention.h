@@ -18,13 +18,36 @@ struct AttnView {   // rows x heads x head_dim elements; strides in elements, th
     int64_t row, head;
 };
 
+// How the workgroups of a launch go over the work: `blocks` blocks of each of `units` units (heads, or key heads and parts) of every sequence.
+//
+// Workgroups go to the eight XCDs in turn, and blocks of one unit share what they read, so an XCD takes whole units; sequences are as long as they
+// are, so no XCD is to have more of one than another: an eighth of each where units divide so, else units in turn, single blocks where even
+// those are few.  (24 histories of 100 to 1000 rows, 8 heads: an eighth of all units in a row for each XCD 58 us, an eighth of each history 48.)
+// The blocks with the most to do come first.  Where causal blocks differ in that and all that is read fits the XCDs' L2, the first blocks of all units
+// come before all second ones, so that the last workgroups are short ones (16 causal histories of 100 to 1000 rows, forward and the two gradient
+// kernels unit by unit 32 + 44 + 73 us, block by block 31 + 41 + 63; two of 4096 211 + 263 + 431, 195 + 250 + 440; but 24 that are not causal 47, 56).
+struct AttnOrder {
+    int units, blocks, wide;    // wide: units of an XCD, or of all where single blocks go to XCDs
+    int single, by_block;
+};
+inline AttnOrder attn_order(int64_t units, int64_t blocks, int64_t n_seq, int causal, int64_t bytes) {
+    AttnOrder o;
+    o.units = (int)units;
+    o.blocks = (int)blocks;
+    o.single = units % 8 != 0 && units * n_seq < 64;
+    o.wide = (int)(o.single ? units * n_seq : (units * n_seq + 7) / 8);
+    o.by_block = causal && bytes <= (int64_t)8 * (4 << 20);
+    return o;
+}
+inline unsigned attn_grid(const AttnOrder &o) { return (unsigned)((int64_t)(o.single ? 1 : 8) * o.wide * o.blocks); }
+
 struct AttnArgs {
     AttnView q, k, v, out;
     const int64_t *q_ptr, *k_ptr;   // NULL: sequence s has rows s * max .. (s + 1) * max
     const int32_t *k_len;           // NULL: all of a sequence's key rows are used
     int64_t q_rows, k_rows;
     int n_seq, heads, kv_heads, group, dim, max_q, max_k, causal, n_buckets;
-    int stretch;                    // see attn_item
+    AttnOrder order;
     float scale, scale2;            // scale2 = scale * log2(e): probabilities are powers of two here
     const float *bias;              // [n_buckets][heads]
     float *lse;                     // [heads][q_rows], natural logarithm, or NULL
@@ -41,19 +64,11 @@ struct AttnArgs {
     int pieces, piece_len;
 };
 
-// The stretch for `blocks` blocks of each of `units` units (heads, or key heads and parts) of a sequence.  Sequences are as long as they are, so
-// no XCD is to have more of one than another: an eighth of each where units divide so; else whole units where there are many, single blocks
-// where there are not.  (24 histories of 100 to 1000 rows, 8 heads: an eighth of all items in a row for each XCD 58 us,
-// so 48.)
-inline int attn_stretch(int64_t units, int64_t blocks, int64_t n_seq) {
-    return (int)(units % 8 == 0 ? units / 8 * blocks : units * n_seq >= 64 ? blocks : 1);
-}
 // Where a launch has no more workgroups than there are compute units and its keys are several tiles, two groups of four waves share a workgroup's
 // queries and take the tiles in turn.  us forward and backward with one group and two (causal): 64 workgroups, 500 keys 13.4 + 45.8, 12.4 + 44.6;
 // 256, 1000 keys 22.3 + 85.1, 19.4 + 80.3; 256, 2000 keys of 128 elements 48.9 + 217.8, 41.3 + 181.1; but 512, 1000 keys 44.3 + 193, 53.4 + 199;
 // 4, 100 keys 7.1 + 23.8, 7.7 + 24.8.
 inline bool attn_two_groups(int64_t workgroups, int64_t max_k) { return workgroups <= 256 && max_k >= 256; }
-inline unsigned attn_grid(int64_t items, int stretch) { return (unsigned)((items + 8 * (int64_t)stretch - 1) / (8 * (int64_t)stretch) * 8 * stretch); }
 
 struct AttnCuts {
     int32_t at[kAttnBuckets - 1];   // ascending
@@ -127,11 +142,25 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s) {
     return r;
 }
 
-// Workgroups go to the eight XCDs in turn.  Items of one stretch of the order share keys (or queries), so an XCD takes `stretch` of them, the next
-// stretch the next XCD.
-__device__ __forceinline__ int64_t attn_item(int stretch) {
-    const int64_t at = blockIdx.x / 8;
-    return (at / stretch * 8 + blockIdx.x % 8) * stretch + at % stretch;
+struct AttnItem {
+    int seq, unit, block;   // seq < 0: none
+};
+__device__ __forceinline__ AttnItem attn_item(const AttnOrder &o, int n_seq) {
+    AttnItem it;
+    const int at = o.single ? blockIdx.x : blockIdx.x / 8, xcd = blockIdx.x % 8;
+    int unit = o.by_block ? at % o.wide : at / o.blocks;
+    it.block = o.by_block ? at / o.wide : at % o.blocks;
+    if (o.units % 8 == 0) {
+        const int eighth = o.units / 8;
+        it.seq = unit / eighth;
+        it.unit = xcd * eighth + unit % eighth;
+    } else {
+        if (!o.single) unit = unit * 8 + xcd;
+        it.seq = unit / o.units;
+        it.unit = unit % o.units;
+    }
+    if (it.seq >= n_seq) it.seq = -1;
+    return it;
 }
 
 // A lane's row as an operand: elements 16 * s + 8 * half .. + 7 in regs[s], zeros past the head's.

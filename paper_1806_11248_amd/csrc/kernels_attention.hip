@@ -28,11 +28,10 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
 
-    const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
-    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
-    if (item >= items) return;
+    const AttnItem item = attn_item(a.order, a.n_seq);
+    if (item.seq < 0) return;
     // the blocks that see the most keys first
-    const int block = q_blocks - 1 - (int)(item % q_blocks), head = (int)(item / q_blocks % a.heads), seq = (int)(item / q_blocks / a.heads);
+    const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
     const AttnSeq rows = attn_seq(a, seq);
     const int first = block * kAttnQueries;
     if (first >= rows.nq) return;
@@ -431,8 +430,8 @@ template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
     AttnArgs b = a;
-    b.stretch = attn_stretch(a.heads, blocks, a.n_seq);
-    const unsigned grid = attn_grid(blocks * a.heads * a.n_seq, b.stretch);
+    b.order = attn_order(a.heads, blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
+    const unsigned grid = attn_grid(b.order);
     if (attn_two_groups(blocks * a.heads * a.n_seq, a.max_k)) attention_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
     else attention_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
     return hipGetLastError();

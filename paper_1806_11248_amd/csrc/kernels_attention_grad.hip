@@ -51,10 +51,9 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
 
-    const int q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
-    const int64_t items = (int64_t)q_blocks * a.heads * a.n_seq, item = attn_item(a.stretch);
-    if (item >= items) return;
-    const int block = q_blocks - 1 - (int)(item % q_blocks), head = (int)(item / q_blocks % a.heads), seq = (int)(item / q_blocks / a.heads);
+    const AttnItem item = attn_item(a.order, a.n_seq);
+    if (item.seq < 0) return;
+    const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
     const AttnSeq rows = attn_seq(a, seq);
     const int first = block * kAttnQueries;
     const bool bias = a.n_buckets > 0;
@@ -240,11 +239,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     __shared__ float sums[kWaves][kAttnBuckets];   // the head's bias gradient of this workgroup's keys, by wave
     __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
 
-    const int k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries, parts = a.head_parts * a.q_parts;
-    const int64_t items = (int64_t)k_blocks * parts * a.kv_heads * a.n_seq, item = attn_item(a.stretch);
-    if (item >= items) return;
-    const int block = (int)(item % k_blocks), part = (int)(item / k_blocks % parts);
-    const int kv_head = (int)(item / k_blocks / parts % a.kv_heads), seq = (int)(item / k_blocks / parts / a.kv_heads);
+    const int k_blocks = a.order.blocks, parts = a.head_parts * a.q_parts;
+    const AttnItem item = attn_item(a.order, a.n_seq);
+    if (item.seq < 0) return;
+    const int block = item.block, part = item.unit % parts, kv_head = item.unit / parts, seq = item.seq;
     const int q_part = part % a.q_parts, head_part = part / a.q_parts;
     const int g_from = a.group * head_part / a.head_parts, g_to = a.group * (head_part + 1) / a.head_parts;
     const AttnSeq rows = attn_seq(a, seq);
@@ -568,8 +566,8 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     hipError_t e = hipSuccess;
     if (q_blocks > 0 && a.n_seq > 0) {
         AttnArgs b = a;
-        b.stretch = attn_stretch(a.heads, q_blocks, a.n_seq);
-        const unsigned grid = attn_grid(q_blocks * a.heads * a.n_seq, b.stretch);
+        b.order = attn_order(a.heads, q_blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
+        const unsigned grid = attn_grid(b.order);
         if (attn_two_groups(q_blocks * a.heads * a.n_seq, a.max_k)) grad_queries_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
         else grad_queries_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
         e = hipGetLastError();
@@ -578,8 +576,8 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         constexpr int kWaves = DP == 128 ? 8 : 4;
         const int64_t units = (int64_t)a.kv_heads * a.head_parts * a.q_parts;
         AttnArgs b = a;
-        b.stretch = attn_stretch(units, k_blocks, a.n_seq);
-        grad_keys_kernel<P, DP, kWaves><<<attn_grid(k_blocks * units * a.n_seq, b.stretch), 64 * kWaves, 0, stream>>>(b, c);
+        b.order = attn_order(units, k_blocks, a.n_seq, a.causal, 4 * a.q_rows * a.heads * a.dim);
+        grad_keys_kernel<P, DP, kWaves><<<attn_grid(b.order), 64 * kWaves, 0, stream>>>(b, c);
         e = hipGetLastError();
         if (e == hipSuccess && a.head_parts * a.q_parts > 1) {
             grad_join_kernel<P><<<(unsigned)((int64_t)(a.max_k + 3) / 4 * a.n_seq), 256, 0, stream>>>(a);
