@@ -542,22 +542,24 @@ __global__ __launch_bounds__(256) void grad_join_kernel(AttnArgs a) {
     }
 }
 
-// The strips of every head together, in a fixed order: a workgroup takes a head, a thread every (256 / buckets)-th strip of a bucket.
-__global__ __launch_bounds__(256) void grad_bias_kernel(AttnArgs a) {
-    __shared__ double part[256];
-    const int head = blockIdx.x, n = a.n_buckets, lanes = 256 / n;   // threads of a bucket
+// The strips of every head together, in a fixed order: a workgroup takes a head, 2^k threads a bucket, which are then added up in pairs.
+__global__ __launch_bounds__(1024) void grad_bias_kernel(AttnArgs a) {
+    __shared__ double part[1024];
+    const int head = blockIdx.x, n = a.n_buckets, lanes = 1 << (31 - __clz(1024 / n));
     const int64_t strips = (int64_t)a.n_seq * ((a.max_k + kAttnQueries - 1) / kAttnQueries) * a.q_parts;
     const float *from = a.strips + (int64_t)head * strips * n;
     const int b = threadIdx.x % n, l = threadIdx.x / n;
     double sum = 0.0;
-    if (l < lanes)
+    if (l < lanes) {
+#pragma unroll 8
         for (int64_t s = l; s < strips; s += lanes) sum += from[s * n + b];
-    part[threadIdx.x] = sum;
-    __syncthreads();
-    if (l == 0) {
-        for (int i = 1; i < lanes; ++i) sum += part[i * n + b];
-        a.dbias[(int64_t)b * a.heads + head] = (float)sum;
     }
+    part[threadIdx.x] = sum;
+    for (int w = lanes / 2; w > 0; w /= 2) {
+        __syncthreads();
+        if (l < w) part[threadIdx.x] += part[threadIdx.x + w * n];
+    }
+    if (l == 0) a.dbias[(int64_t)b * a.heads + head] = (float)part[threadIdx.x];
 }
 
 template <typename P, int DP>
@@ -585,7 +587,7 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         }
     }
     if (e == hipSuccess && a.n_buckets > 0) {
-        grad_bias_kernel<<<(unsigned)a.heads, 256, 0, stream>>>(a);
+        grad_bias_kernel<<<(unsigned)a.heads, 1024, 0, stream>>>(a);
         e = hipGetLastError();
     }
     return e;
