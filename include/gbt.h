@@ -558,7 +558,7 @@ typedef struct gbt_attention_params {
 } gbt_attention_params;
 
 /*
- * out [dev] as q.  Rows of no sequence are not written.  For gbt_attention_backward:
+ * out [dev] as q, overlapping no input.  Rows of no sequence are not written.  For gbt_attention_backward:
  *   lse_out  [dev] float[heads][q_rows], or NULL: log sum_j exp S, -inf for a query without keys
  *   rest_out [dev] [q_rows][heads][head_dim] of dtype, 16-byte aligned, or NULL: what rounding took from out
  * Asynchronous.  workspace [dev]: gbt_attention_workspace_bytes (0: none needed, NULL allowed).  The workspace

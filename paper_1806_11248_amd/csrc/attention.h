@@ -321,9 +321,9 @@ __device__ __forceinline__ void ring_head(DistanceRing<SIZE> &ring, const AttnAr
 // The bucket of distance t0 + lane, for a whole wave.  The lane of each cut among the 64 distances marks its place in LDS; how many marks are at
 // or before a distance is then a count of bits.
 __device__ __forceinline__ int lane_bucket(uint8_t *mark, const LaneCuts &cuts, int t0, int lane) {
-    const int lo = cuts.lo - t0, hi = cuts.hi - t0;
+    const uint32_t lo = (uint32_t)cuts.lo - (uint32_t)t0, hi = (uint32_t)cuts.hi - (uint32_t)t0;
     int n = __popcll(__ballot(cuts.lo < t0)) + __popcll(__ballot(cuts.hi < t0));
-    const bool lo_in = cuts.lo >= t0 && (uint32_t)lo < 64u, hi_in = cuts.hi >= t0 && (uint32_t)hi < 64u;
+    const bool lo_in = cuts.lo >= t0 && lo < 64u, hi_in = cuts.hi >= t0 && hi < 64u;
     if (__any(lo_in || hi_in)) {
         mark[lane] = 0;
         __builtin_amdgcn_wave_barrier();

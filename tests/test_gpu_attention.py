@@ -357,3 +357,62 @@ def test_without_what_rounding_took(ctx):
     for name, x in (("dk", dk), ("dv", dv), ("dbias", dbias)):
         close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
     assert float((dq.cpu().double() - ref.dq).norm() / ref.dq.norm()) < 2.0 ** -7
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """Rows whose bytes lie beyond 4 GB: at the end of a long store, and far apart."""
+    H, D = 8, 128
+    rows = (1 << 32) // (2 * H * D) + 5_000
+    k, v = (torch.zeros(rows, H, D, dtype=BF, device="cuda") for _ in range(2))
+    n = [700, 1, 300]
+    ptr = [rows - 2_000, rows - 1_200, rows - 900, rows - 600]
+    rng = torch.Generator().manual_seed(20)
+    small = [torch.randn(2_000, H, D, generator=rng).to(BF) for _ in range(2)]
+    for big, x in ((k, small[0]), (v, small[1])):
+        big[-2_000:] = x.cuda()
+    for m in (1, 150):                     # new events, and blocks of queries with their gradients
+        q = torch.randn(3 * m, H, D, generator=rng).to(BF).cuda()
+        dout = torch.randn(3 * m, H, D, generator=rng).to(BF).cuda()
+        args = dict(q_ptr=torch.arange(4, device="cuda") * m, k_ptr=torch.tensor(ptr, device="cuda"), k_len=torch.tensor(n, dtype=torch.int32, device="cuda"),
+                    max_q=m, max_k=700)
+        spans = [(i * m, m, ptr[i] - (rows - 2_000), n[i]) for i in range(3)]
+        ref = Reference(q.cpu(), *small, spans, False, D ** -0.5, None, None, dout.cpu())
+        out, saved = ctx.attention(q, k, v, save=True, **args)
+        close(out, ref.out, ref.out_tol, "out")
+        if m > 1:
+            dq, dk, dv, _ = ctx.attention_backward(dout, q, k, v, out, saved, **args)
+            close(dq, ref.dq, ref.dq_tol, "dq")
+            close(dk[-2_000:], ref.dk, ref.dk_tol, "dk")
+            close(dv[-2_000:], ref.dv, ref.dv_tol, "dv")
+            assert not dk[:-2_000].any()
+            del dk, dv
+    del k, v
+    # 300 rows of 2^23 elements each, of which a head is used: 5 GB
+    wide = torch.zeros(300, 1 << 23, dtype=BF, device="cuda")
+    x = torch.randn(300, 3, 64, generator=rng).to(BF)
+    wide[:, :192] = x.view(300, 192).cuda()
+    q, k, v = (wide[:, 64 * i:64 * i + 64].unflatten(1, (1, 64)) for i in range(3))
+    ref = Reference(x[:, :1], x[:, 1:2], x[:, 2:], [(0, 300, 0, 300)], True, 64 ** -0.5)
+    close(ctx.attention(q, k, v, causal=True), ref.out, ref.out_tol, "out")
+    close(ctx.attention(q[-3:], k, v, causal=True), ref.out[-3:], ref.out_tol[-3:], "out")
+
+
+def test_a_full_table_of_buckets_against_a_store(ctx):
+    """128 buckets and 32 columns of 128 elements: the most LDS that the form for few rows takes."""
+    _check(ctx, _make([1, 1], [700, 90], 32, 1, 128, BF, causal=True, buckets=128, far=600, room=4, seed=21), backward=False)
+
+
+def test_parts_of_a_block_of_keys(ctx):
+    """Few blocks of keys for many query heads and long queries: a block's workgroups, by heads and by queries, and the sum of their parts."""
+    for nq, nk, H, K, D in (([1500], [90], 6, 1, 64), ([900, 10], [130, 260], 4, 2, 128), ([600], [600], 5, 1, 96), ([2100], [40], 1, 1, 32)):
+        _check(ctx, _make(nq, nk, H, K, D, BF, causal=False, buckets=12, seed=22))
+        _check(ctx, _make(nq, nk, H, K, D, HF, causal=True, buckets=12, seed=23))
+
+
+def test_many_sequences(ctx):
+    """More (sequence, head) units than XCDs, in numbers that no eighth divides; most sequences empty or short."""
+    rng = np.random.default_rng(24)
+    nq = [int(x) for x in rng.integers(0, 40, 90)]
+    nq[13] = 300
+    _check(ctx, _make(nq, nq, 3, 1, 16, BF, causal=True, buckets=6, seed=25))
+    _check(ctx, _make(nq[:20], nq[:20], 3, 3, 16, HF, causal=False, buckets=6, seed=26))
