@@ -518,7 +518,7 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
  *     t      = j - (i + nk - nq)       distance: 0 the query's own place (the last query is at the last key)
  *     S      = scale * q_i . k_j + bias[bucket(t)][h],  bucket(t) = #{cuts <= t} as symbols are binned above;
  *              causal: keys with t > 0 do not count
- *     out_i  = sum_j softmax_j(S) v_j;   a query without any key: zeros
+ *     out_i  = sum_j softmax_j(S) v_j;   a query without any key, or with all of them shut out: zeros
  * Scores, softmax statistics and all sums are held in 32 bits; probabilities are rounded to the inputs' type as
  * operands of the products with v and out's gradient, scores' gradients as operands of those with q and k.
  * A non-finite element of a sequence makes that sequence's results of its key head non-finite in part; no
@@ -533,6 +533,7 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
 #define GBT_F16 2
 #define GBT_MAX_HEAD_DIM 128
 #define GBT_MAX_BUCKETS 128
+#define GBT_BIAS_SHUT -1e5f /* a bias below it shuts its bucket out, as -inf does */
 
 typedef struct gbt_heads {       /* [dev] rows x heads x head_dim elements */
     void *data;
@@ -553,12 +554,13 @@ typedef struct gbt_attention_params {
     const int64_t *k_ptr;        /* [dev] int64[n_seq + 1]; NULL: the same with max_k */
     const int32_t *k_len;        /* [dev] int32[n_seq], or NULL: only the first k_len[s] rows of the slot
                                     k_ptr[s] .. k_ptr[s + 1] are used (a store with room to grow) */
-    const float *bias;           /* [dev] float[n_buckets][heads] */
+    const float *bias;           /* [dev] float[n_buckets][heads]; meant for magnitudes to 1e5, lower: GBT_BIAS_SHUT */
     const int32_t *cuts;         /* [host] int32[n_buckets - 1], strictly increasing */
 } gbt_attention_params;
 
 /*
- * out [dev] as q, overlapping no input.  Rows of no sequence are not written.  For gbt_attention_backward:
+ * out [dev] as q, overlapping no input.  Rows of no sequence get zeros.  For gbt_attention_backward
+ * (rows of no sequence are not written):
  *   lse_out  [dev] float[heads][q_rows], or NULL: log sum_j exp S, -inf for a query without keys
  *   rest_out [dev] [q_rows][heads][head_dim] of dtype, 16-byte aligned, or NULL: what rounding took from out
  * Asynchronous.  workspace [dev]: gbt_attention_workspace_bytes (0: none needed, NULL allowed).  The workspace
@@ -574,7 +576,7 @@ GBT_API int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *params, 
  * what gbt_attention returned for the same parameters (rest may be NULL; dq is then less exact).
  *   dbias_out [dev] float[n_buckets][heads], overwritten (ignored where n_buckets = 0)
  * Probabilities are recomputed; sums are taken in a fixed order, so results are the same on every run.  Rows of
- * no sequence, and key rows beyond k_len, are not written.  Asynchronous.
+ * no sequence, key rows beyond k_len among them, get zeros.  dq, dk and dv overlap no input.  Asynchronous.
  */
 GBT_API size_t gbt_attention_backward_workspace_bytes(const gbt_attention_params *params);
 GBT_API int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_params *params, const gbt_heads *dout,

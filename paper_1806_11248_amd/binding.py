@@ -715,6 +715,7 @@ class Context:
         k_len         int32[n_seq] on the device: how many rows of each slot of k and v are in use (None: all)
         max_q, max_k  the longest sequence (None: taken to be all rows, which costs idle workgroups)
         bias, cuts    float32 [n_buckets][heads] and the ascending cuts between buckets of distance, on the host
+        Rows of no sequence, and queries without keys, get zeros; a bias below GBT_BIAS_SHUT (-1e5) shuts its bucket out.
         save          also return what attention_backward needs: (out, saved)
         """
         p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
@@ -740,8 +741,8 @@ class Context:
 
     def attention_backward(self, dout, q, k, v, out, saved, *, q_ptr=None, k_ptr=None, k_len=None, max_q=None, max_k=None, causal=False,
                            scale=None, bias=None, cuts=None):
-        """(dq, dk, dv, dbias) of attention(..., save=True) with the same arguments; dbias is None without a bias.  Rows of k and v
-        that no sequence uses get zeros."""
+        """(dq, dk, dv, dbias) of attention(..., save=True) with the same arguments; dbias is None without a bias.  Rows of no
+        sequence get zeros, rows beyond k_len too."""
         p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
         dtype = q.dtype
         rows, heads, dim = q.shape
@@ -758,9 +759,7 @@ class Context:
         ws_bytes = lib.gbt_attention_backward_workspace_bytes(at)
         with self._on_stream((dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias)) or _NO_STREAM:
             dq = self.empty((rows, heads, dim), dtype)
-            make = torch.empty if k_len is None else torch.zeros
-            dk = make((k_rows, kv_heads, dim), dtype=dtype, device=self.device)
-            dv = make((k_rows, kv_heads, dim), dtype=dtype, device=self.device)
+            dk, dv = self.empty((k_rows, kv_heads, dim), dtype), self.empty((k_rows, kv_heads, dim), dtype)
             dbias = None if bias is None else self.empty(bias.shape, torch.float32)
             ws = self.workspace("attention", ws_bytes)
         hdq, hdk, hdv = Heads(dq.data_ptr(), heads * dim, dim), Heads(dk.data_ptr(), kv_heads * dim, dim), Heads(dv.data_ptr(), kv_heads * dim, dim)

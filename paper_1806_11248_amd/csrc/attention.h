@@ -48,6 +48,7 @@ struct AttnArgs {
     int64_t q_rows, k_rows;
     int n_seq, heads, kv_heads, group, dim, max_q, max_k, causal, n_buckets;
     AttnOrder order;
+    unsigned work;                  // workgroups of the launch; those behind them zero the rows of no sequence
     float scale, scale2;            // scale2 = scale * log2(e): probabilities are powers of two here
     const float *bias;              // [n_buckets][heads]
     float *lse;                     // [heads][q_rows], natural logarithm, or NULL
@@ -161,6 +162,50 @@ __device__ __forceinline__ AttnItem attn_item(const AttnOrder &o, int n_seq) {
     }
     if (it.seq >= n_seq) it.seq = -1;
     return it;
+}
+
+// Rows of no sequence.  What follows attention, and what the gradients of its inputs go into, runs over whole tensors, so such rows are zeros and not
+// whatever was in memory.  They lie before a sequence and behind the one before it; workgroups at the end of a launch look for them: all waves share
+// those before the first sequence and behind the last, where padding is, others take a wave each.  Pointers that lie outside or do not ascend
+// describe no sequences, and which of their rows are zeros is open.
+constexpr unsigned kGapWorkgroups = 64;
+inline unsigned attn_gap_workgroups(const AttnArgs &a, bool queries, bool keys) {
+    return (queries && (a.q_ptr || (int64_t)a.n_seq * a.max_q < a.q_rows)) || (keys && (a.k_ptr || a.k_len || (int64_t)a.n_seq * a.max_k < a.k_rows))
+               ? kGapWorkgroups : 0;
+}
+__device__ __forceinline__ void zero_gaps(const AttnArgs &a, const AttnView &x, bool keys) {
+    const int lane = threadIdx.x & 63, waves = kGapWorkgroups * (blockDim.x >> 6), wave = (blockIdx.x - a.work) * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    const int64_t all = keys ? a.k_rows : a.q_rows;
+    const int each = a.dim / 8, pieces = (keys ? a.kv_heads : a.heads) * each;   // of 16 bytes
+    auto zero = [&](int64_t from, int64_t to, int64_t step) {
+        for (int64_t row = from; row < to; row += step)
+            for (int p = lane; p < pieces; p += 64) *(i32x4 *)(x.data + (row * x.row + p / each * x.head + p % each * 8) * 2) = i32x4{0, 0, 0, 0};
+    };
+    auto gap = [&](int s, int64_t &from, int64_t &to) {   // between sequences s - 1 and s
+        from = 0, to = all;
+        if (s > 0) {
+            const AttnSeq before = attn_seq(a, s - 1);
+            from = min(all, max((int64_t)0, keys ? before.k0 + before.nk : before.q0 + before.nq));
+        }
+        if (s < a.n_seq) {
+            const AttnSeq behind = attn_seq(a, s);
+            to = min(all, keys ? behind.k0 : behind.q0);
+        }
+    };
+    int64_t from, to;
+    gap(0, from, to);
+    zero(from + wave, to, waves);
+    if (a.n_seq == 0) return;
+    gap(a.n_seq, from, to);
+    zero(from + wave, to, waves);
+    for (int64_t s0 = 1 + (int64_t)wave * 64; s0 < a.n_seq; s0 += (int64_t)waves * 64) {
+        from = to = 0;
+        if (s0 + lane < a.n_seq) gap((int)s0 + lane, from, to);
+        for (uint64_t some = __ballot(from < to); some; some &= some - 1) {
+            const int l = __ffsll((unsigned long long)some) - 1;
+            zero(__shfl(from, l), __shfl(to, l), 1);
+        }
+    }
 }
 
 // A lane's row as an operand: elements 16 * s + 8 * half .. + 7 in regs[s], zeros past the head's.
@@ -314,9 +359,12 @@ template <int SIZE>
 __device__ __forceinline__ void ring_cuts(DistanceRing<SIZE> &ring, const AttnArgs &a, const AttnCuts &c) {
     if (threadIdx.x < kAttnBuckets) ring.cut[threadIdx.x] = (int)threadIdx.x < a.n_buckets - 1 ? c.at[threadIdx.x] : INT32_MAX;
 }
+// Times log2(e).  Scores of 32 bits that large have nothing left of the products, so a bias that can only be meant as a mask is one: rows that it
+// leaves without keys are zeros, whichever low value stands for it, and not the mean of the values or, in the gradients, 2^(score - lse) of anything.
+__device__ __forceinline__ float bias_value(float x) { return x < GBT_BIAS_SHUT ? -INFINITY : x * GBT_LOG2E; }
 template <int SIZE>
 __device__ __forceinline__ void ring_head(DistanceRing<SIZE> &ring, const AttnArgs &a, int head) {
-    for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) ring.of_bucket[i] = a.bias[(int64_t)i * a.heads + head] * GBT_LOG2E;
+    for (int i = threadIdx.x; i < a.n_buckets; i += blockDim.x) ring.of_bucket[i] = bias_value(a.bias[(int64_t)i * a.heads + head]);
 }
 // The bucket of distance t0 + lane, for a whole wave.  The lane of each cut among the 64 distances marks its place in LDS; how many marks are at
 // or before a distance is then a count of bits.

@@ -42,7 +42,7 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
     *code = GBT_EINVAL;
     if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads || p.heads > (1 << 16)) return "heads is no multiple of kv_heads, or out of range";
     if (p.n_seq < 0 || p.max_q < 0 || p.max_k < 0 || p.max_q > (1 << 29) || p.max_k > (1 << 29)) return "n_seq, max_q or max_k out of range";
-    if (p.q_rows < 0 || p.k_rows < 0) return "q_rows or k_rows < 0";
+    if (p.q_rows < 0 || p.k_rows < 0 || p.q_rows > ((int64_t)1 << 40) || p.k_rows > ((int64_t)1 << 40)) return "q_rows or k_rows out of range";
     if (p.n_buckets < 0) return "n_buckets < 0";
     if (!(p.scale >= 1e-6f && p.scale <= 1e6f)) return "scale outside 1e-6..1e6";
     if (p.n_seq > 0 && !p.q_ptr && p.q_rows / p.n_seq < p.max_q) return "q_rows < n_seq * max_q without q_ptr";
@@ -122,7 +122,7 @@ extern "C" int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *param
     GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
     GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     GBT_REQUIRE(ctx, ((uintptr_t)workspace & 15u) == 0 || need == 0, GBT_EINVAL, "workspace is not 16-byte aligned");
-    if (p.n_seq == 0 || p.max_q == 0 || p.q_rows == 0) return GBT_OK;
+    if (p.q_rows == 0) return GBT_OK;
     AttnArgs a;
     AttnCuts c;
     fill(a, c, p);
@@ -132,7 +132,7 @@ extern "C" int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *param
     a.out = view(out);
     a.lse = lse_out;
     a.rest = (char *)rest_out;
-    if (takes_few(p)) {
+    if (p.n_seq > 0 && p.max_q > 0 && takes_few(p)) {
         const FewPlan f = few_plan(p);
         a.pieces = f.pieces;
         a.piece_len = f.piece_len;

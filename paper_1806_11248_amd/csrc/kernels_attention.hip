@@ -28,6 +28,7 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
 
+    if (blockIdx.x >= a.work) return zero_gaps(a, a.out, false);
     const AttnItem item = attn_item(a.order, a.n_seq);
     if (item.seq < 0) return;
     // the blocks that see the most keys first
@@ -217,6 +218,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     __shared__ float join_top[4][32], join_sum[4][32];
     extern __shared__ float table[];   // [n_buckets][32 columns]: the bias, times log2(e)
 
+    if (blockIdx.x >= a.work) return zero_gaps(a, a.out, false);
     const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
     const int64_t item = blockIdx.x;
     const int piece = (int)(item % a.pieces), block = (int)(item / a.pieces % blocks);
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     const LaneCuts cuts{lane < a.n_buckets - 1 ? c.at[lane] : INT32_MAX, lane + 64 < a.n_buckets - 1 ? c.at[lane + 64] : INT32_MAX};
     if (bias) {
         const float *from = a.bias + (there ? head : 0);
-        for (int i = 2 * wave + half; i < a.n_buckets; i += 8) table[32 * i + col] = from[(int64_t)i * a.heads] * GBT_LOG2E;
+        for (int i = 2 * wave + half; i < a.n_buckets; i += 8) table[32 * i + col] = bias_value(from[(int64_t)i * a.heads]);
     }
     arrived(qf);
     if (start < end) {
@@ -431,7 +433,9 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
     AttnArgs b = a;
     b.order = attn_order(a.heads, blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
-    const unsigned grid = attn_grid(b.order);
+    b.work = attn_grid(b.order);
+    const unsigned grid = b.work + attn_gap_workgroups(a, true, false);
+    if (grid == 0) return hipSuccess;
     if (attn_two_groups(blocks * a.heads * a.n_seq, a.max_k)) attention_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
     else attention_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
     return hipGetLastError();
@@ -440,7 +444,9 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
 template <typename P, int DP>
 hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t columns = (int64_t)a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
-    attention_few_kernel<P, DP><<<(unsigned)(a.pieces * blocks * a.kv_heads * a.n_seq), 256, a.n_buckets * 32 * sizeof(float), stream>>>(a, c);
+    AttnArgs b = a;
+    b.work = (unsigned)(a.pieces * blocks * a.kv_heads * a.n_seq);
+    attention_few_kernel<P, DP><<<b.work + attn_gap_workgroups(a, true, false), 256, a.n_buckets * 32 * sizeof(float), stream>>>(b, c);
     if (a.pieces > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -51,6 +51,11 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
 
+    if (blockIdx.x >= a.work) {
+        zero_gaps(a, a.dq, false);
+        zero_gaps(a, a.dk, true);
+        return zero_gaps(a, a.dv, true);
+    }
     const AttnItem item = attn_item(a.order, a.n_seq);
     if (item.seq < 0) return;
     const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
@@ -456,6 +461,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
             }
         }
     }
+    if constexpr (kValuesInLds) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the values, if nobody has read them
     if constexpr (kWaves == 8) {   // the two halves' sums together, through LDS; 0 .. 3 hold them then
         float *mine = (float *)(key_wave < 2 ? &q_tile[0][0] : &g_tile[0][0]) + (key_wave & 1) * kBlocks * 16 * 64 + lane;
         auto join = [&](f32x16 (&x)[kBlocks]) {
@@ -566,11 +572,13 @@ template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const int64_t q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries, k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
     hipError_t e = hipSuccess;
-    if (q_blocks > 0 && a.n_seq > 0) {
+    {
         AttnArgs b = a;
         b.order = attn_order(a.heads, q_blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
-        const unsigned grid = attn_grid(b.order);
-        if (attn_two_groups(q_blocks * a.heads * a.n_seq, a.max_k)) grad_queries_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
+        b.work = attn_grid(b.order);
+        const unsigned grid = b.work + attn_gap_workgroups(a, true, true);
+        if (grid == 0) {
+        } else if (attn_two_groups(q_blocks * a.heads * a.n_seq, a.max_k)) grad_queries_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
         else grad_queries_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
         e = hipGetLastError();
     }

@@ -217,14 +217,15 @@ def test_rows_far_apart(ctx):
 
 
 def test_pointers_beyond_the_rows_describe_nothing(ctx):
-    """Row pointers come from the device unchecked: what does not lie inside the tensors is not read, and not written."""
+    """Row pointers come from the device unchecked: what does not lie inside the tensors is not read, and its rows are those of no sequence."""
     q, k, v, dout, args, spans = _make([40, 40], [40, 40], 2, 2, 64, BF, causal=True, buckets=4, seed=12)
     out = torch.full_like(q, 5.0)
     for bad in ([0, 10 ** 12, 80], [-5, 40, 10 ** 15], [60, 20, 10]):
         a = dict(args, q_ptr=torch.tensor(bad).cuda(), k_ptr=torch.tensor(bad).cuda())
+        out.fill_(5.0)
         ctx.attention(q, k, v, out=out, **a)
         torch.cuda.synchronize()
-    assert bool((out[10:] == 5.0).any())
+        assert not out.any()
 
 
 def test_another_stream_than_the_current_one(ctx):
@@ -416,3 +417,75 @@ def test_many_sequences(ctx):
     nq[13] = 300
     _check(ctx, _make(nq, nq, 3, 1, 16, BF, causal=True, buckets=6, seed=25))
     _check(ctx, _make(nq[:20], nq[:20], 3, 3, 16, HF, causal=False, buckets=6, seed=26))
+
+
+def test_rows_of_no_sequence_get_zeros(ctx):
+    """Before the first sequence, behind the last, beyond k_len and beyond the longest: whatever memory held, and whatever q, k and v hold there."""
+    rng = torch.Generator().manual_seed(30)
+    H, K, D = 4, 2, 64
+    for nq, nk, room, causal in (([150, 0, 90], [150, 20, 90], 0, True), ([30, 400, 2], [260, 400, 1], 9, False), ([1, 2, 0], [300, 1500, 4], 70, True), ([0, 0], [5, 0], 3, False)):
+        q_ptr, k_ptr = [7 + x for x in rows_of(nq)], [5 + x for x in rows_of([n + room for n in nk])]
+        q, dout = (torch.randn(q_ptr[-1] + 1_000, H, D, generator=rng).to(BF) for _ in range(2))
+        k, v = (torch.randn(k_ptr[-1] + 300, K, D, generator=rng).to(BF) for _ in range(2))
+        spans = list(zip(q_ptr[:-1], nq, k_ptr[:-1], nk))
+        bias, cuts = torch.randn(5, H, generator=rng), [-90, -7, 0, 12]
+        ref = Reference(q, k, v, spans, causal, D ** -0.5, bias, cuts, dout)
+        for t, covered in ((q, ref.covered_q), (dout, ref.covered_q), (k, ref.covered_k), (v, ref.covered_k)):
+            t[~covered] = math.nan
+        q, k, v, dout = q.cuda(), k.cuda(), v.cuda(), dout.cuda()
+        args = dict(q_ptr=torch.tensor(q_ptr).cuda(), k_ptr=torch.tensor(k_ptr).cuda(), k_len=torch.tensor(nk, dtype=torch.int32).cuda() if room else None,
+                    max_q=max(nq), max_k=max(nk), causal=causal, bias=bias.cuda(), cuts=cuts)
+        for _ in range(3):                 # memory that held something else before
+            torch.full((q.numel() + 4 * k.numel(),), math.nan, dtype=BF, device="cuda")
+            out, saved = ctx.attention(q, k, v, save=True, **args)
+            got = (out, *ctx.attention_backward(dout, q, k, v, out, saved, **args))
+        for name, x in zip(("out", "dq", "dk", "dv", "dbias"), got):
+            if name != "dbias":
+                covered = ref.covered_k if name in ("dk", "dv") else ref.covered_q
+                assert not x.cpu()[~covered].any(), name
+            close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
+    # more rows than n_seq * max
+    q = torch.randn(50, H, D, generator=rng).to(BF).cuda()
+    none = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out = torch.full_like(q, 3.0)
+    ctx.attention(q, q, q, q_ptr=none, k_ptr=none, max_q=0, max_k=0, out=out)
+    assert not out.any()
+
+
+def test_many_gaps(ctx):
+    """More sequences than the lanes that look for gaps between them."""
+    n, room = 20_000, 3
+    rng = torch.Generator().manual_seed(31)
+    k_len = torch.randint(0, 4, (n,), generator=rng, dtype=torch.int32)
+    k, q, dout = (torch.randn(rows, 1, 8, generator=rng).to(BF).cuda() for rows in (n * room, n, n))
+    k_ptr = (torch.arange(n + 1) * room).cuda()
+    args = dict(q_ptr=torch.arange(n + 1).cuda(), k_ptr=k_ptr, k_len=k_len.cuda(), max_q=1, max_k=room)
+    for _ in range(2):
+        torch.full((4 * k.numel(),), math.nan, dtype=BF, device="cuda")
+        out, saved = ctx.attention(q, k, k, save=True, **args)
+        dq, dk, dv, _ = ctx.attention_backward(dout, q, k, k, out, saved, **args)
+    unused = (torch.arange(room) >= k_len[:, None]).flatten()
+    assert not dk.cpu()[unused].any() and not dv.cpu()[unused].any()
+    assert not out.cpu()[k_len == 0].any() and not dq.cpu()[k_len == 0].any()
+    for x in (out, dq, dk, dv):
+        assert torch.isfinite(x).all()
+
+
+@pytest.mark.parametrize("nq", [1, 200])
+def test_low_values_in_the_bias_shut_a_bucket_out(ctx, nq):
+    """Whichever low value stands for a mask, results are those of -inf; rows that it leaves without keys are zeros, with zero gradients."""
+    q, k, v, dout, args, spans = _make([nq, nq], [200, 330], 4, 2, 64, BF, causal=False, buckets=4, far=40, seed=32, spread=8.0)
+    bias = args["bias"]
+    for shut in ([0], [1, 2], [0, 1, 2, 3]):
+        want = None
+        for low in (-math.inf, torch.finfo(torch.float32).min, -1e10, -1e9, -2e5):
+            args["bias"] = bias.clone()
+            args["bias"][shut] = low
+            out, saved = ctx.attention(q, k, v, save=True, **args)
+            got = (out, saved[0], *ctx.attention_backward(dout, q, k, v, out, saved, **args))
+            if want is None:
+                want = got
+                ref = _reference(q, k, v, args, spans, dout)
+                close(out, ref.out, ref.out_tol, "out")
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert not any(x.any() for i, x in enumerate(want) if i != 1)
