@@ -275,13 +275,11 @@ def distance_cuts(n_buckets: int, far: int, causal: bool = True) -> list:
     return [-s for s in reversed(steps)] + [s + 1 for s in steps[:n - back]]
 
 
-def _heads(t, name, dtype, rows=None, heads=None, dim=None):
-    """gbt_heads of a tensor [rows][heads][head_dim] whose last axis is contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 3):
-        raise TypeError(f"{name}: expected a CUDA tensor [rows][heads][head_dim] of {dtype}")
-    n, h, d = t.shape
-    if (rows is not None and n != rows) or (heads is not None and h != heads) or (dim is not None and d != dim):
-        raise TypeError(f"{name}: expected [{rows}][{heads}][{dim}], not {tuple(t.shape)}")
+def _heads(t, name, dtype, shape=None):
+    """gbt_heads of a tensor [rows][heads][head_dim] (of that shape) whose last axis is contiguous."""
+    n, h, d = shape or t.shape
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == (n, h, d)):
+        raise TypeError(f"{name}: expected a CUDA tensor [{n}][{h}][{d}] of {dtype}")
     row, head, one = t.stride()
     if one != 1 and n and h and d > 1:
         raise TypeError(f"{name}: expected a contiguous last axis")
@@ -671,6 +669,8 @@ class Context:
             raise TypeError("q, k: expected tensors [rows][heads][head_dim]")
         rows, heads, dim = q.shape
         k_rows, kv_heads, _ = k.shape
+        if not (q.is_cuda and k.is_cuda):
+            raise TypeError("q, k: expected CUDA tensors")
         n_seq = None
         if q_ptr is not None:
             n_seq = _need(q_ptr, torch.int64, "q_ptr").numel() - 1
@@ -720,19 +720,19 @@ class Context:
         """
         p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
         dtype = q.dtype
-        rows, heads, dim = q.shape
-        k_rows, kv_heads, _ = k.shape
-        hq, hk, hv = _heads(q, "q", dtype), _heads(k, "k", dtype, k_rows, kv_heads, dim), _heads(v, "v", dtype, k_rows, kv_heads, dim)
+        of_q = rows, heads, dim = q.shape
+        of_k = p.k_rows, p.kv_heads, dim
+        hq, hk, hv = _heads(q, "q", dtype, of_q), _heads(k, "k", dtype, of_k), _heads(v, "v", dtype, of_k)
         lib, at = self.lib, C.byref(p)
         ws_bytes = lib.gbt_attention_workspace_bytes(at)
         lse = rest = None
         with self._on_stream((q, k, v, q_ptr, k_ptr, k_len, bias, out)) or _NO_STREAM:
             if out is None:
-                out = self.empty((rows, heads, dim), dtype)
+                out = q.new_empty(rows, heads, dim)
             if save:
-                lse, rest = self.empty((heads, rows), torch.float32), self.empty((rows, heads, dim), dtype)
+                lse, rest = self.empty((heads, rows), torch.float32), q.new_empty(rows, heads, dim)
             ws = self.workspace("attention", ws_bytes) if ws_bytes else None
-        ho = _heads(out, "out", dtype, rows, heads, dim)
+        ho = _heads(out, "out", dtype, of_q)
         st = lib.gbt_attention(self.h, at, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr() if save else None,
                                rest.data_ptr() if save else None, ws.data_ptr() if ws_bytes else None, ws_bytes)
         if st:
@@ -745,22 +745,21 @@ class Context:
         sequence get zeros, rows beyond k_len too."""
         p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
         dtype = q.dtype
-        rows, heads, dim = q.shape
-        k_rows, kv_heads, _ = k.shape
+        of_q = rows, heads, dim = q.shape
+        of_k = k_rows, kv_heads, dim = p.k_rows, p.kv_heads, dim
         lse, rest = saved
         _need(lse, torch.float32, "saved[0]")
         if rest is not None:
             _need(rest, dtype, "saved[1]")
-        if lse.shape != (heads, rows) or (rest is not None and rest.shape != q.shape):
+        if lse.shape != (heads, rows) or (rest is not None and rest.shape != of_q):
             raise TypeError(f"saved: not of a call with q of {tuple(q.shape)}")
-        hg, hq, ho = (_heads(t, n, dtype, rows, heads, dim) for t, n in ((dout, "dout"), (q, "q"), (out, "out")))
-        hk, hv = _heads(k, "k", dtype, k_rows, kv_heads, dim), _heads(v, "v", dtype, k_rows, kv_heads, dim)
+        hg, hq, ho = _heads(dout, "dout", dtype, of_q), _heads(q, "q", dtype, of_q), _heads(out, "out", dtype, of_q)
+        hk, hv = _heads(k, "k", dtype, of_k), _heads(v, "v", dtype, of_k)
         lib, at = self.lib, C.byref(p)
         ws_bytes = lib.gbt_attention_backward_workspace_bytes(at)
         with self._on_stream((dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias)) or _NO_STREAM:
-            dq = self.empty((rows, heads, dim), dtype)
-            dk, dv = self.empty((k_rows, kv_heads, dim), dtype), self.empty((k_rows, kv_heads, dim), dtype)
-            dbias = None if bias is None else self.empty(bias.shape, torch.float32)
+            dq, dk, dv = q.new_empty(rows, heads, dim), q.new_empty(k_rows, kv_heads, dim), q.new_empty(k_rows, kv_heads, dim)
+            dbias = None if bias is None else torch.empty_like(bias)
             ws = self.workspace("attention", ws_bytes)
         hdq, hdk, hdv = Heads(dq.data_ptr(), heads * dim, dim), Heads(dk.data_ptr(), kv_heads * dim, dim), Heads(dv.data_ptr(), kv_heads * dim, dim)
         st = lib.gbt_attention_backward(self.h, at, C.byref(hg), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr(),
