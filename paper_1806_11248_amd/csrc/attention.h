@@ -65,11 +65,20 @@ struct AttnArgs {
     int pieces, piece_len;
 };
 
-// Where a launch has no more workgroups than there are compute units and its keys are several tiles, two groups of four waves share a workgroup's
-// queries and take the tiles in turn.  us forward and backward with one group and two (causal): 64 workgroups, 500 keys 13.4 + 45.8, 12.4 + 44.6;
-// 256, 1000 keys 22.3 + 85.1, 19.4 + 80.3; 256, 2000 keys of 128 elements 48.9 + 217.8, 41.3 + 181.1; but 512, 1000 keys 44.3 + 193, 53.4 + 199;
-// 4, 100 keys 7.1 + 23.8, 7.7 + 24.8.
-inline bool attn_two_groups(int64_t workgroups, int64_t max_k) { return workgroups <= 256 && max_k >= 256; }
+// How many queries a workgroup of the kernels that own queries takes, 32 a wave, and in how many groups of waves that take the tiles of keys in turn.
+// Where a launch has no more workgroups than there are compute units and its keys are several tiles, how many steps follow one another is what counts:
+// two groups, of 64 queries where LDS has room for two such workgroups a compute unit.  us forward and backward, 128 queries and one group, 128 and two,
+// 64 and two (heads of 64 elements, causal): 4 histories of 100 to 1000 rows, 8 heads 19.0 + 64, 16.2 + 61, 14.7 + 58; 4 of 1000 21.9 + 78, 18.4 + 74,
+// 16.9 + 71; one of 4096, 4 heads 65 + 143, 48 + 122, 40 + 110; but 16 of 1000 35.7 + 132, 45.7 + 146, 47.4 + 141; 32 of 100 13.0 + 28, 13.1 + 32,
+// 12.5 + 31.
+struct AttnForm {
+    int queries, groups;
+};
+inline AttnForm attn_form(const AttnArgs &a, int DP) {
+    const int64_t workgroups = (a.max_q + 127) / 128 * (int64_t)a.heads * a.n_seq;
+    if (workgroups > 256 || a.max_k < 256) return AttnForm{128, 1};
+    return AttnForm{DP <= 64 ? 64 : 128, 2};
+}
 
 struct AttnCuts {
     int32_t at[kAttnBuckets - 1];   // ascending
@@ -240,25 +249,27 @@ __device__ __forceinline__ void load_word_to_lds(uint32_t to, const float *base,
 // compute unit reads 219 to 235 bytes a clock so; with rows 16 or 32 bytes further apart instead, 122 to 125 by one kind of read or both.
 template <int DP>
 struct Tile {
-    static constexpr int kRowBytes = DP == 96 ? 256 : DP * 2, kPlaces = kRowBytes / 16, kBytes = 64 * kRowBytes, kLoads = kPlaces / 4;
+    static constexpr int kRowBytes = DP == 96 ? 256 : DP * 2, kPlaces = kRowBytes / 16, kBytes = 64 * kRowBytes;
     static __device__ __forceinline__ constexpr int fold(int row) {
         return kPlaces == 4 ? (row >> 2) & 3 : kPlaces == 8 ? ((row >> 1) & 1) * 4 | ((row >> 2) & 3) : (row & 3) * 4 | ((row >> 2) & 3);
     }
-    // From memory straight into LDS, a wave's 64 pieces at a time, by four waves, of which this one is number `wave`.  Rows past the last and elements past the head's are taken from
+    // From memory straight into LDS, a wave's 64 pieces at a time, by kWaves waves, of which this one is number `wave`.  Rows past the last and elements past the head's are taken from
     // the last there are, so that nothing hangs on a condition: such rows' probabilities are zero, and such elements meet zeros of the
     // other operand or are not stored.  rows, dim > 0; 64 * row_bytes < 2^32.
     // kKeep: addresses may be kept in registers from one call to the next; else they are worked out each time, for kernels that have none to spare (what
     // is kept in memory is waited for together with the loads before it).
-    template <bool kKeep = true>
+    template <bool kKeep = true, int kWaves = 4>
     static __device__ __forceinline__ void fetch(char *tile, const char *base, uint32_t row_bytes, int rows, int dim, int wave) {
         int lane = kKeep ? threadIdx.x & 63 : __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
         if (!kKeep) asm volatile("" : "+v"(lane));
-        constexpr int kRows = 64 / kPlaces;                       // of a wave's load
-        const int row = wave * kRows + lane / kPlaces;            // the i-th load's is 4 * kRows further, with the same fold
-        const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;
+        constexpr int kRows = 64 / kPlaces, kNext = kWaves * kRows;   // of a wave's load, and how much further its next one is
+        const int row = wave * kRows + lane / kPlaces;
         const uint32_t to = lds_address(tile) + wave * 1024;
+        const uint32_t col = min(lane % kPlaces ^ fold(row), dim / 8 - 1) * 16;
+        const uint32_t odd = kNext % 16 == 0 ? col : min(lane % kPlaces ^ fold(row + kNext), dim / 8 - 1) * 16;   // a fold has a period of 16 rows
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_to_lds(to + i * 4096, base, (uint32_t)min(row + i * 4 * kRows, rows - 1) * row_bytes + col);
+        for (int i = 0; i < kPlaces / kWaves; ++i)
+            load_to_lds(to + i * kWaves * 1024, base, (uint32_t)min(row + i * kNext, rows - 1) * row_bytes + (i & 1 ? odd : col));
     }
     // The first 32 rows likewise, by one wave.
     static constexpr int kHalfLoads = kPlaces / 2;

@@ -18,12 +18,12 @@ constexpr float kSlack = 8.0f;
 // ------------------------------------------------------------------------------------------------ blocks of queries --
 // A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.  Of two groups of four
 // waves each takes every other tile for the same queries, and they are joined at the end: half the steps one after the other.
-template <typename P, int DP, int kGroups>
-__global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
+template <typename P, int DP, int kQWaves, int kGroups>
+__global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups, kQueries = 32 * kQWaves, kWaves = kQWaves * kGroups;
     __shared__ __align__(16) char k_tile[2][kGroups * T::kBytes];
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
@@ -34,16 +34,16 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     // the blocks that see the most keys first
     const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
     const AttnSeq rows = attn_seq(a, seq);
-    const int first = block * kAttnQueries;
+    const int first = block * kQueries;
     if (first >= rows.nq) return;
     const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int wave = kGroups == 2 ? any_wave & 3 : any_wave, group = kGroups == 2 ? any_wave >> 2 : 0;
+    const int wave = kGroups == 2 ? any_wave % kQWaves : any_wave, group = kGroups == 2 ? any_wave / kQWaves : 0;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool bias = a.n_buckets > 0;
     // keys 0 .. last are seen by this lane's query; `end` by any of the workgroup's
     const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
-    const int end = a.causal ? min(rows.nk, min(first + kAttnQueries, rows.nq) + off) : rows.nk;
+    const int end = a.causal ? min(rows.nk, min(first + kQueries, rows.nq) + off) : rows.nk;
     const int wave_first = first + wave * 32;                                               // the wave's keys end before
     const int wave_end = a.causal ? min(rows.nk, min(wave_first + 32, rows.nq) + off) : rows.nk;
     const int wave_all = a.causal ? min(rows.nk, wave_first + off + 1) : rows.nk;           // and all of its queries see those before
@@ -53,8 +53,8 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
 
     auto fetch = [&](int which, int kb) {
-        T::fetch(k_tile[which] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
-        T::fetch(v_tile[which] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
+        T::template fetch<true, kQWaves>(k_tile[which] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::template fetch<true, kQWaves>(v_tile[which] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
     };
     if (64 * group < end) fetch(0, 64 * group);
     V8 qf[kSteps];
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
     float top = -INFINITY, sum = 0.0f;
     arrived(qf);
     __syncthreads();
-    if (bias && any_wave < 2 + kGroups) ring_put(ring, 64 * any_wave - (first + 127 + off), any_wave, lane);
+    if (bias && any_wave < kQWaves / 2 + kGroups) ring_put(ring, 64 * any_wave - (first + kQueries - 1 + off), any_wave, lane);
 
     // one tile; which of the two copies it lies in is known at compile time, so that LDS addresses are constants of the lane
     auto step = [&](auto which, int k0) {
@@ -80,9 +80,9 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
         const int kb = k0 + 64 * group;
         tiles_ready();
         if (kb + kStride < end) fetch(1 - kNow, kb + kStride);
-        const int lowest = k0 - (first + 127 + off);   // distance
-        const int turn = (any_wave - (k0 >> 6)) & (4 * kGroups - 1);
-        if (bias && turn < kGroups) ring_put(ring, lowest + 127 + kStride + 64 * turn, any_wave, lane);
+        const int lowest = k0 - (first + kQueries - 1 + off);   // distance
+        const int turn = (any_wave - (k0 >> 6)) & (kWaves - 1);
+        if (bias && turn < kGroups) ring_put(ring, lowest + kQueries - 1 + kStride + 64 * turn, any_wave, lane);
         if (kb >= wave_end) return;
 
         f32x16 s[2];
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256 * kGroups, 2) void attention_kernel(AttnArgs a,
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         // scores in powers of two are s * factor + add
-        const int at = (lowest & ring.kMask) + 64 * group + 96 - 32 * wave;   // of the wave's lowest distance, of 95
+        const int at = (lowest & ring.kMask) + 64 * group + kQueries - 32 - 32 * wave;   // of the wave's lowest distance, of 95
         const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;
         float factor = a.scale2, add = 0.0f;
         if (b0 != b1) {
@@ -430,14 +430,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
 
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
-    const int64_t blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries;
+    const AttnForm form = attn_form(a, DP);
+    const int64_t blocks = (a.max_q + form.queries - 1) / form.queries;
     AttnArgs b = a;
     b.order = attn_order(a.heads, blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
     b.work = attn_grid(b.order);
     const unsigned grid = b.work + attn_gap_workgroups(a, true, false);
     if (grid == 0) return hipSuccess;
-    if (attn_two_groups(blocks * a.heads * a.n_seq, a.max_k)) attention_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
-    else attention_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
+    constexpr int kQWaves = DP <= 64 ? 2 : 4;
+    if (form.groups == 2) attention_kernel<P, DP, kQWaves, 2><<<grid, 128 * kQWaves, 0, stream>>>(b, c);
+    else attention_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
     return hipGetLastError();
 }
 

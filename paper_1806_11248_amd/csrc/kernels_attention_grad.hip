@@ -41,12 +41,12 @@ __device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int n
 
 // ---------------------------------------------------------------------------------------------------------- queries --
 // As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS, one group of four waves or two.
-template <typename P, int DP, int kGroups>
-__global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
+template <typename P, int DP, int kQWaves, int kGroups>
+__global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
     typedef Tile<DP> T;
-    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32, kStride = 64 * kGroups, kQueries = 32 * kQWaves, kWaves = kQWaves * kGroups;
     __shared__ __align__(16) char k_tile[2][kGroups * T::kBytes];
     __shared__ __align__(16) char v_tile[2][kGroups * T::kBytes];
     __shared__ DistanceRing<256 * kGroups> ring;
@@ -60,16 +60,16 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
     if (item.seq < 0) return;
     const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
     const AttnSeq rows = attn_seq(a, seq);
-    const int first = block * kAttnQueries;
+    const int first = block * kQueries;
     const bool bias = a.n_buckets > 0;
     if (first >= rows.nq) return;
     const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int wave = kGroups == 2 ? any_wave & 3 : any_wave, group = kGroups == 2 ? any_wave >> 2 : 0;
+    const int wave = kGroups == 2 ? any_wave % kQWaves : any_wave, group = kGroups == 2 ? any_wave / kQWaves : 0;
     const int off = rows.nk - rows.nq;
     const int query = first + wave * 32 + (lane & 31);
     const bool there = query < rows.nq;
     const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
-    const int end = a.causal ? min(rows.nk, min(first + kAttnQueries, rows.nq) + off) : rows.nk;
+    const int end = a.causal ? min(rows.nk, min(first + kQueries, rows.nq) + off) : rows.nk;
     const int wave_first = first + wave * 32;
     const int wave_end = wave_first >= rows.nq ? 0 : a.causal ? min(rows.nk, min(wave_first + 32, rows.nq) + off) : rows.nk;
     const int wave_all = a.causal ? min(rows.nk, wave_first + off + 1) : rows.nk;
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
     const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
 
     auto fetch = [&](int n, int kb) {
-        T::fetch(k_tile[n] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
-        T::fetch(v_tile[n] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
+        T::template fetch<true, kQWaves>(k_tile[n] + group * T::kBytes, k_base + (int64_t)kb * a.k.row * 2, (uint32_t)a.k.row * 2, end - kb, a.dim, wave);
+        T::template fetch<true, kQWaves>(v_tile[n] + group * T::kBytes, v_base + (int64_t)kb * a.v.row * 2, (uint32_t)a.v.row * 2, end - kb, a.dim, wave);
     };
     if (64 * group < end) fetch(0, 64 * group);
     const int64_t row = rows.q0 + min(query, rows.nq - 1);
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
     arrived(qf);
     arrived(gf);
     __syncthreads();
-    if (bias && any_wave < 2 + kGroups) ring_put(ring, 64 * any_wave - (first + 127 + off), any_wave, lane);
+    if (bias && any_wave < kQWaves / 2 + kGroups) ring_put(ring, 64 * any_wave - (first + kQueries - 1 + off), any_wave, lane);
 
     auto step = [&](auto which, int k0) {
         constexpr int kNow = decltype(which)::value;
@@ -123,14 +123,14 @@ __global__ __launch_bounds__(256 * kGroups, 2) void grad_queries_kernel(AttnArgs
         const int kb = k0 + 64 * group;
         tiles_ready();
         if (kb + kStride < end) fetch(1 - kNow, kb + kStride);
-        const int lowest = k0 - (first + 127 + off);
-        const int turn = (any_wave - (k0 >> 6)) & (4 * kGroups - 1);
-        if (bias && turn < kGroups) ring_put(ring, lowest + 127 + kStride + 64 * turn, any_wave, lane);
+        const int lowest = k0 - (first + kQueries - 1 + off);
+        const int turn = (any_wave - (k0 >> 6)) & (kWaves - 1);
+        if (bias && turn < kGroups) ring_put(ring, lowest + kQueries - 1 + kStride + 64 * turn, any_wave, lane);
         if (kb >= wave_end) return;
 
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int at = (lowest & ring.kMask) + 64 * group + 96 - 32 * wave + 32 * b;   // of this 32 x 32 result's lowest distance, of 63
+            const int at = (lowest & ring.kMask) + 64 * group + kQueries - 32 - 32 * wave + 32 * b;   // of this 32 x 32 result's lowest distance, of 63
             const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
             f32x16 s, dp;
 #pragma unroll
@@ -247,10 +247,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     const int k_blocks = a.order.blocks, parts = a.head_parts * a.q_parts;
     const AttnItem item = attn_item(a.order, a.n_seq);
     if (item.seq < 0) return;
-    const int block = item.block, part = item.unit % parts, kv_head = item.unit / parts, seq = item.seq;
+    const int part = item.unit % parts, kv_head = item.unit / parts, seq = item.seq;
     const int q_part = part % a.q_parts, head_part = part / a.q_parts;
     const int g_from = a.group * head_part / a.head_parts, g_to = a.group * (head_part + 1) / a.head_parts;
     const AttnSeq rows = attn_seq(a, seq);
+    // a causal block of keys has as many queries to meet as lie behind it: counted from the sequence's end, the same for all of one turn
+    int block = item.block;
+    if (a.causal) {
+        block -= k_blocks - (rows.nk + kAttnQueries - 1) / kAttnQueries;
+        if (block < 0) block += k_blocks;
+    }
     const int first = block * kAttnQueries;
     const bool bias = a.n_buckets > 0;
     auto strip = [&](int head) {
@@ -570,16 +576,18 @@ __global__ __launch_bounds__(1024) void grad_bias_kernel(AttnArgs a) {
 
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
-    const int64_t q_blocks = (a.max_q + kAttnQueries - 1) / kAttnQueries, k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
+    const AttnForm form = attn_form(a, DP);
+    const int64_t q_blocks = (a.max_q + form.queries - 1) / form.queries, k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
     hipError_t e = hipSuccess;
     {
         AttnArgs b = a;
         b.order = attn_order(a.heads, q_blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
         b.work = attn_grid(b.order);
+        constexpr int kQWaves = DP <= 64 ? 2 : 4;
         const unsigned grid = b.work + attn_gap_workgroups(a, true, true);
         if (grid == 0) {
-        } else if (attn_two_groups(q_blocks * a.heads * a.n_seq, a.max_k)) grad_queries_kernel<P, DP, 2><<<grid, 512, 0, stream>>>(b, c);
-        else grad_queries_kernel<P, DP, 1><<<grid, 256, 0, stream>>>(b, c);
+        } else if (form.groups == 2) grad_queries_kernel<P, DP, kQWaves, 2><<<grid, 128 * kQWaves, 0, stream>>>(b, c);
+        else grad_queries_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {
