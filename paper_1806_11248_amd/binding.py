@@ -663,6 +663,13 @@ class Context:
                 t.record_stream(self.stream)
         return torch.cuda.stream(self.stream)
 
+    def _scratch(self, key, nbytes):
+        """The workspace of that name.  A graph that is being recorded gets memory of its own: the workspace is given back when a larger
+        one takes its place, and replays would go on writing there."""
+        if torch.cuda.is_current_stream_capturing():
+            return self.empty((max(nbytes, 16),), torch.uint8)
+        return self.workspace(key, nbytes)
+
     def _attention_params(self, q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts):
         """(gbt_attention_params, what it points to on the host)."""
         if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3):
@@ -731,7 +738,7 @@ class Context:
                 out = q.new_empty(rows, heads, dim)
             if save:
                 lse, rest = self.empty((heads, rows), torch.float32), q.new_empty(rows, heads, dim)
-            ws = self.workspace("attention", ws_bytes) if ws_bytes else None
+            ws = self._scratch("attention", ws_bytes) if ws_bytes else None
         ho = _heads(out, "out", dtype, of_q)
         st = lib.gbt_attention(self.h, at, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr() if save else None,
                                rest.data_ptr() if save else None, ws.data_ptr() if ws_bytes else None, ws_bytes)
@@ -760,7 +767,7 @@ class Context:
         with self._on_stream((dout, q, k, v, out, lse, rest, q_ptr, k_ptr, k_len, bias)) or _NO_STREAM:
             dq, dk, dv = q.new_empty(rows, heads, dim), q.new_empty(k_rows, kv_heads, dim), q.new_empty(k_rows, kv_heads, dim)
             dbias = None if bias is None else torch.empty_like(bias)
-            ws = self.workspace("attention", ws_bytes)
+            ws = self._scratch("attention", ws_bytes)
         hdq, hdk, hdv = Heads(dq.data_ptr(), heads * dim, dim), Heads(dk.data_ptr(), kv_heads * dim, dim), Heads(dv.data_ptr(), kv_heads * dim, dim)
         st = lib.gbt_attention_backward(self.h, at, C.byref(hg), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr(),
                                         None if rest is None else rest.data_ptr(), C.byref(hdq), C.byref(hdk), C.byref(hdv),
@@ -796,7 +803,7 @@ class Context:
         on the device.  A norm that is not finite leaves the values as they are."""
         with self._on_stream(gradients.both) or _NO_STREAM:
             norm = self.empty((), torch.float32)
-            ws = self.workspace("clip", 16384)
+            ws = self._scratch("clip", 16384)
         st = self.lib.gbt_clip_gradients(self.h, gradients.table.data_ptr(), gradients.pieces, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel())
         if st:
             self._check(st)

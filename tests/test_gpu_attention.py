@@ -489,3 +489,34 @@ def test_low_values_in_the_bias_shut_a_bucket_out(ctx, nq):
                 close(out, ref.out, ref.out_tol, "out")
             assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert not any(x.any() for i, x in enumerate(want) if i != 1)
+
+
+def test_a_graph_keeps_its_workspace(ctx):
+    """A graph recorded before a larger call: its replays write to no memory that has been given back since."""
+    import paper_1806_11248_amd as g
+    side = torch.cuda.Stream()
+    own = g.Context(0, stream=side)
+    try:
+        with torch.cuda.stream(side):
+            small = _make([150, 90], [150, 90], 4, 2, 64, BF, causal=True, buckets=12, seed=40)
+            large = _make([700] * 6, [700] * 6, 4, 2, 64, BF, causal=True, buckets=12, seed=41)
+            few, many = (_make([1, 1], [n, 40], 4, 2, 64, BF, causal=True, buckets=12, seed=n) for n in (3_000, 30_000))
+
+            def run(made):
+                q, k, v, dout, args, _ = made
+                out, saved = own.attention(q, k, v, save=True, **args)
+                return (out, *own.attention_backward(dout, q, k, v, out, saved, **args))
+            eager = [run(m) for m in (small, few)]
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                recorded = [run(m) for m in (small, few)]
+            for _ in range(2):
+                run(large), run(many)                      # larger workspaces take the place of the first ones
+                others = [torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in [1 << 12, 1 << 16, 1 << 18, 1 << 20, 1 << 21, 1 << 22] for _ in range(4)]
+                graph.replay()
+                side.synchronize()
+                assert all(bool((x == 9).all()) for x in others)
+                assert all(torch.equal(a, b) for x, y in zip(recorded, eager) for a, b in zip(x, y))
+    finally:
+        own.close()
