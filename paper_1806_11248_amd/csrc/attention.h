@@ -66,18 +66,23 @@ struct AttnArgs {
 };
 
 // How many queries a workgroup of the kernels that own queries takes, 32 a wave, and in how many groups of waves that take the tiles of keys in turn.
-// Where a launch has no more workgroups than there are compute units and its keys are several tiles, how many steps follow one another is what counts:
-// two groups, of 64 queries where LDS has room for two such workgroups a compute unit.  us forward and backward, 128 queries and one group, 128 and two,
-// 64 and two (heads of 64 elements, causal): 4 histories of 100 to 1000 rows, 8 heads 19.0 + 64, 16.2 + 61, 14.7 + 58; 4 of 1000 21.9 + 78, 18.4 + 74,
-// 16.9 + 71; one of 4096, 4 heads 65 + 143, 48 + 122, 40 + 110; but 16 of 1000 35.7 + 132, 45.7 + 146, 47.4 + 141; 32 of 100 13.0 + 28, 13.1 + 32,
-// 12.5 + 31.
+// Where there are fewer workgroups of 128 than compute units and keys are several tiles, how many steps follow one another is what counts: two groups
+// halve them.  Two groups of 64 queries spread over twice as many compute units; with heads of more than 64 elements LDS has room for only one such
+// workgroup on each, so they must all run at once.  Workgroups are counted as the rows give them, not as max_q would.
+// us forward and backward, 128 queries and one group, 128 and two, 64 and two, causal: heads of 64 elements, 4 histories of 100 to 1000 rows, 8 heads
+// 19.0 + 64, 16.2 + 61, 14.7 + 58; one of 4096, 4 heads 65 + 143, 48 + 122, 40 + 110; but 16 of 1000 35.7 + 132, 45.7 + 146, 47.4 + 141; heads of 80, 3 of
+// 300 to 800, 6 heads 20.1 + 65, 17.8 + 61, 16.8 + 58; 5 20.1 + 68, 17.1 + 64, 20.0 + 65; not causal 20.9 + 71, 18.6 + 69, 27.0 + 77; 9 23.2 + 89,
+// 25.0 + 91, 36.3 + 101; one of 2000, 16 heads 46.9 + 173, 38.5 + 165, 65.3 + 193; heads of 128, 3 21.9 + 68, 19.3 + 71, 18.1 + 63; 5 22.2 + 77, 19.9 + 79, 22.8 + 76 (two groups of the backward kernel at 128
+// queries have too few registers, so there it has one).
 struct AttnForm {
     int queries, groups;
 };
-inline AttnForm attn_form(const AttnArgs &a, int DP) {
-    const int64_t workgroups = (a.max_q + 127) / 128 * (int64_t)a.heads * a.n_seq;
-    if (workgroups > 256 || a.max_k < 256) return AttnForm{128, 1};
-    return AttnForm{DP <= 64 ? 64 : 128, 2};
+inline AttnForm attn_form(const AttnArgs &a, int DP, bool backward) {
+    const int64_t most = (a.max_q + 127) / 128 * (int64_t)a.n_seq, workgroups = a.heads * std::min(most, a.q_rows / 128 + (a.n_seq + 1) / 2);
+    if (a.max_k < 256 || workgroups > 256 || a.heads * most > (1 << 20)) return AttnForm{128, 1};   // (the launch is as large as max_q says)
+    const bool even = a.heads % 8 == 0 || a.n_seq == 1;   // over the XCDs
+    if (DP <= 64 || workgroups <= (even ? 128 : 96)) return AttnForm{64, 2};
+    return AttnForm{128, backward && DP == 128 ? 1 : 2};
 }
 
 struct AttnCuts {

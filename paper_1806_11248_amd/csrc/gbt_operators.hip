@@ -54,11 +54,10 @@ const char *params_fault(const gbt_attention_params &p, int32_t *code) {
         for (int i = 1; i < p.n_buckets - 1; ++i)
             if (p.cuts[i] <= p.cuts[i - 1]) return "cuts do not increase";
     }
-    const int64_t limit = (int64_t)1 << 30;   // workgroups of a launch
-    const FewPlan f = few_plan(p);
-    if (std::max(blocks_of(p.max_q) * p.heads, (p.max_k + 3) / 4 * (int64_t)p.kv_heads) > limit / std::max(1, p.n_seq) ||
-        f.columns * p.kv_heads > limit / std::max(1, p.n_seq))
-        return "too many sequences";
+    const int64_t limit = ((int64_t)1 << 23) - 1024;   // workgroups of a launch, of up to 512 threads, of which there can be 2^32
+    if (std::max({blocks_of(p.max_q) * p.heads, blocks_of(p.max_k) * p.kv_heads, takes_few(p) ? (int64_t)p.max_q * p.heads : 0}) >
+        limit / std::max(1, p.n_seq))
+        return "too many sequences for max_q or max_k";
     return nullptr;
 }
 

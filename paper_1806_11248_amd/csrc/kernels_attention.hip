@@ -430,16 +430,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
 
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
-    const AttnForm form = attn_form(a, DP);
+    const AttnForm form = attn_form(a, DP, false);
     const int64_t blocks = (a.max_q + form.queries - 1) / form.queries;
     AttnArgs b = a;
     b.order = attn_order(a.heads, blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
     b.work = attn_grid(b.order);
     const unsigned grid = b.work + attn_gap_workgroups(a, true, false);
     if (grid == 0) return hipSuccess;
-    constexpr int kQWaves = DP <= 64 ? 2 : 4;
-    if (form.groups == 2) attention_kernel<P, DP, kQWaves, 2><<<grid, 128 * kQWaves, 0, stream>>>(b, c);
-    else attention_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
+    if (form.queries == 64) attention_kernel<P, DP, 2, 2><<<grid, 256, 0, stream>>>(b, c);
+    else if (form.groups == 1) attention_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
+    else if constexpr (DP > 64) attention_kernel<P, DP, 4, 2><<<grid, 512, 0, stream>>>(b, c);
     return hipGetLastError();
 }
 

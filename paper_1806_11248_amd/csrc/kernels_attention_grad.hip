@@ -576,18 +576,18 @@ __global__ __launch_bounds__(1024) void grad_bias_kernel(AttnArgs a) {
 
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
-    const AttnForm form = attn_form(a, DP);
+    const AttnForm form = attn_form(a, DP, true);
     const int64_t q_blocks = (a.max_q + form.queries - 1) / form.queries, k_blocks = (a.max_k + kAttnQueries - 1) / kAttnQueries;
     hipError_t e = hipSuccess;
     {
         AttnArgs b = a;
         b.order = attn_order(a.heads, q_blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
         b.work = attn_grid(b.order);
-        constexpr int kQWaves = DP <= 64 ? 2 : 4;
         const unsigned grid = b.work + attn_gap_workgroups(a, true, true);
         if (grid == 0) {
-        } else if (form.groups == 2) grad_queries_kernel<P, DP, kQWaves, 2><<<grid, 128 * kQWaves, 0, stream>>>(b, c);
-        else grad_queries_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
+        } else if (form.queries == 64) grad_queries_kernel<P, DP, 2, 2><<<grid, 256, 0, stream>>>(b, c);
+        else if (form.groups == 1) grad_queries_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
+        else if constexpr (DP == 96) grad_queries_kernel<P, DP, 4, 2><<<grid, 512, 0, stream>>>(b, c);
         e = hipGetLastError();
     }
     if (e == hipSuccess && k_blocks > 0 && a.n_seq > 0) {

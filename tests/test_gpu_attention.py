@@ -323,6 +323,8 @@ def test_refusals(ctx):
     refused(b.EINVAL, lambda: ctx.attention(q, three, three))
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, cuts=[1, 1, 2])))
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, scale=math.inf)))
+    refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, max_q=1 << 29)))          # more workgroups than a launch can have
+    refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, max_k=(1 << 29) + 1)))
     shifted = torch.zeros(20 * 4 * 64 + 8, dtype=BF, device="cuda")[4:20 * 4 * 64 + 4].view(20, 4, 64)
     refused(b.EINVAL, lambda: ctx.attention(shifted, k, v, **args))
     many = torch.zeros(300, 4, device="cuda")
