@@ -115,10 +115,11 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
             add = ring.of_bucket[b0];
         }
         if (kb + 64 > wave_all) {
+            const int past = last - kb - 4 * half;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = kb + 32 * b + result_row(r, half) <= last ? s[b][r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + result_row(r, 0) <= past ? s[b][r] : -INFINITY;
         }
         float now = -INFINITY;
 #pragma unroll
@@ -288,11 +289,9 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
             add = table[32 * b0 + col];
         }
         if (kb + 32 > all) {
+            const int past = min(last, end - 1) - kb - 4 * half;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = kb + result_row(r, half);
-                s[r] = key <= last && key < end ? s[r] : -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r) s[r] = result_row(r, 0) <= past ? s[r] : -INFINITY;
         }
         float now = -INFINITY;
 #pragma unroll

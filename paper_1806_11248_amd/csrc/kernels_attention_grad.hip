@@ -162,8 +162,9 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel
                 for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, add[result_row(r, half)] + minus));
             }
             if (kb + 32 * b + 32 > wave_all) {
+                const int past = last - (kb + 32 * b) - 4 * half;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = kb + 32 * b + result_row(r, half) <= last ? s[r] : 0.0f;
+                for (int r = 0; r < 16; ++r) s[r] = result_row(r, 0) <= past ? s[r] : 0.0f;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -399,11 +400,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                     }
                 }
                 if (qb + 32 * b < wave_all || qb + 32 * b + 32 > rows.nq) {   // rows past the last are the last one's copies
+                    const int since = sees - (qb + 32 * b) - 4 * half, past = rows.nq - (qb + 32 * b) - 4 * half;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int q = qb + 32 * b + result_row(r, half);
-                        s[r] = q >= sees && q < rows.nq ? s[r] : 0.0f;
-                    }
+                    for (int r = 0; r < 16; ++r) s[r] = result_row(r, 0) >= since && result_row(r, 0) < past ? s[r] : 0.0f;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] *= s[r];
