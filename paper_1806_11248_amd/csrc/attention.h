@@ -309,6 +309,28 @@ struct Tile {
         const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(typename P::vec8, both);
     }
+    // The same where the tile is not known at compile time: one address for all reads, which differ in bits that are zero in a tile's own (aligned
+    // to 256 bytes) and in constants that the instruction adds; `further` is that of another tile.  (fold(row + 8) is fold(row) ^ 2.)
+    static __device__ __forceinline__ uint32_t rows_base(const char *tile, int row0, int lane) {
+        const int row = lane & 31;
+        return lds_address(tile) + row0 * kRowBytes + row * kRowBytes + (((lane >> 5) ^ fold(row)) << 4);
+    }
+    template <typename P>
+    static __device__ __forceinline__ typename P::vec8 rows_at(uint32_t base, int step, int further) {
+        return *(const __attribute__((address_space(3))) typename P::vec8 *)(uintptr_t)((base ^ (step << 5)) + further);
+    }
+    static __device__ __forceinline__ uint32_t cols_base(const char *tile, int row0, int lane) {
+        const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        return lds_address(tile) + row0 * kRowBytes + row * kRowBytes + ((piece ^ fold(row)) << 4) + 8 * (lane & 1);
+    }
+    template <typename P>
+    static __device__ __forceinline__ typename P::vec8 cols_at(uint32_t base, int row0, int block, int further) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)((base ^ (block << 6)) + row0 * kRowBytes + further));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)((base ^ (block << 6) ^ 32) + (row0 + 8) * kRowBytes + further));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(typename P::vec8, both);
+    }
 };
 // The compiler waits for loaded registers where they are first used, and inside a loop for everything under way.  Done with them here.
 template <typename V, int N>

@@ -237,9 +237,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     typedef Tile<DP> T;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32, kThreads = 64 * kWaves;
     constexpr bool kValuesInLds = kWaves == 8 && DP == 128;
-    __shared__ __align__(16) char q_tile[2][T::kBytes];
-    __shared__ __align__(16) char g_tile[2][T::kBytes];
-    __shared__ __align__(16) char v_block[kValuesInLds ? 2 * T::kBytes : 16];
+    __shared__ __align__(256) char tiles[2][2][T::kBytes];   // of queries and of output gradients, two of each in turn
+    __shared__ __align__(256) char v_block[kValuesInLds ? 2 * T::kBytes : 16];
     __shared__ __align__(16) float row_less[2][64], row_minus[2][64];
     __shared__ DistanceRing<256> ring;
     __shared__ float sums[kWaves][kAttnBuckets];   // the head's bias gradient of this workgroup's keys, by wave
@@ -298,8 +297,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         for (int i = threadIdx.x; i < 128 * T::kPlaces; i += kThreads)
             if ((i % T::kPlaces ^ T::fold(i / T::kPlaces)) >= a.dim / 8) *(i32x4 *)(v_block + 16 * i) = i32x4{0, 0, 0, 0};
     }
-    auto values = [&](int i, int lane) {
-        if constexpr (kValuesInLds) return T::template rows<P>(v_block + (key_wave >> 1) * T::kBytes, 32 * (key_wave & 1), i, lane);
+    auto values = [&](uint32_t base, int i) {
+        if constexpr (kValuesInLds) return T::template rows_at<P>(base, i, 0);
         else return vf[i];
     };
     f32x16 dk[kBlocks], dv[kBlocks];
@@ -325,8 +324,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         float run = 0.0f;  // this lane's part of the sum over results of one bucket
         int run_bucket = 0;
         auto fetch = [&](int n, int qb) {
-            if (kWaves == 4 || wave < 4) T::template fetch<DP <= 64>(q_tile[n], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
-            if (kWaves == 4 || wave >= 4) T::template fetch<DP <= 64>(g_tile[n], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
+            if (kWaves == 4 || wave < 4) T::template fetch<DP <= 64>(tiles[n][0], q_base + (int64_t)qb * a.q.row * 2, (uint32_t)a.q.row * 2, rows.nq - qb, a.dim, key_wave);
+            if (kWaves == 4 || wave >= 4) T::template fetch<DP <= 64>(tiles[n][1], g_base + (int64_t)qb * a.dout.row * 2, (uint32_t)a.dout.row * 2, rows.nq - qb, a.dim, key_wave);
             const uint32_t at = min(lane, rows.nq - qb - 1) * 4;
             if (wave == 0) load_word_to_lds(lds_address(row_less[n]), a.row_less + at_row + qb, at);
             if (wave == 1) load_word_to_lds(lds_address(row_minus[n]), a.row_minus + at_row + qb, at);
@@ -343,7 +342,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
         for (int qb = from; qb < to; qb += 64, now ^= 1) {
             tiles_ready();
             if (qb + 64 < to) fetch(1 - now, qb + 64);
-            const char *q_now = q_tile[now], *g_now = g_tile[now];
             const int lowest = first - (qb + 63 + off);
             if (bias && wave == ((qb >> 6) & (kWaves - 1))) ring_put(ring, lowest - 64, wave, lane);
 #pragma unroll 1
@@ -355,6 +353,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 if (qb + 32 * b + 31 < wave_from || qb + 32 * b >= rows.nq) continue;
                 const int at = (lowest & 255) + 32 * key_wave + 32 - 32 * b;   // of this result's lowest distance, of 63
                 const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
+                const uint32_t rows_here = T::rows_base(tiles[now][0], 32 * b, here);
+                const uint32_t values_here = kValuesInLds ? T::rows_base(v_block, 32 * key_wave, here) : 0;
                 f32x16 s, dp;
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
@@ -367,8 +367,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 }
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    s = P::mma(T::template rows<P>(q_now, 32 * b, i, here), kf[i], s);
-                    dp = P::mma(T::template rows<P>(g_now, 32 * b, i, here), values(i, here), dp);
+                    s = P::mma(T::template rows_at<P>(rows_here, i, 0), kf[i], s);
+                    dp = P::mma(T::template rows_at<P>(rows_here, i, T::kBytes), values(values_here, i), dp);
                 }
                 // reads two products ahead, and no further: registers are what there is least of
                 constexpr int kReads = kValuesInLds ? 3 : 2;
@@ -436,13 +436,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                     add_runs(sums[wave], v, ring.bucket[at + min(here, 62)], ring.bucket[at + min(here + 1, 62)], here);
                 }
                 __builtin_amdgcn_sched_barrier(0);
+                const uint32_t cols_here = T::cols_base(tiles[now][0], 32 * b, here);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const V8 p = operand<P>(s, i), ds = operand<P>(dp, i);
 #pragma unroll
                     for (int d = 0; d < kBlocks; ++d) {
-                        dv[d] = P::mma(T::template cols<P>(g_now, 32 * b + 16 * i, d, here), p, dv[d]);
-                        dk[d] = P::mma(T::template cols<P>(q_now, 32 * b + 16 * i, d, here), ds, dk[d]);
+                        dv[d] = P::mma(T::template cols_at<P>(cols_here, 16 * i, d, T::kBytes), p, dv[d]);
+                        dk[d] = P::mma(T::template cols_at<P>(cols_here, 16 * i, d, 0), ds, dk[d]);
                     }
                 }
                 __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     }
     if constexpr (kValuesInLds) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the values, if nobody has read them
     if constexpr (kWaves == 8) {   // the two halves' sums together, through LDS; 0 .. 3 hold them then
-        float *mine = (float *)(key_wave < 2 ? &q_tile[0][0] : &g_tile[0][0]) + (key_wave & 1) * kBlocks * 16 * 64 + lane;
+        float *mine = (float *)&tiles[0][0][0] + key_wave * kBlocks * 16 * 64 + lane;
         auto join = [&](f32x16 (&x)[kBlocks]) {
             __syncthreads();
             if (wave >= 4) {
