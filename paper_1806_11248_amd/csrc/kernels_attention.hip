@@ -85,6 +85,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
         if (bias && turn < kGroups) ring_put(ring, lowest + kQueries - 1 + kStride + 64 * turn, any_wave, lane);
         if (kb >= wave_end) return;
 
+        __builtin_amdgcn_s_setprio(1);   // products before the other waves' arithmetic
         f32x16 s[2];
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.0f;
@@ -100,6 +101,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        __builtin_amdgcn_s_setprio(0);
         // scores in powers of two are s * factor + add
         const int at = (lowest & ring.kMask) + 64 * group + kQueries - 32 - 32 * wave;   // of the wave's lowest distance, of 95
         const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 94]) : 0;

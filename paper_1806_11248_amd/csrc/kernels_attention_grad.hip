@@ -39,6 +39,22 @@ __device__ __forceinline__ void add_runs(float *sums, float v, int bucket, int n
     __builtin_amdgcn_wave_barrier();
 }
 
+// The sums of lo and hi over all lanes, in lanes 31 and 63: halves first, so that each half of the wave has one of the two.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ void sum_step(float &v) {
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROW_MASK, 0xf, false));
+}
+__device__ __forceinline__ float pair_sum(float lo, float hi) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, lo), __builtin_bit_cast(int, hi), false, false);
+    float v = __builtin_bit_cast(float, (int)both[0]) + __builtin_bit_cast(float, (int)both[1]);
+    sum_step<0x111, 0xf>(v);
+    sum_step<0x112, 0xf>(v);
+    sum_step<0x114, 0xf>(v);
+    sum_step<0x118, 0xf>(v);
+    sum_step<0x142, 0xa>(v);
+    return v;
+}
+
 // ---------------------------------------------------------------------------------------------------------- queries --
 // As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS, one group of four waves or two.
 template <typename P, int DP, int kQWaves, int kGroups>
@@ -132,6 +148,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel
         for (int b = 0; b < 2; ++b) {
             const int at = (lowest & ring.kMask) + 64 * group + kQueries - 32 - 32 * wave + 32 * b;   // of this 32 x 32 result's lowest distance, of 63
             const int b0 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at]) : 0, b1 = bias ? __builtin_amdgcn_readfirstlane(ring.bucket[at + 62]) : 0;
+            __builtin_amdgcn_s_setprio(1);   // products before the other waves' arithmetic
             f32x16 s, dp;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -152,6 +169,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel
             }
             __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
             if (b0 == b1) {
                 const float add = (bias ? ring.of_bucket[b0] : 0.0f) + minus;
 #pragma unroll
@@ -228,8 +246,8 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel
 // was twice as far off.)  Where there are few blocks of keys, several workgroups share one, by heads and by
 // queries, and their sums are added up by a kernel of its own.
 //
-// Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane.  Others are laid out by
-// diagonals in LDS, eight rows at a time, and added up along them (63 distances, one a lane), and then over each run of lanes of one bucket.
+// Bias gradient.  A 32 x 32 result all of whose distances are in one bucket adds to one running sum in each lane, one with a single cut among them to
+// two, which are added up over the lanes.  Others are laid out by diagonals in LDS, eight rows at a time, and added up along them (63 distances, one a lane), and then over each run of lanes of one bucket.
 template <typename P, int DP, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
@@ -413,14 +431,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
                 }
                 if (bias && b0 == b1) {
                     if (b0 != run_bucket) {
-                        const float v = wave_sum(run);
-                        if (lane == 0) sums[wave][run_bucket] += v;
+                        const float v = pair_sum(run, 0.0f);
+                        if (lane == 31) sums[wave][run_bucket] += v;
                         __builtin_amdgcn_wave_barrier();
                         run = 0.0f;
                         run_bucket = b0;
                     }
 #pragma unroll
                     for (int r = 0; r < 16; ++r) run += dp[r];
+                } else if (bias && b1 == b0 + 1) {
+                    // one cut among the result's 63 distances, of which a row's in this lane's column is the (31 + column - row)-th
+                    const int distance = first + 32 * key_wave - (qb + 32 * b + 31 + off);   // the lowest
+                    const int rows_above = 31 + (here & 31) - (ring.cut[b0] - distance) - 4 * half;
+                    float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool above = result_row(r, 0) <= rows_above;
+                        hi += above ? dp[r] : 0.0f;
+                        lo += above ? 0.0f : dp[r];
+                    }
+                    const float v = pair_sum(lo, hi);
+                    if ((here & 31) == 31) sums[wave][b0 + half] += v;
+                    __builtin_amdgcn_wave_barrier();
                 } else if (bias) {
                     float *sk = skew[wave], v = 0.0f;
 #pragma unroll
@@ -457,8 +489,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
             }
         }
         if (bias) {
-            const float v = wave_sum(run);
-            if (lane == 0) sums[wave][run_bucket] += v;
+            const float v = pair_sum(run, 0.0f);
+            if (lane == 31) sums[wave][run_bucket] += v;
             __syncthreads();
             for (int i = threadIdx.x; i < a.n_buckets; i += kThreads) {
                 float v = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
