@@ -2,7 +2,10 @@
 //
 // Two launches over the same pieces: one adds up squares, the other scales (every workgroup adds up the few partial sums for itself,
 // so no third launch stands between).  Squares are summed in 64 bits: a square of any float is representable there, so neither large
-// nor tiny gradients leave the range, and the order of the partial sums is fixed.  Bound: memory.
+// nor tiny gradients leave the range, and the order of the partial sums is fixed.  Bound: memory,
+// of which the gradients are read twice, since the factor needs all of them.  220 tensors of 1000 to 5,000,000 elements, 310 MB: 79 us and 102, together
+// 5.1 TB/s, the rate of a large copy (some of the second reading is met in the cache behind L2, and its dirty lines are written while the next norm is
+// taken); 14 of 30 to 9000: 3.2 and 3.6 us.
 #include "gbt_internal.h"
 
 namespace {
