@@ -526,7 +526,7 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
  *
  * Rows of q, k and v may be any distance apart (parts of one fused projection, slots of a store): strides are in
  * elements, multiples of 8, as head_dim, rows less than 2^24 apart; data is 16-byte aligned; a head's elements
- * lie side by side.
+ * lie side by side.  Rows and heads of inputs may be the same memory (strides of 0), those of outputs may not.
  */
 #define GBT_F32 0
 #define GBT_BF16 1

@@ -65,11 +65,24 @@ bool view_ok(const gbt_heads *h) {
     return h && ((uintptr_t)h->data & 15u) == 0 && h->row_stride >= 0 && h->head_stride >= 0 && h->row_stride % 8 == 0 && h->head_stride % 8 == 0 &&
            h->row_stride < ((int64_t)1 << 24) && h->head_stride < ((int64_t)1 << 40);
 }
+// No two of its heads' rows share elements: what is written to.
+bool apart(const gbt_heads &h, int64_t rows, int64_t heads, int64_t dim) {
+    int64_t near = h.row_stride, n_near = rows, far = h.head_stride, n_far = heads;
+    if (n_far <= 1 || (n_near > 1 && near > far)) {
+        std::swap(near, far);
+        std::swap(n_near, n_far);
+    }
+    if (n_near <= 1) return n_far <= 1 || far >= dim;
+    return near >= dim && (n_far <= 1 || (far - dim) / near >= n_near - 1);
+}
 AttnView view(const gbt_heads *h) { return AttnView{(char *)h->data, h->row_stride, h->head_stride}; }
 
 #define GBT_VIEW(ctx, h, rows)                                                                                                        \
     GBT_REQUIRE(ctx, view_ok(h), GBT_EINVAL, #h ": NULL, not 16-byte aligned, or strides that are negative, no multiples of 8 or (rows) 2^24 and more");    \
     GBT_REQUIRE(ctx, (h)->data || (rows) == 0, GBT_EINVAL, #h ": data is NULL")
+#define GBT_VIEW_OUT(ctx, h, rows, heads)                                                                                             \
+    GBT_VIEW(ctx, h, rows);                                                                                                           \
+    GBT_REQUIRE(ctx, apart(*(h), rows, heads, p.head_dim), GBT_EINVAL, #h ": rows or heads overlap")
 
 void fill(AttnArgs &a, AttnCuts &c, const gbt_attention_params &p) {
     memset(&a, 0, sizeof a);
@@ -115,7 +128,7 @@ extern "C" int32_t gbt_attention(gbt_ctx *ctx, const gbt_attention_params *param
     GBT_VIEW(ctx, q, p.q_rows);
     GBT_VIEW(ctx, k, p.k_rows);
     GBT_VIEW(ctx, v, p.k_rows);
-    GBT_VIEW(ctx, out, p.q_rows);
+    GBT_VIEW_OUT(ctx, out, p.q_rows, p.heads);
     GBT_REQUIRE(ctx, ((uintptr_t)rest_out & 15u) == 0 && ((uintptr_t)lse_out & 3u) == 0, GBT_EINVAL, "rest_out or lse_out is not aligned");
     const size_t need = gbt_attention_workspace_bytes(params);
     GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
@@ -197,9 +210,9 @@ extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_para
     GBT_VIEW(ctx, k, p.k_rows);
     GBT_VIEW(ctx, v, p.k_rows);
     GBT_VIEW(ctx, out, p.q_rows);
-    GBT_VIEW(ctx, dq, p.q_rows);
-    GBT_VIEW(ctx, dk, p.k_rows);
-    GBT_VIEW(ctx, dv, p.k_rows);
+    GBT_VIEW_OUT(ctx, dq, p.q_rows, p.heads);
+    GBT_VIEW_OUT(ctx, dk, p.k_rows, p.kv_heads);
+    GBT_VIEW_OUT(ctx, dv, p.k_rows, p.kv_heads);
     GBT_REQUIRE(ctx, lse || p.q_rows == 0, GBT_EINVAL, "lse is NULL");
     GBT_REQUIRE(ctx, dbias_out || p.n_buckets == 0, GBT_EINVAL, "dbias_out is NULL");
     GBT_REQUIRE(ctx, ((uintptr_t)rest & 15u) == 0 && (((uintptr_t)lse | (uintptr_t)dbias_out) & 3u) == 0, GBT_EINVAL,

@@ -323,6 +323,12 @@ def test_refusals(ctx):
     refused(b.EINVAL, lambda: ctx.attention(q, three, three))
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, cuts=[1, 1, 2])))
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, scale=math.inf)))
+    for wrong in (torch.empty_like(q[:1]).expand(20, 4, 64), torch.empty_like(q[:, :1]).expand(20, 4, 64),
+                  torch.empty(64 * 30, dtype=BF, device="cuda").as_strided((20, 4, 64), (64, 64, 1)),
+                  torch.empty(64 * 90, dtype=BF, device="cuda").as_strided((20, 4, 64), (256, 56, 1))):
+        refused(b.EINVAL, lambda: ctx.attention(q, k, v, out=wrong, **args))
+    by_head = torch.empty(4, 20, 64, dtype=BF, device="cuda").transpose(0, 1)
+    assert torch.equal(ctx.attention(q, k, v, out=by_head, **args), out)
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, max_q=1 << 29)))          # more workgroups than a launch can have
     refused(b.EINVAL, lambda: ctx.attention(q, k, v, **dict(args, max_k=(1 << 29) + 1)))
     shifted = torch.zeros(20 * 4 * 64 + 8, dtype=BF, device="cuda")[4:20 * 4 * 64 + 4].view(20, 4, 64)
@@ -522,3 +528,23 @@ def test_a_graph_keeps_its_workspace(ctx):
                 assert all(torch.equal(a, b) for x, y in zip(recorded, eager) for a, b in zip(x, y))
     finally:
         own.close()
+
+
+@pytest.mark.parametrize("nq", [1, 90])
+def test_broadcast_inputs(ctx, nq):
+    """Heads and rows that are the same memory; gradients are those of each element, for the caller to add up."""
+    rng = torch.Generator().manual_seed(50)
+    q = torch.randn(nq, 1, 64, generator=rng).to(BF).expand(nq, 4, 64)
+    k = torch.randn(200, 1, 64, generator=rng).to(BF).expand(200, 2, 64)
+    v = torch.randn(1, 2, 64, generator=rng).to(BF).expand(200, 2, 64)
+    dout = torch.randn(1, 4, 64, generator=rng).to(BF).expand(nq, 4, 64)
+    ref = Reference(q, k, v, [(0, nq, 0, 200)], True, 64 ** -0.5, None, None, dout)
+    base = [torch.randn(0)] * 4
+    for i, x in enumerate((q, k, v, dout)):
+        base[i] = x[:x.stride(0) and x.shape[0] or 1, :x.stride(1) and x.shape[1] or 1].cuda().expand(x.shape)
+    q, k, v, dout = base
+    assert 0 in q.stride() + k.stride() and v.stride(0) == 0 and (nq == 1 or dout.stride(0) == 0)
+    out, saved = ctx.attention(q, k, v, causal=True, save=True)
+    close(out, ref.out, ref.out_tol, "out")
+    for name, x in zip(("dq", "dk", "dv"), ctx.attention_backward(dout, q, k, v, out, saved, causal=True)):
+        close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
