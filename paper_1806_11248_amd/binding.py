@@ -678,17 +678,16 @@ class Context:
         k_rows, kv_heads, _ = k.shape
         if not (q.is_cuda and k.is_cuda):
             raise TypeError("q, k: expected CUDA tensors")
-        n_seq = None
+        n_q = n_k = n_len = at_q = at_k = at_len = None
         if q_ptr is not None:
-            n_seq = _need(q_ptr, torch.int64, "q_ptr").numel() - 1
-        for t, dtype, extra, name in ((k_ptr, torch.int64, 1, "k_ptr"), (k_len, torch.int32, 0, "k_len")):
-            if t is not None:
-                n = _need(t, dtype, name).numel() - extra
-                if n_seq is not None and n != n_seq:
-                    raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
-                n_seq = n
-        if n_seq is None:
-            n_seq = 1
+            n_q, at_q = _need(q_ptr, torch.int64, "q_ptr").numel() - 1, q_ptr.data_ptr()
+        if k_ptr is not None:
+            n_k, at_k = (n_q, at_q) if k_ptr is q_ptr else (_need(k_ptr, torch.int64, "k_ptr").numel() - 1, k_ptr.data_ptr())
+        if k_len is not None:
+            n_len, at_len = _need(k_len, torch.int32, "k_len").numel(), k_len.data_ptr()
+        n_seq = n_q if n_q is not None else n_k if n_k is not None else 1 if n_len is None else n_len
+        if (n_k is not None and n_k != n_seq) or (n_len is not None and n_len != n_seq):
+            raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
         if q_ptr is None:
             each = rows // max(1, n_seq)
             if each * n_seq != rows or max_q not in (None, each):
@@ -702,15 +701,15 @@ class Context:
         n_buckets, table, edges = 0, None, None
         if bias is not None:
             _need(bias, torch.float32, "bias")
-            if bias.dim() != 2 or bias.shape[1] != heads or bias.shape[0] < 1:
-                raise TypeError(f"bias: expected [n_buckets][{heads}], not {tuple(bias.shape)}")
-            n_buckets, table = bias.shape[0], bias.data_ptr()
+            shape = bias.shape
+            if len(shape) != 2 or shape[1] != heads or shape[0] < 1:
+                raise TypeError(f"bias: expected [n_buckets][{heads}], not {tuple(shape)}")
+            n_buckets, table = shape[0], bias.data_ptr()
             if cuts is None or len(cuts) != n_buckets - 1:
                 raise TypeError(f"cuts: expected {n_buckets - 1} of them")
-            edges = array.array("i", cuts.tolist() if hasattr(cuts, "tolist") else cuts)
+            edges = array.array("i", cuts if type(cuts) is list else cuts.tolist() if hasattr(cuts, "tolist") else cuts)
         p = AttentionParams(DTYPES.get(q.dtype, -1), heads, kv_heads, dim, n_seq, rows if max_q is None else max_q, k_rows if max_k is None else max_k,
-                            causal, n_buckets, dim ** -0.5 if scale is None else scale, rows, k_rows, None if q_ptr is None else q_ptr.data_ptr(),
-                            None if k_ptr is None else k_ptr.data_ptr(), None if k_len is None else k_len.data_ptr(), table,
+                            causal, n_buckets, dim ** -0.5 if scale is None else scale, rows, k_rows, at_q, at_k, at_len, table,
                             None if edges is None else edges.buffer_info()[0])
         return p, edges
 
@@ -802,7 +801,7 @@ class Context:
         """Scales every tensor of the list by min(1, max_norm / (norm + 1e-6)) into its out; returns the global norm, a float32 scalar
         on the device.  A norm that is not finite leaves the values as they are."""
         with self._on_stream(gradients.both) or _NO_STREAM:
-            norm = self.empty((), torch.float32)
+            norm = gradients.table.new_empty((), dtype=torch.float32)
             ws = self._scratch("clip", 16384)
         st = self.lib.gbt_clip_gradients(self.h, gradients.table.data_ptr(), gradients.pieces, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel())
         if st:

@@ -59,6 +59,17 @@ def test_norm_and_values(ctx, sizes, ratio):
     _check(ctx, ts, ratio * _norm(ts), [torch.full_like(t, 9.0) for t in ts])     # into other tensors
 
 
+@pytest.mark.parametrize("count", [1, 15, 16, 17, 24, 25, 33])
+def test_few_pieces(ctx, count):
+    """One workgroup, a wave to a piece, up to the number of pieces from which there are more; whole pieces, short and unaligned ones."""
+    for size in (2048, 2047, 3):
+        ts = _tensors([size] * count, seed=count)
+        _check(ctx, [t.clone() for t in ts], 0.4 * _norm(ts))
+        _check(ctx, ts, 0.4 * _norm(ts), [torch.full_like(t, 9.0) for t in ts])
+        shifted = [torch.cat([t[:1], t])[1:] for t in ts]
+        _check(ctx, shifted, 0.4 * _norm(ts))
+
+
 def test_the_smaller_side_of_the_limit_changes_nothing(ctx):
     ts = _tensors([1000, 77])
     keep = [t.clone() for t in ts]
