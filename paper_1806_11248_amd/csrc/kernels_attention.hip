@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
     __shared__ DistanceRing<256 * kGroups> ring;
 
     if (blockIdx.x >= a.work) return zero_gaps(a, a.out, false);
-    const AttnItem item = attn_item(a.order, a.n_seq);
+    const AttnItem item = attn_item(a);
     if (item.seq < 0) return;
     // the blocks that see the most keys first
     const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
@@ -445,7 +445,7 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const AttnForm form = attn_form(a, DP, false);
     const int64_t blocks = (a.max_q + form.queries - 1) / form.queries;
     AttnArgs b = a;
-    b.order = attn_order(a.heads, blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
+    b.order = attn_order(a, a.heads, blocks, true);
     b.work = attn_grid(b.order);
     const unsigned grid = b.work + attn_gap_workgroups(a, true, false);
     if (grid == 0) return hipSuccess;

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel
         zero_gaps(a, a.dk, true);
         return zero_gaps(a, a.dv, true);
     }
-    const AttnItem item = attn_item(a.order, a.n_seq);
+    const AttnItem item = attn_item(a);
     if (item.seq < 0) return;
     const int block = a.order.blocks - 1 - item.block, head = item.unit, seq = item.seq;
     const AttnSeq rows = attn_seq(a, seq);
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     __shared__ float skew[kWaves][8 * 64];         // [query][key - query + 31]: eight rows of a result by its diagonals
 
     const int k_blocks = a.order.blocks, parts = a.head_parts * a.q_parts;
-    const AttnItem item = attn_item(a.order, a.n_seq);
+    const AttnItem item = attn_item(a);
     if (item.seq < 0) return;
     const int part = item.unit % parts, kv_head = item.unit / parts, seq = item.seq;
     const int q_part = part % a.q_parts, head_part = part / a.q_parts;
@@ -620,7 +620,7 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     hipError_t e = hipSuccess;
     {
         AttnArgs b = a;
-        b.order = attn_order(a.heads, q_blocks, a.n_seq, a.causal, 4 * a.k_rows * a.kv_heads * a.dim);
+        b.order = attn_order(a, a.heads, q_blocks, true);
         b.work = attn_grid(b.order);
         const unsigned grid = b.work + attn_gap_workgroups(a, true, true);
         if (grid == 0) {
@@ -633,7 +633,7 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
         constexpr int kWaves = DP == 128 ? 8 : 4;
         const int64_t units = (int64_t)a.kv_heads * a.head_parts * a.q_parts;
         AttnArgs b = a;
-        b.order = attn_order(units, k_blocks, a.n_seq, a.causal, 4 * a.q_rows * a.heads * a.dim);
+        b.order = attn_order(a, units, k_blocks, false);
         grad_keys_kernel<P, DP, kWaves><<<attn_grid(b.order), 64 * kWaves, 0, stream>>>(b, c);
         e = hipGetLastError();
     }

@@ -548,3 +548,33 @@ def test_broadcast_inputs(ctx, nq):
     close(out, ref.out, ref.out_tol, "out")
     for name, x in zip(("dq", "dk", "dv"), ctx.attention_backward(dout, q, k, v, out, saved, causal=True)):
         close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
+
+
+@pytest.mark.parametrize("seqs", [2, 31, 33, 64, 65])
+@pytest.mark.parametrize("causal", [False, True])
+def test_sequences_by_length(ctx, seqs, causal):
+    """Lengths alike, apart, none; queries and keys of different lengths: whichever is taken first, each is taken once."""
+    rng = np.random.default_rng(seqs)
+    nq = [int(x) for x in rng.choice([0, 1, 127, 128, 129, 200, 300, 512], seqs)]
+    nk = [int(x) for x in rng.choice([0, 1, 128, 140, 260, 512], seqs)]
+    nq[0], nk[-1] = 520, 513
+    _check(ctx, _make(nq, nk, 1, 1, 8, BF, causal=causal, buckets=5, seed=seqs))
+    _check(ctx, _make(nq[:5], nk[-5:], 2, 1, 128, HF, causal=causal, buckets=5, seed=seqs, room=9))
+
+
+def test_causal_sequences_by_length(ctx):
+    """Causal histories beyond what the L2 holds are taken by length too; most of the rows belong to one that is not looked at."""
+    rows, H, D = 140_000, 1, 128                       # 4 * 140,000 * 128 bytes of keys and values
+    nq, nk = [300, 10, 0, 420, 257], [300, 200, 40, 500, 257]
+    q, k, v, dout, args, spans = _make(nq, nk, H, H, D, BF, causal=True, buckets=6, seed=60)
+    big = {}
+    for name, x in (("q", q), ("k", k), ("v", v), ("dout", dout)):
+        big[name] = torch.zeros(rows, H, D, dtype=BF, device="cuda")
+        big[name][:len(x)] = x
+    out, saved = ctx.attention(big["q"], big["k"], big["v"], save=True, **args)
+    got = ctx.attention_backward(big["dout"], big["q"], big["k"], big["v"], out, saved, **args)
+    ref = _reference(q, k, v, args, spans, dout)
+    for name, x, n in zip(("out", "dq", "dk", "dv"), (out, *got), (len(q), len(q), len(k), len(k))):
+        close(x[:n], getattr(ref, name), getattr(ref, name + "_tol"), name)
+        assert not x[n:].any()
+    close(got[3], ref.dbias, ref.dbias_tol, "dbias")
