@@ -23,9 +23,9 @@ constexpr float kSlack = 8.0f;
 // Bound: the matrix units together with the exponentials and the arithmetic around them, which take turns more than they overlap: 64 keys against 32
 // queries are 32 matrix instructions at 128 elements a head, 16 at 64, and either way some 130 others, 32 of them exponentials of four times an
 // addition's time.  So large heads come nearer the rate of a large library product (1198 TFLOP/s in bfloat16 here): 8192 causal rows, 16 heads of 128
-// elements 297 us, 927 TFLOP/s of the pairs that count; not causal 128 queries a head against 16384 keys 1024 without a bias, 946 with one; heads of 64
+// elements 304 us, 904 TFLOP/s of the pairs that count; not causal 128 queries a head against 16384 keys 1024 without a bias, 946 with one; heads of 64
 // 676 and 621; the matrix units are busy 39% of the time, LDS 24%, without bank conflicts (two causal histories of 4096).  Ragged short histories are
-// bound by how their blocks fall on the compute units: 24 of 100 to 1000 rows, 8 heads of 64 44 us, where blocks enough would take 27.
+// bound by how their blocks fall on the compute units: 24 of 100 to 1000 rows, 8 heads of 64 40 us, where blocks enough would take 27.
 template <typename P, int DP, int kQWaves, int kGroups>
 __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
