@@ -736,7 +736,7 @@ class Context:
             if out is None:
                 out = q.new_empty(rows, heads, dim)
             if save:
-                lse, rest = self.empty((heads, rows), torch.float32), q.new_empty(rows, heads, dim)
+                lse, rest = q.new_empty((heads, rows), dtype=torch.float32), q.new_empty(rows, heads, dim)
             ws = self._scratch("attention", ws_bytes) if ws_bytes else None
         ho = _heads(out, "out", dtype, of_q)
         st = lib.gbt_attention(self.h, at, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), lse.data_ptr() if save else None,

@@ -17,8 +17,8 @@ namespace {
 constexpr float kSlack = 8.0f;
 
 // ------------------------------------------------------------------------------------------------ blocks of queries --
-// A workgroup takes 128 queries of one head, a wave 32 of them (its columns); keys and values pass through LDS, 64 at a time.  Of two groups of four
-// waves each takes every other tile for the same queries, and they are joined at the end: half the steps one after the other.
+// A wave takes 32 queries of one head (its columns), a workgroup 128 or 64 (attn_form); keys and values pass through LDS, 64 at a time.  Of two groups
+// of waves each takes every other tile for the same queries, and they are joined at the end: half the steps one after the other.
 //
 // Bound: the matrix units together with the exponentials and the arithmetic around them, which take turns more than they overlap: 64 keys against 32
 // queries are 32 matrix instructions at 128 elements a head, 16 at 64, and either way some 130 others, 32 of them exponentials of four times an

@@ -61,7 +61,7 @@ __device__ __forceinline__ float pair_sum(float lo, float hi) {
 }
 
 // ---------------------------------------------------------------------------------------------------------- queries --
-// As the forward kernel: 128 queries of one head, 32 a wave, keys and values through LDS, one group of four waves or two.
+// As the forward kernel: 128 or 64 queries of one head, 32 a wave, keys and values through LDS, one group of waves or two.
 template <typename P, int DP, int kQWaves, int kGroups>
 __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void grad_queries_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
