@@ -8,9 +8,10 @@
 namespace {
 
 // Workgroups that a call with few query rows is cut into where its keys allow, were all sequences the longest: two are on a compute unit at a time, and
-// with four turns of them the last, partly empty one costs little.  A row's pieces are joined by 256 lanes.  (Stores of 2000 to 30000 rows, kernel and
-// join, for 1024, 2048, 4096, 8192: 124, 126, 132, 157 us; few events for 64 rows 54, 53, 57, 67.)
-constexpr int64_t kFewWorkgroups = 2048, kFewPieces = 256;
+// most sequences are shorter.  A row's pieces are joined by 256 lanes at most.  (us for 512, 2048, 4096: 64 stores of 30 to 3000 rows, 8 key heads of 64
+// elements, 58, 51, 51; 128 102, 93, 89; 128 of 30 to 10000 320, 284, 253; 200 of 3000 246, 246, 223; 16 of 2000 to 30000, 4 of 128, 134, 115, 116; but 1000
+// of 30 to 1500, 1 of 64 for 8 heads 49, 55, 55.)
+constexpr int64_t kFewWorkgroups = 4096, kFewPieces = 256;
 // Shorter pieces cost more by their beginnings and ends than they gain by being many: 32 stores of 1000 rows, 8 heads of 128 elements, at least 256, 512,
 // 1024 rows a piece: 32, 29, 25 us; 4 of 2000, 2 heads of 64: 9.3, 10.3, 12.3; 4 of 500: 9.2, 7.0, 7.0.
 constexpr int64_t kFewLeast = 1024;

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
 // keys are under way as soon as the products with the last have been made, the next values likewise.  The waves are joined at the
 // end, the pieces by a second launch.
 // Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 112 us (5.0 TB/s, where a large copy moves 5.1) and
-// 7 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 7.  Four short ones: 9.7 us, the time of one step after
+// 7 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 5.  Four short ones: 9.7 us, the time of one step after
 // the other.
 template <typename P, int DP>
 __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnCuts c) {
@@ -234,9 +234,11 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
 
     if (blockIdx.x >= a.work) return zero_gaps(a, a.out, false);
     const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
-    const int64_t item = blockIdx.x;
-    const int piece = (int)(item % a.pieces), block = (int)(item / a.pieces % blocks);
-    const int kv_head = (int)(item / a.pieces / blocks % a.kv_heads), seq = (int)(item / a.pieces / blocks / a.kv_heads);
+    // the first pieces of all sequences before the second ones, and each time one further: side by side the later pieces, of which there are fewer, would
+    // all go to some of the XCDs, and without the shift all of a long sequence's to one (128 stores of 30 to 3000 rows, 8 key heads of 64, 115 and 98 us, so 94; 16
+    // of 2000 to 30000, 4 of 128, 113 and 128, so 114)
+    const unsigned units = a.work / a.pieces, turn = blockIdx.x / units, unit = (blockIdx.x + turn) % units;
+    const int piece = (int)turn, block = (int)(unit % blocks), kv_head = (int)(unit / blocks % a.kv_heads), seq = (int)(unit / blocks / a.kv_heads);
     const AttnSeq rows = attn_seq(a, seq);
     const int begin = piece * a.piece_len;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
@@ -440,6 +442,46 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
     }
 }
 
+// The same for up to 16 pieces, a wave a column.  (500 stores of 30 to 1500 rows in two pieces, 8 columns each: kernel and joining 60 -> 54 us.)
+constexpr int kFewJoined = 16;
+template <typename P>
+__global__ __launch_bounds__(256) void attention_join_few_kernel(AttnArgs a) {
+    typedef typename P::elem E;
+    const int columns = a.group * a.max_q, lane = threadIdx.x & 63, at = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int column = at % columns, kv_head = at / columns % a.kv_heads, seq = at / columns / a.kv_heads;
+    if (seq >= a.n_seq) return;
+    const int query = column / a.group, head = kv_head * a.group + column % a.group;
+    const AttnSeq rows = attn_seq(a, seq);
+    if (query >= rows.nq) return;
+    const int n = (rows.nk + a.piece_len - 1) / a.piece_len, wide = a.dim + 2;
+    if (n < 2) return;
+    const float *part = a.part + (int64_t)at * a.pieces * wide;
+    const float top = lane < n ? part[(int64_t)lane * wide + a.dim] : -INFINITY, sum = lane < n ? part[(int64_t)lane * wide + a.dim + 1] : 0.0f;
+    float most = top;
+#pragma unroll
+    for (int s = 8; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    most = __shfl(most, 0);
+    const float factor = __builtin_amdgcn_exp2f(top - (most == -INFINITY ? 0.0f : most)), l = wave_sum(sum * factor);
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    const int d0 = min(lane, a.dim - 1), d1 = min(lane + 64, a.dim - 1);
+    float o0 = 0.0f, o1 = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+        const float f = __shfl(factor, p);
+        o0 = fmaf(part[(int64_t)p * wide + d0], f, o0);
+        o1 = fmaf(part[(int64_t)p * wide + d1], f, o1);
+    }
+    if (a.lse && lane == 0) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = l == 0.0f ? -INFINITY : (most + __builtin_amdgcn_logf(l)) * GBT_LN2;
+    auto put = [&](int d, float x) {
+        if (d >= a.dim) return;
+        const E y = (E)x;
+        ((E *)a.out.data)[(rows.q0 + query) * a.out.row + (int64_t)head * a.out.head + d] = y;
+        if (a.rest) ((E *)a.rest)[((rows.q0 + query) * a.heads + head) * a.dim + d] = (E)(x - (float)y);
+    };
+    put(lane, o0 * inv);
+    put(lane + 64, o1 * inv);
+}
+
 template <typename P, int DP>
 hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     const AttnForm form = attn_form(a, DP, false);
@@ -464,7 +506,9 @@ hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) 
     if (a.pieces > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        attention_join_kernel<P><<<(unsigned)(columns * a.kv_heads * a.n_seq), 256, 0, stream>>>(a);
+        const unsigned all = (unsigned)(columns * a.kv_heads * a.n_seq);
+        if (a.pieces <= kFewJoined) attention_join_few_kernel<P><<<(all + 3) / 4, 256, 0, stream>>>(a);
+        else attention_join_kernel<P><<<all, 256, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
