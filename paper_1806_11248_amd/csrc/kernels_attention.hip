@@ -217,8 +217,8 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
 // workgroup take every fourth 32 keys of its piece of the key axis, each through its own part of LDS, so no wave waits for another.  The next
 // keys are under way as soon as the products with the last have been made, the next values likewise.  The waves are joined at the
 // end, the pieces by a second launch.
-// Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 112 us (5.0 TB/s, where a large copy moves 5.1) and
-// 7 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 5.  Four short ones: 9.7 us, the time of one step after
+// Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 113 us (4.9 TB/s, where a large copy moves 5.1) and
+// 6 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 5.  Four short ones: 9.7 us, the time of one step after
 // the other.
 template <typename P, int DP>
 __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnCuts c) {
