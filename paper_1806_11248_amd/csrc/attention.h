@@ -133,11 +133,6 @@ struct F16 {
     }
 };
 
-template <typename V>
-__device__ __forceinline__ V as_vec(i32x4 x) {
-    return __builtin_bit_cast(V, x);
-}
-
 struct AttnSeq {
     int64_t q0, k0;
     int nq, nk;

@@ -114,7 +114,6 @@ struct ClipPiece {
     void *dst;
     int32_t n, dtype;
 };
-int gbt_clip_blocks(int64_t n_pieces);   // workgroups, and doubles of workspace
 hipError_t gbt_launch_clip(hipStream_t stream, const ClipPiece *pieces, int n_pieces, double max_norm, float *norm_out, double *sums);
 
 // One node for the split kernel.

@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int kClipBlocks = 2048;   // workgroups of 256 threads: what the compute units hold at once
+constexpr int kClipBlocks = 2048;   // workgroups of 256 threads, and doubles of workspace: what the compute units hold at once
 
 template <typename E>
 struct alignas(16) Vec {
@@ -143,14 +143,12 @@ __global__ __launch_bounds__(1024) void clip_few_kernel(const ClipPiece *pieces,
 
 }  // namespace
 
-int gbt_clip_blocks(int64_t n_pieces) { return (int)std::max<int64_t>(1, std::min<int64_t>(n_pieces, kClipBlocks)); }
-
 hipError_t gbt_launch_clip(hipStream_t stream, const ClipPiece *pieces, int n_pieces, double max_norm, float *norm_out, double *sums) {
     if (n_pieces <= kClipFew) {
         clip_few_kernel<<<1, 1024, 0, stream>>>(pieces, n_pieces, max_norm, norm_out);
         return hipGetLastError();
     }
-    const int blocks = gbt_clip_blocks(n_pieces);
+    const int blocks = std::min(n_pieces, kClipBlocks);
     clip_norm_kernel<<<blocks, 256, 0, stream>>>(pieces, n_pieces, sums);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
