@@ -268,14 +268,15 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
 }
 // Sixteen bytes for each lane from base + offset (base and `to` the same in all lanes) to LDS, the lanes' side by side from `to` on.  It has no
 // result in registers; tiles_ready() waits for it.  Not the builtin: with that one the compiler waits for every load under way before LDS reads
-// that it cannot tell apart from the loads' targets, and so for the next tile before it reads this one.
+// that it cannot tell apart from the loads' targets, and so for the next tile before it reads this one.  Into the text it does not see: the wait state
+// between the write of M0 and the load that reads it is kept here.
 __device__ __forceinline__ void load_to_lds(uint32_t to, const char *base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // Four bytes for each lane likewise.
 __device__ __forceinline__ void load_word_to_lds(uint32_t to, const float *base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
 
 // A tile of 64 rows in LDS.  A row's sixteen-byte pieces are stored in an order of its own, piece c at place c ^ fold(row), with which both
