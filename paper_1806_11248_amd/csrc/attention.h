@@ -58,8 +58,9 @@ struct AttnArgs {
     float *strips;                  // [heads][n_seq * k_blocks * q_parts][n_buckets]: the bias gradient of each block of keys
     float *dbias;                   // [n_buckets][heads]
     int head_parts, q_parts;        // a block of keys is shared by so many workgroups: by heads of the group, by queries
-    // partial results: few rows' of the pieces of the key axis; keys' gradients [head_parts * q_parts][2][k_rows][kv_heads][dim]
+    // partial results: few rows' of the pieces of the key axis; keys' gradients [head_parts * q_parts][2][part_rows][kv_heads][dim]
     float *part;
+    int64_t part_rows;              // of the k tensor, or max_k for each sequence where those are fewer: a store may be far larger than what is in use
     int pieces, piece_len;
 };
 
@@ -162,6 +163,11 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s) {
     r.nq = r.q0 >= 0 && q1 <= a.q_rows && q1 > r.q0 ? (int)min(q1 - r.q0, (int64_t)a.max_q) : 0;
     r.nk = r.k0 >= 0 && k1 <= a.k_rows && k1 > r.k0 ? (int)min(k1 - r.k0, (int64_t)a.max_k) : 0;
     return r;
+}
+
+// The row of the partial results that sequence s begins at.
+__device__ __forceinline__ int64_t attn_part_row(const AttnArgs &a, int s, const AttnSeq &rows) {
+    return a.part_rows < a.k_rows ? (int64_t)s * a.max_k : rows.k0;
 }
 
 struct AttnItem {

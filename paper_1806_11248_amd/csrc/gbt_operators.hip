@@ -175,6 +175,7 @@ KeyParts key_parts(const gbt_attention_params &p) {
     k.queries = (int)std::min<int64_t>(std::max<int64_t>(1, want / k.heads), std::max(1, p.max_q / 256));
     return k;
 }
+int64_t part_rows(const gbt_attention_params &p) { return std::min<int64_t>(p.k_rows, (int64_t)p.n_seq * p.max_k); }
 struct BackwardLayout {
     size_t row_minus, strips, part, bytes;
 };
@@ -186,7 +187,7 @@ BackwardLayout backward_layout(const gbt_attention_params &p) {
     l.strips = l.row_minus + row;
     l.part = l.strips + gbt_align((size_t)p.heads * p.n_seq * blocks_of(p.max_k) * k.queries * p.n_buckets * sizeof(float));
     const int parts = k.heads * k.queries;
-    l.bytes = l.part + (parts > 1 ? gbt_align((size_t)parts * 2 * p.k_rows * p.kv_heads * p.head_dim * sizeof(float)) : 0);
+    l.bytes = l.part + (parts > 1 ? gbt_align((size_t)parts * 2 * part_rows(p) * p.kv_heads * p.head_dim * sizeof(float)) : 0);
     return l;
 }
 }  // namespace
@@ -243,6 +244,7 @@ extern "C" int32_t gbt_attention_backward(gbt_ctx *ctx, const gbt_attention_para
     const KeyParts k_parts = key_parts(p);
     a.head_parts = k_parts.heads;
     a.q_parts = k_parts.queries;
+    a.part_rows = part_rows(p);
     a.dbias = dbias_out;
     GBT_HIP(ctx, gbt_launch_attention_grad(ctx->stream, a, c, p.dtype));
     return GBT_OK;

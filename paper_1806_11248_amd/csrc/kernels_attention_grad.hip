@@ -525,8 +525,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void grad_keys_kernel(AttnArgs a, A
     }
     if (!there) return;
     if (parts > 1) {
-        const int64_t tensor = a.k_rows * a.kv_heads * a.dim;
-        float *ko = a.part + 2 * part * tensor + ((rows.k0 + key) * a.kv_heads + kv_head) * a.dim, *vo = ko + tensor;
+        const int64_t tensor = a.part_rows * a.kv_heads * a.dim;
+        float *ko = a.part + 2 * part * tensor + ((attn_part_row(a, seq, rows) + key) * a.kv_heads + kv_head) * a.dim, *vo = ko + tensor;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -591,11 +591,11 @@ __global__ __launch_bounds__(1024) void grad_join_kernel(AttnArgs a) {
     const AttnSeq rows = attn_seq(a, seq);
     if (first >= rows.nk) return;
     const int wide = a.kv_heads * a.dim / 4, parts = a.head_parts * a.q_parts;
-    const int64_t tensor = a.k_rows * a.kv_heads * a.dim;
+    const int64_t tensor = a.part_rows * a.kv_heads * a.dim, part_row = attn_part_row(a, seq, rows) + first;
     for (int i = threadIdx.x; i < min(kJoinRows, rows.nk - first) * wide; i += 1024) {
         const int64_t row = rows.k0 + first + i / wide;
         const int e = i % wide * 4, kv_head = e / a.dim, d = e % a.dim;
-        const float *from = a.part + row * a.kv_heads * a.dim + e;
+        const float *from = a.part + (part_row + i / wide) * a.kv_heads * a.dim + e;
         f32x4 k = {0.0f, 0.0f, 0.0f, 0.0f}, v = k;
 #pragma unroll 4
         for (int p = 0; p < parts; ++p) {

@@ -578,3 +578,21 @@ def test_causal_sequences_by_length(ctx):
         close(x[:n], getattr(ref, name), getattr(ref, name + "_tol"), name)
         assert not x[n:].any()
     close(got[3], ref.dbias, ref.dbias_tol, "dbias")
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_parts_of_a_block_of_keys_in_a_store(ctx, causal):
+    """A block's parts, of sequences whose slots are a small share of a store's rows, and of as many rows as the longest sequences would have or fewer."""
+    for nq, nk, rows, H, K, D in (([1500, 700], [90, 300], 60_000, 6, 1, 64), ([900, 10, 300], [130, 260, 0], 20_000, 4, 2, 128), ([900, 10], [130, 260], 390, 4, 2, 128)):
+        q, k, v, dout, args, spans = _make(nq, nk, H, K, D, BF, causal=causal, buckets=12, seed=70)
+        at = [rows - sum(nk) + x for x in rows_of(nk)]
+        ref = _reference(q, k, v, args, spans, dout)
+        big_k, big_v = (torch.full((rows, K, D), math.nan, dtype=BF, device="cuda") for _ in range(2))
+        big_k[at[0]:], big_v[at[0]:] = k, v
+        args["k_ptr"] = torch.tensor(at).cuda()
+        args["k_len"] = torch.tensor(nk, dtype=torch.int32).cuda()
+        out, saved = ctx.attention(q, big_k, big_v, save=True, **args)
+        dq, dk, dv, dbias = ctx.attention_backward(dout, q, big_k, big_v, out, saved, **args)
+        for name, x in (("dq", dq), ("dk", dk[at[0]:]), ("dv", dv[at[0]:]), ("dbias", dbias)):
+            close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
+        assert not dk[:at[0]].any() and not dv[:at[0]].any()

@@ -53,6 +53,21 @@ def test_workspaces(b):
     assert fwd(None) == 0 and bwd(None) == 0
 
 
+def test_the_backward_workspace_goes_by_the_rows_in_use(b):
+    """Partial sums of the keys' gradients are as many as the sequences can have rows, whatever the size of the store that they lie in."""
+    def need(**kw):
+        return b._lib.gbt_attention_backward_workspace_bytes(C.byref(_params(b, q_ptr=64, k_ptr=64, k_len=64, causal=0, **kw)))
+
+    for kw in (dict(n_seq=3, heads=8, kv_heads=8, head_dim=128, max_q=1500, max_k=700, q_rows=4500), dict(n_seq=2, heads=16, kv_heads=4, head_dim=128, max_q=512,
+               max_k=512, q_rows=1024), dict(n_seq=1, heads=4, kv_heads=1, head_dim=64, max_q=4096, max_k=40, q_rows=4096)):
+        rows = kw["n_seq"] * kw["max_k"]
+        tight = need(k_rows=rows, **kw)
+        two_tensors = 2 * rows * kw["kv_heads"] * kw["head_dim"] * 4
+        assert tight > 2 * two_tensors                                       # several parts
+        assert need(k_rows=rows // 2, **kw) <= tight                         # fewer rows than n_seq * max_k
+        assert need(k_rows=rows + 7, **kw) <= tight + 4096 and need(k_rows=1000 * rows, **kw) <= tight + 4096
+
+
 @pytest.mark.parametrize("wrong", [
     dict(dtype=0), dict(dtype=3), dict(heads=0), dict(kv_heads=3), dict(heads=-8, kv_heads=-2), dict(head_dim=0), dict(head_dim=12), dict(head_dim=136),
     dict(n_seq=-1), dict(max_q=-1), dict(max_k=1 << 30), dict(q_rows=-1), dict(n_buckets=-1), dict(n_buckets=129), dict(scale=0.0), dict(scale=-1.0),
