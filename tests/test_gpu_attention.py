@@ -596,3 +596,29 @@ def test_parts_of_a_block_of_keys_in_a_store(ctx, causal):
         for name, x in (("dq", dq), ("dk", dk[at[0]:]), ("dv", dv[at[0]:]), ("dbias", dbias)):
             close(x, getattr(ref, name), getattr(ref, name + "_tol"), name)
         assert not dk[:at[0]].any() and not dv[:at[0]].any()
+
+
+def test_a_loose_longest_sequence_costs_idle_workgroups_and_no_more(ctx):
+    """Up to 64 sequences are put in order by their lengths, by every workgroup for itself: the same launch but for one more sequence, and so
+    without that order, takes as long, however far the longest sequence lies below the bound that the caller gives."""
+    def call(seqs, bound):
+        nq = [100 + 3 * s for s in range(seqs)]
+        q, k, v, dout, args, spans = _make(nq, nq, 1, 1, 64, BF, causal=False, seed=71)
+        args.update(max_q=bound, max_k=bound)
+        return q, k, v, args, spans
+
+    took = {}
+    for seqs in (64, 65):
+        q, k, v, args, spans = call(seqs, 1 << 20)
+        out = ctx.attention(q, k, v, **args)
+        ref = _reference(q, k, v, args, spans)
+        close(out, ref.out, ref.out_tol, "out")
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(5):
+            ctx.attention(q, k, v, out=out, **args)
+        end.record()
+        end.synchronize()
+        took[seqs] = begin.elapsed_time(end) / 5
+    print(took)
+    assert took[64] < 3 * took[65]
