@@ -670,6 +670,19 @@ class Context:
             return self.empty((max(nbytes, 16),), torch.uint8)
         return self.workspace(key, nbytes)
 
+    def _longest(self, q_ptr, k_ptr, k_len):
+        """The most rows that a sequence has by the pointers given, read from the device; None while a graph is being recorded, when nothing can
+        be read."""
+        if torch.cuda.is_current_stream_capturing():
+            return None
+        with torch.cuda.stream(self.stream):
+            most = {}
+            for ptr, used in ((q_ptr, None), (k_ptr, k_len)):
+                if ptr is not False and (ptr, used) not in most:
+                    lengths = ptr[1:] - ptr[:-1]
+                    most[ptr, used] = max(0, int((lengths if used is None else torch.minimum(lengths, used)).max()))
+            return most.get((q_ptr, None), 0), most.get((k_ptr, k_len), 0)
+
     def _attention_params(self, q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts):
         """(gbt_attention_params, what it points to on the host)."""
         if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3):
@@ -698,6 +711,10 @@ class Context:
             if each * n_seq != k_rows or max_k not in (None, each):
                 raise TypeError(f"k: without k_ptr all of {n_seq} sequences have the same length")
             max_k = each
+        if max_q is None or max_k is None:
+            longest = self._longest(max_q is None and q_ptr, max_k is None and k_ptr, k_len) if n_seq > 1 else None
+            of_q, of_k = longest or (rows, k_rows)
+            max_q, max_k = min(rows, of_q) if max_q is None else max_q, min(k_rows, of_k) if max_k is None else max_k
         n_buckets, table, edges = 0, None, None
         if bias is not None:
             _need(bias, torch.float32, "bias")
@@ -708,8 +725,8 @@ class Context:
             if cuts is None or len(cuts) != n_buckets - 1:
                 raise TypeError(f"cuts: expected {n_buckets - 1} of them")
             edges = array.array("i", cuts if type(cuts) is list else cuts.tolist() if hasattr(cuts, "tolist") else cuts)
-        p = AttentionParams(DTYPES.get(q.dtype, -1), heads, kv_heads, dim, n_seq, rows if max_q is None else max_q, k_rows if max_k is None else max_k,
-                            causal, n_buckets, dim ** -0.5 if scale is None else scale, rows, k_rows, at_q, at_k, at_len, table,
+        p = AttentionParams(DTYPES.get(q.dtype, -1), heads, kv_heads, dim, n_seq, max_q, max_k, causal,
+                            n_buckets, dim ** -0.5 if scale is None else scale, rows, k_rows, at_q, at_k, at_len, table,
                             None if edges is None else edges.buffer_info()[0])
         return p, edges
 
@@ -719,7 +736,8 @@ class Context:
 
         q_ptr, k_ptr  int64[n_seq + 1] on the device: where each sequence's rows begin (None: sequences of one length)
         k_len         int32[n_seq] on the device: how many rows of each slot of k and v are in use (None: all)
-        max_q, max_k  the longest sequence (None: taken to be all rows, which costs idle workgroups)
+        max_q, max_k  the longest sequence.  None: read from the pointers, which waits for the device; in a graph that is being recorded, all rows,
+                      which costs idle workgroups and is refused for many sequences
         bias, cuts    float32 [n_buckets][heads] and the ascending cuts between buckets of distance, on the host
         Rows of no sequence, and queries without keys, get zeros; a bias below GBT_BIAS_SHUT (-1e5) shuts its bucket out.
         save          also return what attention_backward needs: (out, saved)

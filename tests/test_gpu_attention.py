@@ -622,3 +622,42 @@ def test_a_loose_longest_sequence_costs_idle_workgroups_and_no_more(ctx):
         took[seqs] = begin.elapsed_time(end) / 5
     print(took)
     assert took[64] < 3 * took[65]
+
+
+def test_without_the_longest_sequences(ctx):
+    """max_q and max_k left out are what the pointers say: the same results as with them, for many sequences, single events and other streams."""
+    import paper_1806_11248_amd as g
+    rng = np.random.default_rng(72)
+    many = [int(x) for x in rng.integers(0, 40, 4_000)]
+    for nq, nk, room in ((many, many, 0), ([1] * 64, [int(x) for x in rng.integers(0, 900, 64)], 5), ([300, 0, 70], [40, 7, 500], 0), ([0, 0], [3, 0], 0), ([50], [60], 0)):
+        q, k, v, dout, args, spans = _make(nq, nk, 4, 2, 64, BF, causal=True, buckets=6, room=room, seed=73)
+        want, saved = ctx.attention(q, k, v, save=True, **args)
+        grads = ctx.attention_backward(dout, q, k, v, want, saved, **args)
+        for gone in (("max_q",), ("max_k",), ("max_q", "max_k")):
+            less = {n: x for n, x in args.items() if n not in gone}
+            out, saved = ctx.attention(q, k, v, save=True, **less)
+            assert torch.equal(out, want)
+            if len(nq) > 1:
+                assert all(torch.equal(a, b) for a, b in zip(ctx.attention_backward(dout, q, k, v, out, saved, **less), grads))
+    # the context's own stream, and a graph, in which nothing can be read: all rows there
+    side = torch.cuda.Stream()
+    own = g.Context(0, stream=side)
+    try:
+        q, k, v, dout, args, spans = _make([90, 20, 150], [90, 20, 150], 4, 2, 64, BF, causal=True, buckets=6, seed=74)
+        ref = _reference(q, k, v, args, spans)
+        less = {n: x for n, x in args.items() if n not in ("max_q", "max_k")}
+        side.wait_stream(torch.cuda.current_stream())
+        out = own.attention(q, k, v, **less)
+        side.synchronize()
+        close(out, ref.out, ref.out_tol, "out")
+        with torch.cuda.stream(side):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                out = own.attention(q, k, v, **less)
+            for _ in range(2):
+                out.zero_()
+                graph.replay()
+                side.synchronize()
+                close(out, ref.out, ref.out_tol, "out of a graph")
+    finally:
+        own.close()
