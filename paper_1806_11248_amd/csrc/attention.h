@@ -122,6 +122,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 struct Bf16 {
     typedef __bf16 elem;
     typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+    static constexpr float kAbove = 0.0f;   // while a row is summed, its largest probability is 2^kAbove at least
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -129,6 +130,7 @@ struct Bf16 {
 struct F16 {
     typedef _Float16 elem;
     typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+    static constexpr float kAbove = 7.0f;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }

@@ -4,7 +4,9 @@
 //
 // One pass over the keys with a running maximum and sum: out is kept as sum_j 2^(s_ij - m) v_j.  m follows the row's maximum only when
 // that has grown by more than kSlack: some row of a wave meets a new maximum in most tiles, but seldom one that much larger, and a factor of
-// 2^kSlack more or less matters to no 32-bit sum and to no rounding of a probability.
+// 2^kSlack more or less matters to no 32-bit sum and to no rounding of a probability.  float16 has few exponents: there m is kept
+// P::kAbove below the maximum, so that probabilities reach up to 2^15 and those of 2^-21 are still normal numbers.  (One key and 131,000 others at 2^-26
+// of its weight, without: 1.7% off, since the others are in the sum but not in the product.)
 // Sums, maxima and out are held in 32 bits; the probabilities are rounded to the inputs' type for the second product, while their
 // sum is taken of the unrounded ones (the rounding errors of a row then average out in out, whose own last place is of that size).
 // Rows of out are divided by the sum at the end; a row without keys has none and is zeros.
@@ -14,7 +16,7 @@
 
 namespace {
 
-constexpr float kSlack = 8.0f;
+constexpr float kSlack = 8.0f;   // kSlack + P::kAbove < 16: float16 ends before 2^16
 
 // ------------------------------------------------------------------------------------------------ blocks of queries --
 // A wave takes 32 queries of one head (its columns), a workgroup 128 or 64 (attn_form); keys and values pass through LDS, 64 at a time.  Of two groups
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) now = fmaxf(now, s[b][r]);
-        now = fmaxf(top, column_max(fmaf(now, factor, add)));
+        now = fmaxf(top, column_max(fmaf(now, factor, add - P::kAbove)));
         if (__any(now > top + kSlack)) {
             const float shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.0f : now));
             sum *= shrink;
@@ -311,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
         float now = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) now = fmaxf(now, s[r]);
-        now = fmaxf(top, column_max(fmaf(now, factor, add)));
+        now = fmaxf(top, column_max(fmaf(now, factor, add - P::kAbove)));
         if (__any(now > top + kSlack)) {
             const float shrink = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.0f : now));
             sum *= shrink;

@@ -661,3 +661,22 @@ def test_without_the_longest_sequences(ctx):
                 close(out, ref.out, ref.out_tol, "out of a graph")
     finally:
         own.close()
+
+
+def _one_key_and_many_small_ones(n, nq, seed):
+    """Queries that one key, the first, owns but for n others at 2^-26 of it, which are 2^-6 of the sum together where n is 2^20."""
+    q = torch.full((nq, 1, 8), 1.0, dtype=HF)
+    k = torch.zeros(n, 1, 8, dtype=HF)
+    k[0] = 26.0 * math.log(2.0) / 8.0
+    v = torch.full((n, 1, 8), -16.0, dtype=HF) + torch.randn(n, 1, 8, generator=torch.Generator().manual_seed(seed)).to(HF)
+    v[0] = 1.0
+    return q, k, v
+
+
+@pytest.mark.parametrize("nq", [1, 40, 200])
+def test_float16_keeps_small_probabilities(ctx, nq):
+    """What many keys of little weight add up to is in the result: none of them is below what a product in float16 holds."""
+    q, k, v = _one_key_and_many_small_ones(1 << 17, nq, 80)
+    ref = Reference(q, k, v, [(0, nq, 0, len(k))], False, 1.0)
+    out = ctx.attention(q.cuda(), k.cuda(), v.cuda(), scale=1.0)
+    close(out, ref.out, ref.out_tol, "out")
