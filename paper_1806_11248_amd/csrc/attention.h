@@ -53,7 +53,7 @@ struct AttnArgs {
     char *rest;                     // what rounding took from out, [q_rows][heads][dim], or NULL
     // backward
     AttnView dout, dq, dk, dv;
-    float *row_less;                // [heads][q_rows]: what a row's scores lose, -lse * log2(e) (-inf: a row without keys)
+    float *row_less;                // [heads][q_rows]: what a row's scores lose, kLift - lse * log2(e) (-inf: a row without keys)
     float *row_minus;               // [heads][q_rows]: and what its products of gradients with values are added to, -delta
     float *strips;                  // [heads][n_seq * k_blocks * q_parts][n_buckets]: the bias gradient of each block of keys
     float *dbias;                   // [n_buckets][heads]
@@ -122,6 +122,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 struct Bf16 {
     typedef __bf16 elem;
     typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+    static constexpr bool kNarrow = false;   // has too few exponents for what products are made of
     static constexpr float kAbove = 0.0f;   // while a row is summed, its largest probability is 2^kAbove at least
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -130,6 +131,7 @@ struct Bf16 {
 struct F16 {
     typedef _Float16 elem;
     typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+    static constexpr bool kNarrow = true;
     static constexpr float kAbove = 7.0f;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);

@@ -680,3 +680,60 @@ def test_float16_keeps_small_probabilities(ctx, nq):
     ref = Reference(q, k, v, [(0, nq, 0, len(k))], False, 1.0)
     out = ctx.attention(q.cuda(), k.cuda(), v.cuda(), scale=1.0)
     close(out, ref.out, ref.out_tol, "out")
+
+
+def _off(got, want):
+    """Relative errors of dq, dk and dv, and those of rounding the exact ones to float16 alone."""
+    def rel(x, y):
+        return float((x.cpu().double() - y).norm() / y.norm())
+
+    return [rel(x, y) for x, y in zip(got, want)], [rel(y.to(HF), y) for y in want]
+
+
+@pytest.mark.parametrize("D,causal", [(64, False), (128, True), (40, True)])
+def test_float16_gradients_of_small_gradients(ctx, D, causal):
+    """All gradients are linear in dout, so a smaller dout gives them as exactly, but for what the type cannot hold of them: twice each, for
+    roundings that fall differently."""
+    for exponent in (8, 10, 12):
+        q, k, v, dout, args, spans = _make([2048], [2048], 2, 1, D, HF, causal=causal, seed=81)
+        small = (dout.float() * 2.0 ** -exponent).to(HF)
+        large = (small.float() * 2.0 ** exponent).to(HF)                     # dout, but for what small cannot hold
+        assert torch.equal(small.double() * 2.0 ** exponent, large.double())
+        ref = _reference(q, k, v, args, spans, large)
+        out, saved = ctx.attention(q, k, v, save=True, **args)
+        of_large, _ = _off(ctx.attention_backward(large, q, k, v, out, saved, **args)[:3], (ref.dq, ref.dk, ref.dv))
+        of_small, rounding = _off(ctx.attention_backward(small, q, k, v, out, saved, **args)[:3], [x * 2.0 ** -exponent for x in (ref.dq, ref.dk, ref.dv)])
+        print(exponent, of_large, of_small, rounding)
+        for a, b, r in zip(of_small, of_large, rounding):
+            assert a <= 2 * b + 2 * r
+
+
+@pytest.mark.parametrize("nk", [40, 400])
+def test_float16_scores_gradients_beyond_the_type(ctx, nk):
+    """Gradients of scores above 65504, of queries and keys that are small, so that their own gradients are not."""
+    q, k, v, dout, args, spans = _make([nk], [nk], 2, 1, 64, HF, causal=True, seed=82)
+    q, k, v, dout = q * 2.0 ** -6, k * 2.0 ** -6, v * 256.0, dout * 2.0 ** -3
+    large = dout * 2.0 ** 15
+    out, saved = ctx.attention(q, k, v, save=True, **args)
+    ref = _reference(q, k, v, args, spans, dout)
+    of_dout, _ = _off(ctx.attention_backward(dout, q, k, v, out, saved, **args)[:3], (ref.dq, ref.dk, ref.dv))
+    got = ctx.attention_backward(large, q, k, v, out, saved, **args)[:3]
+    of_large, rounding = _off(got, [x * 2.0 ** 15 for x in (ref.dq, ref.dk, ref.dv)])
+    print(of_dout, of_large, rounding)
+    assert all(torch.isfinite(x).all() for x in got)
+    for a, b, r in zip(of_large, of_dout, rounding):
+        assert a <= 2 * b + 2 * r
+
+
+def test_float16_gradients_of_many_keys(ctx):
+    """Probabilities of 2^-19 on average: what the products with dout make of them is as exact as of few keys."""
+    errors = []
+    for nk in (300, 400_000):
+        q, k, v, dout, args, spans = _make([64], [nk], 1, 1, 16, HF, causal=False, seed=83)
+        dout = dout * 1024.0
+        ref = _reference(q, k, v, args, spans, dout)
+        out, saved = ctx.attention(q, k, v, save=True, **args)
+        errors.append(_off(ctx.attention_backward(dout, q, k, v, out, saved, **args)[:3], (ref.dq, ref.dk, ref.dv)))
+    print(errors)
+    for a, b, r in zip(errors[1][0][1:], errors[0][0][1:], errors[1][1][1:]):         # dk and dv
+        assert a <= 2 * b + 2 * r
