@@ -287,10 +287,11 @@ def _heads(t, name, dtype, shape=None):
 
 
 class GradientList:
-    """Tensors laid out for Context.clip_gradients; holds on to them."""
+    """Tensors laid out for Context.clip_gradients; holds on to them, and to the memory that they had then."""
 
     def __init__(self, tensors, outs, table, pieces):
         self.tensors, self.outs, self.table, self.pieces = tensors, outs, table, pieces
+        self.memory = [t.untyped_storage() for t in tensors + outs]     # the table's addresses, also of tensors that are given other memory later
         self.both = tensors + outs + [table]
 
 
@@ -795,7 +796,8 @@ class Context:
 
     def gradient_list(self, tensors, outs=None) -> GradientList:
         """Lays gradient tensors out for clip_gradients; outs receive the results (None: the tensors themselves).  Good for as long
-        as the tensors stay where they are; the list holds on to them."""
+        as the tensors stay where they are: the list holds on to the memory that they have now and goes on with it, also where a tensor is
+        given other memory or another takes its place.  Gradients that are allocated anew each step need a list each step."""
         tensors = list(tensors)
         outs = tensors if outs is None else list(outs)
         if len(outs) != len(tensors):

@@ -190,3 +190,17 @@ def test_refusals(ctx):
     assert lib.gbt_clip_gradients(ctx.h, b._ptr(lst.table), lst.pieces, 1.0, b._ptr(t), b._ptr(ws), 16383) == b.ENOMEM
     assert lib.gbt_clip_gradients(None, None, 0, 1.0, None, None, 0) == b.EINVAL
     assert bool((t == 1).all())
+
+
+def test_a_list_keeps_its_memory(ctx):
+    """Tensors that are given other memory after the list was made: the list goes on with what they had, which nobody else gets."""
+    for n in (1000, 300_000):
+        t, o = torch.full((n,), 2.0, device="cuda"), torch.zeros(n, device="cuda")
+        places = t.data_ptr(), o.data_ptr()
+        lst = ctx.gradient_list([t], [o])
+        t.data, o.data = torch.full((n,), 5.0, device="cuda"), torch.full((n,), 6.0, device="cuda")
+        others = [torch.full((n,), 9.0, device="cuda") for _ in range(8)]
+        assert not {x.data_ptr() for x in [t, o, *others]} & set(places)
+        norm = ctx.clip_gradients(lst, 1.0)
+        assert abs(float(norm) - 2.0 * math.sqrt(n)) <= 1e-6 * float(norm)
+        assert bool((t == 5.0).all()) and bool((o == 6.0).all()) and all(bool((x == 9.0).all()) for x in others)
