@@ -106,7 +106,7 @@ hipError_t gbt_launch_attention(hipStream_t stream, const AttnArgs &a, const Att
 hipError_t gbt_launch_attention_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
 hipError_t gbt_launch_attention_grad(hipStream_t stream, const AttnArgs &a, const AttnCuts &c, int dtype);
 constexpr int kAttnQueries = 128;   // of a workgroup of the block kernels (keys, where a workgroup owns keys)
-constexpr int kAttnFewRows = 32;    // (query, head of the group) columns of a workgroup of the few-rows kernel
+constexpr int kAttnFewRows = 32;    // (query, head of the group) columns of a key head that the few-rows kernel takes at most
 
 #define GBT_LOG2E 1.44269504088896340736f
 #define GBT_LN2 0.69314718055994530942f

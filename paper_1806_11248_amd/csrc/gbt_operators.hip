@@ -17,15 +17,14 @@ constexpr int64_t kFewWorkgroups = 4096, kFewPieces = 256;
 constexpr int64_t kFewLeast = 1024;
 
 struct FewPlan {
-    int64_t columns, blocks;   // (query, head of the group) pairs of a key head, and workgroups of them
-    int pieces, piece_len;     // of the key axis
+    int64_t columns;         // (query, head of the group) pairs of a key head
+    int pieces, piece_len;   // of the key axis
 };
 bool takes_few(const gbt_attention_params &p) { return (int64_t)(p.heads / p.kv_heads) * p.max_q <= kAttnFewRows; }
 FewPlan few_plan(const gbt_attention_params &p) {
     FewPlan f;
     f.columns = (int64_t)(p.heads / p.kv_heads) * p.max_q;
-    f.blocks = (f.columns + kAttnFewRows - 1) / kAttnFewRows;
-    const int64_t base = std::max<int64_t>(1, f.blocks * p.kv_heads * p.n_seq);
+    const int64_t base = std::max<int64_t>(1, (int64_t)p.kv_heads * p.n_seq);
     const int64_t want = std::max<int64_t>(1, kFewWorkgroups / base);
     const int64_t len = std::max<int64_t>(1, std::max((p.max_k + want - 1) / want, (p.max_k + kFewPieces - 1) / kFewPieces));
     f.piece_len = (int)((std::max(len, kFewLeast) + 127) / 128 * 128);

@@ -235,26 +235,26 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     extern __shared__ float table[];   // [n_buckets][32 columns]: the bias, times log2(e)
 
     if (blockIdx.x >= a.work) return zero_gaps(a, a.out, false);
-    const int columns = a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
+    const int columns = a.group * a.max_q;
     // the first pieces of all sequences before the second ones, and each time one further: side by side the later pieces, of which there are fewer, would
     // all go to some of the XCDs, and without the shift all of a long sequence's to one (128 stores of 30 to 3000 rows, 8 key heads of 64, 115 and 98 us, so 94; 16
     // of 2000 to 30000, 4 of 128, 113 and 128, so 114)
     const unsigned units = a.work / a.pieces, turn = blockIdx.x / units, unit = (blockIdx.x + turn) % units;
-    const int piece = (int)turn, block = (int)(unit % blocks), kv_head = (int)(unit / blocks % a.kv_heads), seq = (int)(unit / blocks / a.kv_heads);
+    const int piece = (int)turn, kv_head = (int)(unit % a.kv_heads), seq = (int)(unit / a.kv_heads);
     const AttnSeq rows = attn_seq(a, seq);
     const int begin = piece * a.piece_len;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int column = block * kAttnFewRows + col, query = column / a.group, head = kv_head * a.group + column % a.group;
-    if (block * kAttnFewRows / a.group >= rows.nq) return;
+    const int query = col / a.group, head = kv_head * a.group + col % a.group;
+    if (rows.nq == 0) return;
     if (begin > 0 && begin >= rows.nk) return;   // the first piece writes the rows without keys
     const int off = rows.nk - rows.nq;
     const bool there = query < rows.nq;
     const bool bias = a.n_buckets > 0;
 
-    const int q_low = block * kAttnFewRows / a.group, q_high = min(rows.nq - 1, (block * kAttnFewRows + kAttnFewRows - 1) / a.group);
+    const int q_high = rows.nq - 1;
     const int last = a.causal ? min(rows.nk - 1, query + off) : rows.nk - 1;
     const int end = min(min(rows.nk, begin + a.piece_len), a.causal ? q_high + off + 1 : rows.nk);
-    const int all = a.causal ? min(end, q_low + off + 1) : end;   // every query sees the keys before
+    const int all = a.causal ? min(end, off + 1) : end;   // every query sees the keys before
     const char *k_base = a.k.data + (rows.k0 * a.k.row + (int64_t)kv_head * a.k.head) * 2;
     const char *v_base = a.v.data + (rows.k0 * a.v.row + (int64_t)kv_head * a.v.head) * 2;
     char *k_tile = space + wave * (T::kBytes / 2), *v_tile = k_tile + 2 * T::kBytes;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
         for (int i = 0; i < kSteps; ++i) s = P::mma(T::template rows<P>(k_tile, 0, i, lane), qf[i], s);
         done_reading();
         fetch_k(min(kb + 128, end - 1));   // after the last step some key again, so that the count of loads under way stays the same
-        const int lowest = kb - (q_high + off), span = 31 + q_high - q_low;   // distances lowest .. lowest + span, 63 at most
+        const int lowest = kb - (q_high + off), span = 31 + q_high;   // distances lowest .. lowest + span, 63 at most
         const int mine = bias ? lane_bucket(is_cut[wave], cuts, lowest, lane) : 0;
         const int b0 = __builtin_amdgcn_readfirstlane(mine), b1 = __builtin_amdgcn_readlane(mine, span);
         float factor = a.scale2, add = 0.0f;
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
     for (int w = 0; w < 4; ++w) all_sum += join_sum[w][col] * __builtin_amdgcn_exp2f(join_top[w][col] - base);
     const bool whole = rows.nk <= a.piece_len;   // a sequence of one piece needs no joining
     const float factor = __builtin_amdgcn_exp2f(top - base) * (whole ? all_sum > 0.0f ? 1.0f / all_sum : all_sum == 0.0f ? 0.0f : all_sum : 1.0f);
-    const int64_t part = ((((int64_t)seq * a.kv_heads + kv_head) * columns + column) * a.pieces + piece) * (a.dim + 2);
+    const int64_t part = ((((int64_t)seq * a.kv_heads + kv_head) * columns + col) * a.pieces + piece) * (a.dim + 2);
     if (wave == 0 && half == 0 && there) {
         if (whole) {
             if (a.lse) a.lse[(int64_t)head * a.q_rows + rows.q0 + query] = all_sum == 0.0f ? -INFINITY : (all_top + __builtin_amdgcn_logf(all_sum)) * GBT_LN2;
@@ -374,17 +374,17 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
         for (int r = 0; r < 16; ++r) join_o[wave * kJoin + col * 33 + result_row(r, half)] = o[b][r] * factor;
         __syncthreads();
         for (int i = threadIdx.x; i < 32 * 32; i += 256) {
-            const int cc = i >> 5, d = 32 * b + (i & 31), column2 = block * kAttnFewRows + cc, query2 = column2 / a.group;
+            const int cc = i >> 5, d = 32 * b + (i & 31), query2 = cc / a.group;
             if (query2 >= rows.nq || d >= a.dim) continue;
             const int x = cc * 33 + (i & 31);
             const float w = (join_o[x] + join_o[kJoin + x]) + (join_o[2 * kJoin + x] + join_o[3 * kJoin + x]);
-            const int head2 = kv_head * a.group + column2 % a.group;
+            const int head2 = kv_head * a.group + cc % a.group;
             if (whole) {
                 const E y = (E)w;
                 ((E *)a.out.data)[(rows.q0 + query2) * a.out.row + (int64_t)head2 * a.out.head + d] = y;
                 if (a.rest) ((E *)a.rest)[((rows.q0 + query2) * a.heads + head2) * a.dim + d] = (E)(w - (float)y);
             } else {
-                a.part[((((int64_t)seq * a.kv_heads + kv_head) * columns + column2) * a.pieces + piece) * (a.dim + 2) + d] = w;
+                a.part[((((int64_t)seq * a.kv_heads + kv_head) * columns + cc) * a.pieces + piece) * (a.dim + 2) + d] = w;
             }
         }
     }
@@ -501,9 +501,9 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
 
 template <typename P, int DP>
 hipError_t launch_few(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
-    const int64_t columns = (int64_t)a.group * a.max_q, blocks = (columns + kAttnFewRows - 1) / kAttnFewRows;
+    const int64_t columns = (int64_t)a.group * a.max_q;
     AttnArgs b = a;
-    b.work = (unsigned)(a.pieces * blocks * a.kv_heads * a.n_seq);
+    b.work = (unsigned)((int64_t)a.pieces * a.kv_heads * a.n_seq);
     attention_few_kernel<P, DP><<<b.work + attn_gap_workgroups(a, true, false), 256, a.n_buckets * 32 * sizeof(float), stream>>>(b, c);
     if (a.pieces > 1) {
         const hipError_t e = hipGetLastError();

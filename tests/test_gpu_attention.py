@@ -737,3 +737,10 @@ def test_float16_gradients_of_many_keys(ctx):
     print(errors)
     for a, b, r in zip(errors[1][0][1:], errors[0][0][1:], errors[1][1][1:]):         # dk and dv
         assert a <= 2 * b + 2 * r
+
+
+@pytest.mark.parametrize("group,nq", [(1, 32), (1, 33), (1, 65), (3, 10), (3, 11), (3, 22), (4, 8), (4, 9), (4, 17), (16, 2), (16, 3), (32, 1), (33, 1)])
+def test_around_what_the_form_for_few_rows_takes(ctx, group, nq):
+    """32 pairs of query and head for a key head and a few more: both forms, of several pieces of the keys and of one."""
+    for causal in (False, True):
+        _check(ctx, _make([nq, max(1, nq - 1), 0], [5_000, 40, 9], 2 * group, 2, 64, BF, causal=causal, buckets=9, far=300, room=4, seed=90), backward=False)
