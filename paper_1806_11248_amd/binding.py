@@ -677,12 +677,13 @@ class Context:
         if torch.cuda.is_current_stream_capturing():
             return None
         with torch.cuda.stream(self.stream):
-            most = {}
+            most = []
             for ptr, used in ((q_ptr, None), (k_ptr, k_len)):
-                if ptr is not False and (ptr, used) not in most:
+                if ptr is not False and not (most and ptr is q_ptr and used is None):
                     lengths = ptr[1:] - ptr[:-1]
-                    most[ptr, used] = max(0, int((lengths if used is None else torch.minimum(lengths, used)).max()))
-            return most.get((q_ptr, None), 0), most.get((k_ptr, k_len), 0)
+                    most.append((lengths if used is None else torch.minimum(lengths, used)).max())
+            most = [max(0, x) for x in torch.stack(most).tolist()]       # one wait for both
+        return most[0], most[-1]
 
     def _attention_params(self, q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts):
         """(gbt_attention_params, what it points to on the host)."""
@@ -737,11 +738,12 @@ class Context:
 
         q_ptr, k_ptr  int64[n_seq + 1] on the device: where each sequence's rows begin (None: sequences of one length)
         k_len         int32[n_seq] on the device: how many rows of each slot of k and v are in use (None: all)
-        max_q, max_k  the longest sequence.  None: read from the pointers, which waits for the device; in a graph that is being recorded, all rows,
-                      which costs idle workgroups and is refused for many sequences
+        max_q, max_k  the longest sequence.  None: read from the pointers, which waits for the device (some 30 us a call); in a graph that is being
+                      recorded, all rows, which costs idle workgroups and is refused for many sequences
         bias, cuts    float32 [n_buckets][heads] and the ascending cuts between buckets of distance, on the host
         Rows of no sequence, and queries without keys, get zeros; a bias below GBT_BIAS_SHUT (-1e5) shuts its bucket out.
         save          also return what attention_backward needs: (out, saved)
+        No graph of derivatives is recorded, whether or not the inputs require gradients: attention_backward is the gradient.
         """
         p, edges = self._attention_params(q, k, q_ptr, k_ptr, k_len, max_q, max_k, causal, scale, bias, cuts)
         dtype = q.dtype
