@@ -520,7 +520,9 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
  *              causal: keys with t > 0 do not count
  *     out_i  = sum_j softmax_j(S) v_j;   a query without any key, or with all of them shut out: zeros
  * Scores, softmax statistics and all sums are held in 32 bits; probabilities are rounded to the inputs' type as
- * operands of the products with v and out's gradient, scores' gradients as operands of those with q and k.
+ * operands of the products with v and out's gradient, scores' gradients as operands of those with q and k.  In
+ * float16 those operands are held times powers of two that keep them among its normal numbers.  Few query rows
+ * (heads / kv_heads * max_q <= 32) keep probabilities in two such parts.
  * A non-finite element of a sequence makes that sequence's results of its key head non-finite in part; no
  * sequence depends on elements outside its own rows.
  *
@@ -604,8 +606,9 @@ GBT_API int32_t gbt_gradient_list(gbt_ctx *ctx, const gbt_gradient *gradients, i
 
 /*
  * *norm_out [dev] = sqrt(sum of all elements' squares), summed in 64 bits in a fixed order; every
- * dst = src * min(1, max_norm / (norm + 1e-6)), rounded once.  A norm that is not finite leaves the values as
- * they are (dst = src).  max_norm >= 0.  workspace [dev] >= 16384 bytes.  Asynchronous.
+ * dst = src * min(1, max_norm / (norm + 1e-6)): the factor is taken in 64 bits and rounded to a float, the product
+ * is one in 32 bits, rounded to the tensor's type.  A norm that is not finite leaves the values as they are
+ * (dst = src).  max_norm >= 0.  workspace [dev] >= 16384 bytes.  Asynchronous.
  */
 GBT_API int32_t gbt_clip_gradients(gbt_ctx *ctx, const void *list, int32_t pieces, double max_norm, float *norm_out,
                                    void *workspace, size_t workspace_bytes);

@@ -401,6 +401,15 @@ __device__ __forceinline__ typename P::vec8 operand(const f32x16 &x, int half) {
     return v;
 }
 
+// What rounding took from that.
+template <typename P>
+__device__ __forceinline__ typename P::vec8 operand_rest(const f32x16 &x, int half, typename P::vec8 rounded) {
+    typename P::vec8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (typename P::elem)(x[8 * half + e] - (float)rounded[e]);
+    return v;
+}
+
 // Row of register r of a 32 x 32 result.
 __device__ __forceinline__ constexpr int result_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
 

@@ -219,6 +219,8 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
 // workgroup take every fourth 32 keys of its piece of the key axis, each through its own part of LDS, so no wave waits for another.  The next
 // keys are under way as soon as the products with the last have been made, the next values likewise.  The waves are joined at the
 // end, the pieces by a second launch.
+// Probabilities are operands in two parts, what rounding takes from the first being the second: a few rows are few numbers, in which one rounded probability
+// shows (4 rows of 8 heads, an error of 1.3 to 1.8 times that of rounding the result alone), and the matrix units have the time.
 // Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 113 us (4.9 TB/s, where a large copy moves 5.1) and
 // 6 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 5.  Four short ones: 9.7 us, the time of one step after
 // the other.
@@ -332,9 +334,13 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnC
         T::half_ready();   // the values; the next keys are under way
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const V8 p = operand<P>(s, i);
+            const V8 p = operand<P>(s, i), rest = operand_rest<P>(s, i, p);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_tile, 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) {
+                const V8 values = T::template cols<P>(v_tile, 16 * i, b, lane);
+                o[b] = P::mma(values, p, o[b]);
+                o[b] = P::mma(values, rest, o[b]);
+            }
         }
         done_reading();
         fetch_v(min(kb + 128, end - 1));

@@ -744,3 +744,16 @@ def test_around_what_the_form_for_few_rows_takes(ctx, group, nq):
     """32 pairs of query and head for a key head and a few more: both forms, of several pieces of the keys and of one."""
     for causal in (False, True):
         _check(ctx, _make([nq, max(1, nq - 1), 0], [5_000, 40, 9], 2 * group, 2, 64, BF, causal=causal, buckets=9, far=300, room=4, seed=90), backward=False)
+
+
+@pytest.mark.parametrize("store", range(len(STORES)))
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_few_rows_round_their_result_alone(ctx, store, dtype):
+    """Single new events have few numbers, in which the rounding of a probability would show: theirs are operands in two parts, so the bound
+    is without it, but for the second part's own."""
+    nq, nk, H, K, D, room = STORES[store]
+    q, k, v, dout, args, spans = _make(nq, nk, H, K, D, dtype, causal=True, buckets=8, far=50, room=room, seed=100 + store)
+    ref = _reference(q, k, v, args, spans)
+    spread = _reference(q, k, v.abs(), args, spans).out
+    u = torch.finfo(dtype).eps / 2
+    close(ctx.attention(q, k, v, **args), ref.out, ref.out_tol - 1.01 * u * spread + 1.01 * u * u * spread, "out")
