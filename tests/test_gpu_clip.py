@@ -204,3 +204,16 @@ def test_a_list_keeps_its_memory(ctx):
         norm = ctx.clip_gradients(lst, 1.0)
         assert abs(float(norm) - 2.0 * math.sqrt(n)) <= 1e-6 * float(norm)
         assert bool((t == 5.0).all()) and bool((o == 6.0).all()) and all(bool((x == 9.0).all()) for x in others)
+
+
+@pytest.mark.parametrize("dtype", list(U))
+def test_what_is_rounded(ctx, dtype):
+    """The factor to a float, the product in 32 bits, and that to the type; of whole numbers, whose squares add up exactly."""
+    src = torch.randint(-200, 201, (70_001,), generator=torch.Generator().manual_seed(1)).to(dtype)
+    norm = math.sqrt(float((src.double() ** 2).sum()))
+    for max_norm in (1.0, 77.7, 0.999 * norm):
+        factor = torch.tensor(max_norm / (norm + 1e-6), dtype=torch.float64).float()
+        t = src.cuda()
+        got = ctx.clip_gradients(ctx.gradient_list([t]), max_norm)
+        assert float(got) == float(torch.tensor(norm, dtype=torch.float64).float())
+        assert torch.equal(t.cpu(), (src.float() * factor).to(dtype))
