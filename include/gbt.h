@@ -522,7 +522,7 @@ GBT_API int32_t gbt_predict_sparse(gbt_ctx *ctx, const gbt_tree *trees, int32_t 
  * Scores, softmax statistics and all sums are held in 32 bits; probabilities are rounded to the inputs' type as
  * operands of the products with v and out's gradient, scores' gradients as operands of those with q and k.  In
  * float16 those operands are held times powers of two that keep them among its normal numbers.  Few query rows
- * (heads / kv_heads * max_q <= 32) keep probabilities in two such parts.
+ * (heads / kv_heads * max_q <= 32) and few keys (max_k <= 64) keep out's probabilities in two such parts.
  * A non-finite element of a sequence makes that sequence's results of its key head non-finite in part; no
  * sequence depends on elements outside its own rows.
  *

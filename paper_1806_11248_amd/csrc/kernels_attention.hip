@@ -28,7 +28,13 @@ constexpr float kSlack = 8.0f;   // kSlack + P::kAbove < 16: float16 ends before
 // elements 304 us, 904 TFLOP/s of the pairs that count; not causal 128 queries a head against 16384 keys 1024 without a bias, 946 with one; heads of 64
 // 676 and 621; the matrix units are busy 39% of the time, LDS 24%, without bank conflicts (two causal histories of 4096).  Ragged short histories are
 // bound by how their blocks fall on the compute units: 24 of 100 to 1000 rows, 8 heads of 64 40 us, where blocks enough would take 27.
-template <typename P, int DP, int kQWaves, int kGroups>
+//
+// kParts: probabilities as operands, whole or in two parts.  The rounding errors of few probabilities do not average out, and what is wrong in out is wrong
+// in the backward pass's delta: of histories of 5 to 60 rows, 4 heads of 32, out was 1.12 times as far from the 64-bit result as rounding it alone makes it, and
+// dq 1.48 times.  Calls of at most one tile of keys a sequence take two parts, 1.00 and 1.43: 32 such histories 11.5 us as before, 2000 of 64 rows, heads of 64
+// 145, 150; 20,000 of 0 to 60 416, 461.  Longer ones are nearer anyhow (dq 1.43 to 1.45 times) and would pay as much.
+constexpr int kFewKeys = 64;
+template <typename P, int DP, int kQWaves, int kGroups, int kParts>
 __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(AttnArgs a, AttnCuts c) {
     typedef typename P::elem E;
     typedef typename P::vec8 V8;
@@ -159,8 +165,14 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const V8 p = operand<P>(s[i / 2], i % 2);
+            V8 rest;
+            if constexpr (kParts == 2) rest = operand_rest<P>(s[i / 2], i % 2, p);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = P::mma(T::template cols<P>(v_now, 16 * i, b, lane), p, o[b]);
+            for (int b = 0; b < kBlocks; ++b) {
+                const V8 values = T::template cols<P>(v_now, 16 * i, b, lane);
+                o[b] = P::mma(values, p, o[b]);
+                if constexpr (kParts == 2) o[b] = P::mma(values, rest, o[b]);
+            }
         }
     };
     for (int k0 = 0; k0 < end; k0 += 2 * kStride) {
@@ -499,9 +511,10 @@ hipError_t launch(hipStream_t stream, const AttnArgs &a, const AttnCuts &c) {
     b.work = attn_grid(b.order);
     const unsigned grid = b.work + attn_gap_workgroups(a, true, false);
     if (grid == 0) return hipSuccess;
-    if (form.queries == 64) attention_kernel<P, DP, 2, 2><<<grid, 256, 0, stream>>>(b, c);
-    else if (form.groups == 1) attention_kernel<P, DP, 4, 1><<<grid, 256, 0, stream>>>(b, c);
-    else if constexpr (DP > 64) attention_kernel<P, DP, 4, 2><<<grid, 512, 0, stream>>>(b, c);
+    if (form.queries == 64) attention_kernel<P, DP, 2, 2, 1><<<grid, 256, 0, stream>>>(b, c);
+    else if (a.max_k <= kFewKeys) attention_kernel<P, DP, 4, 1, 2><<<grid, 256, 0, stream>>>(b, c);   // which attn_form gives one group
+    else if (form.groups == 1) attention_kernel<P, DP, 4, 1, 1><<<grid, 256, 0, stream>>>(b, c);
+    else if constexpr (DP > 64) attention_kernel<P, DP, 4, 2, 1><<<grid, 512, 0, stream>>>(b, c);
     return hipGetLastError();
 }
 

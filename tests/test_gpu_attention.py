@@ -757,3 +757,17 @@ def test_few_rows_round_their_result_alone(ctx, store, dtype):
     spread = _reference(q, k, v.abs(), args, spans).out
     u = torch.finfo(dtype).eps / 2
     close(ctx.attention(q, k, v, **args), ref.out, ref.out_tol - 1.01 * u * spread + 1.01 * u * u * spread, "out")
+
+
+@pytest.mark.parametrize("D", [32, 64, 80, 128])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_few_keys_round_their_result_alone(ctx, D, dtype):
+    """Calls of at most 64 keys a sequence likewise, in the form for blocks of queries: the bound is without the rounding of probabilities."""
+    nq = [40, 64, 1, 300, 63, 33, 0, 128]
+    nk = [40, 64, 1, 64, 2, 60, 5, 20]
+    for causal in (False, True):
+        q, k, v, dout, args, spans = _make(nq, nk, 4, 2, D, dtype, causal=causal, buckets=8, far=50, seed=120)
+        ref = _reference(q, k, v, args, spans)
+        spread = _reference(q, k, v.abs(), args, spans).out
+        u = torch.finfo(dtype).eps / 2
+        close(ctx.attention(q, k, v, **args), ref.out, ref.out_tol - 1.01 * u * spread + 1.01 * u * u * spread, "out")
