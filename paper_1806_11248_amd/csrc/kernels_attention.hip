@@ -233,8 +233,8 @@ __global__ __launch_bounds__(64 * kQWaves * kGroups, 2) void attention_kernel(At
 // end, the pieces by a second launch.
 // Probabilities are operands in two parts, what rounding takes from the first being the second: a few rows are few numbers, in which one rounded probability
 // shows (4 rows of 8 heads, an error of 1.3 to 1.8 times that of rounding the result alone), and the matrix units have the time.
-// Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 113 us (4.9 TB/s, where a large copy moves 5.1) and
-// 6 us for the joining; matrix units busy 7%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 43 + 5.  Four short ones: 9.7 us, the time of one step after
+// Bound: memory.  16 stores of 2000 to 30000 rows, 16 heads of 128 elements on 4 key heads, 557 MB: 111 us (5.0 TB/s, where a large copy moves 5.1) and
+// 6 us for the joining; matrix units busy 11%, LDS 5%.  64 stores of 30 to 3000 rows, 220 MB: 45 + 5.  Four short ones: 10 us, the time of one step after
 // the other.
 template <typename P, int DP>
 __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttnArgs a, AttnCuts c) {

@@ -11,10 +11,10 @@
 // little to show in dq, whose dS are rounded as much, but it would be the largest error by far of the bias gradient, which is a
 // 32-bit result.  Since sum_j P_ij = 1, the row sums of the dS so computed are just that error: the first kernel adds them to its delta,
 // and the second works with sums of P dP as exact as 32 bits allow.  (Relative error of the bias gradient in bfloat16 with delta of out
-// and rest 7e-4, with the row sums 2e-7 .. 5e-7; of dq, rows of 5 .. 60 keys, without rest 2.9e-3, with it 2.4e-3.)
+// and rest 7e-4, with the row sums 2e-7 .. 5e-7; of dq, rows of 5 .. 60 keys, without rest 2.8e-3, with it 2.35e-3.)
 //
 // Bound: as the forward kernel's, matrix units and the arithmetic between the products.  Two causal histories of 4096, 16 heads of 128 elements on 4 key
-// heads: queries 243 us, 850 TFLOP/s of its three products, matrix units busy 45%; keys 414 us, 665 of its four, busy 35%: its waves keep 128 sums each and
+// heads: queries 245 us, 843 TFLOP/s of its three products, matrix units busy 45%; keys 414 us, 665 of its four, busy 35%: its waves keep 128 sums each and
 // meet at a barrier every 64 queries, so they do the same at the same time; joining the parts 17 us (83 MB).  16 histories of 100 to 1000 rows, 8 heads of
 // 64: 42 + 60 + 4.5 us.
 #include "attention.h"
