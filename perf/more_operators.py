@@ -326,7 +326,7 @@ def _plain_ortho(state):
     a, b, c = COEFFICIENTS
     for g, out, scale in zip(state["updates"], state["outs"], state["scales"]):
         x = g.float()
-        x = x / ((x.double() * x.double()).sum().sqrt() + 1e-7).float()
+        x = x / (x.double() * x.double()).sum().sqrt().clamp_min(1e-30).float()
         tall = x.shape[0] > x.shape[1]
         x = x.t().contiguous() if tall else x
         for _ in range(STEPS):
@@ -441,7 +441,7 @@ def _exact_ortho(case, state):
     result = []
     for g, scale in zip(state["updates"], state["scales"]):
         x = g.double()
-        x = x / (torch.linalg.vector_norm(x) + 1e-7)
+        x = x / torch.linalg.vector_norm(x)
         tall = x.shape[0] > x.shape[1]
         gram = x.t() @ x if tall else x @ x.t()
         # every step multiplies by a polynomial of one symmetric matrix, which all of them commute with
