@@ -613,6 +613,120 @@ GBT_API int32_t gbt_gradient_list(gbt_ctx *ctx, const gbt_gradient *gradients, i
 GBT_API int32_t gbt_clip_gradients(gbt_ctx *ctx, const void *list, int32_t pieces, double max_norm, float *norm_out,
                                    void *workspace, size_t workspace_bytes);
 
+/* ---- around a tower over histories: embedding, head norms with rotation, orthogonalised updates ------------ */
+
+/*
+ * Rows of a table by id: out_t = scale * table[ids[t]], one rounding; an id outside 0..n_rows-1 gives zeros.
+ * Rows may be any distance apart; a row's elements lie side by side, any width, each tensor aligned to its type
+ * (16-byte aligned rows of a multiple of 8 elements are read and written 16 bytes at a time).
+ */
+typedef struct gbt_embedding_params {
+    int32_t table_dtype, out_dtype; /* GBT_F32, GBT_BF16, GBT_F16 */
+    int32_t id_bytes;               /* 4: ids is int32_t, 8: int64_t */
+    int32_t width;                  /* 1..2^20 */
+    int64_t n_ids, n_rows;          /* 0..2^30 */
+    int64_t table_stride, out_stride; /* elements from row to row; what is written must not overlap */
+    const void *ids;                /* [dev] [n_ids] */
+    float scale;
+} gbt_embedding_params;
+
+/* out [dev] [n_ids] of width, overlapping no input.  Asynchronous. */
+GBT_API int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *params, const void *table, void *out);
+
+/*
+ * The table's gradient: grad_v = scale * (sum of dout_t over all t with ids[t] = v), summed in 32 bits and rounded
+ * once; rows without an id get zeros.  accumulate != 0: added to what grad holds, other rows stay as they are.
+ * table_dtype and table_stride are grad's, out_dtype and out_stride dout's.  Sums are taken in a fixed order: the
+ * same result on every run.  workspace [dev]: gbt_embedding_backward_workspace_bytes (0: none needed, NULL allowed,
+ * or parameters that the call refuses).  Asynchronous.
+ */
+GBT_API size_t gbt_embedding_backward_workspace_bytes(const gbt_embedding_params *params);
+GBT_API int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_params *params, const void *dout, void *grad,
+                                       int32_t accumulate, void *workspace, size_t workspace_bytes);
+
+/*
+ * What queries and keys go through before attention.  For every row and head, x of head_dim elements:
+ *     y = x / sqrt(mean x^2 + eps) * weight          weight: q_weight or k_weight
+ *     and of y's first `turned` elements, pair i turned by position * turns[i] revolutions:
+ *     (a, b) -> (a cos - b sin, a sin + b cos)
+ * halves: pair i is elements i and i + turned / 2; otherwise 2 i and 2 i + 1.  Angles are taken in 64 bits.  All in
+ * 32 bits between, rounded once.
+ *
+ * Rows belong to sequences as in gbt_attention: sequence s has the rows q_ptr[s] .. q_ptr[s + 1], nq of them, and
+ * with k_ptr or k_len it has nk rows of keys, its own the last of them; row i's place is i + nk - nq (nk = nq
+ * without both), and that is its position unless positions are given.  store != 0: k_out and v_out are stores, and
+ * row i's keys and values go to row k_ptr[s] + place, if that lies in the slot and is in use; all other rows of the
+ * stores stay as they are.  store = 0: they go to the rows they come from.  Rows of no sequence get zeros in q_out
+ * and, without a store, in k_out and v_out.  An output may be the very memory of its input (the same strides);
+ * otherwise outputs overlap no input.  Views are as in gbt_attention.
+ */
+typedef struct gbt_norm_rotate_params {
+    int32_t dtype;               /* GBT_BF16 or GBT_F16 (others: GBT_EUNSUPPORTED), of all but weights and turns */
+    int32_t heads, kv_heads;     /* any numbers */
+    int32_t head_dim;            /* 8..128, a multiple of 8 (others: GBT_EUNSUPPORTED) */
+    int32_t turned;              /* 0..head_dim, a multiple of 8 */
+    int32_t halves, store;
+    int32_t n_seq;
+    int32_t position_bytes;      /* 4: positions is int32_t, 8: int64_t */
+    float eps;                   /* 0..1 */
+    int64_t rows, out_rows;      /* of q, k and v; of k_out and v_out (rows, unless store) */
+    const int64_t *q_ptr;        /* [dev] int64[n_seq + 1], ascending; NULL: sequences of rows / n_seq rows each */
+    const int64_t *k_ptr;        /* [dev] int64[n_seq + 1]; NULL: slots of out_rows / n_seq rows each */
+    const int32_t *k_len;        /* [dev] int32[n_seq], or NULL: nk, else all rows of the slot */
+    const void *positions;       /* [dev] [rows], or NULL */
+    const float *q_weight, *k_weight; /* [dev] float[head_dim], or NULL: ones */
+    const double *turns;         /* [dev] double[turned / 2]: revolutions per position */
+} gbt_norm_rotate_params;
+
+/* v and v_out may both be NULL.  Asynchronous. */
+GBT_API int32_t gbt_norm_rotate(gbt_ctx *ctx, const gbt_norm_rotate_params *params, const gbt_heads *q, const gbt_heads *k,
+                                const gbt_heads *v, const gbt_heads *q_out, const gbt_heads *k_out, const gbt_heads *v_out);
+
+/*
+ * Gradients of q and k and of the weights (float[head_dim], overwritten), from those of q_out and k_out and the
+ * inputs of gbt_norm_rotate; store must be 0.  Rows of no sequence get zeros.  dq may be dq_out's or q's very
+ * memory, dk likewise.  Sums are taken in a fixed order.  workspace [dev]:
+ * gbt_norm_rotate_backward_workspace_bytes (0: parameters that the call refuses).  Asynchronous.
+ */
+GBT_API size_t gbt_norm_rotate_backward_workspace_bytes(const gbt_norm_rotate_params *params);
+GBT_API int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_params *params, const gbt_heads *dq_out,
+                                         const gbt_heads *dk_out, const gbt_heads *q, const gbt_heads *k, const gbt_heads *dq,
+                                         const gbt_heads *dk, float *dq_weight, float *dk_weight, void *workspace,
+                                         size_t workspace_bytes);
+
+/*
+ * Updates of weight matrices, orthogonalised: X = G / |G| (the Frobenius norm), then `steps` times
+ *     X <- (a I + b A + c A^2) X,  A = X X^T       (rows and columns exchanged where G has more rows)
+ * and dst = scale * X.  A matrix of zeros gives zeros, one with an element that is no finite number NaN throughout;
+ * no matrix depends on another.  Products take operands in two float16 parts, 22 bits, and are summed in 32: results
+ * are as exact as those of 32-bit products, whatever the type.
+ */
+typedef struct gbt_matrix {      /* rows x cols elements, one row after the other, any alignment of its type */
+    const void *src;             /* [dev] */
+    void *dst;                   /* [dev] may be src; overlaps no other matrix's src or dst */
+    int64_t rows, cols;          /* 0..2^20, the smaller one 0..2^15 */
+    int32_t dtype;               /* GBT_F32, GBT_BF16, GBT_F16 */
+    float scale;
+} gbt_matrix;
+
+/*
+ * Lays matrices out for gbt_orthogonalise, once for as long as addresses, sizes and scales hold: list_out [dev,
+ * 16-byte aligned] of gbt_matrix_list_bytes bytes (0: matrices that the call refuses; at most 65536).
+ * Asynchronous.
+ */
+GBT_API size_t gbt_matrix_list_bytes(const gbt_matrix *matrices, int64_t n_matrices);
+GBT_API int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int64_t n_matrices, void *list_out, size_t list_bytes);
+
+/*
+ * list and matrices: the same as in gbt_matrix_list.  steps 1..32; coefficients under which no singular value of
+ * 0..1 passes 4, nor its factor 64.  workspace [dev, 256-byte aligned]: gbt_orthogonalise_workspace_bytes, some
+ * 16 bytes for each element and 8 for each of the products X X^T, of as many matrices as fit 2 GB (or one).
+ * Asynchronous.
+ */
+GBT_API size_t gbt_orthogonalise_workspace_bytes(const gbt_matrix *matrices, int64_t n_matrices);
+GBT_API int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_matrix *matrices, int64_t n_matrices, int32_t steps,
+                                  float a, float b, float c, void *workspace, size_t workspace_bytes);
+
 /* ---- measurement -------------------------------------------------------- */
 
 /* Kernel classes timed by the optional profiler. */

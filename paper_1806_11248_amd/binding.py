@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import contextlib
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -39,6 +40,9 @@ SYMBOLS = [
     "gbt_grow_tree_sparse_lossguide_workspace_bytes", "gbt_grow_tree_sparse_lossguide",
     "gbt_attention_workspace_bytes", "gbt_attention", "gbt_attention_backward_workspace_bytes", "gbt_attention_backward",
     "gbt_gradient_list_bytes", "gbt_gradient_list", "gbt_clip_gradients",
+    "gbt_embedding", "gbt_embedding_backward_workspace_bytes", "gbt_embedding_backward",
+    "gbt_norm_rotate", "gbt_norm_rotate_backward_workspace_bytes", "gbt_norm_rotate_backward",
+    "gbt_matrix_list_bytes", "gbt_matrix_list", "gbt_orthogonalise_workspace_bytes", "gbt_orthogonalise",
 ]
 
 PROF_LEVELS = 18   # GBT_PROF_LEVELS
@@ -92,6 +96,22 @@ class AttentionParams(C.Structure):
 
 class Gradient(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
+class EmbeddingParams(C.Structure):
+    _fields_ = [("table_dtype", C.c_int32), ("out_dtype", C.c_int32), ("id_bytes", C.c_int32), ("width", C.c_int32), ("n_ids", C.c_int64),
+                ("n_rows", C.c_int64), ("table_stride", C.c_int64), ("out_stride", C.c_int64), ("ids", C.c_void_p), ("scale", C.c_float)]
+
+
+class NormRotateParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("turned", C.c_int32),
+                ("halves", C.c_int32), ("store", C.c_int32), ("n_seq", C.c_int32), ("position_bytes", C.c_int32), ("eps", C.c_float),
+                ("rows", C.c_int64), ("out_rows", C.c_int64), ("q_ptr", C.c_void_p), ("k_ptr", C.c_void_p), ("k_len", C.c_void_p),
+                ("positions", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("turns", C.c_void_p)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32), ("scale", C.c_float)]
 
 
 _NO_STREAM = contextlib.nullcontext()
@@ -175,6 +195,21 @@ def load():
     L.gbt_gradient_list_bytes.restype = sz
     L.gbt_gradient_list.argtypes = [vp, vp, i64, vp, sz, vp]
     L.gbt_clip_gradients.argtypes = [vp, vp, i32, f64, vp, vp, sz]
+    L.gbt_embedding.argtypes = [vp, vp, vp, vp]
+    L.gbt_embedding_backward_workspace_bytes.argtypes = [vp]
+    L.gbt_embedding_backward_workspace_bytes.restype = sz
+    L.gbt_embedding_backward.argtypes = [vp, vp, vp, vp, i32, vp, sz]
+    L.gbt_norm_rotate.argtypes = [vp] * 8
+    L.gbt_norm_rotate_backward_workspace_bytes.argtypes = [vp]
+    L.gbt_norm_rotate_backward_workspace_bytes.restype = sz
+    L.gbt_norm_rotate_backward.argtypes = [vp] * 11 + [sz]
+    L.gbt_matrix_list_bytes.argtypes = [vp, i64]
+    L.gbt_matrix_list_bytes.restype = sz
+    L.gbt_matrix_list.argtypes = [vp, vp, i64, vp, sz]
+    L.gbt_orthogonalise_workspace_bytes.argtypes = [vp, i64]
+    L.gbt_orthogonalise_workspace_bytes.restype = sz
+    f32 = C.c_float
+    L.gbt_orthogonalise.argtypes = [vp, vp, vp, i64, i32, f32, f32, f32, vp, sz]
     L.gbt_profile_enable.argtypes = [vp, i32]
     L.gbt_profile_read.argtypes = [vp, vp]
     L.gbt_measure_stream_read.argtypes = [vp, vp, sz, i32, vp, vp, sz]
@@ -275,6 +310,22 @@ def distance_cuts(n_buckets: int, far: int, causal: bool = True) -> list:
     return [-s for s in reversed(steps)] + [s + 1 for s in steps[:n - back]]
 
 
+def rotation_turns(turned: int, base: float = 10_000.0, device="cuda") -> torch.Tensor:
+    """What norm_rotate turns each pair of the first `turned` elements by, in revolutions per position: base ** (-2 i / turned) radians."""
+    i = torch.arange(0, turned, 2, dtype=torch.float64)
+    return (base ** (-i / max(1, turned)) / (2 * math.pi)).to(device)
+
+
+def _rows_of(t, name, device, n=None, width=None):
+    """The distance between rows of a tensor [n][width] whose last axis is contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype in DTYPES and t.dim() == 2 and n in (None, t.shape[0]) and width in (None, t.shape[1])):
+        raise TypeError(f"{name}: expected a tensor [{'rows' if n is None else n}][{'width' if width is None else width}] of float32, bfloat16 or float16 on {device}")
+    row, one = t.stride()
+    if one != 1 and t.shape[1] > 1 and t.shape[0]:
+        raise TypeError(f"{name}: expected a contiguous last axis")
+    return row if t.shape[0] > 1 else t.shape[1]
+
+
 def _heads(t, name, dtype, shape=None):
     """gbt_heads of a tensor [rows][heads][head_dim] (of that shape) whose last axis is contiguous."""
     n, h, d = shape or t.shape
@@ -293,6 +344,15 @@ class GradientList:
         self.tensors, self.outs, self.table, self.pieces = tensors, outs, table, pieces
         self.memory = [t.untyped_storage() for t in tensors + outs]     # the table's addresses, also of tensors that are given other memory later
         self.both = tensors + outs + [table]
+
+
+class MatrixList:
+    """Matrices laid out for Context.orthogonalise; holds on to them, and to the memory that they had then."""
+
+    def __init__(self, tensors, outs, table, arr, bytes_needed):
+        self.tensors, self.outs, self.table, self.arr, self.workspace_bytes = tensors, outs, table, arr, bytes_needed
+        self.memory = [t.untyped_storage() for t in tensors + outs]
+        self.all = tensors + outs + [table]
 
 
 class Context:
@@ -829,3 +889,203 @@ class Context:
         if st:
             self._check(st)
         return norm
+
+    # -- around a tower over histories ---------------------------------------------
+    def _embedding_params(self, ids, n_rows, table_dtype, out_dtype, width, table_stride, out_stride, scale):
+        if not (isinstance(ids, torch.Tensor) and ids.device == self.device and ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous()):
+            raise TypeError(f"ids: expected a contiguous tensor of int32 or int64 on {self.device}")
+        return EmbeddingParams(DTYPES[table_dtype], DTYPES[out_dtype], ids.element_size(), width, ids.numel(), n_rows, table_stride, out_stride,
+                               ids.data_ptr(), scale)
+
+    def embedding(self, table, ids, *, scale=1.0, dtype=None, out=None):
+        """Rows of table [rows][width] by ids of any shape, times scale: [*ids.shape][width] of `dtype` (None: the table's).  An id
+        outside the table gives zeros, a padding id of -1 for instance.
+
+        out           [ids][width], rows any distance apart: written to, and returned
+        No graph of derivatives is recorded: embedding_backward is the table's gradient.
+        """
+        stride = _rows_of(table, "table", self.device)
+        n_rows, width = table.shape
+        if out is not None:
+            of_out = _rows_of(out, "out", self.device, ids.numel() if isinstance(ids, torch.Tensor) else None, width)
+            if dtype not in (None, out.dtype):
+                raise TypeError(f"out: expected {dtype}")
+            dtype = out.dtype
+        else:
+            of_out, dtype = width, table.dtype if dtype is None else dtype
+        if dtype not in DTYPES:
+            raise TypeError("dtype: expected float32, bfloat16 or float16")
+        p = self._embedding_params(ids, n_rows, table.dtype, dtype, width, stride, of_out, scale)
+        if out is None:
+            with self._on_stream((table, ids)) or _NO_STREAM:
+                out = table.new_empty((*ids.shape, width), dtype=dtype)
+        else:
+            self._on_stream((table, ids, out))
+        st = self.lib.gbt_embedding(self.h, C.byref(p), table.data_ptr(), out.data_ptr())
+        if st:
+            self._check(st)
+        return out
+
+    def embedding_backward(self, dout, ids, rows=None, *, scale=1.0, dtype=torch.float32, out=None, accumulate=False):
+        """The gradient [rows][width] of embedding's table, of `dtype`, from that of its result [*ids.shape][width]: for each row the sum over
+        the places that hold its id, in 32 bits and a fixed order, times scale; zeros for rows without one.
+
+        out           [rows][width], rows any distance apart: written to, and returned
+        accumulate    add to what `out` holds
+        """
+        if not (isinstance(dout, torch.Tensor) and isinstance(ids, torch.Tensor) and dout.dim() >= 1 and dout.shape[:-1] in (ids.shape, (ids.numel(),))):
+            raise TypeError("dout: expected a tensor [*ids.shape][width]")
+        width = dout.shape[-1]
+        dout = dout if dout.dim() == 2 else dout.reshape(ids.numel(), width)
+        of_out = _rows_of(dout, "dout", self.device)
+        if out is not None:
+            stride = _rows_of(out, "out", self.device, rows, width)
+            rows, dtype = out.shape[0], out.dtype
+        elif accumulate or rows is None:
+            raise TypeError("out: expected a tensor to add to" if accumulate else "rows: expected the number of the table's rows")
+        else:
+            stride = width
+        if dtype not in DTYPES:
+            raise TypeError("dtype: expected float32, bfloat16 or float16")
+        p = self._embedding_params(ids, rows, dtype, dout.dtype, width, stride, of_out, scale)
+        ws_bytes = self.lib.gbt_embedding_backward_workspace_bytes(C.byref(p))
+        with self._on_stream((dout, ids, out)) or _NO_STREAM:
+            if out is None:
+                out = dout.new_empty((rows, width), dtype=dtype)
+            ws = self._scratch("embedding", ws_bytes) if ws_bytes else None
+        st = self.lib.gbt_embedding_backward(self.h, C.byref(p), dout.data_ptr(), out.data_ptr(), bool(accumulate), ws.data_ptr() if ws_bytes else None, ws_bytes)
+        if st:
+            self._check(st)
+        return out
+
+    def _norm_rotate_params(self, q, k, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, eps, halves, store_rows):
+        if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3 and q.device == self.device):
+            raise TypeError(f"q, k: expected tensors [rows][heads][head_dim] on {self.device}")
+        rows, heads, dim = q.shape
+        counts = [x.numel() - less for x, less, dtype, name in ((q_ptr, 1, torch.int64, "q_ptr"), (k_ptr, 1, torch.int64, "k_ptr"), (k_len, 0, torch.int32, "k_len"))
+                  if x is not None and _need(x, dtype, name) is x]
+        n_seq = counts[0] if counts else 1
+        if any(n != n_seq for n in counts):
+            raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
+        if q_ptr is None and n_seq > 0 and rows % n_seq:
+            raise TypeError(f"q: without q_ptr all of {n_seq} sequences have the same length")
+        if store_rows is not None and k_ptr is None and n_seq > 0 and store_rows % n_seq:
+            raise TypeError(f"k_out: without k_ptr all of {n_seq} slots have the same length")
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and _need(w, torch.float32, name).shape != (dim,):
+                raise TypeError(f"{name}: expected [{dim}]")
+        turned = 0
+        if turns is not None:
+            if _need(turns, torch.float64, "turns").dim() != 1:
+                raise TypeError("turns: expected [turned / 2]")
+            turned = 2 * turns.numel()
+        wide = 4
+        if positions is not None:
+            if positions.dtype is not torch.int32:
+                _need(positions, torch.int64, "positions")
+                wide = 8
+            if _need(positions, positions.dtype, "positions").shape != (rows,):
+                raise TypeError(f"positions: expected [{rows}]")
+        at = [None if x is None else x.data_ptr() for x in (q_ptr, k_ptr, k_len, positions, q_weight, k_weight, turns)]
+        return NormRotateParams(DTYPES.get(q.dtype, -1), heads, k.shape[1], dim, turned, bool(halves), store_rows is not None, n_seq, wide, eps, rows,
+                                rows if store_rows is None else store_rows, *at)
+
+    def norm_rotate(self, q, k, q_weight, k_weight, turns, *, v=None, q_ptr=None, k_ptr=None, k_len=None, positions=None, eps=1e-6, halves=True,
+                    q_out=None, k_out=None, v_out=None):
+        """Every head of q [rows][heads][head_dim] and k [rows][kv_heads][head_dim] divided by its root mean square (of its elements; eps is added
+        to the mean), times a weight float32 [head_dim] (None: ones), its pairs turned by position * turns revolutions (float64 [turned / 2],
+        rotation_turns; None: not turned).  Returns (q_out, k_out), and v_out with v.
+
+        q_ptr, k_ptr, k_len   the rows of sequences, as for attention: row i of nq has place i + nk - nq, and nk is nq without k_ptr and k_len
+        positions     int32 or int64 [rows] on the device (None: the places)
+        halves        a pair is elements i and i + turned / 2; else 2 i and 2 i + 1
+        k_out, v_out  with k_ptr or k_len: stores, in which a row's keys and values (v, as they are) go to the place in its sequence's slot;
+                      nothing else there is touched
+        Outputs may be the inputs themselves.  Rows of no sequence get zeros, except in stores.
+        No graph of derivatives is recorded: norm_rotate_backward is the gradient.
+        """
+        if (v is None) != (v_out is None) and (v is None or k_out is not None):
+            raise TypeError("v, v_out: one without the other")
+        store = k_out is not None and (k_ptr is not None or k_len is not None)
+        if store and not (isinstance(k_out, torch.Tensor) and k_out.dim() == 3):
+            raise TypeError("k_out: expected a tensor [rows][kv_heads][head_dim]")
+        p = self._norm_rotate_params(q, k, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, eps, halves, k_out.shape[0] if store else None)
+        dtype = q.dtype
+        of_q = rows, heads, dim = q.shape
+        of_k, of_out = (rows, p.kv_heads, dim), (p.out_rows, p.kv_heads, dim)
+        hq, hk = _heads(q, "q", dtype, of_q), _heads(k, "k", dtype, of_k)
+        hv = None if v is None else _heads(v, "v", dtype, of_k)
+        with self._on_stream((q, k, v, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, q_out, k_out, v_out)) or _NO_STREAM:
+            if q_out is None:
+                q_out = q.new_empty(of_q)
+            if k_out is None:
+                k_out = q.new_empty(of_k)
+            if v is not None and v_out is None:
+                v_out = q.new_empty(of_k)
+        hq_out, hk_out = _heads(q_out, "q_out", dtype, of_q), _heads(k_out, "k_out", dtype, of_out)
+        if v is None:
+            st = self.lib.gbt_norm_rotate(self.h, C.byref(p), C.byref(hq), C.byref(hk), None, C.byref(hq_out), C.byref(hk_out), None)
+        else:
+            hv_out = _heads(v_out, "v_out", dtype, of_out)
+            st = self.lib.gbt_norm_rotate(self.h, C.byref(p), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hq_out), C.byref(hk_out), C.byref(hv_out))
+        if st:
+            self._check(st)
+        return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+    def norm_rotate_backward(self, dq_out, dk_out, q, k, q_weight, k_weight, turns, *, q_ptr=None, k_ptr=None, k_len=None, positions=None, eps=1e-6,
+                             halves=True, dq=None, dk=None):
+        """(dq, dk, dq_weight, dk_weight) of norm_rotate with the same arguments and packed outputs, from the gradients of q_out and k_out.  dq and
+        dk: written to where given (parts of one tensor for the projection's gradient, say; or dq_out and dk_out themselves).  Rows of no
+        sequence get zeros."""
+        p = self._norm_rotate_params(q, k, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, eps, halves, None)
+        dtype = q.dtype
+        of_q = rows, heads, dim = q.shape
+        of_k = rows, p.kv_heads, dim
+        hq, hk = _heads(q, "q", dtype, of_q), _heads(k, "k", dtype, of_k)
+        hdq_out, hdk_out = _heads(dq_out, "dq_out", dtype, of_q), _heads(dk_out, "dk_out", dtype, of_k)
+        ws_bytes = self.lib.gbt_norm_rotate_backward_workspace_bytes(C.byref(p))
+        with self._on_stream((dq_out, dk_out, q, k, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, dq, dk)) or _NO_STREAM:
+            if dq is None:
+                dq = q.new_empty(of_q)
+            if dk is None:
+                dk = q.new_empty(of_k)
+            weights = q.new_empty((2, dim), dtype=torch.float32)
+            ws = self._scratch("norm_rotate", ws_bytes)
+        hdq, hdk = _heads(dq, "dq", dtype, of_q), _heads(dk, "dk", dtype, of_k)
+        st = self.lib.gbt_norm_rotate_backward(self.h, C.byref(p), C.byref(hdq_out), C.byref(hdk_out), C.byref(hq), C.byref(hk), C.byref(hdq), C.byref(hdk),
+                                               weights.data_ptr(), weights.data_ptr() + 4 * dim, ws.data_ptr(), ws.numel())
+        if st:
+            self._check(st)
+        return dq, dk, weights[0], weights[1]
+
+    def matrix_list(self, tensors, outs=None, *, scales=1.0) -> MatrixList:
+        """Lays matrices [rows][cols] out for orthogonalise; outs receive the results (None: the tensors themselves), times scales (one for
+        each, or one for all).  Good for as long as the tensors stay where they are, as a gradient_list is."""
+        tensors = list(tensors)
+        outs = tensors if outs is None else list(outs)
+        scales = [float(scales)] * len(tensors) if isinstance(scales, (int, float)) else [float(x) for x in scales]
+        if len(outs) != len(tensors) or len(scales) != len(tensors):
+            raise TypeError("outs, scales: expected one for each tensor")
+        arr = (Matrix * max(1, len(tensors)))()
+        for i, (t, o, scale) in enumerate(zip(tensors, outs, scales)):
+            if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dim() == 2 and t.is_contiguous() and t.dtype in DTYPES):
+                raise TypeError(f"tensors[{i}]: expected a contiguous tensor [rows][cols] of float32, bfloat16 or float16 on {self.device}")
+            if _need(o, t.dtype, f"outs[{i}]").shape != t.shape:
+                raise TypeError(f"outs[{i}]: expected {tuple(t.shape)}")
+            arr[i] = Matrix(t.data_ptr(), o.data_ptr(), *t.shape, DTYPES[t.dtype], scale)
+        nbytes = self.lib.gbt_matrix_list_bytes(arr, len(tensors))
+        with self._on_stream() or _NO_STREAM:
+            table = self.empty((max(16, nbytes),), torch.uint8)
+        self._check(self.lib.gbt_matrix_list(self.h, arr, len(tensors), _ptr(table), table.numel()))
+        return MatrixList(tensors, outs, table, arr, self.lib.gbt_orthogonalise_workspace_bytes(arr, len(tensors)))
+
+    def orthogonalise(self, matrices: MatrixList, *, steps=5, coefficients=(3.4445, -4.7750, 2.0315)):
+        """Every matrix of the list divided by its norm, then `steps` times X <- (a I + b A + c A^2) X with A = X X^T, times its scale, into its
+        out: all singular values end near one.  A matrix of zeros gives zeros, one that is not finite NaN.  Returns the outs."""
+        a, b, c = coefficients
+        with self._on_stream(matrices.all) or _NO_STREAM:
+            ws = self._scratch("orthogonalise", matrices.workspace_bytes)
+        st = self.lib.gbt_orthogonalise(self.h, matrices.table.data_ptr(), matrices.arr, len(matrices.tensors), steps, a, b, c, ws.data_ptr(), ws.numel())
+        if st:
+            self._check(st)
+        return matrices.outs

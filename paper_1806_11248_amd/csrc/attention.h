@@ -10,13 +10,9 @@
 #pragma once
 
 #include "gbt_internal.h"
+#include "heads.h"
 
 constexpr int kAttnBuckets = GBT_MAX_BUCKETS;   // of distance; a power of two
-
-struct AttnView {   // rows x heads x head_dim elements; strides in elements, the head's elements side by side
-    char *data;
-    int64_t row, head;
-};
 
 // How the workgroups of a launch go over the work: `blocks` blocks of each of `units` units (heads, or key heads and parts) of every sequence.
 //

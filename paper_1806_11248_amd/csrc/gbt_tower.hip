@@ -1,0 +1,464 @@
+// The C ABI of the operators around a tower over histories (see include/gbt.h): checks of arguments, workspaces, launches.
+#include <string.h>
+
+#include <new>
+
+#include "embedding.h"
+#include "norm_rotate.h"
+#include "ortho.h"
+
+namespace {
+
+bool known_type(int32_t dtype) { return dtype == GBT_F32 || dtype == GBT_BF16 || dtype == GBT_F16; }
+int64_t size_of(int32_t dtype) { return dtype == GBT_F32 ? 4 : 2; }
+constexpr int64_t kMostWorkgroups = (1 << 23) - 1024;   // of a launch, of up to 512 threads, of which there can be 2^32
+
+// --------------------------------------------------------------- embedding --
+const char *embedding_fault(const gbt_embedding_params &p, int32_t *code) {
+    *code = GBT_EUNSUPPORTED;
+    if (!known_type(p.table_dtype) || !known_type(p.out_dtype)) return "table_dtype or out_dtype is none of GBT_F32, GBT_BF16, GBT_F16";
+    if (p.n_ids > ((int64_t)1 << 30)) return "more than 2^30 ids";
+    if (p.n_rows > ((int64_t)1 << 30)) return "more than 2^30 rows";
+    if (p.width > (1 << 20)) return "width > 2^20";
+    *code = GBT_EINVAL;
+    if (p.id_bytes != 4 && p.id_bytes != 8) return "id_bytes is neither 4 nor 8";
+    if (p.n_ids < 0 || p.n_rows < 0 || p.width < 1) return "n_ids, n_rows or width out of range";
+    if (p.table_stride < 0 || p.out_stride < 0 || p.table_stride > ((int64_t)1 << 40) || p.out_stride > ((int64_t)1 << 40)) return "a stride out of range";
+    if (!isfinite(p.scale)) return "scale is not finite";
+    if (p.n_ids > 0 && (!p.ids || ((uintptr_t)p.ids & (uintptr_t)(p.id_bytes - 1)))) return "ids is NULL or not aligned";
+    return nullptr;
+}
+bool rows_of_eight(const void *x, int64_t stride, int64_t size) { return ((uintptr_t)x & 15u) == 0 && stride * size % 16 == 0; }
+
+void fill(EmbedArgs &a, const gbt_embedding_params &p, const void *table, void *out) {
+    memset(&a, 0, sizeof a);
+    a.ids = p.ids;
+    a.id_bytes = p.id_bytes;
+    a.width = p.width;
+    while (a.log_lanes < 6 && (8 << a.log_lanes) < p.width) ++a.log_lanes;
+    a.slabs = (p.width + (8 << a.log_lanes) - 1) / (8 << a.log_lanes);
+    a.vector = p.width % 8 == 0 && rows_of_eight(table, p.table_stride, size_of(p.table_dtype)) && rows_of_eight(out, p.out_stride, size_of(p.out_dtype));
+    a.n_ids = p.n_ids;
+    a.n_rows = p.n_rows;
+    a.table_stride = p.table_stride;
+    a.out_stride = p.out_stride;
+    a.scale = p.scale;
+    a.table = table;
+    a.out = out;
+    a.table_dtype = p.table_dtype;
+    a.out_dtype = p.out_dtype;
+}
+
+// Few ids are looked for by the workgroups that own rows, unless these are too many.
+constexpr int64_t kFewRowsWorkgroups = 4096;   // aimed at; a workgroup owns 32 rows at most
+bool takes_few_ids(const gbt_embedding_params &p) { return p.n_ids <= kEmbedFewIds && p.n_rows <= kFewRowsWorkgroups * 32; }
+
+struct SortLayout {
+    int passes, bits[4], tiles;
+    int64_t tile, chunk, chunks;
+    size_t key[2], pos[2], hist, part, bytes;
+};
+SortLayout sort_layout(const gbt_embedding_params &p) {
+    SortLayout l;
+    int bits = 1;
+    while (bits < 31 && ((int64_t)1 << bits) <= p.n_rows) ++bits;   // n_rows itself is a key
+    l.passes = (bits + 9) / 10;
+    for (int i = 0; i < l.passes; ++i) l.bits[i] = bits / l.passes + (i < bits % l.passes);
+    l.tile = ((p.n_ids + kSortTiles - 1) / kSortTiles + kSortItems - 1) / kSortItems * kSortItems;
+    l.tiles = (int)((p.n_ids + l.tile - 1) / l.tile);
+    EmbedArgs a;
+    fill(a, p, nullptr, nullptr);
+    // Places that a group of lanes adds up: as many as leave some 8000 waves, within limits of what a run's beginnings and ends cost.
+    const int64_t per_wave = 64 >> a.log_lanes;
+    l.chunk = std::min<int64_t>(64, std::max<int64_t>(16, p.n_ids * a.slabs / (8192 * per_wave)));
+    while ((p.n_ids + l.chunk - 1) / l.chunk * a.slabs > kMostWorkgroups) l.chunk *= 2;
+    l.chunks = (p.n_ids + l.chunk - 1) / l.chunk;
+    const size_t list = gbt_align((size_t)p.n_ids * 4);
+    l.key[0] = 0, l.key[1] = list, l.pos[0] = 2 * list, l.pos[1] = 3 * list;
+    l.hist = 4 * list;
+    l.part = l.hist + gbt_align((size_t)l.tiles * kSortDigits * 4);
+    l.bytes = l.part + (size_t)l.chunks * 2 * a.slabs * (8 << a.log_lanes) * 4;
+    return l;
+}
+
+}  // namespace
+
+extern "C" int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *params, const void *table, void *out) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, params, GBT_EINVAL, "NULL argument");
+    const gbt_embedding_params &p = *params;
+    int32_t code;
+    const char *fault = embedding_fault(p, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    GBT_REQUIRE(ctx, (table || p.n_rows == 0) && (out || p.n_ids == 0), GBT_EINVAL, "table or out is NULL");
+    GBT_REQUIRE(ctx, (((uintptr_t)table & (uintptr_t)(size_of(p.table_dtype) - 1)) | ((uintptr_t)out & (uintptr_t)(size_of(p.out_dtype) - 1))) == 0, GBT_EINVAL,
+                "table or out is not aligned");
+    GBT_REQUIRE(ctx, p.out_stride >= p.width || p.n_ids <= 1, GBT_EINVAL, "out: rows overlap");
+    if (p.n_ids == 0) return GBT_OK;
+    EmbedArgs a;
+    fill(a, p, table, out);
+    GBT_HIP(ctx, gbt_launch_embedding(ctx->stream, a));
+    return GBT_OK;
+}
+
+extern "C" size_t gbt_embedding_backward_workspace_bytes(const gbt_embedding_params *params) {
+    int32_t code;
+    if (!params || embedding_fault(*params, &code) || takes_few_ids(*params) || params->n_ids == 0) return 0;
+    return sort_layout(*params).bytes;
+}
+
+extern "C" int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_params *params, const void *dout, void *grad, int32_t accumulate,
+                                          void *workspace, size_t workspace_bytes) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, params, GBT_EINVAL, "NULL argument");
+    const gbt_embedding_params &p = *params;
+    int32_t code;
+    const char *fault = embedding_fault(p, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    GBT_REQUIRE(ctx, (grad || p.n_rows == 0) && (dout || p.n_ids == 0), GBT_EINVAL, "dout or grad is NULL");
+    GBT_REQUIRE(ctx, (((uintptr_t)grad & (uintptr_t)(size_of(p.table_dtype) - 1)) | ((uintptr_t)dout & (uintptr_t)(size_of(p.out_dtype) - 1))) == 0, GBT_EINVAL,
+                "dout or grad is not aligned");
+    GBT_REQUIRE(ctx, p.table_stride >= p.width || p.n_rows <= 1, GBT_EINVAL, "grad: rows overlap");
+    const size_t need = gbt_embedding_backward_workspace_bytes(params);
+    GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
+    GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    GBT_REQUIRE(ctx, ((uintptr_t)workspace & 15u) == 0 || need == 0, GBT_EINVAL, "workspace is not 16-byte aligned");
+    if (p.n_rows == 0 || (p.n_ids == 0 && accumulate)) return GBT_OK;
+    EmbedArgs a;
+    fill(a, p, grad, const_cast<void *>(dout));
+    a.accumulate = accumulate != 0;
+    if (takes_few_ids(p)) {
+        a.zero_rows = (int)((p.n_rows + kFewRowsWorkgroups - 1) / kFewRowsWorkgroups);
+        GBT_HIP(ctx, gbt_launch_embedding_grad_few(ctx->stream, a));
+        return GBT_OK;
+    }
+    // rows that a wave clears: as many as leave some 8000 waves
+    a.zero_rows = (int)std::min<int64_t>(64, std::max<int64_t>(1, p.n_rows / 8192));
+    if (p.n_ids > 0) {
+        const SortLayout l = sort_layout(p);
+        char *ws = (char *)workspace;
+        SortPass s;
+        memset(&s, 0, sizeof s);
+        s.id_bytes = p.id_bytes;
+        s.n = p.n_ids;
+        s.n_rows = p.n_rows;
+        s.tile = l.tile;
+        s.tiles = l.tiles;
+        s.hist = (uint32_t *)(ws + l.hist);
+        for (int i = 0; i < l.passes; ++i) {
+            s.ids = i == 0 ? p.ids : nullptr;
+            s.key_in = (const uint32_t *)(ws + l.key[(i + 1) & 1]);
+            s.pos_in = (const uint32_t *)(ws + l.pos[(i + 1) & 1]);
+            s.key_out = (uint32_t *)(ws + l.key[i & 1]);
+            s.pos_out = (uint32_t *)(ws + l.pos[i & 1]);
+            s.bits = l.bits[i];
+            GBT_HIP(ctx, gbt_launch_sort_pass(ctx->stream, s));
+            s.shift += s.bits;
+        }
+        a.key = s.key_out;
+        a.pos = s.pos_out;
+        a.part = (float *)(ws + l.part);
+        a.chunk = (int)l.chunk;
+        a.chunks = (int)l.chunks;
+    }
+    GBT_HIP(ctx, gbt_launch_embedding_grad(ctx->stream, a));
+    return GBT_OK;
+}
+
+// ------------------------------------------------- head norms and rotation --
+namespace {
+
+const char *rotate_fault(const gbt_norm_rotate_params &p, int32_t *code) {
+    *code = GBT_EUNSUPPORTED;
+    if (p.dtype != GBT_BF16 && p.dtype != GBT_F16) return "dtype is neither GBT_BF16 nor GBT_F16";
+    if (p.head_dim < 8 || p.head_dim > GBT_MAX_HEAD_DIM || p.head_dim % 8) return "head_dim is no multiple of 8 in 8..128";
+    if (p.turned % 8) return "turned is no multiple of 8";
+    *code = GBT_EINVAL;
+    if (p.heads < 1 || p.kv_heads < 1 || p.heads > (1 << 16) || p.kv_heads > (1 << 16)) return "heads or kv_heads out of range";
+    if (p.turned < 0 || p.turned > p.head_dim) return "turned outside 0..head_dim";
+    if (p.rows < 0 || p.rows > ((int64_t)1 << 40) || p.out_rows < 0 || p.out_rows > ((int64_t)1 << 40)) return "rows or out_rows out of range";
+    if (p.n_seq < 0) return "n_seq < 0";
+    if (!p.q_ptr && p.n_seq > 0 && p.rows % p.n_seq) return "rows is no multiple of n_seq without q_ptr";
+    if (p.store && !p.k_ptr && p.n_seq > 0 && p.out_rows % p.n_seq) return "out_rows is no multiple of n_seq without k_ptr";
+    if (!p.store && p.out_rows != p.rows) return "out_rows is not rows without a store";
+    if (!(p.eps >= 0.0f && p.eps <= 1.0f)) return "eps outside 0..1";
+    if (p.positions && p.position_bytes != 4 && p.position_bytes != 8) return "position_bytes is neither 4 nor 8";
+    if (p.positions && ((uintptr_t)p.positions & (uintptr_t)(p.position_bytes - 1))) return "positions is not aligned";
+    if (p.turned > 0 && (!p.turns || ((uintptr_t)p.turns & 7u))) return "turns is NULL or not aligned";
+    if ((((uintptr_t)p.q_weight | (uintptr_t)p.k_weight | (uintptr_t)p.k_len) & 3u) || (((uintptr_t)p.q_ptr | (uintptr_t)p.k_ptr) & 7u))
+        return "a weight or pointer array is not aligned";
+    return nullptr;
+}
+
+void fill(RotateArgs &a, const gbt_norm_rotate_params &p, int lines) {
+    memset(&a, 0, sizeof a);
+    a.q_ptr = p.q_ptr;
+    a.k_ptr = p.k_ptr;
+    a.k_len = p.k_len;
+    a.positions = p.positions;
+    a.position_bytes = p.position_bytes;
+    a.q_weight = p.q_weight;
+    a.k_weight = p.k_weight;
+    a.turns = p.turns;
+    a.rows = p.rows;
+    a.out_rows = p.out_rows;
+    a.n_seq = p.n_seq;
+    a.heads = p.heads;
+    a.kv_heads = p.kv_heads;
+    a.lines = lines;
+    a.dim = p.head_dim;
+    a.turned = p.turned;
+    a.halves = p.halves != 0;
+    a.store = p.store != 0;
+    a.slots = p.k_ptr || p.k_len;
+    a.eps = p.eps;
+    while ((8 << a.log_lanes) < p.head_dim) ++a.log_lanes;
+    const int at_once = 64 >> a.log_lanes;
+    a.row_group = std::max(1, at_once / lines);
+    a.passes = (lines + at_once - 1) / at_once;
+    a.parts = 1;
+}
+constexpr int kRotateBlocks = 2048;        // workgroups of four waves, which go on with the next rows
+constexpr int kRotateGradBlocks = 1024;    // each leaves a sum of the weights' gradients
+
+}  // namespace
+
+extern "C" int32_t gbt_norm_rotate(gbt_ctx *ctx, const gbt_norm_rotate_params *params, const gbt_heads *q, const gbt_heads *k, const gbt_heads *v,
+                                   const gbt_heads *q_out, const gbt_heads *k_out, const gbt_heads *v_out) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, params, GBT_EINVAL, "NULL argument");
+    const gbt_norm_rotate_params &p = *params;
+    int32_t code;
+    const char *fault = rotate_fault(p, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    GBT_REQUIRE(ctx, !v == !v_out, GBT_EINVAL, "v and v_out: one without the other");
+    GBT_VIEW(ctx, q, p.rows);
+    GBT_VIEW(ctx, k, p.rows);
+    GBT_VIEW_OUT(ctx, q_out, p.rows, p.heads);
+    GBT_VIEW_OUT(ctx, k_out, p.out_rows, p.kv_heads);
+    if (v) {
+        GBT_VIEW(ctx, v, p.rows);
+        GBT_VIEW_OUT(ctx, v_out, p.out_rows, p.kv_heads);
+    }
+    if (p.rows == 0) return GBT_OK;
+    RotateArgs a;
+    fill(a, p, p.heads + p.kv_heads * (v ? 2 : 1));
+    a.q = view(q);
+    a.k = view(k);
+    a.q_out = view(q_out);
+    a.k_out = view(k_out);
+    if (v) {
+        a.v = view(v);
+        a.v_out = view(v_out);
+    }
+    const int64_t groups = (p.rows + a.row_group - 1) / a.row_group;
+    if (groups * a.passes <= 4 * kRotateBlocks) a.parts = a.passes;   // few rows: a wave for each of a row's passes
+    a.blocks = (int)std::min<int64_t>((groups * a.parts + 3) / 4, kRotateBlocks);
+    GBT_HIP(ctx, gbt_launch_norm_rotate(ctx->stream, a, p.dtype));
+    return GBT_OK;
+}
+
+extern "C" size_t gbt_norm_rotate_backward_workspace_bytes(const gbt_norm_rotate_params *params) {
+    int32_t code;
+    if (!params || rotate_fault(*params, &code)) return 0;
+    return (size_t)kRotateGradBlocks * 2 * kRotateDim * sizeof(float);
+}
+
+extern "C" int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_params *params, const gbt_heads *dq_out, const gbt_heads *dk_out,
+                                            const gbt_heads *q, const gbt_heads *k, const gbt_heads *dq, const gbt_heads *dk, float *dq_weight,
+                                            float *dk_weight, void *workspace, size_t workspace_bytes) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, params, GBT_EINVAL, "NULL argument");
+    const gbt_norm_rotate_params &p = *params;
+    int32_t code;
+    const char *fault = rotate_fault(p, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    GBT_REQUIRE(ctx, !p.store, GBT_EUNSUPPORTED, "the gradient of keys in a store");
+    GBT_VIEW(ctx, dq_out, p.rows);
+    GBT_VIEW(ctx, dk_out, p.rows);
+    GBT_VIEW(ctx, q, p.rows);
+    GBT_VIEW(ctx, k, p.rows);
+    GBT_VIEW_OUT(ctx, dq, p.rows, p.heads);
+    GBT_VIEW_OUT(ctx, dk, p.rows, p.kv_heads);
+    GBT_REQUIRE(ctx, dq_weight && dk_weight && (((uintptr_t)dq_weight | (uintptr_t)dk_weight) & 3u) == 0, GBT_EINVAL,
+                "dq_weight or dk_weight is NULL or not aligned");
+    const size_t need = gbt_norm_rotate_backward_workspace_bytes(params);
+    GBT_REQUIRE(ctx, workspace, GBT_EINVAL, "workspace is NULL");
+    GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    GBT_REQUIRE(ctx, ((uintptr_t)workspace & 15u) == 0, GBT_EINVAL, "workspace is not 16-byte aligned");
+    RotateArgs a;
+    fill(a, p, p.heads + p.kv_heads);
+    a.q = view(q);
+    a.k = view(k);
+    a.q_out = view(dq_out);
+    a.k_out = view(dk_out);
+    a.dq = view(dq);
+    a.dk = view(dk);
+    a.dq_weight = dq_weight;
+    a.dk_weight = dk_weight;
+    a.part = (float *)workspace;
+    a.blocks = (int)std::min<int64_t>(std::max<int64_t>(1, ((p.rows + a.row_group - 1) / a.row_group + 3) / 4), kRotateGradBlocks);
+    GBT_HIP(ctx, gbt_launch_norm_rotate_grad(ctx->stream, a, p.dtype));
+    return GBT_OK;
+}
+
+// --------------------------------------------------- orthogonalised updates --
+namespace {
+
+constexpr int64_t kMostMatrices = 1 << 16;
+constexpr int64_t kGroupBytes = (int64_t)2 << 30;   // of workspace that matrices taken together may need, where one alone does not need more
+
+const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
+    *code = GBT_EINVAL;
+    if (n < 0 || (n > 0 && !m)) return "n_matrices < 0 or matrices is NULL";
+    *code = GBT_EUNSUPPORTED;
+    if (n > kMostMatrices) return "more than 65536 matrices";
+    for (int64_t i = 0; i < n; ++i) {
+        *code = GBT_EUNSUPPORTED;
+        if (!known_type(m[i].dtype)) return "a matrix's dtype is none of GBT_F32, GBT_BF16, GBT_F16";
+        if (std::max(m[i].rows, m[i].cols) > (1 << 20) || std::min(m[i].rows, m[i].cols) > (1 << 15)) return "a matrix of more than 2^20 x 2^15";
+        *code = GBT_EINVAL;
+        if (m[i].rows < 0 || m[i].cols < 0) return "a matrix's rows or cols < 0";
+        if (!isfinite(m[i].scale)) return "a matrix's scale is not finite";
+        if (m[i].rows > 0 && m[i].cols > 0 && (!m[i].src || !m[i].dst || (((uintptr_t)m[i].src | (uintptr_t)m[i].dst) & (uintptr_t)(size_of(m[i].dtype) - 1))))
+            return "a matrix's src or dst is NULL or not aligned";
+    }
+    return nullptr;
+}
+
+// The matrices in groups that are worked on together.  What a group needs, and, into `list` where that is not NULL, its matrices as the kernels take them.
+struct OrthoGroup {
+    int64_t first, count;   // of the list: matrices with elements
+    int64_t pieces, fill_tiles, sym_tiles, full_tiles;
+    size_t bytes;
+};
+// The next group of matrices[*at ..]; false: there is none.
+bool next_group(const gbt_matrix *matrices, int64_t n, int64_t *at, int64_t *in_list, OrthoGroup *g, OrthoMatrix *list) {
+    *g = OrthoGroup{*in_list, 0, 0, 0, 0, 0, 0};
+    int64_t used = 0;
+    for (; *at < n; ++*at) {
+        const gbt_matrix &m = matrices[*at];
+        if (m.rows == 0 || m.cols == 0) continue;
+        OrthoMatrix o;
+        memset(&o, 0, sizeof o);
+        o.tall = m.rows > m.cols;
+        o.p = (int32_t)std::min(m.rows, m.cols);
+        o.w = (int32_t)std::max(m.rows, m.cols);
+        o.pp = (o.p + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
+        o.ww = (o.w + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
+        const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 4 * of_x + 2 * of_a;
+        const int64_t down = o.pp / kOrthoTile, across = o.ww / kOrthoTile, fill = 4 * down * across;
+        if (g->count > 0 && (used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) return true;
+        o.src = m.src;
+        o.dst = m.dst;
+        o.cols = m.cols;
+        o.dtype = m.dtype;
+        o.scale = m.scale;
+        o.pieces = (int32_t)((m.rows * m.cols + kOrthoPiece - 1) / kOrthoPiece);
+        o.piece_begin = g->pieces;
+        o.fill_begin = g->fill_tiles;
+        o.sym_begin = g->sym_tiles;
+        o.full_begin = g->full_tiles;
+        o.x[0] = used, o.x[1] = used + of_x, o.xt[0] = used + 2 * of_x, o.xt[1] = used + 3 * of_x;
+        o.a = used + 4 * of_x, o.b = o.a + of_a;
+        if (list) list[*in_list] = o;
+        ++*in_list;
+        ++g->count;
+        used += need;
+        g->pieces += o.pieces;
+        g->fill_tiles += fill;
+        g->sym_tiles += down * (down + 1) / 2;
+        g->full_tiles += down * across;
+        g->bytes = (size_t)used + gbt_align((size_t)g->pieces * sizeof(double));
+    }
+    return g->count > 0;
+}
+
+}  // namespace
+
+extern "C" size_t gbt_matrix_list_bytes(const gbt_matrix *matrices, int64_t n_matrices) {
+    int32_t code;
+    if (matrices_fault(matrices, n_matrices, &code)) return 0;
+    return std::max<size_t>(16, (size_t)n_matrices * sizeof(OrthoMatrix));
+}
+
+extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int64_t n_matrices, void *list_out, size_t list_bytes) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, list_out, GBT_EINVAL, "NULL argument");
+    GBT_REQUIRE(ctx, ((uintptr_t)list_out & 15u) == 0, GBT_EINVAL, "list_out is not 16-byte aligned");
+    int32_t code;
+    const char *fault = matrices_fault(matrices, n_matrices, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    const size_t need = gbt_matrix_list_bytes(matrices, n_matrices);
+    GBT_REQUIRE(ctx, list_bytes >= need, GBT_ENOMEM, "list of %zu bytes, %zu needed", list_bytes, need);
+    OrthoMatrix *table = new (std::nothrow) OrthoMatrix[(size_t)std::max<int64_t>(1, n_matrices)];
+    GBT_REQUIRE(ctx, table, GBT_ENOMEM, "no host memory for the list");
+    int64_t at = 0, count = 0;
+    OrthoGroup g;
+    while (next_group(matrices, n_matrices, &at, &count, &g, table)) {
+    }
+    int32_t st = GBT_OK;
+    // in pieces that the staging takes
+    for (int64_t i = 0; i < count && st == GBT_OK; i += 8192)
+        st = gbt_upload(ctx, table + i, (size_t)std::min<int64_t>(8192, count - i) * sizeof(OrthoMatrix), (OrthoMatrix *)list_out + i);
+    delete[] table;
+    return st;
+}
+
+extern "C" size_t gbt_orthogonalise_workspace_bytes(const gbt_matrix *matrices, int64_t n_matrices) {
+    int32_t code;
+    if (matrices_fault(matrices, n_matrices, &code)) return 0;
+    size_t most = 0;
+    int64_t at = 0, count = 0;
+    OrthoGroup g;
+    while (next_group(matrices, n_matrices, &at, &count, &g, nullptr)) most = std::max(most, g.bytes);
+    return most;
+}
+
+extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_matrix *matrices, int64_t n_matrices, int32_t steps, float a, float b, float c,
+                                     void *workspace, size_t workspace_bytes) {
+    if (!ctx) return GBT_EINVAL;
+    GBT_REQUIRE(ctx, list, GBT_EINVAL, "NULL argument");
+    GBT_REQUIRE(ctx, ((uintptr_t)list & 15u) == 0, GBT_EINVAL, "list is not 16-byte aligned");
+    int32_t code;
+    const char *fault = matrices_fault(matrices, n_matrices, &code);
+    GBT_REQUIRE(ctx, !fault, code, "%s", fault);
+    GBT_REQUIRE(ctx, steps >= 1 && steps <= 32, GBT_EINVAL, "steps outside 1..32");
+    // how large singular values can become, and the factor that they are multiplied by: what is kept in sixteen bits has to hold both
+    GBT_REQUIRE(ctx, isfinite(a) && isfinite(b) && isfinite(c), GBT_EINVAL, "a coefficient is not finite");
+    double most = 1.0, factor = 0.0;
+    for (int s = 0; s < steps; ++s) {
+        double next = 0.0;
+        for (int i = 0; i <= 4096; ++i) {
+            const double x = most * i / 4096.0, f = fabs((double)a + (double)b * x * x + (double)c * x * x * x * x);
+            factor = std::max(factor, f);
+            next = std::max(next, x * f);
+        }
+        most = next;
+        GBT_REQUIRE(ctx, most <= 4.0 && factor <= 64.0, GBT_EINVAL, "coefficients under which singular values pass 4 or their factors 64");
+    }
+    const size_t need = gbt_orthogonalise_workspace_bytes(matrices, n_matrices);
+    GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
+    GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    GBT_REQUIRE(ctx, ((uintptr_t)workspace & 255u) == 0 || need == 0, GBT_EINVAL, "workspace is not 256-byte aligned");
+    int64_t at = 0, count = 0;
+    OrthoGroup g;
+    while (next_group(matrices, n_matrices, &at, &count, &g, nullptr)) {
+        OrthoArgs o;
+        memset(&o, 0, sizeof o);
+        o.list = (const OrthoMatrix *)list + g.first;
+        o.count = (int)g.count;
+        o.workspace = (char *)workspace;
+        o.squares = (double *)((char *)workspace + g.bytes - gbt_align((size_t)g.pieces * sizeof(double)));
+        o.a = a;
+        o.b = b;
+        o.c = c;
+        GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
+        for (int s = 0; s < steps; ++s) {
+            o.from = s & 1;
+            o.last = s == steps - 1;
+            GBT_HIP(ctx, gbt_launch_ortho_step(ctx->stream, o, g.sym_tiles, g.full_tiles));
+        }
+    }
+    return GBT_OK;
+}

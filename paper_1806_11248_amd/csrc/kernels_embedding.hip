@@ -1,0 +1,443 @@
+// Rows of an embedding table by id, and the table's gradient.
+//
+// Lookup: out[t] = scale * table[id_t], one rounding.  Gradient: grad[v] = scale * (sum of dout[t] over the places t with id_t = v), a sum of rows that
+// lie anywhere, of which one id may have none and another a third of all.  Places are sorted by id (stable, by digits), and a group of lanes adds up
+// a chunk of them, however the ids are spread; sums of ids that go on in the next chunk are written aside in 32 bits and added up by a second launch in
+// the chunks' order.  No atomics on values: the same result on every run.  Bound: memory.
+#include "embedding.h"
+
+namespace {
+
+template <typename E>
+struct alignas(sizeof(E) * 8 < 16 ? sizeof(E) * 8 : 16) Eight {
+    E x[8];
+};
+
+// Eight elements of a row for each lane: next to each other where rows are aligned for it, otherwise as many apart as the group has lanes.
+struct Lane {
+    int first, step, width;   // element e is column first + e * step
+    __device__ Lane(const EmbedArgs &a, int slab, int lane) {
+        const int lanes = 1 << a.log_lanes;
+        width = a.width;
+        step = a.vector ? 1 : lanes;
+        first = slab * 8 * lanes + (a.vector ? lane * 8 : lane);
+    }
+    __device__ bool some() const { return first < width; }
+};
+
+template <typename E, bool kVector>
+__device__ __forceinline__ void read_eight(float (&x)[8], const E *row, const Lane &l) {
+    if (kVector) {
+        const Eight<E> v = *(const Eight<E> *)(row + l.first);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)v.x[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = l.first + e * l.step < l.width ? (float)row[l.first + e * l.step] : 0.0f;
+    }
+}
+template <typename E, bool kVector>
+__device__ __forceinline__ void write_eight(E *row, const float (&x)[8], const Lane &l) {
+    if (kVector) {
+        Eight<E> v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.x[e] = (E)x[e];
+        *(Eight<E> *)(row + l.first) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (l.first + e * l.step < l.width) row[l.first + e * l.step] = (E)x[e];
+    }
+}
+
+// The id as an unsigned number; whatever lies outside the table is n_rows.
+__device__ __forceinline__ uint32_t id_at(const void *ids, int id_bytes, int64_t i, int64_t n_rows) {
+    const uint64_t id = id_bytes == 4 ? (uint64_t)(int64_t)((const int32_t *)ids)[i] : ((const uint64_t *)ids)[i];
+    return (uint32_t)min(id, (uint64_t)n_rows);
+}
+
+// ------------------------------------------------------------------ lookup --
+template <typename T, typename O, bool kVector>
+__global__ __launch_bounds__(256) void embedding_kernel(EmbedArgs a) {
+    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
+    const int64_t groups = (int64_t)gridDim.x * (256 >> a.log_lanes);
+    for (int64_t i = (int64_t)blockIdx.x * (256 >> a.log_lanes) + (threadIdx.x >> a.log_lanes); i < a.n_ids; i += groups) {
+        const uint32_t id = id_at(a.ids, a.id_bytes, i, a.n_rows);
+        const T *row = (const T *)a.table + (int64_t)id * a.table_stride;
+        O *to = (O *)a.out + i * a.out_stride;
+#pragma unroll 4
+        for (int slab = 0; slab < a.slabs; ++slab) {
+            const Lane l(a, slab, lane);
+            if (!l.some()) break;
+            float x[8] = {};
+            if (id < a.n_rows) {
+                read_eight<T, kVector>(x, row, l);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= a.scale;
+            }
+            write_eight<O, kVector>(to, x, l);
+        }
+    }
+}
+
+// -------------------------------------------------------------------- sort --
+// One pass of a stable sort by digits: each workgroup's tile of ids is counted by digit in one launch, and placed in the next, in which every workgroup
+// adds up for itself what comes before its own.
+__device__ __forceinline__ uint32_t sort_key(const SortPass &p, int64_t i) { return p.ids ? id_at(p.ids, p.id_bytes, i, p.n_rows) : p.key_in[i]; }
+
+__global__ __launch_bounds__(512) void sort_count_kernel(SortPass p) {
+    __shared__ uint32_t count[kSortDigits];
+    const int digits = 1 << p.bits;
+    for (int d = threadIdx.x; d < digits; d += 512) count[d] = 0;
+    __syncthreads();
+    const int64_t end = min(p.n, (blockIdx.x + 1) * p.tile);
+    for (int64_t i = blockIdx.x * p.tile + threadIdx.x; i < end; i += 512) atomicAdd(&count[(sort_key(p, i) >> p.shift) & (digits - 1)], 1u);
+    __syncthreads();
+    for (int d = threadIdx.x; d < digits; d += 512) p.hist[(int64_t)blockIdx.x * digits + d] = count[d];
+}
+
+__global__ __launch_bounds__(512) void sort_place_kernel(SortPass p) {
+    __shared__ uint32_t total[kSortDigits], base[kSortDigits], count[8][kSortDigits], of_wave[8];
+    const int digits = 1 << p.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int d = threadIdx.x; d < digits; d += 512) total[d] = base[d] = 0;
+    __syncthreads();
+    // all tiles' counts of each digit, and those of the tiles before this one
+    const int stride = max(1, 512 / digits);
+    for (int d = threadIdx.x & (digits - 1); d < digits; d += 512) {
+        uint32_t all = 0, before = 0;
+#pragma unroll 8
+        for (int t = threadIdx.x / digits; t < p.tiles; t += stride) {
+            const uint32_t c = p.hist[(int64_t)t * digits + d];
+            all += c;
+            before += t < (int)blockIdx.x ? c : 0;
+        }
+        atomicAdd(&total[d], all);
+        atomicAdd(&base[d], before);
+    }
+    __syncthreads();
+    // and those of the smaller digits: two neighbouring digits a thread
+    const int d0 = 2 * threadIdx.x;
+    const uint32_t c0 = d0 < digits ? total[d0] : 0, c1 = d0 + 1 < digits ? total[d0 + 1] : 0;
+    uint32_t upto = c0 + c1;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const uint32_t x = __shfl_up(upto, s);
+        if (lane >= s) upto += x;
+    }
+    if (lane == 63) of_wave[wave] = upto;
+    __syncthreads();
+    uint32_t smaller = upto - c0 - c1;
+    for (int w = 0; w < wave; ++w) smaller += of_wave[w];
+    if (d0 < digits) base[d0] += smaller;
+    if (d0 + 1 < digits) base[d0 + 1] += smaller + c0;
+
+    const int64_t end = min(p.n, (blockIdx.x + 1) * p.tile);
+    for (int64_t first = blockIdx.x * p.tile; first < end; first += kSortItems) {
+        for (int d = threadIdx.x; d < 8 * digits; d += 512) count[d / digits][d & (digits - 1)] = 0;
+        __syncthreads();
+        // a wave ranks 512 ids in a row, 64 at a time
+        uint32_t key[8], pos[8], rank[8];
+        const int64_t mine = first + wave * 512 + lane;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (mine + r * 64 < end) {
+                key[r] = sort_key(p, mine + r * 64);
+                pos[r] = p.ids ? (uint32_t)(mine + r * 64) : p.pos_in[mine + r * 64];
+            }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const bool there = mine + r * 64 < end;
+            const uint32_t digit = there ? (key[r] >> p.shift) & (digits - 1) : 0;
+            uint64_t same = __ballot(there);
+            for (int b = 0; b < p.bits; ++b) {
+                const uint64_t with = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? with : ~with;
+            }
+            if (there) {
+                const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
+                volatile uint32_t *at = &count[wave][digit];
+                const uint32_t before = *at;
+                rank[r] = before + below;
+                if (below == 0) *at = before + __popcll(same);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        for (int d = threadIdx.x; d < digits; d += 512) {
+            uint32_t at = base[d];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const uint32_t c = count[w][d];
+                count[w][d] = at;
+                at += c;
+            }
+            base[d] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (mine + r * 64 < end) {
+                const uint32_t to = count[wave][(key[r] >> p.shift) & (digits - 1)] + rank[r];
+                p.key_out[to] = key[r];
+                p.pos_out[to] = pos[r];
+            }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- gradient --
+template <typename T, bool kVector>
+__device__ __forceinline__ void finish(const EmbedArgs &a, uint32_t id, float (&sum)[8], const Lane &l) {
+    T *row = (T *)a.table + (int64_t)id * a.table_stride;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] *= a.scale;
+    if (a.accumulate) {
+        float old[8];
+        read_eight<T, kVector>(old, row, l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += old[e];
+    }
+    write_eight<T, kVector>(row, sum, l);
+}
+
+// The first sorted place from `from` on whose key is at least `key`.
+__device__ __forceinline__ int64_t lower_bound(const uint32_t *keys, int64_t from, int64_t to, uint32_t key) {
+    while (from < to) {
+        const int64_t mid = (from + to) >> 1;
+        if (keys[mid] < key) from = mid + 1;
+        else to = mid;
+    }
+    return from;
+}
+
+// Workgroups before the first `sums` clear rows without places, the others add up chunks.
+template <typename T, typename O, bool kVector>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, unsigned sums) {
+    constexpr int kAhead = 8;   // rows under way
+    const float zeros[8] = {};
+    if (blockIdx.x >= sums) {
+        const int lane = threadIdx.x & 63;
+        const int64_t row0 = ((int64_t)(blockIdx.x - sums) * 4 + (threadIdx.x >> 6)) * a.zero_rows, row1 = min(a.n_rows, row0 + a.zero_rows);
+        if (row0 >= row1) return;
+        const int64_t lo = lower_bound(a.key, 0, a.n_ids, (uint32_t)row0), hi = lower_bound(a.key, lo, a.n_ids, (uint32_t)row1);
+        bool without = false;
+        if (row0 + lane < row1) {
+            const int64_t at = lower_bound(a.key, lo, hi, (uint32_t)(row0 + lane));
+            without = at >= hi || a.key[at] != (uint32_t)(row0 + lane);
+        }
+        const int lanes = 1 << a.log_lanes, group = lane >> a.log_lanes, groups = 64 >> a.log_lanes;
+        const uint64_t empty = __ballot(without);
+        for (int r = group; r < row1 - row0; r += groups)
+            if ((empty >> r) & 1)
+                for (int slab = 0; slab < a.slabs; ++slab) {
+                    const Lane l(a, slab, lane & (lanes - 1));
+                    if (l.some()) write_eight<T, kVector>((T *)a.table + (row0 + r) * a.table_stride, zeros, l);
+                }
+        return;
+    }
+    const int64_t unit = (int64_t)blockIdx.x * (256 >> a.log_lanes) + (threadIdx.x >> a.log_lanes);
+    const int chunk = (int)(unit / a.slabs), slab = (int)(unit % a.slabs);
+    const Lane l(a, slab, threadIdx.x & ((1 << a.log_lanes) - 1));
+    if (chunk >= a.chunks || !l.some()) return;
+    const int64_t first = (int64_t)chunk * a.chunk;
+    const int count = (int)min((int64_t)a.chunk, a.n_ids - first);
+    const uint32_t *keys = a.key + first, *places = a.pos + first;
+    const uint32_t none = (uint32_t)a.n_rows;
+    uint32_t run = keys[0];
+    if (run == none) return;
+    bool from_left = first > 0 && keys[-1] == run;
+    float *part = a.part + ((int64_t)chunk * 2 * a.slabs + slab) * (8 << a.log_lanes) + (threadIdx.x & ((1 << a.log_lanes) - 1)) * 8;
+    const int64_t to_second = (int64_t)a.slabs * (8 << a.log_lanes);
+    float sum[8] = {};
+    auto put_aside = [&](float *to) {
+        *(float4 *)to = float4{sum[0], sum[1], sum[2], sum[3]};
+        *(float4 *)(to + 4) = float4{sum[4], sum[5], sum[6], sum[7]};
+    };
+    for (int i = 0; i < count; i += kAhead) {
+        uint32_t key[kAhead];
+        float x[kAhead][8];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) key[u] = i + u < count ? keys[i + u] : none;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (key[u] != none) read_eight<O, kVector>(x[u], (const O *)a.out + (int64_t)places[i + u] * a.out_stride, l);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (key[u] == none) break;
+            if (key[u] != run) {
+                if (from_left) put_aside(part);
+                else finish<T, kVector>(a, run, sum, l);
+                from_left = false;
+                run = key[u];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += x[u][e];
+        }
+    }
+    if (from_left) put_aside(part);
+    else if (first + count < a.n_ids && keys[count] == run) put_aside(part + to_second);
+    else finish<T, kVector>(a, run, sum, l);
+}
+
+// By 256 threads, a group of lanes each an equal share of `count` rows, read by `row(i)` into eight floats; their sum to the first group, in a fixed order.
+template <typename Read>
+__device__ __forceinline__ void shared_sum(float (&sum)[8], int log_lanes, int count, float (*part)[8], Read read) {
+    const int groups = 256 >> log_lanes, group = threadIdx.x >> log_lanes, each = (count + groups - 1) / groups;
+    const int from = group * each, to = min(count, from + each);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+        float x[8];
+        read(x, i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    if (group == 0)
+        for (int g = 1; g < min(groups, (count + max(each, 1) - 1) / max(each, 1)); ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += part[(g << log_lanes) + threadIdx.x][e];
+}
+
+// The run that begins in a chunk and goes on, if there is one: its parts, in the chunks' order.
+template <typename T, bool kVector>
+__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a) {
+    __shared__ float shared[256][8];
+    const int chunk = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
+    const int64_t first = (int64_t)chunk * a.chunk, last = first + a.chunk - 1;   // a whole chunk, or it would have no next one
+    const uint32_t run = a.key[last];
+    if (run == (uint32_t)a.n_rows || a.key[last + 1] != run) return;
+    if (a.key[first] == run && first > 0 && a.key[first - 1] == run) return;
+    const int64_t end = lower_bound(a.key, last + 1, a.n_ids, run + 1);
+    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
+    const int64_t row = (int64_t)a.slabs * (8 << a.log_lanes), at = (int64_t)slab * (8 << a.log_lanes) + lane * 8;
+    float sum[8];
+    shared_sum(sum, a.log_lanes, (int)((end - 1) / a.chunk - chunk + 1), shared, [&](float (&x)[8], int i) {
+        const float *from = a.part + (int64_t)(chunk + i) * 2 * row + (i == 0 ? row : 0) + at;
+        const float4 lo = *(const float4 *)from, hi = *(const float4 *)(from + 4);
+        x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
+    });
+    const Lane l(a, slab, lane);
+    if (threadIdx.x < (1u << a.log_lanes) && l.some()) finish<T, kVector>(a, run, sum, l);
+}
+
+// Few ids: a workgroup owns some rows of the table, and looks through all ids for theirs.  One launch, nothing sorted.
+template <typename T, typename O, bool kVector>
+__global__ __launch_bounds__(256) void embedding_few_kernel(EmbedArgs a) {
+    __shared__ float shared[256][8];
+    __shared__ uint16_t place[kEmbedFewIds];
+    __shared__ uint8_t of_row[kEmbedFewIds];
+    __shared__ int of_wave[4];
+    __shared__ uint32_t present;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int slab = blockIdx.x % a.slabs;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.slabs) * a.zero_rows;
+    const int rows = (int)min((int64_t)a.zero_rows, a.n_rows - row0);
+    if (threadIdx.x == 0) present = 0;
+    int found = 0;
+    for (int first = 0; first < (int)a.n_ids; first += 256) {
+        const int i = first + threadIdx.x;
+        const int64_t r = i < (int)a.n_ids ? (int64_t)id_at(a.ids, a.id_bytes, i, a.n_rows) - row0 : -1;
+        const bool mine = r >= 0 && r < rows;
+        const uint64_t some = __ballot(mine);
+        if (lane == 0) of_wave[wave] = __popcll(some);
+        __syncthreads();
+        int at = found + __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0u));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            at += w < wave ? of_wave[w] : 0;
+            found += of_wave[w];
+        }
+        if (mine) {
+            place[at] = (uint16_t)i;
+            of_row[at] = (uint8_t)r;
+            atomicOr(&present, 1u << r);
+        }
+        __syncthreads();
+    }
+    __syncthreads();
+    const Lane l(a, slab, threadIdx.x & ((1 << a.log_lanes) - 1));
+    const float zeros[8] = {};
+    const uint32_t there = present;
+    if (!a.accumulate && l.some())
+        for (int r = threadIdx.x >> a.log_lanes; r < rows; r += 256 >> a.log_lanes)
+            if (!((there >> r) & 1)) write_eight<T, kVector>((T *)a.table + (row0 + r) * a.table_stride, zeros, l);
+    for (uint32_t left = there; left; left &= left - 1) {
+        const int r = __ffs(left) - 1;
+        float sum[8];
+        shared_sum(sum, a.log_lanes, found, shared, [&](float (&x)[8], int i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+            if (l.some() && of_row[i] == r) read_eight<O, kVector>(x, (const O *)a.out + (int64_t)place[i] * a.out_stride, l);
+        });
+        if (threadIdx.x < (1u << a.log_lanes) && l.some()) finish<T, kVector>(a, (uint32_t)(row0 + r), sum, l);
+    }
+}
+
+template <typename Launch>
+void by_type(int dtype, Launch launch) {
+    if (dtype == GBT_F32) launch(0.0f);
+    else if (dtype == GBT_BF16) launch((__bf16)0.0f);
+    else launch((_Float16)0.0f);
+}
+constexpr int64_t kMostWorkgroups = 1 << 16;   // of the lookup, which goes on with the next ids
+
+}  // namespace
+
+hipError_t gbt_launch_embedding(hipStream_t stream, const EmbedArgs &a) {
+    const int each = 256 >> a.log_lanes;
+    const unsigned grid = (unsigned)std::min<int64_t>((a.n_ids + each - 1) / each, kMostWorkgroups);
+    by_type(a.table_dtype, [&](auto t) {
+        by_type(a.out_dtype, [&](auto o) {
+            if (a.vector) embedding_kernel<decltype(t), decltype(o), true><<<grid, 256, 0, stream>>>(a);
+            else embedding_kernel<decltype(t), decltype(o), false><<<grid, 256, 0, stream>>>(a);
+        });
+    });
+    return hipGetLastError();
+}
+
+hipError_t gbt_launch_sort_pass(hipStream_t stream, const SortPass &p) {
+    sort_count_kernel<<<p.tiles, 512, 0, stream>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    sort_place_kernel<<<p.tiles, 512, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t gbt_launch_embedding_grad(hipStream_t stream, const EmbedArgs &a) {
+    const int64_t units = (int64_t)a.chunks * a.slabs, each = 256 >> a.log_lanes;
+    const unsigned sums = (unsigned)((units + each - 1) / each);
+    const int64_t waves = (a.n_rows + a.zero_rows - 1) / a.zero_rows;
+    const unsigned clears = a.accumulate ? 0 : (unsigned)((waves + 3) / 4);
+    by_type(a.table_dtype, [&](auto t) {
+        by_type(a.out_dtype, [&](auto o) {
+            if (a.vector) embedding_sum_kernel<decltype(t), decltype(o), true><<<sums + clears, 256, 0, stream>>>(a, sums);
+            else embedding_sum_kernel<decltype(t), decltype(o), false><<<sums + clears, 256, 0, stream>>>(a, sums);
+        });
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.chunks < 2) return e;
+    by_type(a.table_dtype, [&](auto t) {
+        const unsigned grid = (unsigned)((a.chunks - 1) * a.slabs);
+        if (a.vector) embedding_join_kernel<decltype(t), true><<<grid, 256, 0, stream>>>(a);
+        else embedding_join_kernel<decltype(t), false><<<grid, 256, 0, stream>>>(a);
+    });
+    return hipGetLastError();
+}
+
+hipError_t gbt_launch_embedding_grad_few(hipStream_t stream, const EmbedArgs &a) {
+    const unsigned grid = (unsigned)((a.n_rows + a.zero_rows - 1) / a.zero_rows * a.slabs);
+    by_type(a.table_dtype, [&](auto t) {
+        by_type(a.out_dtype, [&](auto o) {
+            if (a.vector) embedding_few_kernel<decltype(t), decltype(o), true><<<grid, 256, 0, stream>>>(a);
+            else embedding_few_kernel<decltype(t), decltype(o), false><<<grid, 256, 0, stream>>>(a);
+        });
+    });
+    return hipGetLastError();
+}

@@ -1,0 +1,30 @@
+// What the kernels of head norms with rotation and their entry points share.
+#pragma once
+
+#include "gbt_internal.h"
+#include "heads.h"
+
+struct RotateArgs {
+    AttnView q, k, v, q_out, k_out, v_out;   // v: data is NULL where there is none
+    AttnView dq, dk;                         // backward: the gradients of q_out and k_out are in q_out and k_out
+    const int64_t *q_ptr, *k_ptr;            // NULL: sequences of one length
+    const int32_t *k_len;                    // NULL: all of a slot
+    const void *positions;                   // NULL: the place in the sequence
+    int position_bytes;
+    const float *q_weight, *k_weight;        // NULL: ones
+    const double *turns;
+    int64_t rows, out_rows;                  // of q, k and v; of k_out and v_out
+    int n_seq, heads, kv_heads, lines;       // lines of a row: heads, key heads, and value heads to be copied
+    int dim, turned, halves, store, slots;   // slots: positions are counted in slots of k_ptr or k_len
+    float eps;
+    int log_lanes;                           // 1 << log_lanes lanes for a line, of which dim / 8 work
+    int row_group, passes;                   // rows a wave takes side by side, and how often it goes on to their next lines
+    int parts;                               // forward: a row's passes are shared by so many waves
+    int blocks;
+    float *part;                             // [blocks][2][128]: the weights' gradients
+    float *dq_weight, *dk_weight;
+};
+constexpr int kRotateDim = GBT_MAX_HEAD_DIM;
+
+hipError_t gbt_launch_norm_rotate(hipStream_t stream, const RotateArgs &a, int dtype);
+hipError_t gbt_launch_norm_rotate_grad(hipStream_t stream, const RotateArgs &a, int dtype);
