@@ -190,7 +190,7 @@ const char *rotate_fault(const gbt_norm_rotate_params &p, int32_t *code) {
     return nullptr;
 }
 
-void fill(RotateArgs &a, const gbt_norm_rotate_params &p, int lines) {
+void fill(RotateArgs &a, const gbt_norm_rotate_params &p) {
     memset(&a, 0, sizeof a);
     a.q_ptr = p.q_ptr;
     a.k_ptr = p.k_ptr;
@@ -205,7 +205,6 @@ void fill(RotateArgs &a, const gbt_norm_rotate_params &p, int lines) {
     a.n_seq = p.n_seq;
     a.heads = p.heads;
     a.kv_heads = p.kv_heads;
-    a.lines = lines;
     a.dim = p.head_dim;
     a.turned = p.turned;
     a.halves = p.halves != 0;
@@ -214,8 +213,7 @@ void fill(RotateArgs &a, const gbt_norm_rotate_params &p, int lines) {
     a.eps = p.eps;
     while ((8 << a.log_lanes) < p.head_dim) ++a.log_lanes;
     const int at_once = 64 >> a.log_lanes;
-    a.row_group = std::max(1, at_once / lines);
-    a.passes = (lines + at_once - 1) / at_once;
+    a.row_group = std::max(1, at_once / std::max(p.heads, p.kv_heads));
     a.parts = 1;
 }
 constexpr int kRotateBlocks = 2048;        // workgroups of four waves, which go on with the next rows
@@ -242,7 +240,7 @@ extern "C" int32_t gbt_norm_rotate(gbt_ctx *ctx, const gbt_norm_rotate_params *p
     }
     if (p.rows == 0) return GBT_OK;
     RotateArgs a;
-    fill(a, p, p.heads + p.kv_heads * (v ? 2 : 1));
+    fill(a, p);
     a.q = view(q);
     a.k = view(k);
     a.q_out = view(q_out);
@@ -252,7 +250,8 @@ extern "C" int32_t gbt_norm_rotate(gbt_ctx *ctx, const gbt_norm_rotate_params *p
         a.v_out = view(v_out);
     }
     const int64_t groups = (p.rows + a.row_group - 1) / a.row_group;
-    if (groups * a.passes <= 4 * kRotateBlocks) a.parts = a.passes;   // few rows: a wave for each of a row's passes
+    const int at_once = 64 >> a.log_lanes, passes = (p.heads + at_once - 1) / at_once + (v ? 2 : 1) * ((p.kv_heads + at_once - 1) / at_once);
+    if (groups * passes <= 4 * kRotateBlocks) a.parts = passes;   // few rows: a wave for each of a row's passes
     a.blocks = (int)std::min<int64_t>((groups * a.parts + 3) / 4, kRotateBlocks);
     GBT_HIP(ctx, gbt_launch_norm_rotate(ctx->stream, a, p.dtype));
     return GBT_OK;
@@ -287,7 +286,7 @@ extern "C" int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_
     GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     GBT_REQUIRE(ctx, ((uintptr_t)workspace & 15u) == 0, GBT_EINVAL, "workspace is not 16-byte aligned");
     RotateArgs a;
-    fill(a, p, p.heads + p.kv_heads);
+    fill(a, p);
     a.q = view(q);
     a.k = view(k);
     a.q_out = view(dq_out);

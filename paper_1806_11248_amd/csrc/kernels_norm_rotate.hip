@@ -90,6 +90,7 @@ template <typename E>
 struct Raw {   // a lane's eight elements as they lie in memory
     Four<E> lo, hi;
     __device__ void read(const char *row, const Part &p) { lo = *(const Four<E> *)(row + p.lo * 2), hi = *(const Four<E> *)(row + p.hi * 2); }
+    __device__ void write(char *row, const Part &p) const { *(Four<E> *)(row + p.lo * 2) = lo, *(Four<E> *)(row + p.hi * 2) = hi; }
     __device__ void to(float (&x)[8], bool some) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = some ? (float)lo.x[e] : 0.0f, x[4 + e] = some ? (float)hi.x[e] : 0.0f;
@@ -104,9 +105,64 @@ __device__ __forceinline__ void write_parts(char *row, const float (&x)[8], cons
     *(Four<E> *)(row + p.hi * 2) = hi;
 }
 
+// Over the 1 << LOG lanes of a line: neighbours, pairs, then mirrored within eight and sixteen, where all lanes of a half hold the same.
+template <int CTRL>
+__device__ __forceinline__ float plus_lane(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int LOG>
+__device__ __forceinline__ float line_sum(float x) {
+    if (LOG > 0) x = plus_lane<0xb1>(x);    // quad_perm 1, 0, 3, 2
+    if (LOG > 1) x = plus_lane<0x4e>(x);    // quad_perm 2, 3, 0, 1
+    if (LOG > 2) x = plus_lane<0x141>(x);   // row_half_mirror
+    if (LOG > 3) x = plus_lane<0x140>(x);   // row_mirror
+    return x;
+}
+
+// The heads of one tensor by a wave: lines of 1 << LOG lanes, as many at once as a wave has, of one row; where a row has fewer, of a few whole rows side by
+// side (kSide).  All but the lane's own offset is the same in all lanes, and so a scalar.
+template <int LOG, bool kSide>
+struct Stream {
+    static constexpr int kAtOnce = 64 >> LOG;
+    int heads, row_off, head;   // the lane's row among those side by side, and its head there, in the first pass
+    bool works;
+    __device__ Stream(const RotateArgs &a, int heads, const Part &part) : heads(heads) {
+        const int sub = (threadIdx.x & 63) >> LOG;
+        row_off = kSide ? sub / heads : 0;
+        head = kSide ? sub - row_off * heads : sub;
+        works = part.works && row_off < a.row_group;
+    }
+    __device__ int passes() const { return kSide ? 1 : (heads + kAtOnce - 1) / kAtOnce; }
+    __device__ int64_t offset(const AttnView &x) const { return (row_off * x.row + head * x.head) * 2; }
+    __device__ bool live(const RotateArgs &a, int64_t row0, int pass) const {
+        return works && (kSide ? row0 + row_off < a.rows : head + pass * kAtOnce < heads);
+    }
+};
+
+template <bool kSide>
+__device__ __forceinline__ Place place_for(const RotateArgs &a, int64_t row0, int row_off) {
+    const int64_t row = kSide ? min(row0 + row_off, a.rows - 1) : row0;
+    int seq = 0;
+    if (a.n_seq == 0) {
+    } else if (a.q_ptr) {
+        seq = sequence_of(a.q_ptr, a.n_seq, row0);
+        if (kSide)
+            for (int n = a.n_seq - seq; n > 1;) {
+                const bool behind = a.q_ptr[seq + n / 2] <= row;
+                seq += behind ? n / 2 : 0;
+                n = behind ? n - n / 2 : n / 2;
+            }
+        else seq = __builtin_amdgcn_readfirstlane(seq);
+    } else {
+        seq = (int)min(row / max((int64_t)1, a.rows / a.n_seq), (int64_t)a.n_seq - 1);
+    }
+    return place_of(a, row, seq);
+}
+
+// What a lane multiplies the two elements of each of its pairs by: the weight times the turn's cosine and sine.
 struct Turn {
     float cos[4], sin[4];
-    __device__ void set(const RotateArgs &a, const Part &p, const double (&turns)[4], int64_t position) {
+    __device__ void set(const Part &p, const double (&turns)[4], int64_t position) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const double whole = (double)position * turns[i];
@@ -115,201 +171,186 @@ struct Turn {
             sin[i] = p.turned ? __builtin_amdgcn_sinf(part) : 0.0f;
         }
     }
-    // Pairs are (0, 4), (1, 5) .. of the eight as halves, (0, 1), (2, 3) .. as neighbours; sign -1: back.
-    __device__ void apply(float (&x)[8], bool halves, float sign) const {
+};
+// Pairs are (0, 4), (1, 5) .. of a lane's eight as halves, (0, 1), (2, 3) .. as neighbours.
+template <bool kHalves>
+__device__ __forceinline__ constexpr int first_of(int pair) { return kHalves ? pair : 2 * pair; }
+template <bool kHalves>
+__device__ __forceinline__ constexpr int second_of(int pair) { return kHalves ? 4 + pair : 2 * pair + 1; }
+
+__device__ __forceinline__ void read_weight(float (&w)[8], const float *weight, const Part &part) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float &a = halves ? x[i] : x[2 * i], &b = halves ? x[4 + i] : x[2 * i + 1];
-            const float s = sign * sin[i], was = a;
-            a = fmaf(was, cos[i], -b * s);
-            b = fmaf(was, s, b * cos[i]);
+    for (int e = 0; e < 8; ++e) w[e] = part.works && weight ? weight[part.element(e)] : 1.0f;
+}
+__device__ __forceinline__ void read_turns(double (&turns)[4], const RotateArgs &a, const Part &part) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turns[i] = part.turned ? a.turns[part.pair + i] : 0.0;
+}
+
+// The heads of q or k of an item's rows.
+template <typename E, bool kHalves, int LOG, bool kSide, bool kStore>
+__device__ __forceinline__ void turn_heads(const RotateArgs &a, const Stream<LOG, kSide> &st, const Part &part, const AttnView &in, const AttnView &out,
+                                           int64_t row0, const Place &place, const Turn &turn, const float (&w)[8], int from, int to) {
+    constexpr int kAhead = 4;   // passes under way
+    float ac[4], as[4], bc[4], bs[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float wa = place.there ? w[first_of<kHalves>(i)] : 0.0f, wb = place.there ? w[second_of<kHalves>(i)] : 0.0f;
+        ac[i] = wa * turn.cos[i], as[i] = wa * turn.sin[i], bc[i] = wb * turn.cos[i], bs[i] = wb * turn.sin[i];
+    }
+    const float each = 1.0f / a.dim;
+    const char *src = in.data + row0 * in.row * 2;
+    // where a row goes is its own affair in a store, and with rows side by side the lane's
+    char *dst = out.data + (kStore ? (kSide ? max(place.store, (int64_t)0) : place.store) : row0) * out.row * 2;
+    const int64_t src_lane = st.offset(in), dst_lane = kStore ? st.head * out.head * 2 : st.offset(out);
+    for (int pass0 = from; pass0 < to; pass0 += kAhead) {
+        Raw<E> raw[kAhead];
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b)
+            if (pass0 + b < to && st.live(a, row0, pass0 + b)) raw[b].read(src + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            if (pass0 + b >= to) break;
+            const bool live = st.live(a, row0, pass0 + b);
+            float x[8], squares = 0.0f;
+            raw[b].to(x, live && place.there);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) squares = fmaf(x[e], x[e], squares);
+            const float mean = fmaf(line_sum<LOG>(squares), each, a.eps);
+            const float s = place.there ? __builtin_amdgcn_rsqf(mean) : 0.0f;
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float xa = x[first_of<kHalves>(i)] * s, xb = x[second_of<kHalves>(i)] * s;
+                y[first_of<kHalves>(i)] = fmaf(xa, ac[i], -xb * bs[i]);
+                y[second_of<kHalves>(i)] = fmaf(xa, as[i], xb * bc[i]);
+            }
+            if (live && (!kStore || place.store >= 0)) write_parts<E>(dst + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, y, part);
         }
     }
-};
-
-template <int LOG>
-__device__ __forceinline__ float line_sum(float x) {
-#pragma unroll
-    for (int s = 0; s < LOG; ++s) x += __shfl_xor(x, 1 << s);
-    return x;
+}
+template <typename E, int LOG, bool kSide, bool kStore>
+__device__ __forceinline__ void copy_heads(const RotateArgs &a, const Stream<LOG, kSide> &st, const Part &part, const AttnView &in, const AttnView &out,
+                                           int64_t row0, const Place &place, int from, int to) {
+    const char *src = in.data + row0 * in.row * 2;
+    char *dst = out.data + (kStore ? (kSide ? max(place.store, (int64_t)0) : place.store) : row0) * out.row * 2;
+    const int64_t src_lane = st.offset(in), dst_lane = kStore ? st.head * out.head * 2 : st.offset(out);
+    for (int pass = from; pass < to; ++pass)
+        if (st.live(a, row0, pass)) {
+            Raw<E> raw = {};
+            if (place.there) raw.read(src + pass * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
+            if (!kStore || place.store >= 0) raw.write(dst + pass * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, part);
+        }
 }
 
-// A wave's rows, and its lanes' places among them: lines of 1 << LOG lanes, of one row or of a few whole ones side by side.
-template <int LOG>
-struct Lines {
-    static constexpr int kAtOnce = 64 >> LOG;
-    int lane, sub, row_off, first;   // of the line; which of the wave's lines; its row; its line there in the first pass
-    __device__ Lines(const RotateArgs &a) {
-        lane = threadIdx.x & ((1 << LOG) - 1);
-        sub = (threadIdx.x & 63) >> LOG;
-        row_off = a.row_group > 1 ? sub / a.lines : 0;
-        first = a.row_group > 1 ? (row_off < a.row_group ? sub % a.lines : a.lines) : sub;
-    }
-};
-
-__device__ __forceinline__ Place my_place(const RotateArgs &a, int64_t row0, int row_off) {
-    const int64_t row = min(row0 + row_off, a.rows - 1);
-    int seq = 0;
-    if (a.n_seq == 0) {
-    } else if (a.q_ptr) {
-        seq = sequence_of(a.q_ptr, a.n_seq, row0);
-        if (a.row_group > 1)
-            for (int n = a.n_seq - seq; n > 1;) {
-                const bool behind = a.q_ptr[seq + n / 2] <= row;
-                seq += behind ? n / 2 : 0;
-                n = behind ? n - n / 2 : n / 2;
-            }
-    } else {
-        seq = (int)min(row / max((int64_t)1, a.rows / a.n_seq), (int64_t)a.n_seq - 1);
-    }
-    return place_of(a, row, seq);
-}
-
-// What a lane keeps for all its rows.
-template <int LOG>
-struct Fixed {
-    Lines<LOG> lines;
-    Part part;
+template <typename E, bool kHalves, int LOG, bool kSide, bool kStore>
+__global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a) {
+    const Part part(a, threadIdx.x & ((1 << LOG) - 1));
+    const Stream<LOG, kSide> of_q(a, a.heads, part), of_k(a, a.kv_heads, part);
     double turns[4];
     float wq[8], wk[8];
-    __device__ Fixed(const RotateArgs &a) : lines(a), part(a, lines.lane) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) turns[i] = part.turned ? a.turns[part.pair + i] : 0.0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            wq[e] = part.works && a.q_weight ? a.q_weight[part.element(e)] : 1.0f;
-            wk[e] = part.works && a.k_weight ? a.k_weight[part.element(e)] : 1.0f;
-        }
-    }
-};
-// Which head of what a line is.
-struct Line {
-    bool is_q, is_v;
-    int head;
-    __device__ Line(const RotateArgs &a, int line) {
-        is_q = line < a.heads, is_v = line >= a.heads + a.kv_heads;
-        head = line - (is_q ? 0 : is_v ? a.heads + a.kv_heads : a.heads);
-    }
-};
-__device__ __forceinline__ int64_t bytes_to(const AttnView &x, int64_t row, int head) { return (row * x.row + head * x.head) * 2; }
-
-template <typename E, bool kHalves, int LOG>
-__global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a) {
-    constexpr int kAhead = 4;   // lines under way
-    const Fixed<LOG> f(a);
-    const float each = 1.0f / a.dim;
+    read_turns(turns, a, part);
+    read_weight(wq, a.q_weight, part);
+    read_weight(wk, a.k_weight, part);
     const int64_t items = (a.rows + a.row_group - 1) / a.row_group * a.parts;
-    const int passes = (a.passes + a.parts - 1) / a.parts;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-        const int64_t row0 = item / a.parts * a.row_group, row = row0 + f.lines.row_off;
-        const bool mine = f.part.works && row < a.rows;
-        const int from = (int)(item % a.parts) * passes, to = min(a.passes, from + passes);
-        Place place;
+    const int q_passes = of_q.passes(), k_passes = of_k.passes(), all = q_passes + k_passes * (a.v.data ? 2 : 1);
+    const int64_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    for (int64_t item = wave; item < items; item += (int64_t)gridDim.x * 4) {
+        const int64_t row0 = item / a.parts * a.row_group;
+        // one of `parts` stretches of the row's passes: those of q, of k, of v
+        const int part_of = (int)(item % a.parts), first = (int)((int64_t)all * part_of / a.parts), last = (int)((int64_t)all * (part_of + 1) / a.parts);
+        Place place = place_for<kSide>(a, row0, of_q.row_off);
         Turn turn;
-        for (int pass0 = from; pass0 < to; pass0 += kAhead) {
-            Raw<E> raw[kAhead];
+        turn.set(part, turns, place.position);
+        if (first < q_passes)
+            turn_heads<E, kHalves, LOG, kSide, false>(a, of_q, part, a.q, a.q_out, row0, place, turn, wq, first, min(last, q_passes));
+        if (last <= q_passes) continue;
+        if (kSide) {   // a lane's key is not of its query's row
+            place = place_for<kSide>(a, row0, of_k.row_off);
+            turn.set(part, turns, place.position);
+        }
+        const int k_first = max(first - q_passes, 0), k_last = last - q_passes;
+        if (k_first < k_passes)
+            turn_heads<E, kHalves, LOG, kSide, kStore>(a, of_k, part, a.k, a.k_out, row0, place, turn, wk, k_first, min(k_last, k_passes));
+        if (k_last > k_passes) copy_heads<E, LOG, kSide, kStore>(a, of_k, part, a.v, a.v_out, row0, place, max(k_first - k_passes, 0), k_last - k_passes);
+    }
+}
+
+// The gradients of q or k of an item's rows, and what they add to the weight's.
+template <typename E, bool kHalves, int LOG, bool kSide>
+__device__ __forceinline__ void turn_back(const RotateArgs &a, const Stream<LOG, kSide> &st, const Part &part, const AttnView &in, const AttnView &back,
+                                          const AttnView &out, int64_t row0, const Place &place, const Turn &turn, const float (&w)[8], float (&dw)[8]) {
+    constexpr int kAhead = 2;
+    const float each = 1.0f / a.dim;
+    const char *src = in.data + row0 * in.row * 2, *of_out = back.data + row0 * back.row * 2;
+    char *dst = out.data + row0 * out.row * 2;
+    const int64_t src_lane = st.offset(in), back_lane = st.offset(back), dst_lane = st.offset(out);
+    const int passes = st.passes();
+    for (int pass0 = 0; pass0 < passes; pass0 += kAhead) {
+        Raw<E> of_x[kAhead], of_g[kAhead];
 #pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                const int line = f.lines.first + (pass0 + b) * Lines<LOG>::kAtOnce;
-                const Line l(a, line);
-                if (mine && pass0 + b < to && line < a.lines) {
-                    const AttnView &in = l.is_q ? a.q : l.is_v ? a.v : a.k;
-                    raw[b].read(in.data + bytes_to(in, row, l.head), f.part);
-                }
+        for (int b = 0; b < kAhead; ++b)
+            if (pass0 + b < passes && st.live(a, row0, pass0 + b)) {
+                of_x[b].read(src + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
+                of_g[b].read(of_out + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * back.head * 2 + back_lane, part);
             }
-            if (pass0 == from) {
-                place = my_place(a, row0, f.lines.row_off);
-                turn.set(a, f.part, f.turns, place.position);
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) {
+            if (pass0 + b >= passes) break;
+            const bool live = st.live(a, row0, pass0 + b);
+            float x[8], d[8], g[8], u[8], squares = 0.0f, along = 0.0f;
+            of_x[b].to(x, live && place.there);
+            of_g[b].to(d, live && place.there);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float da = d[first_of<kHalves>(i)], db = d[second_of<kHalves>(i)];
+                g[first_of<kHalves>(i)] = fmaf(da, turn.cos[i], db * turn.sin[i]);
+                g[second_of<kHalves>(i)] = fmaf(db, turn.cos[i], -da * turn.sin[i]);
             }
 #pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                if (pass0 + b >= to) break;
-                const int line = f.lines.first + (pass0 + b) * Lines<LOG>::kAtOnce;
-                const Line l(a, line);
-                const bool live = mine && line < a.lines;
-                float x[8], y[8], squares = 0.0f;
-                raw[b].to(x, live && place.there);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) squares = fmaf(x[e], x[e], squares);
-                const float s = 1.0f / sqrtf(fmaf(line_sum<LOG>(squares), each, a.eps));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = x[e] * s * (l.is_q ? f.wq[e] : f.wk[e]);
-                turn.apply(y, kHalves, 1.0f);
-                const int64_t to_row = l.is_q ? row : place.store;
-                const AttnView &out = l.is_q ? a.q_out : l.is_v ? a.v_out : a.k_out;
-                if (live && to_row >= 0) {
-                    if (!place.there) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = 0.0f;
-                    }
-                    write_parts<E>(out.data + bytes_to(out, to_row, l.head), l.is_v ? x : y, f.part);
-                }
+            for (int e = 0; e < 8; ++e) {
+                u[e] = g[e] * w[e];
+                squares = fmaf(x[e], x[e], squares);
+                along = fmaf(x[e], u[e], along);
             }
+            squares = line_sum<LOG>(squares);
+            along = line_sum<LOG>(along);
+            // (of no row: zeros, also where eps is zero)
+            const float s = live && place.there ? __builtin_amdgcn_rsqf(fmaf(squares, each, a.eps)) : 0.0f;
+            const float less = along * each * s * s;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                dw[e] = fmaf(g[e], x[e] * s, dw[e]);
+                u[e] = s * fmaf(x[e], -less, u[e]);
+            }
+            if (live) write_parts<E>(dst + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, u, part);
         }
     }
 }
 
-template <typename E, bool kHalves, int LOG>
+template <typename E, bool kHalves, int LOG, bool kSide>
 __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateArgs a) {
-    constexpr int kAhead = 2;
     __shared__ float shared[4][2][kRotateDim];
-    const Fixed<LOG> f(a);
-    float dwq[8] = {}, dwk[8] = {};
-    const float each = 1.0f / a.dim;
+    const Part part(a, threadIdx.x & ((1 << LOG) - 1));
+    const Stream<LOG, kSide> of_q(a, a.heads, part), of_k(a, a.kv_heads, part);
+    double turns[4];
+    float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
+    read_turns(turns, a, part);
+    read_weight(wq, a.q_weight, part);
+    read_weight(wk, a.k_weight, part);
     const int64_t items = (a.rows + a.row_group - 1) / a.row_group;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-        const int64_t row0 = item * a.row_group, row = row0 + f.lines.row_off;
-        const bool mine = f.part.works && row < a.rows;
-        Place place;
+    const int64_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    for (int64_t item = wave; item < items; item += (int64_t)gridDim.x * 4) {
+        const int64_t row0 = item * a.row_group;
+        Place place = place_for<kSide>(a, row0, of_q.row_off);
         Turn turn;
-        for (int pass0 = 0; pass0 < a.passes; pass0 += kAhead) {
-            Raw<E> of_x[kAhead], of_g[kAhead];
-#pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                const int line = f.lines.first + (pass0 + b) * Lines<LOG>::kAtOnce;
-                const Line l(a, line);
-                if (mine && line < a.lines) {
-                    const AttnView &in = l.is_q ? a.q : a.k, &back = l.is_q ? a.q_out : a.k_out;
-                    of_x[b].read(in.data + bytes_to(in, row, l.head), f.part);
-                    of_g[b].read(back.data + bytes_to(back, row, l.head), f.part);
-                }
-            }
-            if (pass0 == 0) {
-                place = my_place(a, row0, f.lines.row_off);
-                turn.set(a, f.part, f.turns, place.position);
-            }
-#pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                const int line = f.lines.first + (pass0 + b) * Lines<LOG>::kAtOnce;
-                const Line l(a, line);
-                const bool live = mine && line < a.lines;
-                float x[8], g[8], u[8];
-                of_x[b].to(x, live && place.there);
-                of_g[b].to(g, live && place.there);
-                turn.apply(g, kHalves, -1.0f);
-                float squares = 0.0f, along = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    u[e] = g[e] * (l.is_q ? f.wq[e] : f.wk[e]);
-                    squares = fmaf(x[e], x[e], squares);
-                    along = fmaf(x[e], u[e], along);
-                }
-                // (of no row: zeros, also where eps is zero)
-                squares = line_sum<LOG>(squares);
-                along = line_sum<LOG>(along);
-                const float s = live && place.there ? 1.0f / sqrtf(fmaf(squares, each, a.eps)) : 0.0f;
-                const float less = along * each * s * s;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float of_weight = g[e] * (x[e] * s);
-                    dwq[e] += l.is_q ? of_weight : 0.0f;
-                    dwk[e] += l.is_q ? 0.0f : of_weight;
-                    u[e] = s * fmaf(x[e], -less, u[e]);
-                }
-                const AttnView &out = l.is_q ? a.dq : a.dk;
-                if (live) write_parts<E>(out.data + bytes_to(out, row, l.head), u, f.part);
-            }
+        turn.set(part, turns, place.position);
+        turn_back<E, kHalves, LOG, kSide>(a, of_q, part, a.q, a.q_out, a.dq, row0, place, turn, wq, dwq);
+        if (kSide) {
+            place = place_for<kSide>(a, row0, of_k.row_off);
+            turn.set(part, turns, place.position);
         }
+        turn_back<E, kHalves, LOG, kSide>(a, of_k, part, a.k, a.k_out, a.dk, row0, place, turn, wk, dwk);
     }
     // the weights' gradients: over the lines of a wave, then its workgroup's waves
 #pragma unroll
@@ -318,9 +359,9 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateArgs a) {
             dwq[e] += __shfl_xor(dwq[e], 1 << s);
             dwk[e] += __shfl_xor(dwk[e], 1 << s);
         }
-        if (f.part.works && f.lines.sub == 0) {
-            shared[threadIdx.x >> 6][0][f.part.element(e)] = dwq[e];
-            shared[threadIdx.x >> 6][1][f.part.element(e)] = dwk[e];
+        if (part.works && (threadIdx.x & 63) >> LOG == 0) {
+            shared[threadIdx.x >> 6][0][part.element(e)] = dwq[e];
+            shared[threadIdx.x >> 6][1][part.element(e)] = dwk[e];
         }
     }
     __syncthreads();
@@ -356,26 +397,40 @@ void by_lanes(int log_lanes, Launch launch) {
     }
 }
 
+template <typename Launch>
+void by_flag(bool flag, Launch launch) {
+    if (flag) launch(std::true_type());
+    else launch(std::false_type());
+}
+
 }  // namespace
 
 hipError_t gbt_launch_norm_rotate(hipStream_t stream, const RotateArgs &a, int dtype) {
     by_lanes(a.log_lanes, [&](auto log) {
-        constexpr int L = decltype(log)::value;
-        if (dtype == GBT_BF16 && a.halves) norm_rotate_kernel<__bf16, true, L><<<a.blocks, 256, 0, stream>>>(a);
-        else if (dtype == GBT_BF16) norm_rotate_kernel<__bf16, false, L><<<a.blocks, 256, 0, stream>>>(a);
-        else if (a.halves) norm_rotate_kernel<_Float16, true, L><<<a.blocks, 256, 0, stream>>>(a);
-        else norm_rotate_kernel<_Float16, false, L><<<a.blocks, 256, 0, stream>>>(a);
+        by_flag(a.halves, [&](auto halves) {
+            by_flag(a.row_group > 1, [&](auto side) {
+                by_flag(a.store, [&](auto store) {
+                    constexpr int L = decltype(log)::value;
+                    constexpr bool H = decltype(halves)::value, S = decltype(side)::value, T = decltype(store)::value;
+                    if (dtype == GBT_BF16) norm_rotate_kernel<__bf16, H, L, S, T><<<a.blocks, 256, 0, stream>>>(a);
+                    else norm_rotate_kernel<_Float16, H, L, S, T><<<a.blocks, 256, 0, stream>>>(a);
+                });
+            });
+        });
     });
     return hipGetLastError();
 }
 
 hipError_t gbt_launch_norm_rotate_grad(hipStream_t stream, const RotateArgs &a, int dtype) {
     by_lanes(a.log_lanes, [&](auto log) {
-        constexpr int L = decltype(log)::value;
-        if (dtype == GBT_BF16 && a.halves) norm_rotate_grad_kernel<__bf16, true, L><<<a.blocks, 256, 0, stream>>>(a);
-        else if (dtype == GBT_BF16) norm_rotate_grad_kernel<__bf16, false, L><<<a.blocks, 256, 0, stream>>>(a);
-        else if (a.halves) norm_rotate_grad_kernel<_Float16, true, L><<<a.blocks, 256, 0, stream>>>(a);
-        else norm_rotate_grad_kernel<_Float16, false, L><<<a.blocks, 256, 0, stream>>>(a);
+        by_flag(a.halves, [&](auto halves) {
+            by_flag(a.row_group > 1, [&](auto side) {
+                constexpr int L = decltype(log)::value;
+                constexpr bool H = decltype(halves)::value, S = decltype(side)::value;
+                if (dtype == GBT_BF16) norm_rotate_grad_kernel<__bf16, H, L, S><<<a.blocks, 256, 0, stream>>>(a);
+                else norm_rotate_grad_kernel<_Float16, H, L, S><<<a.blocks, 256, 0, stream>>>(a);
+            });
+        });
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -14,12 +14,12 @@ struct RotateArgs {
     const float *q_weight, *k_weight;        // NULL: ones
     const double *turns;
     int64_t rows, out_rows;                  // of q, k and v; of k_out and v_out
-    int n_seq, heads, kv_heads, lines;       // lines of a row: heads, key heads, and value heads to be copied
+    int n_seq, heads, kv_heads;
     int dim, turned, halves, store, slots;   // slots: positions are counted in slots of k_ptr or k_len
     float eps;
     int log_lanes;                           // 1 << log_lanes lanes for a line, of which dim / 8 work
-    int row_group, passes;                   // rows a wave takes side by side, and how often it goes on to their next lines
-    int parts;                               // forward: a row's passes are shared by so many waves
+    int row_group;                           // rows that a wave takes side by side
+    int parts;                               // forward: a row's heads are shared by so many waves
     int blocks;
     float *part;                             // [blocks][2][128]: the weights' gradients
     float *dq_weight, *dk_weight;
