@@ -260,7 +260,7 @@ extern "C" int32_t gbt_norm_rotate(gbt_ctx *ctx, const gbt_norm_rotate_params *p
 extern "C" size_t gbt_norm_rotate_backward_workspace_bytes(const gbt_norm_rotate_params *params) {
     int32_t code;
     if (!params || rotate_fault(*params, &code)) return 0;
-    return (size_t)kRotateGradBlocks * 2 * kRotateDim * sizeof(float);
+    return (size_t)kRotateGradBlocks * kRotateDim * sizeof(float);
 }
 
 extern "C" int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_params *params, const gbt_heads *dq_out, const gbt_heads *dk_out,
@@ -296,7 +296,15 @@ extern "C" int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_
     a.dq_weight = dq_weight;
     a.dk_weight = dk_weight;
     a.part = (float *)workspace;
-    a.blocks = (int)std::min<int64_t>(std::max<int64_t>(1, ((p.rows + a.row_group - 1) / a.row_group + 3) / 4), kRotateGradBlocks);
+    // workgroups for q and for k, by their waves' passes
+    const int at_once = 64 >> a.log_lanes;
+    a.row_group = std::max(1, at_once / p.heads);
+    a.k_row_group = std::max(1, at_once / p.kv_heads);
+    const int64_t q_items = (p.rows + a.row_group - 1) / a.row_group, k_items = (p.rows + a.k_row_group - 1) / a.k_row_group;
+    const int64_t q_work = q_items * ((p.heads + at_once - 1) / at_once), k_work = k_items * ((p.kv_heads + at_once - 1) / at_once);
+    const int64_t q_most = std::max<int64_t>(1, (q_items + 3) / 4), k_most = std::max<int64_t>(1, (k_items + 3) / 4);
+    a.q_blocks = (int)std::min(q_most, std::max<int64_t>(1, std::min<int64_t>(kRotateGradBlocks - 1, kRotateGradBlocks * q_work / std::max<int64_t>(1, q_work + k_work))));
+    a.blocks = a.q_blocks + (int)std::min<int64_t>(k_most, kRotateGradBlocks - a.q_blocks);
     GBT_HIP(ctx, gbt_launch_norm_rotate_grad(ctx->stream, a, p.dtype));
     return GBT_OK;
 }

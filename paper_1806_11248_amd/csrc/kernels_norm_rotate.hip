@@ -126,11 +126,11 @@ struct Stream {
     static constexpr int kAtOnce = 64 >> LOG;
     int heads, row_off, head;   // the lane's row among those side by side, and its head there, in the first pass
     bool works;
-    __device__ Stream(const RotateArgs &a, int heads, const Part &part) : heads(heads) {
+    __device__ Stream(int heads, int row_group, const Part &part) : heads(heads) {
         const int sub = (threadIdx.x & 63) >> LOG;
         row_off = kSide ? sub / heads : 0;
         head = kSide ? sub - row_off * heads : sub;
-        works = part.works && row_off < a.row_group;
+        works = part.works && row_off < row_group;
     }
     __device__ int passes() const { return kSide ? 1 : (heads + kAtOnce - 1) / kAtOnce; }
     __device__ int64_t offset(const AttnView &x) const { return (row_off * x.row + head * x.head) * 2; }
@@ -246,7 +246,7 @@ __device__ __forceinline__ void copy_heads(const RotateArgs &a, const Stream<LOG
 template <typename E, bool kHalves, int LOG, bool kSide, bool kStore>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a) {
     const Part part(a, threadIdx.x & ((1 << LOG) - 1));
-    const Stream<LOG, kSide> of_q(a, a.heads, part), of_k(a, a.kv_heads, part);
+    const Stream<LOG, kSide> of_q(a.heads, a.row_group, part), of_k(a.kv_heads, a.row_group, part);
     double turns[4];
     float wq[8], wk[8];
     read_turns(turns, a, part);
@@ -328,47 +328,49 @@ __device__ __forceinline__ void turn_back(const RotateArgs &a, const Stream<LOG,
     }
 }
 
+// All rows' heads of q or of k by `blocks` workgroups, of which this one is number `block`.
 template <typename E, bool kHalves, int LOG, bool kSide>
-__global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateArgs a) {
-    __shared__ float shared[4][2][kRotateDim];
-    const Part part(a, threadIdx.x & ((1 << LOG) - 1));
-    const Stream<LOG, kSide> of_q(a, a.heads, part), of_k(a, a.kv_heads, part);
+__device__ __forceinline__ void turn_all_back(const RotateArgs &a, int heads, int row_group, const AttnView &in, const AttnView &back, const AttnView &out,
+                                              const float *weight, int block, int blocks, const Part &part, float (&dw)[8]) {
+    const Stream<LOG, kSide> st(heads, row_group, part);
     double turns[4];
-    float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
+    float w[8];
     read_turns(turns, a, part);
-    read_weight(wq, a.q_weight, part);
-    read_weight(wk, a.k_weight, part);
-    const int64_t items = (a.rows + a.row_group - 1) / a.row_group;
-    const int64_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    for (int64_t item = wave; item < items; item += (int64_t)gridDim.x * 4) {
-        const int64_t row0 = item * a.row_group;
-        Place place = place_for<kSide>(a, row0, of_q.row_off);
+    read_weight(w, weight, part);
+    const int64_t items = (a.rows + row_group - 1) / row_group;
+    for (int64_t item = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)); item < items; item += (int64_t)blocks * 4) {
+        const Place place = place_for<kSide>(a, item * row_group, st.row_off);
         Turn turn;
         turn.set(part, turns, place.position);
-        turn_back<E, kHalves, LOG, kSide>(a, of_q, part, a.q, a.q_out, a.dq, row0, place, turn, wq, dwq);
-        if (kSide) {
-            place = place_for<kSide>(a, row0, of_k.row_off);
-            turn.set(part, turns, place.position);
-        }
-        turn_back<E, kHalves, LOG, kSide>(a, of_k, part, a.k, a.k_out, a.dk, row0, place, turn, wk, dwk);
+        turn_back<E, kHalves, LOG, kSide>(a, st, part, in, back, out, item * row_group, place, turn, w, dw);
     }
-    // the weights' gradients: over the lines of a wave, then its workgroup's waves
+}
+
+// The first blocks take q, the others k: a wave's registers hold one weight and its gradient.
+template <typename E, bool kHalves, int LOG>
+__global__ __launch_bounds__(256, 4) void norm_rotate_grad_kernel(RotateArgs a) {
+    __shared__ float shared[4][kRotateDim];
+    const Part part(a, threadIdx.x & ((1 << LOG) - 1));
+    float dw[8] = {};
+    const int block = blockIdx.x - a.q_blocks;
+    if (block < 0) {
+        if (a.row_group > 1) turn_all_back<E, kHalves, LOG, true>(a, a.heads, a.row_group, a.q, a.q_out, a.dq, a.q_weight, blockIdx.x, a.q_blocks, part, dw);
+        else turn_all_back<E, kHalves, LOG, false>(a, a.heads, 1, a.q, a.q_out, a.dq, a.q_weight, blockIdx.x, a.q_blocks, part, dw);
+    } else {
+        const int blocks = a.blocks - a.q_blocks;
+        if (a.k_row_group > 1) turn_all_back<E, kHalves, LOG, true>(a, a.kv_heads, a.k_row_group, a.k, a.k_out, a.dk, a.k_weight, block, blocks, part, dw);
+        else turn_all_back<E, kHalves, LOG, false>(a, a.kv_heads, 1, a.k, a.k_out, a.dk, a.k_weight, block, blocks, part, dw);
+    }
+    // the weight's gradient: over the lines of a wave, then the workgroup's waves
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        for (int s = LOG; s < 6; ++s) {
-            dwq[e] += __shfl_xor(dwq[e], 1 << s);
-            dwk[e] += __shfl_xor(dwk[e], 1 << s);
-        }
-        if (part.works && (threadIdx.x & 63) >> LOG == 0) {
-            shared[threadIdx.x >> 6][0][part.element(e)] = dwq[e];
-            shared[threadIdx.x >> 6][1][part.element(e)] = dwk[e];
-        }
+#pragma unroll
+        for (int s = LOG; s < 6; ++s) dw[e] += __shfl_xor(dw[e], 1 << s);
+        if (part.works && (threadIdx.x & 63) >> LOG == 0) shared[threadIdx.x >> 6][part.element(e)] = dw[e];
     }
     __syncthreads();
-    const int which = threadIdx.x / kRotateDim, at = threadIdx.x % kRotateDim;
-    if (at < a.dim)
-        a.part[(int64_t)blockIdx.x * 2 * kRotateDim + threadIdx.x] =
-            (shared[0][which][at] + shared[1][which][at]) + (shared[2][which][at] + shared[3][which][at]);
+    const int at = threadIdx.x;
+    if (at < a.dim) a.part[(int64_t)blockIdx.x * kRotateDim + at] = (shared[0][at] + shared[1][at]) + (shared[2][at] + shared[3][at]);
 }
 
 // The workgroups' sums, eight elements of a weight by each workgroup, in 64 bits and a fixed order.
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(256) void norm_rotate_weights_kernel(RotateArgs a) 
     const int which = blockIdx.y, at = blockIdx.x * 8 + (threadIdx.x & 7), share = threadIdx.x >> 3;
     double sum = 0.0;
 #pragma unroll 8
-    for (int b = share; b < a.blocks; b += 32) sum += (double)a.part[((int64_t)b * 2 + which) * kRotateDim + at];
+    for (int b = (which ? a.q_blocks : 0) + share; b < (which ? a.blocks : a.q_blocks); b += 32) sum += (double)a.part[(int64_t)b * kRotateDim + at];
     shared[share][threadIdx.x & 7] = sum;
     __syncthreads();
     if (share == 0) {
@@ -424,12 +426,10 @@ hipError_t gbt_launch_norm_rotate(hipStream_t stream, const RotateArgs &a, int d
 hipError_t gbt_launch_norm_rotate_grad(hipStream_t stream, const RotateArgs &a, int dtype) {
     by_lanes(a.log_lanes, [&](auto log) {
         by_flag(a.halves, [&](auto halves) {
-            by_flag(a.row_group > 1, [&](auto side) {
-                constexpr int L = decltype(log)::value;
-                constexpr bool H = decltype(halves)::value, S = decltype(side)::value;
-                if (dtype == GBT_BF16) norm_rotate_grad_kernel<__bf16, H, L, S><<<a.blocks, 256, 0, stream>>>(a);
-                else norm_rotate_grad_kernel<_Float16, H, L, S><<<a.blocks, 256, 0, stream>>>(a);
-            });
+            constexpr int L = decltype(log)::value;
+            constexpr bool H = decltype(halves)::value;
+            if (dtype == GBT_BF16) norm_rotate_grad_kernel<__bf16, H, L><<<a.blocks, 256, 0, stream>>>(a);
+            else norm_rotate_grad_kernel<_Float16, H, L><<<a.blocks, 256, 0, stream>>>(a);
         });
     });
     const hipError_t e = hipGetLastError();

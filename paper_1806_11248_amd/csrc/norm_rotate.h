@@ -21,7 +21,8 @@ struct RotateArgs {
     int row_group;                           // rows that a wave takes side by side
     int parts;                               // forward: a row's heads are shared by so many waves
     int blocks;
-    float *part;                             // [blocks][2][128]: the weights' gradients
+    int k_row_group, q_blocks;               // backward: rows of k side by side; workgroups for q, the others take k
+    float *part;                             // [blocks][128]: the weights' gradients
     float *dq_weight, *dk_weight;
 };
 constexpr int kRotateDim = GBT_MAX_HEAD_DIM;
