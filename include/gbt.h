@@ -720,7 +720,7 @@ GBT_API int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int64_
 /*
  * list and matrices: the same as in gbt_matrix_list.  steps 1..32; coefficients under which no singular value of
  * 0..1 passes 4, nor its factor 64.  workspace [dev, 256-byte aligned]: gbt_orthogonalise_workspace_bytes, some
- * 16 bytes for each element and 8 for each of the products X X^T, of as many matrices as fit 2 GB (or one).
+ * 12 bytes for each element and 20 for each one of X X^T, of as many matrices as fit 2 GB (or one).
  * Asynchronous.
  */
 GBT_API size_t gbt_orthogonalise_workspace_bytes(const gbt_matrix *matrices, int64_t n_matrices);

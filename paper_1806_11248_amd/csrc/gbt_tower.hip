@@ -333,19 +333,38 @@ const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
     return nullptr;
 }
 
-// The matrices in groups that are worked on together.  What a group needs, and, into `list` where that is not NULL, its matrices as the kernels take them.
+// The matrices with elements in the order that they are worked on in: those of 32 bits first, and of either kind those with the most to do.
+struct OrthoOrder {
+    int32_t *at;
+    int64_t count = 0;
+    OrthoOrder(const gbt_matrix *m, int64_t n) : at(new (std::nothrow) int32_t[(size_t)std::max<int64_t>(1, n)]) {
+        if (!at) return;
+        for (int64_t i = 0; i < n; ++i)
+            if (m[i].rows > 0 && m[i].cols > 0) at[count++] = (int32_t)i;
+        std::sort(at, at + count, [m](int32_t x, int32_t y) {
+            const bool wide_x = m[x].dtype == GBT_F32, wide_y = m[y].dtype == GBT_F32;
+            if (wide_x != wide_y) return wide_x;
+            const int64_t of_x = m[x].rows * m[x].cols * std::min(m[x].rows, m[x].cols), of_y = m[y].rows * m[y].cols * std::min(m[y].rows, m[y].cols);
+            return of_x != of_y ? of_x > of_y : x < y;
+        });
+    }
+    ~OrthoOrder() { delete[] at; }
+    OrthoOrder(const OrthoOrder &) = delete;
+    OrthoOrder &operator=(const OrthoOrder &) = delete;
+};
+// Matrices of one kind that are worked on together, and what they need.
 struct OrthoGroup {
-    int64_t first, count;   // of the list: matrices with elements
+    int64_t first, count;   // of the order
+    bool wide;              // results of 32 bits
     int64_t pieces, fill_tiles, sym_tiles, full_tiles;
     size_t bytes;
 };
-// The next group of matrices[*at ..]; false: there is none.
-bool next_group(const gbt_matrix *matrices, int64_t n, int64_t *at, int64_t *in_list, OrthoGroup *g, OrthoMatrix *list) {
-    *g = OrthoGroup{*in_list, 0, 0, 0, 0, 0, 0};
+// The next group, from *at on; false: there is none.  Into `list` where that is not NULL, its matrices as the kernels take them.
+bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at, OrthoGroup *g, OrthoMatrix *list) {
+    *g = OrthoGroup{*at, 0, false, 0, 0, 0, 0, 0};
     int64_t used = 0;
-    for (; *at < n; ++*at) {
-        const gbt_matrix &m = matrices[*at];
-        if (m.rows == 0 || m.cols == 0) continue;
+    for (; *at < order.count; ++*at) {
+        const gbt_matrix &m = matrices[order.at[*at]];
         OrthoMatrix o;
         memset(&o, 0, sizeof o);
         o.tall = m.rows > m.cols;
@@ -353,9 +372,10 @@ bool next_group(const gbt_matrix *matrices, int64_t n, int64_t *at, int64_t *in_
         o.w = (int32_t)std::max(m.rows, m.cols);
         o.pp = (o.p + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
         o.ww = (o.w + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
-        const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 4 * of_x + 2 * of_a;
+        const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 3 * of_x + 5 * of_a;
         const int64_t down = o.pp / kOrthoTile, across = o.ww / kOrthoTile, fill = 4 * down * across;
-        if (g->count > 0 && (used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) return true;
+        const bool wide = m.dtype == GBT_F32;
+        if (g->count > 0 && (wide != g->wide || used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) return true;
         o.src = m.src;
         o.dst = m.dst;
         o.cols = m.cols;
@@ -366,10 +386,10 @@ bool next_group(const gbt_matrix *matrices, int64_t n, int64_t *at, int64_t *in_
         o.fill_begin = g->fill_tiles;
         o.sym_begin = g->sym_tiles;
         o.full_begin = g->full_tiles;
-        o.x[0] = used, o.x[1] = used + of_x, o.xt[0] = used + 2 * of_x, o.xt[1] = used + 3 * of_x;
-        o.a = used + 4 * of_x, o.b = o.a + of_a;
-        if (list) list[*in_list] = o;
-        ++*in_list;
+        o.x = used, o.xt[0] = used + of_x, o.xt[1] = used + 2 * of_x;
+        o.gram = used + 3 * of_x, o.factor = o.gram + of_a, o.both = o.factor + of_a, o.total[0] = o.both + of_a, o.total[1] = o.total[0] + of_a;
+        if (list) list[*at] = o;
+        g->wide = wide;
         ++g->count;
         used += need;
         g->pieces += o.pieces;
@@ -379,6 +399,12 @@ bool next_group(const gbt_matrix *matrices, int64_t n, int64_t *at, int64_t *in_
         g->bytes = (size_t)used + gbt_align((size_t)g->pieces * sizeof(double));
     }
     return g->count > 0;
+}
+// Steps that are taken on A alone before X is multiplied: an error of A grows by the factor's square with each.
+int steps_together(double factor, bool wide) {
+    int n = 1;
+    while (n < 8 && pow(factor, n + 1) <= 200.0 && pow(factor * factor, n) <= (wide ? 16.0 : 256.0)) ++n;
+    return n;
 }
 
 }  // namespace
@@ -400,14 +426,15 @@ extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int
     GBT_REQUIRE(ctx, list_bytes >= need, GBT_ENOMEM, "list of %zu bytes, %zu needed", list_bytes, need);
     OrthoMatrix *table = new (std::nothrow) OrthoMatrix[(size_t)std::max<int64_t>(1, n_matrices)];
     GBT_REQUIRE(ctx, table, GBT_ENOMEM, "no host memory for the list");
-    int64_t at = 0, count = 0;
+    const OrthoOrder order(matrices, n_matrices);
+    int32_t st = order.at ? GBT_OK : gbt_fail(ctx, GBT_ENOMEM, "no host memory for the list");
+    int64_t at = 0;
     OrthoGroup g;
-    while (next_group(matrices, n_matrices, &at, &count, &g, table)) {
+    while (st == GBT_OK && next_group(matrices, order, &at, &g, table)) {
     }
-    int32_t st = GBT_OK;
     // in pieces that the staging takes
-    for (int64_t i = 0; i < count && st == GBT_OK; i += 8192)
-        st = gbt_upload(ctx, table + i, (size_t)std::min<int64_t>(8192, count - i) * sizeof(OrthoMatrix), (OrthoMatrix *)list_out + i);
+    for (int64_t i = 0; i < order.count && st == GBT_OK; i += 8192)
+        st = gbt_upload(ctx, table + i, (size_t)std::min<int64_t>(8192, order.count - i) * sizeof(OrthoMatrix), (OrthoMatrix *)list_out + i);
     delete[] table;
     return st;
 }
@@ -416,9 +443,11 @@ extern "C" size_t gbt_orthogonalise_workspace_bytes(const gbt_matrix *matrices, 
     int32_t code;
     if (matrices_fault(matrices, n_matrices, &code)) return 0;
     size_t most = 0;
-    int64_t at = 0, count = 0;
+    const OrthoOrder order(matrices, n_matrices);
+    if (!order.at) return 0;
+    int64_t at = 0;
     OrthoGroup g;
-    while (next_group(matrices, n_matrices, &at, &count, &g, nullptr)) most = std::max(most, g.bytes);
+    while (next_group(matrices, order, &at, &g, nullptr)) most = std::max(most, g.bytes);
     return most;
 }
 
@@ -448,9 +477,11 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
     GBT_REQUIRE(ctx, workspace || need == 0, GBT_EINVAL, "workspace is NULL");
     GBT_REQUIRE(ctx, workspace_bytes >= need, GBT_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     GBT_REQUIRE(ctx, ((uintptr_t)workspace & 255u) == 0 || need == 0, GBT_EINVAL, "workspace is not 256-byte aligned");
-    int64_t at = 0, count = 0;
+    const OrthoOrder order(matrices, n_matrices);
+    GBT_REQUIRE(ctx, order.at, GBT_ENOMEM, "no host memory for the order of the matrices");
+    int64_t at = 0;
     OrthoGroup g;
-    while (next_group(matrices, n_matrices, &at, &count, &g, nullptr)) {
+    while (next_group(matrices, order, &at, &g, nullptr)) {
         OrthoArgs o;
         memset(&o, 0, sizeof o);
         o.list = (const OrthoMatrix *)list + g.first;
@@ -460,11 +491,28 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.a = a;
         o.b = b;
         o.c = c;
+        o.sym_tiles = g.sym_tiles;
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
-        for (int s = 0; s < steps; ++s) {
-            o.from = s & 1;
-            o.last = s == steps - 1;
-            GBT_HIP(ctx, gbt_launch_ortho_step(ctx->stream, o, g.sym_tiles, g.full_tiles));
+        auto product = [&](OrthoProduct of, int64_t tiles) { return gbt_launch_ortho_product(ctx->stream, o, of, tiles, ctx->num_cu); };
+        const int together = steps_together(factor, g.wide);
+        for (int s = 0; s < steps; s += together) {
+            const int n = std::min(together, steps - s);
+            GBT_HIP(ctx, product(kOrthoGram, g.sym_tiles));
+            for (int i = 0; i < n; ++i) {
+                o.first = i == 0;
+                GBT_HIP(ctx, product(kOrthoFactor, g.sym_tiles));
+                if (i < n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
+                    GBT_HIP(ctx, product(kOrthoBoth, o.first ? g.sym_tiles : 2 * g.sym_tiles));
+                    if (!o.first) o.total ^= 1;
+                    GBT_HIP(ctx, product(kOrthoNext, g.sym_tiles));
+                } else if (!o.first) {
+                    GBT_HIP(ctx, product(kOrthoTotal, g.sym_tiles));
+                    o.total ^= 1;
+                }
+            }
+            o.last = s + n == steps;
+            GBT_HIP(ctx, product(kOrthoApply, g.full_tiles));
+            o.xt ^= 1;
         }
     }
     return GBT_OK;

@@ -1,13 +1,18 @@
-// Updates of weight matrices, orthogonalised: X = G / |G|, then X <- (a I + b A + c A^2) X with A = X X^T, a few times, which takes all singular values
-// towards one.
+// Updates of weight matrices, orthogonalised: X = G / |G|, then X <- F X with F = a I + b A + c A^2, A = X X^T, a few times, which takes all singular
+// values towards one.
 //
-// Such steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
+// All F and A of one X commute: A after a step is F A F, so several steps are taken on the p x p matrices alone, and X is multiplied once by the product
+// of their factors.  That halves the work where X is wide, and costs nothing where it is square (a step on X is 1.5 w/p + 0.5 products of p x p x p, one on
+// A is 2; symmetric ones count half).  But an error of A grows by a^2 with each such step where singular values are small, so X is multiplied after two
+// steps where results have 32 bits, three where they have sixteen (gbt_tower.hip), and A taken anew.
+//
+// Steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
 // between products, and matrix instructions on 32 bits run at a sixteenth of the rate.  Everything between products is held in two float16 parts, high
 // and low, 22 bits in all, and a product is three on the matrix units: high * high + high * low + low * high, added up in 32 bits.  All values are held times
 // 2^8: X's entries lie around 1 / sqrt(w), and so their low parts stay among float16's normal numbers.  The errors left are those of 32-bit products.
 //
-// All products have both operands' rows along the sum: A = X X^T, A^2 = A A^T, and B X = B (X^T)^T, for which X's transpose is kept beside it.  The first
-// two are symmetric: their upper tiles are computed, and written twice.
+// All products have both operands' rows along the sum: X X^T, products of symmetric matrices, and F X = F (X^T)^T, for which X's transpose is kept beside it.
+// Of symmetric results the upper tiles are computed, and written twice.
 #include "ortho.h"
 #include "attention.h"
 
@@ -16,6 +21,15 @@ namespace {
 constexpr float kUp = 256.0f, kDown = 1.0f / 256.0f;   // of what is held in two parts
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// A matrix in two parts lies in blocks of 64 rows by 32 columns, a row of blocks after the other, each block's high parts and then its low ones, 4 KB each: a
+// tile's step along the sum is then whole 8 KB of memory, copied to LDS as they are, with the places of a row's sixteen-byte pieces as they are read there
+// (Tile<32>: piece c at place c ^ fold(row)).
+typedef Tile<32> Step;
+constexpr int kBlock = 64 * 32, kPair = 2 * kBlock;    // elements of a part, of both
+__device__ __forceinline__ int64_t place(int row, int col, int cols) {   // of a high part; its low part is kBlock further
+    return ((int64_t)(row >> 6) * (cols >> 5) + (col >> 5)) * kPair + (row & 63) * 32 + ((((col >> 3) & 3) ^ Step::fold(row & 63)) << 3) + (col & 7);
+}
 
 // The matrix whose tiles tile number `tile` belongs to, the same in all lanes; list[i].*begin ascends.
 __device__ __forceinline__ int matrix_of(const OrthoArgs &a, int64_t OrthoMatrix::*begin, int64_t tile) {
@@ -55,7 +69,7 @@ __global__ __launch_bounds__(256) void ortho_squares_kernel(OrthoArgs a) {
     const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::piece_begin, blockIdx.x)];
     const int64_t from = (blockIdx.x - m.piece_begin) * kOrthoPiece, to = min(from + kOrthoPiece, (int64_t)m.p * m.w);
     double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = from + threadIdx.x; i < to; i += 256) {
         const double x = (double)element(m, i);
         sum = fma(x, x, sum);
@@ -90,50 +104,66 @@ __global__ __launch_bounds__(256) void ortho_fill_kernel(OrthoArgs a) {
         tile[m.tall ? col : r][m.tall ? r : col] = x;
     }
     __syncthreads();
-    _Float16 *x = (_Float16 *)(a.workspace + m.x[0]), *xt = (_Float16 *)(a.workspace + m.xt[0]);
-    const int64_t plane = (int64_t)m.pp * m.ww;
-    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
-        _Float16 high, low;
-        split(tile[r][col], high, low);
-        const int64_t to = (int64_t)(i0 + r) * m.ww + j0 + col;
-        x[to] = high, x[plane + to] = low;
-        split(tile[col][r], high, low);
-        const int64_t tt = (int64_t)(j0 + r) * m.pp + i0 + col;
-        xt[tt] = high, xt[plane + tt] = low;
+    _Float16 *x = (_Float16 *)(a.workspace + m.x), *xt = (_Float16 *)(a.workspace + m.xt[0]);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {   // sixteen-byte pieces of X, then of its transpose
+        const int row = (threadIdx.x >> 3) + 32 * (n & 1), piece = (threadIdx.x & 7) * 8;
+        f16x8 high, low;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            split(n < 2 ? tile[row][piece + e] : tile[piece + e][row], h, l);
+            high[e] = h, low[e] = l;
+        }
+        _Float16 *to = n < 2 ? x + place(i0 + row, j0 + piece, m.ww) : xt + place(j0 + row, i0 + piece, m.pp);
+        *(f16x8 *)to = high;
+        *(f16x8 *)(to + kBlock) = low;
     }
 }
 
 // ---------------------------------------------------------------- products --
-// 128 x 128 of P Q^T by four waves of 64 x 64 each: rows of P and Q along the sum, `depth` of them, in two parts each.
-typedef Tile<32> Step;   // 64 rows, 32 along the sum
+// 128 x 128 of P Q^T by four waves of 64 x 64 each: two rows of blocks of P and of Q, 32 along the sum at a time, in kStages stages of 32 KB of LDS.
 struct Stage {
-    alignas(256) char p[2][2][Step::kBytes], q[2][2][Step::kBytes];   // [part][half]
+    alignas(256) char p[2][2][Step::kBytes], q[2][2][Step::kBytes];   // [row of blocks][part]
 };
+constexpr int kLoads = sizeof(Stage) / 4096;   // of sixteen bytes a lane, by each wave
 
-__device__ __forceinline__ void fetch_stage(Stage &s, const _Float16 *p, const _Float16 *q, int64_t p_plane, int64_t q_plane, int row, int k, int wave) {
+// p, q: this wave's quarter of a pair of blocks; rows of blocks are `row` bytes apart.
+__device__ __forceinline__ void fetch_stage(Stage &s, const char *p, const char *q, int64_t row, int wave, uint32_t lane_bytes) {
+    const uint32_t to = lds_address(&s) + wave * 2048;
 #pragma unroll
-    for (int part = 0; part < 2; ++part)
+    for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            Step::fetch(s.p[part][half], (const char *)(p + part * p_plane + (int64_t)half * 64 * row + k), (uint32_t)row * 2, 64, 32, wave);
-            Step::fetch(s.q[part][half], (const char *)(q + part * q_plane + (int64_t)half * 64 * row + k), (uint32_t)row * 2, 64, 32, wave);
+        for (int n = 0; n < 2; ++n) {
+            load_to_lds(to + half * 8192 + n * 1024, p + half * row + n * 1024, lane_bytes);
+            load_to_lds(to + 16384 + half * 8192 + n * 1024, q + half * row + n * 1024, lane_bytes);
         }
 }
 
-__device__ __forceinline__ void product(f32x16 (&acc)[2][2], Stage (&stage)[2], const _Float16 *p, const _Float16 *q, int64_t p_plane, int64_t q_plane,
-                                        int row, int depth) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Sums of more than 512 products each are added up in pieces of 512, so that their roundings are those of small numbers.
+constexpr int kPiece = 16;   // steps
+
+template <int kStages>
+__device__ __forceinline__ void product(f32x16 (&sum)[2][2], Stage *stage, const _Float16 *p, const _Float16 *q, int depth) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps = depth / 32;
+    const int64_t row = (int64_t)steps * kPair * 2;
+    const char *of_p = (const char *)p + wave * 2048, *of_q = (const char *)q + wave * 2048;
+    f32x16 acc[2][2] = {};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j) sum[i][j] = f32x16{};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    fetch_stage(stage[0], p, q, p_plane, q_plane, row, 0, wave);
-    for (int k = 0; k < depth; k += 32) {
-        tiles_ready();
-        const Stage &s = stage[(k >> 5) & 1];
-        if (k + 32 < depth) fetch_stage(stage[((k >> 5) & 1) ^ 1], p, q, p_plane, q_plane, row, k + 32, wave);
+    for (int s = 0; s < kStages - 1; ++s)
+        if (s < steps) fetch_stage(stage[s], of_p + s * (kPair * 2), of_q + s * (kPair * 2), row, wave, lane * 16);
+    int now = 0;
+    for (int k = 0; k < steps; ++k) {
+        // this step's loads are done, those of the steps behind it under way; and all waves are done with the step before
+        if (k + kStages - 1 <= steps) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads * (kStages - 2)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        const int next = k + kStages - 1, at = now == 0 ? kStages - 1 : now - 1;
+        if (next < steps) fetch_stage(stage[at], of_p + (int64_t)next * (kPair * 2), of_q + (int64_t)next * (kPair * 2), row, wave, lane * 16);
+        const Stage &s = stage[now];
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
             f16x8 x[2][2], y[2][2];
@@ -141,8 +171,8 @@ __device__ __forceinline__ void product(f32x16 (&acc)[2][2], Stage (&stage)[2], 
             for (int part = 0; part < 2; ++part)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    x[part][i] = Step::rows<F16>(s.p[part][wave >> 1], 32 * i, step, lane);
-                    y[part][i] = Step::rows<F16>(s.q[part][wave & 1], 32 * i, step, lane);
+                    x[part][i] = Step::rows<F16>(s.p[wave >> 1][part], 32 * i, step, lane);
+                    y[part][i] = Step::rows<F16>(s.q[wave & 1][part], 32 * i, step, lane);
                 }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -154,100 +184,120 @@ __device__ __forceinline__ void product(f32x16 (&acc)[2][2], Stage (&stage)[2], 
                 }
         }
         done_reading();
+        now = now + 1 == kStages ? 0 : now + 1;
+        if ((k & (kPiece - 1)) == kPiece - 1 || k == steps - 1) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    sum[i][j] += acc[i][j];
+                    acc[i][j] = f32x16{};
+                }
+        }
     }
 }
 
-// Tile number `at` of the upper half of n x n tiles: the last column first would be as good; columns j, rows i <= j.
-__device__ __forceinline__ void upper_tile(int64_t at, int &i, int &j) {
-    j = (int)((sqrt(8.0 * (double)at + 1.0) - 1.0) * 0.5);
-    while ((int64_t)(j + 1) * (j + 2) / 2 <= at) ++j;
-    while ((int64_t)j * (j + 1) / 2 > at) --j;
-    i = (int)(at - (int64_t)j * (j + 1) / 2);
+// Workgroups go to the eight XCDs in turn: each takes an eighth of a matrix's tiles in a row, and of these eight rows of tiles at a time, so that what it reads
+// stays in its L2.
+__device__ __forceinline__ int64_t of_xcd(int64_t at, int64_t tiles) {
+    const int64_t eighth = tiles / 8;
+    return at < eighth * 8 ? at % 8 * eighth + at / 8 : at;
+}
+__device__ __forceinline__ void full_tile(int64_t at, int down, int across, int &i, int &j) {
+    at = of_xcd(at, (int64_t)down * across);
+    const int band = (int)(at / (8 * across)), rows = min(8, down - 8 * band);
+    at -= (int64_t)band * 8 * across;
+    i = 8 * band + (int)(at % rows);
+    j = (int)(at / rows);
+}
+// Of n x n tiles those with i <= j.
+__device__ __forceinline__ void upper_tile(int64_t at, int n, int &i, int &j) {
+    at = of_xcd(at, (int64_t)n * (n + 1) / 2);
+    int first = 0;   // row of the band; a column j of it has min(8, j - first + 1) rows
+    for (;; first += 8) {
+        const int m = n - first;
+        const int64_t in_band = m >= 8 ? 36 + 8 * (int64_t)(m - 8) : (int64_t)m * (m + 1) / 2;
+        if (at < in_band) break;
+        at -= in_band;
+    }
+    if (at >= 36) {
+        i = first + (int)((at - 36) & 7);
+        j = first + 8 + (int)((at - 36) >> 3);
+    } else {
+        int c = 0;
+        while (at > c) at -= ++c;
+        i = first + (int)at;
+        j = first + c;
+    }
 }
 
-// Four values of rows i .. i + 3 of column j, into a matrix in two parts and into its transpose.
-__device__ __forceinline__ void put_four(_Float16 *m, int64_t plane, int row, _Float16 *t, int64_t t_plane, int t_row, int i, int j, const float (&v)[4],
-                                         bool direct) {
+// Sixteen-bit values of four rows in the column of each of four lanes, and back: the lane's own row's values of the four columns.
+struct Exchange {
+    int quad;
+    uint32_t sel0, sel1, keep, give;
+    __device__ Exchange(int lane) {
+        quad = lane & 3;
+        // bytes 0 to 3 are of what the lane keeps (its column, and that of two lanes on), 4 to 7 of what it is given
+        const bool odd = quad & 1, high = quad & 2;
+        sel0 = odd ? (high ? 0x03020706u : 0x01000504u) : (high ? 0x07060302u : 0x05040100u);
+        sel1 = odd ? (high ? 0x01000504u : 0x03020706u) : (high ? 0x05040100u : 0x07060302u);
+        keep = odd ? 0x07060302u : 0x05040100u;   // of (other, mine): both high halves, or both low ones
+        give = odd ? 0x05040100u : 0x07060302u;
+    }
+    __device__ f16x4 operator()(f16x4 v) const {
+        const uint64_t both = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = (uint32_t)both, hi = (uint32_t)(both >> 32), mine = quad & 2 ? hi : lo, theirs = quad & 2 ? lo : hi;
+        const uint32_t other = __builtin_amdgcn_mov_dpp(theirs, 0x4e, 0xf, 0xf, true);   // of the lane two on
+        const uint32_t kept = __builtin_amdgcn_perm(other, mine, keep);
+        const uint32_t given = __builtin_amdgcn_mov_dpp(__builtin_amdgcn_perm(other, mine, give), 0xb1, 0xf, 0xf, true);   // of the neighbour
+        return __builtin_bit_cast(f16x4, (uint64_t)__builtin_amdgcn_perm(given, kept, sel1) << 32 | __builtin_amdgcn_perm(given, kept, sel0));
+    }
+};
+
+// Four values of rows i .. i + 3 of column j into a matrix's transpose and, if `direct`, into the matrix.
+__device__ __forceinline__ void put_four(_Float16 *m, int cols, _Float16 *t, int t_cols, int i, int j, const float (&v)[4], bool direct, const Exchange &swap) {
     f16x4 high, low;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         _Float16 h, l;
         split(v[e], h, l);
         high[e] = h, low[e] = l;
-        if (direct) {
-            const int64_t at = (int64_t)(i + e) * row + j;
-            m[at] = h, m[plane + at] = l;
-        }
     }
-    const int64_t at = (int64_t)j * t_row + i;
-    *(f16x4 *)(t + at) = high;
-    *(f16x4 *)(t + t_plane + at) = low;
+    _Float16 *to = t + place(j, i, t_cols);
+    *(f16x4 *)to = high;
+    *(f16x4 *)(to + kBlock) = low;
+    if (direct) {
+        to = m + place(i + swap.quad, j & ~3, cols);
+        *(f16x4 *)to = swap(high);
+        *(f16x4 *)(to + kBlock) = swap(low);
+    }
 }
 
-__global__ __launch_bounds__(256, 2) void ortho_gram_kernel(OrthoArgs a) {
-    __shared__ Stage stage[2];
-    const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::sym_begin, blockIdx.x)];
+template <int kProduct, int kStages>
+__global__ __launch_bounds__(256, 2) void ortho_product_kernel(OrthoArgs a) {
+    extern __shared__ __attribute__((aligned(256))) char lds[];
+    constexpr bool kApply = kProduct == kOrthoApply;
+    const bool second = kProduct == kOrthoBoth && blockIdx.x >= a.sym_tiles;
+    const int64_t tile = blockIdx.x - (second ? a.sym_tiles : 0);
+    const OrthoMatrix &m = a.list[matrix_of(a, kApply ? &OrthoMatrix::full_begin : &OrthoMatrix::sym_begin, tile)];
+    const int down = m.pp / kOrthoTile, across = m.ww / kOrthoTile;
     int ti, tj;
-    upper_tile(blockIdx.x - m.sym_begin, ti, tj);
-    const _Float16 *x = (const _Float16 *)(a.workspace + m.x[a.from]);
-    const int64_t plane = (int64_t)m.pp * m.ww, to_plane = (int64_t)m.pp * m.pp;
+    if (kApply) full_tile(tile - m.full_begin, down, across, ti, tj);
+    else upper_tile(tile - m.sym_begin, down, ti, tj);
+    auto at = [&](int64_t offset) { return (_Float16 *)(a.workspace + offset); };
+    // a step's factor; the first one of some begins their product
+    const int64_t factor = a.first ? m.total[a.total] : m.factor;
+    const _Float16 *p = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor ? m.gram : kProduct == kOrthoNext ? m.both : kApply ? m.total[a.total] : factor);
+    const _Float16 *q = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor ? m.gram : kProduct == kOrthoNext ? factor : kApply ? m.xt[a.xt]
+                           : kProduct == kOrthoTotal || second ? m.total[a.total] : m.gram);
+    _Float16 *to = at(kProduct == kOrthoGram || kProduct == kOrthoNext ? m.gram : kProduct == kOrthoFactor ? factor : kApply ? m.x
+                      : kProduct == kOrthoTotal || second ? m.total[a.total ^ 1] : m.both);
+    _Float16 *to_t = kApply ? at(m.xt[a.xt ^ 1]) : to;
+    const int depth = kProduct == kOrthoGram ? m.ww : m.pp, cols = kApply ? m.ww : m.pp;
     f32x16 acc[2][2];
-    product(acc, stage, x + (int64_t)ti * kOrthoTile * m.ww, x + (int64_t)tj * kOrthoTile * m.ww, plane, plane, m.ww, m.ww);
-    _Float16 *to = (_Float16 *)(a.workspace + m.a);
+    product<kStages>(acc, (Stage *)lds, p + (int64_t)ti * 2 * (depth / 32) * kPair, q + (int64_t)tj * 2 * (depth / 32) * kPair, depth);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * i + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
-                const float v[4] = {acc[i][j][r] * kDown, acc[i][j][r + 1] * kDown, acc[i][j][r + 2] * kDown, acc[i][j][r + 3] * kDown};
-                put_four(to, to_plane, m.pp, to, to_plane, m.pp, row, col, v, ti != tj);
-            }
-}
-
-__global__ __launch_bounds__(256, 2) void ortho_factor_kernel(OrthoArgs a) {
-    __shared__ Stage stage[2];
-    const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::sym_begin, blockIdx.x)];
-    int ti, tj;
-    upper_tile(blockIdx.x - m.sym_begin, ti, tj);
-    const _Float16 *from = (const _Float16 *)(a.workspace + m.a);
-    const int64_t plane = (int64_t)m.pp * m.pp;
-    f32x16 acc[2][2];
-    product(acc, stage, from + (int64_t)ti * kOrthoTile * m.pp, from + (int64_t)tj * kOrthoTile * m.pp, plane, plane, m.pp, m.pp);
-    _Float16 *to = (_Float16 *)(a.workspace + m.b);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * i + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
-                // A is symmetric: its four values of this column lie side by side in the row of that number
-                const f16x4 high = *(const f16x4 *)(from + (int64_t)col * m.pp + row), low = *(const f16x4 *)(from + plane + (int64_t)col * m.pp + row);
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = fmaf(a.c * kDown, acc[i][j][r + e], a.b * ((float)high[e] + (float)low[e]));
-                    if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
-                }
-                put_four(to, plane, m.pp, to, plane, m.pp, row, col, v, ti != tj);
-            }
-}
-
-__global__ __launch_bounds__(256, 2) void ortho_apply_kernel(OrthoArgs a) {
-    __shared__ Stage stage[2];
-    const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::full_begin, blockIdx.x)];
-    const int64_t at = blockIdx.x - m.full_begin;
-    const int down = m.pp / kOrthoTile, ti = (int)(at % down), tj = (int)(at / down);
-    const _Float16 *b = (const _Float16 *)(a.workspace + m.b), *xt = (const _Float16 *)(a.workspace + m.xt[a.from]);
-    const int64_t plane = (int64_t)m.pp * m.ww;
-    f32x16 acc[2][2];
-    product(acc, stage, b + (int64_t)ti * kOrthoTile * m.pp, xt + (int64_t)tj * kOrthoTile * m.pp, (int64_t)m.pp * m.pp, plane, m.pp, m.pp);
-    _Float16 *to = (_Float16 *)(a.workspace + m.x[a.from ^ 1]), *to_t = (_Float16 *)(a.workspace + m.xt[a.from ^ 1]);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Exchange swap(lane);
     const float scale = m.scale * kDown;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -256,15 +306,40 @@ __global__ __launch_bounds__(256, 2) void ortho_apply_kernel(OrthoArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * i + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
-                float v[4] = {acc[i][j][r] * kDown, acc[i][j][r + 1] * kDown, acc[i][j][r + 2] * kDown, acc[i][j][r + 3] * kDown};
-                if (!a.last) {
-                    put_four(to, plane, m.ww, to_t, plane, m.pp, row, col, v, true);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * kDown;
+                if (kProduct == kOrthoFactor) {
+                    // A is symmetric: its four values of this column lie side by side in the row of that number
+                    const _Float16 *from = p + place(col, row, m.pp);
+                    const f16x4 high = *(const f16x4 *)from, low = *(const f16x4 *)(from + kBlock);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
+                        if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                    }
+                }
+                if (!kApply || !a.last) {
+                    put_four(to, cols, to_t, m.pp, row, col, v, kApply || ti != tj, swap);
                 } else if (col < m.w) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (row + e < m.p) put_element(m, m.tall ? (int64_t)col * m.cols + row + e : (int64_t)(row + e) * m.cols + col, v[e] * scale);
                 }
             }
+}
+
+template <int kProduct, int kStages>
+hipError_t launch_stages(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
+    static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_product_kernel<kProduct, kStages>, hipFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)sizeof(Stage));
+    if (ready != hipSuccess) return ready;
+    ortho_product_kernel<kProduct, kStages><<<(unsigned)tiles, 256, kStages * sizeof(Stage), stream>>>(a);
+    return hipGetLastError();
+}
+// Many tiles: two workgroups of two stages on a compute unit; few: one, whose loads are three steps ahead.
+template <int kProduct>
+hipError_t launch(hipStream_t stream, const OrthoArgs &a, int64_t tiles, int num_cu) {
+    return tiles <= num_cu ? launch_stages<kProduct, 4>(stream, a, tiles) : launch_stages<kProduct, 2>(stream, a, tiles);
 }
 
 }  // namespace
@@ -277,13 +352,13 @@ hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_
     return hipGetLastError();
 }
 
-hipError_t gbt_launch_ortho_step(hipStream_t stream, const OrthoArgs &a, int64_t sym_tiles, int64_t full_tiles) {
-    ortho_gram_kernel<<<(unsigned)sym_tiles, 256, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    ortho_factor_kernel<<<(unsigned)sym_tiles, 256, 0, stream>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    ortho_apply_kernel<<<(unsigned)full_tiles, 256, 0, stream>>>(a);
-    return hipGetLastError();
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int64_t tiles, int num_cu) {
+    switch (product) {
+        case kOrthoGram: return launch<kOrthoGram>(stream, a, tiles, num_cu);
+        case kOrthoFactor: return launch<kOrthoFactor>(stream, a, tiles, num_cu);
+        case kOrthoBoth: return launch<kOrthoBoth>(stream, a, tiles, num_cu);
+        case kOrthoTotal: return launch<kOrthoTotal>(stream, a, tiles, num_cu);
+        case kOrthoNext: return launch<kOrthoNext>(stream, a, tiles, num_cu);
+        default: return launch<kOrthoApply>(stream, a, tiles, num_cu);
+    }
 }

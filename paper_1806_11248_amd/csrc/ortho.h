@@ -12,12 +12,13 @@ struct OrthoMatrix {
     const void *src;
     void *dst;
     int64_t cols;                       // of G
-    int32_t p, w, pp, ww;               // ww, pp: padded
+    int32_t p, w, pp, ww;               // pp, ww: padded
     int32_t tall, dtype;                // tall: X is G's transpose
     float scale;
     int32_t pieces;                     // of its elements
     int64_t piece_begin;                // of the group's pieces
-    int64_t x[2], xt[2], a, b;          // bytes into the workspace: X and its transpose, twice, and the two p x p matrices; each a plane of high parts, then one of low parts
+    int64_t x, xt[2];                   // bytes into the workspace: X, its transpose (and the next one)
+    int64_t gram, factor, both, total[2];   // p x p: A, a step's factor F of it, F A, and the product of the factors so far (and the next one)
     int64_t fill_begin, sym_begin, full_begin;   // of the group's tiles: of X, of symmetric products' upper halves, of X
 };
 
@@ -27,8 +28,13 @@ struct OrthoArgs {
     char *workspace;
     double *squares;                    // [pieces of the group]
     float a, b, c;
-    int from, last;                     // which of the two X is read; whether this is the last step
+    int64_t sym_tiles;
+    int xt, total;                      // which of the two transposes is X's, which of the two products of factors the last one
+    int first, last;                    // first: the factor is the first of some, and begins their product; last: the result goes to dst
 };
 
+enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
+
 hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_t pieces, int64_t fill_tiles);
-hipError_t gbt_launch_ortho_step(hipStream_t stream, const OrthoArgs &a, int64_t sym_tiles, int64_t full_tiles);
+// The tiles of a product: a.sym_tiles, twice as many for kOrthoBoth, or those of X for kOrthoApply.
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int64_t tiles, int num_cu);

@@ -82,10 +82,10 @@ def test_matrices(b):
     assert L.gbt_matrix_list_bytes(*_matrices(b)) >= 16 and L.gbt_orthogonalise_workspace_bytes(*_matrices(b)) == 0
     assert L.gbt_matrix_list_bytes(*_matrices(b, ok, ok)) == 2 * L.gbt_matrix_list_bytes(*_matrices(b, ok))
     assert L.gbt_orthogonalise_workspace_bytes(*_matrices(b, (0, 0, 0, 5, 0, 1.0))) == 0                          # nothing of it is read
-    # 16 bytes an element and 8 for each of the products, of whole tiles
+    # 12 bytes an element and 20 for each of X X^T's, of whole tiles
     big = (64, 64, 1024, 4096, 1, 1.0)
     one = L.gbt_orthogonalise_workspace_bytes(*_matrices(b, big))
-    assert 16 * 1024 * 4096 + 8 * 1024 * 1024 <= one <= 1.05 * (16 * 1024 * 4096 + 8 * 1024 * 1024)
+    assert 12 * 1024 * 4096 + 20 * 1024 * 1024 <= one <= 1.05 * (12 * 1024 * 4096 + 20 * 1024 * 1024)
     # as many at a time as fit 2 GB
     assert one < L.gbt_orthogonalise_workspace_bytes(*_matrices(b, *[big] * 100)) <= 2 << 30 | 1 << 20
     huge = (64, 64, 20_000, 20_000, 1, 1.0)
