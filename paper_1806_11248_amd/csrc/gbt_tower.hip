@@ -373,7 +373,7 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.pp = (o.p + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
         o.ww = (o.w + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
         const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 3 * of_x + 5 * of_a;
-        const int64_t down = o.pp / kOrthoTile, across = o.ww / kOrthoTile, fill = 4 * down * across;
+        const int64_t down = o.pp / kOrthoTile, across = o.ww / kOrthoTile, fill = 2 * down * across;
         const bool wide = m.dtype == GBT_F32;
         if (g->count > 0 && (wide != g->wide || used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) return true;
         o.src = m.src;

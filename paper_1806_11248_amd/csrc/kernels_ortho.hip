@@ -63,17 +63,44 @@ __device__ __forceinline__ double block_sum(double x, double *part) {   // of 25
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+template <typename E>
+struct alignas(16) Vec {
+    E x[16 / sizeof(E)];
+};
+template <typename E>
+__device__ __forceinline__ double add_squares(const E *src, int n) {   // by 256 threads, each its own
+    constexpr int kVec = 16 / sizeof(E);
+    double sum[2] = {0.0, 0.0};
+    int i = 0;
+    if (((uintptr_t)src & 15) == 0) {
+#pragma unroll 4
+        for (int at = threadIdx.x; at < n / kVec; at += 256) {
+            const Vec<E> v = ((const Vec<E> *)src)[at];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const double x = (double)(float)v.x[e];
+                sum[e & 1] = fma(x, x, sum[e & 1]);
+            }
+        }
+        i = n / kVec * kVec;
+    }
+    for (i += threadIdx.x; i < n; i += 256) {
+        const double x = (double)(float)src[i];
+        sum[0] = fma(x, x, sum[0]);
+    }
+    return sum[0] + sum[1];
+}
+
 // Squares in 64 bits, where no float's leaves the range.
 __global__ __launch_bounds__(256) void ortho_squares_kernel(OrthoArgs a) {
     __shared__ double part[4];
     const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::piece_begin, blockIdx.x)];
-    const int64_t from = (blockIdx.x - m.piece_begin) * kOrthoPiece, to = min(from + kOrthoPiece, (int64_t)m.p * m.w);
-    double sum = 0.0;
-#pragma unroll 8
-    for (int64_t i = from + threadIdx.x; i < to; i += 256) {
-        const double x = (double)element(m, i);
-        sum = fma(x, x, sum);
-    }
+    const int64_t from = (blockIdx.x - m.piece_begin) * kOrthoPiece;
+    const int n = (int)min((int64_t)kOrthoPiece, (int64_t)m.p * m.w - from);
+    double sum;
+    if (m.dtype == GBT_F32) sum = add_squares((const float *)m.src + from, n);
+    else if (m.dtype == GBT_BF16) sum = add_squares((const __bf16 *)m.src + from, n);
+    else sum = add_squares((const _Float16 *)m.src + from, n);
     sum = block_sum(sum, part);
     if (threadIdx.x == 0) a.squares[blockIdx.x] = sum;
 }
@@ -83,50 +110,76 @@ __device__ __forceinline__ void split(float x, _Float16 &high, _Float16 &low) {
     low = (_Float16)(x - (float)high);
 }
 
-// X and its transpose in two parts, 64 x 64 elements a workgroup, padding included.
+// 64 x 64 elements of G from row r0 and column c0 on, zeros outside, times the factor.
+template <typename E>
+__device__ __forceinline__ void read_tile(float (&tile)[64][65], const OrthoMatrix &m, int r0, int c0, double factor) {
+    const int rows = (m.tall ? m.w : m.p) - r0, cols = (int)m.cols - c0;
+    const E *src = (const E *)m.src + (int64_t)r0 * m.cols + c0;
+    if (cols >= 64 && m.cols % 8 == 0 && ((uintptr_t)m.src & 15) == 0) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int row = (threadIdx.x >> 3) + 32 * n, piece = (threadIdx.x & 7) * 8;
+            Vec<E> v[sizeof(E) / 2] = {};
+            if (row < rows)
+#pragma unroll
+                for (int u = 0; u < (int)sizeof(E) / 2; ++u) v[u] = ((const Vec<E> *)(src + (int64_t)row * m.cols + piece))[u];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[row][piece + e] = (float)((double)(float)v[e / (16 / sizeof(E))].x[e % (16 / sizeof(E))] * factor);
+        }
+        return;
+    }
+    const int col = threadIdx.x & 63;
+#pragma unroll 4
+    for (int row = threadIdx.x >> 6; row < 64; row += 4)
+        tile[row][col] = row < rows && col < cols ? (float)((double)(float)src[(int64_t)row * m.cols + col] * factor) : 0.0f;
+}
+
+// X and its transpose in two parts, padding included: 64 rows and 128 columns of X a workgroup.
 __global__ __launch_bounds__(256) void ortho_fill_kernel(OrthoArgs a) {
     __shared__ double part[4];
-    __shared__ float tile[64][65];
+    __shared__ float tile[2][64][65];
     const OrthoMatrix &m = a.list[matrix_of(a, &OrthoMatrix::fill_begin, blockIdx.x)];
     double sum = 0.0;
+#pragma unroll 4
     for (int i = threadIdx.x; i < m.pieces; i += 256) sum += a.squares[m.piece_begin + i];
     const double norm = sqrt(block_sum(sum, part));
     // a norm of zero leaves zeros; one that is no finite number leaves none anywhere
     const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
     const int64_t at = blockIdx.x - m.fill_begin;
-    const int across = m.ww / 64, i0 = (int)(at / across) * 64, j0 = (int)(at % across) * 64;   // of X
-    const int col = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
-        // rows of memory
-        const int i = m.tall ? i0 + col : i0 + r, j = m.tall ? j0 + r : j0 + col;
-        float x = 0.0f;
-        if (i < m.p && j < m.w) x = (float)((double)element(m, m.tall ? (int64_t)j * m.cols + i : (int64_t)i * m.cols + j) * factor);
-        tile[m.tall ? col : r][m.tall ? r : col] = x;
+    const int across = m.ww / 128, i0 = (int)(at / across) * 64, j0 = (int)(at % across) * 128;   // of X
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int j = j0 + 64 * t, r = m.tall ? j : i0, c = m.tall ? i0 : j;
+        if (m.dtype == GBT_F32) read_tile<float>(tile[t], m, r, c, factor);
+        else if (m.dtype == GBT_BF16) read_tile<__bf16>(tile[t], m, r, c, factor);
+        else read_tile<_Float16>(tile[t], m, r, c, factor);
     }
     __syncthreads();
     _Float16 *x = (_Float16 *)(a.workspace + m.x), *xt = (_Float16 *)(a.workspace + m.xt[0]);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {   // sixteen-byte pieces of X, then of its transpose
-        const int row = (threadIdx.x >> 3) + 32 * (n & 1), piece = (threadIdx.x & 7) * 8;
+    for (int n = 0; n < 8; ++n) {   // sixteen-byte pieces of G's tile as it lies, then of its transpose
+        const int t = n >> 2, row = (threadIdx.x >> 3) + 32 * (n & 1), piece = (threadIdx.x & 7) * 8;
+        const bool along = (n >> 1) & 1;
         f16x8 high, low;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
-            split(n < 2 ? tile[row][piece + e] : tile[piece + e][row], h, l);
+            split(along ? tile[t][piece + e][row] : tile[t][row][piece + e], h, l);
             high[e] = h, low[e] = l;
         }
-        _Float16 *to = n < 2 ? x + place(i0 + row, j0 + piece, m.ww) : xt + place(j0 + row, i0 + piece, m.pp);
+        const int j = j0 + 64 * t;
+        _Float16 *to = along != (m.tall != 0) ? xt + place(j + row, i0 + piece, m.pp) : x + place(i0 + row, j + piece, m.ww);
         *(f16x8 *)to = high;
         *(f16x8 *)(to + kBlock) = low;
     }
 }
 
 // ---------------------------------------------------------------- products --
-// 128 x 128 of P Q^T by four waves of 64 x 64 each: two rows of blocks of P and of Q, 32 along the sum at a time, in kStages stages of 32 KB of LDS.
+// 128 x 128 of P Q^T by four waves of 64 x 64 each: two rows of blocks of P and of Q, 32 along the sum at a time, from one of two stages of 32 KB of LDS while
+// the other is loaded.  With two groups of four waves each takes half of the sum.
 struct Stage {
     alignas(256) char p[2][2][Step::kBytes], q[2][2][Step::kBytes];   // [row of blocks][part]
 };
-constexpr int kLoads = sizeof(Stage) / 4096;   // of sixteen bytes a lane, by each wave
 
 // p, q: this wave's quarter of a pair of blocks; rows of blocks are `row` bytes apart.
 __device__ __forceinline__ void fetch_stage(Stage &s, const char *p, const char *q, int64_t row, int wave, uint32_t lane_bytes) {
@@ -140,29 +193,18 @@ __device__ __forceinline__ void fetch_stage(Stage &s, const char *p, const char 
         }
 }
 
-// Sums of more than 512 products each are added up in pieces of 512, so that their roundings are those of small numbers.
+// Sums of many products are added up in pieces of 512, so that their roundings are those of small numbers, and in two halves, whether one group of waves
+// takes both or two take one each: the same result either way.
 constexpr int kPiece = 16;   // steps
 
-template <int kStages>
-__device__ __forceinline__ void product(f32x16 (&sum)[2][2], Stage *stage, const _Float16 *p, const _Float16 *q, int depth) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps = depth / 32;
-    const int64_t row = (int64_t)steps * kPair * 2;
-    const char *of_p = (const char *)p + wave * 2048, *of_q = (const char *)q + wave * 2048;
+// The sum of steps from .. to, a group's.
+__device__ __forceinline__ void product(f32x16 (&sum)[2][2], Stage (&stage)[2], const char *p, const char *q, int64_t row, int from, int to, int wave, int lane) {
     f32x16 acc[2][2] = {};
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) sum[i][j] = f32x16{};
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s)
-        if (s < steps) fetch_stage(stage[s], of_p + s * (kPair * 2), of_q + s * (kPair * 2), row, wave, lane * 16);
-    int now = 0;
-    for (int k = 0; k < steps; ++k) {
-        // this step's loads are done, those of the steps behind it under way; and all waves are done with the step before
-        if (k + kStages - 1 <= steps) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads * (kStages - 2)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        const int next = k + kStages - 1, at = now == 0 ? kStages - 1 : now - 1;
-        if (next < steps) fetch_stage(stage[at], of_p + (int64_t)next * (kPair * 2), of_q + (int64_t)next * (kPair * 2), row, wave, lane * 16);
+    fetch_stage(stage[0], p + (int64_t)from * (kPair * 2), q + (int64_t)from * (kPair * 2), row, wave, lane * 16);
+    for (int k = from; k < to; ++k) {
+        tiles_ready();
+        const int now = (k - from) & 1;
+        if (k + 1 < to) fetch_stage(stage[now ^ 1], p + (int64_t)(k + 1) * (kPair * 2), q + (int64_t)(k + 1) * (kPair * 2), row, wave, lane * 16);
         const Stage &s = stage[now];
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
@@ -174,18 +216,16 @@ __device__ __forceinline__ void product(f32x16 (&sum)[2][2], Stage *stage, const
                     x[part][i] = Step::rows<F16>(s.p[wave >> 1][part], 32 * i, step, lane);
                     y[part][i] = Step::rows<F16>(s.q[wave & 1][part], 32 * i, step, lane);
                 }
+            // low * high, high * low, high * high: four sums in turn, so that none waits for itself
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int of = 0; of < 3; ++of)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = F16::mma(x[1][i], y[0][j], acc[i][j]);
-                    acc[i][j] = F16::mma(x[0][i], y[1][j], acc[i][j]);
-                    acc[i][j] = F16::mma(x[0][i], y[0][j], acc[i][j]);
-                }
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = F16::mma(x[of == 0][i], y[of == 1][j], acc[i][j]);
         }
         done_reading();
-        now = now + 1 == kStages ? 0 : now + 1;
-        if ((k & (kPiece - 1)) == kPiece - 1 || k == steps - 1) {
+        if (((k - from) & (kPiece - 1)) == kPiece - 1 || k == to - 1) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -273,9 +313,10 @@ __device__ __forceinline__ void put_four(_Float16 *m, int cols, _Float16 *t, int
     }
 }
 
-template <int kProduct, int kStages>
-__global__ __launch_bounds__(256, 2) void ortho_product_kernel(OrthoArgs a) {
+template <int kProduct, int kGroups>
+__global__ __launch_bounds__(256 * kGroups, 2) void ortho_product_kernel(OrthoArgs a) {
     extern __shared__ __attribute__((aligned(256))) char lds[];
+    Stage(*stages)[2] = (Stage(*)[2])lds;
     constexpr bool kApply = kProduct == kOrthoApply;
     const bool second = kProduct == kOrthoBoth && blockIdx.x >= a.sym_tiles;
     const int64_t tile = blockIdx.x - (second ? a.sym_tiles : 0);
@@ -294,21 +335,53 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(OrthoArgs a) {
                       : kProduct == kOrthoTotal || second ? m.total[a.total ^ 1] : m.both);
     _Float16 *to_t = kApply ? at(m.xt[a.xt ^ 1]) : to;
     const int depth = kProduct == kOrthoGram ? m.ww : m.pp, cols = kApply ? m.ww : m.pp;
-    f32x16 acc[2][2];
-    product<kStages>(acc, (Stage *)lds, p + (int64_t)ti * 2 * (depth / 32) * kPair, q + (int64_t)tj * 2 * (depth / 32) * kPair, depth);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Exchange swap(lane);
-    const float scale = m.scale * kDown;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all & 3, group = all >> 2;
+    const int steps = depth / 32;
+    const int64_t row_bytes = (int64_t)steps * kPair * 2;
+    const char *of_p = (const char *)p + (int64_t)ti * 2 * row_bytes + wave * 2048, *of_q = (const char *)q + (int64_t)tj * 2 * row_bytes + wave * 2048;
+    f32x16 acc[2][2] = {}, rest[2][2] = {};
+    if (kGroups == 1) {
+        product(acc, stages[0], of_p, of_q, row_bytes, 0, steps / 2, wave, lane);
+        __syncthreads();
+        product(rest, stages[0], of_p, of_q, row_bytes, steps / 2, steps, wave, lane);
+    } else {
+        product(acc, stages[group], of_p, of_q, row_bytes, group * (steps / 2), (group + 1) * (steps / 2), wave, lane);
+        // each group finishes half of the rows, and gives the other one its sums of the other half
+        __syncthreads();
+        float *give = (float *)lds + (group * 4 + wave) * 64 * 32 + lane * 32, *get = (float *)lds + ((group ^ 1) * 4 + wave) * 64 * 32 + lane * 32;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * i + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
+                const int at = (j * 16 + r) ^ ((lane & 7) << 2);
+                *(f32x4 *)(give + at) = group ? f32x4{acc[0][j][r], acc[0][j][r + 1], acc[0][j][r + 2], acc[0][j][r + 3]}
+                                              : f32x4{acc[1][j][r], acc[1][j][r + 1], acc[1][j][r + 2], acc[1][j][r + 3]};
+            }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 x = *(const f32x4 *)(get + ((j * 16 + r) ^ ((lane & 7) << 2)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    rest[0][j][r + e] = x[e];
+                    acc[0][j][r + e] = group ? acc[1][j][r + e] : acc[0][j][r + e];
+                }
+            }
+    }
+    const Exchange swap(lane);
+    const float scale = m.scale * kDown;
+#pragma unroll
+    for (int i = 0; i < 2 / kGroups; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * (i + group) + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * kDown;
+                for (int e = 0; e < 4; ++e) v[e] = (acc[i][j][r + e] + rest[i][j][r + e]) * kDown;
                 if (kProduct == kOrthoFactor) {
                     // A is symmetric: its four values of this column lie side by side in the row of that number
                     const _Float16 *from = p + place(col, row, m.pp);
@@ -329,17 +402,18 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(OrthoArgs a) {
             }
 }
 
-template <int kProduct, int kStages>
-hipError_t launch_stages(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
-    static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_product_kernel<kProduct, kStages>, hipFuncAttributeMaxDynamicSharedMemorySize, kStages * (int)sizeof(Stage));
+template <int kProduct, int kGroups>
+hipError_t launch_groups(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
+    constexpr int kLds = kGroups * 2 * (int)sizeof(Stage);
+    static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_product_kernel<kProduct, kGroups>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (ready != hipSuccess) return ready;
-    ortho_product_kernel<kProduct, kStages><<<(unsigned)tiles, 256, kStages * sizeof(Stage), stream>>>(a);
+    ortho_product_kernel<kProduct, kGroups><<<(unsigned)tiles, 256 * kGroups, kLds, stream>>>(a);
     return hipGetLastError();
 }
-// Many tiles: two workgroups of two stages on a compute unit; few: one, whose loads are three steps ahead.
+// Few tiles: two groups of waves, as the steps that follow one another are what counts.
 template <int kProduct>
 hipError_t launch(hipStream_t stream, const OrthoArgs &a, int64_t tiles, int num_cu) {
-    return tiles <= num_cu ? launch_stages<kProduct, 4>(stream, a, tiles) : launch_stages<kProduct, 2>(stream, a, tiles);
+    return tiles <= 2 * num_cu ? launch_groups<kProduct, 2>(stream, a, tiles) : launch_groups<kProduct, 1>(stream, a, tiles);
 }
 
 }  // namespace
