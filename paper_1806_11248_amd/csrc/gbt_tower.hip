@@ -352,16 +352,62 @@ struct OrthoOrder {
     OrthoOrder(const OrthoOrder &) = delete;
     OrthoOrder &operator=(const OrthoOrder &) = delete;
 };
+int64_t tiles_of(int64_t side) { return (side + kOrthoTile - 1) / kOrthoTile; }
+
+enum OrthoTiles { kTilesGram, kTilesSym, kTilesFull };   // of X X^T; of products of symmetric matrices; of F X
+
+// The tiles of the matrices order.at[first .. first + count) (of symmetric results the upper halves) in the order of a launch's workgroups; their number,
+// with gaps.  Into `out` where that is not NULL.
+//
+// Workgroups go to the eight XCDs in turn, and tiles of one matrix share what they read.  So a matrix goes to one XCD, or, where that would leave others
+// idle, in parts of at least eight tiles and a hundred-and-twenty-eighth of all the work, each to the XCD with the least so far, the largest matrices first.
+// Of a matrix, eight rows of tiles at a time, column by column.
+int64_t lay_tiles(const gbt_matrix *matrices, const OrthoOrder &order, int64_t first, int64_t count, OrthoTiles kind, OrthoTile *out) {
+    const bool full = kind == kTilesFull;
+    int64_t down, across, tiles, depth;
+    auto look = [&](int64_t i) {
+        const gbt_matrix &m = matrices[order.at[first + i]];
+        const int64_t p = tiles_of(std::min(m.rows, m.cols)), w = tiles_of(std::max(m.rows, m.cols));
+        down = p, across = full ? w : p, depth = kind == kTilesGram ? w : p;
+        tiles = full ? p * w : p * (p + 1) / 2;
+    };
+    double all = 0.0, load[8] = {};
+    int64_t used[8] = {};
+    for (int64_t i = 0; i < count; ++i) {
+        look(i);
+        all += (double)tiles * (double)depth;
+    }
+    for (int64_t i = 0; i < count; ++i) {
+        look(i);
+        const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, tiles / 8), (int64_t)ceil(128.0 * (double)tiles * (double)depth / all)));
+        int64_t next = 0, part = -1;
+        int xcd = 0;
+        for (int64_t band = 0; band < down; band += 8)
+            for (int64_t j = full ? 0 : band; j < across; ++j)
+                for (int64_t r = band; r < std::min(band + 8, full ? down : std::min(down, j + 1)); ++r, ++next) {
+                    if (next * parts / tiles != part) {
+                        part = next * parts / tiles;
+                        xcd = (int)(std::min_element(load, load + 8) - load);
+                    }
+                    if (out) out[used[xcd] * 8 + xcd] = OrthoTile{(int32_t)i, (int16_t)r, (int16_t)j};
+                    ++used[xcd];
+                    load[xcd] += (double)depth;
+                }
+    }
+    return *std::max_element(used, used + 8) * 8;
+}
+
 // Matrices of one kind that are worked on together, and what they need.
 struct OrthoGroup {
     int64_t first, count;   // of the order
     bool wide;              // results of 32 bits
-    int64_t pieces, fill_tiles, sym_tiles, full_tiles;
+    int64_t pieces, fill_tiles, tiles[3];   // tiles: by OrthoTiles
     size_t bytes;
 };
 // The next group, from *at on; false: there is none.  Into `list` where that is not NULL, its matrices as the kernels take them.
 bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at, OrthoGroup *g, OrthoMatrix *list) {
-    *g = OrthoGroup{*at, 0, false, 0, 0, 0, 0, 0};
+    *g = OrthoGroup{};
+    g->first = *at;
     int64_t used = 0;
     for (; *at < order.count; ++*at) {
         const gbt_matrix &m = matrices[order.at[*at]];
@@ -370,12 +416,12 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.tall = m.rows > m.cols;
         o.p = (int32_t)std::min(m.rows, m.cols);
         o.w = (int32_t)std::max(m.rows, m.cols);
-        o.pp = (o.p + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
-        o.ww = (o.w + kOrthoTile - 1) / kOrthoTile * kOrthoTile;
+        const int64_t down = tiles_of(o.p), across = tiles_of(o.w), fill = 2 * down * across;
+        o.pp = (int32_t)down * kOrthoTile;
+        o.ww = (int32_t)across * kOrthoTile;
         const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 3 * of_x + 5 * of_a;
-        const int64_t down = o.pp / kOrthoTile, across = o.ww / kOrthoTile, fill = 2 * down * across;
         const bool wide = m.dtype == GBT_F32;
-        if (g->count > 0 && (wide != g->wide || used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) return true;
+        if (g->count > 0 && (wide != g->wide || used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) break;
         o.src = m.src;
         o.dst = m.dst;
         o.cols = m.cols;
@@ -384,8 +430,6 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.pieces = (int32_t)((m.rows * m.cols + kOrthoPiece - 1) / kOrthoPiece);
         o.piece_begin = g->pieces;
         o.fill_begin = g->fill_tiles;
-        o.sym_begin = g->sym_tiles;
-        o.full_begin = g->full_tiles;
         o.x = used, o.xt[0] = used + of_x, o.xt[1] = used + 2 * of_x;
         o.gram = used + 3 * of_x, o.factor = o.gram + of_a, o.both = o.factor + of_a, o.total[0] = o.both + of_a, o.total[1] = o.total[0] + of_a;
         if (list) list[*at] = o;
@@ -394,11 +438,18 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         used += need;
         g->pieces += o.pieces;
         g->fill_tiles += fill;
-        g->sym_tiles += down * (down + 1) / 2;
-        g->full_tiles += down * across;
         g->bytes = (size_t)used + gbt_align((size_t)g->pieces * sizeof(double));
     }
-    return g->count > 0;
+    if (g->count == 0) return false;
+    for (int kind = 0; kind < 3; ++kind) g->tiles[kind] = lay_tiles(matrices, order, g->first, g->count, (OrthoTiles)kind, nullptr);
+    return true;
+}
+// The list: the matrices in their order, then each group's tiles.
+int64_t list_bytes_of(const gbt_matrix *matrices, const OrthoOrder &order) {
+    int64_t at = 0, tiles = 0;
+    OrthoGroup g;
+    while (next_group(matrices, order, &at, &g, nullptr)) tiles += g.tiles[0] + g.tiles[1] + g.tiles[2];
+    return std::max<int64_t>(16, order.count * (int64_t)sizeof(OrthoMatrix) + tiles * (int64_t)sizeof(OrthoTile));
 }
 // Steps that are taken on A alone before X is multiplied: an error of A grows by the factor's square with each.
 int steps_together(double factor, bool wide) {
@@ -412,7 +463,8 @@ int steps_together(double factor, bool wide) {
 extern "C" size_t gbt_matrix_list_bytes(const gbt_matrix *matrices, int64_t n_matrices) {
     int32_t code;
     if (matrices_fault(matrices, n_matrices, &code)) return 0;
-    return std::max<size_t>(16, (size_t)n_matrices * sizeof(OrthoMatrix));
+    const OrthoOrder order(matrices, n_matrices);
+    return order.at ? (size_t)list_bytes_of(matrices, order) : 0;
 }
 
 extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int64_t n_matrices, void *list_out, size_t list_bytes) {
@@ -422,19 +474,25 @@ extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int
     int32_t code;
     const char *fault = matrices_fault(matrices, n_matrices, &code);
     GBT_REQUIRE(ctx, !fault, code, "%s", fault);
-    const size_t need = gbt_matrix_list_bytes(matrices, n_matrices);
-    GBT_REQUIRE(ctx, list_bytes >= need, GBT_ENOMEM, "list of %zu bytes, %zu needed", list_bytes, need);
-    OrthoMatrix *table = new (std::nothrow) OrthoMatrix[(size_t)std::max<int64_t>(1, n_matrices)];
-    GBT_REQUIRE(ctx, table, GBT_ENOMEM, "no host memory for the list");
     const OrthoOrder order(matrices, n_matrices);
-    int32_t st = order.at ? GBT_OK : gbt_fail(ctx, GBT_ENOMEM, "no host memory for the list");
+    GBT_REQUIRE(ctx, order.at, GBT_ENOMEM, "no host memory for the list");
+    const size_t need = (size_t)list_bytes_of(matrices, order);
+    GBT_REQUIRE(ctx, list_bytes >= need, GBT_ENOMEM, "list of %zu bytes, %zu needed", list_bytes, need);
+    char *table = new (std::nothrow) char[need];
+    GBT_REQUIRE(ctx, table, GBT_ENOMEM, "no host memory for the list");
+    memset(table, 0xff, need);   // tiles of no matrix
     int64_t at = 0;
+    OrthoTile *tiles = (OrthoTile *)(table + order.count * sizeof(OrthoMatrix));
     OrthoGroup g;
-    while (st == GBT_OK && next_group(matrices, order, &at, &g, table)) {
+    while (next_group(matrices, order, &at, &g, (OrthoMatrix *)table)) {
+        for (int kind = 0; kind < 3; ++kind) {
+            lay_tiles(matrices, order, g.first, g.count, (OrthoTiles)kind, tiles);
+            tiles += g.tiles[kind];
+        }
     }
     // in pieces that the staging takes
-    for (int64_t i = 0; i < order.count && st == GBT_OK; i += 8192)
-        st = gbt_upload(ctx, table + i, (size_t)std::min<int64_t>(8192, order.count - i) * sizeof(OrthoMatrix), (OrthoMatrix *)list_out + i);
+    int32_t st = GBT_OK;
+    for (size_t i = 0; i < need && st == GBT_OK; i += 1 << 20) st = gbt_upload(ctx, table + i, std::min<size_t>(1 << 20, need - i), (char *)list_out + i);
     delete[] table;
     return st;
 }
@@ -480,8 +538,9 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
     const OrthoOrder order(matrices, n_matrices);
     GBT_REQUIRE(ctx, order.at, GBT_ENOMEM, "no host memory for the order of the matrices");
     int64_t at = 0;
+    const OrthoTile *tiles = (const OrthoTile *)((const char *)list + order.count * sizeof(OrthoMatrix));
     OrthoGroup g;
-    while (next_group(matrices, order, &at, &g, nullptr)) {
+    for (; next_group(matrices, order, &at, &g, nullptr); tiles += g.tiles[0] + g.tiles[1] + g.tiles[2]) {
         OrthoArgs o;
         memset(&o, 0, sizeof o);
         o.list = (const OrthoMatrix *)list + g.first;
@@ -491,27 +550,31 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.a = a;
         o.b = b;
         o.c = c;
-        o.sym_tiles = g.sym_tiles;
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
-        auto product = [&](OrthoProduct of, int64_t tiles) { return gbt_launch_ortho_product(ctx->stream, o, of, tiles, ctx->num_cu); };
+        auto product = [&](OrthoProduct of, bool both = false) {
+            const OrthoTiles kind = of == kOrthoGram ? kTilesGram : of == kOrthoApply ? kTilesFull : kTilesSym;
+            o.tiles = tiles + (kind > 0 ? g.tiles[0] : 0) + (kind > 1 ? g.tiles[1] : 0);
+            o.count_tiles = g.tiles[kind];
+            return gbt_launch_ortho_product(ctx->stream, o, of, both, ctx->num_cu);
+        };
         const int together = steps_together(factor, g.wide);
         for (int s = 0; s < steps; s += together) {
             const int n = std::min(together, steps - s);
-            GBT_HIP(ctx, product(kOrthoGram, g.sym_tiles));
+            GBT_HIP(ctx, product(kOrthoGram));
             for (int i = 0; i < n; ++i) {
                 o.first = i == 0;
-                GBT_HIP(ctx, product(kOrthoFactor, g.sym_tiles));
+                GBT_HIP(ctx, product(kOrthoFactor));
                 if (i < n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
-                    GBT_HIP(ctx, product(kOrthoBoth, o.first ? g.sym_tiles : 2 * g.sym_tiles));
+                    GBT_HIP(ctx, product(kOrthoBoth, !o.first));
                     if (!o.first) o.total ^= 1;
-                    GBT_HIP(ctx, product(kOrthoNext, g.sym_tiles));
+                    GBT_HIP(ctx, product(kOrthoNext));
                 } else if (!o.first) {
-                    GBT_HIP(ctx, product(kOrthoTotal, g.sym_tiles));
+                    GBT_HIP(ctx, product(kOrthoTotal));
                     o.total ^= 1;
                 }
             }
             o.last = s + n == steps;
-            GBT_HIP(ctx, product(kOrthoApply, g.full_tiles));
+            GBT_HIP(ctx, product(kOrthoApply));
             o.xt ^= 1;
         }
     }

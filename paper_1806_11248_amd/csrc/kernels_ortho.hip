@@ -175,100 +175,97 @@ __global__ __launch_bounds__(256) void ortho_fill_kernel(OrthoArgs a) {
 }
 
 // ---------------------------------------------------------------- products --
-// 128 x 128 of P Q^T by four waves of 64 x 64 each: two rows of blocks of P and of Q, 32 along the sum at a time, from one of two stages of 32 KB of LDS while
-// the other is loaded.  With two groups of four waves each takes half of the sum.
+// 128 x 128 of P Q^T: two rows of blocks of P and of Q, 32 along the sum at a time, in kStages stages of 32 KB of LDS, of which all but one are being loaded.
+// Four waves take 64 x 64 each, eight 64 x 32.
 struct Stage {
     alignas(256) char p[2][2][Step::kBytes], q[2][2][Step::kBytes];   // [row of blocks][part]
 };
 
-// p, q: this wave's quarter of a pair of blocks; rows of blocks are `row` bytes apart.
+// p, q: this wave's part of a pair of blocks; rows of blocks are `row` bytes apart.
+template <int kWaves>
 __device__ __forceinline__ void fetch_stage(Stage &s, const char *p, const char *q, int64_t row, int wave, uint32_t lane_bytes) {
-    const uint32_t to = lds_address(&s) + wave * 2048;
+    const uint32_t to = lds_address(&s) + wave * (8192 / kWaves);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < 8 / kWaves; ++n) {
             load_to_lds(to + half * 8192 + n * 1024, p + half * row + n * 1024, lane_bytes);
             load_to_lds(to + 16384 + half * 8192 + n * 1024, q + half * row + n * 1024, lane_bytes);
         }
 }
 
-// Sums of many products are added up in pieces of 512, so that their roundings are those of small numbers, and in two halves, whether one group of waves
-// takes both or two take one each: the same result either way.
+// Sums of many products are added up in pieces of 512, so that their roundings are those of small numbers.
 constexpr int kPiece = 16;   // steps
 
-// The sum of steps from .. to, a group's.
-__device__ __forceinline__ void product(f32x16 (&sum)[2][2], Stage (&stage)[2], const char *p, const char *q, int64_t row, int from, int to, int wave, int lane) {
-    f32x16 acc[2][2] = {};
-    fetch_stage(stage[0], p + (int64_t)from * (kPair * 2), q + (int64_t)from * (kPair * 2), row, wave, lane * 16);
-    for (int k = from; k < to; ++k) {
-        tiles_ready();
-        const int now = (k - from) & 1;
-        if (k + 1 < to) fetch_stage(stage[now ^ 1], p + (int64_t)(k + 1) * (kPair * 2), q + (int64_t)(k + 1) * (kPair * 2), row, wave, lane * 16);
-        const Stage &s = stage[now];
+// A wave's operands of sixteen steps along the sum: [part][row or column of 32].
+template <int kWaves>
+struct Operands {
+    static constexpr int kAcross = 8 / kWaves;
+    f16x8 x[2][2], y[2][kAcross];
+    __device__ __forceinline__ void read(const Stage &s, int step, int wave, int lane) {
+        const int down = kWaves == 4 ? wave >> 1 : wave >> 2, across = kWaves == 4 ? wave & 1 : (wave & 3) >> 1, first = kWaves == 4 ? 0 : 32 * (wave & 1);
 #pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            f16x8 x[2][2], y[2][2];
+        for (int part = 0; part < 2; ++part) {
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+            for (int i = 0; i < 2; ++i) x[part][i] = Step::rows<F16>(s.p[down][part], 32 * i, step, lane);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    x[part][i] = Step::rows<F16>(s.p[wave >> 1][part], 32 * i, step, lane);
-                    y[part][i] = Step::rows<F16>(s.q[wave & 1][part], 32 * i, step, lane);
-                }
-            // low * high, high * low, high * high: four sums in turn, so that none waits for itself
-#pragma unroll
-            for (int of = 0; of < 3; ++of)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = F16::mma(x[of == 0][i], y[of == 1][j], acc[i][j]);
+            for (int j = 0; j < kAcross; ++j) y[part][j] = Step::rows<F16>(s.q[across][part], first + 32 * j, step, lane);
         }
-        done_reading();
-        if (((k - from) & (kPiece - 1)) == kPiece - 1 || k == to - 1) {
+    }
+    // low * high, high * low, high * high: the sums in turn, so that none waits for itself
+    __device__ __forceinline__ void add(f32x16 (&acc)[2][kAcross]) const {
+#pragma unroll
+        for (int of = 0; of < 3; ++of)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    sum[i][j] += acc[i][j];
-                    acc[i][j] = f32x16{};
-                }
-        }
+                for (int j = 0; j < kAcross; ++j) acc[i][j] = F16::mma(x[of == 0][i], y[of == 1][j], acc[i][j]);
     }
-}
+};
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }   // what is before it is issued before what is behind it
 
-// Workgroups go to the eight XCDs in turn: each takes an eighth of a matrix's tiles in a row, and of these eight rows of tiles at a time, so that what it reads
-// stays in its L2.
-__device__ __forceinline__ int64_t of_xcd(int64_t at, int64_t tiles) {
-    const int64_t eighth = tiles / 8;
-    return at < eighth * 8 ? at % 8 * eighth + at / 8 : at;
-}
-__device__ __forceinline__ void full_tile(int64_t at, int down, int across, int &i, int &j) {
-    at = of_xcd(at, (int64_t)down * across);
-    const int band = (int)(at / (8 * across)), rows = min(8, down - 8 * band);
-    at -= (int64_t)band * 8 * across;
-    i = 8 * band + (int)(at % rows);
-    j = (int)(at / rows);
-}
-// Of n x n tiles those with i <= j.
-__device__ __forceinline__ void upper_tile(int64_t at, int n, int &i, int &j) {
-    at = of_xcd(at, (int64_t)n * (n + 1) / 2);
-    int first = 0;   // row of the band; a column j of it has min(8, j - first + 1) rows
-    for (;; first += 8) {
-        const int m = n - first;
-        const int64_t in_band = m >= 8 ? 36 + 8 * (int64_t)(m - 8) : (int64_t)m * (m + 1) / 2;
-        if (at < in_band) break;
-        at -= in_band;
+// While the matrix units work on one half of a step, the operands of the next half are read, also from the next step, behind the barrier.
+template <int kWaves, int kStages>
+__device__ __forceinline__ void product(f32x16 (&sum)[2][8 / kWaves], Stage *stages, const char *p, const char *q, int64_t row, int steps, int wave, int lane) {
+    constexpr int kAcross = 8 / kWaves, kLoads = 4 * (8 / kWaves);   // of a stage, by each wave
+    f32x16 acc[2][kAcross] = {};
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+        if (s < steps) fetch_stage<kWaves>(stages[s], p + s * (kPair * 2), q + s * (kPair * 2), row, wave, lane * 16);
+    Operands<kWaves> even, odd;
+    int now = 0;
+    for (int k = 0; k < steps; ++k) {
+        // this step's loads are done, those of the steps behind it under way; and all waves are done with the step before
+        if (k + kStages - 1 <= steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (kStages - 2)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int next = k + kStages - 1, at = now == 0 ? kStages - 1 : now - 1;
+        even.read(stages[now], 0, wave, lane);
+        in_order();
+        if (next < steps) fetch_stage<kWaves>(stages[at], p + (int64_t)next * (kPair * 2), q + (int64_t)next * (kPair * 2), row, wave, lane * 16);
+        if (k > 0) {
+            odd.add(acc);
+            if ((k & (kPiece - 1)) == 0) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < kAcross; ++j) {
+                        sum[i][j] += acc[i][j];
+                        acc[i][j] = f32x16{};
+                    }
+            }
+        }
+        in_order();
+        odd.read(stages[now], 1, wave, lane);
+        in_order();
+        even.add(acc);
+        in_order();
+        now = now + 1 == kStages ? 0 : now + 1;
     }
-    if (at >= 36) {
-        i = first + (int)((at - 36) & 7);
-        j = first + 8 + (int)((at - 36) >> 3);
-    } else {
-        int c = 0;
-        while (at > c) at -= ++c;
-        i = first + (int)at;
-        j = first + c;
-    }
+    odd.add(acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < kAcross; ++j) sum[i][j] += acc[i][j];
 }
 
 // Sixteen-bit values of four rows in the column of each of four lanes, and back: the lane's own row's values of the four columns.
@@ -313,18 +310,15 @@ __device__ __forceinline__ void put_four(_Float16 *m, int cols, _Float16 *t, int
     }
 }
 
-template <int kProduct, int kGroups>
-__global__ __launch_bounds__(256 * kGroups, 2) void ortho_product_kernel(OrthoArgs a) {
+template <int kProduct, int kWaves, int kStages>
+__global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs a) {
     extern __shared__ __attribute__((aligned(256))) char lds[];
-    Stage(*stages)[2] = (Stage(*)[2])lds;
     constexpr bool kApply = kProduct == kOrthoApply;
-    const bool second = kProduct == kOrthoBoth && blockIdx.x >= a.sym_tiles;
-    const int64_t tile = blockIdx.x - (second ? a.sym_tiles : 0);
-    const OrthoMatrix &m = a.list[matrix_of(a, kApply ? &OrthoMatrix::full_begin : &OrthoMatrix::sym_begin, tile)];
-    const int down = m.pp / kOrthoTile, across = m.ww / kOrthoTile;
-    int ti, tj;
-    if (kApply) full_tile(tile - m.full_begin, down, across, ti, tj);
-    else upper_tile(tile - m.sym_begin, down, ti, tj);
+    const bool second = kProduct == kOrthoBoth && blockIdx.x >= a.count_tiles;
+    const OrthoTile tile = a.tiles[blockIdx.x - (second ? a.count_tiles : 0)];
+    if (tile.matrix < 0) return;
+    const OrthoMatrix &m = a.list[tile.matrix];
+    const int ti = tile.i, tj = tile.j;
     auto at = [&](int64_t offset) { return (_Float16 *)(a.workspace + offset); };
     // a step's factor; the first one of some begins their product
     const int64_t factor = a.first ? m.total[a.total] : m.factor;
@@ -335,53 +329,24 @@ __global__ __launch_bounds__(256 * kGroups, 2) void ortho_product_kernel(OrthoAr
                       : kProduct == kOrthoTotal || second ? m.total[a.total ^ 1] : m.both);
     _Float16 *to_t = kApply ? at(m.xt[a.xt ^ 1]) : to;
     const int depth = kProduct == kOrthoGram ? m.ww : m.pp, cols = kApply ? m.ww : m.pp;
-    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all & 3, group = all >> 2;
-    const int steps = depth / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps = depth / 32;
     const int64_t row_bytes = (int64_t)steps * kPair * 2;
-    const char *of_p = (const char *)p + (int64_t)ti * 2 * row_bytes + wave * 2048, *of_q = (const char *)q + (int64_t)tj * 2 * row_bytes + wave * 2048;
-    f32x16 acc[2][2] = {}, rest[2][2] = {};
-    if (kGroups == 1) {
-        product(acc, stages[0], of_p, of_q, row_bytes, 0, steps / 2, wave, lane);
-        __syncthreads();
-        product(rest, stages[0], of_p, of_q, row_bytes, steps / 2, steps, wave, lane);
-    } else {
-        product(acc, stages[group], of_p, of_q, row_bytes, group * (steps / 2), (group + 1) * (steps / 2), wave, lane);
-        // each group finishes half of the rows, and gives the other one its sums of the other half
-        __syncthreads();
-        float *give = (float *)lds + (group * 4 + wave) * 64 * 32 + lane * 32, *get = (float *)lds + ((group ^ 1) * 4 + wave) * 64 * 32 + lane * 32;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int at = (j * 16 + r) ^ ((lane & 7) << 2);
-                *(f32x4 *)(give + at) = group ? f32x4{acc[0][j][r], acc[0][j][r + 1], acc[0][j][r + 2], acc[0][j][r + 3]}
-                                              : f32x4{acc[1][j][r], acc[1][j][r + 1], acc[1][j][r + 2], acc[1][j][r + 3]};
-            }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const f32x4 x = *(const f32x4 *)(get + ((j * 16 + r) ^ ((lane & 7) << 2)));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    rest[0][j][r + e] = x[e];
-                    acc[0][j][r + e] = group ? acc[1][j][r + e] : acc[0][j][r + e];
-                }
-            }
-    }
+    f32x16 acc[2][8 / kWaves] = {};
+    product<kWaves, kStages>(acc, (Stage *)lds, (const char *)p + (int64_t)ti * 2 * row_bytes + wave * (8192 / kWaves),
+                             (const char *)q + (int64_t)tj * 2 * row_bytes + wave * (8192 / kWaves), row_bytes, steps, wave, lane);
+    const int first_row = ti * kOrthoTile + (kWaves == 4 ? wave >> 1 : wave >> 2) * 64, first_col = tj * kOrthoTile + (kWaves == 4 ? (wave & 1) * 64 : (wave & 3) * 32);
     const Exchange swap(lane);
     const float scale = m.scale * kDown;
 #pragma unroll
-    for (int i = 0; i < 2 / kGroups; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 8 / kWaves; ++j)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const int row = ti * kOrthoTile + (wave >> 1) * 64 + 32 * (i + group) + result_row(r, lane >> 5), col = tj * kOrthoTile + (wave & 1) * 64 + 32 * j + (lane & 31);
+                const int row = first_row + 32 * i + result_row(r, lane >> 5), col = first_col + 32 * j + (lane & 31);
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (acc[i][j][r + e] + rest[i][j][r + e]) * kDown;
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * kDown;
                 if (kProduct == kOrthoFactor) {
                     // A is symmetric: its four values of this column lie side by side in the row of that number
                     const _Float16 *from = p + place(col, row, m.pp);
@@ -402,18 +367,19 @@ __global__ __launch_bounds__(256 * kGroups, 2) void ortho_product_kernel(OrthoAr
             }
 }
 
-template <int kProduct, int kGroups>
-hipError_t launch_groups(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
-    constexpr int kLds = kGroups * 2 * (int)sizeof(Stage);
-    static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_product_kernel<kProduct, kGroups>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+template <int kProduct, int kWaves, int kStages>
+hipError_t launch_form(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
+    constexpr int kLds = kStages * (int)sizeof(Stage);
+    static const hipError_t ready =
+        hipFuncSetAttribute((const void *)ortho_product_kernel<kProduct, kWaves, kStages>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (ready != hipSuccess) return ready;
-    ortho_product_kernel<kProduct, kGroups><<<(unsigned)tiles, 256 * kGroups, kLds, stream>>>(a);
+    ortho_product_kernel<kProduct, kWaves, kStages><<<(unsigned)tiles, 64 * kWaves, kLds, stream>>>(a);
     return hipGetLastError();
 }
-// Few tiles: two groups of waves, as the steps that follow one another are what counts.
+// Many tiles: two workgroups on a compute unit, with two stages each; few: one with all of the LDS, as the loads' latency is what counts.
 template <int kProduct>
 hipError_t launch(hipStream_t stream, const OrthoArgs &a, int64_t tiles, int num_cu) {
-    return tiles <= 2 * num_cu ? launch_groups<kProduct, 2>(stream, a, tiles) : launch_groups<kProduct, 1>(stream, a, tiles);
+    return tiles <= 2 * num_cu ? launch_form<kProduct, 8, 5>(stream, a, tiles) : launch_form<kProduct, 4, 2>(stream, a, tiles);
 }
 
 }  // namespace
@@ -426,7 +392,8 @@ hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_
     return hipGetLastError();
 }
 
-hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int64_t tiles, int num_cu) {
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, bool both, int num_cu) {
+    const int64_t tiles = both ? 2 * a.count_tiles : a.count_tiles;
     switch (product) {
         case kOrthoGram: return launch<kOrthoGram>(stream, a, tiles, num_cu);
         case kOrthoFactor: return launch<kOrthoFactor>(stream, a, tiles, num_cu);

@@ -19,7 +19,12 @@ struct OrthoMatrix {
     int64_t piece_begin;                // of the group's pieces
     int64_t x, xt[2];                   // bytes into the workspace: X, its transpose (and the next one)
     int64_t gram, factor, both, total[2];   // p x p: A, a step's factor F of it, F A, and the product of the factors so far (and the next one)
-    int64_t fill_begin, sym_begin, full_begin;   // of the group's tiles: of X, of symmetric products' upper halves, of X
+    int64_t fill_begin;                 // of the group's workgroups that lay X out
+};
+// What a workgroup of a product computes: tile (i, j) of one matrix of the group; matrix < 0: nothing.
+struct OrthoTile {
+    int32_t matrix;
+    int16_t i, j;
 };
 
 struct OrthoArgs {
@@ -28,7 +33,8 @@ struct OrthoArgs {
     char *workspace;
     double *squares;                    // [pieces of the group]
     float a, b, c;
-    int64_t sym_tiles;
+    const OrthoTile *tiles;             // of the product
+    int64_t count_tiles;
     int xt, total;                      // which of the two transposes is X's, which of the two products of factors the last one
     int first, last;                    // first: the factor is the first of some, and begins their product; last: the result goes to dst
 };
@@ -36,5 +42,5 @@ struct OrthoArgs {
 enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
 
 hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_t pieces, int64_t fill_tiles);
-// The tiles of a product: a.sym_tiles, twice as many for kOrthoBoth, or those of X for kOrthoApply.
-hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int64_t tiles, int num_cu);
+// a.tiles are those of symmetric products' upper halves, or all of X's for kOrthoApply; `both`: kOrthoBoth computes the product of the factors too.
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, bool both, int num_cu);

@@ -80,7 +80,9 @@ def test_matrices(b):
     L = b._lib
     ok = (64, 64, 10, 20, 0, 1.0)
     assert L.gbt_matrix_list_bytes(*_matrices(b)) >= 16 and L.gbt_orthogonalise_workspace_bytes(*_matrices(b)) == 0
-    assert L.gbt_matrix_list_bytes(*_matrices(b, ok, ok)) == 2 * L.gbt_matrix_list_bytes(*_matrices(b, ok))
+    # an entry for each matrix, and the tiles of each kind of product by eight XCDs
+    assert L.gbt_matrix_list_bytes(*_matrices(b)) < L.gbt_matrix_list_bytes(*_matrices(b, ok)) < L.gbt_matrix_list_bytes(*_matrices(b, ok, ok)) <= 2000
+    assert L.gbt_matrix_list_bytes(*_matrices(b, (64, 64, 4096, 4096, 0, 1.0))) >= 8 * (32 * 32 + 2 * 32 * 33 // 2)
     assert L.gbt_orthogonalise_workspace_bytes(*_matrices(b, (0, 0, 0, 5, 0, 1.0))) == 0                          # nothing of it is read
     # 12 bytes an element and 20 for each of X X^T's, of whole tiles
     big = (64, 64, 1024, 4096, 1, 1.0)
