@@ -333,7 +333,15 @@ const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
     return nullptr;
 }
 
-// The matrices with elements in the order that they are worked on in: those of 32 bits first, and of either kind those with the most to do.
+// Kinds of matrices, which are worked on apart: small or not, and with results of 32 bits or sixteen.
+int kind_of(const gbt_matrix &m) {
+    const bool small = std::min(m.rows, m.cols) <= kOrthoSmallP && std::max(m.rows, m.cols) <= kOrthoSmallW;
+    return (small ? 0 : 2) + (m.dtype == GBT_F32 ? 0 : 1);
+}
+bool small_kind(int kind) { return kind < 2; }
+bool wide_kind(int kind) { return kind % 2 == 0; }
+
+// The matrices with elements in the order that they are worked on in: by kind, and of each kind those with the most to do first.
 struct OrthoOrder {
     int32_t *at;
     int64_t count = 0;
@@ -342,8 +350,7 @@ struct OrthoOrder {
         for (int64_t i = 0; i < n; ++i)
             if (m[i].rows > 0 && m[i].cols > 0) at[count++] = (int32_t)i;
         std::sort(at, at + count, [m](int32_t x, int32_t y) {
-            const bool wide_x = m[x].dtype == GBT_F32, wide_y = m[y].dtype == GBT_F32;
-            if (wide_x != wide_y) return wide_x;
+            if (kind_of(m[x]) != kind_of(m[y])) return kind_of(m[x]) < kind_of(m[y]);
             const int64_t of_x = m[x].rows * m[x].cols * std::min(m[x].rows, m[x].cols), of_y = m[y].rows * m[y].cols * std::min(m[y].rows, m[y].cols);
             return of_x != of_y ? of_x > of_y : x < y;
         });
@@ -400,7 +407,7 @@ int64_t lay_tiles(const gbt_matrix *matrices, const OrthoOrder &order, int64_t f
 // Matrices of one kind that are worked on together, and what they need.
 struct OrthoGroup {
     int64_t first, count;   // of the order
-    bool wide;              // results of 32 bits
+    int kind;
     int64_t pieces, fill_tiles, tiles[3];   // tiles: by OrthoTiles
     size_t bytes;
 };
@@ -420,8 +427,8 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.pp = (int32_t)down * kOrthoTile;
         o.ww = (int32_t)across * kOrthoTile;
         const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 3 * of_x + 5 * of_a;
-        const bool wide = m.dtype == GBT_F32;
-        if (g->count > 0 && (wide != g->wide || used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)) break;
+        const int kind = kind_of(m);
+        if (g->count > 0 && (kind != g->kind || (!small_kind(kind) && (used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)))) break;
         o.src = m.src;
         o.dst = m.dst;
         o.cols = m.cols;
@@ -433,14 +440,16 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.x = used, o.xt[0] = used + of_x, o.xt[1] = used + 2 * of_x;
         o.gram = used + 3 * of_x, o.factor = o.gram + of_a, o.both = o.factor + of_a, o.total[0] = o.both + of_a, o.total[1] = o.total[0] + of_a;
         if (list) list[*at] = o;
-        g->wide = wide;
+        g->kind = kind;
         ++g->count;
+        if (small_kind(kind)) continue;
         used += need;
         g->pieces += o.pieces;
         g->fill_tiles += fill;
         g->bytes = (size_t)used + gbt_align((size_t)g->pieces * sizeof(double));
     }
     if (g->count == 0) return false;
+    if (small_kind(g->kind)) return true;
     for (int kind = 0; kind < 3; ++kind) g->tiles[kind] = lay_tiles(matrices, order, g->first, g->count, (OrthoTiles)kind, nullptr);
     return true;
 }
@@ -486,7 +495,7 @@ extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int
     OrthoGroup g;
     while (next_group(matrices, order, &at, &g, (OrthoMatrix *)table)) {
         for (int kind = 0; kind < 3; ++kind) {
-            lay_tiles(matrices, order, g.first, g.count, (OrthoTiles)kind, tiles);
+            if (g.tiles[kind]) lay_tiles(matrices, order, g.first, g.count, (OrthoTiles)kind, tiles);
             tiles += g.tiles[kind];
         }
     }
@@ -550,6 +559,11 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.a = a;
         o.b = b;
         o.c = c;
+        const int together = steps_together(factor, wide_kind(g.kind));
+        if (small_kind(g.kind)) {
+            GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, steps, together));
+            continue;
+        }
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
         auto product = [&](OrthoProduct of, bool both = false) {
             const OrthoTiles kind = of == kOrthoGram ? kTilesGram : of == kOrthoApply ? kTilesFull : kTilesSym;
@@ -557,7 +571,6 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
             o.count_tiles = g.tiles[kind];
             return gbt_launch_ortho_product(ctx->stream, o, of, both, ctx->num_cu);
         };
-        const int together = steps_together(factor, g.wide);
         for (int s = 0; s < steps; s += together) {
             const int n = std::min(together, steps - s);
             GBT_HIP(ctx, product(kOrthoGram));

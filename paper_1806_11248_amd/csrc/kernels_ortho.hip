@@ -367,6 +367,175 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
             }
 }
 
+// ------------------------------------------------------------------- small --
+// A small matrix by one workgroup, all of it in LDS: X in blocks of 64 rows by 32 columns, and three p x p matrices of two blocks each, four waves a quarter
+// of a product each.  A result goes back over an operand once all waves have it.  B operands that run along columns of X are read transposed, in the order
+// of the sum that such reads give (attention.h), and those they meet in the same order.
+struct Small {
+    char *gram, *factor, *total, *x;
+    int wave, lane;
+};
+__device__ __forceinline__ void small_product(f32x16 &acc, const Small &s, const char *p, const char *q, int blocks) {
+    acc = f32x16{};
+    for (int b = 0; b < blocks; ++b)
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            f16x8 x[2], y[2];
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                x[part] = Step::rows<F16>(p + b * 8192 + part * 4096, 32 * (s.wave >> 1), step, s.lane);
+                y[part] = Step::rows<F16>(q + b * 8192 + part * 4096, 32 * (s.wave & 1), step, s.lane);
+            }
+            acc = F16::mma(x[1], y[0], acc);
+            acc = F16::mma(x[0], y[1], acc);
+            acc = F16::mma(x[0], y[0], acc);
+        }
+}
+// Byte offset of row `col`, elements row .. row + 3 of a symmetric p x p matrix: where a lane's four values belong.
+__device__ __forceinline__ int small_four(const Small &s, int r) {
+    const int row = 32 * (s.wave >> 1) + result_row(r, s.lane >> 5), col = 32 * (s.wave & 1) + (s.lane & 31);
+    return (int)place(col, row, 64) * 2;
+}
+__device__ __forceinline__ void small_put(char *to, const float (&v)[4]) {
+    f16x4 high, low;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        _Float16 h, l;
+        split(v[e], h, l);
+        high[e] = h, low[e] = l;
+    }
+    *(f16x4 *)to = high;
+    *(f16x4 *)(to + kBlock * 2) = low;
+}
+__device__ __forceinline__ void small_write(const Small &s, char *to, const f32x16 &acc) {
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const float v[4] = {acc[r] * kDown, acc[r + 1] * kDown, acc[r + 2] * kDown, acc[r + 3] * kDown};
+        small_put(to + small_four(s, r), v);
+    }
+}
+
+__global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps, int together) {
+    extern __shared__ __attribute__((aligned(256))) char lds[];
+    __shared__ double part[4];
+    const OrthoMatrix &m = a.list[blockIdx.x];
+    const int blocks = (m.w + 31) / 32;
+    Small s;
+    s.gram = lds, s.factor = lds + 16384, s.total = lds + 32768, s.x = lds + 49152;
+    s.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s.lane = threadIdx.x & 63;
+    const int n = m.p * m.w;
+    double sum;
+    if (m.dtype == GBT_F32) sum = add_squares((const float *)m.src, n);
+    else if (m.dtype == GBT_BF16) sum = add_squares((const __bf16 *)m.src, n);
+    else sum = add_squares((const _Float16 *)m.src, n);
+    const double norm = sqrt(block_sum(sum, part));
+    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
+    for (int at = threadIdx.x; at < 64 * blocks * 4; at += 256) {   // sixteen-byte pieces, neighbours in memory by neighbouring lanes
+        const int i = m.tall ? at % 64 : at / (blocks * 4), j = (m.tall ? at / 64 : at % (blocks * 4)) * 8;
+        f16x8 high, low;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = 0.0f;
+            if (i < m.p && j + e < m.w) x = (float)((double)element(m, m.tall ? (int64_t)(j + e) * m.cols + i : (int64_t)i * m.cols + j + e) * factor);
+            _Float16 h, l;
+            split(x, h, l);
+            high[e] = h, low[e] = l;
+        }
+        char *to = s.x + place(i, j, blocks * 32) * 2;
+        *(f16x8 *)to = high;
+        *(f16x8 *)(to + kBlock * 2) = low;
+    }
+    __syncthreads();
+    const Exchange swap(s.lane);
+    const float scale = m.scale * kDown;
+    for (int done = 0; done < steps; done += together) {
+        const int now = min(together, steps - done);
+        f32x16 acc, next;
+        small_product(acc, s, s.x, s.x, blocks);
+        small_write(s, s.gram, acc);
+        __syncthreads();
+        for (int i = 0; i < now; ++i) {
+            char *f = i == 0 ? s.total : s.factor;   // the first factor begins their product
+            small_product(acc, s, s.gram, s.gram, 2);
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int at = small_four(s, r), row = 32 * (s.wave >> 1) + result_row(r, s.lane >> 5), col = 32 * (s.wave & 1) + (s.lane & 31);
+                const f16x4 high = *(const f16x4 *)(s.gram + at), low = *(const f16x4 *)(s.gram + at + kBlock * 2);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = fmaf(a.c, acc[r + e] * kDown, a.b * ((float)high[e] + (float)low[e]));
+                    if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                }
+                small_put(f + at, v);
+            }
+            __syncthreads();
+            if (i > 0) small_product(next, s, f, s.total, 2);
+            if (i < now - 1) small_product(acc, s, f, s.gram, 2);
+            __syncthreads();
+            if (i > 0) small_write(s, s.total, next);
+            if (i < now - 1) small_write(s, s.gram, acc);
+            __syncthreads();
+            if (i < now - 1) {
+                small_product(acc, s, s.gram, f, 2);
+                __syncthreads();
+                small_write(s, s.gram, acc);
+                __syncthreads();
+            }
+        }
+        // X, a block of 32 columns by a wave, in place
+        const bool last = done + now == steps;
+        for (int b = s.wave; b < blocks; b += 4) {
+            char *block = s.x + b * 8192;
+            f16x8 y[2][4];
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[part][k] = Step::cols<F16>(block + part * 4096, 16 * k, 0, s.lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int of = s.lane & 31, half = s.lane >> 5;
+                f32x16 z = {};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f16x8 x[2];
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const char *row = s.total + (k >> 1) * 8192 + part * 4096 + (32 * i + of) * 64 + 8 * half;
+                        const f16x4 lo = *(const f16x4 *)(row + (((2 * (k & 1)) ^ Step::fold(of)) << 4)), hi = *(const f16x4 *)(row + (((2 * (k & 1) + 1) ^ Step::fold(of)) << 4));
+                        x[part] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+                    z = F16::mma(x[1], y[0][k], z);
+                    z = F16::mma(x[0], y[1][k], z);
+                    z = F16::mma(x[0], y[0][k], z);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int row = 32 * i + result_row(r, half), col = 32 * b + of;
+                    if (last) {
+                        if (col < m.w)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (row + e < m.p) put_element(m, m.tall ? (int64_t)col * m.cols + row + e : (int64_t)(row + e) * m.cols + col, z[r + e] * kDown * scale);
+                        continue;
+                    }
+                    f16x4 high, low;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        _Float16 h, l;
+                        split(z[r + e] * kDown, h, l);
+                        high[e] = h, low[e] = l;
+                    }
+                    char *to = block + place(row + swap.quad, of & ~3, 32) * 2;
+                    *(f16x4 *)to = swap(high);
+                    *(f16x4 *)(to + kBlock * 2) = swap(low);
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 template <int kProduct, int kWaves, int kStages>
 hipError_t launch_form(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
     constexpr int kLds = kStages * (int)sizeof(Stage);
@@ -389,6 +558,13 @@ hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     ortho_fill_kernel<<<(unsigned)fill_tiles, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, int steps, int together) {
+    static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmallLds);
+    if (ready != hipSuccess) return ready;
+    ortho_small_kernel<<<a.count, 256, kOrthoSmallLds, stream>>>(a, steps, together);
     return hipGetLastError();
 }
 

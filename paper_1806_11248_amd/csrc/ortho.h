@@ -39,6 +39,11 @@ struct OrthoArgs {
     int first, last;                    // first: the factor is the first of some, and begins their product; last: the result goes to dst
 };
 
+// Matrices that one workgroup takes as a whole: X's blocks and three matrices of p x p in LDS.
+constexpr int kOrthoSmallP = 64, kOrthoSmallW = 384;
+constexpr int kOrthoSmallLds = 3 * 16384 + kOrthoSmallW / 32 * 8192;
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, int steps, int together);
+
 enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
 
 hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_t pieces, int64_t fill_tiles);

@@ -46,7 +46,8 @@ def _check(ctx, updates, steps=5, coefficients=MUON, scales=1.0, outs=None):
     return got
 
 
-SHAPES = [(1, 1), (1, 9), (9, 1), (3, 5), (16, 16), (40, 64), (64, 256), (128, 64), (127, 129), (129, 127), (128, 128), (255, 384), (200, 1000), (1000, 200), (300, 300)]
+SHAPES = [(1, 1), (1, 9), (9, 1), (3, 5), (16, 16), (40, 64), (64, 256), (128, 64), (127, 129), (129, 127), (128, 128), (255, 384), (200, 1000), (1000, 200), (300, 300),
+          (64, 64), (64, 384), (384, 64), (63, 383), (33, 31), (65, 64), (64, 385), (385, 17)]
 
 
 @pytest.mark.parametrize("m,n", SHAPES)

@@ -78,7 +78,9 @@ def _matrices(b, *entries):
 
 def test_matrices(b):
     L = b._lib
-    ok = (64, 64, 10, 20, 0, 1.0)
+    ok = (64, 64, 100, 200, 0, 1.0)
+    assert L.gbt_orthogonalise_workspace_bytes(*_matrices(b, (64, 64, 64, 384, 0, 1.0), (64, 64, 384, 5, 1, 1.0))) == 0      # one workgroup's, without
+    assert L.gbt_orthogonalise_workspace_bytes(*_matrices(b, (64, 64, 65, 65, 0, 1.0))) > 0 and L.gbt_orthogonalise_workspace_bytes(*_matrices(b, (64, 64, 385, 2, 0, 1.0))) > 0
     assert L.gbt_matrix_list_bytes(*_matrices(b)) >= 16 and L.gbt_orthogonalise_workspace_bytes(*_matrices(b)) == 0
     # an entry for each matrix, and the tiles of each kind of product by eight XCDs
     assert L.gbt_matrix_list_bytes(*_matrices(b)) < L.gbt_matrix_list_bytes(*_matrices(b, ok)) < L.gbt_matrix_list_bytes(*_matrices(b, ok, ok)) <= 2000
