@@ -370,26 +370,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
 // ------------------------------------------------------------------- small --
 // A small matrix by one workgroup, all of it in LDS: X in blocks of 64 rows by 32 columns, and three p x p matrices of two blocks each, four waves a quarter
 // of a product each.  A result goes back over an operand once all waves have it.  B operands that run along columns of X are read transposed, in the order
-// of the sum that such reads give (attention.h), and those they meet in the same order.
+// of the sum that such reads give (attention.h), and those they meet in the same order.  What bounds it is how steps wait for one another, and the fetching of
+// code that runs but once: all products of p x p are one loop (40 KB of code 52 us for 64 x 256 in five steps, the loop 34).
 struct Small {
     char *gram, *factor, *total, *x;
     int wave, lane;
 };
+// One wave has nothing but this to do, so its three kinds of products are three sums, that none waits for another.
 __device__ __forceinline__ void small_product(f32x16 &acc, const Small &s, const char *p, const char *q, int blocks) {
-    acc = f32x16{};
-    for (int b = 0; b < blocks; ++b)
+    f32x16 sum[3] = {};
+    for (int b = 0; b < blocks; b += 2) {
+        f16x8 x[4][2], y[4][2];
 #pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            f16x8 x[2], y[2];
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
-                x[part] = Step::rows<F16>(p + b * 8192 + part * 4096, 32 * (s.wave >> 1), step, s.lane);
-                y[part] = Step::rows<F16>(q + b * 8192 + part * 4096, 32 * (s.wave & 1), step, s.lane);
+                const int at = min(b + (k >> 1), blocks - 1) * 8192 + part * 4096;
+                x[k][part] = Step::rows<F16>(p + at, 32 * (s.wave >> 1), k & 1, s.lane);
+                y[k][part] = Step::rows<F16>(q + at, 32 * (s.wave & 1), k & 1, s.lane);
             }
-            acc = F16::mma(x[1], y[0], acc);
-            acc = F16::mma(x[0], y[1], acc);
-            acc = F16::mma(x[0], y[0], acc);
-        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (b + (k >> 1) < blocks) {
+                sum[0] = F16::mma(x[k][1], y[k][0], sum[0]);
+                sum[1] = F16::mma(x[k][0], y[k][1], sum[1]);
+                sum[2] = F16::mma(x[k][0], y[k][0], sum[2]);
+            }
+    }
+    acc = (sum[0] + sum[1]) + sum[2];
 }
 // Byte offset of row `col`, elements row .. row + 3 of a symmetric p x p matrix: where a lane's four values belong.
 __device__ __forceinline__ int small_four(const Small &s, int r) {
@@ -407,11 +415,68 @@ __device__ __forceinline__ void small_put(char *to, const float (&v)[4]) {
     *(f16x4 *)to = high;
     *(f16x4 *)(to + kBlock * 2) = low;
 }
-__device__ __forceinline__ void small_write(const Small &s, char *to, const f32x16 &acc) {
+// X into its blocks, divided by its norm, by pieces of eight elements, neighbours in memory by neighbouring lanes.  All of G is under way at once and in
+// registers until the norm is known.
+template <typename E>
+__device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m, int blocks, double *part) {
+    constexpr int kPieces = 64 * kOrthoSmallW / 8 / 256;
+    const E *src = (const E *)m.src;
+    const int cols = (int)m.cols, across = blocks * 4, pieces = 64 * across;
+    const bool wide = !m.tall && cols % 8 == 0 && ((uintptr_t)src & 15) == 0;
+    float x[kPieces][8];
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-        const float v[4] = {acc[r] * kDown, acc[r + 1] * kDown, acc[r + 2] * kDown, acc[r + 3] * kDown};
-        small_put(to + small_four(s, r), v);
+    for (int n = 0; n < kPieces; ++n) {
+        const int at = threadIdx.x + 256 * n, i = m.tall ? at & 63 : at / across, j = (m.tall ? at >> 6 : at - at / across * across) * 8;
+        if (at >= pieces || i >= m.p) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[n][e] = 0.0f;
+        } else if (wide) {
+            Vec<E> v[sizeof(E) / 2] = {};
+            if (j < cols)
+#pragma unroll
+                for (int u = 0; u < (int)sizeof(E) / 2; ++u) v[u] = ((const Vec<E> *)(src + i * cols + j))[u];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[n][e] = (float)v[e / (16 / sizeof(E))].x[e % (16 / sizeof(E))];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[n][e] = j + e < m.w ? (float)src[m.tall ? (j + e) * cols + i : i * cols + j + e] : 0.0f;
+        }
+    }
+    double sum[2] = {0.0, 0.0};
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e & 1] = fma((double)x[n][e], (double)x[n][e], sum[e & 1]);
+    const double norm = sqrt(block_sum(sum[0] + sum[1], part));
+    // a norm of zero leaves zeros; one that is no finite number leaves none anywhere
+    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+        const int at = threadIdx.x + 256 * n, i = m.tall ? at & 63 : at / across, j = (m.tall ? at >> 6 : at - at / across * across) * 8;
+        if (at >= pieces) break;
+        f16x8 high, low;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            split((float)((double)x[n][e] * factor), h, l);
+            high[e] = h, low[e] = l;
+        }
+        char *to = s.x + place(i, j, blocks * 32) * 2;
+        *(f16x8 *)to = high;
+        *(f16x8 *)(to + kBlock * 2) = low;
+    }
+}
+// A block's half of the result, rows 32 * i on, to G's place.
+template <typename E>
+__device__ __forceinline__ void small_result(const Small &s, const OrthoMatrix &m, const f32x16 &z, int i, int col) {
+    E *dst = (E *)m.dst;
+    const float scale = m.scale * kDown;
+    const int across = m.tall ? 1 : (int)m.cols, along = m.tall ? (int)m.cols : 1, first = 32 * i + 4 * (s.lane >> 5);
+    if (col >= m.w) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int row = first + result_row(r, 0);
+        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * kDown * scale);
     }
 }
 
@@ -423,65 +488,39 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
     Small s;
     s.gram = lds, s.factor = lds + 16384, s.total = lds + 32768, s.x = lds + 49152;
     s.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s.lane = threadIdx.x & 63;
-    const int n = m.p * m.w;
-    double sum;
-    if (m.dtype == GBT_F32) sum = add_squares((const float *)m.src, n);
-    else if (m.dtype == GBT_BF16) sum = add_squares((const __bf16 *)m.src, n);
-    else sum = add_squares((const _Float16 *)m.src, n);
-    const double norm = sqrt(block_sum(sum, part));
-    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
-    for (int at = threadIdx.x; at < 64 * blocks * 4; at += 256) {   // sixteen-byte pieces, neighbours in memory by neighbouring lanes
-        const int i = m.tall ? at % 64 : at / (blocks * 4), j = (m.tall ? at / 64 : at % (blocks * 4)) * 8;
-        f16x8 high, low;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float x = 0.0f;
-            if (i < m.p && j + e < m.w) x = (float)((double)element(m, m.tall ? (int64_t)(j + e) * m.cols + i : (int64_t)i * m.cols + j + e) * factor);
-            _Float16 h, l;
-            split(x, h, l);
-            high[e] = h, low[e] = l;
-        }
-        char *to = s.x + place(i, j, blocks * 32) * 2;
-        *(f16x8 *)to = high;
-        *(f16x8 *)(to + kBlock * 2) = low;
-    }
+    if (m.dtype == GBT_F32) small_read<float>(s, m, blocks, part);
+    else if (m.dtype == GBT_BF16) small_read<__bf16>(s, m, blocks, part);
+    else small_read<_Float16>(s, m, blocks, part);
     __syncthreads();
     const Exchange swap(s.lane);
-    const float scale = m.scale * kDown;
     for (int done = 0; done < steps; done += together) {
         const int now = min(together, steps - done);
-        f32x16 acc, next;
-        small_product(acc, s, s.x, s.x, blocks);
-        small_write(s, s.gram, acc);
-        __syncthreads();
-        for (int i = 0; i < now; ++i) {
-            char *f = i == 0 ? s.total : s.factor;   // the first factor begins their product
-            small_product(acc, s, s.gram, s.gram, 2);
+        // A; then for every step its factor F (the first begins their product), the product of the factors, F A, and A of the next step, (F A) F
+#pragma unroll 1
+        for (int op = -1; op < 4 * now; ++op) {
+            const int i = op >> 2, kind = op < 0 ? -1 : op & 3;
+            if ((kind == 1 && i == 0) || (kind > 1 && i == now - 1)) continue;
+            char *f = i == 0 ? s.total : s.factor;
+            const char *p = kind < 0 ? s.x : kind == 0 || kind == 3 ? s.gram : f, *q = kind < 0 ? s.x : kind == 1 ? s.total : kind == 3 ? f : s.gram;
+            char *to = kind == 0 ? f : kind == 1 ? s.total : s.gram;
+            f32x16 acc;
+            small_product(acc, s, p, q, kind < 0 ? blocks : 2);
+            if (kind > 0) __syncthreads();   // it goes over an operand
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int at = small_four(s, r), row = 32 * (s.wave >> 1) + result_row(r, s.lane >> 5), col = 32 * (s.wave & 1) + (s.lane & 31);
-                const f16x4 high = *(const f16x4 *)(s.gram + at), low = *(const f16x4 *)(s.gram + at + kBlock * 2);
-                float v[4];
+                float v[4] = {acc[r] * kDown, acc[r + 1] * kDown, acc[r + 2] * kDown, acc[r + 3] * kDown};
+                if (kind == 0) {
+                    const f16x4 high = *(const f16x4 *)(s.gram + at), low = *(const f16x4 *)(s.gram + at + kBlock * 2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = fmaf(a.c, acc[r + e] * kDown, a.b * ((float)high[e] + (float)low[e]));
-                    if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
+                        if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                    }
                 }
-                small_put(f + at, v);
+                small_put(to + at, v);
             }
             __syncthreads();
-            if (i > 0) small_product(next, s, f, s.total, 2);
-            if (i < now - 1) small_product(acc, s, f, s.gram, 2);
-            __syncthreads();
-            if (i > 0) small_write(s, s.total, next);
-            if (i < now - 1) small_write(s, s.gram, acc);
-            __syncthreads();
-            if (i < now - 1) {
-                small_product(acc, s, s.gram, f, 2);
-                __syncthreads();
-                small_write(s, s.gram, acc);
-                __syncthreads();
-            }
         }
         // X, a block of 32 columns by a wave, in place
         const bool last = done + now == steps;
@@ -492,10 +531,10 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
             for (int part = 0; part < 2; ++part)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) y[part][k] = Step::cols<F16>(block + part * 4096, 16 * k, 0, s.lane);
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < 2; ++i) {
                 const int of = s.lane & 31, half = s.lane >> 5;
-                f32x16 z = {};
+                f32x16 z[3] = {};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     f16x8 x[2];
@@ -505,25 +544,25 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
                         const f16x4 lo = *(const f16x4 *)(row + (((2 * (k & 1)) ^ Step::fold(of)) << 4)), hi = *(const f16x4 *)(row + (((2 * (k & 1) + 1) ^ Step::fold(of)) << 4));
                         x[part] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                     }
-                    z = F16::mma(x[1], y[0][k], z);
-                    z = F16::mma(x[0], y[1][k], z);
-                    z = F16::mma(x[0], y[0][k], z);
+                    z[0] = F16::mma(x[1], y[0][k], z[0]);
+                    z[1] = F16::mma(x[0], y[1][k], z[1]);
+                    z[2] = F16::mma(x[0], y[0][k], z[2]);
+                }
+                z[0] = (z[0] + z[1]) + z[2];
+                if (last) {
+                    if (m.dtype == GBT_F32) small_result<float>(s, m, z[0], i, 32 * b + of);
+                    else if (m.dtype == GBT_BF16) small_result<__bf16>(s, m, z[0], i, 32 * b + of);
+                    else small_result<_Float16>(s, m, z[0], i, 32 * b + of);
+                    continue;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
-                    const int row = 32 * i + result_row(r, half), col = 32 * b + of;
-                    if (last) {
-                        if (col < m.w)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (row + e < m.p) put_element(m, m.tall ? (int64_t)col * m.cols + row + e : (int64_t)(row + e) * m.cols + col, z[r + e] * kDown * scale);
-                        continue;
-                    }
+                    const int row = 32 * i + result_row(r, half);
                     f16x4 high, low;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         _Float16 h, l;
-                        split(z[r + e] * kDown, h, l);
+                        split(z[0][r + e] * kDown, h, l);
                         high[e] = h, low[e] = l;
                     }
                     char *to = block + place(row + swap.quad, of & ~3, 32) * 2;
