@@ -68,9 +68,10 @@ SortLayout sort_layout(const gbt_embedding_params &p) {
     l.tiles = (int)((p.n_ids + l.tile - 1) / l.tile);
     EmbedArgs a;
     fill(a, p, nullptr, nullptr);
-    // Places that a group of lanes adds up: as many as leave some 8000 waves, within limits of what a run's beginnings and ends cost.
+    // Places that a group of lanes adds up: as many as leave some 4000 waves.  (us of the sums and of joining them for chunks of 16, 32, 64, 128: 900,000 ids
+    // of 12 rows of 64 elements 31 + 36, 25 + 21, 41 + 15, 78 + 11; 32,768 of 120,000 rows of 2048 225 + 24, 220 + 15, 266 + 12, 317 + 8.)
     const int64_t per_wave = 64 >> a.log_lanes;
-    l.chunk = std::min<int64_t>(64, std::max<int64_t>(16, p.n_ids * a.slabs / (8192 * per_wave)));
+    l.chunk = std::min<int64_t>(64, std::max<int64_t>(16, (p.n_ids * a.slabs / (4096 * per_wave) + 7) / 8 * 8));
     while ((p.n_ids + l.chunk - 1) / l.chunk * a.slabs > kMostWorkgroups) l.chunk *= 2;
     l.chunks = (p.n_ids + l.chunk - 1) / l.chunk;
     const size_t list = gbt_align((size_t)p.n_ids * 4);
@@ -333,13 +334,12 @@ const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
     return nullptr;
 }
 
-// Kinds of matrices, which are worked on apart: small or not, and with results of 32 bits or sixteen.
+// Kinds of matrices, which are worked on apart: small or not, and by the type of their results.
 int kind_of(const gbt_matrix &m) {
     const bool small = std::min(m.rows, m.cols) <= kOrthoSmallP && std::max(m.rows, m.cols) <= kOrthoSmallW;
-    return (small ? 0 : 2) + (m.dtype == GBT_F32 ? 0 : 1);
+    return (small ? 0 : 3) + m.dtype;
 }
-bool small_kind(int kind) { return kind < 2; }
-bool wide_kind(int kind) { return kind % 2 == 0; }
+bool small_kind(int kind) { return kind < 3; }
 
 // The matrices with elements in the order that they are worked on in: by kind, and of each kind those with the most to do first.
 struct OrthoOrder {
@@ -460,10 +460,14 @@ int64_t list_bytes_of(const gbt_matrix *matrices, const OrthoOrder &order) {
     while (next_group(matrices, order, &at, &g, nullptr)) tiles += g.tiles[0] + g.tiles[1] + g.tiles[2];
     return std::max<int64_t>(16, order.count * (int64_t)sizeof(OrthoMatrix) + tiles * (int64_t)sizeof(OrthoTile));
 }
-// Steps that are taken on A alone before X is multiplied: an error of A grows by the factor's square with each.
-int steps_together(double factor, bool wide) {
+// Steps that are taken on A alone before X is multiplied, for singular values' factors up to `factor`.  An error of A, some 2^-24 of it, grows by the
+// factor's square with each step where singular values are small, and makes a relative one of the result there.  (Singular values spread over 10^6, 16 x 16
+// and 512 x 512, five steps: float32, two at a time 9e-6 and 8e-6 off; float16, three 2.07e-4 and 2.07e-4, of which rounding the result is 2.0e-4;
+// bfloat16, five 7e-2 and 2.1e-3, of 1.6e-3, so sixteen bits take three too.)  And the product of the factors is held in float16 times 2^6.
+int steps_together(double factor, int dtype) {
+    const double growth = dtype == GBT_F32 ? 16.0 : 256.0;
     int n = 1;
-    while (n < 8 && pow(factor, n + 1) <= 200.0 && pow(factor * factor, n) <= (wide ? 16.0 : 256.0)) ++n;
+    while (n < 8 && pow(factor, n + 1) <= 800.0 && pow(factor * factor, n) <= growth) ++n;
     return n;
 }
 
@@ -559,7 +563,7 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.a = a;
         o.b = b;
         o.c = c;
-        const int together = steps_together(factor, wide_kind(g.kind));
+        const int together = steps_together(factor, g.kind % 3);
         if (small_kind(g.kind)) {
             GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, steps, together));
             continue;

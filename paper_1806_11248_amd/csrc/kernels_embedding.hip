@@ -209,6 +209,19 @@ __device__ __forceinline__ int64_t lower_bound(const uint32_t *keys, int64_t fro
     }
     return from;
 }
+// The same by a whole wave for one key, 64 places at a time: a step is a load's latency (of 900,000 four of them, not twenty).
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *keys, int64_t from, int64_t to, uint32_t key) {
+    const int lane = threadIdx.x & 63;
+    while (from < to) {
+        const int64_t step = (to - from + 63) / 64, at = from + lane * step;   // lane's place, the first of its stretch
+        const int less = __popcll(__ballot(at < to && keys[min(at, to - 1)] < key));
+        if (less == 0) return from;
+        // the first `less` stretches begin below the key, so the bound is in the last of them or right behind it
+        to = min(to, from + less * step);
+        from += (less - 1) * step + 1;
+    }
+    return from;
+}
 
 // Workgroups before the first `sums` clear rows without places, the others add up chunks.
 template <typename T, typename O, bool kVector>
@@ -219,7 +232,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, unsigne
         const int lane = threadIdx.x & 63;
         const int64_t row0 = ((int64_t)(blockIdx.x - sums) * 4 + (threadIdx.x >> 6)) * a.zero_rows, row1 = min(a.n_rows, row0 + a.zero_rows);
         if (row0 >= row1) return;
-        const int64_t lo = lower_bound(a.key, 0, a.n_ids, (uint32_t)row0), hi = lower_bound(a.key, lo, a.n_ids, (uint32_t)row1);
+        const int64_t lo = wave_lower_bound(a.key, 0, a.n_ids, (uint32_t)row0), hi = wave_lower_bound(a.key, lo, a.n_ids, (uint32_t)row1);
         bool without = false;
         if (row0 + lane < row1) {
             const int64_t at = lower_bound(a.key, lo, hi, (uint32_t)(row0 + lane));
@@ -253,14 +266,24 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, unsigne
         *(float4 *)to = float4{sum[0], sum[1], sum[2], sum[3]};
         *(float4 *)(to + 4) = float4{sum[4], sum[5], sum[6], sum[7]};
     };
+    uint32_t next_key[kAhead], next_place[kAhead];
+    auto fetch = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            next_key[u] = i + u < count ? keys[i + u] : none;
+            next_place[u] = i + u < count ? places[i + u] : 0;
+        }
+    };
+    fetch(0);
     for (int i = 0; i < count; i += kAhead) {
         uint32_t key[kAhead];
         float x[kAhead][8];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) key[u] = i + u < count ? keys[i + u] : none;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (key[u] != none) read_eight<O, kVector>(x[u], (const O *)a.out + (int64_t)places[i + u] * a.out_stride, l);
+        for (int u = 0; u < kAhead; ++u) {
+            key[u] = next_key[u];
+            if (key[u] != none) read_eight<O, kVector>(x[u], (const O *)a.out + (int64_t)next_place[u] * a.out_stride, l);
+        }
+        fetch(i + kAhead);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (key[u] == none) break;
@@ -305,26 +328,72 @@ __device__ __forceinline__ void shared_sum(float (&sum)[8], int log_lanes, int c
             for (int e = 0; e < 8; ++e) sum[e] += part[(g << log_lanes) + threadIdx.x][e];
 }
 
-// The run that begins in a chunk and goes on, if there is one: its parts, in the chunks' order.
+// The runs that begin in a chunk and go on: their parts, in the chunks' order.  Each of sixteen waves looks at a chunk; a run of up to kShortRun parts is its own
+// affair, a longer one all waves'.  (As long as a run has more chunks than waves look at, at most one of them begins here.)
+constexpr int kJoinWaves = 16, kShortRun = 16;
 template <typename T, bool kVector>
-__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a) {
-    __shared__ float shared[256][8];
-    const int chunk = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs;
-    const int64_t first = (int64_t)chunk * a.chunk, last = first + a.chunk - 1;   // a whole chunk, or it would have no next one
-    const uint32_t run = a.key[last];
-    if (run == (uint32_t)a.n_rows || a.key[last + 1] != run) return;
-    if (a.key[first] == run && first > 0 && a.key[first - 1] == run) return;
-    const int64_t end = lower_bound(a.key, last + 1, a.n_ids, run + 1);
-    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
-    const int64_t row = (int64_t)a.slabs * (8 << a.log_lanes), at = (int64_t)slab * (8 << a.log_lanes) + lane * 8;
-    float sum[8];
-    shared_sum(sum, a.log_lanes, (int)((end - 1) / a.chunk - chunk + 1), shared, [&](float (&x)[8], int i) {
-        const float *from = a.part + (int64_t)(chunk + i) * 2 * row + (i == 0 ? row : 0) + at;
+__global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(EmbedArgs a) {
+    __shared__ float shared[64 * kJoinWaves][8];
+    __shared__ int long_chunk, long_parts;
+    __shared__ uint32_t long_run;
+    const int slab = blockIdx.x % a.slabs, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t chunk = (int64_t)(blockIdx.x / a.slabs) * kJoinWaves + wave;
+    const int lanes = 1 << a.log_lanes, groups = 64 >> a.log_lanes;
+    const int64_t row = (int64_t)a.slabs * (8 << a.log_lanes), at = (int64_t)slab * (8 << a.log_lanes) + (lane & (lanes - 1)) * 8;
+    const Lane l(a, slab, lane & (lanes - 1));
+    if (threadIdx.x == 0) long_chunk = -1;
+    __syncthreads();
+    // how many parts the run that begins in this chunk has
+    auto parts_of = [&](int64_t c, uint32_t *run) -> int {
+        const int64_t first = c * a.chunk, last = first + a.chunk - 1;   // a whole chunk, or it would have no next one
+        const uint32_t before = a.key[max(first - 1, (int64_t)0)], begin = a.key[first], behind = a.key[last + 1];
+        *run = a.key[last];
+        if (*run == (uint32_t)a.n_rows || behind != *run) return 0;
+        if (begin == *run && first > 0 && before == *run) return 0;
+        return (int)((wave_lower_bound(a.key, last + 1, a.n_ids, *run + 1) - 1) / a.chunk - c + 1);
+    };
+    // part i of the run that begins in chunk c
+    auto add_part = [&](float (&sum)[8], int64_t c, int i) {
+        const float *from = a.part + (c + i) * 2 * row + (i == 0 ? row : 0) + at;
         const float4 lo = *(const float4 *)from, hi = *(const float4 *)(from + 4);
-        x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
-    });
-    const Lane l(a, slab, lane);
-    if (threadIdx.x < (1u << a.log_lanes) && l.some()) finish<T, kVector>(a, run, sum, l);
+        sum[0] += lo.x, sum[1] += lo.y, sum[2] += lo.z, sum[3] += lo.w, sum[4] += hi.x, sum[5] += hi.y, sum[6] += hi.z, sum[7] += hi.w;
+    };
+    // equal shares of the parts by `count` groups, of which this lane's is number `group`, to the first, in their order
+    auto join = [&](int64_t c, int parts, int group, int count, float (&sum)[8]) {
+        const int each = (parts + count - 1) / count, to = min(parts, (group + 1) * each);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+#pragma unroll 8
+        for (int i = group * each; i < to; ++i) add_part(sum, c, i);
+        return (parts + each - 1) / each;   // groups with a share
+    };
+    uint32_t run = 0;
+    const int parts = chunk < a.chunks - 1 ? parts_of(chunk, &run) : 0;
+    float sum[8];
+    if (parts > kShortRun) {
+        if (lane == 0) long_chunk = (int)chunk, long_parts = parts, long_run = run;
+    } else if (parts > 0) {
+        const int shares = join(chunk, parts, lane >> a.log_lanes, groups, sum);
+        for (int g = 1; g < shares; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __shfl(sum[e], (g << a.log_lanes) + (lane & (lanes - 1)));
+                if (lane < lanes) sum[e] += x;
+            }
+        if (lane < lanes && l.some()) finish<T, kVector>(a, run, sum, l);
+    }
+    __syncthreads();
+    const int c = long_chunk;
+    if (c < 0) return;
+    const int shares = join(c, long_parts, threadIdx.x >> a.log_lanes, groups * kJoinWaves, sum);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) shared[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x >= (unsigned)lanes) return;
+    for (int g = 1; g < shares; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += shared[(g << a.log_lanes) + threadIdx.x][e];
+    if (l.some()) finish<T, kVector>(a, long_run, sum, l);
 }
 
 // Few ids: a workgroup owns some rows of the table, and looks through all ids for theirs.  One launch, nothing sorted.
@@ -424,9 +493,9 @@ hipError_t gbt_launch_embedding_grad(hipStream_t stream, const EmbedArgs &a) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.chunks < 2) return e;
     by_type(a.table_dtype, [&](auto t) {
-        const unsigned grid = (unsigned)((a.chunks - 1) * a.slabs);
-        if (a.vector) embedding_join_kernel<decltype(t), true><<<grid, 256, 0, stream>>>(a);
-        else embedding_join_kernel<decltype(t), false><<<grid, 256, 0, stream>>>(a);
+        const unsigned grid = (unsigned)((a.chunks - 1 + kJoinWaves - 1) / kJoinWaves * a.slabs);
+        if (a.vector) embedding_join_kernel<decltype(t), true><<<grid, 64 * kJoinWaves, 0, stream>>>(a);
+        else embedding_join_kernel<decltype(t), false><<<grid, 64 * kJoinWaves, 0, stream>>>(a);
     });
     return hipGetLastError();
 }

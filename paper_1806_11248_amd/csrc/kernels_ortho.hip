@@ -3,13 +3,14 @@
 //
 // All F and A of one X commute: A after a step is F A F, so several steps are taken on the p x p matrices alone, and X is multiplied once by the product
 // of their factors.  That halves the work where X is wide, and costs nothing where it is square (a step on X is 1.5 w/p + 0.5 products of p x p x p, one on
-// A is 2; symmetric ones count half).  But an error of A grows by a^2 with each such step where singular values are small, so X is multiplied after two
-// steps where results have 32 bits, three where they have sixteen (gbt_tower.hip), and A taken anew.
+// A is 2; symmetric ones count half).  But an error of A grows by a^2 with each such step where singular values are small, so X is multiplied and A taken
+// anew after two steps where results have 32 bits, three where they have sixteen (gbt_tower.hip).
 //
 // Steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
 // between products, and matrix instructions on 32 bits run at a sixteenth of the rate.  Everything between products is held in two float16 parts, high
 // and low, 22 bits in all, and a product is three on the matrix units: high * high + high * low + low * high, added up in 32 bits.  All values are held times
-// 2^8: X's entries lie around 1 / sqrt(w), and so their low parts stay among float16's normal numbers.  The errors left are those of 32-bit products.
+// 2^8: X's entries lie around 1 / sqrt(w), and so their low parts stay among float16's normal numbers (the product of the factors times 2^6, as it grows).
+// The errors left are those of 32-bit products.
 //
 // All products have both operands' rows along the sum: X X^T, products of symmetric matrices, and F X = F (X^T)^T, for which X's transpose is kept beside it.
 // Of symmetric results the upper tiles are computed, and written twice.
@@ -19,6 +20,7 @@
 namespace {
 
 constexpr float kUp = 256.0f, kDown = 1.0f / 256.0f;   // of what is held in two parts
+constexpr float kUpTotal = 64.0f, kDownTotal = 1.0f / 64.0f;   // of the product of the factors, which grows to 800
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -337,6 +339,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
     const int first_row = ti * kOrthoTile + (kWaves == 4 ? wave >> 1 : wave >> 2) * 64, first_col = tj * kOrthoTile + (kWaves == 4 ? (wave & 1) * 64 : (wave & 3) * 32);
     const Exchange swap(lane);
     const float scale = m.scale * kDown;
+    // what the first factor, which lies as their product does, is an operand of
+    const float less = kApply || (a.first && (kProduct == kOrthoNext || (kProduct == kOrthoBoth && !second))) ? kDownTotal : kDown;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
                 const int row = first_row + 32 * i + result_row(r, lane >> 5), col = first_col + 32 * j + (lane & 31);
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * kDown;
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * less;
                 if (kProduct == kOrthoFactor) {
                     // A is symmetric: its four values of this column lie side by side in the row of that number
                     const _Float16 *from = p + place(col, row, m.pp);
@@ -355,6 +359,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
                     for (int e = 0; e < 4; ++e) {
                         v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
                         if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                        if (a.first) v[e] *= kUpTotal * kDown;
                     }
                 }
                 if (!kApply || !a.last) {
@@ -476,7 +481,7 @@ __device__ __forceinline__ void small_result(const Small &s, const OrthoMatrix &
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int row = first + result_row(r, 0);
-        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * kDown * scale);
+        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * kDownTotal * scale);
     }
 }
 
@@ -505,17 +510,19 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
             char *to = kind == 0 ? f : kind == 1 ? s.total : s.gram;
             f32x16 acc;
             small_product(acc, s, p, q, kind < 0 ? blocks : 2);
+            const float less = i == 0 && kind > 1 ? kDownTotal : kDown;
             if (kind > 0) __syncthreads();   // it goes over an operand
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int at = small_four(s, r), row = 32 * (s.wave >> 1) + result_row(r, s.lane >> 5), col = 32 * (s.wave & 1) + (s.lane & 31);
-                float v[4] = {acc[r] * kDown, acc[r + 1] * kDown, acc[r + 2] * kDown, acc[r + 3] * kDown};
+                float v[4] = {acc[r] * less, acc[r + 1] * less, acc[r + 2] * less, acc[r + 3] * less};
                 if (kind == 0) {
                     const f16x4 high = *(const f16x4 *)(s.gram + at), low = *(const f16x4 *)(s.gram + at + kBlock * 2);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
                         if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
+                        if (i == 0) v[e] *= kUpTotal * kDown;
                     }
                 }
                 small_put(to + at, v);
@@ -562,7 +569,7 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         _Float16 h, l;
-                        split(z[0][r + e] * kDown, h, l);
+                        split(z[0][r + e] * kDownTotal, h, l);
                         high[e] = h, low[e] = l;
                     }
                     char *to = block + place(row + swap.quad, of & ~3, 32) * 2;
