@@ -334,12 +334,28 @@ const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
     return nullptr;
 }
 
-// Kinds of matrices, which are worked on apart: small or not, and by the type of their results.
-int kind_of(const gbt_matrix &m) {
-    const bool small = std::min(m.rows, m.cols) <= kOrthoSmallP && std::max(m.rows, m.cols) <= kOrthoSmallW;
-    return (small ? 0 : 3) + m.dtype;
+// Kinds of matrices, which are worked on apart: small or not, and by how many steps are taken on A = X X^T alone before X is multiplied and A taken anew.
+//
+// An error of A grows by the square of the singular values' factor with each such step where singular values are small, and makes a relative one of the
+// result there, which rounding the result hides or does not.  (Five steps, averaged gradients: float32, one step at a time, two, and products of 32
+// bits in torch: 64 x 64 7e-7, 1.8e-6, 1.0e-6 off; 400 x 400 2.4e-6, 3.7e-6, 2.0e-6; 900 x 900 3.3e-6, 3.4e-6, 2.7e-6.  Singular values spread over 10^6,
+// 16 x 16: float16, three 2.07e-4, of which rounding the result is 2.00e-4; bfloat16, five 7e-2, of 1.6e-3.)
+enum OrthoKind { kSmallOne, kSmallSome, kOne, kTwo, kSome };
+OrthoKind kind_of(const gbt_matrix &m) {
+    const bool wide = m.dtype == GBT_F32;
+    const int64_t p = std::min(m.rows, m.cols), w = std::max(m.rows, m.cols);
+    if (p <= kOrthoSmallP && w <= kOrthoSmallW) return wide ? kSmallOne : kSmallSome;
+    return !wide ? kSome : p < 768 ? kOne : kTwo;
 }
-bool small_kind(int kind) { return kind < 3; }
+bool small_kind(OrthoKind kind) { return kind <= kSmallSome; }
+// For singular values' factors up to `factor`: errors of float32 results may grow by 2^4, of others by 2^8; and the product of the factors is held in
+// float16 times 2^6.
+int steps_together(double factor, OrthoKind kind) {
+    const double growth = kind == kTwo ? 16.0 : 256.0;
+    int n = 1;
+    while (kind != kSmallOne && kind != kOne && n < 8 && pow(factor, n + 1) <= 800.0 && pow(factor * factor, n) <= growth) ++n;
+    return n;
+}
 
 // The matrices with elements in the order that they are worked on in: by kind, and of each kind those with the most to do first.
 struct OrthoOrder {
@@ -407,7 +423,7 @@ int64_t lay_tiles(const gbt_matrix *matrices, const OrthoOrder &order, int64_t f
 // Matrices of one kind that are worked on together, and what they need.
 struct OrthoGroup {
     int64_t first, count;   // of the order
-    int kind;
+    OrthoKind kind;
     int64_t pieces, fill_tiles, tiles[3];   // tiles: by OrthoTiles
     size_t bytes;
 };
@@ -427,7 +443,7 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.pp = (int32_t)down * kOrthoTile;
         o.ww = (int32_t)across * kOrthoTile;
         const int64_t of_x = (int64_t)o.pp * o.ww * 4, of_a = (int64_t)o.pp * o.pp * 4, need = 3 * of_x + 5 * of_a;
-        const int kind = kind_of(m);
+        const OrthoKind kind = kind_of(m);
         if (g->count > 0 && (kind != g->kind || (!small_kind(kind) && (used + need > kGroupBytes || g->fill_tiles + fill > kMostWorkgroups)))) break;
         o.src = m.src;
         o.dst = m.dst;
@@ -460,17 +476,6 @@ int64_t list_bytes_of(const gbt_matrix *matrices, const OrthoOrder &order) {
     while (next_group(matrices, order, &at, &g, nullptr)) tiles += g.tiles[0] + g.tiles[1] + g.tiles[2];
     return std::max<int64_t>(16, order.count * (int64_t)sizeof(OrthoMatrix) + tiles * (int64_t)sizeof(OrthoTile));
 }
-// Steps that are taken on A alone before X is multiplied, for singular values' factors up to `factor`.  An error of A, some 2^-24 of it, grows by the
-// factor's square with each step where singular values are small, and makes a relative one of the result there.  (Singular values spread over 10^6, 16 x 16
-// and 512 x 512, five steps: float32, two at a time 9e-6 and 8e-6 off; float16, three 2.07e-4 and 2.07e-4, of which rounding the result is 2.0e-4;
-// bfloat16, five 7e-2 and 2.1e-3, of 1.6e-3, so sixteen bits take three too.)  And the product of the factors is held in float16 times 2^6.
-int steps_together(double factor, int dtype) {
-    const double growth = dtype == GBT_F32 ? 16.0 : 256.0;
-    int n = 1;
-    while (n < 8 && pow(factor, n + 1) <= 800.0 && pow(factor * factor, n) <= growth) ++n;
-    return n;
-}
-
 }  // namespace
 
 extern "C" size_t gbt_matrix_list_bytes(const gbt_matrix *matrices, int64_t n_matrices) {
@@ -563,7 +568,7 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.a = a;
         o.b = b;
         o.c = c;
-        const int together = steps_together(factor, g.kind % 3);
+        const int together = steps_together(factor, g.kind);
         if (small_kind(g.kind)) {
             GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, steps, together));
             continue;
