@@ -61,7 +61,7 @@ __device__ __forceinline__ Place place_of(const RotateArgs &a, int64_t row, int 
         }
         int64_t used = k1 - k0;
         if (a.k_len) used = min(used, (int64_t)a.k_len[seq]);
-        if (k0 < 0 || used < 0 || (a.store && k0 + used > a.out_rows)) used = 0;
+        if (k0 < 0 || k1 < k0 || used < 0 || (a.store && k0 + used > a.out_rows)) used = 0;   // (k1 < k0: their difference may have passed 64 bits)
         at += used - (q1 - q0);
         slot = k0, room = used;
     }

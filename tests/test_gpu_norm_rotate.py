@@ -169,7 +169,8 @@ def test_store_without_pointers(ctx):
 def test_store_pointers_that_lie_outside(ctx):
     """Slots beyond the store, negative ones and negative lengths hold no rows: nothing is written there, or anywhere."""
     q, k, v, wq, wk = _inputs(4, 2, 1, 16, BF16)
-    for slots, used in (([0, 5, 100, 105, 1 << 40], [5, 50, 5, 5]), ([-4, 0, -9, 5, 10], [4, 1, 3, -3]), ([9, 4, 4, 20, 20], [1, 1, 1, 1])):
+    for slots, used in (([0, 5, 100, 105, 1 << 40], [5, 50, 5, 5]), ([-4, 0, -9, 5, 10], [4, 1, 3, -3]), ([9, 4, 4, 20, 20], [1, 1, 1, 1]),
+                        ([3, -(1 << 63) + 1, 5, -(1 << 63), 4], [2, 2, 2, 2])):
         ks, vs = torch.full((12, 1, 16), 3.0, dtype=BF16, device="cuda"), torch.full((12, 1, 16), 3.0, dtype=BF16, device="cuda")
         ctx.norm_rotate(q, k, wq, wk, _turns(16), v=v, k_ptr=torch.tensor(slots).cuda(), k_len=torch.tensor(used, dtype=torch.int32).cuda(), k_out=ks, v_out=vs)
         written = (vs != 3.0).flatten(1).any(1)
@@ -179,6 +180,13 @@ def test_store_pointers_that_lie_outside(ctx):
                 assert torch.equal(vs[lo + n - 1], v[s])
                 written[lo + n - 1] = False
         assert not bool(written.any())
+        # and without lengths, where the differences of the last ones pass 64 bits
+        ks.fill_(3.0)
+        ctx.norm_rotate(q, k, wq, wk, _turns(16), k_ptr=torch.tensor(slots).cuda(), k_out=ks)
+        for s in range(4):
+            if 0 <= slots[s] < slots[s + 1] <= 12:
+                ks[slots[s + 1] - 1] = 3.0
+        assert bool((ks == 3.0).all())
 
 
 def test_in_place_and_parts_of_one_tensor(ctx):
