@@ -936,7 +936,9 @@ class Context:
         if not (isinstance(dout, torch.Tensor) and isinstance(ids, torch.Tensor) and dout.dim() >= 1 and dout.shape[:-1] in (ids.shape, (ids.numel(),))):
             raise TypeError("dout: expected a tensor [*ids.shape][width]")
         width = dout.shape[-1]
-        dout = dout if dout.dim() == 2 else dout.reshape(ids.numel(), width)
+        if dout.dim() != 2:
+            with self._on_stream((dout,)) or _NO_STREAM:   # it may be a copy
+                dout = dout.reshape(ids.numel(), width)
         of_out = _rows_of(dout, "dout", self.device)
         if out is not None:
             stride = _rows_of(out, "out", self.device, rows, width)

@@ -245,6 +245,27 @@ def test_another_stream(ctx):
         own.close()
 
 
+def test_a_gradient_that_has_to_be_copied_on_another_stream():
+    """A gradient of three axes that no view makes two of: its copy is the context's stream's work too, so what torch's own stream is busy with does not delay it."""
+    import paper_1806_11248_amd as g
+    side = torch.cuda.Stream()
+    own = g.Context(0, stream=side)
+    try:
+        ids = _ids(2000, 30, 0).view(50, 40).cuda()
+        dout = torch.randn(40, 50, 3, 64, device="cuda")[:, :, 1].transpose(0, 1)
+        whole, a = dout.contiguous(), torch.randn(4096, 4096, device="cuda")
+        torch.cuda.synchronize()
+        want = own.embedding_backward(whole, ids, 30)
+        side.synchronize()
+        for _ in range(20):
+            a = a @ a * 1e-4
+        got = own.embedding_backward(dout, ids, 30)
+        side.synchronize()
+        assert torch.equal(got, want)
+    finally:
+        own.close()
+
+
 def test_refusals(ctx):
     import paper_1806_11248_amd as g
     table, ids = torch.randn(5, 16, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
