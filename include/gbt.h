@@ -703,7 +703,7 @@ GBT_API int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_par
  */
 typedef struct gbt_matrix {      /* rows x cols elements, one row after the other, any alignment of its type */
     const void *src;             /* [dev] */
-    void *dst;                   /* [dev] may be src; overlaps no other matrix's src or dst */
+    void *dst;                   /* [dev] may be src; overlaps nothing else of the matrices' (gbt_matrix_list: GBT_EINVAL) */
     int64_t rows, cols;          /* 0..2^20, the smaller one 0..2^15 */
     int32_t dtype;               /* GBT_F32, GBT_BF16, GBT_F16 */
     float scale;

@@ -1062,7 +1062,8 @@ class Context:
 
     def matrix_list(self, tensors, outs=None, *, scales=1.0) -> MatrixList:
         """Lays matrices [rows][cols] out for orthogonalise; outs receive the results (None: the tensors themselves), times scales (one for
-        each, or one for all).  Good for as long as the tensors stay where they are, as a gradient_list is."""
+        each, or one for all).  Good for as long as the tensors stay where they are, as a gradient_list is.  No out may share memory with another matrix, nor
+        with part of its own."""
         tensors = list(tensors)
         outs = tensors if outs is None else list(outs)
         scales = [float(scales)] * len(tensors) if isinstance(scales, (int, float)) else [float(x) for x in scales]

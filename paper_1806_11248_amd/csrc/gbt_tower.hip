@@ -375,6 +375,32 @@ struct OrthoOrder {
     OrthoOrder(const OrthoOrder &) = delete;
     OrthoOrder &operator=(const OrthoOrder &) = delete;
 };
+// Does a result lie over another matrix's memory, or over its own source but for the same place?  -1: no host memory to find out.
+int results_overlap(const gbt_matrix *m, const OrthoOrder &order) {
+    struct Span {
+        uintptr_t begin, end;
+        bool written;
+    };
+    Span *span = new (std::nothrow) Span[(size_t)std::max<int64_t>(1, 2 * order.count)];
+    if (!span) return -1;
+    int64_t n = 0;
+    for (int64_t i = 0; i < order.count; ++i) {
+        const gbt_matrix &x = m[order.at[i]];
+        const uintptr_t bytes = (uintptr_t)(x.rows * x.cols * size_of(x.dtype)), dst = (uintptr_t)x.dst, src = (uintptr_t)x.src;
+        span[n++] = Span{dst, dst + bytes, true};
+        if (src != dst) span[n++] = Span{src, src + bytes, false};
+    }
+    std::sort(span, span + n, [](const Span &x, const Span &y) { return x.begin < y.begin; });
+    uintptr_t end = 0, end_written = 0;   // of the spans so far, of the written ones
+    int overlap = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        overlap |= span[i].begin < (span[i].written ? end : end_written);
+        end = std::max(end, span[i].end);
+        if (span[i].written) end_written = std::max(end_written, span[i].end);
+    }
+    delete[] span;
+    return overlap;
+}
 int64_t tiles_of(int64_t side) { return (side + kOrthoTile - 1) / kOrthoTile; }
 
 enum OrthoTiles { kTilesGram, kTilesSym, kTilesFull };   // of X X^T; of products of symmetric matrices; of F X
@@ -494,6 +520,9 @@ extern "C" int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int
     GBT_REQUIRE(ctx, !fault, code, "%s", fault);
     const OrthoOrder order(matrices, n_matrices);
     GBT_REQUIRE(ctx, order.at, GBT_ENOMEM, "no host memory for the list");
+    const int overlap = results_overlap(matrices, order);
+    GBT_REQUIRE(ctx, overlap >= 0, GBT_ENOMEM, "no host memory for the list");
+    GBT_REQUIRE(ctx, overlap == 0, GBT_EINVAL, "a matrix's dst overlaps another matrix, or its own src in part");
     const size_t need = (size_t)list_bytes_of(matrices, order);
     GBT_REQUIRE(ctx, list_bytes >= need, GBT_ENOMEM, "list of %zu bytes, %zu needed", list_bytes, need);
     char *table = new (std::nothrow) char[need];

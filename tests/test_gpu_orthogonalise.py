@@ -184,6 +184,21 @@ def test_a_list_keeps_its_memory(ctx):
     assert torch.equal(held, want) and bool((o == 6.0).all()) and all(bool((x == 9.0).all()) for x in others)
 
 
+def test_results_over_one_another_are_refused(ctx):
+    import paper_1806_11248_amd as g
+    flat = torch.ones(4000, device="cuda")
+    a, b, near = flat[:1000].view(20, 50), flat[1000:2000].view(20, 50), flat[980:1980].view(20, 50)
+    for tensors, outs in (([a, a], [a, a]), ([a, b], [b, a]), ([a, b], [near, b]), ([near], [b]), ([a, b], [flat[2000:3000].view(20, 50), flat[2999:3999].view(20, 50)]),
+                          ([b, a, near], [b, flat[2000:3000].view(20, 50), flat[3000:].view(20, 50)])):
+        with pytest.raises(g.GbtError) as e:
+            ctx.matrix_list(tensors, outs)
+        assert e.value.code == g.binding.EINVAL
+    # the same matrix read by two, and neighbours
+    ctx.matrix_list([a, a, near], [flat[2000:3000].view(20, 50), flat[3000:].view(20, 50), torch.ones_like(near)])
+    ctx.matrix_list([a, b])
+    assert bool((flat == 1).all())
+
+
 def test_refusals(ctx):
     import paper_1806_11248_amd as g
     t = torch.ones(10, 10, device="cuda")
