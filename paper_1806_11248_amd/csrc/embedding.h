@@ -20,9 +20,12 @@ struct EmbedArgs {
     const uint32_t *key, *pos;         // sorted ids (n_rows: outside the table) and their places
     float *part;                       // [chunks][2][slabs * (8 << log_lanes)]: sums of runs that go on in other chunks
     int zero_rows;                     // rows that a workgroup of the few-ids kernel owns, or that a wave clears
+    // backward, few rows: a wave adds up `chunk` places, part is [chunks][n_rows][8 << log_lanes]; one slab
+    uint32_t *seen;                    // [chunks]: the rows that it met, a bit for each
 };
 
 constexpr int kEmbedFewIds = 2048;     // more than that are sorted
+constexpr int kEmbedFewRows = 32;      // up to so many are added up in LDS, unsorted
 constexpr int kSortItems = 4096;       // ids that a workgroup of the sort ranks at a time
 constexpr int kSortTiles = 256;        // workgroups of a pass at most
 constexpr int kSortDigits = 1024;      // of a pass at most
@@ -39,4 +42,5 @@ struct SortPass {
 hipError_t gbt_launch_embedding(hipStream_t stream, const EmbedArgs &a);
 hipError_t gbt_launch_sort_pass(hipStream_t stream, const SortPass &p);
 hipError_t gbt_launch_embedding_grad(hipStream_t stream, const EmbedArgs &a);       // of sorted ids
+hipError_t gbt_launch_embedding_grad_rows(hipStream_t stream, const EmbedArgs &a);  // of few rows
 hipError_t gbt_launch_embedding_grad_few(hipStream_t stream, const EmbedArgs &a);

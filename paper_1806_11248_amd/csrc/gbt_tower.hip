@@ -82,6 +82,27 @@ SortLayout sort_layout(const gbt_embedding_params &p) {
     return l;
 }
 
+// Few rows are added up in LDS, up to a width of which a wave takes two places at once: wider ones wait for too many additions behind one another.  (us, bfloat16,
+// of 32 rows in LDS and 33 sorted: 900,000 places of 64 elements 52 and 59, of 8 16 and 87; 10,000 of 64 12 and 26; 2,100 of 256 17 and 22, 30,000 30 and
+// 28, 200,000 57 and 56; 30,000 of 512 42 and 31.  Of 12 rows the first takes 37, and took 86 sorted.)
+bool takes_few_rows(const gbt_embedding_params &p) { return !takes_few_ids(p) && p.n_rows <= kEmbedFewRows && p.width <= 256 && p.n_rows > 0 && p.n_ids > 0; }
+// By up to four waves on a compute unit, as many as its LDS takes (three for 24 rows, two for 32), of at least 16 places for each group of lanes.
+struct RowsLayout {
+    int64_t chunk, chunks;
+    size_t seen, bytes;
+};
+RowsLayout rows_layout(const gbt_embedding_params &p) {
+    RowsLayout l;
+    EmbedArgs a;
+    fill(a, p, nullptr, nullptr);
+    const int64_t waves = 256 * std::min<int64_t>(4, 80 / p.n_rows), step = 8 * (64 >> a.log_lanes);
+    l.chunk = (std::max((p.n_ids + waves - 1) / waves, 2 * step) + step - 1) / step * step;
+    l.chunks = (p.n_ids + l.chunk - 1) / l.chunk;
+    l.seen = (size_t)l.chunks * p.n_rows * (8 << a.log_lanes) * 4;
+    l.bytes = l.seen + gbt_align((size_t)l.chunks * 4);
+    return l;
+}
+
 }  // namespace
 
 extern "C" int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *params, const void *table, void *out) {
@@ -105,7 +126,7 @@ extern "C" int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *param
 extern "C" size_t gbt_embedding_backward_workspace_bytes(const gbt_embedding_params *params) {
     int32_t code;
     if (!params || embedding_fault(*params, &code) || takes_few_ids(*params) || params->n_ids == 0) return 0;
-    return sort_layout(*params).bytes;
+    return takes_few_rows(*params) ? rows_layout(*params).bytes : sort_layout(*params).bytes;
 }
 
 extern "C" int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_params *params, const void *dout, void *grad, int32_t accumulate,
@@ -131,6 +152,15 @@ extern "C" int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_para
     if (takes_few_ids(p)) {
         a.zero_rows = (int)((p.n_rows + kFewRowsWorkgroups - 1) / kFewRowsWorkgroups);
         GBT_HIP(ctx, gbt_launch_embedding_grad_few(ctx->stream, a));
+        return GBT_OK;
+    }
+    if (takes_few_rows(p)) {
+        const RowsLayout l = rows_layout(p);
+        a.part = (float *)workspace;
+        a.seen = (uint32_t *)((char *)workspace + l.seen);
+        a.chunk = (int)l.chunk;
+        a.chunks = (int)l.chunks;
+        GBT_HIP(ctx, gbt_launch_embedding_grad_rows(ctx->stream, a));
         return GBT_OK;
     }
     // rows that a wave clears: as many as leave some 8000 waves

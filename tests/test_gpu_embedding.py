@@ -77,7 +77,9 @@ def test_lookup(ctx, places, rows, width, types):
 
 # few ids, up to the last number of them that are not sorted and the first that are; many; one or two passes of digits, or three; chunks that end inside runs
 SIZES = [(1, 1, 8), (2, 5, 1), (33, 9, 24), (1999, 40, 64), (2048, 3, 100), (2048, 5000, 16), (2049, 3, 100), (2049, 5000, 16), (4097, 1, 8), (9_000, 1023, 33),
-         (9_000, 1024, 40), (20_000, 12, 64), (12_289, 70_000, 12), (8_193, 2_000_000, 3), (5_000, 600, 1032)]
+         (9_000, 1024, 40), (20_000, 12, 64), (12_289, 70_000, 12), (8_193, 2_000_000, 3), (5_000, 600, 1032),
+         # the most rows and columns that are added up in LDS, one more; groups of lanes that have no place
+         (30_000, 32, 24), (30_000, 33, 24), (2_500, 31, 1), (5_000, 7, 256), (3_000, 32, 250), (3_000, 32, 257), (2_049, 32, 8), (100_003, 12, 64), (5_000, 7, 1032)]
 
 
 @pytest.mark.parametrize("places,rows,width", SIZES)
@@ -162,7 +164,7 @@ def test_what_is_not_finite_stays_in_its_row(ctx):
         dout[8, 3] = math.inf
         got = ctx.embedding_backward(dout, ids.cuda(), 100)
         assert bool(got[7].isnan().all()) and bool((got[8, 3] == math.inf)) and bool(got[9:].isfinite().all()) and bool(got[:7].isfinite().all())
-        ids[7] = ids[8] = -1                                                   # padded places are not read
+        ids[7] = ids[8] = -1                                                   # padded places do not count
         assert bool(ctx.embedding_backward(dout, ids.cuda(), 100).isfinite().all())
 
 
