@@ -337,6 +337,12 @@ def _heads(t, name, dtype, shape=None):
     return Heads(t.data_ptr(), row if n > 1 else h * d, head if h > 1 else d)     # an axis of one element has no stride to speak of
 
 
+def _new_heads(like, shape):
+    """A tensor of that shape, and its gbt_heads."""
+    t = like.new_empty(shape)
+    return t, Heads(t.data_ptr(), shape[1] * shape[2], shape[2])
+
+
 class GradientList:
     """Tensors laid out for Context.clip_gradients; holds on to them, and to the memory that they had then."""
 
@@ -964,18 +970,23 @@ class Context:
         if not (isinstance(q, torch.Tensor) and q.dim() == 3 and isinstance(k, torch.Tensor) and k.dim() == 3 and q.device == self.device):
             raise TypeError(f"q, k: expected tensors [rows][heads][head_dim] on {self.device}")
         rows, heads, dim = q.shape
-        counts = [x.numel() - less for x, less, dtype, name in ((q_ptr, 1, torch.int64, "q_ptr"), (k_ptr, 1, torch.int64, "k_ptr"), (k_len, 0, torch.int32, "k_len"))
-                  if x is not None and _need(x, dtype, name) is x]
+        counts = []
+        if q_ptr is not None:
+            counts.append(_need(q_ptr, torch.int64, "q_ptr").numel() - 1)
+        if k_ptr is not None:
+            counts.append(_need(k_ptr, torch.int64, "k_ptr").numel() - 1)
+        if k_len is not None:
+            counts.append(_need(k_len, torch.int32, "k_len").numel())
         n_seq = counts[0] if counts else 1
-        if any(n != n_seq for n in counts):
+        if len(counts) > 1 and any(n != n_seq for n in counts):
             raise TypeError("q_ptr, k_ptr and k_len do not describe the same number of sequences")
         if q_ptr is None and n_seq > 0 and rows % n_seq:
             raise TypeError(f"q: without q_ptr all of {n_seq} sequences have the same length")
         if store_rows is not None and k_ptr is None and n_seq > 0 and store_rows % n_seq:
             raise TypeError(f"k_out: without k_ptr all of {n_seq} slots have the same length")
-        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None and _need(w, torch.float32, name).shape != (dim,):
-                raise TypeError(f"{name}: expected [{dim}]")
+        if q_weight is not None and _need(q_weight, torch.float32, "q_weight").shape != (dim,) or \
+                k_weight is not None and _need(k_weight, torch.float32, "k_weight").shape != (dim,):
+            raise TypeError(f"q_weight, k_weight: expected [{dim}]")
         turned = 0
         if turns is not None:
             if _need(turns, torch.float64, "turns").dim() != 1:
@@ -988,9 +999,9 @@ class Context:
                 wide = 8
             if _need(positions, positions.dtype, "positions").shape != (rows,):
                 raise TypeError(f"positions: expected [{rows}]")
-        at = [None if x is None else x.data_ptr() for x in (q_ptr, k_ptr, k_len, positions, q_weight, k_weight, turns)]
         return NormRotateParams(DTYPES.get(q.dtype, -1), heads, k.shape[1], dim, turned, bool(halves), store_rows is not None, n_seq, wide, eps, rows,
-                                rows if store_rows is None else store_rows, *at)
+                                rows if store_rows is None else store_rows,
+                                *[None if x is None else x.data_ptr() for x in (q_ptr, k_ptr, k_len, positions, q_weight, k_weight, turns)])
 
     def norm_rotate(self, q, k, q_weight, k_weight, turns, *, v=None, q_ptr=None, k_ptr=None, k_len=None, positions=None, eps=1e-6, halves=True,
                     q_out=None, k_out=None, v_out=None):
@@ -1018,17 +1029,13 @@ class Context:
         hq, hk = _heads(q, "q", dtype, of_q), _heads(k, "k", dtype, of_k)
         hv = None if v is None else _heads(v, "v", dtype, of_k)
         with self._on_stream((q, k, v, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, q_out, k_out, v_out)) or _NO_STREAM:
-            if q_out is None:
-                q_out = q.new_empty(of_q)
-            if k_out is None:
-                k_out = q.new_empty(of_k)
-            if v is not None and v_out is None:
-                v_out = q.new_empty(of_k)
-        hq_out, hk_out = _heads(q_out, "q_out", dtype, of_q), _heads(k_out, "k_out", dtype, of_out)
+            q_out, hq_out = _new_heads(q, of_q) if q_out is None else (q_out, _heads(q_out, "q_out", dtype, of_q))
+            k_out, hk_out = _new_heads(q, of_k) if k_out is None else (k_out, _heads(k_out, "k_out", dtype, of_out))
+            if v is not None:
+                v_out, hv_out = _new_heads(q, of_k) if v_out is None else (v_out, _heads(v_out, "v_out", dtype, of_out))
         if v is None:
             st = self.lib.gbt_norm_rotate(self.h, C.byref(p), C.byref(hq), C.byref(hk), None, C.byref(hq_out), C.byref(hk_out), None)
         else:
-            hv_out = _heads(v_out, "v_out", dtype, of_out)
             st = self.lib.gbt_norm_rotate(self.h, C.byref(p), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hq_out), C.byref(hk_out), C.byref(hv_out))
         if st:
             self._check(st)
@@ -1047,18 +1054,16 @@ class Context:
         hdq_out, hdk_out = _heads(dq_out, "dq_out", dtype, of_q), _heads(dk_out, "dk_out", dtype, of_k)
         ws_bytes = self.lib.gbt_norm_rotate_backward_workspace_bytes(C.byref(p))
         with self._on_stream((dq_out, dk_out, q, k, q_weight, k_weight, turns, q_ptr, k_ptr, k_len, positions, dq, dk)) or _NO_STREAM:
-            if dq is None:
-                dq = q.new_empty(of_q)
-            if dk is None:
-                dk = q.new_empty(of_k)
+            dq, hdq = _new_heads(q, of_q) if dq is None else (dq, _heads(dq, "dq", dtype, of_q))
+            dk, hdk = _new_heads(q, of_k) if dk is None else (dk, _heads(dk, "dk", dtype, of_k))
             weights = q.new_empty((2, dim), dtype=torch.float32)
             ws = self._scratch("norm_rotate", ws_bytes)
-        hdq, hdk = _heads(dq, "dq", dtype, of_q), _heads(dk, "dk", dtype, of_k)
+        of_weights = weights.data_ptr()
         st = self.lib.gbt_norm_rotate_backward(self.h, C.byref(p), C.byref(hdq_out), C.byref(hdk_out), C.byref(hq), C.byref(hk), C.byref(hdq), C.byref(hdk),
-                                               weights.data_ptr(), weights.data_ptr() + 4 * dim, ws.data_ptr(), ws.numel())
+                                               of_weights, of_weights + 4 * dim, ws.data_ptr(), ws_bytes)
         if st:
             self._check(st)
-        return dq, dk, weights[0], weights[1]
+        return (dq, dk, *weights.unbind(0))
 
     def matrix_list(self, tensors, outs=None, *, scales=1.0) -> MatrixList:
         """Lays matrices [rows][cols] out for orthogonalise; outs receive the results (None: the tensors themselves), times scales (one for
