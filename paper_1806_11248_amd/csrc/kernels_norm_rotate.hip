@@ -19,6 +19,7 @@ struct alignas(8) Four {
 struct Place {
     int64_t store;       // the row of k_out and v_out, -1: none
     int64_t position;
+    int64_t first, behind;   // the sequence's rows
     bool there;          // a row of a sequence
 };
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ Place place_of(const RotateArgs &a, int64_t row, int 
     Place p;
     int64_t q0, q1;
     if (a.n_seq == 0) {
-        p.store = a.store ? -1 : row, p.position = 0, p.there = false;
+        p.store = a.store ? -1 : row, p.position = p.first = p.behind = 0, p.there = false;
         return p;
     }
     if (a.q_ptr) {
@@ -50,6 +51,7 @@ __device__ __forceinline__ Place place_of(const RotateArgs &a, int64_t row, int 
         q0 = seq * each, q1 = q0 + each;
     }
     p.there = q0 >= 0 && q1 <= a.rows && row >= q0 && row < q1;
+    p.first = q0, p.behind = q1;
     int64_t at = row - q0, slot = 0, room = 0;
     if (a.slots) {
         int64_t k0, k1;
@@ -276,73 +278,82 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a) {
     }
 }
 
-// The gradients of q or k of an item's rows, and what they add to the weight's.
-template <typename E, bool kHalves, int LOG, bool kSide>
-__device__ __forceinline__ void turn_back(const RotateArgs &a, const Stream<LOG, kSide> &st, const Part &part, const AttnView &in, const AttnView &back,
-                                          const AttnView &out, int64_t row0, const Place &place, const Turn &turn, const float (&w)[8], float (&dw)[8]) {
-    constexpr int kAhead = 2;
-    const float each = 1.0f / a.dim;
-    const char *src = in.data + row0 * in.row * 2, *of_out = back.data + row0 * back.row * 2;
-    char *dst = out.data + row0 * out.row * 2;
-    const int64_t src_lane = st.offset(in), back_lane = st.offset(back), dst_lane = st.offset(out);
-    const int passes = st.passes();
-    for (int pass0 = 0; pass0 < passes; pass0 += kAhead) {
-        Raw<E> of_x[kAhead], of_g[kAhead];
-#pragma unroll
-        for (int b = 0; b < kAhead; ++b)
-            if (pass0 + b < passes && st.live(a, row0, pass0 + b)) {
-                of_x[b].read(src + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
-                of_g[b].read(of_out + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * back.head * 2 + back_lane, part);
-            }
-#pragma unroll
-        for (int b = 0; b < kAhead; ++b) {
-            if (pass0 + b >= passes) break;
-            const bool live = st.live(a, row0, pass0 + b);
-            float x[8], d[8], g[8], u[8], squares = 0.0f, along = 0.0f;
-            of_x[b].to(x, live && place.there);
-            of_g[b].to(d, live && place.there);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float da = d[first_of<kHalves>(i)], db = d[second_of<kHalves>(i)];
-                g[first_of<kHalves>(i)] = fmaf(da, turn.cos[i], db * turn.sin[i]);
-                g[second_of<kHalves>(i)] = fmaf(db, turn.cos[i], -da * turn.sin[i]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                u[e] = g[e] * w[e];
-                squares = fmaf(x[e], x[e], squares);
-                along = fmaf(x[e], u[e], along);
-            }
-            squares = line_sum<LOG>(squares);
-            along = line_sum<LOG>(along);
-            // (of no row: zeros, also where eps is zero)
-            const float s = live && place.there ? __builtin_amdgcn_rsqf(fmaf(squares, each, a.eps)) : 0.0f;
-            const float less = along * each * s * s;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                dw[e] = fmaf(g[e], x[e] * s, dw[e]);
-                u[e] = s * fmaf(x[e], -less, u[e]);
-            }
-            if (live) write_parts<E>(dst + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, u, part);
-        }
-    }
-}
-
-// All rows' heads of q or of k by `blocks` workgroups, of which this one is number `block`.
+// The gradients of all rows' heads of q or of k by `blocks` workgroups, of which this one is number `block`, and what they add to the weight's.  A wave's rows lie side by
+// side, so that it looks a sequence up once; while it works on a pass, the next one's elements are under way, across rows too.
+// (30,141 rows of 32 and 8 heads of 128: 201 us, 4.6 TB/s; two passes at a time of rows far apart 221.)
 template <typename E, bool kHalves, int LOG, bool kSide>
 __device__ __forceinline__ void turn_all_back(const RotateArgs &a, int heads, int row_group, const AttnView &in, const AttnView &back, const AttnView &out,
                                               const float *weight, int block, int blocks, const Part &part, float (&dw)[8]) {
+    constexpr int kAtOnce = Stream<LOG, kSide>::kAtOnce;
     const Stream<LOG, kSide> st(heads, row_group, part);
     double turns[4];
     float w[8];
     read_turns(turns, a, part);
     read_weight(w, weight, part);
-    const int64_t items = (a.rows + row_group - 1) / row_group;
-    for (int64_t item = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)); item < items; item += (int64_t)blocks * 4) {
-        const Place place = place_for<kSide>(a, item * row_group, st.row_off);
-        Turn turn;
-        turn.set(part, turns, place.position);
-        turn_back<E, kHalves, LOG, kSide>(a, st, part, in, back, out, item * row_group, place, turn, w, dw);
+    const float each = 1.0f / a.dim;
+    const int64_t src_lane = st.offset(in), back_lane = st.offset(back), dst_lane = st.offset(out);
+    const int passes = st.passes();
+    const int64_t items = (a.rows + row_group - 1) / row_group, waves = (int64_t)blocks * 4;
+    const int64_t wave = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6)), all = items / waves, more = items % waves;
+    int64_t row0 = (wave * all + min(wave, more)) * row_group;
+    const int64_t to = row0 + (all + (wave < more)) * row_group;
+    Place place = {};
+    Turn turn;
+    struct Pass {
+        int64_t row0;
+        int pass;
+        Raw<E> of_x, of_g;
+    } even, odd;
+    int pass = 0;
+    auto fetch = [&](Pass &p) {   // the next one; there need not be one
+        p.row0 = row0, p.pass = pass;
+        if (row0 < to && st.live(a, row0, pass)) {
+            p.of_x.read(in.data + row0 * in.row * 2 + (int64_t)pass * kAtOnce * in.head * 2 + src_lane, part);
+            p.of_g.read(back.data + row0 * back.row * 2 + (int64_t)pass * kAtOnce * back.head * 2 + back_lane, part);
+        }
+        if (++pass == passes) pass = 0, row0 += row_group;
+    };
+    auto work = [&](const Pass &p) {
+        if (p.row0 >= to) return;
+        if (p.pass == 0) {
+            if (!kSide && !a.positions && place.there && p.row0 < place.behind) ++place.position;   // the row behind the last one
+            else place = place_for<kSide>(a, p.row0, st.row_off);
+            turn.set(part, turns, place.position);
+        }
+        const bool live = st.live(a, p.row0, p.pass);
+        float x[8], d[8], g[8], u[8], squares = 0.0f, along = 0.0f;
+        p.of_x.to(x, live && place.there);
+        p.of_g.to(d, live && place.there);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float da = d[first_of<kHalves>(i)], db = d[second_of<kHalves>(i)];
+            g[first_of<kHalves>(i)] = fmaf(da, turn.cos[i], db * turn.sin[i]);
+            g[second_of<kHalves>(i)] = fmaf(db, turn.cos[i], -da * turn.sin[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u[e] = g[e] * w[e];
+            squares = fmaf(x[e], x[e], squares);
+            along = fmaf(x[e], u[e], along);
+        }
+        squares = line_sum<LOG>(squares);
+        along = line_sum<LOG>(along);
+        // (of no row: zeros, also where eps is zero)
+        const float s = live && place.there ? __builtin_amdgcn_rsqf(fmaf(squares, each, a.eps)) : 0.0f;
+        const float less = along * each * s * s;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            dw[e] = fmaf(g[e], x[e] * s, dw[e]);
+            u[e] = s * fmaf(x[e], -less, u[e]);
+        }
+        if (live) write_parts<E>(out.data + p.row0 * out.row * 2 + (int64_t)p.pass * kAtOnce * out.head * 2 + dst_lane, u, part);
+    };
+    fetch(even);
+    while (even.row0 < to) {
+        fetch(odd);
+        work(even);
+        fetch(even);
+        work(odd);
     }
 }
 
@@ -352,15 +363,13 @@ __global__ __launch_bounds__(256, 4) void norm_rotate_grad_kernel(RotateArgs a) 
     __shared__ float shared[4][kRotateDim];
     const Part part(a, threadIdx.x & ((1 << LOG) - 1));
     float dw[8] = {};
-    const int block = blockIdx.x - a.q_blocks;
-    if (block < 0) {
-        if (a.row_group > 1) turn_all_back<E, kHalves, LOG, true>(a, a.heads, a.row_group, a.q, a.q_out, a.dq, a.q_weight, blockIdx.x, a.q_blocks, part, dw);
-        else turn_all_back<E, kHalves, LOG, false>(a, a.heads, 1, a.q, a.q_out, a.dq, a.q_weight, blockIdx.x, a.q_blocks, part, dw);
-    } else {
-        const int blocks = a.blocks - a.q_blocks;
-        if (a.k_row_group > 1) turn_all_back<E, kHalves, LOG, true>(a, a.kv_heads, a.k_row_group, a.k, a.k_out, a.dk, a.k_weight, block, blocks, part, dw);
-        else turn_all_back<E, kHalves, LOG, false>(a, a.kv_heads, 1, a.k, a.k_out, a.dk, a.k_weight, block, blocks, part, dw);
-    }
+    const bool of_q = (int)blockIdx.x < a.q_blocks;
+    const int block = of_q ? blockIdx.x : blockIdx.x - a.q_blocks, blocks = of_q ? a.q_blocks : a.blocks - a.q_blocks;
+    const int heads = of_q ? a.heads : a.kv_heads, row_group = of_q ? a.row_group : a.k_row_group;
+    const AttnView in = of_q ? a.q : a.k, back = of_q ? a.q_out : a.k_out, out = of_q ? a.dq : a.dk;
+    const float *weight = of_q ? a.q_weight : a.k_weight;
+    if (row_group > 1) turn_all_back<E, kHalves, LOG, true>(a, heads, row_group, in, back, out, weight, block, blocks, part, dw);
+    else turn_all_back<E, kHalves, LOG, false>(a, heads, 1, in, back, out, weight, block, blocks, part, dw);
     // the weight's gradient: over the lines of a wave, then the workgroup's waves
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
