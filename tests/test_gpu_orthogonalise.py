@@ -8,7 +8,7 @@ from tower_ref import TINY, U, newton_schulz
 
 pytestmark = pytest.mark.gpu
 
-MUON = (3.4445, -4.7750, 2.0315)
+QUINTIC = (3.4445, -4.7750, 2.0315)
 CUBIC = (1.5, -0.5, 0.0)
 
 
@@ -27,7 +27,7 @@ def _matrix(m, n, seed, dtype=torch.float32, size=1e-3):
     return (g * size).to(dtype).cuda()
 
 
-def _check(ctx, updates, steps=5, coefficients=MUON, scales=1.0, outs=None):
+def _check(ctx, updates, steps=5, coefficients=QUINTIC, scales=1.0, outs=None):
     before = [u.cpu() for u in updates]
     lst = ctx.matrix_list(updates, outs, scales=scales)
     got = ctx.orthogonalise(lst, steps=steps, coefficients=coefficients)
@@ -58,7 +58,7 @@ def test_shapes(ctx, m, n, dtype):
     _check(ctx, [u], outs=[torch.full_like(u, 9.0)], scales=0.2)
 
 
-@pytest.mark.parametrize("steps,coefficients", [(1, MUON), (2, MUON), (3, MUON), (10, MUON), (8, CUBIC), (1, (1.0, 0.0, 0.0)), (4, (2.0, -1.5, 0.5))])
+@pytest.mark.parametrize("steps,coefficients", [(1, QUINTIC), (2, QUINTIC), (3, QUINTIC), (10, QUINTIC), (8, CUBIC), (1, (1.0, 0.0, 0.0)), (4, (2.0, -1.5, 0.5))])
 def test_steps_and_coefficients(ctx, steps, coefficients):
     _check(ctx, [_matrix(70, 150, 1), _matrix(64, 32, 2)], steps=steps, coefficients=coefficients)
 
@@ -78,7 +78,7 @@ def test_equal_singular_values(ctx):
     got = _check(ctx, [u.clone()])[0].cpu().double()
     t = 1 / math.sqrt(96)
     for _ in range(5):
-        t *= MUON[0] + MUON[1] * t ** 2 + MUON[2] * t ** 4
+        t *= QUINTIC[0] + QUINTIC[1] * t ** 2 + QUINTIC[2] * t ** 4
     assert float((got - t * q).abs().max()) < 2.0 ** -17 * t
 
 
@@ -101,12 +101,12 @@ def test_zeros_low_rank_and_what_is_not_finite(ctx):
     outs = [torch.full_like(t, 9.0) for t in (zero, nan, inf, fine, row)]
     ctx.orthogonalise(ctx.matrix_list([zero, nan, inf, fine, row], outs))
     assert bool((outs[0] == 0).all()) and bool(outs[1].isnan().all()) and bool(outs[2].isnan().all()) and torch.equal(outs[3], alone)
-    want, bound = newton_schulz(row.cpu(), 5, MUON)
+    want, bound = newton_schulz(row.cpu(), 5, QUINTIC)
     assert abs(float(outs[4][7, 9]) - float(want[7, 9])) <= bound and int((outs[4] != 0).sum()) == 1
     got = ctx.orthogonalise(ctx.matrix_list([rank_one.clone()]))[0].cpu().double()
     # one singular value; the others are what rounding leaves of zero, which the steps multiply by 3.4445 each
     s = torch.linalg.svdvals(got)
-    assert abs(float(s[0]) - float(torch.linalg.svdvals(newton_schulz(rank_one.cpu()[:1, :1], 5, MUON)[0])[0])) < 1e-4 and float(s[1]) < 3.4445 ** 5 * 2.0 ** -21
+    assert abs(float(s[0]) - float(torch.linalg.svdvals(newton_schulz(rank_one.cpu()[:1, :1], 5, QUINTIC)[0])[0])) < 1e-4 and float(s[1]) < 3.4445 ** 5 * 2.0 ** -21
 
 
 def test_the_same_alone_together_and_on_every_run(ctx):
@@ -125,7 +125,7 @@ def test_the_same_alone_together_and_on_every_run(ctx):
         u.neg_()                                                                # (sums in the matrix units need not round both signs alike)
     ctx.orthogonalise(lst)
     for a, b, u in zip(alone, outs, updates):
-        assert float(torch.linalg.vector_norm(a.double() + b.double())) <= 2 * newton_schulz(u.cpu(), 5, MUON)[1]
+        assert float(torch.linalg.vector_norm(a.double() + b.double())) <= 2 * newton_schulz(u.cpu(), 5, QUINTIC)[1]
 
 
 def test_parts_of_a_buffer(ctx):
