@@ -139,6 +139,17 @@ def test_parts_of_a_buffer(ctx):
             assert torch.equal(keep[:shift], flat[:shift]) and torch.equal(keep[shift + 33 * 47:], flat[shift + 33 * 47:])
 
 
+@pytest.mark.parametrize("m,n", [(72, 100), (100, 72), (70, 99), (99, 70), (132, 66), (66, 132)])
+def test_parts_of_a_buffer_by_several_workgroups(ctx, m, n):
+    """Results that can be written by fours, and those that cannot, for their columns or for where they begin."""
+    for dtype in U:
+        flat = torch.randn(m * n + 16, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+        for shift in (0, 1, 2, 4, 8):
+            keep = flat.clone()
+            _check(ctx, [keep[shift:shift + m * n].view(m, n)])
+            assert torch.equal(keep[:shift], flat[:shift]) and torch.equal(keep[shift + m * n:], flat[shift + m * n:])
+
+
 def test_in_a_graph():
     import paper_1806_11248_amd as g
     side = torch.cuda.Stream()
