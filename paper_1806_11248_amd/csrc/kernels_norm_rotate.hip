@@ -237,12 +237,17 @@ __device__ __forceinline__ void copy_heads(const RotateArgs &a, const Stream<LOG
     const char *src = in.data + row0 * in.row * 2;
     char *dst = out.data + (kStore ? (kSide ? max(place.store, (int64_t)0) : place.store) : row0) * out.row * 2;
     const int64_t src_lane = st.offset(in), dst_lane = kStore ? st.head * out.head * 2 : st.offset(out);
-    for (int pass = from; pass < to; ++pass)
-        if (st.live(a, row0, pass)) {
-            Raw<E> raw = {};
-            if (place.there) raw.read(src + pass * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
-            if (!kStore || place.store >= 0) raw.write(dst + pass * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, part);
-        }
+    constexpr int kAhead = 4;   // passes under way
+    for (int pass0 = from; pass0 < to; pass0 += kAhead) {
+        Raw<E> raw[kAhead] = {};
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b)
+            if (pass0 + b < to && place.there && st.live(a, row0, pass0 + b)) raw[b].read(src + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * in.head * 2 + src_lane, part);
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b)
+            if (pass0 + b < to && st.live(a, row0, pass0 + b) && (!kStore || place.store >= 0))
+                raw[b].write(dst + (pass0 + b) * Stream<LOG, kSide>::kAtOnce * out.head * 2 + dst_lane, part);
+    }
 }
 
 template <typename E, bool kHalves, int LOG, bool kSide, bool kStore>

@@ -386,7 +386,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
     // what the first factor, which lies as their product does, is an operand of
     const float less = kApply || (a.first && (kProduct == kOrthoNext || (kProduct == kOrthoBoth && !second))) ? kDownTotal : kDown;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+        // A is symmetric: its four values of a lane's column lie side by side in the row of that number.  All are read before anything is written.
+        f16x4 high[8 / kWaves][4], low[8 / kWaves][4];
+        if (kProduct == kOrthoFactor)
+#pragma unroll
+            for (int j = 0; j < 8 / kWaves; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const _Float16 *from = p + place(first_col + 32 * j + (lane & 31), first_row + 32 * i + result_row(4 * r, lane >> 5), m.pp);
+                    high[j][r] = *(const f16x4 *)from, low[j][r] = *(const f16x4 *)(from + kBlock);
+                }
 #pragma unroll
         for (int j = 0; j < 8 / kWaves; ++j)
 #pragma unroll
@@ -396,18 +406,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = acc[i][j][r + e] * less;
                 if (kProduct == kOrthoFactor) {
-                    // A is symmetric: its four values of this column lie side by side in the row of that number
-                    const _Float16 *from = p + place(col, row, m.pp);
-                    const f16x4 high = *(const f16x4 *)from, low = *(const f16x4 *)(from + kBlock);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
+                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[j][r / 4][e] + (float)low[j][r / 4][e]));
                         if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
                         if (a.first) v[e] *= kUpTotal * kDown;
                     }
                 }
                 put_four(to, cols, to_t, m.pp, row, col, v, kApply || ti != tj, swap);
             }
+    }
 }
 
 // ------------------------------------------------------------------- small --
