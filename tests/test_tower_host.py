@@ -48,6 +48,12 @@ def test_embedding_workspace(b):
     assert need(C.byref(_embedding(b, n_ids=2048))) == 0 and need(C.byref(_embedding(b, n_ids=0))) == 0          # nothing is sorted
     assert need(C.byref(_embedding(b, n_ids=2048, n_rows=1 << 20))) > 0                                          # too many rows to look through the ids for
     assert need(C.byref(_embedding(b, n_ids=1 << 30, n_rows=1 << 30))) > 16 << 30
+    # few rows: sums of all of them, and which were met, by up to four waves on each of 256 compute units; one row more, or wider ones, are sorted
+    few = need(C.byref(_embedding(b, n_ids=900_000, n_rows=12)))
+    assert 1000 * (12 * 64 * 4 + 4) <= few <= 1024 * (12 * 64 * 4 + 4) + 512
+    assert need(C.byref(_embedding(b, n_ids=900_000, n_rows=32))) < 4 * 4 * 900_000 <= need(C.byref(_embedding(b, n_ids=900_000, n_rows=33)))
+    assert need(C.byref(_embedding(b, n_ids=900_000, n_rows=12, width=257))) >= 4 * 4 * 900_000
+    assert need(C.byref(_embedding(b, n_ids=1 << 30, n_rows=1, width=1))) < 1 << 20
     for wrong in (dict(table_dtype=3), dict(out_dtype=-1), dict(id_bytes=2), dict(width=0), dict(width=(1 << 20) + 1), dict(n_ids=-1), dict(n_ids=(1 << 30) + 1),
                   dict(n_rows=-1), dict(n_rows=(1 << 30) + 1), dict(table_stride=-1), dict(out_stride=-1), dict(scale=math.nan), dict(scale=math.inf), dict(ids=None),
                   dict(ids=4100)):
