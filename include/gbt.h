@@ -698,8 +698,9 @@ GBT_API int32_t gbt_norm_rotate_backward(gbt_ctx *ctx, const gbt_norm_rotate_par
  * Updates of weight matrices, orthogonalised: X = G / |G| (the Frobenius norm), then `steps` times
  *     X <- (a I + b A + c A^2) X,  A = X X^T       (rows and columns exchanged where G has more rows)
  * and dst = scale * X.  A matrix of zeros gives zeros, one with an element that is no finite number NaN throughout;
- * no matrix depends on another.  Products take operands in two float16 parts, 22 bits, and are summed in 32: results
- * are as exact as those of 32-bit products, whatever the type.
+ * no matrix depends on another.  Products take operands in two float16 parts and are summed in 32 bits.  The parts hold 22
+ * bits of an element down to 2^-17 of the largest that the coefficients allow at that step (of X: 1 to begin with), and
+ * smaller ones to within 2^-40 of that.
  */
 typedef struct gbt_matrix {      /* rows x cols elements, one row after the other, any alignment of its type */
     const void *src;             /* [dev] */

@@ -378,14 +378,17 @@ OrthoKind kind_of(const gbt_matrix &m) {
     return !wide ? kSome : p < 768 ? kOne : kTwo;
 }
 bool small_kind(OrthoKind kind) { return kind <= kSmallSome; }
-// For singular values' factors up to `factor`: errors of float32 results may grow by 2^4, of others by 2^8; and the product of the factors is held in
-// float16 times 2^6.
+// For singular values' factors up to `factor`: errors of float32 results may grow by 2^4, of others by 2^8.  (At most four, so that scales stay among float32's
+// normal numbers.)
 int steps_together(double factor, OrthoKind kind) {
     const double growth = kind == kTwo ? 16.0 : 256.0;
     int n = 1;
-    while (kind != kSmallOne && kind != kOne && n < 8 && pow(factor, n + 1) <= 800.0 && pow(factor * factor, n) <= growth) ++n;
+    while (kind != kSmallOne && kind != kOne && n < 4 && pow(factor * factor, n) <= growth) ++n;
     return n;
 }
+
+// The power of two that a matrix with singular values up to `most`, and so with no larger elements, is held times; `least`: as if most were at least 2^least.
+float scale_for(double most, int least) { return most <= ldexp(1.0, least) ? ldexpf(kScaleUp, -least) : (float)exp2(15.0 - ceil(log2(most))); }
 
 // The matrices with elements in the order that they are worked on in: by kind, and of each kind those with the most to do first.
 struct OrthoOrder {
@@ -595,17 +598,22 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
     const char *fault = matrices_fault(matrices, n_matrices, &code);
     GBT_REQUIRE(ctx, !fault, code, "%s", fault);
     GBT_REQUIRE(ctx, steps >= 1 && steps <= 32, GBT_EINVAL, "steps outside 1..32");
-    // how large singular values can become, and the factor that they are multiplied by: what is kept in sixteen bits has to hold both
+    // how large singular values can become, and the factor that they are multiplied by: what is kept in sixteen bits has to hold both, and is scaled by them
     GBT_REQUIRE(ctx, isfinite(a) && isfinite(b) && isfinite(c), GBT_EINVAL, "a coefficient is not finite");
+    OrthoScales up;
     double most = 1.0, factor = 0.0;
+    up.x[0] = scale_for(most, -20);
     for (int s = 0; s < steps; ++s) {
-        double next = 0.0;
+        double next = 0.0, of_step = 0.0;
         for (int i = 0; i <= 4096; ++i) {
             const double x = most * i / 4096.0, f = fabs((double)a + (double)b * x * x + (double)c * x * x * x * x);
-            factor = std::max(factor, f);
+            of_step = std::max(of_step, f);
             next = std::max(next, x * f);
         }
         most = next;
+        factor = std::max(factor, of_step);
+        up.x[s + 1] = scale_for(most, -20);
+        up.factor[s] = scale_for(of_step, -10);
         GBT_REQUIRE(ctx, most <= 4.0 && factor <= 64.0, GBT_EINVAL, "coefficients under which singular values pass 4 or their factors 64");
     }
     const size_t need = gbt_orthogonalise_workspace_bytes(matrices, n_matrices);
@@ -628,8 +636,9 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         o.b = b;
         o.c = c;
         const int together = steps_together(factor, g.kind);
+        o.up_x = up.x[0];
         if (small_kind(g.kind)) {
-            GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, steps, together));
+            GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, up, steps, together));
             continue;
         }
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
@@ -641,20 +650,29 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         };
         for (int s = 0; s < steps; s += together) {
             const int n = std::min(together, steps - s);
+            float up_total = up.factor[s];
+            o.less = o.less_second = kScaleDown;
             GBT_HIP(ctx, product(kOrthoGram));
-            for (int i = 0; i < n; ++i) {
-                o.first = i == 0;
+            for (int t = s; t < s + n; ++t) {
+                o.first = t == s;
+                o.up_gram = up.gram(t);
+                o.up_factor = up.factor[t];
+                o.less = 1.0f / o.up_gram;
                 GBT_HIP(ctx, product(kOrthoFactor));
-                if (i < n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
+                if (!o.first) up_total *= up.factor[t] * kScaleDown;
+                if (t < s + n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
+                    o.less = up.x[t + 1] / (up.x[t] * up.factor[t]);
                     GBT_HIP(ctx, product(kOrthoBoth, !o.first));
                     if (!o.first) o.total ^= 1;
                     GBT_HIP(ctx, product(kOrthoNext));
                 } else if (!o.first) {
+                    o.less = kScaleDown;
                     GBT_HIP(ctx, product(kOrthoTotal));
                     o.total ^= 1;
                 }
             }
             o.last = s + n == steps;
+            o.less = (o.last ? 1.0f : up.x[s + n]) / (up_total * up.x[s]);
             GBT_HIP(ctx, product(kOrthoApply));
             o.xt ^= 1;
         }

@@ -8,9 +8,11 @@
 //
 // Steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
 // between products, and matrix instructions on 32 bits run at a sixteenth of the rate.  Everything between products is held in two float16 parts, high
-// and low, 22 bits in all, and a product is three on the matrix units: high * high + high * low + low * high, added up in 32 bits.  All values are held times
-// 2^8: X's entries lie around 1 / sqrt(w), and so their low parts stay among float16's normal numbers (the product of the factors times 2^6, as it grows).
-// The errors left are those of 32-bit products.
+// and low, 22 bits in all, and a product is three on the matrix units: high * high + high * low + low * high, added up in 32 bits.  Float16 has few exponents, so all
+// is held times powers of two that the coefficients give: X has singular values, and so elements, up to a bound that the host knows for each step, and the scale
+// takes that bound to 2^15.  Elements down to 2^-17 of it then have their 22 bits (X begins with some 1 / sqrt(p w), 2^-12.5 for 4096 x 8192), smaller
+// ones are off by 2^-40 of it: rows and columns of very different size keep theirs.  (512 x 2048, rows of 1 to 1e-4, ten steps, all held times 2^8: 3.6e-5 off, and
+// 32-bit products 4.6e-6.)
 //
 // All products have both operands' rows along the sum: X X^T, products of symmetric matrices, and F X = F (X^T)^T, for which X's transpose is kept beside it.
 // Of symmetric results the upper tiles are computed, and written twice.
@@ -19,8 +21,6 @@
 
 namespace {
 
-constexpr float kUp = 256.0f, kDown = 1.0f / 256.0f;   // of what is held in two parts
-constexpr float kUpTotal = 64.0f, kDownTotal = 1.0f / 64.0f;   // of the product of the factors, which grows to 800
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void ortho_fill_kernel(OrthoArgs a) {
     for (int i = threadIdx.x; i < m.pieces; i += 256) sum += a.squares[m.piece_begin + i];
     const double norm = sqrt(block_sum(sum, part));
     // a norm of zero leaves zeros; one that is no finite number leaves none anywhere
-    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
+    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)a.up_x / norm : (double)NAN;
     const int64_t at = blockIdx.x - m.fill_begin;
     const int across = m.ww / 128, i0 = (int)(at / across) * 64, j0 = (int)(at % across) * 128;   // of X
 #pragma unroll
@@ -306,11 +306,11 @@ __device__ __forceinline__ void put_four(_Float16 *m, int cols, _Float16 *t, int
     }
 }
 
-// A wave's sums, rows of 32 from `row0` and columns of 32 from `col0` on, times `scale` into G's place.  Four rows' values of a column lie side by side in a G with more
+// A wave's sums, rows of 32 from `row0` and columns of 32 from `col0` on, times `less` and the matrix's scale into G's place.  Four rows' values of a column lie side by side in a G with more
 // rows; in another one they are exchanged where they have sixteen bits, so that a lane writes four columns of its row.  (One element at a time, its type looked up for
 // each: 157 us in place of 82 for the last product of 6 x 512 x 512, 6 x 1536, 12 x 2048 and 2 x 777 x 1001.)
 template <typename E, int kAcross>
-__device__ __forceinline__ void put_result(const OrthoMatrix &m, const f32x16 (&acc)[2][kAcross], int row0, int col0, float scale, int lane, const Exchange &swap) {
+__device__ __forceinline__ void put_result(const OrthoMatrix &m, const f32x16 (&acc)[2][kAcross], int row0, int col0, float less, int lane, const Exchange &swap) {
     struct alignas(4 * sizeof(E)) Quad {
         E x[4];
     };
@@ -327,7 +327,7 @@ __device__ __forceinline__ void put_result(const OrthoMatrix &m, const f32x16 (&
                 const int row = row0 + 32 * i + result_row(r, lane >> 5), col = col0 + 32 * j + (lane & 31);
                 Quad v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v.x[e] = (E)(acc[i][j][r + e] * kDownTotal * scale);
+                for (int e = 0; e < 4; ++e) v.x[e] = (E)(acc[i][j][r + e] * less * m.scale);
                 if (tall) {
                     E *to = dst + (int64_t)col * cols + row;
                     if (col < w && quads) {
@@ -377,14 +377,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
     const int first_row = ti * kOrthoTile + (kWaves == 4 ? wave >> 1 : wave >> 2) * 64, first_col = tj * kOrthoTile + (kWaves == 4 ? (wave & 1) * 64 : (wave & 3) * 32);
     const Exchange swap(lane);
     if (kApply && a.last) {
-        const float scale = m.scale * kDown;
-        if (m.dtype == GBT_F32) put_result<float>(m, acc, first_row, first_col, scale, lane, swap);
-        else if (m.dtype == GBT_BF16) put_result<__bf16>(m, acc, first_row, first_col, scale, lane, swap);
-        else put_result<_Float16>(m, acc, first_row, first_col, scale, lane, swap);
+        if (m.dtype == GBT_F32) put_result<float>(m, acc, first_row, first_col, a.less, lane, swap);
+        else if (m.dtype == GBT_BF16) put_result<__bf16>(m, acc, first_row, first_col, a.less, lane, swap);
+        else put_result<_Float16>(m, acc, first_row, first_col, a.less, lane, swap);
         return;
     }
-    // what the first factor, which lies as their product does, is an operand of
-    const float less = kApply || (a.first && (kProduct == kOrthoNext || (kProduct == kOrthoBoth && !second))) ? kDownTotal : kDown;
+    const float less = second ? a.less_second : a.less;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         // A is symmetric: its four values of a lane's column lie side by side in the row of that number.  All are read before anything is written.
@@ -409,8 +407,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[e] = fmaf(a.c, v[e], a.b * ((float)high[j][r / 4][e] + (float)low[j][r / 4][e]));
-                        if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
-                        if (a.first) v[e] *= kUpTotal * kDown;
+                        if (row + e == col) v[e] = fmaf(a.a, a.up_gram, v[e]);
+                        v[e] *= a.up_factor / a.up_gram;
                     }
                 }
                 put_four(to, cols, to_t, m.pp, row, col, v, kApply || ti != tj, swap);
@@ -469,7 +467,7 @@ __device__ __forceinline__ void small_put(char *to, const float (&v)[4]) {
 // X into its blocks, divided by its norm, by pieces of eight elements, neighbours in memory by neighbouring lanes.  All of G is under way at once and in
 // registers until the norm is known.
 template <typename E>
-__device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m, int blocks, double *part) {
+__device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m, int blocks, float up, double *part) {
     constexpr int kPieces = 64 * kOrthoSmallW / 8 / 256;
     const E *src = (const E *)m.src;
     const int cols = (int)m.cols, across = blocks * 4, pieces = 64 * across;
@@ -500,7 +498,7 @@ __device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m,
         for (int e = 0; e < 8; ++e) sum[e & 1] = fma((double)x[n][e], (double)x[n][e], sum[e & 1]);
     const double norm = sqrt(block_sum(sum[0] + sum[1], part));
     // a norm of zero leaves zeros; one that is no finite number leaves none anywhere
-    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)kUp / norm : (double)NAN;
+    const double factor = norm == 0.0 ? 0.0 : isfinite(norm) ? (double)up / norm : (double)NAN;
 #pragma unroll
     for (int n = 0; n < kPieces; ++n) {
         const int at = threadIdx.x + 256 * n, i = m.tall ? at & 63 : at / across, j = (m.tall ? at >> 6 : at - at / across * across) * 8;
@@ -519,19 +517,18 @@ __device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m,
 }
 // A block's half of the result, rows 32 * i on, to G's place.
 template <typename E>
-__device__ __forceinline__ void small_result(const Small &s, const OrthoMatrix &m, const f32x16 &z, int i, int col) {
+__device__ __forceinline__ void small_result(const Small &s, const OrthoMatrix &m, const f32x16 &z, int i, int col, float less) {
     E *dst = (E *)m.dst;
-    const float scale = m.scale * kDown;
     const int across = m.tall ? 1 : (int)m.cols, along = m.tall ? (int)m.cols : 1, first = 32 * i + 4 * (s.lane >> 5);
     if (col >= m.w) return;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int row = first + result_row(r, 0);
-        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * kDownTotal * scale);
+        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * less * m.scale);
     }
 }
 
-__global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps, int together) {
+__global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoScales up, int steps, int together) {
     extern __shared__ __attribute__((aligned(256))) char lds[];
     __shared__ double part[4];
     const OrthoMatrix &m = a.list[blockIdx.x];
@@ -539,9 +536,9 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
     Small s;
     s.gram = lds, s.factor = lds + 16384, s.total = lds + 32768, s.x = lds + 49152;
     s.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s.lane = threadIdx.x & 63;
-    if (m.dtype == GBT_F32) small_read<float>(s, m, blocks, part);
-    else if (m.dtype == GBT_BF16) small_read<__bf16>(s, m, blocks, part);
-    else small_read<_Float16>(s, m, blocks, part);
+    if (m.dtype == GBT_F32) small_read<float>(s, m, blocks, up.x[0], part);
+    else if (m.dtype == GBT_BF16) small_read<__bf16>(s, m, blocks, up.x[0], part);
+    else small_read<_Float16>(s, m, blocks, up.x[0], part);
     __syncthreads();
     const Exchange swap(s.lane);
     for (int done = 0; done < steps; done += together) {
@@ -556,7 +553,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
             char *to = kind == 0 ? f : kind == 1 ? s.total : s.gram;
             f32x16 acc;
             small_product(acc, s, p, q, kind < 0 ? blocks : 2);
-            const float less = i == 0 && kind > 1 ? kDownTotal : kDown;
+            const int t = done + max(i, 0);
+            const float less = kind < 0 || kind == 1 ? kScaleDown : kind == 0 ? 1.0f / up.gram(t) : up.x[t + 1] / (up.x[t] * up.factor[t]);
             if (kind > 0) __syncthreads();   // it goes over an operand
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
@@ -567,8 +565,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
-                        if (row + e == col) v[e] = fmaf(a.a, kUp, v[e]);
-                        if (i == 0) v[e] *= kUpTotal * kDown;
+                        if (row + e == col) v[e] = fmaf(a.a, up.gram(t), v[e]);
+                        v[e] *= up.factor[t] / up.gram(t);
                     }
                 }
                 small_put(to + at, v);
@@ -577,6 +575,9 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
         }
         // X, a block of 32 columns by a wave, in place
         const bool last = done + now == steps;
+        float up_total = up.factor[done];
+        for (int i = 1; i < now; ++i) up_total *= up.factor[done + i] * kScaleDown;
+        const float less = (last ? 1.0f : up.x[done + now]) / (up_total * up.x[done]);
         for (int b = s.wave; b < blocks; b += 4) {
             char *block = s.x + b * 8192;
             f16x8 y[2][4];
@@ -603,9 +604,9 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
                 }
                 z[0] = (z[0] + z[1]) + z[2];
                 if (last) {
-                    if (m.dtype == GBT_F32) small_result<float>(s, m, z[0], i, 32 * b + of);
-                    else if (m.dtype == GBT_BF16) small_result<__bf16>(s, m, z[0], i, 32 * b + of);
-                    else small_result<_Float16>(s, m, z[0], i, 32 * b + of);
+                    if (m.dtype == GBT_F32) small_result<float>(s, m, z[0], i, 32 * b + of, less);
+                    else if (m.dtype == GBT_BF16) small_result<__bf16>(s, m, z[0], i, 32 * b + of, less);
+                    else small_result<_Float16>(s, m, z[0], i, 32 * b + of, less);
                     continue;
                 }
 #pragma unroll
@@ -615,7 +616,7 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, int steps
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         _Float16 h, l;
-                        split(z[0][r + e] * kDownTotal, h, l);
+                        split(z[0][r + e] * less, h, l);
                         high[e] = h, low[e] = l;
                     }
                     char *to = block + place(row + swap.quad, of & ~3, 32) * 2;
@@ -653,10 +654,10 @@ hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_
     return hipGetLastError();
 }
 
-hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, int steps, int together) {
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoScales &up, int steps, int together) {
     static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmallLds);
     if (ready != hipSuccess) return ready;
-    ortho_small_kernel<<<a.count, 256, kOrthoSmallLds, stream>>>(a, steps, together);
+    ortho_small_kernel<<<a.count, 256, kOrthoSmallLds, stream>>>(a, up, steps, together);
     return hipGetLastError();
 }
 

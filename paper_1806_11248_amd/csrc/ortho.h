@@ -27,12 +27,25 @@ struct OrthoTile {
     int16_t i, j;
 };
 
+// What is held in two float16 parts is held times a power of two, of which the products' results and the bounds of what comes of them lie up to 2^15, half of
+// float16's largest number: a low part stays a normal number, and 22 bits are held, of elements down to 2^-17 of the bound; smaller ones are off by 2^-40 of it.
+constexpr float kScaleUp = 32768.0f, kScaleDown = 1.0f / 32768.0f;
+struct OrthoScales {
+    float x[33];                        // of X before each step and after the last
+    float factor[32];                   // of each step's factor
+    // A; F A of a step; the product of two factors is held times the product of their scales less kScaleUp
+    __host__ __device__ float gram(int s) const { return x[s] * x[s] * kScaleDown; }
+};
+
 struct OrthoArgs {
     const OrthoMatrix *list;            // of the group
     int count;
     char *workspace;
     double *squares;                    // [pieces of the group]
     float a, b, c;
+    float up_x;                         // what X is held times as it is laid out
+    float up_gram, up_factor;           // likewise A and its factor of the step
+    float less, less_second;            // from the operands' scales to the result's, and that of kOrthoBoth's second one (kOrthoApply, last: to none)
     const OrthoTile *tiles;             // of the product
     int64_t count_tiles;
     int xt, total;                      // which of the two transposes is X's, which of the two products of factors the last one
@@ -42,7 +55,7 @@ struct OrthoArgs {
 // Matrices that one workgroup takes as a whole: X's blocks and three matrices of p x p in LDS.
 constexpr int kOrthoSmallP = 64, kOrthoSmallW = 384;
 constexpr int kOrthoSmallLds = 3 * 16384 + kOrthoSmallW / 32 * 8192;
-hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, int steps, int together);
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoScales &up, int steps, int together);
 
 enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
 

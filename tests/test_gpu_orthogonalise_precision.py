@@ -1,0 +1,88 @@
+"""How exact orthogonalised updates are: beside the same formulas in 32-bit products (-m gpu).
+
+Errors are against 64 bits.  What float32 results may be off by is three times what 32-bit products are, on the same matrix; nothing in the formulas says which
+of two ways to round is ahead, and the two differ by their operands (22 bits in place of 24) and by the order of their sums.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+QUINTIC = (3.4445, -4.7750, 2.0315)
+TIMES = 3.0
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_1806_11248_amd as g
+    c = g.Context(0)
+    yield c
+    c.close()
+
+
+def exact(g, steps=5, coefficients=QUINTIC):
+    """In 64 bits, by the polynomial of X X^T that all steps together are."""
+    a, b, c = coefficients
+    x = g.double() / torch.linalg.vector_norm(g.double())
+    x = x.t().contiguous() if g.shape[0] > g.shape[1] else x
+    gram = x @ x.t().contiguous()
+    eye = torch.eye(len(gram), dtype=torch.float64, device=g.device)
+    total = eye
+    for _ in range(steps):
+        factor = a * eye + b * gram + c * (gram @ gram)
+        total, gram = factor @ total, factor @ gram @ factor
+    return (total @ x).t() if g.shape[0] > g.shape[1] else total @ x
+
+
+def in_32_bits(g, steps=5, coefficients=QUINTIC):
+    a, b, c = coefficients
+    x = (g.double() / torch.linalg.vector_norm(g.double())).float()
+    x = x.t().contiguous() if g.shape[0] > g.shape[1] else x
+    for _ in range(steps):
+        gram = x @ x.t().contiguous()
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x.t() if g.shape[0] > g.shape[1] else x
+
+
+def off(x, want):
+    return float(torch.linalg.vector_norm(x.double() - want))
+
+
+def off_by_row(x, want):
+    """Of each row, relative to its length."""
+    return torch.linalg.vector_norm(x.double() - want, dim=1) / torch.linalg.vector_norm(want, dim=1)
+
+
+@pytest.mark.parametrize("m,n", [(64, 256), (40, 300), (200, 700), (512, 2048), (900, 1000)])
+@pytest.mark.parametrize("spread", [1e-4, 1e-6])
+@pytest.mark.parametrize("steps", [5, 10])
+def test_rows_of_very_different_size(ctx, m, n, spread, steps):
+    """Rarely used rows of a matrix.  X's elements are held with an error of at most 2^-39 (of a bound between 1 and 2, twice 2^-40), factors with one
+    of 2^-38, of which a row takes the length of a row times X's largest singular value, below 1.2: of a row of length r, their share is (2^-39 sqrt n + 1.2 * 2^-38 sqrt m) / r, in the
+    first step, of which all are at most 1.5 times as much, as such rows grow by 3.4445 in each."""
+    rng = torch.Generator().manual_seed(m)
+    g = torch.randn(m, n, generator=rng) * torch.logspace(0, math.log10(spread), m)[:, None]
+    want, other = exact(g, steps), in_32_bits(g, steps)
+    for tall in (False, True):
+        u = (g.t().contiguous() if tall else g).cuda()
+        got = ctx.orthogonalise(ctx.matrix_list([u], [torch.zeros_like(u)]), steps=steps)[0].cpu()
+        got = got.t() if tall else got
+        assert off(got, want) <= TIMES * off(other, want)
+        r = torch.linalg.vector_norm(g.double(), dim=1) / torch.linalg.vector_norm(g.double())
+        held = 1.5 * (2.0 ** -39 * math.sqrt(n) + 1.2 * 2.0 ** -38 * math.sqrt(m)) / r
+        assert bool((off_by_row(got, want) <= TIMES * off_by_row(other, want).max() + held).all())
+
+
+@pytest.mark.parametrize("steps,factor", [(1, 0.1), (3, 0.1), (4, 0.02)])
+def test_factors_far_below_one(ctx, steps, factor):
+    """Singular values that shrink with every step are held with what they have then."""
+    for m, n in ((40, 64), (130, 150)):
+        for dtype in (torch.float32, torch.bfloat16):
+            g = torch.randn(m, n, generator=torch.Generator().manual_seed(1)).to(dtype)
+            u = g.cuda()
+            got = ctx.orthogonalise(ctx.matrix_list([u]), steps=steps, coefficients=(factor, 0.0, 0.0))[0].cpu()
+            want = exact(g, steps, (factor, 0.0, 0.0))
+            # a rounding of 22 bits for each of three products a step at most, sums in 32 bits, and the result's
+            assert off(got, want) <= (steps * 6 * 2.0 ** -22 + torch.finfo(dtype).eps / 2) * float(torch.linalg.vector_norm(want))
