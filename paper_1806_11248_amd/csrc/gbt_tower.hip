@@ -638,7 +638,14 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         const int together = steps_together(factor, g.kind);
         o.up_x = up.x[0];
         if (small_kind(g.kind)) {
-            GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, up, steps, together));
+            OrthoSmallScales of;
+            memset(&of, 0, sizeof of);
+            of.x = up.x[0];
+            for (int t = 0; t < steps; ++t) {
+                of.step[t] = OrthoSmallScales::Step{{1.0f / up.gram(t), kScaleDown, up.after(t), up.after(t)}, up.gram(t), up.factor[t] / up.gram(t),
+                                                    up.apply(t, std::min(t + together, steps), steps), 0.0f};
+            }
+            GBT_HIP(ctx, gbt_launch_ortho_small(ctx->stream, o, of, steps, together));
             continue;
         }
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
@@ -650,7 +657,6 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
         };
         for (int s = 0; s < steps; s += together) {
             const int n = std::min(together, steps - s);
-            float up_total = up.factor[s];
             o.less = o.less_second = kScaleDown;
             GBT_HIP(ctx, product(kOrthoGram));
             for (int t = s; t < s + n; ++t) {
@@ -659,9 +665,8 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
                 o.up_factor = up.factor[t];
                 o.less = 1.0f / o.up_gram;
                 GBT_HIP(ctx, product(kOrthoFactor));
-                if (!o.first) up_total *= up.factor[t] * kScaleDown;
                 if (t < s + n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
-                    o.less = up.x[t + 1] / (up.x[t] * up.factor[t]);
+                    o.less = up.after(t);
                     GBT_HIP(ctx, product(kOrthoBoth, !o.first));
                     if (!o.first) o.total ^= 1;
                     GBT_HIP(ctx, product(kOrthoNext));
@@ -672,7 +677,7 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
                 }
             }
             o.last = s + n == steps;
-            o.less = (o.last ? 1.0f : up.x[s + n]) / (up_total * up.x[s]);
+            o.less = up.apply(s, s + n, steps);
             GBT_HIP(ctx, product(kOrthoApply));
             o.xt ^= 1;
         }

@@ -315,6 +315,7 @@ __device__ __forceinline__ void put_result(const OrthoMatrix &m, const f32x16 (&
         E x[4];
     };
     E *dst = (E *)m.dst;
+    const float scale = m.scale;
     const int64_t cols = m.cols;
     const int p = m.p, w = m.w;
     const bool tall = m.tall, quads = cols % 4 == 0 && ((uintptr_t)dst & (4 * sizeof(E) - 1)) == 0;
@@ -327,7 +328,7 @@ __device__ __forceinline__ void put_result(const OrthoMatrix &m, const f32x16 (&
                 const int row = row0 + 32 * i + result_row(r, lane >> 5), col = col0 + 32 * j + (lane & 31);
                 Quad v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v.x[e] = (E)(acc[i][j][r + e] * less * m.scale);
+                for (int e = 0; e < 4; ++e) v.x[e] = (E)(acc[i][j][r + e] * less * scale);
                 if (tall) {
                     E *to = dst + (int64_t)col * cols + row;
                     if (col < w && quads) {
@@ -519,26 +520,30 @@ __device__ __forceinline__ void small_read(const Small &s, const OrthoMatrix &m,
 template <typename E>
 __device__ __forceinline__ void small_result(const Small &s, const OrthoMatrix &m, const f32x16 &z, int i, int col, float less) {
     E *dst = (E *)m.dst;
+    const float scale = m.scale;
     const int across = m.tall ? 1 : (int)m.cols, along = m.tall ? (int)m.cols : 1, first = 32 * i + 4 * (s.lane >> 5);
     if (col >= m.w) return;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int row = first + result_row(r, 0);
-        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * less * m.scale);
+        if (row < m.p) dst[row * across + col * along] = (E)(z[r] * less * scale);
     }
 }
 
-__global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoScales up, int steps, int together) {
+__global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoSmallScales scales, int steps, int together) {
     extern __shared__ __attribute__((aligned(256))) char lds[];
     __shared__ double part[4];
+    __shared__ OrthoSmallScales up;   // arguments lie in the host's memory: read once, while G is under way
+    static_assert(sizeof up.step == 1024, "");
+    ((float *)up.step)[threadIdx.x] = ((const float *)scales.step)[threadIdx.x];
     const OrthoMatrix &m = a.list[blockIdx.x];
     const int blocks = (m.w + 31) / 32;
     Small s;
     s.gram = lds, s.factor = lds + 16384, s.total = lds + 32768, s.x = lds + 49152;
     s.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s.lane = threadIdx.x & 63;
-    if (m.dtype == GBT_F32) small_read<float>(s, m, blocks, up.x[0], part);
-    else if (m.dtype == GBT_BF16) small_read<__bf16>(s, m, blocks, up.x[0], part);
-    else small_read<_Float16>(s, m, blocks, up.x[0], part);
+    if (m.dtype == GBT_F32) small_read<float>(s, m, blocks, scales.x, part);
+    else if (m.dtype == GBT_BF16) small_read<__bf16>(s, m, blocks, scales.x, part);
+    else small_read<_Float16>(s, m, blocks, scales.x, part);
     __syncthreads();
     const Exchange swap(s.lane);
     for (int done = 0; done < steps; done += together) {
@@ -553,8 +558,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoScal
             char *to = kind == 0 ? f : kind == 1 ? s.total : s.gram;
             f32x16 acc;
             small_product(acc, s, p, q, kind < 0 ? blocks : 2);
-            const int t = done + max(i, 0);
-            const float less = kind < 0 || kind == 1 ? kScaleDown : kind == 0 ? 1.0f / up.gram(t) : up.x[t + 1] / (up.x[t] * up.factor[t]);
+            const OrthoSmallScales::Step &scale = up.step[done + max(i, 0)];
+            const float up_gram = scale.gram, to_factor = scale.factor, less = kind < 0 ? kScaleDown : scale.less[max(kind, 0)];
             if (kind > 0) __syncthreads();   // it goes over an operand
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
@@ -565,8 +570,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoScal
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
-                        if (row + e == col) v[e] = fmaf(a.a, up.gram(t), v[e]);
-                        v[e] *= up.factor[t] / up.gram(t);
+                        if (row + e == col) v[e] = fmaf(a.a, up_gram, v[e]);
+                        v[e] *= to_factor;
                     }
                 }
                 small_put(to + at, v);
@@ -575,9 +580,7 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoScal
         }
         // X, a block of 32 columns by a wave, in place
         const bool last = done + now == steps;
-        float up_total = up.factor[done];
-        for (int i = 1; i < now; ++i) up_total *= up.factor[done + i] * kScaleDown;
-        const float less = (last ? 1.0f : up.x[done + now]) / (up_total * up.x[done]);
+        const float less = up.step[done].apply;
         for (int b = s.wave; b < blocks; b += 4) {
             char *block = s.x + b * 8192;
             f16x8 y[2][4];
@@ -654,7 +657,7 @@ hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_
     return hipGetLastError();
 }
 
-hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoScales &up, int steps, int together) {
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoSmallScales &up, int steps, int together) {
     static const hipError_t ready = hipFuncSetAttribute((const void *)ortho_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmallLds);
     if (ready != hipSuccess) return ready;
     ortho_small_kernel<<<a.count, 256, kOrthoSmallLds, stream>>>(a, up, steps, together);

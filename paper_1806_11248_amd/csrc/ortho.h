@@ -32,9 +32,23 @@ struct OrthoTile {
 constexpr float kScaleUp = 32768.0f, kScaleDown = 1.0f / 32768.0f;
 struct OrthoScales {
     float x[33];                        // of X before each step and after the last
-    float factor[32];                   // of each step's factor
-    // A; F A of a step; the product of two factors is held times the product of their scales less kScaleUp
-    __host__ __device__ float gram(int s) const { return x[s] * x[s] * kScaleDown; }
+    float factor[32];                   // of each step's factor; a product of factors is held times the product of their scales, a kScaleUp less for each
+    float gram(int s) const { return x[s] * x[s] * kScaleDown; }   // of A; F A is held times that of X before and after the step
+    float after(int s) const { return x[s + 1] / (x[s] * factor[s]); }   // from the operands' scales to F A's, and from its and F's to the next A's
+    // from the scales of X and of the product of the factors of steps s to e to that of X behind them, or to none behind the last
+    float apply(int s, int e, int steps) const {
+        float up = (e < steps ? x[e] : 1.0f) / x[s];
+        for (int t = s; t < e; ++t) up /= t == s ? factor[t] : factor[t] * kScaleDown;
+        return up;
+    }
+};
+// The same as one workgroup takes them, with nothing left to divide.
+struct OrthoSmallScales {
+    struct Step {
+        float less[4];                  // of A A, the product of two factors, F A and F A F
+        float gram, factor, apply, none;   // factor: from A's scale to the factor's; apply: of X after the round that begins with the step
+    } step[32];
+    float x;
 };
 
 struct OrthoArgs {
@@ -55,7 +69,7 @@ struct OrthoArgs {
 // Matrices that one workgroup takes as a whole: X's blocks and three matrices of p x p in LDS.
 constexpr int kOrthoSmallP = 64, kOrthoSmallW = 384;
 constexpr int kOrthoSmallLds = 3 * 16384 + kOrthoSmallW / 32 * 8192;
-hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoScales &up, int steps, int together);
+hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoSmallScales &up, int steps, int together);
 
 enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
 
