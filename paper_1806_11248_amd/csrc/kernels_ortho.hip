@@ -4,7 +4,7 @@
 // All F and A of one X commute: A after a step is F A F, so several steps are taken on the p x p matrices alone, and X is multiplied once by the product
 // of their factors.  That halves the work where X is wide, and costs nothing where it is square (a step on X is 1.5 w/p + 0.5 products of p x p x p, one on
 // A is 2; symmetric ones count half).  But an error of A grows by a^2 with each such step where singular values are small, so X is multiplied and A taken
-// anew after one step or two where results have 32 bits, three where they have sixteen (gbt_tower.hip).
+// anew after as many steps as leave errors like those of 32-bit products, one to three (kind_of, gbt_tower.hip).
 //
 // Steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
 // between products, and matrix instructions on 32 bits run at a sixteenth of the rate.  Everything between products is held in two float16 parts, high

@@ -120,3 +120,17 @@ def test_as_exact_as_32_bit_products(ctx, m, n):
     here = math.sqrt(sum(off(o, w) ** 2 for o, w in zip(outs, want)))
     there = math.sqrt(sum(off(in_32_bits(u), w) ** 2 for u, w in zip(updates, want)))
     assert here <= 1.25 * there, (here, there)
+
+
+@pytest.mark.parametrize("m,n", [s for s in SHAPES if max(s) < 2100])
+def test_sixteen_bit_results_are_rounded_ones(ctx, m, n):
+    """A result of sixteen bits hides an error before its last rounding, except where that lands on the other side of a middle: the share of such elements is the
+    error's mean size by the distance of two numbers.  It is at most three times that of 32-bit products (TIMES), and four standard deviations of a count."""
+    for dtype in (torch.float16, torch.bfloat16):
+        count = max(1, min(24, 400_000 // (m * n)))
+        updates = [_averaged(m, n, seed, dtype) for seed in range(count)]
+        outs = ctx.orthogonalise(ctx.matrix_list(updates, [torch.zeros_like(u) for u in updates]))
+        want = [exact(u).to(dtype) for u in updates]
+        here = sum(int((o != w).sum()) for o, w in zip(outs, want))
+        there = sum(int((in_32_bits(u).to(dtype) != w).sum()) for u, w in zip(updates, want))
+        assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (here, there, count * m * n)
