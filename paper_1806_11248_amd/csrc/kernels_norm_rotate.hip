@@ -66,6 +66,9 @@ __device__ __forceinline__ Place place_of(const RotateArgs &a, int64_t row, int 
         if (k0 < 0 || k1 < k0 || used < 0 || (a.store && k0 + used > a.out_rows)) used = 0;   // (k1 < k0: their difference may have passed 64 bits)
         at += used - (q1 - q0);
         slot = k0, room = used;
+    } else if (a.store) {   // slots of one length, in use from their first row on as far as there are rows
+        room = a.out_rows / a.n_seq;
+        slot = seq * room;
     }
     p.position = at;
     p.store = !a.store ? row : p.there && at >= 0 && at < room ? slot + at : -1;

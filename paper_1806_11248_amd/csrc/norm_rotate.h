@@ -15,7 +15,7 @@ struct RotateArgs {
     const double *turns;
     int64_t rows, out_rows;                  // of q, k and v; of k_out and v_out
     int n_seq, heads, kv_heads;
-    int dim, turned, halves, store, slots;   // slots: positions are counted in slots of k_ptr or k_len
+    int dim, turned, halves, store, slots;   // slots: positions are counted from the end of what k_ptr or k_len say is in use
     float eps;
     int log_lanes;                           // 1 << log_lanes lanes for a line, of which dim / 8 work
     int row_group;                           // rows that a wave takes side by side
