@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
-from tower_ref import TINY, U, places, rotate
+from tower_ref import TINY, TURN, U, places, rotate, rotate_gradient
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +65,23 @@ def test_a_store_of_equal_slots_all_in_use(ctx, n_seq, each, room, ragged):
     kept = torch.ones(n_seq * room, dtype=torch.bool)
     kept[to[goes]] = False
     assert bool((ks.cpu()[kept] == 7).all()) and bool((vs.cpu()[kept] == 7).all())
+
+
+def test_sine_and_cosine(ctx):
+    """Of heads of ones with eps = 0 and a gradient of one in the first element of every pair, the weight's gradient is the cosine and less the sine of each
+    pair's turn, and nothing else is rounded.  In 32 bits: the part of a quarter by which an angle is reduced is off by at most 2^-26, times pi / 2, and a polynomial's last
+    two sums by 2^-25 each: below 2^-23."""
+    rng = torch.Generator().manual_seed(0)
+    D, worst = 128, 0.0
+    edges = torch.tensor([0.0, 0.125, 0.25, 0.375, 0.5, 0.625, 0.75, 0.875, 1.0, 0.12500000001, 0.12499999999, 0.49999999999, 0.50000000001, 1e-9, 1e-4, 3.0], dtype=torch.float64)
+    q = torch.ones(1, 1, D, dtype=BF16, device="cuda")
+    d = torch.zeros_like(q)
+    d[..., :D // 2] = 1
+    for position in (1, -1, 2, 3, 1000, -12_345, (1 << 31) - 1, 1 << 40):
+        for _ in range(4):
+            turns = torch.cat([edges, torch.rand(D // 2 - len(edges), generator=rng, dtype=torch.float64)])
+            _, _, dw, _ = ctx.norm_rotate_backward(d, d, q, q, None, None, turns.cuda(), eps=0.0, positions=torch.tensor([position]).cuda())
+            whole = turns * position
+            angle = (whole - whole.round()) * 2 * torch.pi
+            worst = max(worst, float((dw.cpu().double() - torch.cat([angle.cos(), -angle.sin()])).abs().max()))
+    assert worst <= 2.0 ** -23, worst
