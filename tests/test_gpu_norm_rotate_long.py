@@ -85,3 +85,61 @@ def test_sine_and_cosine(ctx):
             angle = (whole - whole.round()) * 2 * torch.pi
             worst = max(worst, float((dw.cpu().double() - torch.cat([angle.cos(), -angle.sin()])).abs().max()))
     assert worst <= 2.0 ** -23, worst
+
+
+# lengths of sequences; rows before the first and behind the last
+RAGGED = [1, 0, 700, 3, 0, 0, 1500, 64, 65, 1, 1, 1900, 0, 333, 2, 5]
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,turned", [(8, 8, 64, 64), (32, 8, 128, 128), (24, 16, 80, 32), (4, 2, 64, 64), (70, 5, 16, 16)])
+@pytest.mark.parametrize("halves", [True, False])
+def test_many_ragged_rows(ctx, heads, kv_heads, dim, turned, halves):
+    """A wave takes all heads of a row, and many rows one after the other, across sequences' ends, empty ones among them, and rows of none; both directions, packed
+    and, forward, into a store."""
+    ptr = [5]
+    for n in RAGGED * 2:
+        ptr.append(ptr[-1] + n)
+    rows = ptr[-1] + 9
+    rng = torch.Generator(device="cuda").manual_seed(heads)
+    x = (torch.randn(rows, heads + 2 * kv_heads, dim, generator=rng, device="cuda") * torch.exp(torch.randn(heads + 2 * kv_heads, 1, generator=rng, device="cuda"))).to(BF16)
+    q, k, v = x.split([heads, kv_heads, kv_heads], dim=1)
+    there, position, _ = places(rows, ptr)
+    there, position = there.cuda(), position.cuda()
+    for t in (q, k, v):
+        t[~there] = float("nan")
+    wq, wk = (1 + 0.3 * torch.randn(2, dim, generator=rng, device="cuda")).unbind()
+    turns = _turns(turned)
+    at = dict(q_ptr=torch.tensor(ptr).cuda(), halves=halves)
+    q_out, k_out, v_out = ctx.norm_rotate(q, k, wq, wk, turns, v=v, **at)
+    for got, t, w in ((q_out, q, wq), (k_out, k, wk)):
+        _close(got, *rotate(t, w, turns, position, there, 1e-6, halves))
+    assert torch.equal(v_out, torch.where(there[:, None, None], v, torch.zeros((), dtype=BF16, device="cuda")))
+    d = [torch.randn(t.shape, generator=rng, device="cuda").to(BF16) for t in (q, k)]
+    for t in d:
+        t[~there] = float("nan")
+    dq, dk, dwq, dwk = ctx.norm_rotate_backward(*d, q, k, wq, wk, turns, **at)
+    for got, dw, t, w, back in ((dq, dwq, q, wq, d[0]), (dk, dwk, k, wk, d[1])):
+        want, bound, of_weight, of_bound = rotate_gradient(back, t, w, turns, position, there, 1e-6, halves)
+        _close(got, want, bound)
+        # a lane adds up fewer than 64 terms here, some ten more sums join them, in the last ones' 64 bits; the terms' own errors as in tower_ref, with the sine's
+        n = rows * t.shape[1]
+        size = of_bound / (n * 2.0 ** -24 + (2 * dim + 32) * 2.0 ** -24 + TURN)
+        assert bool(((dw.double() - of_weight).abs() <= 2.0 ** -24 * of_weight.abs() + ((80 + 2 * dim + 32) * 2.0 ** -24 + 2.0 ** -23) * size).all())
+    # the same rows into a store, behind 3 of their sequence that were there
+    past, room = 3, [n + 5 for n in RAGGED * 2]
+    slots = [4]
+    for n in room:
+        slots.append(slots[-1] + n)
+    used = torch.tensor([n + past for n in RAGGED * 2], dtype=torch.int32).cuda()
+    ks, vs = (torch.full((slots[-1] + 2, kv_heads, dim), 7.0, dtype=BF16, device="cuda") for _ in range(2))
+    q_store, _, _ = ctx.norm_rotate(q, k, wq, wk, turns, v=v, k_ptr=torch.tensor(slots).cuda(), k_len=used, k_out=ks, v_out=vs, **at)
+    there, position, to = places(rows, ptr, slots, used.tolist())
+    goes = (to >= 0).cuda()
+    assert torch.equal(goes, there.cuda())
+    _close(q_store, *rotate(q, wq, turns, position.cuda(), there.cuda(), 1e-6, halves))
+    want, bound = rotate(k, wk, turns, position.cuda(), there.cuda(), 1e-6, halves)
+    _close(ks[to.cuda()[goes]], want[goes], bound[goes])
+    assert torch.equal(vs[to.cuda()[goes]], v[goes])
+    kept = torch.ones(len(ks), dtype=torch.bool, device="cuda")
+    kept[to.cuda()[goes]] = False
+    assert bool((ks[kept] == 7).all()) and bool((vs[kept] == 7).all())
