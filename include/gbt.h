@@ -650,7 +650,7 @@ GBT_API int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_params 
  *     and of y's first `turned` elements, pair i turned by position * turns[i] revolutions:
  *     (a, b) -> (a cos - b sin, a sin + b cos)
  * halves: pair i is elements i and i + turned / 2; otherwise 2 i and 2 i + 1.  Angles are taken in 64 bits.  All in
- * 32 bits between, rounded once.
+ * 32 bits between, rounded once (squares too: heads with elements past 2^60 can give zeros, as for infinite ones).
  *
  * Rows belong to sequences as in gbt_attention: sequence s has the rows q_ptr[s] .. q_ptr[s + 1], nq of them, and
  * with k_ptr or k_len it has nk rows of keys, its own the last of them; row i's place is i + nk - nq (nk = nq

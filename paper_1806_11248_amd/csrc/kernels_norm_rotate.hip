@@ -124,6 +124,12 @@ __device__ __forceinline__ float line_sum(float x) {
     return x;
 }
 
+// 1 / sqrt(x).  The instruction takes a denormal number, a mean of squares below 2^-126 with no eps, for zero.
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool small = x < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(small ? x * 0x1p96f : x) * (small ? 0x1p48f : 1.0f);
+}
+
 // The heads of one tensor by a wave: lines of 1 << LOG lanes, as many at once as a wave has, of one row; where a row has fewer, of a few whole rows side by
 // side (kSide).  All but the lane's own offset is the same in all lanes, and so a scalar.
 template <int LOG, bool kSide>
@@ -224,7 +230,7 @@ __device__ __forceinline__ void turn_heads(const RotateArgs &a, const Stream<LOG
 #pragma unroll
             for (int e = 0; e < 8; ++e) squares = fmaf(x[e], x[e], squares);
             const float mean = fmaf(line_sum<LOG>(squares), each, a.eps);
-            const float s = place.there ? __builtin_amdgcn_rsqf(mean) : 0.0f;
+            const float s = place.there ? inverse_root(mean) : 0.0f;
             float y[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -349,7 +355,7 @@ __device__ __forceinline__ void turn_all_back(const RotateArgs &a, int heads, in
         squares = line_sum<LOG>(squares);
         along = line_sum<LOG>(along);
         // (of no row: zeros, also where eps is zero)
-        const float s = live && place.there ? __builtin_amdgcn_rsqf(fmaf(squares, each, a.eps)) : 0.0f;
+        const float s = live && place.there ? inverse_root(fmaf(squares, each, a.eps)) : 0.0f;
         const float less = along * each * s * s;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

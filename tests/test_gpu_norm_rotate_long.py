@@ -87,6 +87,27 @@ def test_sine_and_cosine(ctx):
     assert worst <= 2.0 ** -23, worst
 
 
+@pytest.mark.parametrize("exponent", [-60, -63, -64, -66, -69, 60])
+def test_means_of_squares_that_are_denormal(ctx, exponent):
+    """With no eps the smallest rows are of length one behind their norm too, as long as 32 bits hold their squares: 2^-138 has eleven of them, which is more
+    than bfloat16 has."""
+    H, D = 3, 16
+    q = (1 + torch.rand(4, H, D, generator=torch.Generator().manual_seed(1))).to(BF16) * 2.0 ** exponent
+    assert bool((q.double() * 2.0 ** -exponent >= 1).all())
+    d = torch.randn(4, H, D, generator=torch.Generator().manual_seed(2)).to(BF16)
+    there, position = torch.ones(4, dtype=torch.bool), torch.arange(4)
+    turns = _turns(D)
+    q_out, _ = ctx.norm_rotate(q.cuda(), q.cuda(), None, None, turns, eps=0.0)
+    want, bound = rotate(q, torch.ones(D), turns.cpu(), position, there, 0.0, True)
+    # the squares' own roundings, half a step of 2^-149 each, beside their mean
+    denormal = 2.0 ** -150 / 4.0 ** exponent
+    _close(q_out, want, bound + 2 * denormal * want.abs().amax())
+    dq, _, dw, _ = ctx.norm_rotate_backward(d.cuda(), d.cuda(), q.cuda(), q.cuda(), None, None, turns, eps=0.0)
+    dx, of_x, of_weight, of_bound = rotate_gradient(d, q, torch.ones(D), turns.cpu(), position, there, 0.0, True)
+    _close(dq, dx, of_x + 8 * denormal * dx.abs().amax())
+    assert bool(((dw.cpu().double() - of_weight).abs() <= 2.0 ** -24 * of_weight.abs() + of_bound + 8 * denormal * of_weight.abs().amax()).all())
+
+
 # lengths of sequences; rows before the first and behind the last
 RAGGED = [1, 0, 700, 3, 0, 0, 1500, 64, 65, 1, 1, 1900, 0, 333, 2, 5]
 
