@@ -368,6 +368,20 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(EmbedAr
         for (int i = group * each; i < to; ++i) add_part(sum, c, i);
         return (parts + each - 1) / each;   // groups with a share
     };
+    // the same, by sums of 64 parts in 64 bits: a run of 2^24 places was off by 1.5e-4 where they are equal and each addition is rounded the same way
+    auto join_long = [&](int64_t c, int parts, int group, int count, double (&total)[8]) {
+        const int each = (parts + count - 1) / count, to = min(parts, (group + 1) * each);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) total[e] = 0.0;
+        for (int i0 = group * each; i0 < to; i0 += 64) {
+            float sum[8] = {};
+#pragma unroll 8
+            for (int i = i0; i < min(to, i0 + 64); ++i) add_part(sum, c, i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) total[e] += (double)sum[e];
+        }
+        return (parts + each - 1) / each;
+    };
     uint32_t run = 0;
     const int parts = chunk < a.chunks - 1 ? parts_of(chunk, &run) : 0;
     float sum[8];
@@ -386,14 +400,17 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(EmbedAr
     __syncthreads();
     const int c = long_chunk;
     if (c < 0) return;
-    const int shares = join(c, long_parts, threadIdx.x >> a.log_lanes, groups * kJoinWaves, sum);
+    double total[8];
+    const int shares = join_long(c, long_parts, threadIdx.x >> a.log_lanes, groups * kJoinWaves, total);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) shared[threadIdx.x][e] = sum[e];
+    for (int e = 0; e < 8; ++e) shared[threadIdx.x][e] = (float)total[e];
     __syncthreads();
     if (threadIdx.x >= (unsigned)lanes) return;
     for (int g = 1; g < shares; ++g)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += shared[(g << a.log_lanes) + threadIdx.x][e];
+        for (int e = 0; e < 8; ++e) total[e] += (double)shared[(g << a.log_lanes) + threadIdx.x][e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = (float)total[e];
     if (l.some()) finish<T, kVector>(a, long_run, sum, l);
 }
 
@@ -466,68 +483,79 @@ __device__ __forceinline__ void read_raw(Eight<O> &x, const O *row, const Lane &
     }
 }
 
+// A group of lanes adds at most kBehind places up behind one another, then the wave's sums go to those before: an addition is off by half a step of its sum, and
+// a sum of 2^17 equal places, of which each is rounded the same way, was off by 1e-3.
 template <typename O, bool kVector>
 __global__ __launch_bounds__(64) void embedding_rows_kernel(EmbedArgs a) {
     constexpr int kAhead = 8;   // places of a group whose rows are under way while as many are added up
+    constexpr int kBehind = 512;
     extern __shared__ __attribute__((aligned(16))) float4 sums[];   // [n_rows][2][64]
     const int lane = threadIdx.x, lanes = 1 << a.log_lanes, groups = 64 >> a.log_lanes, group = lane >> a.log_lanes, rows = (int)a.n_rows;
-    const int64_t first = (int64_t)blockIdx.x * a.chunk;
-    const int count = (int)(min(a.n_ids, first + a.chunk) - first);
+    const int64_t begin = (int64_t)blockIdx.x * a.chunk, end = min(a.n_ids, begin + a.chunk);
     const Lane l(a, 0, lane & (lanes - 1));
-    for (int r = 0; r < 2 * rows; ++r) sums[r * 64 + lane] = float4{0.0f, 0.0f, 0.0f, 0.0f};
     uint32_t seen = 0;
-    struct Places {
-        uint32_t id[kAhead];
-        Eight<O> x[kAhead];
-    } even, odd;
-    auto fetch_ids = [&](Places &p, int i) {
+    for (int64_t first = begin; first < end; first += kBehind * groups) {
+        const int count = (int)min((int64_t)(kBehind * groups), end - first);
+        for (int r = 0; r < 2 * rows; ++r) sums[r * 64 + lane] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+        struct Places {
+            uint32_t id[kAhead];
+            Eight<O> x[kAhead];
+        } even, odd;
+        auto fetch_ids = [&](Places &p, int i) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const uint32_t id = id_at(a.ids, a.id_bytes, first + min(i + u * groups, count - 1), rows);
-            p.id[u] = i + u * groups < count ? id : (uint32_t)rows;
+            for (int u = 0; u < kAhead; ++u) {
+                const uint32_t id = id_at(a.ids, a.id_bytes, first + min(i + u * groups, count - 1), rows);
+                p.id[u] = i + u * groups < count ? id : (uint32_t)rows;
+            }
+        };
+        auto fetch_rows = [&](Places &p, int i) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) read_raw<O, kVector>(p.x[u], (const O *)a.out + (first + min(i + u * groups, count - 1)) * a.out_stride, l);
+        };
+        auto add = [&](const Places &p) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const bool there = p.id[u] < (uint32_t)rows;
+                const uint32_t row = there ? p.id[u] : 0;
+                seen |= (uint32_t)there << row;
+                float4 *to = sums + row * 128 + lane, lo = to[0], hi = to[64];
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = there ? (float)p.x[u].x[e] : 0.0f;
+                lo.x += x[0], lo.y += x[1], lo.z += x[2], lo.w += x[3], hi.x += x[4], hi.y += x[5], hi.z += x[6], hi.w += x[7];
+                to[0] = lo, to[64] = hi;
+            }
+        };
+        const int step = kAhead * groups;
+        fetch_ids(even, group);
+        fetch_rows(even, group);
+        for (int i = group; i < count + group; i += 2 * step) {   // the same for all groups
+            fetch_ids(odd, i + step);
+            fetch_rows(odd, i + step);
+            add(even);
+            fetch_ids(even, i + 2 * step);
+            fetch_rows(even, i + 2 * step);
+            add(odd);
         }
-    };
-    auto fetch_rows = [&](Places &p, int i) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) read_raw<O, kVector>(p.x[u], (const O *)a.out + (first + min(i + u * groups, count - 1)) * a.out_stride, l);
-    };
-    auto add = [&](const Places &p) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const bool there = p.id[u] < (uint32_t)rows;
-            const uint32_t row = there ? p.id[u] : 0;
-            seen |= (uint32_t)there << row;
-            float4 *to = sums + row * 128 + lane, lo = to[0], hi = to[64];
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = there ? (float)p.x[u].x[e] : 0.0f;
-            lo.x += x[0], lo.y += x[1], lo.z += x[2], lo.w += x[3], hi.x += x[4], hi.y += x[5], hi.z += x[6], hi.w += x[7];
-            to[0] = lo, to[64] = hi;
-        }
-    };
-    const int step = kAhead * groups;
-    fetch_ids(even, group);
-    fetch_rows(even, group);
-    for (int i = group; i < count + group; i += 2 * step) {   // the same for all groups
-        fetch_ids(odd, i + step);
-        fetch_rows(odd, i + step);
-        add(even);
-        fetch_ids(even, i + 2 * step);
-        fetch_rows(even, i + 2 * step);
-        add(odd);
-    }
-    __syncthreads();
-    // the wave's groups, for each lane from another one on, so that no two meet in a bank
-    float *part = a.part + (int64_t)blockIdx.x * rows * 8 * lanes;
-    for (int o = lane; o < 2 * rows * lanes; o += 64) {
-        const int r = o >> a.log_lanes, at = o & (lanes - 1);
-        float4 v{0.0f, 0.0f, 0.0f, 0.0f};
+        __syncthreads();
+        // the wave's groups, for each lane from another one on, so that no two meet in a bank
+        float *part = a.part + (int64_t)blockIdx.x * rows * 8 * lanes;
+        for (int o = lane; o < 2 * rows * lanes; o += 64) {
+            const int r = o >> a.log_lanes, at = o & (lanes - 1);
+            float4 v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
-        for (int g = 0; g < groups; ++g) {
-            const float4 x = sums[r * 64 + (((g + r) & (groups - 1)) << a.log_lanes) + at];
-            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            for (int g = 0; g < groups; ++g) {
+                const float4 x = sums[r * 64 + (((g + r) & (groups - 1)) << a.log_lanes) + at];
+                v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            }
+            float4 *to = (float4 *)(part + ((r >> 1) * lanes + at) * 8 + (r & 1) * 4);
+            if (first > begin) {
+                const float4 x = *to;
+                v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            }
+            *to = v;
         }
-        *(float4 *)(part + ((r >> 1) * lanes + at) * 8 + (r & 1) * 4) = v;
+        __syncthreads();
     }
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) seen |= __shfl_xor(seen, s);
