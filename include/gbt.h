@@ -616,7 +616,8 @@ GBT_API int32_t gbt_clip_gradients(gbt_ctx *ctx, const void *list, int32_t piece
 /* ---- around a tower over histories: embedding, head norms with rotation, orthogonalised updates ------------ */
 
 /*
- * Rows of a table by id: out_t = scale * table[ids[t]], one rounding; an id outside 0..n_rows-1 gives zeros.
+ * Rows of a table by id: out_t = scale * table[ids[t]], a product in 32 bits, rounded to out's type; an id outside
+ * 0..n_rows-1 gives zeros.
  * Rows may be any distance apart; a row's elements lie side by side, any width, each tensor aligned to its type
  * (16-byte aligned rows of a multiple of 8 elements are read and written 16 bytes at a time).
  */
@@ -635,7 +636,8 @@ GBT_API int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *params, 
 
 /*
  * The table's gradient: grad_v = scale * (sum of dout_t over all t with ids[t] = v), summed in 32 bits (by pieces: of
- * 2^28 terms fewer than 1500 roundings lie behind one another), and then rounded to grad's type; rows without an id get zeros.  accumulate != 0: added to what grad holds, other rows stay as they are.
+ * 2^28 terms fewer than 1500 roundings lie behind one another), and then rounded to grad's type; rows without an id
+ * get zeros.  accumulate != 0: added to what grad holds, other rows stay as they are.
  * table_dtype and table_stride are grad's, out_dtype and out_stride dout's.  Sums are taken in a fixed order: the
  * same result on every run.  workspace [dev]: gbt_embedding_backward_workspace_bytes (0: none needed, NULL allowed,
  * or parameters that the call refuses).  Asynchronous.

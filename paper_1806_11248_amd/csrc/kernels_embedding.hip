@@ -1,6 +1,6 @@
 // Rows of an embedding table by id, and the table's gradient.
 //
-// Lookup: out[t] = scale * table[id_t], one rounding.  Gradient: grad[v] = scale * (sum of dout[t] over the places t with id_t = v), a sum of rows that
+// Lookup: out[t] = scale * table[id_t], a product in 32 bits, rounded to out's type.  Gradient: grad[v] = scale * (sum of dout[t] over the places t with id_t = v), a sum of rows that
 // lie anywhere, of which one id may have none and another a third of all.  Places are sorted by id (stable, by digits), and a group of lanes adds up
 // a chunk of them, however the ids are spread; sums of ids that go on in the next chunk are written aside in 32 bits and added up by a second launch in
 // the chunks' order.  Where the table has few rows nothing is sorted: they are added up in LDS.  No atomics on values: the same result on every run.
