@@ -598,7 +598,8 @@ typedef struct gbt_gradient {    /* one tensor of n elements, any alignment of i
 /*
  * Lays a list of tensors out for gbt_clip_gradients, once for as long as their addresses and sizes hold:
  * list_out [dev, 16-byte aligned] of gbt_gradient_list_bytes bytes, *pieces_out [host] its length.  Lists whose
- * table exceeds 4 MB (some 170,000 tensors) are refused with GBT_EUNSUPPORTED (and 0 bytes).  Asynchronous.
+ * table exceeds 4 MB (some 170,000 tensors) are refused with GBT_EUNSUPPORTED (and 0 bytes), as are calls while the context's stream
+ * is being recorded into a graph: lay lists out before.  Asynchronous.
  */
 GBT_API size_t gbt_gradient_list_bytes(const gbt_gradient *gradients, int64_t n_gradients);
 GBT_API int32_t gbt_gradient_list(gbt_ctx *ctx, const gbt_gradient *gradients, int64_t n_gradients, void *list_out,
@@ -714,8 +715,8 @@ typedef struct gbt_matrix {      /* rows x cols elements, one row after the othe
 
 /*
  * Lays matrices out for gbt_orthogonalise, once for as long as addresses, sizes and scales hold: list_out [dev,
- * 16-byte aligned] of gbt_matrix_list_bytes bytes (0: matrices that the call refuses; at most 65536).
- * Asynchronous.
+ * 16-byte aligned] of gbt_matrix_list_bytes bytes (0: matrices that the call refuses; at most 65536).  While the
+ * context's stream is being recorded into a graph: GBT_EUNSUPPORTED.  Asynchronous.
  */
 GBT_API size_t gbt_matrix_list_bytes(const gbt_matrix *matrices, int64_t n_matrices);
 GBT_API int32_t gbt_matrix_list(gbt_ctx *ctx, const gbt_matrix *matrices, int64_t n_matrices, void *list_out, size_t list_bytes);

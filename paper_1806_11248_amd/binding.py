@@ -865,7 +865,8 @@ class Context:
     def gradient_list(self, tensors, outs=None) -> GradientList:
         """Lays gradient tensors out for clip_gradients; outs receive the results (None: the tensors themselves).  Good for as long
         as the tensors stay where they are: the list holds on to the memory that they have now and goes on with it, also where a tensor is
-        given other memory or another takes its place.  Gradients that are allocated anew each step need a list each step."""
+        given other memory or another takes its place.  Gradients that are allocated anew each step need a list each step.  Refused while a
+        graph is being recorded on the context's stream: lists are laid out before."""
         tensors = list(tensors)
         outs = tensors if outs is None else list(outs)
         if len(outs) != len(tensors):
@@ -1068,7 +1069,7 @@ class Context:
     def matrix_list(self, tensors, outs=None, *, scales=1.0) -> MatrixList:
         """Lays matrices [rows][cols] out for orthogonalise; outs receive the results (None: the tensors themselves), times scales (one for
         each, or one for all).  Good for as long as the tensors stay where they are, as a gradient_list is.  No out may share memory with another matrix, nor
-        with part of its own."""
+        with part of its own.  Refused while a graph is being recorded on the context's stream."""
         tensors = list(tensors)
         outs = tensors if outs is None else list(outs)
         scales = [float(scales)] * len(tensors) if isinstance(scales, (int, float)) else [float(x) for x in scales]

@@ -251,7 +251,14 @@ int32_t upload2(gbt_ctx *ctx, const void *a, size_t a_bytes, const void *b, size
 
 }  // namespace
 
-int32_t gbt_upload(gbt_ctx *ctx, const void *host, size_t bytes, void *dev) { return upload(ctx, host, bytes, dev); }
+int32_t gbt_upload(gbt_ctx *ctx, const void *host, size_t bytes, void *dev) {
+    // a recorded copy would read the staging when the graph is replayed, which holds something else by then
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(ctx->stream, &status);
+    if (e != hipSuccess) (void)hipGetLastError();
+    GBT_REQUIRE(ctx, e == hipSuccess && status == hipStreamCaptureStatusNone, GBT_EUNSUPPORTED, "a list is laid out before a graph is recorded, not while");
+    return upload(ctx, host, bytes, dev);
+}
 
 // ------------------------------------------------------------------ context --
 extern "C" const char *gbt_version(void) { return "libgbt 0.1 (gfx950)"; }

@@ -90,7 +90,7 @@ int32_t gbt_fail(gbt_ctx *ctx, int32_t code, const char *fmt, ...);
         if (!(cond)) return gbt_fail((ctx), (code), __VA_ARGS__); \
     } while (0)
 
-// Copies `bytes` bytes of a host table into `dev` on the context's stream, through the pinned staging.
+// Copies `bytes` bytes of a host table into `dev` on the context's stream, through the pinned staging.  GBT_EUNSUPPORTED while a graph is being recorded.
 int32_t gbt_upload(gbt_ctx *ctx, const void *host, size_t bytes, void *dev);
 
 static constexpr inline size_t gbt_align(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
