@@ -134,3 +134,40 @@ def test_sixteen_bit_results_are_rounded_ones(ctx, m, n):
         here = sum(int((o != w).sum()) for o, w in zip(outs, want))
         there = sum(int((in_32_bits(u).to(dtype) != w).sum()) for u, w in zip(updates, want))
         assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (here, there, count * m * n)
+
+
+def _check_list(ctx, updates):
+    """Float32 results beside 32-bit products, all of a shape together; those of sixteen bits by the share that is not the rounded 64-bit one."""
+    scales = [0.5 + 0.25 * (i % 3) for i in range(len(updates))]                     # what they are multiplied by is exact in each type
+    outs = ctx.orthogonalise(ctx.matrix_list(updates, [torch.full_like(u, 9.0) for u in updates], scales=scales))
+    for u, o, scale in zip(updates, outs, scales):
+        want, other = exact(u) * scale, in_32_bits(u) * scale
+        if u.dtype is torch.float32:
+            assert off(o, want) <= 1.25 * off(other, want), (u.shape, off(o, want), off(other, want))
+        else:
+            here, there = (int((x.to(u.dtype) != want.to(u.dtype)).sum()) for x in (o, other))
+            assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (u.shape, u.dtype, here, there)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_more_tiles_than_run_at_once(ctx, dtype):
+    """Symmetric products of more than 512 tiles too, two workgroups on a compute unit: 8 x 45 and 8 x 28 of them, and 16 x 10, wide and tall, with odd sizes."""
+    _check_list(ctx, [_averaged(m, n, seed, dtype) for seed in range(8) for m, n in ((1100, 1400), (1001, 777), (512, 2048), (2048, 512))])
+
+
+def test_all_kinds_in_one_list(ctx):
+    """Kinds one after the other, of which each begins with the first tile of its own."""
+    shapes = [(64, 200), (300, 500), (1100, 900), (200, 1700), (2200, 1300), (40, 40), (129, 1000)]
+    _check_list(ctx, [_averaged(m, n, 100 + i, dtype) for i, (m, n) in enumerate(shapes) for dtype in (torch.bfloat16, torch.float32, torch.float16)])
+
+
+def test_groups_that_share_the_workspace(ctx):
+    """Matrices of 1.6 GB of workspace each are worked on one after the other, in the same memory; the longest rows that there can be."""
+    updates = [_averaged(128, 1 << 20, 1, torch.bfloat16), _averaged(1 << 20, 100, 2, torch.bfloat16), _averaged(90, 70, 3, torch.bfloat16)]
+    lst = ctx.matrix_list(updates, [torch.zeros_like(u) for u in updates])
+    assert (3 << 29) < lst.workspace_bytes <= (2 << 30)
+    outs = ctx.orthogonalise(lst)
+    for u, o in zip(updates, outs):
+        want = exact(u).to(u.dtype)
+        here, there = int((o != want).sum()), int((in_32_bits(u).to(u.dtype) != want).sum())
+        assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (u.shape, here, there)
