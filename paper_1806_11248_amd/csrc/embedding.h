@@ -24,7 +24,7 @@ struct EmbedArgs {
     uint32_t *seen;                    // [chunks]: the rows that it met, a bit for each
 };
 
-constexpr int kEmbedFewIds = 2048;     // more than that are sorted
+constexpr int kEmbedFewIds = 2048;     // more than that are sorted, or added up in LDS
 constexpr int kEmbedFewRows = 32;      // up to so many are added up in LDS, unsorted
 constexpr int kSortItems = 4096;       // ids that a workgroup of the sort ranks at a time
 constexpr int kSortTiles = 256;        // workgroups of a pass at most

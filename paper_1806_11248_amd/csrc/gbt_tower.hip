@@ -49,7 +49,9 @@ void fill(EmbedArgs &a, const gbt_embedding_params &p, const void *table, void *
     a.out_dtype = p.out_dtype;
 }
 
-// Few ids are looked for by the workgroups that own rows, unless these are too many.
+// Few ids are looked for by the workgroups that own rows, unless these are too many.  (us, bfloat16, of ids, rows and columns by those and sorted: 32 of 40 of 64 7.5 and 16;
+// 2000 8.0 and 22; 2000 of 40 of 2048 10 and 23; 500 of 5000 of 512 7.8 and 30, 2000 12 and 34; 2000 of 100,000 of 512 41 and 64.  Only where ids are many and rows so few
+// that most compute units own none it loses: 500 of 2 of 2048 21 and 25, 2048 73 and 22.)
 constexpr int64_t kFewRowsWorkgroups = 4096;   // aimed at; a workgroup owns 32 rows at most
 bool takes_few_ids(const gbt_embedding_params &p) { return p.n_ids <= kEmbedFewIds && p.n_rows <= kFewRowsWorkgroups * 32; }
 

@@ -643,7 +643,10 @@ hipError_t launch_form(hipStream_t stream, const OrthoArgs &a, int64_t tiles) {
     ortho_product_kernel<kProduct, kWaves, kStages><<<(unsigned)tiles, 64 * kWaves, kLds, stream>>>(a);
     return hipGetLastError();
 }
-// Many tiles: two workgroups on a compute unit, with two stages each; few: one with all of the LDS, as the loads' latency is what counts.
+// Many tiles: two workgroups on a compute unit, with two stages each; few: one with all of the LDS, as the loads' latency is what counts.  (us of five steps on matrices of
+// bfloat16, two workgroups everywhere and one: one of 512 x 512, 10 tiles of symmetric products and 16 of F X, 332 and 283; 24, 240 and 384, 478 and 465; 64, 640 and
+// 1024, 1164 and 1201.  Between one and two tiles a compute unit it goes by how they lie: 32 of 512 x 512, 320 and 512, 616 and 693; 12 of 1024 x 1024, 432 and 768,
+// 1178 and 1324; but with two from one tile a compute unit on, 26 matrices of seven sizes, 296 symmetric tiles, 889 in place of 845.)
 template <int kProduct>
 hipError_t launch(hipStream_t stream, const OrthoArgs &a, int64_t tiles, int num_cu) {
     return tiles <= 2 * num_cu ? launch_form<kProduct, 8, 5>(stream, a, tiles) : launch_form<kProduct, 4, 2>(stream, a, tiles);
