@@ -190,9 +190,9 @@ __device__ __forceinline__ void fetch_stage(Stage &s, const char *p, const char 
         }
 }
 
-// Sums of many products are added up in pieces of 128, so that the matrix units' roundings, which do not go to the nearest and so do not cancel, are those of few and small
-// numbers.  (777 x 1001 in float32: pieces of 512 3.2e-6 off, of 128 2.2e-6, of 64 1.9e-6, and 32-bit products 2.4e-6; 4096 x 4096 5.2e-6, 3.4e-6, 3.4e-6 and
-// 8.4e-6.  4096 x 4096, 4096 x 8192 and two of 1024 x 4096 take 10.6, 10.8 and 11.0 ms.)
+// Sums of many products are added up in pieces of 128, so that roundings are those of few and small sums: an instruction's own is off by 0.4 units of its sum's last place (root
+// mean square; one to the nearest by 0.29), and there are three for every 16 products.  (777 x 1001 in float32: pieces of 512 3.2e-6 off, of 128 2.2e-6, of 64 1.9e-6, and
+// 32-bit products 2.4e-6; 4096 x 4096 5.2e-6, 3.4e-6, 3.4e-6 and 8.4e-6.  4096 x 4096, 4096 x 8192 and two of 1024 x 4096 take 10.6, 10.8 and 11.0 ms.)
 constexpr int kPiece = 4;   // steps
 
 // A wave's operands of sixteen steps along the sum: [part][row or column of 32].
@@ -210,20 +210,21 @@ struct Operands {
             for (int j = 0; j < kAcross; ++j) y[part][j] = Step::rows<F16>(s.q[across][part], first + 32 * j, step, lane);
         }
     }
-    // low * high, high * low, high * high: the sums in turn, so that none waits for itself
+    // low * low where that is wanted, low * high, high * low, high * high: the sums in turn, so that none waits for itself
+    template <bool kLow>
     __device__ __forceinline__ void add(f32x16 (&acc)[2][kAcross]) const {
 #pragma unroll
-        for (int of = 0; of < 3; ++of)
+        for (int of = kLow ? -1 : 0; of < 3; ++of)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < kAcross; ++j) acc[i][j] = F16::mma(x[of == 0][i], y[of == 1][j], acc[i][j]);
+                for (int j = 0; j < kAcross; ++j) acc[i][j] = F16::mma(x[of <= 0][i], y[of == 1 || of < 0][j], acc[i][j]);
     }
 };
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }   // what is before it is issued before what is behind it
 
 // While the matrix units work on one half of a step, the operands of the next half are read, also from the next step, behind the barrier.
-template <int kWaves, int kStages>
+template <bool kLow, int kWaves, int kStages>
 __device__ __forceinline__ void product(f32x16 (&sum)[2][8 / kWaves], Stage *stages, const char *p, const char *q, int64_t row, int steps, int wave, int lane) {
     constexpr int kAcross = 8 / kWaves, kLoads = 4 * (8 / kWaves);   // of a stage, by each wave
     f32x16 acc[2][kAcross] = {};
@@ -241,7 +242,7 @@ __device__ __forceinline__ void product(f32x16 (&sum)[2][8 / kWaves], Stage *sta
         in_order();
         if (next < steps) fetch_stage<kWaves>(stages[at], p + (int64_t)next * (kPair * 2), q + (int64_t)next * (kPair * 2), row, wave, lane * 16);
         if (k > 0) {
-            odd.add(acc);
+            odd.template add<kLow>(acc);
             if ((k & (kPiece - 1)) == 0) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -255,11 +256,11 @@ __device__ __forceinline__ void product(f32x16 (&sum)[2][8 / kWaves], Stage *sta
         in_order();
         odd.read(stages[now], 1, wave, lane);
         in_order();
-        even.add(acc);
+        even.template add<kLow>(acc);
         in_order();
         now = now + 1 == kStages ? 0 : now + 1;
     }
-    odd.add(acc);
+    odd.template add<kLow>(acc);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -375,8 +376,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps = depth / 32;
     const int64_t row_bytes = (int64_t)steps * kPair * 2;
     f32x16 acc[2][8 / kWaves] = {};
-    product<kWaves, kStages>(acc, (Stage *)lds, (const char *)p + (int64_t)ti * 2 * row_bytes + wave * (8192 / kWaves),
-                             (const char *)q + (int64_t)tj * 2 * row_bytes + wave * (8192 / kWaves), row_bytes, steps, wave, lane);
+    const char *p_rows = (const char *)p + (int64_t)ti * 2 * row_bytes + wave * (8192 / kWaves);
+    const char *q_rows = (const char *)q + (int64_t)tj * 2 * row_bytes + wave * (8192 / kWaves);
+    // What is left out of X X^T and A A with low * low is never negative on their diagonals, 2^-24.4 of them, and the factor's elements there are small differences of larger ones.  Of a
+    // few long rows, which are nearly orthogonal, that is most of the error; where there are more it is not seen.  (2000 x 30 1.8e-6 off without, 1.4e-6 with, 32-bit products
+    // 1.2e-6; 689 x 15 1.7e-6, 1.25e-6, 1.24e-6; 300 x 300 1.4e-6 either way.  With it in all products, 4096 x 4096, 4096 x 8192 and two of 1024 x 4096 take 12.4 in place of 10.6 ms.)
+    if ((kProduct == kOrthoFactor || kProduct == kOrthoGram) && m.pp == kOrthoTile) product<true, kWaves, kStages>(acc, (Stage *)lds, p_rows, q_rows, row_bytes, steps, wave, lane);
+    else product<false, kWaves, kStages>(acc, (Stage *)lds, p_rows, q_rows, row_bytes, steps, wave, lane);
     const int first_row = ti * kOrthoTile + (kWaves == 4 ? wave >> 1 : wave >> 2) * 64, first_col = tj * kOrthoTile + (kWaves == 4 ? (wave & 1) * 64 : (wave & 3) * 32);
     const Exchange swap(lane);
     if (kApply && a.last) {
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
         else put_result<_Float16>(m, acc, first_row, first_col, a.less, lane, swap);
         return;
     }
-    const float less = second ? a.less_second : a.less;
+    const float less = second ? a.less_second : a.less, to_factor = a.up_factor / a.up_gram;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         // A is symmetric: its four values of a lane's column lie side by side in the row of that number.  All are read before anything is written.
@@ -409,9 +415,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
                 if (kProduct == kOrthoFactor) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[j][r / 4][e] + (float)low[j][r / 4][e]));
-                        if (row + e == col) v[e] = fmaf(a.a, a.up_gram, v[e]);
-                        v[e] *= a.up_factor / a.up_gram;
+                        const float with_a = row + e == col ? a.a * a.up_gram : 0.0f;
+                        v[e] = fmaf(a.c, v[e], fmaf(a.b, (float)high[j][r / 4][e] + (float)low[j][r / 4][e], with_a)) * to_factor;
                     }
                 }
                 put_four(to, cols, to_t, m.pp, row, col, v, kApply || ti != tj, swap);
@@ -428,8 +433,8 @@ struct Small {
     char *gram, *factor, *total, *x;
     int wave, lane;
 };
-// One wave has nothing but this to do, so its three kinds of products are three sums, that none waits for another.
-__device__ __forceinline__ void small_product(f32x16 &acc, const Small &s, const char *p, const char *q, int blocks) {
+// One wave has nothing but this to do, so its three kinds of products are three sums, that none waits for another.  `low`: low * low too, for A A.
+__device__ __forceinline__ void small_product(f32x16 &acc, const Small &s, const char *p, const char *q, int blocks, bool low) {
     f32x16 sum[3] = {};
     for (int b = 0; b < blocks; b += 2) {
         f16x8 x[4][2], y[4][2];
@@ -444,6 +449,7 @@ __device__ __forceinline__ void small_product(f32x16 &acc, const Small &s, const
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (b + (k >> 1) < blocks) {
+                if (low) sum[2] = F16::mma(x[k][1], y[k][1], sum[2]);
                 sum[0] = F16::mma(x[k][1], y[k][0], sum[0]);
                 sum[1] = F16::mma(x[k][0], y[k][1], sum[1]);
                 sum[2] = F16::mma(x[k][0], y[k][0], sum[2]);
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoSmal
             const char *p = kind < 0 ? s.x : kind == 0 || kind == 3 ? s.gram : f, *q = kind < 0 ? s.x : kind == 1 ? s.total : kind == 3 ? f : s.gram;
             char *to = kind == 0 ? f : kind == 1 ? s.total : s.gram;
             f32x16 acc;
-            small_product(acc, s, p, q, kind < 0 ? blocks : 2);
+            small_product(acc, s, p, q, kind < 0 ? blocks : 2, kind == 0);
             const OrthoSmallScales::Step &scale = up.step[done + max(i, 0)];
             const float up_gram = scale.gram, to_factor = scale.factor, less = kind < 0 ? kScaleDown : scale.less[max(kind, 0)];
             if (kind > 0) __syncthreads();   // it goes over an operand
@@ -571,9 +577,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(OrthoArgs a, OrthoSmal
                     const f16x4 high = *(const f16x4 *)(s.gram + at), low = *(const f16x4 *)(s.gram + at + kBlock * 2);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[e] = fmaf(a.c, v[e], a.b * ((float)high[e] + (float)low[e]));
-                        if (row + e == col) v[e] = fmaf(a.a, up_gram, v[e]);
-                        v[e] *= to_factor;
+                        const float with_a = row + e == col ? a.a * up_gram : 0.0f;
+                        v[e] = fmaf(a.c, v[e], fmaf(a.b, (float)high[e] + (float)low[e], with_a)) * to_factor;
                     }
                 }
                 small_put(to + at, v);

@@ -106,14 +106,16 @@ def _averaged(m, n, seed, dtype=torch.float32):
 
 # one workgroup's; one tile; one step on A at a time, several tiles; two steps; rows of tiles past the first eight; more tiles than run at once
 SHAPES = [(64, 64), (64, 256), (384, 40), (100, 120), (128, 128), (200, 1500), (300, 300), (1500, 200), (400, 400), (512, 2048), (700, 2400), (767, 800), (768, 768), (777, 1001),
-          (1001, 777), (900, 900), (1100, 1400), (2100, 4200), (4200, 2100)]
+          (1001, 777), (900, 900), (1100, 1400), (2100, 4200), (4200, 2100),
+          # a few long rows
+          (689, 15), (30, 2000), (12, 1108), (20, 300), (8, 380), (1000, 8)]
 
 
 @pytest.mark.parametrize("m,n", SHAPES)
 def test_as_exact_as_32_bit_products(ctx, m, n):
     """Beside the library's on this card: a quarter more at most, for what errors of one matrix differ from those of the next.  Operands of one part would be off
     a thousand times as far."""
-    count = max(1, min(8, 100_000 // (m * n)))
+    count = max(1, min(24, 200_000 // (m * n)))
     updates = [_averaged(m, n, seed) for seed in range(count)]
     outs = ctx.orthogonalise(ctx.matrix_list(updates, [torch.zeros_like(u) for u in updates]))
     want = [exact(u) for u in updates]
