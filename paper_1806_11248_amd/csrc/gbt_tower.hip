@@ -369,25 +369,25 @@ const char *matrices_fault(const gbt_matrix *m, int64_t n, int32_t *code) {
 // Kinds of matrices, which are worked on apart: small or not, and by how many steps are taken on A = X X^T alone before X is multiplied and A taken anew.
 //
 // An error of A grows by the square of the singular values' factor with each such step where singular values are small, and makes a relative one of the
-// result there.  In large matrices sums leave more than that.  (Five steps, averaged gradients; float32, one step at a time, two, and products of 32 bits in torch: 64 x 64
-// 6.2e-7, 1.8e-6, 1.0e-6 off; 400 x 400 1.6e-6, 2.6e-6, 2.0e-6; 700 x 2400 1.7e-6, 2.2e-6, 2.2e-6; 900 x 900 2.1e-6, 2.2e-6, 2.7e-6; 4096 x 4096 4.0e-6, 3.4e-6, 8.4e-6.
-// float16, the share of elements that are not the rounded 64-bit ones, two steps, three, and 32-bit products rounded: 64 x 64 1.0%, 3.2%, 0.6%; 128 x 128 1.1%, 3.0%,
-// 0.7%; 200 x 1500 1.0%, 1.5%, 0.6%; 300 x 300 1.4%, 1.4%, 1.1%; 512 x 2048 1.4%, 0.8%, 1.0%.  Two in place of one: 4096 x 4096, 4096 x 8192 and two of 1024 x 4096 10.5 in place of
-// 11.4 ms; three in place of two: 26 of 512 x 512 to 512 x 2048 in sixteen bits 845 in place of 917 us.)
-enum OrthoKind { kSmallOne, kSmallTwo, kOne, kTwo, kThree };
+// result there.  In large matrices sums leave more than that, and rounding to sixteen bits hides all but its share.  (Five steps, averaged gradients; float32, one step at a
+// time, two, and products of 32 bits in torch: 64 x 64 6.2e-7, 1.8e-6, 1.0e-6 off; 400 x 400 1.6e-6, 2.6e-6, 2.0e-6; 700 x 2400 1.7e-6, 2.2e-6, 2.2e-6; 900 x 900 2.1e-6,
+// 2.2e-6, 2.7e-6; 4096 x 4096 4.0e-6, 3.4e-6, 8.4e-6.  float16, the share of elements that are not the rounded 64-bit ones, two steps, three, and 32-bit products rounded: 64 x 64
+// 1.0%, 3.2%, 0.6%; 128 x 128 1.1%, 3.0%, 0.7%; 200 x 1500 1.0%, 1.5%, 0.6%; 512 x 2048 1.4%, 0.8%, 1.0%.  Two in place of one: 4096 x 4096, 4096 x 8192 and two of
+// 1024 x 4096 10.5 in place of 11.4 ms.  Three for large matrices of sixteen bits would take 26 of 512 x 512 to 512 x 2048 from 917 us to 845, but as a kind of their own
+// beside small ones most lists of both to a half more: 643 x 2467 and four smaller shapes, 20 matrices, 949 in place of 720.)
+enum OrthoKind { kSmallOne, kSmallTwo, kOne, kTwo };
 OrthoKind kind_of(const gbt_matrix &m) {
     const bool wide = m.dtype == GBT_F32;
     const int64_t p = std::min(m.rows, m.cols), w = std::max(m.rows, m.cols);
     if (p <= kOrthoSmallP && w <= kOrthoSmallW) return wide ? kSmallOne : kSmallTwo;
-    return wide ? (p < 768 ? kOne : kTwo) : (p < 256 ? kTwo : kThree);
+    return wide && p < 768 ? kOne : kTwo;
 }
 bool small_kind(OrthoKind kind) { return kind <= kSmallTwo; }
-// For singular values' factors up to `factor`, of which a larger one than 4 takes fewer: errors may grow by 2^4, or by 2^8.  (At most four, so that scales stay among
+// For singular values' factors up to `factor`, of which one above 4 takes one step at a time: errors may grow by 2^4.  (At most four, so that scales stay among
 // float32's normal numbers.)
 int steps_together(double factor, OrthoKind kind) {
-    const double growth = kind == kThree ? 256.0 : 16.0;
     int n = 1;
-    while (kind != kSmallOne && kind != kOne && n < 4 && pow(factor * factor, n) <= growth) ++n;
+    while (kind != kSmallOne && kind != kOne && n < 4 && pow(factor * factor, n) <= 16.0) ++n;
     return n;
 }
 
