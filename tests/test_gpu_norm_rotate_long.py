@@ -164,3 +164,15 @@ def test_many_ragged_rows(ctx, heads, kv_heads, dim, turned, halves):
     kept = torch.ones(len(ks), dtype=torch.bool, device="cuda")
     kept[to.cuda()[goes]] = False
     assert bool((ks[kept] == 7).all()) and bool((vs[kept] == 7).all())
+
+
+@pytest.mark.parametrize("rows,heads,dim", [(1 << 21, 64, 128), (300_000, 3, 40)])
+def test_long_sums_of_equal_terms(ctx, rows, heads, dim):
+    """Heads of ones and the same gradient everywhere: the weight's gradient is that by sqrt(1 + eps), times rows and heads, of which each addition is rounded the same
+    way.  At most 256 are added up behind one another, some 50 of such sums by a wave, and a few dozen more join those."""
+    ones, d = torch.ones(1, 1, dim, dtype=BF16, device="cuda"), torch.linspace(0.1, 1.9, dim, device="cuda").to(BF16).view(1, 1, dim)
+    q, k = ones.expand(rows, heads, dim), ones.expand(rows, 1, dim)
+    _, _, dwq, dwk = ctx.norm_rotate_backward(d.expand(rows, heads, dim), d.expand(rows, 1, dim), q, k, None, None, None, eps=0.3)
+    for dw, count in ((dwq, rows * heads), (dwk, rows)):
+        want = d.double().flatten() * count / (1 + float(torch.tensor(0.3))) ** 0.5
+        assert float(((dw.double() - want).abs() / want).max()) <= 400 * 2.0 ** -24, float(((dw.double() - want).abs() / want).max())
