@@ -383,13 +383,8 @@ OrthoKind kind_of(const gbt_matrix &m) {
     return wide && p < 768 ? kOne : kTwo;
 }
 bool small_kind(OrthoKind kind) { return kind <= kSmallTwo; }
-// For singular values' factors up to `factor`, of which one above 4 takes one step at a time: errors may grow by 2^4.  (At most four, so that scales stay among
-// float32's normal numbers.)
-int steps_together(double factor, OrthoKind kind) {
-    int n = 1;
-    while (kind != kSmallOne && kind != kOne && n < 4 && pow(factor * factor, n) <= 16.0) ++n;
-    return n;
-}
+// For singular values' factors up to `factor`: an error may grow by 2^4.
+int steps_together(double factor, OrthoKind kind) { return kind == kSmallOne || kind == kOne || factor > 4.0 ? 1 : 2; }
 
 // The power of two that a matrix with singular values up to `most`, and so with no larger elements, is held times; `least`: as if most were at least 2^least.
 float scale_for(double most, int least) { return most <= ldexp(1.0, least) ? ldexpf(kScaleUp, -least) : (float)exp2(15.0 - ceil(log2(most))); }
@@ -517,7 +512,7 @@ bool next_group(const gbt_matrix *matrices, const OrthoOrder &order, int64_t *at
         o.piece_begin = g->pieces;
         o.fill_begin = g->fill_tiles;
         o.x = used, o.xt[0] = used + of_x, o.xt[1] = used + 2 * of_x;
-        o.gram = used + 3 * of_x, o.factor = o.gram + of_a, o.both = o.factor + of_a, o.total[0] = o.both + of_a, o.total[1] = o.total[0] + of_a;
+        o.gram = used + 3 * of_x, o.factor[0] = o.gram + of_a, o.factor[1] = o.gram + 2 * of_a, o.between = o.gram + 3 * of_a, o.total = o.gram + 4 * of_a;
         if (list) list[*at] = o;
         g->kind = kind;
         ++g->count;
@@ -653,33 +648,29 @@ extern "C" int32_t gbt_orthogonalise(gbt_ctx *ctx, const void *list, const gbt_m
             continue;
         }
         GBT_HIP(ctx, gbt_launch_ortho_begin(ctx->stream, o, g.pieces, g.fill_tiles));
-        auto product = [&](OrthoProduct of, bool both = false) {
+        auto product = [&](OrthoProduct of) {
             const OrthoTiles kind = of == kOrthoGram ? kTilesGram : of == kOrthoApply ? kTilesFull : kTilesSym;
             o.tiles = tiles + (kind > 0 ? g.tiles[0] : 0) + (kind > 1 ? g.tiles[1] : 0);
             o.count_tiles = g.tiles[kind];
-            return gbt_launch_ortho_product(ctx->stream, o, of, both, ctx->num_cu);
+            return gbt_launch_ortho_product(ctx->stream, o, of, ctx->num_cu);
         };
         for (int s = 0; s < steps; s += together) {
             const int n = std::min(together, steps - s);
-            o.less = o.less_second = kScaleDown;
+            o.less = kScaleDown;
             GBT_HIP(ctx, product(kOrthoGram));
-            for (int t = s; t < s + n; ++t) {
-                o.first = t == s;
+            for (o.step = 0;; ++o.step) {
+                const int t = s + o.step;
                 o.up_gram = up.gram(t);
                 o.up_factor = up.factor[t];
                 o.less = 1.0f / o.up_gram;
                 GBT_HIP(ctx, product(kOrthoFactor));
-                if (t < s + n - 1) {   // F A and, from the second step on, the product of the factors; then A of the next step
-                    o.less = up.after(t);
-                    GBT_HIP(ctx, product(kOrthoBoth, !o.first));
-                    if (!o.first) o.total ^= 1;
-                    GBT_HIP(ctx, product(kOrthoNext));
-                } else if (!o.first) {
-                    o.less = kScaleDown;
-                    GBT_HIP(ctx, product(kOrthoTotal));
-                    o.total ^= 1;
-                }
+                if (o.step == n - 1) break;
+                o.less = up.after(t);   // F A, then A of the next step
+                GBT_HIP(ctx, product(kOrthoBetween));
+                GBT_HIP(ctx, product(kOrthoNext));
             }
+            o.less = kScaleDown;
+            if (n == 2) GBT_HIP(ctx, product(kOrthoTotal));
             o.last = s + n == steps;
             o.less = up.apply(s, s + n, steps);
             GBT_HIP(ctx, product(kOrthoApply));

@@ -1,10 +1,10 @@
 // Updates of weight matrices, orthogonalised: X = G / |G|, then X <- F X with F = a I + b A + c A^2, A = X X^T, a few times, which takes all singular
 // values towards one.
 //
-// All F and A of one X commute: A after a step is F A F, so several steps are taken on the p x p matrices alone, and X is multiplied once by the product
+// All F and A of one X commute: A after a step is F A F, so two steps can be taken on the p x p matrices alone, and X is multiplied once by the product
 // of their factors.  That halves the work where X is wide, and costs nothing where it is square (a step on X is 1.5 w/p + 0.5 products of p x p x p, one on
 // A is 2; symmetric ones count half).  But an error of A grows by a^2 with each such step where singular values are small, so X is multiplied and A taken
-// anew after as many steps as leave errors like those of 32-bit products, one to three (kind_of, gbt_tower.hip).
+// anew after one step or two, as many as leave errors like those of 32-bit products (kind_of, gbt_tower.hip).
 //
 // Steps multiply small singular values, and with them whatever rounding left there, by a^steps (some 500), so sixteen bits do not do for what lies
 // between products, and matrix instructions on 32 bits run at a sixteenth of the rate.  Everything between products is held in two float16 parts, high
@@ -358,19 +358,16 @@ template <int kProduct, int kWaves, int kStages>
 __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs a) {
     extern __shared__ __attribute__((aligned(256))) char lds[];
     constexpr bool kApply = kProduct == kOrthoApply;
-    const bool second = kProduct == kOrthoBoth && blockIdx.x >= a.count_tiles;
-    const OrthoTile tile = a.tiles[blockIdx.x - (second ? a.count_tiles : 0)];
+    const OrthoTile tile = a.tiles[blockIdx.x];
     if (tile.matrix < 0) return;
     const OrthoMatrix &m = a.list[tile.matrix];
     const int ti = tile.i, tj = tile.j;
     auto at = [&](int64_t offset) { return (_Float16 *)(a.workspace + offset); };
-    // a step's factor; the first one of some begins their product
-    const int64_t factor = a.first ? m.total[a.total] : m.factor;
-    const _Float16 *p = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor ? m.gram : kProduct == kOrthoNext ? m.both : kApply ? m.total[a.total] : factor);
-    const _Float16 *q = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor ? m.gram : kProduct == kOrthoNext ? factor : kApply ? m.xt[a.xt]
-                           : kProduct == kOrthoTotal || second ? m.total[a.total] : m.gram);
-    _Float16 *to = at(kProduct == kOrthoGram || kProduct == kOrthoNext ? m.gram : kProduct == kOrthoFactor ? factor : kApply ? m.x
-                      : kProduct == kOrthoTotal || second ? m.total[a.total ^ 1] : m.both);
+    const _Float16 *p = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor ? m.gram : kProduct == kOrthoBetween ? m.factor[0] : kProduct == kOrthoNext ? m.between
+                           : kProduct == kOrthoTotal ? m.factor[1] : a.step == 0 ? m.factor[0] : m.total);
+    const _Float16 *q = at(kProduct == kOrthoGram ? m.x : kProduct == kOrthoFactor || kProduct == kOrthoBetween ? m.gram : kApply ? m.xt[a.xt] : m.factor[0]);
+    _Float16 *to = at(kProduct == kOrthoGram || kProduct == kOrthoNext ? m.gram : kProduct == kOrthoFactor ? m.factor[a.step] : kProduct == kOrthoBetween ? m.between
+                      : kProduct == kOrthoTotal ? m.total : m.x);
     _Float16 *to_t = kApply ? at(m.xt[a.xt ^ 1]) : to;
     const int depth = kProduct == kOrthoGram ? m.ww : m.pp, cols = kApply ? m.ww : m.pp;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps = depth / 32;
@@ -391,7 +388,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void ortho_product_kernel(OrthoArgs
         else put_result<_Float16>(m, acc, first_row, first_col, a.less, lane, swap);
         return;
     }
-    const float less = second ? a.less_second : a.less, to_factor = a.up_factor / a.up_gram;
+    const float less = a.less, to_factor = a.up_factor / a.up_gram;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         // A is symmetric: its four values of a lane's column lie side by side in the row of that number.  All are read before anything is written.
@@ -674,12 +671,12 @@ hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const 
     return hipGetLastError();
 }
 
-hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, bool both, int num_cu) {
-    const int64_t tiles = both ? 2 * a.count_tiles : a.count_tiles;
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int num_cu) {
+    const int64_t tiles = a.count_tiles;
     switch (product) {
         case kOrthoGram: return launch<kOrthoGram>(stream, a, tiles, num_cu);
         case kOrthoFactor: return launch<kOrthoFactor>(stream, a, tiles, num_cu);
-        case kOrthoBoth: return launch<kOrthoBoth>(stream, a, tiles, num_cu);
+        case kOrthoBetween: return launch<kOrthoBetween>(stream, a, tiles, num_cu);
         case kOrthoTotal: return launch<kOrthoTotal>(stream, a, tiles, num_cu);
         case kOrthoNext: return launch<kOrthoNext>(stream, a, tiles, num_cu);
         default: return launch<kOrthoApply>(stream, a, tiles, num_cu);

@@ -18,7 +18,7 @@ struct OrthoMatrix {
     int32_t pieces;                     // of its elements
     int64_t piece_begin;                // of the group's pieces
     int64_t x, xt[2];                   // bytes into the workspace: X, its transpose (and the next one)
-    int64_t gram, factor, both, total[2];   // p x p: A, a step's factor F of it, F A, and the product of the factors so far (and the next one)
+    int64_t gram, factor[2], between, total;   // p x p: A, the factors F of a round's one or two steps, F A between them, and the product of both
     int64_t fill_begin;                 // of the group's workgroups that lay X out
 };
 // What a workgroup of a product computes: tile (i, j) of one matrix of the group; matrix < 0: nothing.
@@ -59,11 +59,11 @@ struct OrthoArgs {
     float a, b, c;
     float up_x;                         // what X is held times as it is laid out
     float up_gram, up_factor;           // likewise A and its factor of the step
-    float less, less_second;            // from the operands' scales to the result's, and that of kOrthoBoth's second one (kOrthoApply, last: to none)
+    float less;                         // from the operands' scales to the result's (kOrthoApply, last: to none)
     const OrthoTile *tiles;             // of the product
     int64_t count_tiles;
-    int xt, total;                      // which of the two transposes is X's, which of the two products of factors the last one
-    int first, last;                    // first: the factor is the first of some, and begins their product; last: the result goes to dst
+    int xt;                             // which of the two transposes is X's
+    int step, last;                     // step: 0 or 1 of a round (kOrthoApply: its last); last: the result goes to dst
 };
 
 // Matrices that one workgroup takes as a whole: X's blocks and three matrices of p x p in LDS.
@@ -71,8 +71,8 @@ constexpr int kOrthoSmallP = 64, kOrthoSmallW = 384;
 constexpr int kOrthoSmallLds = 3 * 16384 + kOrthoSmallW / 32 * 8192;
 hipError_t gbt_launch_ortho_small(hipStream_t stream, const OrthoArgs &a, const OrthoSmallScales &up, int steps, int together);
 
-enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBoth, kOrthoTotal, kOrthoNext, kOrthoApply };
+enum OrthoProduct { kOrthoGram, kOrthoFactor, kOrthoBetween, kOrthoTotal, kOrthoNext, kOrthoApply };
 
 hipError_t gbt_launch_ortho_begin(hipStream_t stream, const OrthoArgs &a, int64_t pieces, int64_t fill_tiles);
-// a.tiles are those of symmetric products' upper halves, or all of X's for kOrthoApply; `both`: kOrthoBoth computes the product of the factors too.
-hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, bool both, int num_cu);
+// a.tiles are those of symmetric products' upper halves, or all of X's for kOrthoApply.
+hipError_t gbt_launch_ortho_product(hipStream_t stream, const OrthoArgs &a, OrthoProduct product, int num_cu);

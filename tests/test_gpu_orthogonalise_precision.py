@@ -173,3 +173,22 @@ def test_groups_that_share_the_workspace(ctx):
         want = exact(u).to(u.dtype)
         here, there = int((o != want).sum()), int((in_32_bits(u).to(u.dtype) != want).sum())
         assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (u.shape, here, there)
+
+
+@pytest.mark.parametrize("steps", [3, 4, 8, 13])
+@pytest.mark.parametrize("coefficients", [(1.5, -0.5, 0.0), (1.875, -1.25, 0.375)])
+def test_factors_of_less_than_two(ctx, steps, coefficients):
+    """Iterations that end at one without going past it: x f(x) has a slope between zero and f(x), so no step makes a relative error larger, and 32-bit products
+    are off by a few roundings in all.  Results here are off by those of 22 bits and a sign, 2^-23, of X, of F, of what A adds to F (less than F itself is), and by low * low,
+    which is left out and is as much: four of them a step at most."""
+    for m, n, dtype in ((40, 64, torch.float16), (130, 150, torch.float16), (300, 500, torch.float16), (800, 900, torch.float32), (70, 150, torch.float32), (40, 30, torch.float32)):
+        updates = [_averaged(m, n, seed, dtype) for seed in range(max(1, min(8, 100_000 // (m * n))))]
+        outs = ctx.orthogonalise(ctx.matrix_list(updates, [torch.zeros_like(u) for u in updates]), steps=steps, coefficients=coefficients)
+        want, others = [exact(u, steps, coefficients) for u in updates], [in_32_bits(u, steps, coefficients) for u in updates]
+        if dtype is torch.float32:
+            here, there = (math.sqrt(sum(off(o, w) ** 2 for o, w in zip(x, want))) for x in (outs, others))
+            length = math.sqrt(sum(float(torch.linalg.vector_norm(w)) ** 2 for w in want))
+            assert here <= max(TIMES * there, 4 * steps * 2.0 ** -23 * length), (m, n, here, there, length)
+        else:
+            here, there = (sum(int((o.to(dtype) != w.to(dtype)).sum()) for o, w in zip(x, want)) for x in (outs, others))
+            assert here <= TIMES * there + 4 * math.sqrt(TIMES * there + 1), (m, n, here, there)
