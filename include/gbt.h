@@ -640,8 +640,8 @@ GBT_API int32_t gbt_embedding(gbt_ctx *ctx, const gbt_embedding_params *params, 
  * 2^28 terms fewer than 1500 roundings lie behind one another), and then rounded to grad's type; rows without an id
  * get zeros.  accumulate != 0: added to what grad holds, other rows stay as they are.
  * table_dtype and table_stride are grad's, out_dtype and out_stride dout's.  Sums are taken in a fixed order: the
- * same result on every run.  workspace [dev]: gbt_embedding_backward_workspace_bytes (0: none needed, NULL allowed,
- * or parameters that the call refuses).  Asynchronous.
+ * same result on every run.  grad overlaps no input.  workspace [dev]: gbt_embedding_backward_workspace_bytes
+ * (0: none needed, NULL allowed, or parameters that the call refuses).  Asynchronous.
  */
 GBT_API size_t gbt_embedding_backward_workspace_bytes(const gbt_embedding_params *params);
 GBT_API int32_t gbt_embedding_backward(gbt_ctx *ctx, const gbt_embedding_params *params, const void *dout, void *grad,

@@ -908,7 +908,7 @@ class Context:
         """Rows of table [rows][width] by ids of any shape, times scale: [*ids.shape][width] of `dtype` (None: the table's).  An id
         outside the table gives zeros, a padding id of -1 for instance.
 
-        out           [ids][width], rows any distance apart: written to, and returned
+        out           [ids][width], rows any distance apart, apart from table and ids: written to, and returned
         No graph of derivatives is recorded: embedding_backward is the table's gradient.
         """
         stride = _rows_of(table, "table", self.device)
@@ -935,9 +935,10 @@ class Context:
 
     def embedding_backward(self, dout, ids, rows=None, *, scale=1.0, dtype=torch.float32, out=None, accumulate=False):
         """The gradient [rows][width] of embedding's table, of `dtype`, from that of its result [*ids.shape][width]: for each row the sum over
-        the places that hold its id, in 32 bits and a fixed order, times scale; zeros for rows without one.
+        the places that hold its id, in 32 bits and a fixed order, times scale; zeros for rows without one.  The gradient's rows may be any
+        distance apart, or all the same; a row's elements lie side by side (one expanded along its last axis is refused: .contiguous()).
 
-        out           [rows][width], rows any distance apart: written to, and returned
+        out           [rows][width], rows any distance apart, apart from dout and ids: written to, and returned
         accumulate    add to what `out` holds
         """
         if not (isinstance(dout, torch.Tensor) and isinstance(ids, torch.Tensor) and dout.dim() >= 1 and dout.shape[:-1] in (ids.shape, (ids.numel(),))):
@@ -1090,7 +1091,7 @@ class Context:
 
     def orthogonalise(self, matrices: MatrixList, *, steps=5, coefficients=(3.4445, -4.7750, 2.0315)):
         """Every matrix of the list divided by its norm, then `steps` times X <- (a I + b A + c A^2) X with A = X X^T, times its scale, into its
-        out: all singular values end near one.  A matrix of zeros gives zeros, one that is not finite NaN.  Returns the outs."""
+        out: all singular values end near one.  The same coefficients in all steps, under which no singular value passes 4, nor its factor 64.  A matrix of zeros gives zeros, one that is not finite NaN.  Returns the outs."""
         a, b, c = coefficients
         with self._on_stream(matrices.all) or _NO_STREAM:
             ws = self._scratch("orthogonalise", matrices.workspace_bytes)

@@ -11,8 +11,8 @@
 // and low, 22 bits in all, and a product is three on the matrix units: high * high + high * low + low * high, added up in 32 bits.  Float16 has few exponents, so all
 // is held times powers of two that the coefficients give: X has singular values, and so elements, up to a bound that the host knows for each step, and the scale
 // takes that bound to 2^15.  Elements down to 2^-17 of it then have their 22 bits (X begins with some 1 / sqrt(p w), 2^-12.5 for 4096 x 8192), smaller
-// ones are off by 2^-40 of it: rows and columns of very different size keep theirs.  (512 x 2048, rows of 1 to 1e-4, ten steps, all held times 2^8: 3.6e-5 off, and
-// 32-bit products 4.6e-6.)
+// ones are off by 2^-40 of it: rows and columns of very different size keep theirs.  (512 x 2048, rows of 1 to 1e-4, ten steps: all held times 2^8 3.6e-5 off, as it is 2.4e-6,
+// and 32-bit products 7.5e-6; of rows of 1 to 1e-6 the smallest one 1.4e-2 and 1.2e-4 of its length, and 3e-5 to 2e-4.)
 //
 // All products have both operands' rows along the sum: X X^T, products of symmetric matrices, and F X = F (X^T)^T, for which X's transpose is kept beside it.
 // Of symmetric results the upper tiles are computed, and written twice.
